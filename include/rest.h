@@ -8,7 +8,11 @@
  *               rest_retrieve, rest_gather_rows, rest_draft_from_runs: the same in pieces, for a
  *               datastore spread over several GPUs
  * Verify side:  rest_tree_attention, rest_accept           (Sec. 3.2, draft verification / acceptance)
+ *               rest_paged_attention: the same attention over a cache cut into pages
+ *               rest_accept_sampled: acceptance against the verifier's probabilities
  * Between steps: rest_kv_commit                            (the accepted path joins the prefix)
+ *               rest_paged_kv_write, rest_paged_kv_commit, rest_pages_fork, rest_pages_copy,
+ *               rest_pages_reserve, rest_pages_release: the cache in pages
  * Health:       rest_device_error_flags
  * (measurement and planning aids live in rest_aids.h)
  *
@@ -51,7 +55,11 @@ enum {
   REST_CTX_BAD_TOKEN = 1,       /* one of the last n_max context tokens is outside [0, vocab) */
   REST_CTX_BAD_DATASTORE = 2,   /* suffix-array entry out of range, or gathered continuations
                                    not in lexicographic order                                 */
-  REST_CTX_INTERNAL = 3
+  REST_CTX_INTERNAL = 3,
+  /* written by rest_pages_fork and rest_pages_reserve */
+  REST_CTX_NO_PAGES = 4,        /* the pool has too few free pages: nothing was done            */
+  REST_CTX_BAD_PAGES = 5        /* index out of range, child in use or named twice, length that
+                                   the table cannot hold: nothing was done                      */
 };
 
 enum { REST_SAMPLE_STRIDED = 0, REST_SAMPLE_FIRST_K = 1 };
@@ -73,7 +81,10 @@ enum {
   REST_MAX_M = 16,        /* continuation length */
   REST_MAX_N = 256,       /* draft tokens per tree */
   REST_MAX_K = 32768,     /* candidates per context */
-  REST_HEAD_DIM = 128
+  REST_HEAD_DIM = 128,
+  REST_MAX_PAGES = 1 << 20,           /* pages of a pool handed out by rest_pages_fork / _reserve */
+  REST_MAX_FORKS = 1024,              /* forks per rest_pages_fork call */
+  REST_MAX_PAGED_CONTEXTS = 8192      /* contexts per rest_pages_reserve call */
 };
 
 typedef struct rest_datastore rest_datastore;   /* opaque host object holding device pointers */
@@ -342,6 +353,70 @@ rest_status rest_kv_commit(void* d_k, void* d_v, const int64_t* kv_strides, cons
                            const int32_t* d_accept_nodes, const int32_t* d_accept_len, int32_t B,
                            int32_t H_kv, int32_t N, int32_t D, int32_t max_depth,
                            int32_t* d_new_kv_len, void* stream);
+
+/*
+ * A KV cache in pages.  The paper does not describe the cache; a server that keeps many contexts
+ * of unforeseen lengths cuts it into pages.  Row l of context b is row l % page of page
+ * d_table[b * table_stride + l / page]; an entry outside [0, P) means that there is none.
+ *
+ *   d_k_pages, d_v_pages  16-bit elements, element (p,hk,r,d) at p*page_strides[0] +
+ *                   hk*page_strides[1] + r*page_strides[2] + d; strides are host values, multiples
+ *                   of 8 elements; base pointers 16-byte aligned; D = 64 or 128
+ *   P, page         pages in the pool, rows per page: 16, 32, 64, 128 or 256
+ *   d_table         int32, row b at d_table + b*table_stride, table_cols entries
+ *   d_refs          int32[P]: how many contexts hold each page.  A page is free iff its count is
+ *                   0; free pages are handed out lowest number first, to contexts in order
+ *   d_n_pages       int32[B]: table entries of each context in use
+ * Tables are shared by all layers of a model; the row and page copies are made per layer.
+ *
+ * rest_paged_kv_write   rows i < n_nodes[b] (i < N with d_n_nodes NULL) of d_k_new, d_v_new
+ *                   (element (b,i,hk,d) at b*new_strides[0] + i*new_strides[1] + hk*new_strides[2]
+ *                   + d) become rows kv_len[b] + i.  A row whose page does not exist is left out.
+ * rest_paged_kv_commit  rest_kv_commit over pages: row kv_len[b] + accept_nodes[b][i] is copied to
+ *                   row kv_len[b] + i, i < accept_len[b]; d_new_kv_len (may be NULL, may be
+ *                   d_kv_len) receives kv_len + accept_len.  max_depth <= 16.
+ * rest_pages_fork   child context children[f] becomes a copy of parents[f], f < F <= 1024: whole
+ *                   pages of the parent's kv_len rows are shared (their counts rise), a partly
+ *                   filled last page gets a page of its own, named in d_copy_src[f] / d_copy_dst[f]
+ *                   (-1: nothing to copy) for rest_pages_copy.  The child must hold no pages
+ *                   (n_pages = 0); n_pages, kv_len and its table row are written.  d_status[f]:
+ *                   REST_CTX_*.  A child named twice is forked for its first mention only.  All
+ *                   parents count as they were before the call.
+ * rest_pages_copy   page d_dst[i] of K and V becomes a copy of page d_src[i]; pairs with an index
+ *                   outside [0, P) are left out.  No page may be a target twice, or a target and
+ *                   a source.
+ * rest_pages_reserve  context b gets pages until its table holds need_len[b] rows, all of them or
+ *                   none (d_status[b]).
+ * rest_pages_release  context b keeps the pages of its first keep_len[b] rows; with window > 0 also
+ *                   the pages whose rows all lie behind the window of every later token (rows
+ *                   >= sinks and <= keep_len - window) go.  Their table entries become -1.
+ *                   keep_len[b] < 0: the context stays as it is.
+ */
+rest_status rest_paged_kv_write(void* d_k_pages, void* d_v_pages, const int64_t* page_strides, int32_t P,
+                                int32_t page, const int32_t* d_table, int64_t table_stride,
+                                int32_t table_cols, const int32_t* d_kv_len, const void* d_k_new,
+                                const void* d_v_new, const int64_t* new_strides,
+                                const int32_t* d_n_nodes, int32_t B, int32_t H_kv, int32_t N, int32_t D,
+                                void* stream);
+rest_status rest_paged_kv_commit(void* d_k_pages, void* d_v_pages, const int64_t* page_strides, int32_t P,
+                                 int32_t page, const int32_t* d_table, int64_t table_stride,
+                                 int32_t table_cols, const int32_t* d_kv_len,
+                                 const int32_t* d_accept_nodes, const int32_t* d_accept_len, int32_t B,
+                                 int32_t H_kv, int32_t N, int32_t D, int32_t max_depth,
+                                 int32_t* d_new_kv_len, void* stream);
+rest_status rest_pages_fork(int32_t* d_refs, int32_t P, int32_t* d_table, int64_t table_stride,
+                            int32_t table_cols, int32_t* d_n_pages, int32_t* d_kv_len, int32_t B,
+                            int32_t page, const int32_t* d_parents, const int32_t* d_children, int32_t F,
+                            int32_t* d_copy_src, int32_t* d_copy_dst, int32_t* d_status, void* stream);
+rest_status rest_pages_copy(void* d_k_pages, void* d_v_pages, const int64_t* page_strides, int32_t P,
+                            int32_t page, int32_t H_kv, int32_t D, const int32_t* d_src,
+                            const int32_t* d_dst, int32_t n, void* stream);
+rest_status rest_pages_reserve(int32_t* d_refs, int32_t P, int32_t* d_table, int64_t table_stride,
+                               int32_t table_cols, int32_t* d_n_pages, const int32_t* d_need_len,
+                               int32_t B, int32_t page, int32_t* d_status, void* stream);
+rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int64_t table_stride,
+                               int32_t table_cols, int32_t* d_n_pages, const int32_t* d_keep_len,
+                               int32_t B, int32_t page, int32_t window, int32_t sinks, void* stream);
 
 /*
  * rest_suffix_array_build - the datastore's suffix array, built on the device (Sec. 3.2

@@ -38,6 +38,8 @@ EXPORTS = (
     "rest_suffix_array_workspace_bytes", "rest_suffix_array_min_workspace_bytes",
     "rest_suffix_array_build", "rest_suffix_array_build_in_groups", "rest_suffix_array_build_full",
     "rest_suffix_array_append_workspace_bytes", "rest_suffix_array_append", "rest_tree_attention_plan",
+    "rest_paged_kv_write", "rest_paged_kv_commit", "rest_pages_fork", "rest_pages_copy",
+    "rest_pages_reserve", "rest_pages_release",
     "rest_accept", "rest_status_string", "rest_last_cuda_error", "rest_launch_count",
 )
 
@@ -105,6 +107,20 @@ def lib():
     L.rest_accept.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
     L.rest_kv_commit.restype = i32
     L.rest_kv_commit.argtypes = [vp, vp, ctypes.POINTER(i64), vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
+    pool = [vp, vp, ctypes.POINTER(i64), i32, i32]           # K, V, strides, pages, rows per page
+    table = [vp, i64, i32]                                   # block table, row stride, columns
+    L.rest_paged_kv_write.restype = i32
+    L.rest_paged_kv_write.argtypes = pool + table + [vp, vp, vp, ctypes.POINTER(i64), vp, i32, i32, i32, i32, vp]
+    L.rest_paged_kv_commit.restype = i32
+    L.rest_paged_kv_commit.argtypes = pool + table + [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
+    L.rest_pages_copy.restype = i32
+    L.rest_pages_copy.argtypes = pool + [i32, i32, vp, vp, i32, vp]
+    L.rest_pages_fork.restype = i32
+    L.rest_pages_fork.argtypes = [vp, i32] + table + [vp, vp, i32, i32, vp, vp, i32, vp, vp, vp, vp]
+    L.rest_pages_reserve.restype = i32
+    L.rest_pages_reserve.argtypes = [vp, i32] + table + [vp, vp, i32, i32, vp, vp]
+    L.rest_pages_release.restype = i32
+    L.rest_pages_release.argtypes = [vp, i32] + table + [vp, vp, i32, i32, i32, i32, vp]
     L.rest_suffix_array_workspace_bytes.restype = sz
     L.rest_suffix_array_workspace_bytes.argtypes = [u64]
     L.rest_suffix_array_min_workspace_bytes.restype = sz
@@ -449,6 +465,143 @@ def rest_kv_commit(k, v, kv_len, accept_nodes, accept_len, N, new_kv_len=None, s
                           _stream(stream))
     _check(rc, "rest_kv_commit")
     return new_kv_len
+
+
+# ------------------------------------------------------------------------------ cache in pages
+def _same_device(first, *others):
+    """All tensors of a call sit on one CUDA device; the call runs there whatever the current one is."""
+    import torch
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise RestError("all tensors of a call must be on the same CUDA device")
+    return torch.cuda.device(first.device)
+
+
+def _dev_vec(t, name, n=None, dtype=None):
+    """A contiguous CUDA vector (int32 unless told otherwise) of n elements."""
+    import torch
+    dtype = torch.int32 if dtype is None else dtype
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.dim() == 1 and (n is None or t.numel() == n)):
+        raise RestError(f"{name} must be a contiguous {str(dtype).split('.')[-1]} CUDA vector"
+                        + ("" if n is None else f" of {n} elements"))
+    return t
+
+
+def _pool(k_pages, v_pages):
+    """Pointers, strides, pages and rows per page of a pool [P, H_kv, page, D]."""
+    import torch
+    for t, nm in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        if not (t.is_cuda and t.dtype in (torch.bfloat16, torch.float16) and t.dim() == 4 and t.stride(-1) == 1):
+            raise RestError(f"{nm} must be a bf16 or fp16 CUDA tensor [P, H_kv, page, D] with a contiguous last "
+                            "dimension")
+    if k_pages.stride() != v_pages.stride() or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
+        raise RestError("k_pages and v_pages must have the same shape, strides and type")
+    strides = (ctypes.c_int64 * 3)(*k_pages.stride()[:3])
+    return [k_pages.data_ptr(), v_pages.data_ptr(), strides, k_pages.shape[0], k_pages.shape[2]]
+
+
+def _table(table, B=None):
+    import torch
+    if not (table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.stride(1) == 1
+            and (B is None or table.shape[0] == B)):
+        raise RestError("block_table must be an int32 CUDA tensor [B, columns] with contiguous rows")
+    # a single row may come with any stride; the library wants rows that do not overlap
+    stride = table.stride(0) if table.shape[0] > 1 else max(table.stride(0), table.shape[1])
+    return [table.data_ptr(), stride, table.shape[1]]
+
+
+def rest_paged_kv_write(k_pages, v_pages, block_table, kv_len, k_new, v_new, n_nodes=None, stream=None):
+    """Writes new K/V rows k_new, v_new [B,N,H_kv,D] as rows kv_len[b] + i of the contexts' pages
+    (k_pages, v_pages [P,H_kv,page,D] with any 16-byte strides); with n_nodes int32[B] only rows
+    i < n_nodes[b].  Rows whose page does not exist are left out."""
+    B, N, H_kv, D = k_new.shape
+    pool, table = _pool(k_pages, v_pages), _table(block_table, B)
+    for t, nm in ((k_new, "k_new"), (v_new, "v_new")):
+        if not (t.is_cuda and t.dtype == k_pages.dtype and t.stride(-1) == 1):
+            raise RestError(f"{nm} must be a CUDA tensor of the pages' type with a contiguous last dimension")
+    if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or (H_kv, D) != (k_pages.shape[1], k_pages.shape[3]):
+        raise RestError("k_new and v_new must be [B,N,H_kv,D] of the pages' heads, with the same strides")
+    _dev_vec(kv_len, "kv_len", B)
+    if n_nodes is not None:
+        _dev_vec(n_nodes, "n_nodes", B)
+    strides = (ctypes.c_int64 * 3)(*k_new.stride()[:3])
+    with _same_device(k_pages, v_pages, block_table, kv_len, k_new, v_new, n_nodes):
+        _check(lib().rest_paged_kv_write(*pool, *table, kv_len.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), strides,
+                                         _ptr(n_nodes), B, H_kv, N, D, _stream(stream)), "rest_paged_kv_write")
+
+
+def rest_paged_kv_commit(k_pages, v_pages, block_table, kv_len, accept_nodes, accept_len, N, new_kv_len=None,
+                         stream=None):
+    """rest_kv_commit over pages: row kv_len[b] + accept_nodes[b][i] moves to row kv_len[b] + i.
+    new_kv_len (optional int32[B], may be kv_len itself) receives kv_len + accept_len."""
+    _dev_i32(accept_nodes, "accept_nodes")
+    B, max_depth = accept_nodes.shape
+    pool, table = _pool(k_pages, v_pages), _table(block_table, B)
+    for t, nm in ((kv_len, "kv_len"), (accept_len, "accept_len")) + (((new_kv_len, "new_kv_len"),) if new_kv_len is not None else ()):
+        _dev_vec(t, nm, B)
+    with _same_device(k_pages, v_pages, block_table, kv_len, accept_nodes, accept_len, new_kv_len):
+        _check(lib().rest_paged_kv_commit(*pool, *table, kv_len.data_ptr(), accept_nodes.data_ptr(),
+                                          accept_len.data_ptr(), B, k_pages.shape[1], N, k_pages.shape[3], max_depth,
+                                          _ptr(new_kv_len), _stream(stream)), "rest_paged_kv_commit")
+    return new_kv_len
+
+
+def rest_pages_fork(refs, block_table, n_pages, kv_len, parents, children, page, copy_src=None, copy_dst=None,
+                    status=None, stream=None):
+    """Makes context children[f] a copy of parents[f]: whole pages are shared, a partly filled last
+    page is replaced by a page of the child's own.  Returns (copy_src, copy_dst, status) int32[F]:
+    the pages to copy with rest_pages_copy in every layer (-1: none), and REST_CTX_* codes."""
+    import torch
+    F, B = parents.numel(), block_table.shape[0]
+    table = _table(block_table)
+    for t, nm, n in ((refs, "refs", None), (n_pages, "n_pages", B), (kv_len, "kv_len", B), (parents, "parents", F),
+                     (children, "children", F)):
+        _dev_vec(t, nm, n)
+    out = [torch.empty(F, dtype=torch.int32, device=refs.device) if t is None else _dev_vec(t, nm, F)
+           for t, nm in ((copy_src, "copy_src"), (copy_dst, "copy_dst"), (status, "status"))]
+    with _same_device(refs, block_table, n_pages, kv_len, parents, children, *out):
+        _check(lib().rest_pages_fork(refs.data_ptr(), refs.numel(), *table, n_pages.data_ptr(), kv_len.data_ptr(), B,
+                                     page, parents.data_ptr(), children.data_ptr(), F, *(t.data_ptr() for t in out),
+                                     _stream(stream)), "rest_pages_fork")
+    return tuple(out)
+
+
+def rest_pages_copy(k_pages, v_pages, src, dst, stream=None):
+    """Page dst[i] of K and V becomes a copy of page src[i] (entries outside the pool: left out)."""
+    n = src.numel()
+    _dev_vec(src, "src"), _dev_vec(dst, "dst", n)
+    with _same_device(k_pages, v_pages, src, dst):
+        _check(lib().rest_pages_copy(*_pool(k_pages, v_pages), k_pages.shape[1], k_pages.shape[3], src.data_ptr(),
+                                     dst.data_ptr(), n, _stream(stream)), "rest_pages_copy")
+
+
+def rest_pages_reserve(refs, block_table, n_pages, need_len, page, status=None, stream=None):
+    """Gives every context pages until its table holds need_len[b] rows, all or none.  Returns
+    status int32[B] (REST_CTX_*)."""
+    import torch
+    B = block_table.shape[0]
+    table = _table(block_table)
+    for t, nm, n in ((refs, "refs", None), (n_pages, "n_pages", B), (need_len, "need_len", B)):
+        _dev_vec(t, nm, n)
+    status = torch.empty(B, dtype=torch.int32, device=refs.device) if status is None else _dev_vec(status, "status", B)
+    with _same_device(refs, block_table, n_pages, need_len, status):
+        _check(lib().rest_pages_reserve(refs.data_ptr(), refs.numel(), *table, n_pages.data_ptr(),
+                                        need_len.data_ptr(), B, page, status.data_ptr(), _stream(stream)),
+               "rest_pages_reserve")
+    return status
+
+
+def rest_pages_release(refs, block_table, n_pages, keep_len, page, window=0, sinks=0, stream=None):
+    """Gives back the pages beyond each context's first keep_len[b] rows and, with a window, those
+    no later token sees.  keep_len[b] < 0 leaves a context as it is."""
+    B = block_table.shape[0]
+    table = _table(block_table)
+    for t, nm, n in ((refs, "refs", None), (n_pages, "n_pages", B), (keep_len, "keep_len", B)):
+        _dev_vec(t, nm, n)
+    with _same_device(refs, block_table, n_pages, keep_len):
+        _check(lib().rest_pages_release(refs.data_ptr(), refs.numel(), *table, n_pages.data_ptr(),
+                                        keep_len.data_ptr(), B, page, window, sinks, _stream(stream)),
+               "rest_pages_release")
 
 
 def dependent_read_latency_ns(table_bytes: int = 1 << 30, steps: int = 4096, device=None, seed: int = 1) -> float:

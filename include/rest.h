@@ -75,6 +75,9 @@ enum { REST_SAMPLE_STRIDED = 0, REST_SAMPLE_FIRST_K = 1 };
 enum { REST_SEARCH_AUTO = 0, REST_SEARCH_SINGLE = 1, REST_SEARCH_BATCHED = 2 };
 enum { REST_DS_VALIDATE = 1u, REST_DS_INDEX = 2u };
 
+/* Element types of caches, queries and logits. */
+enum { REST_BF16 = 0, REST_FP16 = 1, REST_FP32 = 2 };
+
 /* Limits of this implementation. */
 enum {
   REST_MAX_SUFFIX = 16,   /* n_max */
@@ -84,7 +87,8 @@ enum {
   REST_HEAD_DIM = 128,
   REST_MAX_PAGES = 1 << 20,           /* pages of a pool handed out by rest_pages_fork / _reserve */
   REST_MAX_FORKS = 1024,              /* forks per rest_pages_fork call */
-  REST_MAX_PAGED_CONTEXTS = 8192      /* contexts per rest_pages_reserve call */
+  REST_MAX_PAGED_CONTEXTS = 8192,     /* contexts per rest_pages_reserve call */
+  REST_MAX_VOCAB_SAMPLED = 1 << 18    /* logits per row of rest_accept_sampled */
 };
 
 typedef struct rest_datastore rest_datastore;   /* opaque host object holding device pointers */
@@ -417,6 +421,78 @@ rest_status rest_pages_reserve(int32_t* d_refs, int32_t P, int32_t* d_table, int
 rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int64_t table_stride,
                                int32_t table_cols, int32_t* d_n_pages, const int32_t* d_keep_len,
                                int32_t B, int32_t page, int32_t window, int32_t sinks, void* stream);
+
+/*
+ * rest_paged_attention - attention of N new positions of each context over its KV cache in pages
+ * (the layout described above) and over one another.  The paper's tree attention (Sec. 3.2 "Draft
+ * verification"), for a cache in pages, other head sizes and types, and models with a sliding
+ * window; with N = 1 an ordinary decoding step.
+ *
+ *   For context b, node i, head h (KV head h / (H / H_kv)), L = kv_len[b], n = n_nodes[b]:
+ *   keys: prefix rows l < L, and rows L + j of the nodes j < n that bit j of mask row i names.
+ *   Node i stands at position L + depth - 1, depth = bits set in its mask row (itself and its
+ *   ancestors).  window > 0: of these, a key at position p is seen by a node at position x only if
+ *   p < sinks or p > x - window (prefix row l stands at position l).
+ *   out = softmax(scale * q.k) v in fp32, rounded once; a node that sees nothing gets 0 and an lse
+ *   of -infinity.  Keys that a node does not see never touch its result, whatever they hold
+ *   (infinities and NaN included).
+ *
+ *   d_q, d_out      element (b,i,h,d) at b*strides[0] + i*strides[1] + h*strides[2] + d (d_out: 6..8)
+ *   d_k_pages, d_v_pages  page p, KV head, row, d: strides[3..5]; strides are multiples of 8
+ *                   elements, base pointers 16-byte aligned; dtype REST_BF16 or REST_FP16 for all four
+ *   d_table         a page index outside [0, P) reads as rows of zeros: rows in sight need pages
+ *   d_n_nodes       optional int32[B]: nodes n_nodes[b] .. N-1 do not exist; their rows of d_out and
+ *                   d_lse stay as they were
+ *   d_mask          uint32[B,N,ceil(N/32)] as written by rest_draft, or NULL: node i sees nodes 0..i
+ *                   and stands at position L + i (a run of tokens)
+ *   d_lse           optional float[B,H,N]: log of the softmax denominator (natural log)
+ *   d_ws            scratch of rest_paged_attention_workspace_bytes() bytes, 16-byte aligned (the
+ *                   query answers for the current device).  Calls that may run at the same time,
+ *                   captured graphs among them, need scratch of their own.
+ *   Limits: D = 64 or 128; 1 <= N <= 256; H % H_kv == 0.
+ */
+size_t rest_paged_attention_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t N, int32_t D);
+rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const void* d_v_pages,
+                                 const int64_t* strides, int32_t dtype, int32_t P, int32_t page,
+                                 const int32_t* d_table, int64_t table_stride, int32_t table_cols,
+                                 const int32_t* d_kv_len, const int32_t* d_n_nodes,
+                                 const uint32_t* d_mask, int32_t B, int32_t H, int32_t H_kv, int32_t N,
+                                 int32_t D, int32_t window, int32_t sinks, float scale, void* d_out,
+                                 float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * rest_accept_sampled - draft acceptance against the verifier's probabilities (Sec. 4.1 "Sampling
+ * strategies": temperature and nucleus sampling), from random numbers that the caller supplies.
+ * The tokens that come out are distributed exactly as plain sampling would distribute them.
+ *
+ *   Row s of context b (slot 0: after the prefix, slot i+1: after draft node i, as in
+ *   rest_accept) has weights w_v = exp((logit_v - largest) / temperature[b]), cut to the nucleus:
+ *   in the order (logit descending, token ascending) the shortest run whose weights sum to at least
+ *   top_p[b] of the whole.  Walk from the root.  At a node, r = sum of the weights; its children
+ *   are tried in index order: child c is accepted when uniforms[b][c+1] * r < w(token of c), else
+ *   its token leaves the row (w = 0) and r drops by its weight.  When no child is accepted (or
+ *   max_depth nodes are), the last token is drawn from what the row still holds: the first v with
+ *   w_0 + ... + w_v > uniforms[b][0] * r.  (Drafts from retrieval are given, not drawn, so the
+ *   proposal is certain and this is speculative sampling's rejection rule for it.)
+ *
+ *   d_logits        element (b,s,v) at b*ctx_stride + s*row_stride + v, dtype REST_BF16, REST_FP16
+ *                   or REST_FP32; NaN counts as -infinity (never drawn)
+ *   d_tokens, d_parents int32[B,N], d_n_nodes int32[B]: the tree, as written by rest_draft
+ *   d_uniforms      float[B,N+1], in [0, 1)
+ *   d_temperature, d_top_p  float[B]; temperature 0: the largest logit, lowest token first (then
+ *                   the call equals rest_accept on the rows' argmax); top_p >= 1: no cut
+ *   outputs         as rest_accept; a row without a finite logit gives -1 for the last token
+ *   Weights are held as integers of 2^-44 of the row's largest (exact sums in any order: results
+ *   never depend on scheduling); a token below 2^-45 of the largest counts as impossible.
+ *   Limits: V <= 2^18, max_depth <= 16, N <= 256.
+ */
+rest_status rest_accept_sampled(const void* d_logits, int32_t dtype, int64_t ctx_stride,
+                                int64_t row_stride, int32_t V, const int32_t* d_tokens,
+                                const int32_t* d_parents, const int32_t* d_n_nodes,
+                                const float* d_uniforms, const float* d_temperature,
+                                const float* d_top_p, int32_t B, int32_t N, int32_t max_depth,
+                                int32_t* d_accept_len, int32_t* d_accept_nodes, int32_t* d_out_tokens,
+                                void* stream);
 
 /*
  * rest_suffix_array_build - the datastore's suffix array, built on the device (Sec. 3.2

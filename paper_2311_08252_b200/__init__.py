@@ -25,6 +25,12 @@ REST_SAMPLE_FIRST_K = 1
 REST_SEARCH_AUTO = 0
 REST_SEARCH_SINGLE = 1
 REST_SEARCH_BATCHED = 2
+REST_BF16 = 0
+REST_FP16 = 1
+REST_FP32 = 2
+REST_CTX_OK = 0
+REST_CTX_NO_PAGES = 4
+REST_CTX_BAD_PAGES = 5
 REST_DS_VALIDATE = 1
 REST_DS_INDEX = 2
 
@@ -38,6 +44,7 @@ EXPORTS = (
     "rest_suffix_array_workspace_bytes", "rest_suffix_array_min_workspace_bytes",
     "rest_suffix_array_build", "rest_suffix_array_build_in_groups", "rest_suffix_array_build_full",
     "rest_suffix_array_append_workspace_bytes", "rest_suffix_array_append", "rest_tree_attention_plan",
+    "rest_paged_attention_workspace_bytes", "rest_paged_attention", "rest_accept_sampled",
     "rest_paged_kv_write", "rest_paged_kv_commit", "rest_pages_fork", "rest_pages_copy",
     "rest_pages_reserve", "rest_pages_release",
     "rest_accept", "rest_status_string", "rest_last_cuda_error", "rest_launch_count",
@@ -107,6 +114,13 @@ def lib():
     L.rest_accept.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
     L.rest_kv_commit.restype = i32
     L.rest_kv_commit.argtypes = [vp, vp, ctypes.POINTER(i64), vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
+    L.rest_paged_attention_workspace_bytes.restype = sz
+    L.rest_paged_attention_workspace_bytes.argtypes = [i32] * 5
+    L.rest_paged_attention.restype = i32
+    L.rest_paged_attention.argtypes = [vp, vp, vp, ctypes.POINTER(i64), i32, i32, i32, vp, i64, i32, vp, vp, vp, i32,
+                                       i32, i32, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, sz, vp]
+    L.rest_accept_sampled.restype = i32
+    L.rest_accept_sampled.argtypes = [vp, i32, i64, i64, i32] + [vp] * 6 + [i32, i32, i32] + [vp] * 4
     pool = [vp, vp, ctypes.POINTER(i64), i32, i32]           # K, V, strides, pages, rows per page
     table = [vp, i64, i32]                                   # block table, row stride, columns
     L.rest_paged_kv_write.restype = i32
@@ -508,6 +522,91 @@ def _table(table, B=None):
     # a single row may come with any stride; the library wants rows that do not overlap
     stride = table.stride(0) if table.shape[0] > 1 else max(table.stride(0), table.shape[1])
     return [table.data_ptr(), stride, table.shape[1]]
+
+
+def paged_attention_workspace_bytes(B, H, H_kv, N, D) -> int:
+    """Scratch bytes of rest_paged_attention on the current device."""
+    return int(lib().rest_paged_attention_workspace_bytes(B, H, H_kv, N, D))
+
+
+def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, window=0, sinks=0, n_nodes=None,
+                         out=None, lse=None, workspace=None, stream=None):
+    """Attention of q [B,N,H,D] (bf16 or fp16; D 64 or 128; N = 1: one ordinary token) over a cache
+    in pages k_pages, v_pages [P,H_kv,page,D], and over the new rows kv_len[b] + i themselves.
+    mask: words int32 [B,N,ceil(N/32)] as rest_draft writes them, None: node i sees nodes 0..i.
+    window > 0: a node sees the last `window` positions up to its own and the first `sinks` ones.
+    n_nodes int32[B]: later rows do not exist (their out / lse rows stay as they were).
+    lse: optional float32 [B,H,N].  Returns out [B,N,H,D]."""
+    import torch
+    L = lib()
+    B, N, H, D = q.shape
+    if not (q.is_cuda and q.dtype == k_pages.dtype and q.stride(-1) == 1):
+        raise RestError("q must be a CUDA tensor of the pages' type with a contiguous last dimension")
+    pool, table = _pool(k_pages, v_pages), _table(block_table, B)
+    if k_pages.shape[3] != D:
+        raise RestError("q and the pages differ in head size")
+    _dev_vec(kv_len, "kv_len", B)
+    if n_nodes is not None:
+        _dev_vec(n_nodes, "n_nodes", B)
+    if mask is not None and not (mask.is_cuda and mask.is_contiguous() and mask.element_size() == 4
+                                 and mask.shape == (B, N, (N + 31) // 32)):
+        raise RestError("mask must be a contiguous 32-bit CUDA tensor [B,N,ceil(N/32)]")
+    if lse is not None and not (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous()
+                                and lse.shape == (B, H, N)):
+        raise RestError("lse must be a contiguous float32 CUDA tensor [B,H,N]")
+    if out is None:
+        out = (torch.empty if n_nodes is None else torch.zeros)((B, N, H, D), dtype=q.dtype, device=q.device)
+    elif not (out.is_cuda and out.dtype == q.dtype and out.shape == q.shape and out.stride(-1) == 1):
+        raise RestError("out must be a CUDA tensor like q with a contiguous last dimension")
+    with _same_device(q, k_pages, v_pages, block_table, kv_len, mask, n_nodes, out, lse, workspace):
+        need = L.rest_paged_attention_workspace_bytes(B, H, k_pages.shape[1], N, D)
+        if need and workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        strides = (ctypes.c_int64 * 9)(*q.stride()[:3], *k_pages.stride()[:3], *out.stride()[:3])
+        rc = L.rest_paged_attention(
+            q.data_ptr(), *pool[:2], strides, REST_BF16 if q.dtype == torch.bfloat16 else REST_FP16, *pool[3:], *table,
+            kv_len.data_ptr(), _ptr(n_nodes), _ptr(mask), B, H, k_pages.shape[1], N, D, int(window), int(sinks),
+            float(scale), out.data_ptr(), _ptr(lse), _ptr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(rc, "rest_paged_attention")
+    return out
+
+
+def rest_accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature, top_p, max_depth, out=None,
+                        stream=None):
+    """Acceptance of draft trees against the verifier's probabilities: logits [B,N+1,V] (bf16, fp16
+    or fp32; slot 0 after the prefix, slot i+1 after node i), uniforms float32 [B,N+1] in [0, 1),
+    temperature and top_p float32 [B].  Returns (accept_len, accept_nodes, out_tokens) like
+    rest_accept."""
+    import torch
+    L = lib()
+    types = {torch.bfloat16: REST_BF16, torch.float16: REST_FP16, torch.float32: REST_FP32}
+    for t, nm in ((tokens, "tokens"), (parents, "parents")):
+        _dev_i32(t, nm)
+    B, N = tokens.shape
+    if not (logits.is_cuda and logits.dtype in types and logits.dim() == 3 and logits.shape[:2] == (B, N + 1)
+            and logits.stride(2) == 1):
+        raise RestError("logits must be a bf16, fp16 or fp32 CUDA tensor [B,N+1,V] with contiguous rows")
+    if parents.shape != (B, N):
+        raise RestError("parents must be [B,N] like tokens")
+    _dev_vec(n_nodes, "n_nodes", B)
+    if not (uniforms.is_cuda and uniforms.dtype == torch.float32 and uniforms.is_contiguous()
+            and uniforms.shape == (B, N + 1)):
+        raise RestError("uniforms must be a contiguous float32 CUDA tensor [B,N+1]")
+    _dev_vec(temperature, "temperature", B, torch.float32), _dev_vec(top_p, "top_p", B, torch.float32)
+    if out is None:
+        i32 = dict(dtype=torch.int32, device=tokens.device)
+        out = (torch.empty(B, **i32), torch.empty((B, max_depth), **i32), torch.empty((B, max_depth + 1), **i32))
+    for t, nm, shape in zip(out, ("accept_len", "accept_nodes", "out_tokens"), ((B,), (B, max_depth), (B, max_depth + 1))):
+        if _dev_i32(t, nm).shape != shape:
+            raise RestError(f"{nm} must be {list(shape)}")
+    with _same_device(logits, tokens, parents, n_nodes, uniforms, temperature, top_p, *out):
+        rc = L.rest_accept_sampled(logits.data_ptr(), types[logits.dtype], logits.stride(0), logits.stride(1),
+                                   logits.shape[2], tokens.data_ptr(), parents.data_ptr(), n_nodes.data_ptr(),
+                                   uniforms.data_ptr(), temperature.data_ptr(), top_p.data_ptr(), B, N, max_depth,
+                                   out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), _stream(stream))
+    _check(rc, "rest_accept_sampled")
+    return out
 
 
 def rest_paged_kv_write(k_pages, v_pages, block_table, kv_len, k_new, v_new, n_nodes=None, stream=None):

@@ -107,3 +107,111 @@ def release(refs, table, n_pages, keep_len, page, window=0, sinks=0):
             if 0 <= p < len(refs) and refs[p] > 0:
                 refs[p] -= 1
         n_pages[b] = min(int(n_pages[b]), kept)
+
+
+def attention(q, k, v, table, kv_len, mask, scale, window=0, sinks=0, n_nodes=None):
+    """softmax(scale q.k) v over the visible keys in 64 bits (torch tensors on the CPU, pages
+    [P,H_kv,page,D]).  Returns (out [B,N,H,D], lse [B,H,N], A, S): A = sum p |v| and S = the largest
+    scale * sum |q k| of each row, which error bounds are made of.  Rows past n_nodes are NaN."""
+    import torch
+    B, N, H, D = q.shape
+    P, H_kv, page, _ = k.shape
+    out = torch.full((B, N, H, D), float("nan"), dtype=torch.float64)
+    A, lse = out.clone(), torch.full((B, H, N), float("nan"), dtype=torch.float64)
+    S = torch.zeros((B, H, N), dtype=torch.float64)
+    for b in range(B):
+        L, n = int(kv_len[b]), N if n_nodes is None else int(n_nodes[b])
+        if n == 0:
+            continue
+        sees = torch.zeros((n, L + n), dtype=torch.bool)
+        sees[:, :L] = True
+        for i in range(n):
+            for j in range(n):
+                sees[i, L + j] = j <= i if mask is None else bool((int(mask[b, i, j >> 5]) >> (j & 31)) & 1)
+        depth = (np.arange(N) + 1 if mask is None else
+                 np.array([sum(bin(int(w) & 0xFFFFFFFF).count("1") for w in mask[b, i]) for i in range(N)]))
+        at = torch.tensor(list(range(L)) + [L + max(int(depth[j]), 1) - 1 for j in range(n)])
+        if window:
+            sees &= (at[None] < sinks) | (at[None] > at[L:, None] - window)
+        keys = [row_of(table, page, P, b, r) for r in range(L + n)]
+        K = torch.stack([k[p[0], :, p[1]].double() if p else torch.zeros((H_kv, D), dtype=torch.float64) for p in keys])
+        V = torch.stack([v[p[0], :, p[1]].double() if p else torch.zeros((H_kv, D), dtype=torch.float64) for p in keys])
+        for h in range(H):
+            kk, vv, qq = K[:, h // (H // H_kv)], V[:, h // (H // H_kv)], q[b, :n, h].double()
+            for i in range(n):
+                on = sees[i].nonzero()[:, 0]
+                if len(on) == 0:
+                    out[b, i, h], A[b, i, h], lse[b, h, i] = 0.0, 0.0, -float("inf")
+                    continue
+                x = scale * (kk[on] @ qq[i])
+                p = torch.softmax(x, 0)
+                out[b, i, h], A[b, i, h] = p @ vv[on], p @ vv[on].abs()
+                lse[b, h, i] = torch.logsumexp(x, 0)
+                S[b, h, i] = scale * (kk[on].abs() @ qq[i].abs()).max()
+    return out, lse, A, S
+
+
+def assert_attention(got, got_lse, ref, dtype, n_keys):
+    """Every element within what its roundings allow.  With e = half a step of the type (2^-8 bf16,
+    2^-11 fp16): the output's rounding e |out|; the probabilities' rounding e A, and for fp16 half of
+    its smallest step (2^-25 of the largest) for each key; scores in 32 bits, 128 products added in any
+    order, the scale and the exponential: 2^-16 (S + 1) relative for each probability and for their
+    sum, so 2 * 2^-16 (S + 1) A.  lse: 2^-16 (S + 1), and 2^-22 of its value for log and product."""
+    import torch
+    out, lse, A, S = ref
+    e = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -11
+    rel = (S + 1).transpose(1, 2)[..., None] * 2.0 ** -15
+    tol = e * out.abs() + (e + rel) * A * (1 + e) + (0 if dtype == torch.bfloat16 else n_keys * 2.0 ** -25 * 8) + 1e-30
+    got, live = got.double().cpu(), ~out.isnan()
+    over = ((got - out).abs() - tol)[live]
+    assert not got[live].isnan().any() and over.max() <= 0, float(over.max())
+    if got_lse is not None:
+        g, w = got_lse.double().cpu(), lse
+        seen = w.isfinite()
+        assert torch.equal(g[w.isinf()], w[w.isinf()])
+        if seen.any():
+            over = ((g - w).abs() - (S + 1) * 2.0 ** -16 - w.abs() * 2.0 ** -22)[seen]
+            assert over.max() <= 0, float(over.max())
+
+
+def accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature, top_p, max_depth):
+    """The acceptance walk in 64 bits (numpy; logits float64 [B,N+1,V])."""
+    B, N = tokens.shape
+    V = logits.shape[2]
+    lens, nodes, out = np.zeros(B, np.int32), np.full((B, max_depth), -1, np.int32), np.full((B, max_depth + 1), -1, np.int32)
+    for b in range(B):
+        cur, n = -1, 0
+        u = np.clip(np.nan_to_num(uniforms[b].astype(np.float64), nan=0.0), 0.0, np.float64(np.float32(0.99999994)))
+        while True:
+            x = logits[b, cur + 1].astype(np.float64).copy()
+            x[np.isnan(x)] = -np.inf
+            if not (x > -np.inf).any():
+                break                                              # nothing can be drawn: -1
+            order = np.lexsort((np.arange(V), -x))
+            w = np.zeros(V)
+            if temperature[b] > 0:
+                with np.errstate(invalid="ignore", over="ignore"):
+                    w = np.where(x == x.max(), 1.0, np.exp((x - x.max()) / np.float64(temperature[b])))
+                w[w < 2.0 ** -45] = 0.0
+                if top_p[b] < 1:
+                    before = np.cumsum(w[order]) - w[order]
+                    drop = before >= np.float64(top_p[b]) * w.sum()
+                    drop[0] = False
+                    w[order[drop]] = 0.0
+            else:
+                w[order[0]] = 1.0
+            child = -1
+            for c in range(min(max(int(n_nodes[b]), 0), N)):
+                if n < max_depth and parents[b, c] == cur and 0 <= tokens[b, c] < V and w[tokens[b, c]] > 0:
+                    if u[c + 1] * w.sum() < w[tokens[b, c]]:
+                        child = c
+                        break
+                    w[tokens[b, c]] = 0.0
+            if child < 0:
+                cdf = np.cumsum(w)
+                out[b, n] = int(np.argmax(cdf > u[0] * cdf[-1]))
+                break
+            nodes[b, n], out[b, n] = child, tokens[b, child]
+            n, cur = n + 1, child
+        lens[b] = n
+    return lens, nodes, out

@@ -82,3 +82,36 @@ def test_the_plain_model_shares_and_returns_pages():
     assert refs[:5].tolist() == [3, 3, 1, 1, 1] and kv_len.tolist() == [10] * 3
     plain.release(refs, table, n_pages, np.zeros(3, int), page)
     assert refs.sum() == 0 and (table == -1).all()
+
+
+def attend(st=None, dtype=0, P=4, page=16, ts=3, cols=3, H=8, H_kv=2, N=4, D=128, window=0, sinks=0, scale=1.0, q=256,
+           mask=256, B=1):
+    st = strides(4096, 1024, 128, 4096, 2048, 128, 4096, 1024, 128) if st is None else st
+    return rest.lib().rest_paged_attention(q, 256, 256, st, dtype, P, page, 256, ts, cols, 256, None, mask, B, H, H_kv,
+                                           N, D, window, sinks, scale, 256, None, None, 0, None)
+
+
+def test_attention_refuses():
+    assert attend(B=0) == OK
+    assert attend(D=96) == UNSUPPORTED and attend(N=257) == UNSUPPORTED and attend(H_kv=3) == UNSUPPORTED
+    assert attend(page=8) == UNSUPPORTED and attend(page=48) == UNSUPPORTED
+    assert attend(dtype=2) == INVALID and attend(dtype=-1) == INVALID
+    assert attend(scale=0.0) == INVALID and attend(scale=float("inf")) == INVALID and attend(scale=float("nan")) == INVALID
+    assert attend(window=-1) == INVALID and attend(sinks=-1) == INVALID and attend(P=0) == INVALID
+    assert attend(q=None) == INVALID and attend(q=264) == INVALID and attend(ts=2) == INVALID
+    assert attend(strides(4096, 1024, 128, 4096, 2048, 124, 4096, 1024, 128)) == INVALID
+    assert attend(strides(4096, 1024, 128, 4096, 2048, 64, 4096, 1024, 128)) == INVALID      # rows that overlap
+    assert rest.paged_attention_workspace_bytes(1, 8, 3, 4, 128) == 0
+    assert rest.paged_attention_workspace_bytes(1, 8, 2, 4, 96) == 0
+
+
+def sampled(dtype=0, V=100, B=1, N=4, depth=4, logits=256, ctx=500):
+    return rest.lib().rest_accept_sampled(logits, dtype, ctx, 100, V, 256, 256, 256, 256, 256, 256, B, N, depth, 256, 256,
+                                          256, None)
+
+
+def test_sampled_acceptance_refuses():
+    assert sampled(B=0) == OK
+    assert sampled(V=(1 << 18) + 1) == UNSUPPORTED and sampled(N=257) == UNSUPPORTED and sampled(depth=17) == UNSUPPORTED
+    assert sampled(dtype=3) == INVALID and sampled(V=0) == INVALID and sampled(depth=0) == INVALID
+    assert sampled(logits=None) == INVALID and sampled(ctx=-1) == INVALID and sampled(B=-1) == INVALID

@@ -17,9 +17,12 @@ cudaError_t ensure_dynamic_smem(const void* kernel, int kernel_slot, size_t byte
 // Streaming multiprocessors of the current device (asked once per device); 0 when there is no
 // usable device.
 int sm_count();
+// Reads and clears the error bits of the paged-attention kernels on the current device.
+rest_status take_paged_error_flags(uint32_t* h_flags);
 // One slot per kernel instance, library-wide: two kernels on one slot would skip each other's
-// attribute call.  The draft kernel's instances take kSmemSlotDraft + 0 ... 19.
-constexpr int kSmemSlotDraft = 0, kSmemSlotAttn = 20, kSmemSlotAttnWide = 21, kSmemSlots = 22;
+// attribute call.  The draft kernel's instances take kSmemSlotDraft + 0 ... 19, the paged
+// attention's kSmemSlotPaged + 0 ... 7.
+constexpr int kSmemSlotDraft = 0, kSmemSlotAttn = 20, kSmemSlotAttnWide = 21, kSmemSlotPaged = 22, kSmemSlots = 32;
 
 #define REST_CUDA_TRY(expr)                                              \
   do {                                                                   \

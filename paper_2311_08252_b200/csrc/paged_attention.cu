@@ -1,4 +1,38 @@
-// rest_paged_attention: attention of draft rows (or single tokens) over a KV cache in pages.
+// rest_paged_attention: attention of draft rows (or single tokens) over a KV cache in pages, with
+// an optional sliding window and first tokens that stay visible.
+//
+// The G = H / H_kv query heads of a KV head times the n nodes of a context give R = G n rows that
+// all read the same keys, so the rows (node-major, r = i G + g) are packed into 128-row tiles of
+// tcgen05.mma: S = Q K^T, then O += P V.
+//
+// Work.  The key tiles of all (context, KV head) units stand in one flat list, and every thread
+// block ("team" of RB blocks when R needs several row blocks) takes an equal, contiguous share of
+// it: uneven lengths, windows, one long context or hundreds of short ones all give the same even
+// load in a single wave, and the shares follow from the lengths on the device alone.  A unit that
+// a share's border cuts leaves partial rows (unnormalised O, maximum, sum) in the caller's
+// scratch, which a second small kernel joins.  With a window the tiles between the sinks and the
+// earliest visible position are not in the list at all.
+//
+// Two kernel shapes, picked by R (rows per KV head):
+//   R <= 128  one 128-row tile, 64-key steps, two blocks per SM: bound by the K/V stream, so what
+//             counts is bytes in flight (5 tiles of 16 KB a block) and a second block that fills the
+//             first one's gaps.  S is double-buffered in TMEM: the tensor core runs a step ahead.
+//   R > 128   two 128-row tiles that share each 128-key K/V tile (read once for 256 rows), one block
+//             per SM: bound by tensor core and exponentials, so one tile's softmax runs while the
+//             tensor core works for the other.
+// P is written back over S in TMEM and is the A operand of P V from there: no shared-memory round
+// trip for it (with 128-key steps the K, V and Q reads alone keep shared memory busy half the time).
+// O stays in TMEM and accumulates; its reference maximum is only raised when a tile exceeds it by
+// 2^8, and only then is the O row rescaled.
+//
+// K and V tiles arrive by TMA, one box per page (or per 64/128-key slice of a larger page) and
+// 64-element half of the head, in the 128-byte-swizzled operand layout; a page index that is out
+// of range reads as zeros.  Every wait is bounded (see rest_device_error_flags).
+//
+// Precision: scores, maxima, sums and O in 32 bits; P is rounded to the cache's type for the
+// tensor core (half a step, 2^-9 of each probability in bf16 - the output is rounded as much), the
+// sum takes the unrounded values, so lse carries none of it.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -7,86 +41,825 @@
 
 #include "common.cuh"
 #include "rest.h"
+#include "tensor_core.cuh"
 
 namespace {
 
+using namespace rest_tc;
+typedef unsigned long long u64;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kRescaleStep = 8.f;                     // log2 units
+
 struct Args {
-  const void *q, *k, *v;
+  const void* q;
   void* out;
   float* lse;
+  const void *k, *v;                                    // only read again for non-finite values
   const int32_t *table, *kv_len, *n_nodes;
   const uint32_t* mask;
+  int4* meta;                                           // per block: unit it starts and leaves unfinished
+  float *ws_o, *ws_ml;                                  // partial rows [block][2][rows][D], [..][2]
   int64_t q_b, q_n, q_h, p_p, p_h, p_r, o_b, o_n, o_h, table_stride;
-  int B, H, group, N, Wm, D, P, page_log, table_cols, window, sinks;
-  float scale;
+  int B, H, H_kv, G, N, Wm, P, page_log, table_cols, window, sinks, teams, RB, rows;
+  int slot[3];                                          // tensor-map coordinate (1..3) of row, head, page
+  float scale_log2;
 };
 
-template <typename T> __device__ __forceinline__ float to_f(T x) { return (float)x; }
+// One context's keys and its list of visible tiles: the first ns tiles hold the sinks, the others
+// run from tile w0 to the end.
+struct Ctx { int L, n, w0, ns; long long nt; };
+template <int BN>
+__device__ __forceinline__ Ctx context(const Args& a, int b) {
+  Ctx c;
+  const int cap = a.table_cols << a.page_log;           // a longer length has no pages behind it
+  c.L = min(max(a.kv_len[b], 0), cap);
+  c.n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.N) : a.N;
+  c.w0 = c.ns = 0;
+  const int first = c.L - a.window + 1;                 // earliest position in any node's window
+  if (a.window > 0 && first > 0) {
+    c.w0 = first / BN;
+    c.ns = min((min(a.sinks, c.L) + BN - 1) / BN, c.w0);
+  }
+  c.nt = c.n == 0 ? 0 : c.ns + (c.L + c.n + BN - 1) / BN - c.w0;
+  return c;
+}
+template <int BN>
+__device__ __forceinline__ int tile_key(const Ctx& c, int t) { return (t < c.ns ? t : t - c.ns + c.w0) * BN; }
 
-// depth of node i in its tree (its own position among its ancestors, 1-based) and "i sees node j"
+// A block's share of the flat tile list, piece by piece; every role of the block walks it alike.
+struct Piece { Ctx c; int b, hk, t0, len, rows; bool first, whole; };
+template <int BN, int ROWS>
+struct Walk {
+  const Args& a;
+  int b, rb;
+  long long off, left;
+  bool at_start = true;
+  __device__ Walk(const Args& a_, int b_, long long off_, long long left_, int rb_)
+      : a(a_), b(b_), rb(rb_), off(off_), left(left_) {}
+  __device__ __forceinline__ bool next(Piece& p) {
+    while (left > 0) {
+      p.c = context<BN>(a, b);
+      if (off >= a.H_kv * p.c.nt) { off -= a.H_kv * p.c.nt; ++b; continue; }
+      p.b = b;
+      p.hk = (int)(off / p.c.nt);
+      p.t0 = (int)(off - p.hk * p.c.nt);
+      p.len = (int)min(p.c.nt - (long long)p.t0, left);
+      p.first = at_start;
+      at_start = false;
+      p.whole = p.len == (int)p.c.nt;
+      off += p.len;
+      left -= p.len;
+      p.rows = a.G * p.c.n - rb * ROWS;
+      if (p.rows > 0) { p.rows = min(p.rows, ROWS); return true; }
+    }
+    return false;
+  }
+};
+
+template <typename T> struct Type;
+template <> struct Type<__nv_bfloat16> {
+  static constexpr uint32_t format = 1, exponent = 0x7F80u;
+  __device__ static uint32_t pack(float lo, float hi) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+  }
+  __device__ static float2 unpack(uint32_t x) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&x)); }
+};
+template <> struct Type<__half> {
+  static constexpr uint32_t format = 0, exponent = 0x7C00u;
+  __device__ static uint32_t pack(float lo, float hi) {
+    __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+  }
+  __device__ static float2 unpack(uint32_t x) { return __half22float2(*reinterpret_cast<__half2*>(&x)); }
+};
+
+// instruction descriptor: T x T -> fp32, M = 128, A K-major, B K-major (0) or MN-major (1)
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t idesc(int N, int b_mn_major) {
+  return (1u << 4) | (Type<T>::format << 7) | (Type<T>::format << 10) | ((uint32_t)b_mn_major << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
+}
+// A from TMEM
+__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc_,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}\n"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc_), "r"(accumulate), "r"(0u)
+      : "memory");
+}
+
+__device__ unsigned int g_paged_error;                  // bit 0: wait gave up, bit 1: smem misaligned
+
+template <int D, int NT> struct Shape {
+  static constexpr int BN = NT == 1 ? 64 : 128;         // keys per step
+  static constexpr int kHalves = D / 64;
+  static constexpr int kRows = 128 * NT;
+  static constexpr int kQTile = 128 * D * 2, kTile = BN * D * 2;
+  static constexpr int KS = D == 128 ? 2 : 4, VS = D == 128 ? 3 : 5;      // ring stages
+  static constexpr int kBars = NT * kQTile + (KS + VS) * kTile;           // barriers behind the tiles
+  static constexpr int kSmem = kBars + 512;
+  static constexpr int kSoftmax = 4 * NT;               // softmax warps; then K loader, V loader, MMA
+  static constexpr int kThreads = 32 * (kSoftmax + 3);
+  static constexpr uint32_t kTmem = NT == 1 ? 256 : 512;
+  static constexpr uint32_t kColO = 2 * BN;
+};
+// byte offsets behind kBars
+enum {
+  kKFull = 0, kKFree = 40, kVFull = 80, kVFree = 120, kSFull = 160, kPFull = 176, kOFull = 192, kQFull = 208,
+  kTmemSlot = 224, kAbort = 228, kBad = 232, kStartB = 240, kStartOff = 248, kStartLeft = 256, kScan = 264   // 11 x 8
+};
+
+// one 64-element x box-rows box of the pool -> shared memory
+__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int c0, int row, int head, int page,
+                                         const int (&slot)[3], uint32_t bar) {
+  const int c1 = slot[0] == 1 ? row : slot[1] == 1 ? head : page;
+  const int c2 = slot[0] == 2 ? row : slot[1] == 2 ? head : page;
+  const int c3 = slot[0] == 3 ? row : slot[1] == 3 ? head : page;
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+
+// bits [lo, hi) of a 64-bit word, clipped to it
+__device__ __forceinline__ u64 bits_between(int lo, int hi) {
+  lo = max(lo, 0);
+  hi = min(hi, 64);
+  if (hi <= lo) return 0ull;
+  return (hi == 64 ? ~0ull : (1ull << hi) - 1ull) & ~((1ull << lo) - 1ull);
+}
 __device__ __forceinline__ int node_depth(const Args& a, int b, int i) {
   if (!a.mask) return i + 1;
   const uint32_t* m = a.mask + ((int64_t)b * a.N + i) * a.Wm;
   int d = 0;
-  for (int w = 0; w < a.Wm; ++w) d += __popc(m[w]);
+  for (int w = 0; w < a.Wm; ++w) d += __popc(__ldg(m + w));
   return d;
 }
-
-// One block per (node, head, context), four warps that take the keys in turn.
-template <typename T>
-__global__ void __launch_bounds__(128) rest_paged_attention_simple_kernel(Args a) {
-  const int i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int nn = a.n_nodes ? min(max(a.n_nodes[b], 0), a.N) : a.N;
-  if (i >= nn) return;
-  const int L = max(a.kv_len[b], 0), per = a.D / 32;
-  const T* q = static_cast<const T*>(a.q) + b * a.q_b + i * a.q_n + h * a.q_h;
-  float qv[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-  for (int e = 0; e < per; ++e) qv[e] = to_f(q[lane * per + e]) * a.scale;
-  const int depth = node_depth(a, b, i), pos = L + max(depth, 1) - 1;
-  for (int key = warp; key < L + nn; key += 4) {
-    int at = key;
-    bool seen = true;
-    if (key >= L) {
-      const int j = key - L;
-      seen = a.mask ? (a.mask[((int64_t)b * a.N + i) * a.Wm + (j >> 5)] >> (j & 31)) & 1u : j <= i;
-      if (seen && a.window) at = L + node_depth(a, b, j) - 1;
+// which of the keys k0 .. k0 + 63 node i (of depth `depth`) of context b sees
+__device__ __forceinline__ u64 visible(const Args& a, const Ctx& c, int b, int i, int depth, int k0) {
+  const int pos = c.L + max(depth, 1) - 1;
+  u64 v;
+  if (a.window == 0)
+    v = bits_between(0, c.L - k0);
+  else
+    v = bits_between(0, min(a.sinks, c.L) - k0) | bits_between(max(pos - a.window + 1, 0) - k0, c.L - k0);
+  if (k0 + 64 > c.L) {
+    u64 m[4] = {0ull, 0ull, 0ull, 0ull};
+    if (a.mask) {
+      const uint32_t* mp = a.mask + ((int64_t)b * a.N + i) * a.Wm;
+#pragma unroll
+      for (int w = 0; w < 8; ++w)
+        if (w < a.Wm) m[w >> 1] |= (u64)__ldg(mp + w) << (32 * (w & 1));
+    } else {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) m[w] = bits_between(0, i + 1 - 64 * w);
     }
-    if (a.window) seen = seen && (at < a.sinks || at > pos - a.window);
-    const int col = key >> a.page_log;
-    if (!seen || col >= a.table_cols) continue;
-    const int p = a.table[b * a.table_stride + col];
-    const bool there = p >= 0 && p < a.P;
-    const int64_t off = p * a.p_p + (h / a.group) * a.p_h + (key & ((1 << a.page_log) - 1)) * a.p_r + lane * per;
-    float s = 0.f, kv[4];
-    for (int e = 0; e < per; ++e) s += there ? qv[e] * to_f(static_cast<const T*>(a.k)[off + e]) : 0.f;
-    for (int e = 0; e < per; ++e) kv[e] = there ? to_f(static_cast<const T*>(a.v)[off + e]) : 0.f;
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
-    const float mn = fmaxf(m, s), alpha = mn == -INFINITY ? 1.f : expf(m - mn), w = mn == -INFINITY ? 0.f : expf(s - mn);
-    l = l * alpha + w;
-    for (int e = 0; e < per; ++e) o[e] = o[e] * alpha + w * kv[e];
-    m = mn;
+    const int shift = k0 - c.L;
+    u64 t = mask_window(m, shift) & bits_between(-shift, c.n - shift);
+    if (a.window > 0 && a.window < a.N) {               // only then can a path be longer than the window
+      for (u64 rest_ = t; rest_; rest_ &= rest_ - 1) {
+        const int bit = __ffsll((long long)rest_) - 1;
+        const int at = c.L + node_depth(a, b, shift + bit) - 1;
+        if (!(at < a.sinks || at > pos - a.window)) t &= ~(1ull << bit);
+      }
+    }
+    v |= t;
   }
-  __shared__ float s_m[4], s_l[4], s_o[4][128];
-  if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
-  for (int e = 0; e < per; ++e) s_o[warp][lane * per + e] = o[e];
+  return v;
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(Shape<D, NT>::kThreads, NT == 1 ? 2 : 1)
+paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+  using S_ = Shape<D, NT>;
+  constexpr int BN = S_::BN, KS = S_::KS, VS = S_::VS, kHalves = S_::kHalves;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t sbase = smem_u32(smem);
+  const uint32_t sQ = sbase, sK = sQ + NT * S_::kQTile, sV = sK + KS * S_::kTile;
+  const uint32_t bars = sbase + S_::kBars;
+  unsigned char* ctl = smem + S_::kBars;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + kTmemSlot);
+  volatile uint32_t* abort_word = reinterpret_cast<volatile uint32_t*>(ctl + kAbort);
+  volatile int* s_bad = reinterpret_cast<volatile int*>(ctl + kBad);       // piece number + 1, by parity
+  const int team = blockIdx.x / a.RB, rb = blockIdx.x % a.RB;
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if ((sbase & 1023u) != 0) {   // the swizzled operand layout needs a 1024-byte aligned base
+    if (tid == 0) atomicOr(&g_paged_error, 2u);
+    return;                     // uniform over the grid: every block sees the same offset
+  }
+  if (tid == 0) {
+    for (int i = 0; i < KS; ++i) { mbar_init(bars + kKFull + 8 * i, 1); mbar_init(bars + kKFree + 8 * i, 1); }
+    for (int i = 0; i < VS; ++i) { mbar_init(bars + kVFull + 8 * i, 1); mbar_init(bars + kVFree + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bars + kSFull + 8 * i, 1);
+      mbar_init(bars + kPFull + 8 * i, 4);              // one arrival per softmax warp
+      mbar_init(bars + kOFull + 8 * i, 1);
+      mbar_init(bars + kQFull + 8 * i, 4);
+      s_bad[i] = 0;
+    }
+    *abort_word = 0u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                 "r"(S_::kTmem)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // everything above is independent of the inputs; from here on global memory is read
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  // ---- this team's share [x0, x1) of the flat tile list, and the context that x0 lies in
+  long long x0, x1;
+  int teams;
+  {
+    const int per = (a.B + S_::kThreads - 1) / S_::kThreads;
+    long long mine = 0;
+    for (int i = 0; i < per; ++i)
+      if (tid * per + i < a.B) mine += a.H_kv * context<BN>(a, tid * per + i).nt;
+    long long inc = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long y = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+      if (lane >= d) inc += y;
+    }
+    long long* s_scan = reinterpret_cast<long long*>(ctl + kScan);
+    if (lane == 31) s_scan[warp] = inc;
+    __syncthreads();
+    long long before = 0, total = 0;
+    for (int w = 0; w < S_::kThreads / 32; ++w) {
+      if (w == warp) before = total;
+      total += s_scan[w];
+    }
+    teams = total < a.teams ? (int)total : a.teams;     // fewer tiles than teams: one each, the rest idle
+    x0 = team < teams ? total * team / teams : total;
+    x1 = team < teams ? total * (team + 1) / teams : total;
+    long long at = before + inc - mine;
+    if (x0 < x1 && at <= x0 && x0 < at + mine) {        // one thread
+      int b = tid * per;
+      for (;; ++b) {
+        const long long n = a.H_kv * context<BN>(a, b).nt;
+        if (x0 < at + n) break;
+        at += n;
+      }
+      *reinterpret_cast<int*>(ctl + kStartB) = b;
+      *reinterpret_cast<long long*>(ctl + kStartOff) = x0 - at;
+    }
+    if (tid == 0) {
+      if (x0 >= x1) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);      // else the MMA warp writes it
+      *reinterpret_cast<long long*>(ctl + kScan + 88) = total;
+    }
+  }
+  tc_fence_before();
   __syncthreads();
-  const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  float sum = 0.f, x = 0.f;
-  for (int w = 0; w < 4; ++w) {
-    const float c = s_m[w] == -INFINITY ? 0.f : expf(s_m[w] - top);
-    sum += c * s_l[w];
-    if (threadIdx.x < a.D && c != 0.f) x += c * s_o[w][threadIdx.x];
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  Walk<BN, S_::kRows> walk(a, *reinterpret_cast<int*>(ctl + kStartB), *reinterpret_cast<long long*>(ctl + kStartOff),
+                           x1 - x0, rb);
+  if (x0 >= x1) walk.left = 0;
+  Piece p;
+
+  if (warp == S_::kSoftmax || warp == S_::kSoftmax + 1) {
+    // ------------------------------------------------------------------ K loader, V loader
+    const bool is_v = warp == S_::kSoftmax + 1;
+    const int stages = is_v ? VS : KS;
+    const uint32_t ring = is_v ? sV : sK, full = bars + (is_v ? kVFull : kKFull), free_ = bars + (is_v ? kVFree : kKFree);
+    const CUtensorMap* map = is_v ? &tm_v : &tm_k;
+    const int box = min(1 << a.page_log, BN);           // rows of one box
+    const int pg = lane / kHalves, half = lane % kHalves;
+    const bool active = pg * box < BN;
+    int slot = 0, filled = 0;
+    uint32_t parity = 1;                                // a fresh ring's slots count as free
+    bool ok = true;
+    while (ok && walk.next(p)) {
+      const int32_t* table = a.table + p.b * a.table_stride;
+      for (int it = 0; it < p.len; ++it) {
+        const int row = tile_key<BN>(p.c, p.t0 + it) + pg * box, col = row >> a.page_log;
+        int page = active && col < a.table_cols ? __ldg(table + col) : -1;
+        if (page < 0 || page >= a.P) page = a.P;        // outside the map: reads as zeros
+        if (filled >= stages)
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait_abortable(free_ + slot * 8, parity, abort_word)) != 0;
+        if (!ok) break;
+        if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)S_::kTile);
+        __syncwarp();
+        if (active)
+          tma_page(ring + slot * S_::kTile + half * (BN * 128) + pg * (box * 128), map, half * 64,
+                   row & ((1 << a.page_log) - 1), p.hk, page, a.slot, full + slot * 8);
+        ++filled;
+        if (++slot == stages) { slot = 0; parity ^= 1; }
+      }
+    }
+    if (*abort_word != 0u) {
+      // giving up: let the copies in flight land before this block goes away
+      for (int i = max(0, filled - stages); i < filled; ++i)
+        mbar_wait(full + (i % stages) * 8, (uint32_t)((i / stages) & 1));
+    }
+  } else if (warp == S_::kSoftmax + 2) {
+    // ------------------------------------------------------------------------- MMA issuer
+    if (lane == 0) {
+      constexpr uint32_t idesc_s = idesc<T>(BN, 0), idesc_o = idesc<T>(D, 1);
+      const uint64_t dq = umma_desc(sQ, 16, 1024), dk = umma_desc(sK, 16, 1024), dv = umma_desc(sV, BN * 128, 1024);
+      int kslot = 0, vslot = 0;
+      uint32_t kpar = 0, vpar = 0;
+      uint32_t n_s[2] = {0u, 0u}, n_q[2] = {0u, 0u};    // tiles whose P was taken, Q tiles taken
+      uint32_t issued = 0;                              // NT = 1: S tiles issued
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && mbar_wait_abortable(bar, parity, abort_word); return ok; };
+      auto qk = [&](int s, uint32_t buf) {
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint32_t qoff = (uint32_t)(s * S_::kQTile + (ks >> 2) * (128 * 128) + (ks & 3) * 32);
+          const uint32_t koff = (uint32_t)(kslot * S_::kTile + (ks >> 2) * (BN * 128) + (ks & 3) * 32);
+          umma_f16(tmem + buf * BN, dq + (qoff >> 4), dk + (koff >> 4), idesc_s, ks > 0);
+        }
+        umma_commit(bars + kSFull + buf * 8);
+      };
+      auto pv = [&](int s, uint32_t buf, bool fresh) {
+        tc_fence_after();
+#pragma unroll
+        for (int kk = 0; kk < BN / 16; ++kk)
+          umma_f16_ts(tmem + S_::kColO + s * 128, tmem + buf * BN + kk * 8, dv + ((vslot * S_::kTile + kk * 2048) >> 4),
+                      idesc_o, (fresh && kk == 0) ? 0u : 1u);
+        umma_commit(bars + kOFull + s * 8);
+      };
+      auto next_k = [&]() { umma_commit(bars + kKFree + kslot * 8); if (++kslot == KS) { kslot = 0; kpar ^= 1; } };
+      auto next_v = [&]() { umma_commit(bars + kVFree + vslot * 8); if (++vslot == VS) { vslot = 0; vpar ^= 1; } };
+      while (ok && walk.next(p)) {
+        if constexpr (NT == 1) {
+          if (!wait(bars + kQFull, n_q[0]++ & 1)) break;
+          auto next_s = [&]() {
+            if (!wait(bars + kKFull + kslot * 8, kpar)) return;
+            qk(0, issued++ & 1);
+            next_k();
+          };
+          next_s();
+          if (p.len > 1) next_s();
+          for (int it = 0; ok && it < p.len; ++it) {
+            const uint32_t buf = n_s[0] & 1;
+            if (!wait(bars + kPFull + buf * 8, (n_s[0] >> 1) & 1) || !wait(bars + kVFull + vslot * 8, vpar)) break;
+            ++n_s[0];
+            pv(0, buf, it == 0);
+            next_v();
+            // S(it + 2) goes over P(it): the tensor core works in order of issue, so P V is done with it
+            if (it + 2 < p.len) next_s();
+          }
+        } else {
+          const int act = p.rows > 128 ? 2 : 1;
+          if (!wait(bars + kKFull + kslot * 8, kpar)) break;
+          for (int s = 0; ok && s < act; ++s)
+            if (wait(bars + kQFull + s * 8, n_q[s]++ & 1)) qk(s, s);
+          if (!ok) break;
+          next_k();
+          for (int it = 0; ok && it < p.len; ++it) {
+            for (int s = 0; s < act; ++s) {
+              if (!wait(bars + kPFull + s * 8, n_s[s] & 1) || (s == 0 && !wait(bars + kVFull + vslot * 8, vpar))) break;
+              ++n_s[s];
+              pv(s, s, it == 0);
+              if (it + 1 < p.len) {
+                if (s == 0 && !wait(bars + kKFull + kslot * 8, kpar)) break;
+                qk(s, s);
+              }
+            }
+            if (!ok) break;
+            next_v();
+            if (it + 1 < p.len) next_k();
+          }
+        }
+      }
+    } else if (lane == 1 && x0 < x1) {
+      // The unit that this share starts but does not finish (if any) goes to the joining kernel:
+      // {pieces, context, KV head}.  Its later pieces are the first pieces of the blocks that follow.
+      Walk<BN, S_::kRows> w = walk;
+      int4 m = make_int4(0, 0, 0, 0);
+      // step over whole contexts to the last tile of the share
+      long long off = w.off, left = w.left;
+      int b = w.b;
+      for (;;) {
+        const long long n = a.H_kv * context<BN>(a, b).nt;
+        if (off + left <= n) break;
+        left -= n - off;
+        off = 0;
+        ++b;
+      }
+      const long long nt = context<BN>(a, b).nt, end = off + left;      // end > 0, inside context b
+      const long long u0 = (end - 1) / nt * nt, u1 = u0 + nt;           // its unit
+      const long long base = x1 - end;                                  // flat position of context b
+      if (u1 > end && base + u0 >= x0) {
+        const long long total = *reinterpret_cast<long long*>(ctl + kScan + 88);
+        int c = team + 1;
+        while (total * (c + 1) / teams < base + u1) ++c;
+        m = make_int4(c - team + 1, b, (int)(u0 / nt), 0);
+      }
+      a.meta[blockIdx.x] = m;
+    }
+  } else {
+    // ----------------------------------------------------------------------- softmax warps
+    const int s = warp >> 2, t = tid & 127;             // which 128-row tile, row inside it
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t o_col = tmem + lanes + S_::kColO + s * 128;
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {   // warp-uniform, so TMEM accesses stay converged
+      return __all_sync(0xFFFFFFFFu, mbar_wait_abortable(bar, parity, abort_word) ? 1 : 0) != 0;
+    };
+    uint32_t n = 0, vslot = 0, vpar = 0;
+    int piece = 0;
+    bool ok = true;
+    while (ok && walk.next(p)) {
+      ++piece;
+      if (s * 128 >= p.rows) continue;                  // (NT = 2: the second tile has no rows)
+      const int r0 = rb * S_::kRows + s * 128;          // first packed row of this tile
+      const int rows = min(128, p.rows - s * 128);
+      {  // Q rows -> shared memory, K-major 128-byte-swizzled; rows past the last one hold zeros
+        const T* q = static_cast<const T*>(a.q) + p.b * a.q_b + (int64_t)p.hk * a.G * a.q_h;
+        constexpr int kChunks = D / 8;                  // 16-byte chunks per row
+#pragma unroll
+        for (int j0 = 0; j0 < kChunks; j0 += 8) {
+          uint4 x[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int e = (j0 + j) * 128 + t, row = e / kChunks, chunk = e % kChunks;
+            x[j] = make_uint4(0u, 0u, 0u, 0u);
+            if (row < rows) {
+              const int i = (r0 + row) / a.G, g = (r0 + row) - i * a.G;
+              x[j] = *reinterpret_cast<const uint4*>(q + i * a.q_n + g * a.q_h + chunk * 8);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int e = (j0 + j) * 128 + t, row = e / kChunks, chunk = e % kChunks;
+            const uint32_t dst = sQ + s * S_::kQTile + (chunk >> 3) * (128 * 128) + (row >> 3) * 1024 + (row & 7) * 128 +
+                                 (((chunk & 7) ^ (row & 7)) << 4);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(x[j].x), "r"(x[j].y), "r"(x[j].z),
+                         "r"(x[j].w)
+                         : "memory");
+          }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + kQFull + s * 8);
+      }
+      const bool warp_live = (warp & 3) * 32 < rows, live = t < rows;
+      const int node = live ? (r0 + t) / a.G : 0, head = p.hk * a.G + (live ? (r0 + t) % a.G : 0);
+      const int depth = live ? node_depth(a, p.b, node) : 1;
+      float m_used = -INFINITY, l_run = 0.f;
+      for (int it = 0; it < p.len; ++it) {
+        const int key0 = tile_key<BN>(p.c, p.t0 + it);
+        const uint32_t buf = NT == 1 ? (n & 1) : (uint32_t)s, par = NT == 1 ? ((n >> 1) & 1) : (n & 1);
+        // every row of the block sees every key of the tile
+        const bool plain = key0 + BN <= p.c.L &&
+                           (a.window == 0 || key0 + BN <= a.sinks || key0 > p.c.L + p.c.n - 1 - a.window);
+        if (!plain && s == 0) {
+          // Values of V that are not finite would reach rows that do not see their key (0 x NaN): take
+          // them out of the tile, and remember the piece if the key exists (see the epilogue).
+          if (!wait(bars + kVFull + vslot * 8, vpar)) { ok = false; break; }
+          bool bad = false;
+#pragma unroll 4
+          for (int j = 0; j < S_::kTile / 16 / 128; ++j) {
+            const uint32_t at = (uint32_t)((j * 128 + t) * 16);
+            const uint32_t src = sV + vslot * S_::kTile + at;
+            uint32_t w[4];
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src) : "memory");
+            bool hit = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              constexpr uint32_t lo = Type<T>::exponent, hi = lo << 16;
+              if ((w[e] & lo) == lo) { w[e] &= 0xFFFF0000u; hit = true; }
+              if ((w[e] & hi) == hi) { w[e] &= 0x0000FFFFu; hit = true; }
+            }
+            if (hit) {
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(src), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+              bad = bad || key0 + (int)((at % (BN * 128)) >> 7) < p.c.L + p.c.n;
+            }
+          }
+          if (bad) s_bad[piece & 1] = piece + 1;
+          fence_async_smem();
+        }
+        if (!wait(bars + kSFull + buf * 8, par)) { ok = false; break; }
+        tc_fence_after();
+        if (warp_live) {
+          uint32_t x[BN / 32][32];
+#pragma unroll
+          for (int c = 0; c < BN / 32; ++c) tmem_ld_32x32(tmem + lanes + buf * BN + c * 32, x[c]);
+          tmem_wait_ld();
+          if (!plain) {
+#pragma unroll
+            for (int h = 0; h < BN / 64; ++h) {
+              const u64 vis = live ? visible(a, p.c, p.b, node, depth, key0 + 64 * h) : 0ull;
+              const uint32_t lo = (uint32_t)vis, hi = (uint32_t)(vis >> 32);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                if (!((lo >> j) & 1u)) x[2 * h][j] = 0xFF800000u;       // -inf
+                if (!((hi >> j) & 1u)) x[2 * h + 1][j] = 0xFF800000u;
+              }
+            }
+          }
+          // maximum of the raw scores (the scale is positive, so it commutes with max); the scale
+          // is applied inside the exponent's multiply-add
+          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < BN / 64; ++c)
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[2 * c][j]), __uint_as_float(x[2 * c + 1][j]));
+          const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
+          if (__any_sync(0xFFFFFFFFu, mx > m_used + kRescaleStep)) {
+            const float m_new = fmaxf(m_used, mx);
+            const float alpha = m_new == -INFINITY ? 1.f : ex2(m_used - m_new);   // m_used = -inf gives 0
+            if (it > 0) {
+              if (!wait(bars + kOFull + s * 8, (n - 1) & 1)) { ok = false; break; }
+              tc_fence_after();
+#pragma unroll
+              for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                tmem_ld_32x32(o_col + c * 32, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                tmem_st_32x32(o_col + c * 32, o);
+              }
+            }
+            l_run *= alpha;
+            m_used = m_new;
+          }
+          const float neg = m_used == -INFINITY ? 0.f : -m_used;
+          float ps[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int h = 0; h < BN / 64; ++h) {           // 64 keys: 32 packed columns of P
+            uint32_t pk[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const uint32_t(&xs)[32] = x[2 * h + (j >> 4)];
+              float e0, e1;
+              fma2(e0, e1, __uint_as_float(xs[2 * (j & 15)]), __uint_as_float(xs[2 * (j & 15) + 1]), a.scale_log2, neg);
+              e0 = ex2(e0);
+              e1 = ex2(e1);
+              add2(ps[(j & 1) * 2], ps[(j & 1) * 2 + 1], e0, e1);
+              pk[j] = Type<T>::pack(e0, e1);
+            }
+            tmem_st_32x32(tmem + lanes + buf * BN + h * 32, pk);
+          }
+          l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+          tmem_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + kPFull + buf * 8);
+        ++n;
+        if (++vslot == VS) { vslot = 0; vpar ^= 1; }
+      }
+      if (!ok || !wait(bars + kOFull + s * 8, (n - 1) & 1)) { ok = false; break; }
+      tc_fence_after();
+      // ---- epilogue: a finished unit's rows go to the output, others to the scratch
+      const bool bad = s_bad[piece & 1] == piece + 1;
+      // scratch slot 1: the unit's first piece; 0: a later one (then it is the block's first piece)
+      const int64_t wrow = ((int64_t)blockIdx.x * 2 + (p.t0 == 0 ? 1 : 0)) * a.rows + s * 128 + t;
+      const float inv = l_run != 0.f ? 1.f / l_run : 0.f;
+      if (warp_live) {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          __syncwarp();
+          tmem_ld_32x32(o_col + c * 32, o);
+          tmem_wait_ld();
+          if (!live) continue;
+          if (bad) {
+            // rare: add what was taken out of V, for the keys that this row does see
+            for (int it = 0; it < p.len; ++it) {
+              const int key0 = tile_key<BN>(p.c, p.t0 + it);
+              if (key0 + BN <= p.c.L && (a.window == 0 || key0 + BN <= a.sinks || key0 > p.c.L + p.c.n - 1 - a.window))
+                continue;
+              for (int h = 0; h < BN / 64; ++h) {
+                for (u64 vis = visible(a, p.c, p.b, node, depth, key0 + 64 * h); vis; vis &= vis - 1) {
+                  const int key = key0 + 64 * h + __ffsll((long long)vis) - 1, col = key >> a.page_log;
+                  const int page = col < a.table_cols ? a.table[p.b * a.table_stride + col] : -1;
+                  if (page < 0 || page >= a.P) continue;
+                  const T* v = static_cast<const T*>(a.v) + page * a.p_p + p.hk * a.p_h +
+                               (key & ((1 << a.page_log) - 1)) * a.p_r + c * 32;
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) {
+                    const float f = (float)v[j];
+                    if (!isfinite(f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + f);
+                  }
+                }
+              }
+            }
+          }
+          if (p.whole) {
+            T* op = static_cast<T*>(a.out) + p.b * a.o_b + node * a.o_n + head * a.o_h + c * 32;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t w[4];
+#pragma unroll
+              for (int f = 0; f < 4; ++f)
+                w[f] = Type<T>::pack(__uint_as_float(o[8 * e + 2 * f]) * inv, __uint_as_float(o[8 * e + 2 * f + 1]) * inv);
+              *reinterpret_cast<uint4*>(op + e * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          } else {
+            float4* wo = reinterpret_cast<float4*>(a.ws_o + wrow * D + c * 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              wo[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                  __uint_as_float(o[4 * e + 3]));
+          }
+        }
+        if (live) {
+          if (!p.whole)
+            *reinterpret_cast<float2*>(a.ws_ml + wrow * 2) = make_float2(m_used, l_run);
+          else if (a.lse)
+            a.lse[((int64_t)p.b * a.H + head) * a.N + node] = l_run != 0.f ? (m_used + log2f(l_run)) * kLn2 : -INFINITY;
+        }
+      }
+      tc_fence_before();                                // O is read: the next piece's P V may overwrite it
+    }
   }
-  if (threadIdx.x < a.D)
-    static_cast<T*>(a.out)[b * a.o_b + i * a.o_n + h * a.o_h + threadIdx.x] = (T)(sum == 0.f ? 0.f : x / sum);
-  if (threadIdx.x == 0 && a.lse) a.lse[((int64_t)b * a.H + h) * a.N + i] = sum == 0.f ? -INFINITY : top + logf(sum);
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_word != 0u && tid == 0) atomicOr(&g_paged_error, 1u);
+  if (warp == 0)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S_::kTmem) : "memory");
+}
+
+// Joins the pieces of the units that shares' borders cut.  Block x = (share that holds the unit's
+// first piece, row block), block y takes every gridDim.y-th row.  Eight warps: a row each, or - for
+// units cut into more than eight pieces - eight ranges of one row's pieces, added in a fixed order.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) paged_attention_join_kernel(Args a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  __shared__ float s_m[8], s_l[8], s_o[8][D];
+  const int4 meta = a.meta[blockIdx.x];
+  const int np = meta.x, b = meta.y, hk = meta.z;
+  if (np == 0) return;
+  const int rb = blockIdx.x % a.RB, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.N) : a.N;
+  const int r0 = rb * a.rows, rows = min(a.G * n - r0, a.rows);
+  constexpr int E = D / 32;
+  const bool wide = np > 8;
+  const int lo = wide ? np * warp / 8 : 0, hi = wide ? np * (warp + 1) / 8 : np;
+  for (int row0 = wide ? blockIdx.y : blockIdx.y * 8; row0 < rows; row0 += gridDim.y * (wide ? 1 : 8)) {
+    const int row = wide ? row0 : row0 + warp;
+    float m = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    if (row < rows) {
+      auto at = [&](int i) -> int64_t {                 // piece i: slot 1 of the first block, slot 0 of the others
+        return (((int64_t)blockIdx.x + (int64_t)i * a.RB) * 2 + (i == 0 ? 1 : 0)) * a.rows + row;
+      };
+      float2 ml[2];
+      for (int i = lo + lane; i < hi; i += 32) m = fmaxf(m, a.ws_ml[at(i) * 2]);
+#pragma unroll
+      for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+#pragma unroll 4
+      for (int i = lo; i < hi; ++i) {
+        const int64_t x = at(i);
+        ml[0] = *reinterpret_cast<const float2*>(a.ws_ml + x * 2);
+        const float w = ml[0].x == -INFINITY ? 0.f : ex2(ml[0].x - m);
+        l += ml[0].y * w;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float v = a.ws_o[x * D + lane * E + e];
+          if (w != 0.f) o[e] += v * w;
+        }
+      }
+    }
+    if (wide) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
+      if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
+      __syncthreads();
+      if (warp != 0) continue;
+      m = -INFINITY;
+      l = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) m = fmaxf(m, s_m[w]);
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        const float c = s_m[w] == -INFINITY ? 0.f : ex2(s_m[w] - m);
+        l += s_l[w] * c;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (c != 0.f) o[e] += s_o[w][lane * E + e] * c;
+      }
+    }
+    if (row >= rows) continue;
+    const int node = (r0 + row) / a.G, head = hk * a.G + (r0 + row) % a.G;
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + b * a.o_b + node * a.o_n + head * a.o_h + lane * E);
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) op[e] = Type<T>::pack(o[2 * e] * inv, o[2 * e + 1] * inv);
+    if (a.lse && lane == 0)
+      a.lse[((int64_t)b * a.H + head) * a.N + node] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  }
+}
+
+// ------------------------------------------------------------------------------------- host
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() {
+  static EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult st;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &st) != cudaSuccess ||
+        st != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+
+// Map of a pool (d, rows of a page, heads, pages), outer dimensions in order of increasing stride.
+bool encode_pool(CUtensorMap* map, const void* base, int dtype, int D, int page, int H_kv, int P, const int64_t* strides,
+                 int box_rows, int (&slot)[3]) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const int64_t size[3] = {page, H_kv, P}, stride[3] = {strides[2], strides[1], strides[0]};
+  int order[3] = {0, 1, 2};
+  auto key = [&](int i) { return size[i] > 1 ? stride[i] : (int64_t)1 << 60; };   // extent 1: stride unused, last
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (key(order[j]) < key(order[i])) { const int t = order[i]; order[i] = order[j]; order[j] = t; }
+  cuuint64_t dims[4] = {(cuuint64_t)D, 1, 1, 1}, bytes[3] = {0, 0, 0}, prev = (cuuint64_t)D * 2;
+  cuuint32_t box[4] = {64, 1, 1, 1};
+  const cuuint32_t step[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 3; ++i) {
+    const int which = order[i];
+    slot[which] = i + 1;
+    dims[i + 1] = (cuuint64_t)size[which];
+    cuuint64_t st = size[which] > 1 ? (cuuint64_t)stride[which] * 2 : prev;
+    if (st < prev) st = prev;
+    bytes[i] = prev = st;
+    if (which == 0) box[i + 1] = (cuuint32_t)box_rows;
+  }
+  return fn(map, dtype == REST_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+            const_cast<void*>(base), dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Plan { int NT, RB, teams, rows; };
+Plan plan(int H, int H_kv, int N) {
+  Plan p;
+  const int64_t R = (int64_t)(H / H_kv) * N;
+  p.NT = R > 128 ? 2 : 1;
+  p.RB = (int)((R + 128 * p.NT - 1) / (128 * p.NT));
+  const int sms = rest::sm_count(), blocks = (p.NT == 1 ? 2 : 1) * (sms > 0 ? sms : 148);
+  p.teams = blocks / p.RB > 0 ? blocks / p.RB : 1;
+  p.rows = R < 128 * p.NT ? (int)R : 128 * p.NT;
+  return p;
+}
+size_t workspace_bytes(const Plan& p, int D) {
+  const size_t blocks = (size_t)p.teams * p.RB;
+  return blocks * sizeof(int4) + blocks * 2 * p.rows * (D + 2) * sizeof(float);
+}
+
+template <typename T, int D, int NT>
+rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int smem_slot, cudaStream_t st) {
+  using S_ = Shape<D, NT>;
+  REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(paged_attention_kernel<T, D, NT>), smem_slot, S_::kSmem));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.teams * a.RB), 1, 1);
+  cfg.blockDim = dim3((unsigned)S_::kThreads, 1, 1);
+  cfg.dynamicSmemBytes = S_::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_attention_kernel<T, D, NT>, a, tm_k, tm_v));
+  rest::count_launch();
+  // about eight blocks of 256 threads per SM in all, never more than there are rows to share
+  const int per = 8 * 148 / (a.teams * a.RB);
+  cfg.gridDim = dim3((unsigned)(a.teams * a.RB), (unsigned)(per < 1 ? 1 : per > a.rows ? a.rows : per), 1);
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.dynamicSmemBytes = 0;
+  REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<T, D>, a));
+  rest::count_launch();
+  return REST_OK;
 }
 
 }  // namespace
 
+// error bits of this file's kernels, read and cleared (see rest_device_error_flags)
+rest_status rest::take_paged_error_flags(uint32_t* h_flags) {
+  unsigned int v = 0, zero = 0;
+  REST_CUDA_TRY(cudaMemcpyFromSymbol(&v, g_paged_error, sizeof(v)));
+  if (v != 0) REST_CUDA_TRY(cudaMemcpyToSymbol(g_paged_error, &zero, sizeof(zero)));
+  *h_flags = v;
+  return REST_OK;
+}
+
 extern "C" size_t rest_paged_attention_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t N, int32_t D) {
-  if (B <= 0 || H <= 0 || H_kv <= 0 || N <= 0 || (D != 64 && D != 128) || H % H_kv) return 0;
-  return 0;
+  if (B <= 0 || H <= 0 || H_kv <= 0 || N <= 0 || N > REST_MAX_N || (D != 64 && D != 128) || H % H_kv) return 0;
+  return workspace_bytes(plan(H, H_kv, N), D);
 }
 
 extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const void* d_v_pages,
@@ -103,7 +876,7 @@ extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pag
   if (table_cols < 1 || table_stride < table_cols) return REST_INVALID_ARG;
   if (!(scale > 0.f) || !(scale < INFINITY)) return REST_INVALID_ARG;
   if ((D != 64 && D != 128) || N > REST_MAX_N || (H % H_kv) != 0) return REST_UNSUPPORTED;
-  if (page < 16 || page > 256 || (page & (page - 1)) != 0 || (int64_t)table_cols * page > 0x7FFFFF00ll)
+  if (page < 16 || page > 256 || (page & (page - 1)) != 0 || (int64_t)table_cols * page > 0x7FFF0000ll || H > 65536)
     return REST_UNSUPPORTED;
   const int64_t extent[9] = {B, N, H, P, H_kv, page, B, N, H};
   for (int i = 0; i < 9; ++i) {
@@ -111,9 +884,11 @@ extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pag
     if (extent[i] > 1 && strides[i] < D) return REST_INVALID_ARG;
   }
   if ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_k_pages) |
-       reinterpret_cast<uintptr_t>(d_v_pages) | reinterpret_cast<uintptr_t>(d_out)) & 15)
+       reinterpret_cast<uintptr_t>(d_v_pages) | reinterpret_cast<uintptr_t>(d_out) | reinterpret_cast<uintptr_t>(d_ws)) & 15)
     return REST_INVALID_ARG;
-  (void)d_ws; (void)ws_bytes;
+  const Plan pl = plan(H, H_kv, N);
+  if (!d_ws) return REST_INVALID_ARG;
+  if (ws_bytes < workspace_bytes(pl, D)) return REST_WORKSPACE_TOO_SMALL;
   Args a;
   a.q = d_q; a.k = d_k_pages; a.v = d_v_pages; a.out = d_out; a.lse = d_lse;
   a.table = d_table; a.kv_len = d_kv_len; a.n_nodes = d_n_nodes; a.mask = d_mask;
@@ -121,16 +896,26 @@ extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pag
   a.p_p = strides[3]; a.p_h = strides[4]; a.p_r = strides[5];
   a.o_b = strides[6]; a.o_n = strides[7]; a.o_h = strides[8];
   a.table_stride = table_stride;
-  a.B = B; a.H = H; a.group = H / H_kv; a.N = N; a.Wm = (N + 31) / 32; a.D = D; a.P = P; a.table_cols = table_cols;
-  a.window = window; a.sinks = sinks; a.scale = scale;
+  a.B = B; a.H = H; a.H_kv = H_kv; a.G = H / H_kv; a.N = N; a.Wm = (N + 31) / 32; a.P = P; a.table_cols = table_cols;
+  a.window = window; a.sinks = sinks; a.teams = pl.teams; a.RB = pl.RB; a.rows = pl.rows;
+  a.scale_log2 = scale * kLog2e;
   a.page_log = 4;
   while ((1 << a.page_log) < page) ++a.page_log;
-  if (H > 65535 || B > 65535) return REST_UNSUPPORTED;
-  const dim3 grid((unsigned)N, (unsigned)H, (unsigned)B);
+  const size_t blocks = (size_t)pl.teams * pl.RB;
+  a.meta = static_cast<int4*>(d_ws);
+  a.ws_o = reinterpret_cast<float*>(static_cast<char*>(d_ws) + blocks * sizeof(int4));
+  a.ws_ml = a.ws_o + blocks * 2 * pl.rows * D;
+  const int bn = pl.NT == 1 ? 64 : 128;
+  CUtensorMap tm_k, tm_v;
+  if (!encode_pool(&tm_k, d_k_pages, dtype, D, page, H_kv, P, strides + 3, page < bn ? page : bn, a.slot) ||
+      !encode_pool(&tm_v, d_v_pages, dtype, D, page, H_kv, P, strides + 3, page < bn ? page : bn, a.slot))
+    return rest::note_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (dtype == REST_BF16) rest_paged_attention_simple_kernel<__nv_bfloat16><<<grid, 128, 0, st>>>(a);
-  else rest_paged_attention_simple_kernel<__half><<<grid, 128, 0, st>>>(a);
-  REST_CUDA_TRY(cudaGetLastError());
-  rest::count_launch();
-  return REST_OK;
+  const int smem_slot = rest::kSmemSlotPaged + (dtype == REST_FP16) * 4 + (D == 64) * 2 + (pl.NT == 1);
+  if (dtype == REST_BF16) {
+    if (D == 128) return pl.NT == 1 ? run<__nv_bfloat16, 128, 1>(a, tm_k, tm_v, smem_slot, st) : run<__nv_bfloat16, 128, 2>(a, tm_k, tm_v, smem_slot, st);
+    return pl.NT == 1 ? run<__nv_bfloat16, 64, 1>(a, tm_k, tm_v, smem_slot, st) : run<__nv_bfloat16, 64, 2>(a, tm_k, tm_v, smem_slot, st);
+  }
+  if (D == 128) return pl.NT == 1 ? run<__half, 128, 1>(a, tm_k, tm_v, smem_slot, st) : run<__half, 128, 2>(a, tm_k, tm_v, smem_slot, st);
+  return pl.NT == 1 ? run<__half, 64, 1>(a, tm_k, tm_v, smem_slot, st) : run<__half, 64, 2>(a, tm_k, tm_v, smem_slot, st);
 }

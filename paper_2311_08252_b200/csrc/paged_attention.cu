@@ -151,6 +151,28 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
       : "memory");
 }
 
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+// waits for TMEM loads; the values are named so that nothing that uses them can move ahead of the wait
+__device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+      : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+        "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+        "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]),
+        "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+        "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+        "+r"(r[30]), "+r"(r[31])
+      :
+      : "memory");
+}
+
 __device__ unsigned int g_paged_error;                  // bit 0: wait gave up, bit 1: smem misaligned
 
 template <int D, int NT> struct Shape {
@@ -169,7 +191,8 @@ template <int D, int NT> struct Shape {
 // byte offsets behind kBars
 enum {
   kKFull = 0, kKFree = 40, kVFull = 80, kVFree = 120, kSFull = 160, kPFull = 176, kOFull = 192, kQFull = 208,
-  kTmemSlot = 224, kAbort = 228, kBad = 232, kStartB = 240, kStartOff = 248, kStartLeft = 256, kScan = 264   // 11 x 8
+  kTmemSlot = 224, kAbort = 228, kBad = 232, kStartB = 240, kStartOff = 248, kStartLeft = 256, kScan = 264,  // 12 x 8
+  kTotal = 360
 };
 
 // one 64-element x box-rows box of the pool -> shared memory
@@ -313,7 +336,7 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
     }
     if (tid == 0) {
       if (x0 >= x1) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);      // else the MMA warp writes it
-      *reinterpret_cast<long long*>(ctl + kScan + 88) = total;
+      *reinterpret_cast<long long*>(ctl + kTotal) = total;
     }
   }
   tc_fence_before();
@@ -452,14 +475,14 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
       const long long u0 = (end - 1) / nt * nt, u1 = u0 + nt;           // its unit
       const long long base = x1 - end;                                  // flat position of context b
       if (u1 > end && base + u0 >= x0) {
-        const long long total = *reinterpret_cast<long long*>(ctl + kScan + 88);
+        const long long total = *reinterpret_cast<long long*>(ctl + kTotal);
         int c = team + 1;
         while (total * (c + 1) / teams < base + u1) ++c;
         m = make_int4(c - team + 1, b, (int)(u0 / nt), 0);
       }
       a.meta[blockIdx.x] = m;
     }
-  } else {
+  } else if (warp < S_::kSoftmax) {
     // ----------------------------------------------------------------------- softmax warps
     const int s = warp >> 2, t = tid & 127;             // which 128-row tile, row inside it
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -543,30 +566,32 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
         if (!wait(bars + kSFull + buf * 8, par)) { ok = false; break; }
         tc_fence_after();
         if (warp_live) {
-          uint32_t x[BN / 32][32];
-#pragma unroll
-          for (int c = 0; c < BN / 32; ++c) tmem_ld_32x32(tmem + lanes + buf * BN + c * 32, x[c]);
-          tmem_wait_ld();
-          if (!plain) {
-#pragma unroll
-            for (int h = 0; h < BN / 64; ++h) {
-              const u64 vis = live ? visible(a, p.c, p.b, node, depth, key0 + 64 * h) : 0ull;
-              const uint32_t lo = (uint32_t)vis, hi = (uint32_t)(vis >> 32);
-#pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                if (!((lo >> j) & 1u)) x[2 * h][j] = 0xFF800000u;       // -inf
-                if (!((hi >> j) & 1u)) x[2 * h + 1][j] = 0xFF800000u;
-              }
-            }
-          }
-          // maximum of the raw scores (the scale is positive, so it commutes with max); the scale
-          // is applied inside the exponent's multiply-add
+          // S is read twice, 32 columns at a time with the next 32 on their way: holding a row of
+          // 128 scores would take most of a thread's registers
+          const uint32_t s_col = tmem + lanes + buf * BN;
+          uint32_t x[2][32];
           float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          u64 vis = 0;
+          tmem_ld_32x32(s_col, x[0]);
 #pragma unroll
-          for (int c = 0; c < BN / 64; ++c)
+          for (int c = 0; c < BN / 32; ++c) {
+            tmem_wait_ld_of(x[c & 1]);
+            if (c + 1 < BN / 32) tmem_ld_32x32(s_col + (c + 1) * 32, x[(c + 1) & 1]);
+            if (!plain) {
+              if ((c & 1) == 0) vis = live ? visible(a, p.c, p.b, node, depth, key0 + 32 * c) : 0ull;
+              const uint32_t seen = (uint32_t)(vis >> (32 * (c & 1)));
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-              mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[2 * c][j]), __uint_as_float(x[2 * c + 1][j]));
+              for (int j = 0; j < 32; ++j)
+                if (!((seen >> j) & 1u)) x[c & 1][j] = 0xFF800000u;     // -inf
+              tmem_st_32x32(s_col + c * 32, x[c & 1]);
+            }
+            // maximum of the raw scores (the scale is positive, so it commutes with max); the scale
+            // is applied inside the exponent's multiply-add
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[c & 1][2 * j]), __uint_as_float(x[c & 1][2 * j + 1]));
+          }
+          if (!plain) tmem_wait_st();
           const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
           if (__any_sync(0xFFFFFFFFu, mx > m_used + kRescaleStep)) {
             const float m_new = fmaxf(m_used, mx);
@@ -578,7 +603,7 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
               for (int c = 0; c < D / 32; ++c) {
                 uint32_t o[32];
                 tmem_ld_32x32(o_col + c * 32, o);
-                tmem_wait_ld();
+                tmem_wait_ld_of(o);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
                 tmem_st_32x32(o_col + c * 32, o);
@@ -589,20 +614,22 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
           }
           const float neg = m_used == -INFINITY ? 0.f : -m_used;
           float ps[4] = {0.f, 0.f, 0.f, 0.f};
+          tmem_ld_32x32(s_col, x[0]);
 #pragma unroll
-          for (int h = 0; h < BN / 64; ++h) {           // 64 keys: 32 packed columns of P
-            uint32_t pk[32];
+          for (int c = 0; c < BN / 32; ++c) {           // 32 keys: 16 packed columns of P over S's first half
+            tmem_wait_ld_of(x[c & 1]);
+            if (c + 1 < BN / 32) tmem_ld_32x32(s_col + (c + 1) * 32, x[(c + 1) & 1]);
+            uint32_t pk[16];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const uint32_t(&xs)[32] = x[2 * h + (j >> 4)];
+            for (int j = 0; j < 16; ++j) {
               float e0, e1;
-              fma2(e0, e1, __uint_as_float(xs[2 * (j & 15)]), __uint_as_float(xs[2 * (j & 15) + 1]), a.scale_log2, neg);
+              fma2(e0, e1, __uint_as_float(x[c & 1][2 * j]), __uint_as_float(x[c & 1][2 * j + 1]), a.scale_log2, neg);
               e0 = ex2(e0);
               e1 = ex2(e1);
               add2(ps[(j & 1) * 2], ps[(j & 1) * 2 + 1], e0, e1);
               pk[j] = Type<T>::pack(e0, e1);
             }
-            tmem_st_32x32(tmem + lanes + buf * BN + h * 32, pk);
+            tmem_st_32x16(s_col + c * 16, pk);
           }
           l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
           tmem_wait_st();
@@ -626,7 +653,7 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
           uint32_t o[32];
           __syncwarp();
           tmem_ld_32x32(o_col + c * 32, o);
-          tmem_wait_ld();
+          tmem_wait_ld_of(o);
           if (!live) continue;
           if (bad) {
             // rare: add what was taken out of V, for the keys that this row does see

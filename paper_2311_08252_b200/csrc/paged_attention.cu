@@ -14,18 +14,19 @@
 // earliest visible position are not in the list at all.
 //
 // Two kernel shapes, picked by R (rows per KV head):
-//   R <= 128  one 128-row tile, 64-key steps, two blocks per SM: bound by the K/V stream, so what
-//             counts is bytes in flight (5 tiles of 16 KB a block) and a second block that fills the
-//             first one's gaps.  S is double-buffered in TMEM: the tensor core runs a step ahead.
-//   R > 128   two 128-row tiles that share each 128-key K/V tile (read once for 256 rows), one block
-//             per SM: bound by tensor core and exponentials, so one tile's softmax runs while the
-//             tensor core works for the other.
+//   R <= 128  one 128-row tile, two blocks per SM: bound by the K/V stream, so what counts is bytes
+//             in flight (5 tiles of 16 KB a block) and a second block that fills the first one's gaps.
+//   R > 128   two 128-row tiles that share each 64-key K/V tile (read once for 256 rows), one block
+//             per SM: bound by exponentials and the tensor core.
+// S has two buffers in TMEM for each row tile, so the tensor core runs a key tile ahead of the softmax
+// warps and neither waits for the other's round trip (one 128-key buffer per row tile instead, which
+// spends a fifth less tensor time, needed 5500 cycles per 128 keys and 256 rows).
 // P is written back over S in TMEM and is the A operand of P V from there: no shared-memory round
-// trip for it (with 128-key steps the K, V and Q reads alone keep shared memory busy half the time).
+// trip for it.
 // O stays in TMEM and accumulates; its reference maximum is only raised when a tile exceeds it by
 // 2^8, and only then is the O row rescaled.
 //
-// K and V tiles arrive by TMA, one box per page (or per 64/128-key slice of a larger page) and
+// K and V tiles arrive by TMA, one box per page (or per 64-key slice of a larger page) and
 // 64-element half of the head, in the 128-byte-swizzled operand layout; a page index that is out
 // of range reads as zeros.  Every wait is bounded (see rest_device_error_flags).
 //
@@ -141,6 +142,11 @@ __device__ __forceinline__ constexpr uint32_t idesc(int N, int b_mn_major) {
   return (1u << 4) | (Type<T>::format << 7) | (Type<T>::format << 10) | ((uint32_t)b_mn_major << 16) |
          ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
 }
+__device__ __forceinline__ uint32_t elect_one() {       // true in one lane of a converged warp
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}\n" : "=r"(p));
+  return p;
+}
 // A from TMEM
 __device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc_,
                                             uint32_t accumulate) {
@@ -176,23 +182,22 @@ __device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {
 __device__ unsigned int g_paged_error;                  // bit 0: wait gave up, bit 1: smem misaligned
 
 template <int D, int NT> struct Shape {
-  static constexpr int BN = NT == 1 ? 64 : 128;         // keys per step
+  static constexpr int BN = 64;                         // keys per step
   static constexpr int kHalves = D / 64;
   static constexpr int kRows = 128 * NT;
   static constexpr int kQTile = 128 * D * 2, kTile = BN * D * 2;
-  static constexpr int KS = D == 128 ? 2 : 4, VS = D == 128 ? 3 : 5;      // ring stages
+  static constexpr int KS = NT == 1 && D == 128 ? 2 : 4, VS = NT == 1 && D == 128 ? 3 : 6;      // ring stages
   static constexpr int kBars = NT * kQTile + (KS + VS) * kTile;           // barriers behind the tiles
   static constexpr int kSmem = kBars + 512;
   static constexpr int kSoftmax = 4 * NT;               // softmax warps; then K loader, V loader, MMA
   static constexpr int kThreads = 32 * (kSoftmax + 3);
   static constexpr uint32_t kTmem = NT == 1 ? 256 : 512;
-  static constexpr uint32_t kColO = 2 * BN;
+  static constexpr uint32_t kColO = 2 * NT * BN;        // behind two S buffers for each row tile
 };
 // byte offsets behind kBars
 enum {
-  kKFull = 0, kKFree = 40, kVFull = 80, kVFree = 120, kSFull = 160, kPFull = 176, kOFull = 192, kQFull = 208,
-  kTmemSlot = 224, kAbort = 228, kBad = 232, kStartB = 240, kStartOff = 248, kStartLeft = 256, kScan = 264,  // 12 x 8
-  kTotal = 360
+  kKFull = 0, kKFree = 32, kVFull = 64, kVFree = 112, kSFull = 160, kPFull = 192, kOFull = 224, kQFull = 240,
+  kTmemSlot = 256, kAbort = 260, kBad = 264, kStartB = 272, kStartOff = 280, kTotal = 288, kScan = 296   // 11 x 8
 };
 
 // one 64-element x box-rows box of the pool -> shared memory
@@ -222,8 +227,13 @@ __device__ __forceinline__ int node_depth(const Args& a, int b, int i) {
   for (int w = 0; w < a.Wm; ++w) d += __popc(__ldg(m + w));
   return d;
 }
+// every row of the block sees every key of the tile at key0
+template <int BN>
+__device__ __forceinline__ bool all_see(const Args& a, const Ctx& c, int key0) {
+  return key0 + BN <= c.L && (a.window == 0 || key0 + BN <= a.sinks || key0 > c.L + c.n - 1 - a.window);
+}
 // which of the keys k0 .. k0 + 63 node i (of depth `depth`) of context b sees
-__device__ __forceinline__ u64 visible(const Args& a, const Ctx& c, int b, int i, int depth, int k0) {
+__device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int depth, int k0) {
   const int pos = c.L + max(depth, 1) - 1;
   u64 v;
   if (a.window == 0)
@@ -255,13 +265,35 @@ __device__ __forceinline__ u64 visible(const Args& a, const Ctx& c, int b, int i
   return v;
 }
 
+// What was taken out of V (see below), added to columns d0 .. d0 + 31 of a row that does see its key.
+template <typename T, int BN>
+__device__ __noinline__ void add_back(const Args& a, Piece p, int node, int depth, int d0, uint32_t (&o)[32]) {
+  for (int it = 0; it < p.len; ++it) {
+    const int key0 = tile_key<BN>(p.c, p.t0 + it);
+    if (all_see<BN>(a, p.c, key0)) continue;
+    for (int h = 0; h < BN / 64; ++h) {
+      for (u64 vis = visible(a, p.c, p.b, node, depth, key0 + 64 * h); vis; vis &= vis - 1) {
+        const int key = key0 + 64 * h + __ffsll((long long)vis) - 1, col = key >> a.page_log;
+        const int page = col < a.table_cols ? a.table[p.b * a.table_stride + col] : -1;
+        if (page < 0 || page >= a.P) continue;
+        const T* v = static_cast<const T*>(a.v) + page * a.p_p + p.hk * a.p_h +
+                     (key & ((1 << a.page_log) - 1)) * a.p_r + d0;
+        for (int j = 0; j < 32; ++j) {
+          const float f = (float)v[j];
+          if (!isfinite(f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + f);
+        }
+      }
+    }
+  }
+}
+
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, NT == 1 ? 2 : 1)
-paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   using S_ = Shape<D, NT>;
   constexpr int BN = S_::BN, KS = S_::KS, VS = S_::VS, kHalves = S_::kHalves;
   extern __shared__ __align__(1024) unsigned char smem[];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   const uint32_t sbase = smem_u32(smem);
   const uint32_t sQ = sbase, sK = sQ + NT * S_::kQTile, sV = sK + KS * S_::kTile;
   const uint32_t bars = sbase + S_::kBars;
@@ -279,9 +311,11 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
   if (tid == 0) {
     for (int i = 0; i < KS; ++i) { mbar_init(bars + kKFull + 8 * i, 1); mbar_init(bars + kKFree + 8 * i, 1); }
     for (int i = 0; i < VS; ++i) { mbar_init(bars + kVFull + 8 * i, 1); mbar_init(bars + kVFree + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(bars + kSFull + 8 * i, 1);
       mbar_init(bars + kPFull + 8 * i, 4);              // one arrival per softmax warp
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(bars + kOFull + 8 * i, 1);
       mbar_init(bars + kQFull + 8 * i, 4);
       s_bad[i] = 0;
@@ -342,7 +376,7 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
   Walk<BN, S_::kRows> walk(a, *reinterpret_cast<int*>(ctl + kStartB), *reinterpret_cast<long long*>(ctl + kStartOff),
                            x1 - x0, rb);
   if (x0 >= x1) walk.left = 0;
@@ -362,9 +396,16 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
     bool ok = true;
     while (ok && walk.next(p)) {
       const int32_t* table = a.table + p.b * a.table_stride;
+      // the page of this lane's box, looked up a tile ahead
+      auto find = [&](int it, int& row) -> int {
+        row = tile_key<BN>(p.c, p.t0 + it) + pg * box;
+        const int col = row >> a.page_log;
+        return active && col < a.table_cols ? __ldg(table + col) : -1;
+      };
+      int row, page = find(0, row);
       for (int it = 0; it < p.len; ++it) {
-        const int row = tile_key<BN>(p.c, p.t0 + it) + pg * box, col = row >> a.page_log;
-        int page = active && col < a.table_cols ? __ldg(table + col) : -1;
+        int next_row = row;
+        const int next_page = it + 1 < p.len ? find(it + 1, next_row) : page;
         if (page < 0 || page >= a.P) page = a.P;        // outside the map: reads as zeros
         if (filled >= stages)
           ok = __all_sync(0xFFFFFFFFu, mbar_wait_abortable(free_ + slot * 8, parity, abort_word)) != 0;
@@ -374,6 +415,8 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
         if (active)
           tma_page(ring + slot * S_::kTile + half * (BN * 128) + pg * (box * 128), map, half * 64,
                    row & ((1 << a.page_log) - 1), p.hk, page, a.slot, full + slot * 8);
+        row = next_row;
+        page = next_page;
         ++filled;
         if (++slot == stages) { slot = 0; parity ^= 1; }
       }
@@ -383,87 +426,13 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
       for (int i = max(0, filled - stages); i < filled; ++i)
         mbar_wait(full + (i % stages) * 8, (uint32_t)((i / stages) & 1));
     }
-  } else if (warp == S_::kSoftmax + 2) {
-    // ------------------------------------------------------------------------- MMA issuer
-    if (lane == 0) {
-      constexpr uint32_t idesc_s = idesc<T>(BN, 0), idesc_o = idesc<T>(D, 1);
-      const uint64_t dq = umma_desc(sQ, 16, 1024), dk = umma_desc(sK, 16, 1024), dv = umma_desc(sV, BN * 128, 1024);
-      int kslot = 0, vslot = 0;
-      uint32_t kpar = 0, vpar = 0;
-      uint32_t n_s[2] = {0u, 0u}, n_q[2] = {0u, 0u};    // tiles whose P was taken, Q tiles taken
-      uint32_t issued = 0;                              // NT = 1: S tiles issued
-      bool ok = true;
-      auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && mbar_wait_abortable(bar, parity, abort_word); return ok; };
-      auto qk = [&](int s, uint32_t buf) {
-        tc_fence_after();
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          const uint32_t qoff = (uint32_t)(s * S_::kQTile + (ks >> 2) * (128 * 128) + (ks & 3) * 32);
-          const uint32_t koff = (uint32_t)(kslot * S_::kTile + (ks >> 2) * (BN * 128) + (ks & 3) * 32);
-          umma_f16(tmem + buf * BN, dq + (qoff >> 4), dk + (koff >> 4), idesc_s, ks > 0);
-        }
-        umma_commit(bars + kSFull + buf * 8);
-      };
-      auto pv = [&](int s, uint32_t buf, bool fresh) {
-        tc_fence_after();
-#pragma unroll
-        for (int kk = 0; kk < BN / 16; ++kk)
-          umma_f16_ts(tmem + S_::kColO + s * 128, tmem + buf * BN + kk * 8, dv + ((vslot * S_::kTile + kk * 2048) >> 4),
-                      idesc_o, (fresh && kk == 0) ? 0u : 1u);
-        umma_commit(bars + kOFull + s * 8);
-      };
-      auto next_k = [&]() { umma_commit(bars + kKFree + kslot * 8); if (++kslot == KS) { kslot = 0; kpar ^= 1; } };
-      auto next_v = [&]() { umma_commit(bars + kVFree + vslot * 8); if (++vslot == VS) { vslot = 0; vpar ^= 1; } };
-      while (ok && walk.next(p)) {
-        if constexpr (NT == 1) {
-          if (!wait(bars + kQFull, n_q[0]++ & 1)) break;
-          auto next_s = [&]() {
-            if (!wait(bars + kKFull + kslot * 8, kpar)) return;
-            qk(0, issued++ & 1);
-            next_k();
-          };
-          next_s();
-          if (p.len > 1) next_s();
-          for (int it = 0; ok && it < p.len; ++it) {
-            const uint32_t buf = n_s[0] & 1;
-            if (!wait(bars + kPFull + buf * 8, (n_s[0] >> 1) & 1) || !wait(bars + kVFull + vslot * 8, vpar)) break;
-            ++n_s[0];
-            pv(0, buf, it == 0);
-            next_v();
-            // S(it + 2) goes over P(it): the tensor core works in order of issue, so P V is done with it
-            if (it + 2 < p.len) next_s();
-          }
-        } else {
-          const int act = p.rows > 128 ? 2 : 1;
-          if (!wait(bars + kKFull + kslot * 8, kpar)) break;
-          for (int s = 0; ok && s < act; ++s)
-            if (wait(bars + kQFull + s * 8, n_q[s]++ & 1)) qk(s, s);
-          if (!ok) break;
-          next_k();
-          for (int it = 0; ok && it < p.len; ++it) {
-            for (int s = 0; s < act; ++s) {
-              if (!wait(bars + kPFull + s * 8, n_s[s] & 1) || (s == 0 && !wait(bars + kVFull + vslot * 8, vpar))) break;
-              ++n_s[s];
-              pv(s, s, it == 0);
-              if (it + 1 < p.len) {
-                if (s == 0 && !wait(bars + kKFull + kslot * 8, kpar)) break;
-                qk(s, s);
-              }
-            }
-            if (!ok) break;
-            next_v();
-            if (it + 1 < p.len) next_k();
-          }
-        }
-      }
-    } else if (lane == 1 && x0 < x1) {
+    if (is_v && lane == 0 && x0 < x1) {
       // The unit that this share starts but does not finish (if any) goes to the joining kernel:
       // {pieces, context, KV head}.  Its later pieces are the first pieces of the blocks that follow.
-      Walk<BN, S_::kRows> w = walk;
       int4 m = make_int4(0, 0, 0, 0);
       // step over whole contexts to the last tile of the share
-      long long off = w.off, left = w.left;
-      int b = w.b;
+      long long off = *reinterpret_cast<long long*>(ctl + kStartOff), left = x1 - x0;
+      int b = *reinterpret_cast<int*>(ctl + kStartB);
       for (;;) {
         const long long n = a.H_kv * context<BN>(a, b).nt;
         if (off + left <= n) break;
@@ -481,6 +450,76 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
         m = make_int4(c - team + 1, b, (int)(u0 / nt), 0);
       }
       a.meta[blockIdx.x] = m;
+    }
+  } else if (warp == S_::kSoftmax + 2) {
+    // ------------------------------------------------------------------------- MMA issuer
+    // The whole warp walks the loop, so that descriptors and addresses stay in uniform registers, and one
+    // elected lane issues (a loop in one lane moved them there before every instruction: about 100 cycles
+    // each, three times what the tensor core needs).
+    {
+      const uint32_t leader = elect_one();
+      constexpr uint32_t idesc_s = idesc<T>(BN, 0), idesc_o = idesc<T>(D, 1);
+      const uint64_t dq = umma_desc(sQ, 16, 1024), dk = umma_desc(sK, 16, 1024), dv = umma_desc(sV, BN * 128, 1024);
+      int kslot = 0, vslot = 0;
+      uint32_t kpar = 0, vpar = 0;
+      uint32_t n_p[2] = {0u, 0u}, n_q[2] = {0u, 0u}, n_s[2] = {0u, 0u};   // per row tile: P, Q taken, S issued
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_abortable(bar, parity, abort_word) ? 1 : 0) != 0;
+        return ok;
+      };
+      // S of the next key tile for the first `act` row tiles, from one on (the K tile is given back
+      // after the last one)
+      auto qk = [&](int s, int act) {
+        if (s == 0 && !wait(bars + kKFull + kslot * 8, kpar)) return;
+        tc_fence_after();
+        const uint32_t buf = 2 * s + (n_s[s]++ & 1);
+        if (leader) {
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const uint32_t qoff = (uint32_t)(s * S_::kQTile + (ks >> 2) * (128 * 128) + (ks & 3) * 32);
+            const uint32_t koff = (uint32_t)(kslot * S_::kTile + (ks >> 2) * (BN * 128) + (ks & 3) * 32);
+            umma_f16(tmem + buf * BN, dq + (qoff >> 4), dk + (koff >> 4), idesc_s, ks > 0);
+          }
+          umma_commit(bars + kSFull + buf * 8);
+          if (s + 1 == act) umma_commit(bars + kKFree + kslot * 8);
+        }
+        __syncwarp();
+        if (s + 1 == act && ++kslot == KS) { kslot = 0; kpar ^= 1; }
+      };
+      while (ok && walk.next(p)) {
+        const int act = NT == 2 && p.rows > 128 ? 2 : 1;
+#pragma unroll
+        for (int s = 0; s < NT; ++s)
+          if (s < act) wait(bars + kQFull + s * 8, n_q[s]++ & 1);
+        for (int it = 0; it < 2 && it < p.len; ++it)
+#pragma unroll
+          for (int s = 0; s < NT; ++s)
+            if (ok && s < act) qk(s, act);
+        for (int it = 0; ok && it < p.len; ++it) {
+#pragma unroll
+          for (int s = 0; s < NT; ++s) {
+            if (!ok || s >= act) break;
+            const uint32_t buf = 2 * s + (n_p[s] & 1);
+            if (!wait(bars + kPFull + buf * 8, (n_p[s] >> 1) & 1)) break;
+            if (s == 0 && !wait(bars + kVFull + vslot * 8, vpar)) break;
+            ++n_p[s];
+            tc_fence_after();
+            if (leader) {
+#pragma unroll
+              for (int kk = 0; kk < BN / 16; ++kk)
+                umma_f16_ts(tmem + S_::kColO + s * 128, tmem + buf * BN + kk * 8,
+                            dv + ((vslot * S_::kTile + kk * 2048) >> 4), idesc_o, (it == 0 && kk == 0) ? 0u : 1u);
+              umma_commit(bars + kOFull + s * 8);
+              if (s + 1 == act) umma_commit(bars + kVFree + vslot * 8);
+            }
+            __syncwarp();
+            if (s + 1 == act && ++vslot == VS) { vslot = 0; vpar ^= 1; }
+            // S(it + 2) goes over P(it): the tensor core works in order of issue, so P V is done with it
+            if (it + 2 < p.len) qk(s, act);
+          }
+        }
+      }
     }
   } else if (warp < S_::kSoftmax) {
     // ----------------------------------------------------------------------- softmax warps
@@ -533,10 +572,8 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
       float m_used = -INFINITY, l_run = 0.f;
       for (int it = 0; it < p.len; ++it) {
         const int key0 = tile_key<BN>(p.c, p.t0 + it);
-        const uint32_t buf = NT == 1 ? (n & 1) : (uint32_t)s, par = NT == 1 ? ((n >> 1) & 1) : (n & 1);
-        // every row of the block sees every key of the tile
-        const bool plain = key0 + BN <= p.c.L &&
-                           (a.window == 0 || key0 + BN <= a.sinks || key0 > p.c.L + p.c.n - 1 - a.window);
+        const uint32_t buf = 2 * s + (n & 1), par = (n >> 1) & 1;
+        const bool plain = all_see<BN>(a, p.c, key0);
         if (!plain && s == 0) {
           // Values of V that are not finite would reach rows that do not see their key (0 x NaN): take
           // them out of the tile, and remember the piece if the key exists (see the epilogue).
@@ -566,32 +603,27 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
         if (!wait(bars + kSFull + buf * 8, par)) { ok = false; break; }
         tc_fence_after();
         if (warp_live) {
-          // S is read twice, 32 columns at a time with the next 32 on their way: holding a row of
-          // 128 scores would take most of a thread's registers
           const uint32_t s_col = tmem + lanes + buf * BN;
           uint32_t x[2][32];
-          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          u64 vis = 0;
           tmem_ld_32x32(s_col, x[0]);
+          tmem_ld_32x32(s_col + 32, x[1]);
+          tmem_wait_ld_of(x[0]);
+          tmem_wait_ld_of(x[1]);
+          if (!plain) {
+            const u64 vis = live ? visible(a, p.c, p.b, node, depth, key0) : 0ull;
+            const uint32_t lo = (uint32_t)vis, hi = (uint32_t)(vis >> 32);
 #pragma unroll
-          for (int c = 0; c < BN / 32; ++c) {
-            tmem_wait_ld_of(x[c & 1]);
-            if (c + 1 < BN / 32) tmem_ld_32x32(s_col + (c + 1) * 32, x[(c + 1) & 1]);
-            if (!plain) {
-              if ((c & 1) == 0) vis = live ? visible(a, p.c, p.b, node, depth, key0 + 32 * c) : 0ull;
-              const uint32_t seen = (uint32_t)(vis >> (32 * (c & 1)));
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (!((seen >> j) & 1u)) x[c & 1][j] = 0xFF800000u;     // -inf
-              tmem_st_32x32(s_col + c * 32, x[c & 1]);
+            for (int j = 0; j < 32; ++j) {
+              if (!((lo >> j) & 1u)) x[0][j] = 0xFF800000u;             // -inf
+              if (!((hi >> j) & 1u)) x[1][j] = 0xFF800000u;
             }
-            // maximum of the raw scores (the scale is positive, so it commutes with max); the scale
-            // is applied inside the exponent's multiply-add
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[c & 1][2 * j]), __uint_as_float(x[c & 1][2 * j + 1]));
           }
-          if (!plain) tmem_wait_st();
+          // maximum of the raw scores (the scale is positive, so it commutes with max); the scale
+          // is applied inside the exponent's multiply-add
+          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[0][j]), __uint_as_float(x[1][j]));
           const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
           if (__any_sync(0xFFFFFFFFu, mx > m_used + kRescaleStep)) {
             const float m_new = fmaxf(m_used, mx);
@@ -614,16 +646,13 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
           }
           const float neg = m_used == -INFINITY ? 0.f : -m_used;
           float ps[4] = {0.f, 0.f, 0.f, 0.f};
-          tmem_ld_32x32(s_col, x[0]);
 #pragma unroll
-          for (int c = 0; c < BN / 32; ++c) {           // 32 keys: 16 packed columns of P over S's first half
-            tmem_wait_ld_of(x[c & 1]);
-            if (c + 1 < BN / 32) tmem_ld_32x32(s_col + (c + 1) * 32, x[(c + 1) & 1]);
+          for (int c = 0; c < 2; ++c) {                 // 32 keys: 16 packed columns of P over S's first half
             uint32_t pk[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
               float e0, e1;
-              fma2(e0, e1, __uint_as_float(x[c & 1][2 * j]), __uint_as_float(x[c & 1][2 * j + 1]), a.scale_log2, neg);
+              fma2(e0, e1, __uint_as_float(x[c][2 * j]), __uint_as_float(x[c][2 * j + 1]), a.scale_log2, neg);
               e0 = ex2(e0);
               e1 = ex2(e1);
               add2(ps[(j & 1) * 2], ps[(j & 1) * 2 + 1], e0, e1);
@@ -655,27 +684,13 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
           tmem_ld_32x32(o_col + c * 32, o);
           tmem_wait_ld_of(o);
           if (!live) continue;
-          if (bad) {
-            // rare: add what was taken out of V, for the keys that this row does see
-            for (int it = 0; it < p.len; ++it) {
-              const int key0 = tile_key<BN>(p.c, p.t0 + it);
-              if (key0 + BN <= p.c.L && (a.window == 0 || key0 + BN <= a.sinks || key0 > p.c.L + p.c.n - 1 - a.window))
-                continue;
-              for (int h = 0; h < BN / 64; ++h) {
-                for (u64 vis = visible(a, p.c, p.b, node, depth, key0 + 64 * h); vis; vis &= vis - 1) {
-                  const int key = key0 + 64 * h + __ffsll((long long)vis) - 1, col = key >> a.page_log;
-                  const int page = col < a.table_cols ? a.table[p.b * a.table_stride + col] : -1;
-                  if (page < 0 || page >= a.P) continue;
-                  const T* v = static_cast<const T*>(a.v) + page * a.p_p + p.hk * a.p_h +
-                               (key & ((1 << a.page_log) - 1)) * a.p_r + c * 32;
+          if (bad) {                                    // rare; a copy, so that o stays in registers otherwise
+            uint32_t y[32];
 #pragma unroll
-                  for (int j = 0; j < 32; ++j) {
-                    const float f = (float)v[j];
-                    if (!isfinite(f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + f);
-                  }
-                }
-              }
-            }
+            for (int j = 0; j < 32; ++j) y[j] = o[j];
+            add_back<T, BN>(a, p, node, depth, c * 32, y);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = y[j];
           }
           if (p.whole) {
             T* op = static_cast<T*>(a.out) + p.b * a.o_b + node * a.o_n + head * a.o_h + c * 32;
@@ -712,21 +727,45 @@ paged_attention_kernel(Args a, const __grid_constant__ CUtensorMap tm_k, const _
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S_::kTmem) : "memory");
 }
 
-// Joins the pieces of the units that shares' borders cut.  Block x = (share that holds the unit's
-// first piece, row block), block y takes every gridDim.y-th row.  Eight warps: a row each, or - for
-// units cut into more than eight pieces - eight ranges of one row's pieces, added in a fixed order.
+// Joins the pieces of the units that shares' borders cut.  Block x = (n-th such unit, row block); the
+// n-th unit is found by counting the shares that left one, unless there may be one for every share.
+// Blocks y take eight rows in turn, a warp each, or - for units cut into more than 16 pieces - one row
+// in turn, a warp for each of eight ranges of its pieces, added in a fixed order.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) paged_attention_join_kernel(Args a) {
+__global__ void __launch_bounds__(256) paged_attention_join_kernel(const __grid_constant__ Args a) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   __shared__ float s_m[8], s_l[8], s_o[8][D];
-  const int4 meta = a.meta[blockIdx.x];
+  __shared__ int s_team, s_count[8];
+  const int rb = blockIdx.x % a.RB, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int team = blockIdx.x / a.RB;
+  if ((int)gridDim.x < a.teams * a.RB) {
+    const int nth = team;
+    if (threadIdx.x == 0) s_team = -1;
+    int before = 0;
+    for (int base = 0; base < a.teams; base += 256) {   // (teams <= two blocks an SM: one or two rounds)
+      const int i = base + threadIdx.x;
+      const bool has = i < a.teams && a.meta[(int64_t)i * a.RB + rb].x != 0;
+      const unsigned bal = __ballot_sync(0xFFFFFFFFu, has);
+      __syncthreads();
+      if (lane == 0) s_count[warp] = __popc(bal);
+      __syncthreads();
+      int mine = before + __popc(bal & ((1u << lane) - 1u));
+      for (int w = 0; w < 8; ++w) { if (w < warp) mine += s_count[w]; before += s_count[w]; }
+      if (has && mine == nth) s_team = i;
+    }
+    __syncthreads();
+    team = s_team;
+    if (team < 0) return;
+  }
+  const int64_t block = (int64_t)team * a.RB + rb;
+  const int4 meta = a.meta[block];
   const int np = meta.x, b = meta.y, hk = meta.z;
   if (np == 0) return;
-  const int rb = blockIdx.x % a.RB, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.N) : a.N;
   const int r0 = rb * a.rows, rows = min(a.G * n - r0, a.rows);
   constexpr int E = D / 32;
-  const bool wide = np > 8;
+  const bool wide = np > 16;
   const int lo = wide ? np * warp / 8 : 0, hi = wide ? np * (warp + 1) / 8 : np;
   for (int row0 = wide ? blockIdx.y : blockIdx.y * 8; row0 < rows; row0 += gridDim.y * (wide ? 1 : 8)) {
     const int row = wide ? row0 : row0 + warp;
@@ -735,23 +774,23 @@ __global__ void __launch_bounds__(256) paged_attention_join_kernel(Args a) {
     for (int e = 0; e < E; ++e) o[e] = 0.f;
     if (row < rows) {
       auto at = [&](int i) -> int64_t {                 // piece i: slot 1 of the first block, slot 0 of the others
-        return (((int64_t)blockIdx.x + (int64_t)i * a.RB) * 2 + (i == 0 ? 1 : 0)) * a.rows + row;
+        return ((block + (int64_t)i * a.RB) * 2 + (i == 0 ? 1 : 0)) * a.rows + row;
       };
-      float2 ml[2];
       for (int i = lo + lane; i < hi; i += 32) m = fmaxf(m, a.ws_ml[at(i) * 2]);
 #pragma unroll
       for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
 #pragma unroll 4
       for (int i = lo; i < hi; ++i) {
         const int64_t x = at(i);
-        ml[0] = *reinterpret_cast<const float2*>(a.ws_ml + x * 2);
-        const float w = ml[0].x == -INFINITY ? 0.f : ex2(ml[0].x - m);
-        l += ml[0].y * w;
+        const float2 ml = *reinterpret_cast<const float2*>(a.ws_ml + x * 2);
+        float v[E];
+        if constexpr (E == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(a.ws_o + x * D + lane * E);
+        else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(a.ws_o + x * D + lane * E);
+        const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - m);
+        l += ml.y * w;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float v = a.ws_o[x * D + lane * E + e];
-          if (w != 0.f) o[e] += v * w;
-        }
+        for (int e = 0; e < E; ++e)
+          if (w != 0.f) o[e] += v[e] * w;
       }
     }
     if (wide) {
@@ -863,9 +902,12 @@ rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
   cfg.numAttrs = 1;
   REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_attention_kernel<T, D, NT>, a, tm_k, tm_v));
   rest::count_launch();
-  // about eight blocks of 256 threads per SM in all, never more than there are rows to share
-  const int per = 8 * 148 / (a.teams * a.RB);
-  cfg.gridDim = dim3((unsigned)(a.teams * a.RB), (unsigned)(per < 1 ? 1 : per > a.rows ? a.rows : per), 1);
+  // never more cut units than shares or units; about eight blocks per SM in all, eight rows each at least
+  // (one where units may be cut into more than 16 pieces)
+  const int64_t units = (int64_t)a.B * a.H_kv;
+  const int cut = units < a.teams ? (int)units : a.teams, per = 8 * 148 / (cut * a.RB);
+  const int most = a.teams > 16 * units ? a.rows : (a.rows + 7) / 8;
+  cfg.gridDim = dim3((unsigned)(cut * a.RB), (unsigned)(per < 1 ? 1 : per > most ? most : per), 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.dynamicSmemBytes = 0;
   REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<T, D>, a));
@@ -932,7 +974,7 @@ extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pag
   a.meta = static_cast<int4*>(d_ws);
   a.ws_o = reinterpret_cast<float*>(static_cast<char*>(d_ws) + blocks * sizeof(int4));
   a.ws_ml = a.ws_o + blocks * 2 * pl.rows * D;
-  const int bn = pl.NT == 1 ? 64 : 128;
+  const int bn = 64;                                    // keys per tile
   CUtensorMap tm_k, tm_v;
   if (!encode_pool(&tm_k, d_k_pages, dtype, D, page, H_kv, P, strides + 3, page < bn ? page : bn, a.slot) ||
       !encode_pool(&tm_v, d_v_pages, dtype, D, page, H_kv, P, strides + 3, page < bn ? page : bn, a.slot))

@@ -21,8 +21,8 @@ int sm_count();
 rest_status take_paged_error_flags(uint32_t* h_flags);
 // One slot per kernel instance, library-wide: two kernels on one slot would skip each other's
 // attribute call.  The draft kernel's instances take kSmemSlotDraft + 0 ... 19, the paged
-// attention's kSmemSlotPaged + 0 ... 7.
-constexpr int kSmemSlotDraft = 0, kSmemSlotAttn = 20, kSmemSlotAttnWide = 21, kSmemSlotPaged = 22, kSmemSlots = 32;
+// attention's kSmemSlotPaged + 0 ... 15.
+constexpr int kSmemSlotDraft = 0, kSmemSlotAttn = 20, kSmemSlotAttnWide = 21, kSmemSlotPaged = 22, kSmemSlots = 38;
 
 #define REST_CUDA_TRY(expr)                                              \
   do {                                                                   \

@@ -157,16 +157,29 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
       : "memory");
 }
 
-__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+__device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
       : "memory");
 }
-
-// waits for TMEM loads; the values are named so that nothing that uses them can move ahead of the wait
+// TMEM columns taddr .. of the thread's lane into registers.  The wait names the values, so that nothing
+// that uses them can move ahead of it.
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+      : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+        "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+        "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+      :
+      : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
       : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
@@ -177,6 +190,18 @@ __device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {
         "+r"(r[30]), "+r"(r[31])
       :
       : "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[32]) {
+  tmem_ld_32x32(taddr, r);
+  tmem_wait_ld_of(r);
+}
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[64]) {
+  uint32_t (&lo)[32] = *reinterpret_cast<uint32_t (*)[32]>(&r[0]);
+  uint32_t (&hi)[32] = *reinterpret_cast<uint32_t (*)[32]>(&r[32]);
+  tmem_ld_32x32(taddr, lo);
+  tmem_ld_32x32(taddr + 32, hi);
+  tmem_wait_ld_of(lo);
+  tmem_wait_ld_of(hi);
 }
 
 __device__ unsigned int g_paged_error;                  // bit 0: wait gave up, bit 1: smem misaligned
@@ -189,16 +214,32 @@ template <int D, int NT> struct Shape {
   static constexpr int KS = NT == 1 && D == 128 ? 2 : 4, VS = NT == 1 && D == 128 ? 3 : 6;      // ring stages
   static constexpr int kBars = NT * kQTile + (KS + VS) * kTile;           // barriers behind the tiles
   static constexpr int kSmem = kBars + 512;
-  static constexpr int kSoftmax = 4 * NT;               // softmax warps; then K loader, V loader, MMA
-  static constexpr int kThreads = 32 * (kSoftmax + 3);
+  static constexpr int kSoftmax = 4 * NT;               // softmax warps; then K loader, V loader, MMA warps
+  static constexpr int kThreads = 32 * (kSoftmax + 2 + NT);
   static constexpr uint32_t kTmem = NT == 1 ? 256 : 512;
   static constexpr uint32_t kColO = 2 * NT * BN;        // behind two S buffers for each row tile
+  static constexpr int kStage = D == 128 ? 32 : 16;     // columns joined at a time through the Q tile's memory
 };
 // byte offsets behind kBars
 enum {
   kKFull = 0, kKFree = 32, kVFull = 64, kVFree = 112, kSFull = 160, kPFull = 192, kOFull = 224, kQFull = 240,
-  kTmemSlot = 256, kAbort = 260, kBad = 264, kStartB = 272, kStartOff = 280, kTotal = 288, kScan = 296   // 11 x 8
+  kTmemSlot = 256, kAbort = 260, kBad = 264 /* 8 x 4 */, kStartB = 296, kStartOff = 304, kTotal = 312,
+  kScan = 320 /* 12 x 8 */, kJoin = 416
 };
+
+// Bounded wait of a whole warp, with one result for all lanes (TMEM accesses and elected lanes need
+// them together).  The first look comes without the clock and the abort word: most barriers are ready.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* abort_word) {
+  uint32_t ready;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.b32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(ready)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  if (__all_sync(0xFFFFFFFFu, ready != 0)) return true;
+  return __all_sync(0xFFFFFFFFu, mbar_wait_abortable(bar, parity, abort_word) ? 1 : 0) != 0;
+}
 
 // one 64-element x box-rows box of the pool -> shared memory
 __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int c0, int row, int head, int page,
@@ -265,9 +306,10 @@ __device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int dept
   return v;
 }
 
-// What was taken out of V (see below), added to columns d0 .. d0 + 31 of a row that does see its key.
+// What was taken out of V (see below), added to columns d0 .. d0 + cols - 1 of a row that
+// does see its key.
 template <typename T, int BN>
-__device__ __noinline__ void add_back(const Args& a, Piece p, int node, int depth, int d0, uint32_t (&o)[32]) {
+__device__ __noinline__ void add_back(const Args& a, Piece p, int node, int depth, int d0, int cols, uint32_t* o) {
   for (int it = 0; it < p.len; ++it) {
     const int key0 = tile_key<BN>(p.c, p.t0 + it);
     if (all_see<BN>(a, p.c, key0)) continue;
@@ -278,7 +320,7 @@ __device__ __noinline__ void add_back(const Args& a, Piece p, int node, int dept
         if (page < 0 || page >= a.P) continue;
         const T* v = static_cast<const T*>(a.v) + page * a.p_p + p.hk * a.p_h +
                      (key & ((1 << a.page_log) - 1)) * a.p_r + d0;
-        for (int j = 0; j < 32; ++j) {
+        for (int j = 0; j < cols; ++j) {
           const float f = (float)v[j];
           if (!isfinite(f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + f);
         }
@@ -287,7 +329,7 @@ __device__ __noinline__ void add_back(const Args& a, Piece p, int node, int dept
   }
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, int C>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, NT == 1 ? 2 : 1)
 paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   using S_ = Shape<D, NT>;
@@ -300,7 +342,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
   unsigned char* ctl = smem + S_::kBars;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + kTmemSlot);
   volatile uint32_t* abort_word = reinterpret_cast<volatile uint32_t*>(ctl + kAbort);
-  volatile int* s_bad = reinterpret_cast<volatile int*>(ctl + kBad);       // piece number + 1, by parity
+  volatile int* s_bad = reinterpret_cast<volatile int*>(ctl + kBad);       // [piece % 8]: piece + 1
   const int team = blockIdx.x / a.RB, rb = blockIdx.x % a.RB;
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -309,8 +351,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     return;                     // uniform over the grid: every block sees the same offset
   }
   if (tid == 0) {
-    for (int i = 0; i < KS; ++i) { mbar_init(bars + kKFull + 8 * i, 1); mbar_init(bars + kKFree + 8 * i, 1); }
-    for (int i = 0; i < VS; ++i) { mbar_init(bars + kVFull + 8 * i, 1); mbar_init(bars + kVFree + 8 * i, 1); }
+    for (int i = 0; i < KS; ++i) { mbar_init(bars + kKFull + 8 * i, 1); mbar_init(bars + kKFree + 8 * i, NT); }
+    for (int i = 0; i < VS; ++i) { mbar_init(bars + kVFull + 8 * i, 1); mbar_init(bars + kVFree + 8 * i, NT); }
     for (int i = 0; i < 4; ++i) {
       mbar_init(bars + kSFull + 8 * i, 1);
       mbar_init(bars + kPFull + 8 * i, 4);              // one arrival per softmax warp
@@ -318,8 +360,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     for (int i = 0; i < 2; ++i) {
       mbar_init(bars + kOFull + 8 * i, 1);
       mbar_init(bars + kQFull + 8 * i, 4);
-      s_bad[i] = 0;
     }
+    mbar_init(bars + kJoin, S_::kSoftmax);
+    for (int i = 0; i < 8; ++i) s_bad[i] = 0;
     *abort_word = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -408,7 +451,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         const int next_page = it + 1 < p.len ? find(it + 1, next_row) : page;
         if (page < 0 || page >= a.P) page = a.P;        // outside the map: reads as zeros
         if (filled >= stages)
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait_abortable(free_ + slot * 8, parity, abort_word)) != 0;
+          ok = wait_warp(free_ + slot * 8, parity, abort_word);
         if (!ok) break;
         if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)S_::kTile);
         __syncwarp();
@@ -451,100 +494,99 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       }
       a.meta[blockIdx.x] = m;
     }
-  } else if (warp == S_::kSoftmax + 2) {
-    // ------------------------------------------------------------------------- MMA issuer
+  } else if (warp >= S_::kSoftmax + 2) {
+    // ------------------------------------------------------------- MMA issuers, one per row tile
     // The whole warp walks the loop, so that descriptors and addresses stay in uniform registers, and one
     // elected lane issues (a loop in one lane moved them there before every instruction: about 100 cycles
-    // each, three times what the tensor core needs).
-    {
-      const uint32_t leader = elect_one();
-      constexpr uint32_t idesc_s = idesc<T>(BN, 0), idesc_o = idesc<T>(D, 1);
-      const uint64_t dq = umma_desc(sQ, 16, 1024), dk = umma_desc(sK, 16, 1024), dv = umma_desc(sV, BN * 128, 1024);
-      int kslot = 0, vslot = 0;
-      uint32_t kpar = 0, vpar = 0;
-      uint32_t n_p[2] = {0u, 0u}, n_q[2] = {0u, 0u}, n_s[2] = {0u, 0u};   // per row tile: P, Q taken, S issued
-      bool ok = true;
-      auto wait = [&](uint32_t bar, uint32_t parity) {
-        ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_abortable(bar, parity, abort_word) ? 1 : 0) != 0;
-        return ok;
-      };
-      // S of the next key tile for the first `act` row tiles, from one on (the K tile is given back
-      // after the last one)
-      auto qk = [&](int s, int act) {
-        if (s == 0 && !wait(bars + kKFull + kslot * 8, kpar)) return;
+    // each, three times what the tensor core needs).  With two row tiles, one's waits are filled by the
+    // other's instructions.
+    const int s = warp - (S_::kSoftmax + 2);
+    const uint32_t leader = elect_one();
+    constexpr uint32_t idesc_s = idesc<T>(BN, 0), idesc_o = idesc<T>(D, 1);
+    const uint64_t dq = umma_desc(sQ + s * S_::kQTile, 16, 1024), dk = umma_desc(sK, 16, 1024),
+                   dv = umma_desc(sV, BN * 128, 1024);
+    const uint32_t t_s = tmem + 2 * s * BN, t_o = tmem + S_::kColO + s * 128;
+    const uint32_t b_s = bars + kSFull + 16 * s, b_p = bars + kPFull + 16 * s, b_o = bars + kOFull + 8 * s;
+    uint32_t base = 0, n_s = 0, n_p = 0, n_q = 0;       // key tiles before this piece; S issued, P and Q taken
+    bool ok = true;
+    while (ok && walk.next(p)) {
+      // one row tile's rows only: the two row tiles take the key tiles in turn
+      const bool turns = NT == 2 && p.rows <= 128;
+      const int step = turns ? 2 : 1;
+      auto qk = [&](int it) {                           // S of key tile `it`
+        const uint32_t g = base + it, slot = g % KS, buf = n_s++ & 1;
+        ok = ok && wait_warp(bars + kKFull + slot * 8, (g / KS) & 1, abort_word);
+        if (!ok) return;
         tc_fence_after();
-        const uint32_t buf = 2 * s + (n_s[s]++ & 1);
         if (leader) {
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t qoff = (uint32_t)(s * S_::kQTile + (ks >> 2) * (128 * 128) + (ks & 3) * 32);
-            const uint32_t koff = (uint32_t)(kslot * S_::kTile + (ks >> 2) * (BN * 128) + (ks & 3) * 32);
-            umma_f16(tmem + buf * BN, dq + (qoff >> 4), dk + (koff >> 4), idesc_s, ks > 0);
+            const uint32_t qoff = (uint32_t)((ks >> 2) * (128 * 128) + (ks & 3) * 32);
+            const uint32_t koff = (uint32_t)((ks >> 2) * (BN * 128) + (ks & 3) * 32);
+            umma_f16(t_s + buf * BN, dq + (qoff >> 4), dk + ((slot * S_::kTile + koff) >> 4), idesc_s, ks > 0);
           }
-          umma_commit(bars + kSFull + buf * 8);
-          if (s + 1 == act) umma_commit(bars + kKFree + kslot * 8);
+          umma_commit(b_s + buf * 8);
+          umma_commit(bars + kKFree + slot * 8);
+          if (turns) umma_commit(bars + kKFree + slot * 8);      // for both row tiles
         }
         __syncwarp();
-        if (s + 1 == act && ++kslot == KS) { kslot = 0; kpar ^= 1; }
       };
-      while (ok && walk.next(p)) {
-        const int act = NT == 2 && p.rows > 128 ? 2 : 1;
+      int it = turns ? s : 0;
+      ok = wait_warp(bars + kQFull + s * 8, n_q++ & 1, abort_word);
+      if (ok && it < p.len) qk(it);
+      if (ok && it + step < p.len) qk(it + step);
+      for (bool fresh = true; ok && it < p.len; it += step, fresh = false) {
+        const uint32_t g = base + it, slot = g % VS, buf = n_p & 1;
+        ok = wait_warp(bars + kVFull + slot * 8, (g / VS) & 1, abort_word) &&
+             wait_warp(b_p + buf * 8, (n_p >> 1) & 1, abort_word);
+        if (!ok) break;
+        ++n_p;
+        tc_fence_after();
+        if (leader) {
 #pragma unroll
-        for (int s = 0; s < NT; ++s)
-          if (s < act) wait(bars + kQFull + s * 8, n_q[s]++ & 1);
-        for (int it = 0; it < 2 && it < p.len; ++it)
-#pragma unroll
-          for (int s = 0; s < NT; ++s)
-            if (ok && s < act) qk(s, act);
-        for (int it = 0; ok && it < p.len; ++it) {
-#pragma unroll
-          for (int s = 0; s < NT; ++s) {
-            if (!ok || s >= act) break;
-            const uint32_t buf = 2 * s + (n_p[s] & 1);
-            if (!wait(bars + kPFull + buf * 8, (n_p[s] >> 1) & 1)) break;
-            if (s == 0 && !wait(bars + kVFull + vslot * 8, vpar)) break;
-            ++n_p[s];
-            tc_fence_after();
-            if (leader) {
-#pragma unroll
-              for (int kk = 0; kk < BN / 16; ++kk)
-                umma_f16_ts(tmem + S_::kColO + s * 128, tmem + buf * BN + kk * 8,
-                            dv + ((vslot * S_::kTile + kk * 2048) >> 4), idesc_o, (it == 0 && kk == 0) ? 0u : 1u);
-              umma_commit(bars + kOFull + s * 8);
-              if (s + 1 == act) umma_commit(bars + kVFree + vslot * 8);
-            }
-            __syncwarp();
-            if (s + 1 == act && ++vslot == VS) { vslot = 0; vpar ^= 1; }
-            // S(it + 2) goes over P(it): the tensor core works in order of issue, so P V is done with it
-            if (it + 2 < p.len) qk(s, act);
-          }
+          for (int kk = 0; kk < BN / 16; ++kk)
+            umma_f16_ts(t_o, t_s + buf * BN + kk * 8, dv + ((slot * S_::kTile + kk * 2048) >> 4), idesc_o,
+                        (fresh && kk == 0) ? 0u : 1u);
+          umma_commit(b_o);
+          umma_commit(bars + kVFree + slot * 8);
+          if (turns) umma_commit(bars + kVFree + slot * 8);
         }
+        __syncwarp();
+        // S two tiles on goes over this P: the tensor core works in order of issue, so P V is done with it
+        if (it + 2 * step < p.len) qk(it + 2 * step);
       }
+      base += p.len;
     }
-  } else if (warp < S_::kSoftmax) {
+  } else {
     // ----------------------------------------------------------------------- softmax warps
-    const int s = warp >> 2, t = tid & 127;             // which 128-row tile, row inside it
+    // A thread owns one row of its row tile.  With C copies (few rows) the tile holds the same 128 / C
+    // packed rows C times and copy ci takes the ci-th 64 / C keys of every key tile, so that all four
+    // warps work; the P of its other keys is zero.  Two row tiles that take the key tiles in turn are
+    // two copies as well.  Copies have maxima, sums and O of their own and are joined at the end.
+    constexpr int kCopyRows = 128 / C, KP = BN / C;     // rows of a copy, keys of a thread per key tile
+    const int s = warp >> 2, t = tid & 127;             // which row tile, row inside it
+    const int ci = t / kCopyRows, tr = t % kCopyRows;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t o_col = tmem + lanes + S_::kColO + s * 128;
-    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {   // warp-uniform, so TMEM accesses stay converged
-      return __all_sync(0xFFFFFFFFu, mbar_wait_abortable(bar, parity, abort_word) ? 1 : 0) != 0;
-    };
-    uint32_t n = 0, vslot = 0, vpar = 0;
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return wait_warp(bar, parity, abort_word); };
+    uint32_t n = 0, base = 0, joins = 0;
     int piece = 0;
     bool ok = true;
-    while (ok && walk.next(p)) {
+    for (; ok && walk.next(p); base += p.len) {
       ++piece;
-      if (s * 128 >= p.rows) continue;                  // (NT = 2: the second tile has no rows)
-      const int r0 = rb * S_::kRows + s * 128;          // first packed row of this tile
-      const int rows = min(128, p.rows - s * 128);
+      const bool turns = NT == 2 && p.rows <= 128;
+      const int step = turns ? 2 : 1;
+      const int r0 = rb * S_::kRows + (turns ? 0 : s * 128);               // first packed row of this tile
+      const int rows = min(kCopyRows, p.rows - (turns ? 0 : s * 128));
       {  // Q rows -> shared memory, K-major 128-byte-swizzled; rows past the last one hold zeros
         const T* q = static_cast<const T*>(a.q) + p.b * a.q_b + (int64_t)p.hk * a.G * a.q_h;
         constexpr int kChunks = D / 8;                  // 16-byte chunks per row
+        constexpr int kStep = kChunks / C < 4 ? kChunks / C : 4;
+#pragma unroll 1
+        for (int j0 = 0; j0 < kChunks / C; j0 += kStep) {   // each row is read once and written for every copy
+          uint4 x[kStep];
 #pragma unroll
-        for (int j0 = 0; j0 < kChunks; j0 += 8) {
-          uint4 x[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
+          for (int j = 0; j < kStep; ++j) {
             const int e = (j0 + j) * 128 + t, row = e / kChunks, chunk = e % kChunks;
             x[j] = make_uint4(0u, 0u, 0u, 0u);
             if (row < rows) {
@@ -553,36 +595,44 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             }
           }
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int e = (j0 + j) * 128 + t, row = e / kChunks, chunk = e % kChunks;
-            const uint32_t dst = sQ + s * S_::kQTile + (chunk >> 3) * (128 * 128) + (row >> 3) * 1024 + (row & 7) * 128 +
-                                 (((chunk & 7) ^ (row & 7)) << 4);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(x[j].x), "r"(x[j].y), "r"(x[j].z),
-                         "r"(x[j].w)
-                         : "memory");
+          for (int j = 0; j < kStep; ++j) {
+            const int e = (j0 + j) * 128 + t, chunk = e % kChunks;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+              const int row = e / kChunks + c * kCopyRows;
+              const uint32_t dst = sQ + s * S_::kQTile + (chunk >> 3) * (128 * 128) + (row >> 3) * 1024 + (row & 7) * 128 +
+                                   (((chunk & 7) ^ (row & 7)) << 4);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(x[j].x), "r"(x[j].y), "r"(x[j].z),
+                           "r"(x[j].w)
+                           : "memory");
+            }
           }
         }
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + kQFull + s * 8);
       }
-      const bool warp_live = (warp & 3) * 32 < rows, live = t < rows;
-      const int node = live ? (r0 + t) / a.G : 0, head = p.hk * a.G + (live ? (r0 + t) % a.G : 0);
+      const bool warp_live = tr - lane < rows, live = tr < rows;
+      const int node = live ? (r0 + tr) / a.G : 0, head = p.hk * a.G + (live ? (r0 + tr) % a.G : 0);
       const int depth = live ? node_depth(a, p.b, node) : 1;
       float m_used = -INFINITY, l_run = 0.f;
-      for (int it = 0; it < p.len; ++it) {
+      int it = turns ? s : 0;
+      for (bool fresh = true; it < p.len; it += step, fresh = false) {
         const int key0 = tile_key<BN>(p.c, p.t0 + it);
         const uint32_t buf = 2 * s + (n & 1), par = (n >> 1) & 1;
         const bool plain = all_see<BN>(a, p.c, key0);
-        if (!plain && s == 0) {
+        if (!plain) {
           // Values of V that are not finite would reach rows that do not see their key (0 x NaN): take
-          // them out of the tile, and remember the piece if the key exists (see the epilogue).
-          if (!wait(bars + kVFull + vslot * 8, vpar)) { ok = false; break; }
-          bool bad = false;
+          // them out of the tile, and remember the piece if the key exists (see the epilogue).  Both row
+          // tiles do it when both use the tile, each before its own P V; the piece is remembered before a
+          // value is cleared, so whoever finds it cleared finds it remembered.  (One row tile is never
+          // more than six key tiles ahead of the other, so eight pieces are told apart.)
+          const uint32_t g = base + it, slot = g % VS;
+          if (!wait(bars + kVFull + slot * 8, (g / VS) & 1)) { ok = false; break; }
 #pragma unroll 4
           for (int j = 0; j < S_::kTile / 16 / 128; ++j) {
             const uint32_t at = (uint32_t)((j * 128 + t) * 16);
-            const uint32_t src = sV + vslot * S_::kTile + at;
+            const uint32_t src = sV + slot * S_::kTile + at;
             uint32_t w[4];
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src) : "memory");
             bool hit = false;
@@ -593,49 +643,42 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
               if ((w[e] & hi) == hi) { w[e] &= 0x0000FFFFu; hit = true; }
             }
             if (hit) {
+              if (key0 + (int)((at % (BN * 128)) >> 7) < p.c.L + p.c.n) { s_bad[piece & 7] = piece + 1; __threadfence_block(); }
               asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(src), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-              bad = bad || key0 + (int)((at % (BN * 128)) >> 7) < p.c.L + p.c.n;
             }
           }
-          if (bad) s_bad[piece & 1] = piece + 1;
           fence_async_smem();
         }
         if (!wait(bars + kSFull + buf * 8, par)) { ok = false; break; }
         tc_fence_after();
         if (warp_live) {
           const uint32_t s_col = tmem + lanes + buf * BN;
-          uint32_t x[2][32];
-          tmem_ld_32x32(s_col, x[0]);
-          tmem_ld_32x32(s_col + 32, x[1]);
-          tmem_wait_ld_of(x[0]);
-          tmem_wait_ld_of(x[1]);
+          uint32_t x[KP];
+          tmem_load(s_col + ci * KP, x);
           if (!plain) {
-            const u64 vis = live ? visible(a, p.c, p.b, node, depth, key0) : 0ull;
+            const u64 vis = live ? visible(a, p.c, p.b, node, depth, key0) >> (ci * KP) : 0ull;
             const uint32_t lo = (uint32_t)vis, hi = (uint32_t)(vis >> 32);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              if (!((lo >> j) & 1u)) x[0][j] = 0xFF800000u;             // -inf
-              if (!((hi >> j) & 1u)) x[1][j] = 0xFF800000u;
-            }
+            for (int j = 0; j < KP; ++j)
+              if (!(((j < 32 ? lo : hi) >> (j & 31)) & 1u)) x[j] = 0xFF800000u;       // -inf
           }
           // maximum of the raw scores (the scale is positive, so it commutes with max); the scale
           // is applied inside the exponent's multiply-add
           float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[0][j]), __uint_as_float(x[1][j]));
+          for (int j = 0; j < KP / 2; ++j)
+            mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
           const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
           if (__any_sync(0xFFFFFFFFu, mx > m_used + kRescaleStep)) {
             const float m_new = fmaxf(m_used, mx);
             const float alpha = m_new == -INFINITY ? 1.f : ex2(m_used - m_new);   // m_used = -inf gives 0
-            if (it > 0) {
+            if (!fresh) {
               if (!wait(bars + kOFull + s * 8, (n - 1) & 1)) { ok = false; break; }
               tc_fence_after();
 #pragma unroll
               for (int c = 0; c < D / 32; ++c) {
                 uint32_t o[32];
-                tmem_ld_32x32(o_col + c * 32, o);
-                tmem_wait_ld_of(o);
+                tmem_load(o_col + c * 32, o);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
                 tmem_st_32x32(o_col + c * 32, o);
@@ -646,19 +689,26 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           }
           const float neg = m_used == -INFINITY ? 0.f : -m_used;
           float ps[4] = {0.f, 0.f, 0.f, 0.f};
+          // P: 64 keys in 32 packed columns over S's first half, eight columns at a time
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {                 // 32 keys: 16 packed columns of P over S's first half
-            uint32_t pk[16];
+          for (int c = 0; c < 4; ++c) {
+            if (C == 1 || c / (4 / C) == ci) {          // (warp-uniform)
+              const int c0 = C == 1 ? c : c % (4 / C);
+              uint32_t pk[8];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              float e0, e1;
-              fma2(e0, e1, __uint_as_float(x[c][2 * j]), __uint_as_float(x[c][2 * j + 1]), a.scale_log2, neg);
-              e0 = ex2(e0);
-              e1 = ex2(e1);
-              add2(ps[(j & 1) * 2], ps[(j & 1) * 2 + 1], e0, e1);
-              pk[j] = Type<T>::pack(e0, e1);
+              for (int j = 0; j < 8; ++j) {
+                float e0, e1;
+                fma2(e0, e1, __uint_as_float(x[c0 * 16 + 2 * j]), __uint_as_float(x[c0 * 16 + 2 * j + 1]), a.scale_log2, neg);
+                e0 = ex2(e0);
+                e1 = ex2(e1);
+                add2(ps[(j & 1) * 2], ps[(j & 1) * 2 + 1], e0, e1);
+                pk[j] = Type<T>::pack(e0, e1);
+              }
+              tmem_st_32x8(s_col + c * 8, pk);
+            } else {
+              const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+              tmem_st_32x8(s_col + c * 8, zero);
             }
-            tmem_st_32x16(s_col + c * 16, pk);
           }
           l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
           tmem_wait_st();
@@ -667,55 +717,128 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + kPFull + buf * 8);
         ++n;
-        if (++vslot == VS) { vslot = 0; vpar ^= 1; }
       }
-      if (!ok || !wait(bars + kOFull + s * 8, (n - 1) & 1)) { ok = false; break; }
+      if (!ok) break;
+      if ((turns ? s : 0) < p.len && !wait(bars + kOFull + s * 8, (n - 1) & 1)) { ok = false; break; }
       tc_fence_after();
       // ---- epilogue: a finished unit's rows go to the output, others to the scratch
-      const bool bad = s_bad[piece & 1] == piece + 1;
       // scratch slot 1: the unit's first piece; 0: a later one (then it is the block's first piece)
-      const int64_t wrow = ((int64_t)blockIdx.x * 2 + (p.t0 == 0 ? 1 : 0)) * a.rows + s * 128 + t;
-      const float inv = l_run != 0.f ? 1.f / l_run : 0.f;
-      if (warp_live) {
+      const int64_t w0 = ((int64_t)blockIdx.x * 2 + (p.t0 == 0 ? 1 : 0)) * a.rows + (turns ? 0 : s * 128);
+      if (C == 1 && !turns) {
+        const bool bad = s_bad[piece & 7] == piece + 1;
+        const float inv = l_run != 0.f ? 1.f / l_run : 0.f;
+        if (warp_live) {
 #pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t o[32];
-          __syncwarp();
-          tmem_ld_32x32(o_col + c * 32, o);
-          tmem_wait_ld_of(o);
-          if (!live) continue;
-          if (bad) {                                    // rare; a copy, so that o stays in registers otherwise
-            uint32_t y[32];
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            __syncwarp();
+            tmem_load(o_col + c * 32, o);
+            if (!live) continue;
+            if (bad) {                                  // rare; a copy, so that o stays in registers otherwise
+              uint32_t y[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) y[j] = o[j];
-            add_back<T, BN>(a, p, node, depth, c * 32, y);
+              for (int j = 0; j < 32; ++j) y[j] = o[j];
+              add_back<T, BN>(a, p, node, depth, c * 32, 32, y);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = y[j];
-          }
-          if (p.whole) {
-            T* op = static_cast<T*>(a.out) + p.b * a.o_b + node * a.o_n + head * a.o_h + c * 32;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t w[4];
-#pragma unroll
-              for (int f = 0; f < 4; ++f)
-                w[f] = Type<T>::pack(__uint_as_float(o[8 * e + 2 * f]) * inv, __uint_as_float(o[8 * e + 2 * f + 1]) * inv);
-              *reinterpret_cast<uint4*>(op + e * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int j = 0; j < 32; ++j) o[j] = y[j];
             }
-          } else {
-            float4* wo = reinterpret_cast<float4*>(a.ws_o + wrow * D + c * 32);
+            if (p.whole) {
+              T* op = static_cast<T*>(a.out) + p.b * a.o_b + node * a.o_n + head * a.o_h + c * 32;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              wo[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
-                                  __uint_as_float(o[4 * e + 3]));
+              for (int e = 0; e < 4; ++e) {
+                uint32_t w[4];
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+                  w[f] = Type<T>::pack(__uint_as_float(o[8 * e + 2 * f]) * inv, __uint_as_float(o[8 * e + 2 * f + 1]) * inv);
+                *reinterpret_cast<uint4*>(op + e * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+              }
+            } else {
+              float4* wo = reinterpret_cast<float4*>(a.ws_o + (w0 + t) * D + c * 32);
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                wo[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                    __uint_as_float(o[4 * e + 3]));
+            }
           }
         }
-        if (live) {
-          if (!p.whole)
-            *reinterpret_cast<float2*>(a.ws_ml + wrow * 2) = make_float2(m_used, l_run);
-          else if (a.lse)
-            a.lse[((int64_t)p.b * a.H + head) * a.N + node] = l_run != 0.f ? (m_used + log2f(l_run)) * kLn2 : -INFINITY;
+      } else {
+        // Join the copies: maxima and sums, then O a few columns at a time, through the memory of the Q
+        // tile (its last reader, this piece's last S, is done; the next Q comes from these warps).
+        constexpr int kCopies = NT == 2 ? 2 : C, kAll = 128 * NT, kCols = S_::kStage;
+        float2* s_ml = reinterpret_cast<float2*>(smem + kAll * kCols * 4);         // [kAll]
+        auto sync = [&]() -> bool {                     // all softmax warps, with a bounded wait
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bars + kJoin);
+          ok = wait(bars + kJoin, joins++ & 1);
+          return ok;
+        };
+        if (!sync()) break;                             // (NT = 2: the other tile's last S is done too)
+        s_ml[tid] = make_float2(m_used, l_run);
+        if (!sync()) break;
+        const int first = NT == 2 ? t : tr, apart = NT == 2 ? 128 : kCopyRows;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) top = fmaxf(top, s_ml[first + c * apart].x);
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) {
+          const float2 ml = s_ml[first + c * apart];
+          if (ml.x != -INFINITY) sum += ml.y * ex2(ml.x - top);
         }
+        const bool bad = s_bad[piece & 7] == piece + 1;
+        const bool lead_copy = tid < apart;
+        float w = m_used == -INFINITY ? 0.f : ex2(m_used - top);
+        const float inv = p.whole ? (sum != 0.f ? 1.f / sum : 0.f) : 1.f;
+        w *= inv;
+        if (live && lead_copy) { m_used = top; l_run = sum; }
+#pragma unroll 1
+        for (int c = 0; c < D / kCols; ++c) {
+          if (c && !sync()) break;
+          if (warp_live) {
+            uint32_t o[kCols];
+            tmem_load(o_col + c * kCols, o);
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
+            if (bad && lead_copy && live) {
+              uint32_t y[kCols];
+#pragma unroll
+              for (int j = 0; j < kCols; ++j) y[j] = o[j];
+              add_back<T, BN>(a, p, node, depth, c * kCols, kCols, y);
+#pragma unroll
+              for (int j = 0; j < kCols; ++j) o[j] = y[j];
+            }
+#pragma unroll
+            for (int e = 0; e < kCols / 4; ++e)
+              *reinterpret_cast<uint4*>(smem + ((size_t)tid * kCols + ((e ^ (lane & (kCols / 4 - 1))) * 4)) * 4) =
+                  make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          }
+          if (!sync()) break;
+          for (int e = tid; e < rows * (kCols / 4); e += kAll) {
+            const int row = e / (kCols / 4), col = e % (kCols / 4);
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) {
+              const int from = row + k * apart;
+              const float4 z = *reinterpret_cast<const float4*>(smem + ((size_t)from * kCols + ((col ^ (from & (kCols / 4 - 1))) * 4)) * 4);
+              y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+            }
+            const int d = c * kCols + col * 4;
+            if (p.whole) {
+              const int i = (r0 + row) / a.G, hd = p.hk * a.G + (r0 + row) - i * a.G;
+              *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + p.b * a.o_b + i * a.o_n + hd * a.o_h + d) =
+                  make_uint2(Type<T>::pack(y.x, y.y), Type<T>::pack(y.z, y.w));
+            } else {
+              *reinterpret_cast<float4*>(a.ws_o + (w0 + row) * D + d) = y;
+            }
+          }
+        }
+        if (!ok || !sync()) break;                      // the Q tile's memory is free again
+        if (!lead_copy) { tc_fence_before(); continue; }
+      }
+      if (live) {
+        if (!p.whole)
+          *reinterpret_cast<float2*>(a.ws_ml + (w0 + tr) * 2) = make_float2(m_used, l_run);
+        else if (a.lse)
+          a.lse[((int64_t)p.b * a.H + head) * a.N + node] = l_run != 0.f ? (m_used + log2f(l_run)) * kLn2 : -INFINITY;
       }
       tc_fence_before();                                // O is read: the next piece's P V may overwrite it
     }
@@ -886,10 +1009,10 @@ size_t workspace_bytes(const Plan& p, int D) {
   return blocks * sizeof(int4) + blocks * 2 * p.rows * (D + 2) * sizeof(float);
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, int C>
 rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int smem_slot, cudaStream_t st) {
   using S_ = Shape<D, NT>;
-  REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(paged_attention_kernel<T, D, NT>), smem_slot, S_::kSmem));
+  REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(paged_attention_kernel<T, D, NT, C>), smem_slot, S_::kSmem));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.teams * a.RB), 1, 1);
   cfg.blockDim = dim3((unsigned)S_::kThreads, 1, 1);
@@ -900,7 +1023,7 @@ rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_attention_kernel<T, D, NT>, a, tm_k, tm_v));
+  REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_attention_kernel<T, D, NT, C>, a, tm_k, tm_v));
   rest::count_launch();
   // never more cut units than shares or units; about eight blocks per SM in all, eight rows each at least
   // (one where units may be cut into more than 16 pieces)
@@ -913,6 +1036,15 @@ rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
   REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<T, D>, a));
   rest::count_launch();
   return REST_OK;
+}
+
+template <typename T, int D>
+rest_status pick(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Plan& pl, int slot, cudaStream_t st) {
+  slot += rest::kSmemSlotPaged;
+  if (pl.NT == 2) return run<T, D, 2, 1>(a, tm_k, tm_v, slot, st);
+  if (pl.rows > 64) return run<T, D, 1, 1>(a, tm_k, tm_v, slot + 1, st);
+  if (pl.rows > 32) return run<T, D, 1, 2>(a, tm_k, tm_v, slot + 2, st);
+  return run<T, D, 1, 4>(a, tm_k, tm_v, slot + 3, st);
 }
 
 }  // namespace
@@ -980,11 +1112,7 @@ extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pag
       !encode_pool(&tm_v, d_v_pages, dtype, D, page, H_kv, P, strides + 3, page < bn ? page : bn, a.slot))
     return rest::note_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int smem_slot = rest::kSmemSlotPaged + (dtype == REST_FP16) * 4 + (D == 64) * 2 + (pl.NT == 1);
-  if (dtype == REST_BF16) {
-    if (D == 128) return pl.NT == 1 ? run<__nv_bfloat16, 128, 1>(a, tm_k, tm_v, smem_slot, st) : run<__nv_bfloat16, 128, 2>(a, tm_k, tm_v, smem_slot, st);
-    return pl.NT == 1 ? run<__nv_bfloat16, 64, 1>(a, tm_k, tm_v, smem_slot, st) : run<__nv_bfloat16, 64, 2>(a, tm_k, tm_v, smem_slot, st);
-  }
-  if (D == 128) return pl.NT == 1 ? run<__half, 128, 1>(a, tm_k, tm_v, smem_slot, st) : run<__half, 128, 2>(a, tm_k, tm_v, smem_slot, st);
-  return pl.NT == 1 ? run<__half, 64, 1>(a, tm_k, tm_v, smem_slot, st) : run<__half, 64, 2>(a, tm_k, tm_v, smem_slot, st);
+  const bool bf16 = dtype == REST_BF16;
+  if (D == 128) return bf16 ? pick<__nv_bfloat16, 128>(a, tm_k, tm_v, pl, 0, st) : pick<__half, 128>(a, tm_k, tm_v, pl, 4, st);
+  return bf16 ? pick<__nv_bfloat16, 64>(a, tm_k, tm_v, pl, 8, st) : pick<__half, 64>(a, tm_k, tm_v, pl, 12, st);
 }

@@ -449,7 +449,7 @@ rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int
  *   d_ws            scratch of rest_paged_attention_workspace_bytes() bytes, 16-byte aligned (the
  *                   query answers for the current device).  Calls that may run at the same time,
  *                   captured graphs among them, need scratch of their own.
- *   Limits: D = 64 or 128; 1 <= N <= 256; H % H_kv == 0.
+ *   Limits: D = 64 or 128; 1 <= N <= 256; H % H_kv == 0, H / H_kv <= 1024, H <= 65536.
  */
 size_t rest_paged_attention_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t N, int32_t D);
 rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const void* d_v_pages,

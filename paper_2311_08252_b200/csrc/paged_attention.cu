@@ -63,10 +63,19 @@ struct Args {
   float *ws_o, *ws_ml;                                  // partial rows [block][2][rows][D], [..][2]
   int64_t q_b, q_n, q_h, p_p, p_h, p_r, o_b, o_n, o_h, table_stride;
   int B, H, H_kv, G, N, Wm, P, page_log, table_cols, window, sinks, teams, RB, rows;
+  uint32_t g_inverse;                                   // ceil(2^32 / G), G > 1
   int slot[3];                                          // tensor-map coordinate (1..3) of row, head, page
   float scale_log2;
 };
 
+// packed row r = node * G + head within the group (r * G < 2^32: the product's error stays below 1)
+__device__ __forceinline__ int node_of(const Args& a, int r) {
+  return a.G == 1 ? r : (int)__umulhi((uint32_t)r, a.g_inverse);
+}
+// n / d; most are small, and a 64-bit division takes some hundred instructions
+__device__ __forceinline__ long long divide(long long n, long long d) {
+  return ((n | d) >> 32) == 0 ? (long long)((uint32_t)n / (uint32_t)d) : n / d;
+}
 // One context's keys and its list of visible tiles: the first ns tiles hold the sinks, the others
 // run from tile w0 to the end.
 struct Ctx { int L, n, w0, ns; long long nt; };
@@ -103,7 +112,7 @@ struct Walk {
       p.c = context<BN>(a, b);
       if (off >= a.H_kv * p.c.nt) { off -= a.H_kv * p.c.nt; ++b; continue; }
       p.b = b;
-      p.hk = (int)(off / p.c.nt);
+      p.hk = (int)divide(off, p.c.nt);
       p.t0 = (int)(off - p.hk * p.c.nt);
       p.len = (int)min(p.c.nt - (long long)p.t0, left);
       p.first = at_start;
@@ -222,7 +231,7 @@ template <int D, int NT> struct Shape {
 };
 // byte offsets behind kBars
 enum {
-  kKFull = 0, kKFree = 32, kVFull = 64, kVFree = 112, kSFull = 160, kPFull = 192, kOFull = 224, kQFull = 240,
+  kKFull = 0, kKFree = 32, kVFull = 64, kVFree = 112, kSFull = 160, kPFull = 192, kOFull = 224, kQFull = 240, kQFree = 248,
   kTmemSlot = 256, kAbort = 260, kBad = 264 /* 8 x 4 */, kStartB = 296, kStartOff = 304, kTotal = 312,
   kScan = 320 /* 12 x 8 */, kJoin = 416
 };
@@ -359,8 +368,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bars + kOFull + 8 * i, 1);
-      mbar_init(bars + kQFull + 8 * i, 4);
     }
+    mbar_init(bars + kQFull, 1);
+    mbar_init(bars + kQFree, NT);                       // one arrival per row tile
     mbar_init(bars + kJoin, S_::kSoftmax);
     for (int i = 0; i < 8; ++i) s_bad[i] = 0;
     *abort_word = 0u;
@@ -398,8 +408,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       total += s_scan[w];
     }
     teams = total < a.teams ? (int)total : a.teams;     // fewer tiles than teams: one each, the rest idle
-    x0 = team < teams ? total * team / teams : total;
-    x1 = team < teams ? total * (team + 1) / teams : total;
+    x0 = team < teams ? divide(total * team, teams) : total;
+    x1 = team < teams ? divide(total * (team + 1), teams) : total;
     long long at = before + inc - mine;
     if (x0 < x1 && at <= x0 && x0 < at + mine) {        // one thread
       int b = tid * per;
@@ -437,8 +447,41 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     int slot = 0, filled = 0;
     uint32_t parity = 1;                                // a fresh ring's slots count as free
     bool ok = true;
+    uint32_t pieces = 0;
     while (ok && walk.next(p)) {
       const int32_t* table = a.table + p.b * a.table_stride;
+      if (is_v) {
+        // Q rows of the piece -> shared memory, K-major 128-byte-swizzled, each for every copy of its row.
+        // Rows past the last one keep whatever is there: their scores are never looked at.  This warp gets
+        // here while the softmax warps are still busy with the piece before, so the copies (thousands of
+        // cycles behind the key tiles in flight) are under way by the time that Q is free for them.
+        if (pieces > 0) ok = wait_warp(bars + kQFree, (pieces - 1) & 1, abort_word);
+        if (!ok) break;
+        ++pieces;
+        const bool turns = NT == 2 && p.rows <= 128;
+        constexpr int kChunks = D / 8, kRowsAtOnce = 32 / kChunks;
+        const int chunk = lane % kChunks;
+        const T* q = static_cast<const T*>(a.q) + p.b * a.q_b + (int64_t)p.hk * a.G * a.q_h + chunk * 8;
+        for (int row32 = 0; row32 < p.rows; row32 += 32) {
+          const int r = rb * S_::kRows + row32 + lane, node = node_of(a, r);
+          const long long mine = node * a.q_n + (r - node * a.G) * a.q_h;  // where this lane's row starts
+#pragma unroll 4
+          for (int j = 0; j < kChunks; ++j) {
+            const int row = row32 + j * kRowsAtOnce + lane / kChunks;
+            const long long at = __shfl_sync(0xFFFFFFFFu, mine, row & 31);
+            if (row < p.rows) {
+#pragma unroll
+              for (int c = 0; c < (NT == 2 ? 2 : C); ++c) {
+                if (NT == 2 && c == 1 && !turns) break;
+                const int to = (row & 127) + (NT == 2 ? 0 : c * (128 / C));
+                const uint32_t dst = sQ + (NT == 2 ? (row >> 7) + c : 0) * S_::kQTile + (chunk >> 3) * (128 * 128) +
+                                     (to >> 3) * 1024 + (to & 7) * 128 + (((chunk & 7) ^ (to & 7)) << 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(q + at) : "memory");
+              }
+            }
+          }
+        }
+      }
       // the page of this lane's box, looked up a tile ahead
       auto find = [&](int it, int& row) -> int {
         row = tile_key<BN>(p.c, p.t0 + it) + pg * box;
@@ -460,6 +503,12 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
                    row & ((1 << a.page_log) - 1), p.hk, page, a.slot, full + slot * 8);
         row = next_row;
         page = next_page;
+        if (is_v && it == 0) {                          // the first V tile is on its way; now Q has to be there
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bars + kQFull);
+        }
         ++filled;
         if (++slot == stages) { slot = 0; parity ^= 1; }
       }
@@ -528,11 +577,12 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           umma_commit(b_s + buf * 8);
           umma_commit(bars + kKFree + slot * 8);
           if (turns) umma_commit(bars + kKFree + slot * 8);      // for both row tiles
+          if (C == 1 && !turns && it + 1 == p.len) umma_commit(bars + kQFree);
         }
         __syncwarp();
       };
       int it = turns ? s : 0;
-      ok = wait_warp(bars + kQFull + s * 8, n_q++ & 1, abort_word);
+      ok = wait_warp(bars + kQFull, n_q++ & 1, abort_word);
       if (ok && it < p.len) qk(it);
       if (ok && it + step < p.len) qk(it + step);
       for (bool fresh = true; ok && it < p.len; it += step, fresh = false) {
@@ -578,43 +628,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       const int step = turns ? 2 : 1;
       const int r0 = rb * S_::kRows + (turns ? 0 : s * 128);               // first packed row of this tile
       const int rows = min(kCopyRows, p.rows - (turns ? 0 : s * 128));
-      {  // Q rows -> shared memory, K-major 128-byte-swizzled; rows past the last one hold zeros
-        const T* q = static_cast<const T*>(a.q) + p.b * a.q_b + (int64_t)p.hk * a.G * a.q_h;
-        constexpr int kChunks = D / 8;                  // 16-byte chunks per row
-        constexpr int kStep = kChunks / C < 4 ? kChunks / C : 4;
-#pragma unroll 1
-        for (int j0 = 0; j0 < kChunks / C; j0 += kStep) {   // each row is read once and written for every copy
-          uint4 x[kStep];
-#pragma unroll
-          for (int j = 0; j < kStep; ++j) {
-            const int e = (j0 + j) * 128 + t, row = e / kChunks, chunk = e % kChunks;
-            x[j] = make_uint4(0u, 0u, 0u, 0u);
-            if (row < rows) {
-              const int i = (r0 + row) / a.G, g = (r0 + row) - i * a.G;
-              x[j] = *reinterpret_cast<const uint4*>(q + i * a.q_n + g * a.q_h + chunk * 8);
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < kStep; ++j) {
-            const int e = (j0 + j) * 128 + t, chunk = e % kChunks;
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-              const int row = e / kChunks + c * kCopyRows;
-              const uint32_t dst = sQ + s * S_::kQTile + (chunk >> 3) * (128 * 128) + (row >> 3) * 1024 + (row & 7) * 128 +
-                                   (((chunk & 7) ^ (row & 7)) << 4);
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(x[j].x), "r"(x[j].y), "r"(x[j].z),
-                           "r"(x[j].w)
-                           : "memory");
-            }
-          }
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bars + kQFull + s * 8);
-      }
       const bool warp_live = tr - lane < rows, live = tr < rows;
-      const int node = live ? (r0 + tr) / a.G : 0, head = p.hk * a.G + (live ? (r0 + tr) % a.G : 0);
-      const int depth = live ? node_depth(a, p.b, node) : 1;
+      const int node = live ? node_of(a, r0 + tr) : 0, head = p.hk * a.G + (live ? r0 + tr - node * a.G : 0);
+      const int depth = live && a.window > 0 ? node_depth(a, p.b, node) : 1;   // (only windows need it)
       float m_used = -INFINITY, l_run = 0.f;
       int it = turns ? s : 0;
       for (bool fresh = true; it < p.len; it += step, fresh = false) {
@@ -724,9 +740,10 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       // ---- epilogue: a finished unit's rows go to the output, others to the scratch
       // scratch slot 1: the unit's first piece; 0: a later one (then it is the block's first piece)
       const int64_t w0 = ((int64_t)blockIdx.x * 2 + (p.t0 == 0 ? 1 : 0)) * a.rows + (turns ? 0 : s * 128);
-      if (C == 1 && !turns) {
-        const bool bad = s_bad[piece & 7] == piece + 1;
-        const float inv = l_run != 0.f ? 1.f / l_run : 0.f;
+      const long long mine = p.whole ? p.b * a.o_b + node * a.o_n + head * a.o_h : (w0 + tr) * D;
+      const bool bad = s_bad[piece & 7] == piece + 1;
+      if (C == 1 && !turns) {                           // no copies: every thread writes its row
+        const float w = p.whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f;
         if (warp_live) {
 #pragma unroll 1
           for (int c = 0; c < D / 32; ++c) {
@@ -734,6 +751,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             __syncwarp();
             tmem_load(o_col + c * 32, o);
             if (!live) continue;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
             if (bad) {                                  // rare; a copy, so that o stays in registers otherwise
               uint32_t y[32];
 #pragma unroll
@@ -743,102 +762,119 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
               for (int j = 0; j < 32; ++j) o[j] = y[j];
             }
             if (p.whole) {
-              T* op = static_cast<T*>(a.out) + p.b * a.o_b + node * a.o_n + head * a.o_h + c * 32;
+              T* op = static_cast<T*>(a.out) + mine + c * 32;
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                uint32_t w[4];
+                uint32_t v[4];
 #pragma unroll
                 for (int f = 0; f < 4; ++f)
-                  w[f] = Type<T>::pack(__uint_as_float(o[8 * e + 2 * f]) * inv, __uint_as_float(o[8 * e + 2 * f + 1]) * inv);
-                *reinterpret_cast<uint4*>(op + e * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+                  v[f] = Type<T>::pack(__uint_as_float(o[8 * e + 2 * f]), __uint_as_float(o[8 * e + 2 * f + 1]));
+                *reinterpret_cast<uint4*>(op + e * 8) = make_uint4(v[0], v[1], v[2], v[3]);
               }
             } else {
-              float4* wo = reinterpret_cast<float4*>(a.ws_o + (w0 + t) * D + c * 32);
+              float* wo = a.ws_o + mine + c * 32;
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                wo[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
-                                    __uint_as_float(o[4 * e + 3]));
+              for (int e = 0; e < 4; ++e)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(wo + 8 * e), "r"(o[8 * e]),
+                             "r"(o[8 * e + 1]), "r"(o[8 * e + 2]), "r"(o[8 * e + 3]), "r"(o[8 * e + 4]), "r"(o[8 * e + 5]),
+                             "r"(o[8 * e + 6]), "r"(o[8 * e + 7])
+                             : "memory");
             }
           }
         }
-      } else {
-        // Join the copies: maxima and sums, then O a few columns at a time, through the memory of the Q
-        // tile (its last reader, this piece's last S, is done; the next Q comes from these warps).
-        constexpr int kCopies = NT == 2 ? 2 : C, kAll = 128 * NT, kCols = S_::kStage;
-        float2* s_ml = reinterpret_cast<float2*>(smem + kAll * kCols * 4);         // [kAll]
-        auto sync = [&]() -> bool {                     // all softmax warps, with a bounded wait
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bars + kJoin);
-          ok = wait(bars + kJoin, joins++ & 1);
-          return ok;
-        };
+        if (live) {
+          if (!p.whole)
+            *reinterpret_cast<float2*>(a.ws_ml + (w0 + t) * 2) = make_float2(m_used, l_run);
+          else if (a.lse)
+            a.lse[((int64_t)p.b * a.H + head) * a.N + node] = l_run != 0.f ? (m_used + log2f(l_run)) * kLn2 : -INFINITY;
+        }
+        tc_fence_before();                              // O is read: the next piece's P V may overwrite it
+        continue;
+      }
+      // Copies are joined kCols columns at a time through the memory of the Q tile: its last reader, this
+      // piece's last S, is done, and the next Q is let in behind the join.
+      constexpr int kAll = 128 * NT, kCols = S_::kStage, kVecs = kCols / 4;
+      auto stage = [&](int row, int vec) -> unsigned char* {       // 16 bytes; each row tile in its own Q tile
+        return smem + (row >> 7) * S_::kQTile + (row & 127) * (kCols * 4) + ((vec ^ (row & (kVecs - 1))) << 4);
+      };
+      constexpr int copies = NT == 2 ? 2 : C, apart = NT == 2 ? 128 : kCopyRows;
+      const bool lead_copy = tid < apart;
+      float w, top, sum;
+      auto sync = [&]() -> bool {                       // of the warps that share rows, with a bounded wait
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + kJoin);
+        ok = wait(bars + kJoin, joins++ & 1);
+        return ok;
+      };
+      {                                                 // the copies' maxima and sums
+        float2* s_ml = reinterpret_cast<float2*>(smem + 128 * kCols * 4);          // [kAll]
         if (!sync()) break;                             // (NT = 2: the other tile's last S is done too)
         s_ml[tid] = make_float2(m_used, l_run);
         if (!sync()) break;
-        const int first = NT == 2 ? t : tr, apart = NT == 2 ? 128 : kCopyRows;
-        float top = -INFINITY, sum = 0.f;
+        const int mine0 = NT == 2 ? t : tr;
+        top = -INFINITY;
+        sum = 0.f;
 #pragma unroll
-        for (int c = 0; c < kCopies; ++c) top = fmaxf(top, s_ml[first + c * apart].x);
+        for (int c = 0; c < copies; ++c) top = fmaxf(top, s_ml[mine0 + c * apart].x);
 #pragma unroll
-        for (int c = 0; c < kCopies; ++c) {
-          const float2 ml = s_ml[first + c * apart];
+        for (int c = 0; c < copies; ++c) {
+          const float2 ml = s_ml[mine0 + c * apart];
           if (ml.x != -INFINITY) sum += ml.y * ex2(ml.x - top);
         }
-        const bool bad = s_bad[piece & 7] == piece + 1;
-        const bool lead_copy = tid < apart;
-        float w = m_used == -INFINITY ? 0.f : ex2(m_used - top);
-        const float inv = p.whole ? (sum != 0.f ? 1.f / sum : 0.f) : 1.f;
-        w *= inv;
-        if (live && lead_copy) { m_used = top; l_run = sum; }
+        w = m_used == -INFINITY ? 0.f : ex2(m_used - top);
+      }
+      if (p.whole) w *= sum != 0.f ? 1.f / sum : 0.f;
+      // the warps that hold copies of the same 32 rows share them out again: four or eight rows at a time
+      constexpr int kTogether = 32 / kVecs;
+      const int my_copy = NT == 2 ? s : ci, col = lane % kVecs;
 #pragma unroll 1
-        for (int c = 0; c < D / kCols; ++c) {
-          if (c && !sync()) break;
-          if (warp_live) {
-            uint32_t o[kCols];
-            tmem_load(o_col + c * kCols, o);
+      for (int c = 0; c < D / kCols; ++c) {
+        if (warp_live) {
+          uint32_t o[kCols];
+          tmem_load(o_col + c * kCols, o);
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
-            if (bad && lead_copy && live) {
-              uint32_t y[kCols];
+          for (int j = 0; j < kCols; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
+          if (bad && lead_copy && live) {               // rare; a copy, so that o stays in registers otherwise
+            uint32_t y[kCols];
 #pragma unroll
-              for (int j = 0; j < kCols; ++j) y[j] = o[j];
-              add_back<T, BN>(a, p, node, depth, c * kCols, kCols, y);
+            for (int j = 0; j < kCols; ++j) y[j] = o[j];
+            add_back<T, BN>(a, p, node, depth, c * kCols, kCols, y);
 #pragma unroll
-              for (int j = 0; j < kCols; ++j) o[j] = y[j];
-            }
-#pragma unroll
-            for (int e = 0; e < kCols / 4; ++e)
-              *reinterpret_cast<uint4*>(smem + ((size_t)tid * kCols + ((e ^ (lane & (kCols / 4 - 1))) * 4)) * 4) =
-                  make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            for (int j = 0; j < kCols; ++j) o[j] = y[j];
           }
-          if (!sync()) break;
-          for (int e = tid; e < rows * (kCols / 4); e += kAll) {
-            const int row = e / (kCols / 4), col = e % (kCols / 4);
-            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < kCopies; ++k) {
-              const int from = row + k * apart;
-              const float4 z = *reinterpret_cast<const float4*>(smem + ((size_t)from * kCols + ((col ^ (from & (kCols / 4 - 1))) * 4)) * 4);
-              y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
-            }
-            const int d = c * kCols + col * 4;
-            if (p.whole) {
-              const int i = (r0 + row) / a.G, hd = p.hk * a.G + (r0 + row) - i * a.G;
-              *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + p.b * a.o_b + i * a.o_n + hd * a.o_h + d) =
-                  make_uint2(Type<T>::pack(y.x, y.y), Type<T>::pack(y.z, y.w));
-            } else {
-              *reinterpret_cast<float4*>(a.ws_o + (w0 + row) * D + d) = y;
+          for (int e = 0; e < kVecs; ++e)
+            *reinterpret_cast<uint4*>(stage(tid, e)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+        }
+        if (!sync()) break;
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j) {
+          const int row = j * kTogether + lane / kVecs;                    // of this warp's 32
+          const long long at = __shfl_sync(0xFFFFFFFFu, mine, row) + c * kCols + col * 4;
+          if (j % copies == my_copy) {
+            if (tr - lane + row < rows) {
+              float4 y = *reinterpret_cast<const float4*>(stage(tr - lane + row, col));
+#pragma unroll
+              for (int k = 1; k < copies; ++k) {
+                const float4 z = *reinterpret_cast<const float4*>(stage(tr - lane + row + k * apart, col));
+                y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+              }
+              if (p.whole)
+                *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at) = make_uint2(Type<T>::pack(y.x, y.y), Type<T>::pack(y.z, y.w));
+              else
+                *reinterpret_cast<float4*>(a.ws_o + at) = y;
             }
           }
         }
-        if (!ok || !sync()) break;                      // the Q tile's memory is free again
-        if (!lead_copy) { tc_fence_before(); continue; }
+        if (!sync()) break;                             // the stage is free again
       }
-      if (live) {
+      if (!ok) break;
+      if (NT == 2 ? t == 0 : tid < 1) mbar_arrive(bars + kQFree);
+      if (live && lead_copy) {
         if (!p.whole)
-          *reinterpret_cast<float2*>(a.ws_ml + (w0 + tr) * 2) = make_float2(m_used, l_run);
+          *reinterpret_cast<float2*>(a.ws_ml + (w0 + tr) * 2) = make_float2(top, sum);
         else if (a.lse)
-          a.lse[((int64_t)p.b * a.H + head) * a.N + node] = l_run != 0.f ? (m_used + log2f(l_run)) * kLn2 : -INFINITY;
+          a.lse[((int64_t)p.b * a.H + head) * a.N + node] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
       }
       tc_fence_before();                                // O is read: the next piece's P V may overwrite it
     }
@@ -939,7 +975,7 @@ __global__ void __launch_bounds__(256) paged_attention_join_kernel(const __grid_
       }
     }
     if (row >= rows) continue;
-    const int node = (r0 + row) / a.G, head = hk * a.G + (r0 + row) % a.G;
+    const int node = node_of(a, r0 + row), head = hk * a.G + r0 + row - node * a.G;
     const float inv = l != 0.f ? 1.f / l : 0.f;
     uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + b * a.o_b + node * a.o_n + head * a.o_h + lane * E);
 #pragma unroll
@@ -1006,7 +1042,7 @@ Plan plan(int H, int H_kv, int N) {
 }
 size_t workspace_bytes(const Plan& p, int D) {
   const size_t blocks = (size_t)p.teams * p.RB;
-  return blocks * sizeof(int4) + blocks * 2 * p.rows * (D + 2) * sizeof(float);
+  return 32 + (blocks + 1) / 2 * 2 * sizeof(int4) + blocks * 2 * p.rows * (D + 2) * sizeof(float);
 }
 
 template <typename T, int D, int NT, int C>
@@ -1077,7 +1113,8 @@ extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pag
   if (table_cols < 1 || table_stride < table_cols) return REST_INVALID_ARG;
   if (!(scale > 0.f) || !(scale < INFINITY)) return REST_INVALID_ARG;
   if ((D != 64 && D != 128) || N > REST_MAX_N || (H % H_kv) != 0) return REST_UNSUPPORTED;
-  if (page < 16 || page > 256 || (page & (page - 1)) != 0 || (int64_t)table_cols * page > 0x7FFF0000ll || H > 65536)
+  if (page < 16 || page > 256 || (page & (page - 1)) != 0 || (int64_t)table_cols * page > 0x7FFF0000ll ||
+      H > 65536 || H / H_kv > 1024)
     return REST_UNSUPPORTED;
   const int64_t extent[9] = {B, N, H, P, H_kv, page, B, N, H};
   for (int i = 0; i < 9; ++i) {
@@ -1099,12 +1136,13 @@ extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pag
   a.table_stride = table_stride;
   a.B = B; a.H = H; a.H_kv = H_kv; a.G = H / H_kv; a.N = N; a.Wm = (N + 31) / 32; a.P = P; a.table_cols = table_cols;
   a.window = window; a.sinks = sinks; a.teams = pl.teams; a.RB = pl.RB; a.rows = pl.rows;
+  a.g_inverse = (uint32_t)((((u64)1 << 32) + a.G - 1) / a.G);
   a.scale_log2 = scale * kLog2e;
   a.page_log = 4;
   while ((1 << a.page_log) < page) ++a.page_log;
   const size_t blocks = (size_t)pl.teams * pl.RB;
-  a.meta = static_cast<int4*>(d_ws);
-  a.ws_o = reinterpret_cast<float*>(static_cast<char*>(d_ws) + blocks * sizeof(int4));
+  a.meta = reinterpret_cast<int4*>((reinterpret_cast<uintptr_t>(d_ws) + 31) & ~(uintptr_t)31);     // 32-byte stores
+  a.ws_o = reinterpret_cast<float*>(a.meta + (blocks + 1) / 2 * 2);
   a.ws_ml = a.ws_o + blocks * 2 * pl.rows * D;
   const int bn = 64;                                    // keys per tile
   CUtensorMap tm_k, tm_v;

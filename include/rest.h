@@ -484,15 +484,20 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
  *   outputs         as rest_accept; a row without a finite logit gives -1 for the last token
  *   Weights are held as integers of 2^-44 of the row's largest (exact sums in any order: results
  *   never depend on scheduling); a token below 2^-45 of the largest counts as impossible.
+ *   d_ws            optional scratch of rest_accept_sampled_workspace_bytes() bytes, 8-byte aligned
+ *                   (the query answers for the current device and may be 0), not shared by calls
+ *                   that may run at the same time.  Only for speed: with it the rows of few
+ *                   contexts are all worked on at once, without it each context walks row by row.
  *   Limits: V <= 2^18, max_depth <= 16, N <= 256.
  */
+size_t rest_accept_sampled_workspace_bytes(int32_t B, int32_t N);
 rest_status rest_accept_sampled(const void* d_logits, int32_t dtype, int64_t ctx_stride,
                                 int64_t row_stride, int32_t V, const int32_t* d_tokens,
                                 const int32_t* d_parents, const int32_t* d_n_nodes,
                                 const float* d_uniforms, const float* d_temperature,
                                 const float* d_top_p, int32_t B, int32_t N, int32_t max_depth,
                                 int32_t* d_accept_len, int32_t* d_accept_nodes, int32_t* d_out_tokens,
-                                void* stream);
+                                void* d_ws, size_t ws_bytes, void* stream);
 
 /*
  * rest_suffix_array_build - the datastore's suffix array, built on the device (Sec. 3.2

@@ -44,7 +44,8 @@ EXPORTS = (
     "rest_suffix_array_workspace_bytes", "rest_suffix_array_min_workspace_bytes",
     "rest_suffix_array_build", "rest_suffix_array_build_in_groups", "rest_suffix_array_build_full",
     "rest_suffix_array_append_workspace_bytes", "rest_suffix_array_append", "rest_tree_attention_plan",
-    "rest_paged_attention_workspace_bytes", "rest_paged_attention", "rest_accept_sampled",
+    "rest_paged_attention_workspace_bytes", "rest_paged_attention", "rest_accept_sampled_workspace_bytes",
+    "rest_accept_sampled",
     "rest_paged_kv_write", "rest_paged_kv_commit", "rest_pages_fork", "rest_pages_copy",
     "rest_pages_reserve", "rest_pages_release",
     "rest_accept", "rest_status_string", "rest_last_cuda_error", "rest_launch_count",
@@ -120,7 +121,9 @@ def lib():
     L.rest_paged_attention.argtypes = [vp, vp, vp, ctypes.POINTER(i64), i32, i32, i32, vp, i64, i32, vp, vp, vp, i32,
                                        i32, i32, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, sz, vp]
     L.rest_accept_sampled.restype = i32
-    L.rest_accept_sampled.argtypes = [vp, i32, i64, i64, i32] + [vp] * 6 + [i32, i32, i32] + [vp] * 4
+    L.rest_accept_sampled.argtypes = [vp, i32, i64, i64, i32] + [vp] * 6 + [i32, i32, i32] + [vp] * 4 + [sz, vp]
+    L.rest_accept_sampled_workspace_bytes.restype = sz
+    L.rest_accept_sampled_workspace_bytes.argtypes = [i32, i32]
     pool = [vp, vp, ctypes.POINTER(i64), i32, i32]           # K, V, strides, pages, rows per page
     table = [vp, i64, i32]                                   # block table, row stride, columns
     L.rest_paged_kv_write.restype = i32
@@ -482,46 +485,70 @@ def rest_kv_commit(k, v, kv_len, accept_nodes, accept_len, N, new_kv_len=None, s
 
 
 # ------------------------------------------------------------------------------ cache in pages
-def _same_device(first, *others):
-    """All tensors of a call sit on one CUDA device; the call runs there whatever the current one is."""
+# These calls are made many times per decoding step, so their checks go through few, cheap tensor
+# queries: get_device() says both that a tensor is on a GPU (-1: it is not) and on which.
+_I64x3 = ctypes.c_int64 * 3
+_I64x9 = ctypes.c_int64 * 9
+
+
+def _call(fn, what, index, stream, *args):
+    """fn(*args, stream) on GPU `index`, whatever the current device is; raises on an error status."""
     import torch
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise RestError("all tensors of a call must be on the same CUDA device")
-    return torch.cuda.device(first.device)
+    if index < 0:
+        raise RestError(f"{what}: the tensors must be on a CUDA device")
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return _call(fn, what, index, stream, *args)
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(index)
+    else:
+        raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    rc = fn(*args, raw)
+    if rc:
+        _check(rc, what)
 
 
-def _dev_vec(t, name, n=None, dtype=None):
-    """A contiguous CUDA vector (int32 unless told otherwise) of n elements."""
+def _vec(t, name, index, n=None, dtype=None):
+    """Pointer of a contiguous vector (int32 unless told otherwise) of n elements on GPU `index`."""
     import torch
     dtype = torch.int32 if dtype is None else dtype
-    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.dim() == 1 and (n is None or t.numel() == n)):
-        raise RestError(f"{name} must be a contiguous {str(dtype).split('.')[-1]} CUDA vector"
-                        + ("" if n is None else f" of {n} elements"))
-    return t
+    if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous() or t.dim() != 1 or (
+            n is not None and t.numel() != n):
+        raise RestError(f"{name} must be a contiguous {str(dtype).split('.')[-1]} vector"
+                        + ("" if n is None else f" of {n} elements") + " on the same CUDA device as the others")
+    return t.data_ptr()
+
+
+def _array(t, name, index, shape, dtype):
+    """Pointer of a contiguous tensor of that shape and type on GPU `index`."""
+    if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous() or t.shape != shape:
+        raise RestError(f"{name} must be a contiguous {str(dtype).split('.')[-1]} tensor {list(shape)} on the same "
+                        "CUDA device as the others")
+    return t.data_ptr()
 
 
 def _pool(k_pages, v_pages):
-    """Pointers, strides, pages and rows per page of a pool [P, H_kv, page, D]."""
+    """Device, shape, and (pointers, strides, pages, rows per page) of a pool [P, H_kv, page, D]."""
     import torch
-    for t, nm in ((k_pages, "k_pages"), (v_pages, "v_pages")):
-        if not (t.is_cuda and t.dtype in (torch.bfloat16, torch.float16) and t.dim() == 4 and t.stride(-1) == 1):
-            raise RestError(f"{nm} must be a bf16 or fp16 CUDA tensor [P, H_kv, page, D] with a contiguous last "
-                            "dimension")
-    if k_pages.stride() != v_pages.stride() or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
-        raise RestError("k_pages and v_pages must have the same shape, strides and type")
-    strides = (ctypes.c_int64 * 3)(*k_pages.stride()[:3])
-    return [k_pages.data_ptr(), v_pages.data_ptr(), strides, k_pages.shape[0], k_pages.shape[2]]
+    index, shape, strides, dtype = k_pages.get_device(), k_pages.shape, k_pages.stride(), k_pages.dtype
+    if len(shape) != 4 or strides[3] != 1 or not (dtype is torch.bfloat16 or dtype is torch.float16):
+        raise RestError("k_pages must be a bf16 or fp16 tensor [P, H_kv, page, D] with a contiguous last dimension")
+    if v_pages.stride() != strides or v_pages.shape != shape or v_pages.dtype is not dtype or v_pages.get_device() != index:
+        raise RestError("k_pages and v_pages must have the same shape, strides, type and device")
+    return index, shape, (k_pages.data_ptr(), v_pages.data_ptr(), _I64x3(*strides[:3]), shape[0], shape[2])
 
 
-def _table(table, B=None):
+def _table(table, index, B=None):
+    """Pointer, row stride and columns of a block table."""
     import torch
-    if not (table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.stride(1) == 1
-            and (B is None or table.shape[0] == B)):
-        raise RestError("block_table must be an int32 CUDA tensor [B, columns] with contiguous rows")
+    shape = table.shape
+    if table.dtype is not torch.int32 or table.get_device() != index or len(shape) != 2 or table.stride(1) != 1 or (
+            B is not None and shape[0] != B):
+        raise RestError("block_table must be an int32 tensor [B, columns] with contiguous rows on the same CUDA device "
+                        "as the others")
+    stride = table.stride(0)
     # a single row may come with any stride; the library wants rows that do not overlap
-    stride = table.stride(0) if table.shape[0] > 1 else max(table.stride(0), table.shape[1])
-    return [table.data_ptr(), stride, table.shape[1]]
+    return table.data_ptr(), stride if shape[0] > 1 else max(stride, shape[1]), shape[1]
 
 
 def paged_attention_workspace_bytes(B, H, H_kv, N, D) -> int:
@@ -536,76 +563,80 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
     mask: words int32 [B,N,ceil(N/32)] as rest_draft writes them, None: node i sees nodes 0..i.
     window > 0: a node sees the last `window` positions up to its own and the first `sinks` ones.
     n_nodes int32[B]: later rows do not exist (their out / lse rows stay as they were).
-    lse: optional float32 [B,H,N].  Returns out [B,N,H,D]."""
+    lse: optional float32 [B,H,N].  workspace: a uint8 tensor of paged_attention_workspace_bytes(),
+    not shared by calls that may overlap; None: one is allocated.  Returns out [B,N,H,D]."""
     import torch
-    L = lib()
-    B, N, H, D = q.shape
-    if not (q.is_cuda and q.dtype == k_pages.dtype and q.stride(-1) == 1):
-        raise RestError("q must be a CUDA tensor of the pages' type with a contiguous last dimension")
-    pool, table = _pool(k_pages, v_pages), _table(block_table, B)
-    if k_pages.shape[3] != D:
-        raise RestError("q and the pages differ in head size")
-    _dev_vec(kv_len, "kv_len", B)
+    L = _lib or lib()
+    index, (P, H_kv, page, Dk), pool = _pool(k_pages, v_pages)
+    dtype, shape, qs = q.dtype, q.shape, q.stride()
+    if len(shape) != 4 or qs[3] != 1 or dtype is not k_pages.dtype or shape[3] != Dk or q.get_device() != index:
+        raise RestError("q must be [B,N,H,D] with a contiguous last dimension, of the pages' type, head size and device")
+    B, N, H, D = shape
+    table = _table(block_table, index, B)
+    mask_ptr = lse_ptr = nodes_ptr = ws_ptr = ws_bytes = 0
+    if mask is not None:
+        if mask.element_size() != 4 or mask.get_device() != index or not mask.is_contiguous() or (
+                mask.shape != (B, N, (N + 31) // 32)):
+            raise RestError("mask must be a contiguous 32-bit tensor [B,N,ceil(N/32)] on the same CUDA device")
+        mask_ptr = mask.data_ptr()
     if n_nodes is not None:
-        _dev_vec(n_nodes, "n_nodes", B)
-    if mask is not None and not (mask.is_cuda and mask.is_contiguous() and mask.element_size() == 4
-                                 and mask.shape == (B, N, (N + 31) // 32)):
-        raise RestError("mask must be a contiguous 32-bit CUDA tensor [B,N,ceil(N/32)]")
-    if lse is not None and not (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous()
-                                and lse.shape == (B, H, N)):
-        raise RestError("lse must be a contiguous float32 CUDA tensor [B,H,N]")
+        nodes_ptr = _vec(n_nodes, "n_nodes", index, B)
+    if lse is not None:
+        lse_ptr = _array(lse, "lse", index, (B, H, N), torch.float32)
     if out is None:
-        out = (torch.empty if n_nodes is None else torch.zeros)((B, N, H, D), dtype=q.dtype, device=q.device)
-    elif not (out.is_cuda and out.dtype == q.dtype and out.shape == q.shape and out.stride(-1) == 1):
-        raise RestError("out must be a CUDA tensor like q with a contiguous last dimension")
-    with _same_device(q, k_pages, v_pages, block_table, kv_len, mask, n_nodes, out, lse, workspace):
-        need = L.rest_paged_attention_workspace_bytes(B, H, k_pages.shape[1], N, D)
-        if need and workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        strides = (ctypes.c_int64 * 9)(*q.stride()[:3], *k_pages.stride()[:3], *out.stride()[:3])
-        rc = L.rest_paged_attention(
-            q.data_ptr(), *pool[:2], strides, REST_BF16 if q.dtype == torch.bfloat16 else REST_FP16, *pool[3:], *table,
-            kv_len.data_ptr(), _ptr(n_nodes), _ptr(mask), B, H, k_pages.shape[1], N, D, int(window), int(sinks),
-            float(scale), out.data_ptr(), _ptr(lse), _ptr(workspace),
-            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
-    _check(rc, "rest_paged_attention")
+        out = (torch.empty if n_nodes is None else torch.zeros)(shape, dtype=dtype, device=q.device)
+    elif out.dtype is not dtype or out.shape != shape or out.stride(3) != 1 or out.get_device() != index:
+        raise RestError("out must be a tensor like q with a contiguous last dimension")
+    if workspace is None:
+        if torch.cuda.current_device() != index:          # the size goes by the device
+            with torch.cuda.device(index):
+                need = L.rest_paged_attention_workspace_bytes(B, H, H_kv, N, D)
+        else:
+            need = L.rest_paged_attention_workspace_bytes(B, H, H_kv, N, D)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise RestError("workspace must be a contiguous tensor on the same CUDA device")
+    if workspace is not None:
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    strides = _I64x9(*qs[:3], *pool[2], *out.stride()[:3])
+    _call(L.rest_paged_attention, "rest_paged_attention", index, stream, q.data_ptr(), pool[0], pool[1], strides,
+          REST_BF16 if dtype is torch.bfloat16 else REST_FP16, P, page, *table, _vec(kv_len, "kv_len", index, B),
+          nodes_ptr, mask_ptr, B, H, H_kv, N, D, window, sinks, scale, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes)
     return out
 
 
 def rest_accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature, top_p, max_depth, out=None,
-                        stream=None):
+                        stream=None, workspace=None):
     """Acceptance of draft trees against the verifier's probabilities: logits [B,N+1,V] (bf16, fp16
     or fp32; slot 0 after the prefix, slot i+1 after node i), uniforms float32 [B,N+1] in [0, 1),
-    temperature and top_p float32 [B].  Returns (accept_len, accept_nodes, out_tokens) like
-    rest_accept."""
+    temperature and top_p float32 [B].  workspace: a uint8 tensor of
+    rest_accept_sampled_workspace_bytes() bytes, not shared by calls that may overlap; None: one is
+    allocated when the library asks for it; False: none (each context walks row by row).  Returns
+    (accept_len, accept_nodes, out_tokens) like rest_accept."""
     import torch
-    L = lib()
-    types = {torch.bfloat16: REST_BF16, torch.float16: REST_FP16, torch.float32: REST_FP32}
-    for t, nm in ((tokens, "tokens"), (parents, "parents")):
-        _dev_i32(t, nm)
-    B, N = tokens.shape
-    if not (logits.is_cuda and logits.dtype in types and logits.dim() == 3 and logits.shape[:2] == (B, N + 1)
-            and logits.stride(2) == 1):
-        raise RestError("logits must be a bf16, fp16 or fp32 CUDA tensor [B,N+1,V] with contiguous rows")
-    if parents.shape != (B, N):
-        raise RestError("parents must be [B,N] like tokens")
-    _dev_vec(n_nodes, "n_nodes", B)
-    if not (uniforms.is_cuda and uniforms.dtype == torch.float32 and uniforms.is_contiguous()
-            and uniforms.shape == (B, N + 1)):
-        raise RestError("uniforms must be a contiguous float32 CUDA tensor [B,N+1]")
-    _dev_vec(temperature, "temperature", B, torch.float32), _dev_vec(top_p, "top_p", B, torch.float32)
+    L = _lib or lib()
+    index, (B, N), i32, f32 = tokens.get_device(), tokens.shape, torch.int32, torch.float32
+    dtype, shape, ls = logits.dtype, logits.shape, logits.stride()
+    kind = {torch.bfloat16: REST_BF16, torch.float16: REST_FP16, f32: REST_FP32}.get(dtype)
+    if kind is None or len(shape) != 3 or shape[0] != B or shape[1] != N + 1 or ls[2] != 1 or logits.get_device() != index:
+        raise RestError("logits must be a bf16, fp16 or fp32 tensor [B,N+1,V] with contiguous rows on the same CUDA device")
     if out is None:
-        i32 = dict(dtype=torch.int32, device=tokens.device)
-        out = (torch.empty(B, **i32), torch.empty((B, max_depth), **i32), torch.empty((B, max_depth + 1), **i32))
-    for t, nm, shape in zip(out, ("accept_len", "accept_nodes", "out_tokens"), ((B,), (B, max_depth), (B, max_depth + 1))):
-        if _dev_i32(t, nm).shape != shape:
-            raise RestError(f"{nm} must be {list(shape)}")
-    with _same_device(logits, tokens, parents, n_nodes, uniforms, temperature, top_p, *out):
-        rc = L.rest_accept_sampled(logits.data_ptr(), types[logits.dtype], logits.stride(0), logits.stride(1),
-                                   logits.shape[2], tokens.data_ptr(), parents.data_ptr(), n_nodes.data_ptr(),
-                                   uniforms.data_ptr(), temperature.data_ptr(), top_p.data_ptr(), B, N, max_depth,
-                                   out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), _stream(stream))
-    _check(rc, "rest_accept_sampled")
+        out = (torch.empty(B, dtype=i32, device=tokens.device), torch.empty((B, max_depth), dtype=i32, device=tokens.device),
+               torch.empty((B, max_depth + 1), dtype=i32, device=tokens.device))
+    ws_ptr = ws_bytes = 0
+    if workspace is None:
+        need = L.rest_accept_sampled_workspace_bytes(B, N)
+        workspace = torch.empty(need, dtype=torch.uint8, device=tokens.device) if need else False
+    if workspace is not False:
+        if workspace.get_device() != index or not workspace.is_contiguous():
+            raise RestError("workspace must be a contiguous tensor on the same CUDA device")
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _call(L.rest_accept_sampled, "rest_accept_sampled", index, stream, logits.data_ptr(), kind, ls[0], ls[1], shape[2],
+          _array(tokens, "tokens", index, (B, N), i32), _array(parents, "parents", index, (B, N), i32),
+          _vec(n_nodes, "n_nodes", index, B), _array(uniforms, "uniforms", index, (B, N + 1), f32),
+          _vec(temperature, "temperature", index, B, f32), _vec(top_p, "top_p", index, B, f32), B, N, max_depth,
+          _vec(out[0], "accept_len", index, B), _array(out[1], "accept_nodes", index, (B, max_depth), i32),
+          _array(out[2], "out_tokens", index, (B, max_depth + 1), i32), ws_ptr, ws_bytes)
     return out
 
 
@@ -613,35 +644,31 @@ def rest_paged_kv_write(k_pages, v_pages, block_table, kv_len, k_new, v_new, n_n
     """Writes new K/V rows k_new, v_new [B,N,H_kv,D] as rows kv_len[b] + i of the contexts' pages
     (k_pages, v_pages [P,H_kv,page,D] with any 16-byte strides); with n_nodes int32[B] only rows
     i < n_nodes[b].  Rows whose page does not exist are left out."""
-    B, N, H_kv, D = k_new.shape
-    pool, table = _pool(k_pages, v_pages), _table(block_table, B)
-    for t, nm in ((k_new, "k_new"), (v_new, "v_new")):
-        if not (t.is_cuda and t.dtype == k_pages.dtype and t.stride(-1) == 1):
-            raise RestError(f"{nm} must be a CUDA tensor of the pages' type with a contiguous last dimension")
-    if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or (H_kv, D) != (k_pages.shape[1], k_pages.shape[3]):
-        raise RestError("k_new and v_new must be [B,N,H_kv,D] of the pages' heads, with the same strides")
-    _dev_vec(kv_len, "kv_len", B)
-    if n_nodes is not None:
-        _dev_vec(n_nodes, "n_nodes", B)
-    strides = (ctypes.c_int64 * 3)(*k_new.stride()[:3])
-    with _same_device(k_pages, v_pages, block_table, kv_len, k_new, v_new, n_nodes):
-        _check(lib().rest_paged_kv_write(*pool, *table, kv_len.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), strides,
-                                         _ptr(n_nodes), B, H_kv, N, D, _stream(stream)), "rest_paged_kv_write")
+    index, (P, H_kv, page, D), pool = _pool(k_pages, v_pages)
+    shape, ns = k_new.shape, k_new.stride()
+    if len(shape) != 4 or shape[2] != H_kv or shape[3] != D or ns[3] != 1 or k_new.dtype is not k_pages.dtype or (
+            k_new.get_device() != index):
+        raise RestError("k_new must be [B,N,H_kv,D] of the pages' heads, type and device, with a contiguous last dimension")
+    if v_new.shape != shape or v_new.stride() != ns or v_new.dtype is not k_new.dtype or v_new.get_device() != index:
+        raise RestError("k_new and v_new must have the same shape, strides, type and device")
+    B, N = shape[0], shape[1]
+    _call((_lib or lib()).rest_paged_kv_write, "rest_paged_kv_write", index, stream, *pool, *_table(block_table, index, B),
+          _vec(kv_len, "kv_len", index, B), k_new.data_ptr(), v_new.data_ptr(), _I64x3(*ns[:3]),
+          0 if n_nodes is None else _vec(n_nodes, "n_nodes", index, B), B, H_kv, N, D)
 
 
 def rest_paged_kv_commit(k_pages, v_pages, block_table, kv_len, accept_nodes, accept_len, N, new_kv_len=None,
                          stream=None):
     """rest_kv_commit over pages: row kv_len[b] + accept_nodes[b][i] moves to row kv_len[b] + i.
     new_kv_len (optional int32[B], may be kv_len itself) receives kv_len + accept_len."""
-    _dev_i32(accept_nodes, "accept_nodes")
+    import torch
+    index, (P, H_kv, page, D), pool = _pool(k_pages, v_pages)
     B, max_depth = accept_nodes.shape
-    pool, table = _pool(k_pages, v_pages), _table(block_table, B)
-    for t, nm in ((kv_len, "kv_len"), (accept_len, "accept_len")) + (((new_kv_len, "new_kv_len"),) if new_kv_len is not None else ()):
-        _dev_vec(t, nm, B)
-    with _same_device(k_pages, v_pages, block_table, kv_len, accept_nodes, accept_len, new_kv_len):
-        _check(lib().rest_paged_kv_commit(*pool, *table, kv_len.data_ptr(), accept_nodes.data_ptr(),
-                                          accept_len.data_ptr(), B, k_pages.shape[1], N, k_pages.shape[3], max_depth,
-                                          _ptr(new_kv_len), _stream(stream)), "rest_paged_kv_commit")
+    _call((_lib or lib()).rest_paged_kv_commit, "rest_paged_kv_commit", index, stream, *pool,
+          *_table(block_table, index, B), _vec(kv_len, "kv_len", index, B),
+          _array(accept_nodes, "accept_nodes", index, (B, max_depth), torch.int32),
+          _vec(accept_len, "accept_len", index, B), B, H_kv, N, D, max_depth,
+          0 if new_kv_len is None else _vec(new_kv_len, "new_kv_len", index, B))
     return new_kv_len
 
 
@@ -651,56 +678,44 @@ def rest_pages_fork(refs, block_table, n_pages, kv_len, parents, children, page,
     page is replaced by a page of the child's own.  Returns (copy_src, copy_dst, status) int32[F]:
     the pages to copy with rest_pages_copy in every layer (-1: none), and REST_CTX_* codes."""
     import torch
-    F, B = parents.numel(), block_table.shape[0]
-    table = _table(block_table)
-    for t, nm, n in ((refs, "refs", None), (n_pages, "n_pages", B), (kv_len, "kv_len", B), (parents, "parents", F),
-                     (children, "children", F)):
-        _dev_vec(t, nm, n)
-    out = [torch.empty(F, dtype=torch.int32, device=refs.device) if t is None else _dev_vec(t, nm, F)
-           for t, nm in ((copy_src, "copy_src"), (copy_dst, "copy_dst"), (status, "status"))]
-    with _same_device(refs, block_table, n_pages, kv_len, parents, children, *out):
-        _check(lib().rest_pages_fork(refs.data_ptr(), refs.numel(), *table, n_pages.data_ptr(), kv_len.data_ptr(), B,
-                                     page, parents.data_ptr(), children.data_ptr(), F, *(t.data_ptr() for t in out),
-                                     _stream(stream)), "rest_pages_fork")
-    return tuple(out)
+    F, B, index = parents.numel(), block_table.shape[0], refs.get_device()
+    out = tuple(torch.empty(F, dtype=torch.int32, device=refs.device) if t is None else t
+                for t in (copy_src, copy_dst, status))
+    _call((_lib or lib()).rest_pages_fork, "rest_pages_fork", index, stream, _vec(refs, "refs", index), refs.numel(),
+          *_table(block_table, index), _vec(n_pages, "n_pages", index, B), _vec(kv_len, "kv_len", index, B), B, page,
+          _vec(parents, "parents", index, F), _vec(children, "children", index, F), F, _vec(out[0], "copy_src", index, F),
+          _vec(out[1], "copy_dst", index, F), _vec(out[2], "status", index, F))
+    return out
 
 
 def rest_pages_copy(k_pages, v_pages, src, dst, stream=None):
     """Page dst[i] of K and V becomes a copy of page src[i] (entries outside the pool: left out)."""
+    index, shape, pool = _pool(k_pages, v_pages)
     n = src.numel()
-    _dev_vec(src, "src"), _dev_vec(dst, "dst", n)
-    with _same_device(k_pages, v_pages, src, dst):
-        _check(lib().rest_pages_copy(*_pool(k_pages, v_pages), k_pages.shape[1], k_pages.shape[3], src.data_ptr(),
-                                     dst.data_ptr(), n, _stream(stream)), "rest_pages_copy")
+    _call((_lib or lib()).rest_pages_copy, "rest_pages_copy", index, stream, *pool, shape[1], shape[3],
+          _vec(src, "src", index), _vec(dst, "dst", index, n), n)
 
 
 def rest_pages_reserve(refs, block_table, n_pages, need_len, page, status=None, stream=None):
     """Gives every context pages until its table holds need_len[b] rows, all or none.  Returns
     status int32[B] (REST_CTX_*)."""
     import torch
-    B = block_table.shape[0]
-    table = _table(block_table)
-    for t, nm, n in ((refs, "refs", None), (n_pages, "n_pages", B), (need_len, "need_len", B)):
-        _dev_vec(t, nm, n)
-    status = torch.empty(B, dtype=torch.int32, device=refs.device) if status is None else _dev_vec(status, "status", B)
-    with _same_device(refs, block_table, n_pages, need_len, status):
-        _check(lib().rest_pages_reserve(refs.data_ptr(), refs.numel(), *table, n_pages.data_ptr(),
-                                        need_len.data_ptr(), B, page, status.data_ptr(), _stream(stream)),
-               "rest_pages_reserve")
+    B, index = block_table.shape[0], refs.get_device()
+    if status is None:
+        status = torch.empty(B, dtype=torch.int32, device=refs.device)
+    _call((_lib or lib()).rest_pages_reserve, "rest_pages_reserve", index, stream, _vec(refs, "refs", index),
+          refs.numel(), *_table(block_table, index), _vec(n_pages, "n_pages", index, B),
+          _vec(need_len, "need_len", index, B), B, page, _vec(status, "status", index, B))
     return status
 
 
 def rest_pages_release(refs, block_table, n_pages, keep_len, page, window=0, sinks=0, stream=None):
     """Gives back the pages beyond each context's first keep_len[b] rows and, with a window, those
     no later token sees.  keep_len[b] < 0 leaves a context as it is."""
-    B = block_table.shape[0]
-    table = _table(block_table)
-    for t, nm, n in ((refs, "refs", None), (n_pages, "n_pages", B), (keep_len, "keep_len", B)):
-        _dev_vec(t, nm, n)
-    with _same_device(refs, block_table, n_pages, keep_len):
-        _check(lib().rest_pages_release(refs.data_ptr(), refs.numel(), *table, n_pages.data_ptr(),
-                                        keep_len.data_ptr(), B, page, window, sinks, _stream(stream)),
-               "rest_pages_release")
+    B, index = block_table.shape[0], refs.get_device()
+    _call((_lib or lib()).rest_pages_release, "rest_pages_release", index, stream, _vec(refs, "refs", index),
+          refs.numel(), *_table(block_table, index), _vec(n_pages, "n_pages", index, B),
+          _vec(keep_len, "keep_len", index, B), B, page, window, sinks)
 
 
 def dependent_read_latency_ns(table_bytes: int = 1 << 30, steps: int = 4096, device=None, seed: int = 1) -> float:

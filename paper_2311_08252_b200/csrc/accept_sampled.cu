@@ -1,5 +1,24 @@
 // rest_accept_sampled: draft acceptance against the verifier's probabilities (Sec. 4.1 "Sampling
-// strategies": temperature, nucleus).  One block per context walks from the root, row by row.
+// strategies": temperature, nucleus).
+//
+// One block works on one row of logits at a time and says where a walk that reaches that row goes:
+// to a child, or to an end with a drawn token.  Its steps:
+//   1. the row into shared memory (larger ones are read again from L2), and its largest logit;
+//   2. every token's weight as an integer of 2^-44 of the largest, their exact sum, and a histogram
+//      of the weights over bins of 1/16 in log2 (approximate, 13 bits a token);
+//   3. with a nucleus: the bin in which the sum reaches its target, found in the histogram and checked
+//      with exact sums; the tokens of that bin (some hundred) are ordered against one another;
+//   4. the children of the row's node in index order;
+//   5. if none is accepted: the drawn token, by sums over the tokens in order.
+// Integer sums are exact, so the result depends neither on the order of addition nor on the number of
+// threads; weights are computed in 64 bits (error about 4e-11 of each, where 32 bits would move the
+// borders between neighbouring tokens often enough to be seen in a large batch).
+//
+// A walk visits 1 + accepted rows of N + 1.  Either one block per context walks, a row after the
+// other, reading only those rows; or, when the rows of all contexts are few enough to run at once,
+// every row gets a block of its own and a second small kernel follows the outcomes.  Bound: a row of
+// 32000 takes about 10 double-precision instructions a token for the sums (64 lanes an SM), more than
+// its bytes take; a walk is a chain of such rows.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -12,8 +31,11 @@
 namespace {
 
 typedef unsigned long long u64;
-constexpr int kThreads = 1024;
-constexpr double kOne = 17592186044416.0;      // 2^44: the weight of a row's largest logit
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr u64 kOne = 1ull << 44;                // the weight of a row's largest logit
+constexpr int kBins = 45 * 16 + 1;              // bins of 1/16 in log2, down to 2^-45
+constexpr int kList = 1024;                     // tokens of one bin that are ordered pairwise
+constexpr size_t kRowBytes = 200 * 1024;        // longest row kept in shared memory
 
 struct Args {
   const void* logits;
@@ -21,189 +43,527 @@ struct Args {
   const int32_t *tokens, *parents, *n_nodes;
   const float *uniforms, *temperature, *top_p;
   int32_t *accept_len, *accept_nodes, *out_tokens;
+  int2* outcome;                                // [B][N + 1] {child or -1, token} when every row has a block
   int V, N, max_depth;
 };
 
-template <typename T> __device__ __forceinline__ float load(const T* p, int v) { return (float)p[v] + 0.f; }
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// order-preserving integer of a logit; NaN and -infinity are 0 (impossible)
+// order-preserving integer of a logit (-0 counts as 0); NaN and -infinity are 0 (impossible)
 __device__ __forceinline__ uint32_t key_of(float x) {
   if (!(x > -INFINITY)) return 0u;
-  const uint32_t b = __float_as_uint(x);
+  const uint32_t b = __float_as_uint(x + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-
-struct Row { float top; double inv_t; uint32_t cut_key; int cut_tie; bool greedy; };
-
-// weight of logit x in 2^-44 of the largest, before the nucleus cut
-__device__ __forceinline__ u64 weight(const Row& r, float x) {
-  if (!(x > -INFINITY)) return 0ull;
-  if (x == r.top) return (u64)kOne;
-  if (r.greedy) return 0ull;
-  return __double2ull_rn(exp(((double)x - (double)r.top) * r.inv_t) * kOne);
-}
-__device__ __forceinline__ bool kept(const Row& r, uint32_t key, int v) {
-  return key > r.cut_key || (key == r.cut_key && v <= r.cut_tie);
+__device__ __forceinline__ float of_key(uint32_t k) {
+  return k == 0 ? -INFINITY : __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
 
-__device__ u64 block_sum(u64 x, u64* s) {
+struct Shared {
+  double pow16[16];                             // 2^(j/16)
+  u64 sum[kWarps], sum2[kWarps], left, above, bin_mass, seg_before;
+  u64 w[kList];
+  uint32_t key[kList];
+  int idx[kList];
+  uint32_t hist[kBins];
+  uint32_t red[kWarps], cut_key;
+  int cut_tie, bin, n_list, child, n_refused, refused[REST_MAX_N], token, seg, depth;
+};
+
+// A row's scale: y = log2 of a token's weight = (x - top) * c
+struct Row {
+  float top;
+  double c, top_d;
+  bool greedy, inf;
+};
+
+// log2 weight in sixteenths, rounded (monotonic in x), and the rest of y
+__device__ __forceinline__ bool split(const Row& r, float x, int& k, double& f) {
+  if (!(x > -INFINITY)) return false;
+  // float -> double by its bits (a conversion instruction runs at a quarter of the rate); denormals
+  // and zero come out as some 1e-38
+  const uint32_t b = __float_as_uint(x);
+  const double d = __hiloint2double((int)(((b & 0x7FFFFFFFu) >> 3) + 0x38000000u | (b & 0x80000000u)), (int)(b << 29));
+  const double y = (d - r.top_d) * r.c;         // exactly 0 for the largest, whatever the temperature
+  if (!(y >= -45.0)) return false;
+  constexpr double kMagic = 6755399441055744.0 / 16.0;       // 1.5 * 2^48: adding it rounds to 1/16
+  const double t = y + kMagic;
+  k = __double2loint(t);
+  f = y - (t - kMagic);
+  return true;
+}
+// 2^44 * 2^(k/16 + f), |f| <= 1/32: the table and the Taylor series of 2^f to the fourth power (the
+// fifth is 4e-11), rounded to an integer by adding 2^52
+__device__ __forceinline__ u64 weight_of(const Shared& sh, int k, double f) {
+  constexpr double a1 = 0.6931471805599453, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4;
+  const double t = sh.pow16[k & 15];
+  const double scaled = __hiloint2double(__double2hiint(t) + (((k >> 4) + 44) << 20), __double2loint(t));
+  double p = fma(f, a4, a3);
+  p = fma(f, p, a2);
+  p = fma(f, p, a1);
+  p = fma(f, p, 1.0);
+  return (u64)__double_as_longlong(fma(p, scaled, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+}
+// weight before the nucleus cut (see Row): an infinite logit takes all of the mass
+__device__ __forceinline__ u64 weight(const Shared& sh, const Row& r, float x) {
+  if (r.inf || r.greedy) return x == r.top ? kOne : 0ull;
+  int k;
+  double f;
+  return split(r, x, k, f) ? weight_of(sh, k, f) : 0ull;
+}
+
+__device__ __forceinline__ u64 warp_sum(u64 x) {
+#pragma unroll
   for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+  return x;
+}
+__device__ __forceinline__ u64 warp_scan(u64 x) {     // inclusive
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const u64 y = __shfl_up_sync(0xFFFFFFFFu, x, d);
+    if ((int)(threadIdx.x & 31) >= d) x += y;
+  }
+  return x;
+}
+// sums over the block of two values, for every thread
+__device__ __forceinline__ void block_sum2(Shared& sh, u64& x, u64& y) {
+  x = warp_sum(x);
+  y = warp_sum(y);
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
+  if ((threadIdx.x & 31) == 0) { sh.sum[threadIdx.x >> 5] = x; sh.sum2[threadIdx.x >> 5] = y; }
   __syncthreads();
-  u64 t = 0;
-  for (int w = 0; w < kThreads / 32; ++w) t += s[w];
-  return t;
+  x = warp_sum(sh.sum[threadIdx.x & 31]);
+  y = warp_sum(sh.sum2[threadIdx.x & 31]);
+}
+__device__ __forceinline__ u64 block_sum(Shared& sh, u64 x) {
+  u64 zero = 0;
+  block_sum2(sh, x, zero);
+  return x;
+}
+// inclusive prefix sum over the block's threads
+__device__ __forceinline__ u64 block_scan(Shared& sh, u64 x) {
+  x = warp_scan(x);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 31) sh.sum[threadIdx.x >> 5] = x;
+  __syncthreads();
+  const u64 upto = warp_scan(sh.sum[threadIdx.x & 31]);
+  const int warp = threadIdx.x >> 5;
+  const u64 before = __shfl_sync(0xFFFFFFFFu, upto, warp ? warp - 1 : 0);
+  return x + (warp ? before : 0);
+}
+__device__ __forceinline__ double uniform(const float* u, int s) {
+  return u[s] > 0.f ? (double)fminf(u[s], 0.99999994f) : 0.0;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) rest_accept_sampled_kernel(Args a) {
-  extern __shared__ uint32_t s_gone[];            // one bit per token: refused at the current node
-  __shared__ u64 s_sum[kThreads / 32];
-  __shared__ u64 s_left;
-  __shared__ int s_child, s_n_rej, s_rej[REST_MAX_N], s_token;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// The outcome of row `cur` (-1: the root's) of context b: an accepted child, or -1 and the drawn token
+// (-1: nothing can be drawn).  children = false: a walk that is as deep as allowed only draws.
+template <typename T, bool KEPT>
+__device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int b, int cur, bool children) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nn = min(max(a.n_nodes[b], 0), a.N);
   const int32_t *tok = a.tokens + (int64_t)b * a.N, *par = a.parents + (int64_t)b * a.N;
   const float* uni = a.uniforms + (int64_t)b * (a.N + 1);
   const float temp = a.temperature[b], top_p = a.top_p[b];
-  for (int d = tid; d < a.max_depth; d += kThreads) a.accept_nodes[(int64_t)b * a.max_depth + d] = -1;
-  for (int d = tid; d <= a.max_depth; d += kThreads) a.out_tokens[(int64_t)b * (a.max_depth + 1) + d] = -1;
-  for (int w = tid; w < (a.V + 31) / 32; w += kThreads) s_gone[w] = 0u;
-  auto uniform = [&](int s) -> double { const float u = uni[s]; return u > 0.f ? (double)fminf(u, 0.99999994f) : 0.0; };
-  int cur = -1;
-  for (int len = 0;; ++len) {
-    const T* row = static_cast<const T*>(a.logits) + b * a.s_ctx + (int64_t)(cur + 1) * a.s_row;
-    Row r;
-    r.greedy = !(temp > 0.f);
-    r.inv_t = r.greedy ? 0.0 : 1.0 / (double)temp;
-    // the largest logit
-    uint32_t top = 0;
-    for (int v = tid; v < a.V; v += kThreads) top = max(top, key_of(load(row, v)));
-    top = __reduce_max_sync(0xFFFFFFFFu, top);
-    __syncthreads();
-    if (lane == 0) s_sum[warp] = top;
-    __syncthreads();
-    for (int w = 0; w < kThreads / 32; ++w) top = max(top, (uint32_t)s_sum[w]);
-    r.top = top == 0 ? -INFINITY : __uint_as_float(top & 0x80000000u ? top & 0x7FFFFFFFu : ~top);
-    r.cut_key = 0u; r.cut_tie = 0x7FFFFFFF;
-    __syncthreads();
-    // the whole mass, then the nucleus: the smallest key whose tokens and all above reach the target
-    u64 mass = 0;
-    for (int v = tid; v < a.V; v += kThreads) mass += weight(r, load(row, v));
-    mass = block_sum(mass, s_sum);
-    if (top != 0 && (r.greedy || top_p < 1.f)) {
-      u64 target = 1;
-      if (!r.greedy && top_p > 0.f) target = max((u64)1, (u64)ceil((double)top_p * (double)mass));
-      uint32_t cut = 0;
-      for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t at = cut | (1u << bit);
-        u64 above = 0;
-        for (int v = tid; v < a.V; v += kThreads) { const float x = load(row, v); if (key_of(x) >= at) above += weight(r, x); }
-        if (block_sum(above, s_sum) >= target) cut = at;
-      }
-      u64 above = 0;
-      for (int v = tid; v < a.V; v += kThreads) { const float x = load(row, v); if (key_of(x) > cut) above += weight(r, x); }
-      above = block_sum(above, s_sum);
-      const u64 each = weight(r, __uint_as_float(cut & 0x80000000u ? cut & 0x7FFFFFFFu : ~cut));
-      const u64 ties = (target - above + each - 1) / each;             // tokens at the cut that stay, lowest first
-      int lo = 0, hi = a.V;                                            // smallest `hi` with `ties` of them below it
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        u64 n = 0;
-        for (int v = tid; v < mid; v += kThreads) n += key_of(load(row, v)) == cut;
-        if (block_sum(n, s_sum) >= ties) hi = mid; else lo = mid;
-      }
-      r.cut_key = cut; r.cut_tie = hi - 1;
-      mass = above + ties * each;
-    }
-    // children, in index order
-    if (warp == 0) {
-      int child = -1, n_rej = 0;
-      u64 left = mass;
-      for (int base = 0; base < nn && child < 0 && len < a.max_depth; base += 32) {
-        const int i = base + lane;
-        const bool is = i < nn && par[i] == cur;
-        const int t = is ? tok[i] : -1;
-        u64 w = 0;
-        double u = 0.0;
-        if (is && t >= 0 && t < a.V) {
-          const float x = load(row, t);
-          if (kept(r, key_of(x), t)) w = weight(r, x);
-          u = uniform(i + 1);
-          for (int j = 0; j < n_rej; ++j) if (s_rej[j] == t) w = 0;
+  const T* row = static_cast<const T*>(a.logits) + b * a.s_ctx + (int64_t)(cur + 1) * a.s_row;
+  const int V = a.V;
+  // KEPT: the row's 16-byte vectors, at the same offset from a 16-byte border as in memory.  Otherwise
+  // this memory is one bit per token: refused at this node.
+  const int shift = KEPT ? (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)) : 0;
+  T* s_val = reinterpret_cast<T*>(s_row) + shift;
+  uint32_t* s_gone = reinterpret_cast<uint32_t*>(s_row);
+  auto get = [&](int v) -> float { return KEPT ? (float)s_val[v] : (float)row[v]; };
+
+  // ---- 1. the row and its largest logit
+  uint32_t top = 0;
+  __syncthreads();                              // the row before it is done with
+  if (KEPT) {
+    constexpr int kPer = 16 / sizeof(T);
+    const int first = shift ? min(V, kPer - shift) : 0, vecs = (V - first) / kPer, last = first + vecs * kPer;
+    const uint4* src = reinterpret_cast<const uint4*>(row + first);
+    uint4* dst = reinterpret_cast<uint4*>(s_val + first);
+    for (int i0 = tid; i0 < vecs; i0 += 8 * kThreads) {
+      uint4 x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (i0 + j * kThreads < vecs) x[j] = __ldcs(src + i0 + j * kThreads);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (i0 + j * kThreads < vecs) {
+          dst[i0 + j * kThreads] = x[j];
+          const T* e = reinterpret_cast<const T*>(&x[j]);
+#pragma unroll
+          for (int k = 0; k < kPer; ++k) top = max(top, key_of((float)e[k]));
         }
-        unsigned todo = __ballot_sync(0xFFFFFFFFu, is && w != 0);
-        while (todo) {
-          const int l = __ffs(todo) - 1;
-          todo &= todo - 1;
-          const u64 wl = __shfl_sync(0xFFFFFFFFu, w, l);
-          const double ul = __shfl_sync(0xFFFFFFFFu, u, l);
-          const int tl = __shfl_sync(0xFFFFFFFFu, t, l);
-          if (wl == 0) continue;
-          if (ul * (double)left < (double)wl) { child = base + l; break; }
-          left -= wl;
-          if (lane == 0) s_rej[n_rej] = tl;
-          __syncwarp();
-          ++n_rej;
-          if (t == tl) w = 0;
-        }
-      }
-      if (lane == 0) { s_child = child; s_left = left; s_n_rej = n_rej; s_token = -1; }
     }
-    __syncthreads();
-    const int child = s_child;
-    if (child >= 0) {
-      if (tid == 0) {
-        a.accept_nodes[(int64_t)b * a.max_depth + len] = child;
-        a.out_tokens[(int64_t)b * (a.max_depth + 1) + len] = tok[child];
-      }
-      cur = child;
-      __syncthreads();
-      continue;
+    for (int v = tid; v < first + (V - last); v += kThreads) {
+      const int at = v < first ? v : last + v - first;
+      s_val[at] = row[at];
+      top = max(top, key_of((float)row[at]));
     }
-    // the last token, from what the refused children leave
-    for (int j = tid; j < s_n_rej; j += kThreads) atomicOr(&s_gone[s_rej[j] >> 5], 1u << (s_rej[j] & 31));
-    __syncthreads();
-    auto rest_weight = [&](int v) -> u64 {
-      const float x = load(row, v);
-      return kept(r, key_of(x), v) && !((s_gone[v >> 5] >> (v & 31)) & 1u) ? weight(r, x) : 0ull;
-    };
-    const int per = ((a.V + kThreads - 1) / kThreads) * 32, v0 = warp * per, v1 = min(a.V, v0 + per);
-    u64 sum = 0;
-    for (int v = v0 + lane; v < v1; v += 32) sum += rest_weight(v);
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-    if (lane == 0) s_sum[warp] = sum;
-    __syncthreads();
-    u64 before = 0;
-    for (int w = 0; w < warp; ++w) before += s_sum[w];
-    const double goal = uniform(0) * (double)s_left;
-    if (sum != 0 && !((double)before > goal) && (double)(before + sum) > goal) {   // one warp
-      for (int base = v0; base < v1; base += 32) {
-        u64 inc = base + lane < v1 ? rest_weight(base + lane) : 0;
-        for (int d = 1; d < 32; d <<= 1) { const u64 y = __shfl_up_sync(0xFFFFFFFFu, inc, d); if (lane >= d) inc += y; }
-        const unsigned hit = __ballot_sync(0xFFFFFFFFu, (double)(before + inc) > goal);
-        if (hit) { if (lane == 0) s_token = base + __ffs(hit) - 1; break; }
-        before += __shfl_sync(0xFFFFFFFFu, inc, 31);
-      }
-    }
-    __syncthreads();
-    if (tid == 0) {
-      a.out_tokens[(int64_t)b * (a.max_depth + 1) + len] = s_token;
-      a.accept_len[b] = len;
-    }
-    return;
+  } else {
+    for (int w = tid; w < (V + 31) / 32; w += kThreads) s_gone[w] = 0u;
+#pragma unroll 4
+    for (int v = tid; v < V; v += kThreads) top = max(top, key_of((float)row[v]));
   }
+  for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0u;
+  top = __reduce_max_sync(0xFFFFFFFFu, top);
+  if (lane == 0) sh.red[warp] = top;
+  if (tid == 0) { sh.cut_tie = 0x7FFFFFFF; sh.bin = kBins - 1; }
+  __syncthreads();
+  top = __reduce_max_sync(0xFFFFFFFFu, sh.red[lane]);
+  if (top == 0) return make_int2(-1, -1);
+  Row r;
+  r.top = of_key(top);
+  r.greedy = !(temp > 0.f);
+  r.inf = r.top == INFINITY;
+  r.c = r.greedy ? 0.0 : 1.4426950408889634 / (double)temp;
+  r.top_d = (double)r.top;
+  const bool smooth = !r.greedy && !r.inf;      // weights between 0 and 1
+
+  // ---- 2. the mass, and the histogram if there will be a cut
+  const bool cut = r.greedy || top_p < 1.f;
+  u64 mass = 0;
+  if (smooth) {
+#pragma unroll 2
+    for (int v = tid; v < V; v += kThreads) {
+      int k;
+      double f;
+      if (split(r, get(v), k, f)) {
+        const u64 w = weight_of(sh, k, f);
+        mass += w;
+        const int bin = max(-k, 0);
+        if (cut) atomicAdd(&sh.hist[bin], (uint32_t)(w >> max(32 - (bin >> 4), 0)));
+      }
+    }
+  } else {
+    for (int v = tid; v < V; v += kThreads) mass += get(v) == r.top ? kOne : 0ull;
+  }
+  mass = block_sum(sh, mass);
+
+  // ---- 3. the nucleus: tokens from (cut_key, cut_tie) up
+  uint32_t cut_key = 0;
+  int cut_tie = 0x7FFFFFFF;
+  if (cut) {
+    u64 target = 1;
+    if (!r.greedy && top_p > 0.f) target = max((u64)1, (u64)ceil((double)top_p * (double)mass));
+    u64 above = 0;                              // exact mass of what is surely kept
+    bool ordered = false;
+    uint32_t lo = top, hi = top;                // keys among which the cut lies, if it is not found by order
+    if (smooth) {
+      const u64 mine = tid < kBins ? (u64)sh.hist[tid] << max(32 - (tid >> 4), 0) : 0ull;
+      const u64 upto = block_scan(sh, mine);
+      if (tid < kBins && upto >= target && upto - mine < target) sh.bin = tid;
+      __syncthreads();
+      // the histogram may be a bin off: move until the exact sums agree (each move is towards the bin)
+      for (int tries = 0; tries < kBins; ++tries) {
+        const int bin = sh.bin;
+        __syncthreads();
+        if (tid == 0) sh.n_list = 0;
+        __syncthreads();
+        u64 over = 0, inside = 0;
+        for (int v = tid; v < V; v += kThreads) {
+          const float x = get(v);
+          int k;
+          double f;
+          if (split(r, x, k, f) && -k <= bin) {
+            const u64 w = weight_of(sh, k, f);
+            if (max(-k, 0) < bin) {
+              over += w;
+            } else {
+              inside += w;
+              const int at = atomicAdd(&sh.n_list, 1);
+              if (at < kList) { sh.key[at] = key_of(x); sh.idx[at] = v; sh.w[at] = w; }
+            }
+          }
+        }
+        block_sum2(sh, over, inside);
+        above = over;
+        if (over >= target && bin > 0) { if (tid == 0) sh.bin = bin - 1; }
+        else if (over + inside < target && bin + 1 < kBins) { if (tid == 0) sh.bin = bin + 1; }
+        else break;
+        __syncthreads();
+      }
+      const int n = sh.n_list;
+      if (n <= kList) {
+        ordered = true;
+        if (tid < n) {
+          const uint32_t key = sh.key[tid];
+          const int idx = sh.idx[tid];
+          u64 before = above;
+          for (int j = 0; j < n; ++j)
+            if (sh.key[j] > key || (sh.key[j] == key && sh.idx[j] < idx)) before += sh.w[j];
+          if (before < target && before + sh.w[tid] >= target) {
+            sh.cut_key = key;
+            sh.cut_tie = idx;
+            sh.left = before + sh.w[tid];
+          }
+        }
+        __syncthreads();
+        cut_key = sh.cut_key;
+        cut_tie = sh.cut_tie;
+        mass = sh.left;
+      } else {                                  // a crowd in one bin (flat rows): bisect its keys
+        uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+        for (int v = tid; v < V; v += kThreads) {
+          const float x = get(v);
+          int k;
+          double f;
+          if (split(r, x, k, f) && max(-k, 0) == sh.bin) { kmin = min(kmin, key_of(x)); kmax = max(kmax, key_of(x)); }
+        }
+        kmin = __reduce_min_sync(0xFFFFFFFFu, kmin);
+        kmax = __reduce_max_sync(0xFFFFFFFFu, kmax);
+        __syncthreads();
+        if (lane == 0) { sh.red[warp] = kmin; sh.idx[warp] = (int)kmax; }
+        __syncthreads();
+        lo = __reduce_min_sync(0xFFFFFFFFu, sh.red[lane]);
+        hi = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)sh.idx[lane]);
+      }
+    }
+    if (!ordered) {
+      // the largest key that reaches the target, then how many of its tokens stay, lowest index first
+      const u64 base = above;
+      while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2 + 1;
+        u64 more = 0;
+        for (int v = tid; v < V; v += kThreads) {
+          const float x = get(v);
+          int k;
+          double f;
+          if (key_of(x) >= mid && split(r, x, k, f) && max(-k, 0) == sh.bin) more += weight_of(sh, k, f);
+        }
+        if (base + block_sum(sh, more) >= target) lo = mid; else hi = mid - 1;
+      }
+      cut_key = lo;
+      u64 over = 0;
+      if (smooth) {
+        for (int v = tid; v < V; v += kThreads) {
+          const float x = get(v);
+          int k;
+          double f;
+          if (key_of(x) > cut_key && split(r, x, k, f) && max(-k, 0) == sh.bin) over += weight_of(sh, k, f);
+        }
+        over = block_sum(sh, over);
+      }
+      const u64 each = weight(sh, r, of_key(cut_key));
+      const u64 ties = (target - base - over + each - 1) / each;
+      const int per = (V + kThreads - 1) / kThreads, v0 = min(V, tid * per), v1 = min(V, v0 + per);
+      u64 mine = 0;
+      for (int v = v0; v < v1; ++v) mine += key_of(get(v)) == cut_key;
+      u64 upto = block_scan(sh, mine);
+      if (upto >= ties && upto - mine < ties) {
+        u64 n = upto - mine;
+        for (int v = v0; v < v1; ++v)
+          if (key_of(get(v)) == cut_key && ++n == ties) { sh.cut_tie = v; break; }
+      }
+      __syncthreads();
+      cut_tie = sh.cut_tie;
+      mass = base + over + ties * each;
+    }
+  }
+  auto kept_weight = [&](float x, int v) -> u64 {
+    const uint32_t key = key_of(x);
+    if (key < cut_key || (key == cut_key && v > cut_tie)) return 0ull;
+    return weight(sh, r, x);
+  };
+
+  // ---- 4. children, in index order
+  if (warp == 0) {
+    int child = -1, n_refused = 0;
+    u64 left = mass;
+    for (int base = 0; children && base < nn && child < 0; base += 32) {
+      const int i = base + lane;
+      const bool is = i < nn && par[i] == cur;
+      const int t = is ? tok[i] : -1;
+      u64 w = 0;
+      double u = 0.0;
+      if (is && t >= 0 && t < V) {
+        w = kept_weight(get(t), t);
+        u = uniform(uni, i + 1);
+        for (int j = 0; j < n_refused; ++j)
+          if (sh.refused[j] == t) w = 0;
+      }
+      unsigned todo = __ballot_sync(0xFFFFFFFFu, w != 0);
+      while (todo) {
+        const int l = __ffs(todo) - 1;
+        todo &= todo - 1;
+        const u64 wl = __shfl_sync(0xFFFFFFFFu, w, l);
+        const double ul = __shfl_sync(0xFFFFFFFFu, u, l);
+        const int tl = __shfl_sync(0xFFFFFFFFu, t, l);
+        if (wl == 0) continue;                  // its token was refused before
+        if (ul * (double)left < (double)wl) { child = base + l; break; }
+        left -= wl;
+        if (lane == 0) sh.refused[n_refused] = tl;
+        __syncwarp();
+        ++n_refused;
+        if (t == tl) w = 0;
+      }
+    }
+    if (lane == 0) { sh.child = child; sh.left = left; sh.n_refused = n_refused; sh.token = -1; sh.seg = kWarps - 1; sh.seg_before = 0; }
+  }
+  __syncthreads();
+  if (sh.child >= 0) return make_int2(sh.child, tok[sh.child]);
+
+  // ---- 5. the drawn token, from what the refused children leave: first the 1/32 of the row that holds
+  // it (a warp's share), then the token in it
+  for (int j = tid; j < sh.n_refused; j += kThreads) {
+    if (KEPT) s_val[sh.refused[j]] = (T)(-INFINITY);
+    else atomicOr(&s_gone[sh.refused[j] >> 5], 1u << (sh.refused[j] & 31));
+  }
+  __syncthreads();
+  auto rest_weight = [&](int v) -> u64 {
+    if (!KEPT && ((s_gone[v >> 5] >> (v & 31)) & 1u)) return 0ull;
+    return kept_weight(get(v), v);
+  };
+  const int per = ((V + kThreads - 1) / kThreads) * 32, v0 = min(V, warp * per), v1 = min(V, v0 + per);
+  u64 sum = 0;
+  for (int v = v0 + lane; v < v1; v += 32) sum += rest_weight(v);
+  sum = warp_sum(sum);
+  if (lane == 0) sh.sum[warp] = sum;
+  __syncthreads();
+  const double goal = uniform(uni, 0) * (double)sh.left;
+  if (warp == 0) {
+    const u64 mine = sh.sum[lane], upto = warp_scan(mine);
+    if ((double)upto > goal && !((double)(upto - mine) > goal)) { sh.seg = lane; sh.seg_before = upto - mine; }
+  }
+  __syncthreads();
+  const int s0 = min(V, sh.seg * per), s1 = min(V, s0 + per);
+  u64 before = sh.seg_before;
+  for (int base = s0; base < s1; base += kThreads) {      // (more than one round for more than 32768 tokens)
+    const u64 mine = base + tid < s1 ? rest_weight(base + tid) : 0ull;
+    const u64 upto = before + block_scan(sh, mine);
+    if ((double)upto > goal && !((double)(upto - mine) > goal)) sh.token = base + tid;
+    if (tid == kThreads - 1) sh.above = upto;
+    __syncthreads();
+    before = sh.above;
+  }
+  return make_int2(-1, sh.token);
+}
+
+__device__ __forceinline__ void fill_table(Shared& sh) {
+  if (threadIdx.x < 16) sh.pow16[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+}
+
+// One block per context walks.
+template <typename T, bool KEPT>
+__global__ void __launch_bounds__(kThreads) rest_accept_sampled_walk_kernel(const __grid_constant__ Args a) {
+  extern __shared__ __align__(16) unsigned char s_row[];
+  __shared__ Shared sh;
+  fill_table(sh);
+  grid_wait();
+  const int b = blockIdx.x, tid = threadIdx.x;
+  int32_t *an = a.accept_nodes + (int64_t)b * a.max_depth, *ot = a.out_tokens + (int64_t)b * (a.max_depth + 1);
+  int cur = -1, len = 0;
+  for (;;) {
+    const int2 o = row_outcome<T, KEPT>(a, sh, s_row, b, cur, len < a.max_depth);
+    if (tid == 0) ot[len] = o.y;
+    if (o.x < 0) break;
+    if (tid == 0) an[len] = o.x;
+    cur = o.x;
+    ++len;
+  }
+  if (tid == 0) a.accept_len[b] = len;
+  for (int d = len + tid; d < a.max_depth; d += kThreads) { an[d] = -1; ot[d + 1] = -1; }
+}
+
+// Every row has a block; blockIdx.x = row, blockIdx.y = context.
+template <typename T, bool KEPT>
+__global__ void __launch_bounds__(kThreads) rest_accept_sampled_rows_kernel(const __grid_constant__ Args a) {
+  extern __shared__ __align__(16) unsigned char s_row[];
+  __shared__ Shared sh;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  fill_table(sh);
+  grid_wait();
+  const int b = blockIdx.y, cur = (int)blockIdx.x - 1, tid = threadIdx.x;
+  if (cur >= min(max(a.n_nodes[b], 0), a.N)) return;
+  if (tid == kThreads - 1) {                    // how deep a walk is when it gets here, as far as that matters
+    int depth = 0;
+    for (int i = cur; i >= 0 && i < a.N && depth <= a.max_depth; i = a.parents[(int64_t)b * a.N + i]) ++depth;
+    sh.depth = depth;
+  }
+  __syncthreads();
+  const int depth = sh.depth;
+  if (depth > a.max_depth) return;              // no walk does
+  const int2 o = row_outcome<T, KEPT>(a, sh, s_row, b, cur, depth < a.max_depth);
+  if (tid == 0) a.outcome[(int64_t)b * (a.N + 1) + cur + 1] = o;
+}
+
+__global__ void __launch_bounds__(128) rest_accept_sampled_follow_kernel(const __grid_constant__ Args a) {
+  __shared__ int2 s[REST_MAX_N + 1];
+  grid_wait();
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int rows = min(max(a.n_nodes[b], 0), a.N) + 1;
+  for (int i = tid; i < rows; i += 128) s[i] = a.outcome[(int64_t)b * (a.N + 1) + i];
+  __syncthreads();
+  int32_t *an = a.accept_nodes + (int64_t)b * a.max_depth, *ot = a.out_tokens + (int64_t)b * (a.max_depth + 1);
+  int cur = -1, len = 0;
+  for (;;) {                                    // every thread walks; a row at full depth has no child
+    const int2 o = s[cur + 1];
+    if (tid == 0) ot[len] = o.y;
+    if (o.x < 0 || len == a.max_depth) break;
+    if (tid == 0) an[len] = o.x;
+    cur = o.x;
+    ++len;
+  }
+  if (tid == 0) a.accept_len[b] = len;
+  for (int d = len + tid; d < a.max_depth; d += 128) { an[d] = -1; ot[d + 1] = -1; }
+}
+
+// Every row of its own block pays when all of them run in about two rounds of one block an SM: a walk
+// is rarely shorter than three rows, one after the other.
+bool every_row(int B, int N) {
+  const int sms = rest::sm_count();
+  return (int64_t)B * (N + 1) <= 2 * (sms > 0 ? sms : 148);
+}
+
+template <typename T, bool KEPT>
+rest_status run(const Args& a, int B, size_t smem, int smem_slot, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (a.outcome) {
+    REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(rest_accept_sampled_rows_kernel<T, KEPT>), smem_slot, smem));
+    cfg.gridDim = dim3((unsigned)(a.N + 1), (unsigned)B, 1);
+    REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, rest_accept_sampled_rows_kernel<T, KEPT>, a));
+    rest::count_launch();
+    cfg.gridDim = dim3((unsigned)B, 1, 1);
+    cfg.blockDim = dim3(128, 1, 1);
+    cfg.dynamicSmemBytes = 0;
+    REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, rest_accept_sampled_follow_kernel, a));
+  } else {
+    REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(rest_accept_sampled_walk_kernel<T, KEPT>), smem_slot + 1, smem));
+    cfg.gridDim = dim3((unsigned)B, 1, 1);
+    REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, rest_accept_sampled_walk_kernel<T, KEPT>, a));
+  }
+  rest::count_launch();
+  return REST_OK;
+}
+
+template <typename T>
+rest_status pick(const Args& a, int B, int smem_slot, cudaStream_t st) {
+  const size_t row = ((size_t)a.V * sizeof(T) + 31) / 16 * 16;
+  if (row <= kRowBytes) return run<T, true>(a, B, row, smem_slot, st);
+  return run<T, false>(a, B, 4 * (((size_t)a.V + 31) / 32), smem_slot + 2, st);
 }
 
 }  // namespace
+
+extern "C" size_t rest_accept_sampled_workspace_bytes(int32_t B, int32_t N) {
+  if (B <= 0 || N <= 0 || N > REST_MAX_N) return 0;
+  return every_row(B, N) ? sizeof(int2) * (size_t)B * (N + 1) : 0;
+}
 
 extern "C" rest_status rest_accept_sampled(const void* d_logits, int32_t dtype, int64_t ctx_stride, int64_t row_stride,
                                            int32_t V, const int32_t* d_tokens, const int32_t* d_parents,
                                            const int32_t* d_n_nodes, const float* d_uniforms,
                                            const float* d_temperature, const float* d_top_p, int32_t B, int32_t N,
                                            int32_t max_depth, int32_t* d_accept_len, int32_t* d_accept_nodes,
-                                           int32_t* d_out_tokens, void* stream) {
+                                           int32_t* d_out_tokens, void* d_ws, size_t ws_bytes, void* stream) {
   if (B < 0 || N < 1 || max_depth < 1 || V < 1 || ctx_stride < 0 || row_stride < 0) return REST_INVALID_ARG;
   if (dtype != REST_BF16 && dtype != REST_FP16 && dtype != REST_FP32) return REST_INVALID_ARG;
   if (B == 0) return REST_OK;
@@ -211,18 +571,21 @@ extern "C" rest_status rest_accept_sampled(const void* d_logits, int32_t dtype, 
       !d_accept_len || !d_accept_nodes || !d_out_tokens)
     return REST_INVALID_ARG;
   if (V > REST_MAX_VOCAB_SAMPLED || max_depth > REST_MAX_M || N > REST_MAX_N) return REST_UNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(d_logits) % (dtype == REST_FP32 ? 4 : 2)) return REST_INVALID_ARG;
   Args a;
   a.logits = d_logits; a.s_ctx = ctx_stride; a.s_row = row_stride;
   a.tokens = d_tokens; a.parents = d_parents; a.n_nodes = d_n_nodes;
   a.uniforms = d_uniforms; a.temperature = d_temperature; a.top_p = d_top_p;
   a.accept_len = d_accept_len; a.accept_nodes = d_accept_nodes; a.out_tokens = d_out_tokens;
   a.V = V; a.N = N; a.max_depth = max_depth;
-  const size_t smem = 4 * (((size_t)V + 31) / 32);
+  a.outcome = nullptr;
+  // without the scratch the contexts walk: slower for few contexts, the same results
+  if (every_row(B, N) && d_ws && ws_bytes >= rest_accept_sampled_workspace_bytes(B, N)) {
+    if (reinterpret_cast<uintptr_t>(d_ws) & 7) return REST_INVALID_ARG;
+    a.outcome = static_cast<int2*>(d_ws);
+  }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (dtype == REST_BF16) rest_accept_sampled_kernel<__nv_bfloat16><<<B, kThreads, smem, st>>>(a);
-  else if (dtype == REST_FP16) rest_accept_sampled_kernel<__half><<<B, kThreads, smem, st>>>(a);
-  else rest_accept_sampled_kernel<float><<<B, kThreads, smem, st>>>(a);
-  REST_CUDA_TRY(cudaGetLastError());
-  rest::count_launch();
-  return REST_OK;
+  if (dtype == REST_BF16) return pick<__nv_bfloat16>(a, B, rest::kSmemSlotAccept, st);
+  if (dtype == REST_FP16) return pick<__half>(a, B, rest::kSmemSlotAccept + 4, st);
+  return pick<float>(a, B, rest::kSmemSlotAccept + 8, st);
 }

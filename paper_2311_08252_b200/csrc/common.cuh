@@ -21,8 +21,9 @@ int sm_count();
 rest_status take_paged_error_flags(uint32_t* h_flags);
 // One slot per kernel instance, library-wide: two kernels on one slot would skip each other's
 // attribute call.  The draft kernel's instances take kSmemSlotDraft + 0 ... 19, the paged
-// attention's kSmemSlotPaged + 0 ... 15.
-constexpr int kSmemSlotDraft = 0, kSmemSlotAttn = 20, kSmemSlotAttnWide = 21, kSmemSlotPaged = 22, kSmemSlots = 38;
+// attention's kSmemSlotPaged + 0 ... 15, the sampled acceptance's kSmemSlotAccept + 0 ... 11.
+constexpr int kSmemSlotDraft = 0, kSmemSlotAttn = 20, kSmemSlotAttnWide = 21, kSmemSlotPaged = 22,
+              kSmemSlotAccept = 38, kSmemSlots = 50;
 
 #define REST_CUDA_TRY(expr)                                              \
   do {                                                                   \

@@ -29,10 +29,11 @@ def run(logits, tokens, parents, nodes, uni, temp, top_p, depth, **kw):
 
 
 def check(logits, tokens, parents, nodes, uni, temp, top_p, depth):
-    got = run(logits, tokens, parents, nodes, uni, temp, top_p, depth)
     want = plain.accept_sampled(logits.double().cpu().numpy(), tokens, parents, nodes, uni, temp, top_p, depth)
-    for g, w in zip(got, want):
-        assert np.array_equal(g, w), (g, w)
+    for workspace in (None, False):                       # every row at once (few contexts), and row by row
+        got = run(logits, tokens, parents, nodes, uni, temp, top_p, depth, workspace=workspace)
+        for g, w in zip(got, want):
+            assert np.array_equal(g, w), (g, w)
     return got
 
 

@@ -107,11 +107,11 @@ def test_attention_refuses():
 
 def sampled(dtype=0, V=100, B=1, N=4, depth=4, logits=256, ctx=500):
     return rest.lib().rest_accept_sampled(logits, dtype, ctx, 100, V, 256, 256, 256, 256, 256, 256, B, N, depth, 256, 256,
-                                          256, None)
+                                          256, None, 0, None)
 
 
 def test_sampled_acceptance_refuses():
     assert sampled(B=0) == OK
     assert sampled(V=(1 << 18) + 1) == UNSUPPORTED and sampled(N=257) == UNSUPPORTED and sampled(depth=17) == UNSUPPORTED
     assert sampled(dtype=3) == INVALID and sampled(V=0) == INVALID and sampled(depth=0) == INVALID
-    assert sampled(logits=None) == INVALID and sampled(ctx=-1) == INVALID and sampled(B=-1) == INVALID
+    assert sampled(logits=257) == INVALID and sampled(logits=None) == INVALID and sampled(ctx=-1) == INVALID and sampled(B=-1) == INVALID

@@ -4,15 +4,17 @@
 // One block works on one row of logits at a time and says where a walk that reaches that row goes:
 // to a child, or to an end with a drawn token.  Its steps:
 //   1. the row into shared memory (larger ones are read again from L2), and its largest logit;
-//   2. every token's weight as an integer of 2^-44 of the largest, their exact sum, and a histogram
-//      of the weights over bins of 1/16 in log2 (approximate, 13 bits a token);
-//   3. with a nucleus: the bin in which the sum reaches its target, found in the histogram and checked
-//      with exact sums; the tokens of that bin (some hundred) are ordered against one another;
+//   2. every token's weight as an integer of 2^-44 of the largest (rounded to 28 bits), their sum, and
+//      the sums of bins of 1/16 in log2 - for tokens heavy enough to be in the nucleus: those below
+//      (1 - top_p) / V of the largest are not, whatever the rest of the row holds;
+//   3. with a nucleus: the bin in which the running sum reaches its target; the tokens of that bin (some
+//      hundred) are ordered against one another;
 //   4. the children of the row's node in index order;
 //   5. if none is accepted: the drawn token, by sums over the tokens in order.
 // Integer sums are exact, so the result depends neither on the order of addition nor on the number of
-// threads; weights are computed in 64 bits (error about 4e-11 of each, where 32 bits would move the
-// borders between neighbouring tokens often enough to be seen in a large batch).
+// threads.  A weight is computed in 64 bits and off by 2^-28 of itself at most, either way alike: errors
+// of 32-bit arithmetic (the product of a far logit and 1 / temperature alone: 1e-6) would move the
+// borders between tokens often enough to be seen in a large batch.
 //
 // A walk visits 1 + accepted rows of N + 1.  Either one block per context walks, a row after the
 // other, reading only those rows; or, when the rows of all contexts are few enough to run at once,
@@ -61,12 +63,13 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 
 struct Shared {
   double pow16[16];                             // 2^(j/16)
-  u64 sum[kWarps], sum2[kWarps], left, above, bin_mass, seg_before;
+  u64 sum[kWarps], left, above, seg_before;
   u64 w[kList];
   uint32_t key[kList];
   int idx[kList];
-  uint32_t hist[kBins];
+  uint32_t bin_lo[kBins], bin_hi[kBins];        // sums of the low 14 and the higher bits of 28-bit weights
   uint32_t red[kWarps], cut_key;
+  int32_t tok[REST_MAX_N], par[REST_MAX_N];
   int cut_tie, bin, n_list, child, n_refused, refused[REST_MAX_N], token, seg, depth;
 };
 
@@ -92,18 +95,20 @@ __device__ __forceinline__ bool split(const Row& r, float x, int& k, double& f) 
   f = y - (t - kMagic);
   return true;
 }
-// 2^44 * 2^(k/16 + f), |f| <= 1/32: the table and the Taylor series of 2^f to the fourth power (the
-// fifth is 4e-11), rounded to an integer by adding 2^52
-__device__ __forceinline__ u64 weight_of(const Shared& sh, int k, double f) {
+// The weight 2^(k/16 + f), |f| <= 1/32, as an integer m of 28 bits at most: m << up(k) in units of 2^-44.
+// The table and the Taylor series of 2^f to the fourth power (the fifth is 4e-11), rounded by adding 2^52.
+__device__ __forceinline__ int up(int k) { return 17 - min(-(k >> 4), 17); }
+__device__ __forceinline__ uint32_t weight28(const Shared& sh, int k, double f) {
   constexpr double a1 = 0.6931471805599453, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4;
   const double t = sh.pow16[k & 15];
-  const double scaled = __hiloint2double(__double2hiint(t) + (((k >> 4) + 44) << 20), __double2loint(t));
+  const double scaled = __hiloint2double(__double2hiint(t) + (((k >> 4) + 44 - up(k)) << 20), __double2loint(t));
   double p = fma(f, a4, a3);
   p = fma(f, p, a2);
   p = fma(f, p, a1);
   p = fma(f, p, 1.0);
-  return (u64)__double_as_longlong(fma(p, scaled, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+  return (uint32_t)__double2loint(fma(p, scaled, 4503599627370496.0));
 }
+__device__ __forceinline__ u64 weight_of(const Shared& sh, int k, double f) { return (u64)weight28(sh, k, f) << up(k); }
 // weight before the nucleus cut (see Row): an infinite logit takes all of the mass
 __device__ __forceinline__ u64 weight(const Shared& sh, const Row& r, float x) {
   if (r.inf || r.greedy) return x == r.top ? kOne : 0ull;
@@ -125,20 +130,12 @@ __device__ __forceinline__ u64 warp_scan(u64 x) {     // inclusive
   }
   return x;
 }
-// sums over the block of two values, for every thread
-__device__ __forceinline__ void block_sum2(Shared& sh, u64& x, u64& y) {
-  x = warp_sum(x);
-  y = warp_sum(y);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) { sh.sum[threadIdx.x >> 5] = x; sh.sum2[threadIdx.x >> 5] = y; }
-  __syncthreads();
-  x = warp_sum(sh.sum[threadIdx.x & 31]);
-  y = warp_sum(sh.sum2[threadIdx.x & 31]);
-}
 __device__ __forceinline__ u64 block_sum(Shared& sh, u64 x) {
-  u64 zero = 0;
-  block_sum2(sh, x, zero);
-  return x;
+  x = warp_sum(x);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh.sum[threadIdx.x >> 5] = x;
+  __syncthreads();
+  return warp_sum(sh.sum[threadIdx.x & 31]);
 }
 // inclusive prefix sum over the block's threads
 __device__ __forceinline__ u64 block_scan(Shared& sh, u64 x) {
@@ -166,49 +163,71 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
   const float temp = a.temperature[b], top_p = a.top_p[b];
   const T* row = static_cast<const T*>(a.logits) + b * a.s_ctx + (int64_t)(cur + 1) * a.s_row;
   const int V = a.V;
-  // KEPT: the row's 16-byte vectors, at the same offset from a 16-byte border as in memory.  Otherwise
-  // this memory is one bit per token: refused at this node.
+  // KEPT: the row's 16-byte vectors, at the same offset from a 16-byte border as in memory, padded with
+  // -infinity on both sides.  Otherwise this memory is one bit per token: refused at this node.
+  constexpr int kPer = 16 / sizeof(T);
   const int shift = KEPT ? (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)) : 0;
+  const int vecs = (shift + V + kPer - 1) / kPer;
   T* s_val = reinterpret_cast<T*>(s_row) + shift;
   uint32_t* s_gone = reinterpret_cast<uint32_t*>(s_row);
   auto get = [&](int v) -> float { return KEPT ? (float)s_val[v] : (float)row[v]; };
+  // fn(token, logit) for all tokens, or for those of vectors / tokens [from, to) by this thread and those
+  // `step` on
+  auto each = [&](int from, int to, int step, auto fn) {
+    if (KEPT) {
+      for (int i = from; i < to; i += step) {
+        const uint4 x = reinterpret_cast<const uint4*>(s_row)[i];
+        const T* e = reinterpret_cast<const T*>(&x);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) fn(i * kPer + k - shift, (float)e[k]);
+      }
+    } else {
+#pragma unroll 4
+      for (int v = from; v < to; v += step) fn(v, (float)row[v]);
+    }
+  };
+  const int units = KEPT ? vecs : V;
 
-  // ---- 1. the row and its largest logit
+  // ---- 1. the row and its largest logit; the tree
   uint32_t top = 0;
   __syncthreads();                              // the row before it is done with
+  for (int i = tid; i < nn; i += kThreads) { sh.tok[i] = tok[i]; sh.par[i] = par[i]; }
   if (KEPT) {
-    constexpr int kPer = 16 / sizeof(T);
-    const int first = shift ? min(V, kPer - shift) : 0, vecs = (V - first) / kPer, last = first + vecs * kPer;
-    const uint4* src = reinterpret_cast<const uint4*>(row + first);
-    uint4* dst = reinterpret_cast<uint4*>(s_val + first);
-    for (int i0 = tid; i0 < vecs; i0 += 8 * kThreads) {
+    const T* base = row - shift;                // whole vectors inside the row; its ragged ends one by one
+    const int first = shift ? 1 : 0, last = (shift + V) / kPer;
+    for (int i0 = first + tid; i0 < last; i0 += 8 * kThreads) {
       uint4 x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (i0 + j * kThreads < vecs) x[j] = __ldcs(src + i0 + j * kThreads);
+        if (i0 + j * kThreads < last) x[j] = __ldcs(reinterpret_cast<const uint4*>(base) + i0 + j * kThreads);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (i0 + j * kThreads < vecs) {
-          dst[i0 + j * kThreads] = x[j];
+        if (i0 + j * kThreads < last) {
+          reinterpret_cast<uint4*>(s_row)[i0 + j * kThreads] = x[j];
           const T* e = reinterpret_cast<const T*>(&x[j]);
+          float most = -INFINITY;               // (fmaxf passes NaN over)
 #pragma unroll
-          for (int k = 0; k < kPer; ++k) top = max(top, key_of((float)e[k]));
+          for (int k = 0; k < kPer; ++k) most = fmaxf(most, (float)e[k]);
+          top = max(top, key_of(most));
         }
     }
-    for (int v = tid; v < first + (V - last); v += kThreads) {
-      const int at = v < first ? v : last + v - first;
-      s_val[at] = row[at];
-      top = max(top, key_of((float)row[at]));
+    if (tid < 2 * kPer) {
+      const int at = tid < kPer ? tid : (vecs - 1) * kPer + tid - kPer, v = at - shift;
+      const bool ragged = tid < kPer ? first == 1 : last < vecs && (vecs > 1 || first == 0);
+      if (ragged) {
+        const T x = v >= 0 && v < V ? row[v] : (T)(-INFINITY);
+        reinterpret_cast<T*>(s_row)[at] = x;
+        top = max(top, key_of((float)x));
+      }
     }
   } else {
     for (int w = tid; w < (V + 31) / 32; w += kThreads) s_gone[w] = 0u;
-#pragma unroll 4
-    for (int v = tid; v < V; v += kThreads) top = max(top, key_of((float)row[v]));
+    each(tid, units, kThreads, [&](int, float x) { top = max(top, key_of(x)); });
   }
-  for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0u;
+  for (int i = tid; i < kBins; i += kThreads) sh.bin_lo[i] = sh.bin_hi[i] = 0u;
   top = __reduce_max_sync(0xFFFFFFFFu, top);
   if (lane == 0) sh.red[warp] = top;
-  if (tid == 0) { sh.cut_tie = 0x7FFFFFFF; sh.bin = kBins - 1; }
+  if (tid == 0) { sh.cut_tie = 0x7FFFFFFF; sh.bin = -1; sh.n_list = 0; }
   __syncthreads();
   top = __reduce_max_sync(0xFFFFFFFFu, sh.red[lane]);
   if (top == 0) return make_int2(-1, -1);
@@ -220,23 +239,26 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
   r.top_d = (double)r.top;
   const bool smooth = !r.greedy && !r.inf;      // weights between 0 and 1
 
-  // ---- 2. the mass, and the histogram if there will be a cut
+  // ---- 2. the mass, and the bins' if there will be a cut
   const bool cut = r.greedy || top_p < 1.f;
   u64 mass = 0;
   if (smooth) {
-#pragma unroll 2
-    for (int v = tid; v < V; v += kThreads) {
+    // the last bin that can be in the nucleus: 16 log2(V / (1 - top_p)), and two more for its roundings
+    const int bins = cut ? (top_p > 0.f ? min(kBins, (int)(16.f * (log2f((float)V) - log2f(1.f - top_p))) + 3) : 1) : 0;
+    each(tid, units, kThreads, [&](int, float x) {
       int k;
       double f;
-      if (split(r, get(v), k, f)) {
-        const u64 w = weight_of(sh, k, f);
-        mass += w;
-        const int bin = max(-k, 0);
-        if (cut) atomicAdd(&sh.hist[bin], (uint32_t)(w >> max(32 - (bin >> 4), 0)));
+      if (split(r, x, k, f)) {
+        const uint32_t w = weight28(sh, k, f);
+        mass += (u64)w << up(k);
+        if (-k < bins) {
+          atomicAdd(&sh.bin_lo[max(-k, 0)], w & 0x3FFFu);
+          atomicAdd(&sh.bin_hi[max(-k, 0)], w >> 14);
+        }
       }
-    }
+    });
   } else {
-    for (int v = tid; v < V; v += kThreads) mass += get(v) == r.top ? kOne : 0ull;
+    each(tid, units, kThreads, [&](int, float x) { mass += x == r.top ? kOne : 0ull; });
   }
   mass = block_sum(sh, mass);
 
@@ -246,57 +268,52 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
   if (cut) {
     u64 target = 1;
     if (!r.greedy && top_p > 0.f) target = max((u64)1, (u64)ceil((double)top_p * (double)mass));
-    u64 above = 0;                              // exact mass of what is surely kept
+    u64 above = 0;                              // mass of the bins that are surely kept
     bool ordered = false;
     uint32_t lo = top, hi = top;                // keys among which the cut lies, if it is not found by order
+    float x_lo = 0.f, x_hi = 0.f;               // logits of the bin lie between them
     if (smooth) {
-      const u64 mine = tid < kBins ? (u64)sh.hist[tid] << max(32 - (tid >> 4), 0) : 0ull;
+      const u64 mine = tid < kBins ? (u64)sh.bin_lo[tid] + ((u64)sh.bin_hi[tid] << 14) << up(-tid) : 0ull;
       const u64 upto = block_scan(sh, mine);
-      if (tid < kBins && upto >= target && upto - mine < target) sh.bin = tid;
+      if (upto >= target && upto - mine < target) { sh.bin = tid; sh.above = upto - mine; }
       __syncthreads();
-      // the histogram may be a bin off: move until the exact sums agree (each move is towards the bin)
-      for (int tries = 0; tries < kBins; ++tries) {
-        const int bin = sh.bin;
-        __syncthreads();
-        if (tid == 0) sh.n_list = 0;
-        __syncthreads();
-        u64 over = 0, inside = 0;
-        for (int v = tid; v < V; v += kThreads) {
-          const float x = get(v);
-          int k;
-          double f;
-          if (split(r, x, k, f) && -k <= bin) {
-            const u64 w = weight_of(sh, k, f);
-            if (max(-k, 0) < bin) {
-              over += w;
-            } else {
-              inside += w;
-              const int at = atomicAdd(&sh.n_list, 1);
-              if (at < kList) { sh.key[at] = key_of(x); sh.idx[at] = v; sh.w[at] = w; }
-            }
-          }
+      const int bin = sh.bin;
+      above = sh.above;
+      // a little wider than half a bin on both sides, so that only few tokens are looked at closely
+      x_hi = (float)(r.top_d - ((double)bin - 0.51) / 16.0 / r.c);
+      x_lo = (float)(r.top_d - ((double)bin + 0.51) / 16.0 / r.c);
+      x_hi += fabsf(x_hi) * 1e-6f;
+      x_lo -= fabsf(x_lo) * 1e-6f;
+      each(tid, units, kThreads, [&](int v, float x) {
+        int k;
+        double f;
+        if (x >= x_lo && x <= x_hi && split(r, x, k, f) && max(-k, 0) == bin) {
+          const int at = atomicAdd(&sh.n_list, 1);
+          if (at < kList) { sh.key[at] = key_of(x); sh.idx[at] = v; sh.w[at] = weight_of(sh, k, f); }
         }
-        block_sum2(sh, over, inside);
-        above = over;
-        if (over >= target && bin > 0) { if (tid == 0) sh.bin = bin - 1; }
-        else if (over + inside < target && bin + 1 < kBins) { if (tid == 0) sh.bin = bin + 1; }
-        else break;
-        __syncthreads();
-      }
+      });
+      __syncthreads();
       const int n = sh.n_list;
       if (n <= kList) {
         ordered = true;
-        if (tid < n) {
-          const uint32_t key = sh.key[tid];
-          const int idx = sh.idx[tid];
-          u64 before = above;
-          for (int j = 0; j < n; ++j)
-            if (sh.key[j] > key || (sh.key[j] == key && sh.idx[j] < idx)) before += sh.w[j];
-          if (before < target && before + sh.w[tid] >= target) {
-            sh.cut_key = key;
-            sh.cut_tie = idx;
-            sh.left = before + sh.w[tid];
+        // the mass before each token of the bin; several lanes share a token when there are few
+        int parts = 1;
+        while (parts < 32 && n * parts * 2 <= kThreads) parts *= 2;
+        const int e = tid / parts, part = tid % parts;
+        const uint32_t key = e < n ? sh.key[e] : 0u;
+        const int idx = e < n ? sh.idx[e] : 0;
+        u64 before = 0;
+        if (e < n)
+          for (int j = part; j < n; j += parts) {
+            const uint32_t other = sh.key[j];
+            if (other > key || (other == key && sh.idx[j] < idx)) before += sh.w[j];
           }
+        for (int d = 1; d < parts; d <<= 1) before += __shfl_xor_sync(0xFFFFFFFFu, before, d);
+        before += above;
+        if (e < n && part == 0 && before < target && before + sh.w[e] >= target) {
+          sh.cut_key = key;
+          sh.cut_tie = idx;
+          sh.left = before + sh.w[e];
         }
         __syncthreads();
         cut_key = sh.cut_key;
@@ -304,12 +321,11 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
         mass = sh.left;
       } else {                                  // a crowd in one bin (flat rows): bisect its keys
         uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
-        for (int v = tid; v < V; v += kThreads) {
-          const float x = get(v);
+        each(tid, units, kThreads, [&](int, float x) {
           int k;
           double f;
-          if (split(r, x, k, f) && max(-k, 0) == sh.bin) { kmin = min(kmin, key_of(x)); kmax = max(kmax, key_of(x)); }
-        }
+          if (x >= x_lo && x <= x_hi && split(r, x, k, f) && max(-k, 0) == sh.bin) { kmin = min(kmin, key_of(x)); kmax = max(kmax, key_of(x)); }
+        });
         kmin = __reduce_min_sync(0xFFFFFFFFu, kmin);
         kmax = __reduce_max_sync(0xFFFFFFFFu, kmax);
         __syncthreads();
@@ -325,39 +341,49 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
       while (lo < hi) {
         const uint32_t mid = lo + (hi - lo) / 2 + 1;
         u64 more = 0;
-        for (int v = tid; v < V; v += kThreads) {
-          const float x = get(v);
+        each(tid, units, kThreads, [&](int, float x) {
           int k;
           double f;
-          if (key_of(x) >= mid && split(r, x, k, f) && max(-k, 0) == sh.bin) more += weight_of(sh, k, f);
-        }
+          if (x >= x_lo && x <= x_hi && key_of(x) >= mid && split(r, x, k, f) && max(-k, 0) == sh.bin) more += weight_of(sh, k, f);
+        });
         if (base + block_sum(sh, more) >= target) lo = mid; else hi = mid - 1;
       }
       cut_key = lo;
       u64 over = 0;
-      if (smooth) {
-        for (int v = tid; v < V; v += kThreads) {
-          const float x = get(v);
+      if (smooth)
+        each(tid, units, kThreads, [&](int, float x) {
           int k;
           double f;
-          if (key_of(x) > cut_key && split(r, x, k, f) && max(-k, 0) == sh.bin) over += weight_of(sh, k, f);
-        }
-        over = block_sum(sh, over);
-      }
-      const u64 each = weight(sh, r, of_key(cut_key));
-      const u64 ties = (target - base - over + each - 1) / each;
-      const int per = (V + kThreads - 1) / kThreads, v0 = min(V, tid * per), v1 = min(V, v0 + per);
+          if (x >= x_lo && x <= x_hi && key_of(x) > cut_key && split(r, x, k, f) && max(-k, 0) == sh.bin) over += weight_of(sh, k, f);
+        });
+      over = block_sum(sh, over);
+      const u64 one = weight(sh, r, of_key(cut_key)), ties = (target - base - over + one - 1) / one;
+      // every warp counts in a run of its own; the warp whose run holds the last one finds it
+      const int per = (units + kWarps - 1) / kWarps, u0 = min(units, warp * per), u1 = min(units, u0 + per);
       u64 mine = 0;
-      for (int v = v0; v < v1; ++v) mine += key_of(get(v)) == cut_key;
-      u64 upto = block_scan(sh, mine);
-      if (upto >= ties && upto - mine < ties) {
+      each(u0 + lane, u1, 32, [&](int, float x) { mine += key_of(x) == cut_key; });
+      mine = warp_sum(mine);
+      __syncthreads();
+      if (lane == 0) sh.sum[warp] = mine;
+      __syncthreads();
+      const u64 counts = warp_scan(sh.sum[lane]);
+      const u64 upto = __shfl_sync(0xFFFFFFFFu, counts, warp);
+      if (upto >= ties && upto - mine < ties) {           // (one warp)
         u64 n = upto - mine;
-        for (int v = v0; v < v1; ++v)
-          if (key_of(get(v)) == cut_key && ++n == ties) { sh.cut_tie = v; break; }
+        const int v0 = max(KEPT ? u0 * kPer - shift : u0, 0), v1 = min(V, KEPT ? u1 * kPer - shift : u1);
+        for (int base_v = v0; base_v < v1; base_v += 32) {
+          const bool is = base_v + lane < v1 && key_of(get(base_v + lane)) == cut_key;
+          const unsigned bal = __ballot_sync(0xFFFFFFFFu, is);
+          if (n + __popc(bal) >= ties) {
+            if (is && n + __popc(bal & ((2u << lane) - 1u)) == ties) sh.cut_tie = base_v + lane;
+            break;
+          }
+          n += __popc(bal);
+        }
       }
       __syncthreads();
       cut_tie = sh.cut_tie;
-      mass = base + over + ties * each;
+      mass = base + over + ties * one;
     }
   }
   auto kept_weight = [&](float x, int v) -> u64 {
@@ -372,8 +398,8 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
     u64 left = mass;
     for (int base = 0; children && base < nn && child < 0; base += 32) {
       const int i = base + lane;
-      const bool is = i < nn && par[i] == cur;
-      const int t = is ? tok[i] : -1;
+      const bool is = i < nn && sh.par[i] == cur;
+      const int t = is ? sh.tok[i] : -1;
       u64 w = 0;
       double u = 0.0;
       if (is && t >= 0 && t < V) {
@@ -401,7 +427,7 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
     if (lane == 0) { sh.child = child; sh.left = left; sh.n_refused = n_refused; sh.token = -1; sh.seg = kWarps - 1; sh.seg_before = 0; }
   }
   __syncthreads();
-  if (sh.child >= 0) return make_int2(sh.child, tok[sh.child]);
+  if (sh.child >= 0) return make_int2(sh.child, sh.tok[sh.child]);
 
   // ---- 5. the drawn token, from what the refused children leave: first the 1/32 of the row that holds
   // it (a warp's share), then the token in it
@@ -410,13 +436,13 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
     else atomicOr(&s_gone[sh.refused[j] >> 5], 1u << (sh.refused[j] & 31));
   }
   __syncthreads();
-  auto rest_weight = [&](int v) -> u64 {
+  auto rest_weight = [&](int v, float x) -> u64 {
     if (!KEPT && ((s_gone[v >> 5] >> (v & 31)) & 1u)) return 0ull;
-    return kept_weight(get(v), v);
+    return kept_weight(x, v);
   };
-  const int per = ((V + kThreads - 1) / kThreads) * 32, v0 = min(V, warp * per), v1 = min(V, v0 + per);
+  const int per = (units + kWarps - 1) / kWarps, u0 = min(units, warp * per), u1 = min(units, u0 + per);
   u64 sum = 0;
-  for (int v = v0 + lane; v < v1; v += 32) sum += rest_weight(v);
+  each(u0 + lane, u1, 32, [&](int v, float x) { sum += rest_weight(v, x); });
   sum = warp_sum(sum);
   if (lane == 0) sh.sum[warp] = sum;
   __syncthreads();
@@ -426,10 +452,11 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
     if ((double)upto > goal && !((double)(upto - mine) > goal)) { sh.seg = lane; sh.seg_before = upto - mine; }
   }
   __syncthreads();
-  const int s0 = min(V, sh.seg * per), s1 = min(V, s0 + per);
+  const int g0 = min(units, sh.seg * per), g1 = min(units, g0 + per);
+  const int s0 = max(KEPT ? g0 * kPer - shift : g0, 0), s1 = min(V, KEPT ? g1 * kPer - shift : g1);
   u64 before = sh.seg_before;
   for (int base = s0; base < s1; base += kThreads) {      // (more than one round for more than 32768 tokens)
-    const u64 mine = base + tid < s1 ? rest_weight(base + tid) : 0ull;
+    const u64 mine = base + tid < s1 ? rest_weight(base + tid, get(base + tid)) : 0ull;
     const u64 upto = before + block_scan(sh, mine);
     if ((double)upto > goal && !((double)(upto - mine) > goal)) sh.token = base + tid;
     if (tid == kThreads - 1) sh.above = upto;
@@ -445,7 +472,7 @@ __device__ __forceinline__ void fill_table(Shared& sh) {
 
 // One block per context walks.
 template <typename T, bool KEPT>
-__global__ void __launch_bounds__(kThreads) rest_accept_sampled_walk_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, 1) rest_accept_sampled_walk_kernel(const __grid_constant__ Args a) {
   extern __shared__ __align__(16) unsigned char s_row[];
   __shared__ Shared sh;
   fill_table(sh);
@@ -467,7 +494,7 @@ __global__ void __launch_bounds__(kThreads) rest_accept_sampled_walk_kernel(cons
 
 // Every row has a block; blockIdx.x = row, blockIdx.y = context.
 template <typename T, bool KEPT>
-__global__ void __launch_bounds__(kThreads) rest_accept_sampled_rows_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, 1) rest_accept_sampled_rows_kernel(const __grid_constant__ Args a) {
   extern __shared__ __align__(16) unsigned char s_row[];
   __shared__ Shared sh;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

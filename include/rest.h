@@ -482,7 +482,7 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
  *   d_temperature, d_top_p  float[B]; temperature 0: the largest logit, lowest token first (then
  *                   the call equals rest_accept on the rows' argmax); top_p >= 1: no cut
  *   outputs         as rest_accept; a row without a finite logit gives -1 for the last token
- *   Weights are held as integers of 2^-44 of the row's largest, of 28 bits (exact sums in any order:
+ *   Weights are held as integers of 2^-44 of the row's largest, of 27 bits (exact sums in any order:
  *   results never depend on scheduling); a token below 2^-45 of the largest counts as impossible.
  *   d_ws            optional scratch of rest_accept_sampled_workspace_bytes() bytes, 8-byte aligned
  *                   (the query answers for the current device and may be 0), not shared by calls

@@ -4,7 +4,7 @@
 // One block works on one row of logits at a time and says where a walk that reaches that row goes:
 // to a child, or to an end with a drawn token.  Its steps:
 //   1. the row into shared memory (larger ones are read again from L2), and its largest logit;
-//   2. every token's weight as an integer of 2^-44 of the largest (rounded to 28 bits), their sum, and
+//   2. every token's weight as an integer of 2^-44 of the largest (rounded to 27 bits), their sum, and
 //      the sums of bins of 1/16 in log2 - for tokens heavy enough to be in the nucleus: those below
 //      (1 - top_p) / V of the largest are not, whatever the rest of the row holds;
 //   3. with a nucleus: the bin in which the running sum reaches its target; the tokens of that bin (some
@@ -12,15 +12,14 @@
 //   4. the children of the row's node in index order;
 //   5. if none is accepted: the drawn token, by sums over the tokens in order.
 // Integer sums are exact, so the result depends neither on the order of addition nor on the number of
-// threads.  A weight is computed in 64 bits and off by 2^-28 of itself at most, either way alike: errors
-// of 32-bit arithmetic (the product of a far logit and 1 / temperature alone: 1e-6) would move the
-// borders between tokens often enough to be seen in a large batch.
+// threads.  A weight is off by 2^-27 of itself at most, either way alike: plain 32-bit arithmetic (the
+// product of a far logit and 1 / temperature alone: 1e-6) would move the borders between tokens often
+// enough to be seen in a large batch.
 //
 // A walk visits 1 + accepted rows of N + 1.  Either one block per context walks, a row after the
 // other, reading only those rows; or, when the rows of all contexts are few enough to run at once,
-// every row gets a block of its own and a second small kernel follows the outcomes.  Bound: a row of
-// 32000 takes about 10 double-precision instructions a token for the sums (64 lanes an SM), more than
-// its bytes take; a walk is a chain of such rows.
+// every row gets a block of its own and a second small kernel follows the outcomes.  Bound: instructions
+// (about 30 a token for the sums, more time than the row's bytes take), and a walk is a chain of rows.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -62,59 +61,65 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 }
 
 struct Shared {
-  double pow16[16];                             // 2^(j/16)
+  uint2 pow16[16];                              // 2^(26 + j/16) as a float and as an integer
   u64 sum[kWarps], left, above, seg_before;
   u64 w[kList];
   uint32_t key[kList];
   int idx[kList];
-  uint32_t bin_lo[kBins], bin_hi[kBins];        // sums of the low 14 and the higher bits of 28-bit weights
+  uint32_t bin_lo[kBins], bin_hi[kBins];        // sums of the low 14 and the higher bits of 27-bit weights
   uint32_t red[kWarps], cut_key;
   int32_t tok[REST_MAX_N], par[REST_MAX_N];
-  int cut_tie, bin, n_list, child, n_refused, refused[REST_MAX_N], token, seg, depth;
+  int cut_tie, bin, n_list, child, n_refused, refused[REST_MAX_N], token, seg;
 };
 
-// A row's scale: y = log2 of a token's weight = (x - top) * c
+// A row's scale: 16 log2 of a token's weight = (x - top) * c16, with c16 as a sum of two floats (held
+// below 1e30, where any two different logits are worlds apart)
 struct Row {
-  float top;
-  double c, top_d;
+  float top, c16_hi, c16_lo;
+  double c16;
   bool greedy, inf;
 };
 
-// log2 weight in sixteenths, rounded (monotonic in x), and the rest of y
-__device__ __forceinline__ bool split(const Row& r, float x, int& k, double& f) {
-  if (!(x > -INFINITY)) return false;
-  // float -> double by its bits (a conversion instruction runs at a quarter of the rate); denormals
-  // and zero come out as some 1e-38
-  const uint32_t b = __float_as_uint(x);
-  const double d = __hiloint2double((int)(((b & 0x7FFFFFFFu) >> 3) + 0x38000000u | (b & 0x80000000u)), (int)(b << 29));
-  const double y = (d - r.top_d) * r.c;         // exactly 0 for the largest, whatever the temperature
-  if (!(y >= -45.0)) return false;
-  constexpr double kMagic = 6755399441055744.0 / 16.0;       // 1.5 * 2^48: adding it rounds to 1/16
-  const double t = y + kMagic;
-  k = __double2loint(t);
-  f = y - (t - kMagic);
+// log2 weight in sixteenths, rounded (monotonic in x), and the rest f, |f| <= 1/2.  The product is kept to
+// 48 bits (its rounding error, the low half of c16, for fp32 logits the rounding of the difference too):
+// f is off by some 1e-8, where a plain product of a far logit would be off by 4e-5.  32-bit arithmetic
+// throughout: the same in 64 bits issues at half the rate and took twice the time.
+template <typename T>
+__device__ __forceinline__ bool split(const Row& r, float x, int& k, float& f) {
+  constexpr float kMagic = 12582912.f;          // 1.5 * 2^23: adding it rounds to an integer
+  const float d = __fsub_rn(x, r.top), y = __fmul_rn(d, r.c16_hi);
+  if (!(y >= -720.5f)) return false;            // below 2^-45, -infinity and NaN
+  float rest = fmaf(d, r.c16_lo, fmaf(d, r.c16_hi, -y));
+  if (sizeof(T) == 4) {
+    const float b = __fsub_rn(d, x), e = __fsub_rn(__fsub_rn(x, __fsub_rn(d, b)), __fadd_rn(r.top, b));
+    rest = fmaf(e, r.c16_hi, rest);
+  }
+  const float t = __fadd_rn(y, kMagic);
+  k = __float_as_int(t) - 0x4B400000;
+  f = __fadd_rn(__fsub_rn(y, __fsub_rn(t, kMagic)), rest);
   return true;
 }
-// The weight 2^(k/16 + f), |f| <= 1/32, as an integer m of 28 bits at most: m << up(k) in units of 2^-44.
-// The table and the Taylor series of 2^f to the fourth power (the fifth is 4e-11), rounded by adding 2^52.
-__device__ __forceinline__ int up(int k) { return 17 - min(-(k >> 4), 17); }
-__device__ __forceinline__ uint32_t weight28(const Shared& sh, int k, double f) {
-  constexpr double a1 = 0.6931471805599453, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4;
-  const double t = sh.pow16[k & 15];
-  const double scaled = __hiloint2double(__double2hiint(t) + (((k >> 4) + 44 - up(k)) << 20), __double2loint(t));
-  double p = fma(f, a4, a3);
-  p = fma(f, p, a2);
-  p = fma(f, p, a1);
-  p = fma(f, p, 1.0);
-  return (uint32_t)__double2loint(fma(p, scaled, 4503599627370496.0));
+// The weight 2^((k + f)/16) as an integer m of 27 bits at most: m << up(k) in units of 2^-44.  From a table
+// of 2^(j/16) and q = 2^(f/16) - 1 by its Taylor series (|q| < 0.022, the fifth power is 4e-11): q is off
+// by 2^-24 of itself, so the product by less than one.
+__device__ __forceinline__ int up(int k) { return max(18 + (k >> 4), 0); }
+__device__ __forceinline__ uint32_t weight27(const Shared& sh, int k, float f) {
+  constexpr double l = 0.6931471805599453 / 16.0;
+  constexpr float a1 = (float)l, a2 = (float)(l * l / 2), a3 = (float)(l * l * l / 6), a4 = (float)(l * l * l * l / 24);
+  const float q = f * fmaf(f, fmaf(f, fmaf(f, a4, a3), a2), a1);
+  const uint2 t = sh.pow16[k & 15];
+  const uint32_t m = t.y + (__float_as_uint(fmaf(__uint_as_float(t.x), q, 12582912.f)) - 0x4B400000u);
+  const int small = max(-18 - (k >> 4), 0);     // fewer bits below 2^-18 of the largest
+  return (m + ((1u << small) >> 1)) >> small;
 }
-__device__ __forceinline__ u64 weight_of(const Shared& sh, int k, double f) { return (u64)weight28(sh, k, f) << up(k); }
+__device__ __forceinline__ u64 weight_of(const Shared& sh, int k, float f) { return (u64)weight27(sh, k, f) << up(k); }
 // weight before the nucleus cut (see Row): an infinite logit takes all of the mass
+template <typename T>
 __device__ __forceinline__ u64 weight(const Shared& sh, const Row& r, float x) {
   if (r.inf || r.greedy) return x == r.top ? kOne : 0ull;
   int k;
-  double f;
-  return split(r, x, k, f) ? weight_of(sh, k, f) : 0ull;
+  float f;
+  return split<T>(r, x, k, f) ? weight_of(sh, k, f) : 0ull;
 }
 
 __device__ __forceinline__ u64 warp_sum(u64 x) {
@@ -153,9 +158,10 @@ __device__ __forceinline__ double uniform(const float* u, int s) {
 }
 
 // The outcome of row `cur` (-1: the root's) of context b: an accepted child, or -1 and the drawn token
-// (-1: nothing can be drawn).  children = false: a walk that is as deep as allowed only draws.
+// (-1: nothing can be drawn).  depth: nodes accepted on the way, -1: to be counted here; a walk that is as
+// deep as allowed only draws.
 template <typename T, bool KEPT>
-__device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int b, int cur, bool children) {
+__device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int b, int cur, int depth) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nn = min(max(a.n_nodes[b], 0), a.N);
   const int32_t *tok = a.tokens + (int64_t)b * a.N, *par = a.parents + (int64_t)b * a.N;
@@ -191,7 +197,7 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
   // ---- 1. the row and its largest logit; the tree
   uint32_t top = 0;
   __syncthreads();                              // the row before it is done with
-  for (int i = tid; i < nn; i += kThreads) { sh.tok[i] = tok[i]; sh.par[i] = par[i]; }
+  for (int i = tid; i < a.N; i += kThreads) { sh.tok[i] = tok[i]; sh.par[i] = par[i]; }
   if (KEPT) {
     const T* base = row - shift;                // whole vectors inside the row; its ragged ends one by one
     const int first = shift ? 1 : 0, last = (shift + V) / kPer;
@@ -235,8 +241,9 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
   r.top = of_key(top);
   r.greedy = !(temp > 0.f);
   r.inf = r.top == INFINITY;
-  r.c = r.greedy ? 0.0 : 1.4426950408889634 / (double)temp;
-  r.top_d = (double)r.top;
+  r.c16 = r.greedy ? 0.0 : fmin(16.0 * 1.4426950408889634 / (double)temp, 1e30);
+  r.c16_hi = (float)r.c16;
+  r.c16_lo = (float)(r.c16 - (double)r.c16_hi);
   const bool smooth = !r.greedy && !r.inf;      // weights between 0 and 1
 
   // ---- 2. the mass, and the bins' if there will be a cut
@@ -247,9 +254,9 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
     const int bins = cut ? (top_p > 0.f ? min(kBins, (int)(16.f * (log2f((float)V) - log2f(1.f - top_p))) + 3) : 1) : 0;
     each(tid, units, kThreads, [&](int, float x) {
       int k;
-      double f;
-      if (split(r, x, k, f)) {
-        const uint32_t w = weight28(sh, k, f);
+      float f;
+      if (split<T>(r, x, k, f)) {
+        const uint32_t w = weight27(sh, k, f);
         mass += (u64)w << up(k);
         if (-k < bins) {
           atomicAdd(&sh.bin_lo[max(-k, 0)], w & 0x3FFFu);
@@ -280,14 +287,14 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
       const int bin = sh.bin;
       above = sh.above;
       // a little wider than half a bin on both sides, so that only few tokens are looked at closely
-      x_hi = (float)(r.top_d - ((double)bin - 0.51) / 16.0 / r.c);
-      x_lo = (float)(r.top_d - ((double)bin + 0.51) / 16.0 / r.c);
+      x_hi = (float)((double)r.top - ((double)bin - 0.51) / r.c16);
+      x_lo = (float)((double)r.top - ((double)bin + 0.51) / r.c16);
       x_hi += fabsf(x_hi) * 1e-6f;
       x_lo -= fabsf(x_lo) * 1e-6f;
       each(tid, units, kThreads, [&](int v, float x) {
         int k;
-        double f;
-        if (x >= x_lo && x <= x_hi && split(r, x, k, f) && max(-k, 0) == bin) {
+        float f;
+        if (x >= x_lo && x <= x_hi && split<T>(r, x, k, f) && max(-k, 0) == bin) {
           const int at = atomicAdd(&sh.n_list, 1);
           if (at < kList) { sh.key[at] = key_of(x); sh.idx[at] = v; sh.w[at] = weight_of(sh, k, f); }
         }
@@ -323,8 +330,8 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
         uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
         each(tid, units, kThreads, [&](int, float x) {
           int k;
-          double f;
-          if (x >= x_lo && x <= x_hi && split(r, x, k, f) && max(-k, 0) == sh.bin) { kmin = min(kmin, key_of(x)); kmax = max(kmax, key_of(x)); }
+          float f;
+          if (x >= x_lo && x <= x_hi && split<T>(r, x, k, f) && max(-k, 0) == sh.bin) { kmin = min(kmin, key_of(x)); kmax = max(kmax, key_of(x)); }
         });
         kmin = __reduce_min_sync(0xFFFFFFFFu, kmin);
         kmax = __reduce_max_sync(0xFFFFFFFFu, kmax);
@@ -343,8 +350,8 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
         u64 more = 0;
         each(tid, units, kThreads, [&](int, float x) {
           int k;
-          double f;
-          if (x >= x_lo && x <= x_hi && key_of(x) >= mid && split(r, x, k, f) && max(-k, 0) == sh.bin) more += weight_of(sh, k, f);
+          float f;
+          if (x >= x_lo && x <= x_hi && key_of(x) >= mid && split<T>(r, x, k, f) && max(-k, 0) == sh.bin) more += weight_of(sh, k, f);
         });
         if (base + block_sum(sh, more) >= target) lo = mid; else hi = mid - 1;
       }
@@ -353,11 +360,11 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
       if (smooth)
         each(tid, units, kThreads, [&](int, float x) {
           int k;
-          double f;
-          if (x >= x_lo && x <= x_hi && key_of(x) > cut_key && split(r, x, k, f) && max(-k, 0) == sh.bin) over += weight_of(sh, k, f);
+          float f;
+          if (x >= x_lo && x <= x_hi && key_of(x) > cut_key && split<T>(r, x, k, f) && max(-k, 0) == sh.bin) over += weight_of(sh, k, f);
         });
       over = block_sum(sh, over);
-      const u64 one = weight(sh, r, of_key(cut_key)), ties = (target - base - over + one - 1) / one;
+      const u64 one = weight<T>(sh, r, of_key(cut_key)), ties = (target - base - over + one - 1) / one;
       // every warp counts in a run of its own; the warp whose run holds the last one finds it
       const int per = (units + kWarps - 1) / kWarps, u0 = min(units, warp * per), u1 = min(units, u0 + per);
       u64 mine = 0;
@@ -389,13 +396,18 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
   auto kept_weight = [&](float x, int v) -> u64 {
     const uint32_t key = key_of(x);
     if (key < cut_key || (key == cut_key && v > cut_tie)) return 0ull;
-    return weight(sh, r, x);
+    return weight<T>(sh, r, x);
   };
 
   // ---- 4. children, in index order
   if (warp == 0) {
     int child = -1, n_refused = 0;
     u64 left = mass;
+    if (depth < 0) {                            // (as far as it matters; no walk gets to deeper rows)
+      depth = 0;
+      for (int i = cur; i >= 0 && i < a.N && depth <= a.max_depth; i = sh.par[i]) ++depth;
+    }
+    const bool children = depth < a.max_depth;
     for (int base = 0; children && base < nn && child < 0; base += 32) {
       const int i = base + lane;
       const bool is = i < nn && sh.par[i] == cur;
@@ -467,7 +479,10 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
 }
 
 __device__ __forceinline__ void fill_table(Shared& sh) {
-  if (threadIdx.x < 16) sh.pow16[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+  if (threadIdx.x < 16) {
+    const double p = exp2(26.0 + (double)threadIdx.x / 16.0);
+    sh.pow16[threadIdx.x] = make_uint2(__float_as_uint((float)p), (uint32_t)(p + 0.5));
+  }
 }
 
 // One block per context walks.
@@ -481,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 1) rest_accept_sampled_walk_kernel(c
   int32_t *an = a.accept_nodes + (int64_t)b * a.max_depth, *ot = a.out_tokens + (int64_t)b * (a.max_depth + 1);
   int cur = -1, len = 0;
   for (;;) {
-    const int2 o = row_outcome<T, KEPT>(a, sh, s_row, b, cur, len < a.max_depth);
+    const int2 o = row_outcome<T, KEPT>(a, sh, s_row, b, cur, len);
     if (tid == 0) ot[len] = o.y;
     if (o.x < 0) break;
     if (tid == 0) an[len] = o.x;
@@ -502,15 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1) rest_accept_sampled_rows_kernel(c
   grid_wait();
   const int b = blockIdx.y, cur = (int)blockIdx.x - 1, tid = threadIdx.x;
   if (cur >= min(max(a.n_nodes[b], 0), a.N)) return;
-  if (tid == kThreads - 1) {                    // how deep a walk is when it gets here, as far as that matters
-    int depth = 0;
-    for (int i = cur; i >= 0 && i < a.N && depth <= a.max_depth; i = a.parents[(int64_t)b * a.N + i]) ++depth;
-    sh.depth = depth;
-  }
-  __syncthreads();
-  const int depth = sh.depth;
-  if (depth > a.max_depth) return;              // no walk does
-  const int2 o = row_outcome<T, KEPT>(a, sh, s_row, b, cur, depth < a.max_depth);
+  const int2 o = row_outcome<T, KEPT>(a, sh, s_row, b, cur, -1);
   if (tid == 0) a.outcome[(int64_t)b * (a.N + 1) + cur + 1] = o;
 }
 

@@ -480,10 +480,11 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
  *   d_tokens, d_parents int32[B,N], d_n_nodes int32[B]: the tree, as written by rest_draft
  *   d_uniforms      float[B,N+1], in [0, 1)
  *   d_temperature, d_top_p  float[B]; temperature 0: the largest logit, lowest token first (then
- *                   the call equals rest_accept on the rows' argmax); top_p >= 1: no cut
+ *                   the call equals rest_accept on the rows' argmax), above 1e30: 1e30; top_p >= 1:
+ *                   no cut
  *   outputs         as rest_accept; a row without a finite logit gives -1 for the last token
  *   Weights are held as integers of 2^-44 of the row's largest, of 27 bits (exact sums in any order:
- *   results never depend on scheduling); a token below 2^-45 of the largest counts as impossible.
+ *   results never depend on scheduling); a token below 2^-44 of the largest counts as impossible.
  *   d_ws            optional scratch of rest_accept_sampled_workspace_bytes() bytes, 8-byte aligned
  *                   (the query answers for the current device and may be 0), not shared by calls
  *                   that may run at the same time.  Only for speed: with it the rows of few

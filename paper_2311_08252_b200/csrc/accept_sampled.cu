@@ -62,64 +62,60 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 
 struct Shared {
   uint2 pow16[16];                              // 2^(26 + j/16) as a float and as an integer
-  u64 sum[kWarps], left, above, seg_before;
-  u64 w[kList];
-  uint32_t key[kList];
-  int idx[kList];
+  u64 sum[kWarps], left, above, seg_before, cut;
+  ulonglong2 list[kList];                       // {order: key, then ~index; weight}, largest order first
   uint32_t bin_lo[kBins], bin_hi[kBins];        // sums of the low 14 and the higher bits of 27-bit weights
-  uint32_t red[kWarps], cut_key;
+  uint32_t red[kWarps], red2[kWarps];
   int32_t tok[REST_MAX_N], par[REST_MAX_N];
   int cut_tie, bin, n_list, child, n_refused, refused[REST_MAX_N], token, seg;
 };
 
 // A row's scale: 16 log2 of a token's weight = (x - top) * c16, with c16 as a sum of two floats (held
-// below 1e30, where any two different logits are worlds apart)
+// below 1e30, where any two different logits are worlds apart); differences beyond `least` weigh nothing
 struct Row {
-  float top, c16_hi, c16_lo;
+  float top, c16_hi, c16_lo, least;
   double c16;
   bool greedy, inf;
 };
 
-// log2 weight in sixteenths, rounded (monotonic in x), and the rest f, |f| <= 1/2.  The product is kept to
-// 48 bits (its rounding error, the low half of c16, for fp32 logits the rounding of the difference too):
-// f is off by some 1e-8, where a plain product of a far logit would be off by 4e-5.  32-bit arithmetic
-// throughout: the same in 64 bits issues at half the rate and took twice the time.
+// log2 weight in sixteenths, rounded (monotonic in x), and the rest f, |f| <= 1/2; no branches.  The
+// product is kept to 48 bits (its rounding error, the low half of c16, for fp32 logits the rounding of the
+// difference too): f is off by some 1e-8, where a plain product of a far logit would be off by 4e-5.
+// 32-bit arithmetic throughout: 64-bit instructions issue at half the rate.
 template <typename T>
-__device__ __forceinline__ bool split(const Row& r, float x, int& k, float& f) {
+__device__ __forceinline__ void split(const Row& r, float x, int& k, float& f) {
   constexpr float kMagic = 12582912.f;          // 1.5 * 2^23: adding it rounds to an integer
-  const float d = __fsub_rn(x, r.top), y = __fmul_rn(d, r.c16_hi);
-  if (!(y >= -720.5f)) return false;            // below 2^-45, -infinity and NaN
+  const float raw = __fsub_rn(x, r.top), d = fmaxf(raw, r.least), y = __fmul_rn(d, r.c16_hi);   // NaN: least
   float rest = fmaf(d, r.c16_lo, fmaf(d, r.c16_hi, -y));
   if (sizeof(T) == 4) {
-    const float b = __fsub_rn(d, x), e = __fsub_rn(__fsub_rn(x, __fsub_rn(d, b)), __fadd_rn(r.top, b));
-    rest = fmaf(e, r.c16_hi, rest);
+    const float b = __fsub_rn(raw, x), e = __fsub_rn(__fsub_rn(x, __fsub_rn(raw, b)), __fadd_rn(r.top, b));
+    rest = fmaf(raw > r.least ? e : 0.f, r.c16_hi, rest);
   }
   const float t = __fadd_rn(y, kMagic);
   k = __float_as_int(t) - 0x4B400000;
   f = __fadd_rn(__fsub_rn(y, __fsub_rn(t, kMagic)), rest);
-  return true;
 }
-// The weight 2^((k + f)/16) as an integer m of 27 bits at most: m << up(k) in units of 2^-44.  From a table
-// of 2^(j/16) and q = 2^(f/16) - 1 by its Taylor series (|q| < 0.022, the fifth power is 4e-11): q is off
-// by 2^-24 of itself, so the product by less than one.
-__device__ __forceinline__ int up(int k) { return max(18 + (k >> 4), 0); }
-__device__ __forceinline__ uint32_t weight27(const Shared& sh, int k, float f) {
+// The weight 2^((k + f)/16) in units of 2^-44, of 27 bits at most (see up).  From a table of 2^(j/16) and
+// q = 2^(f/16) - 1 by its Taylor series (|q| < 0.022, the fifth power is 4e-11): q is off by 2^-24 of
+// itself, so the product of 27 bits by less than one.
+__device__ __forceinline__ u64 weight_of(const Shared& sh, int k, float f) {
   constexpr double l = 0.6931471805599453 / 16.0;
   constexpr float a1 = (float)l, a2 = (float)(l * l / 2), a3 = (float)(l * l * l / 6), a4 = (float)(l * l * l * l / 24);
   const float q = f * fmaf(f, fmaf(f, fmaf(f, a4, a3), a2), a1);
   const uint2 t = sh.pow16[k & 15];
   const uint32_t m = t.y + (__float_as_uint(fmaf(__uint_as_float(t.x), q, 12582912.f)) - 0x4B400000u);
-  const int small = max(-18 - (k >> 4), 0);     // fewer bits below 2^-18 of the largest
-  return (m + ((1u << small) >> 1)) >> small;
+  return ((u64)m << 18) >> -(k >> 4);
 }
-__device__ __forceinline__ u64 weight_of(const Shared& sh, int k, float f) { return (u64)weight27(sh, k, f) << up(k); }
+// zero bits at the end of such a weight
+__device__ __forceinline__ int up(int k) { return max(18 + (k >> 4), 0); }
 // weight before the nucleus cut (see Row): an infinite logit takes all of the mass
 template <typename T>
 __device__ __forceinline__ u64 weight(const Shared& sh, const Row& r, float x) {
   if (r.inf || r.greedy) return x == r.top ? kOne : 0ull;
   int k;
   float f;
-  return split<T>(r, x, k, f) ? weight_of(sh, k, f) : 0ull;
+  split<T>(r, x, k, f);
+  return weight_of(sh, k, f);
 }
 
 __device__ __forceinline__ u64 warp_sum(u64 x) {
@@ -241,9 +237,10 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
   r.top = of_key(top);
   r.greedy = !(temp > 0.f);
   r.inf = r.top == INFINITY;
-  r.c16 = r.greedy ? 0.0 : fmin(16.0 * 1.4426950408889634 / (double)temp, 1e30);
+  r.c16 = r.greedy ? 0.0 : 16.0 * 1.4426950408889634 / fmax((double)fminf(temp, 1e30f), 1e-29);
   r.c16_hi = (float)r.c16;
   r.c16_lo = (float)(r.c16 - (double)r.c16_hi);
+  r.least = r.greedy ? 0.f : (float)(-760.0 / r.c16);     // 2^-47.5: rounds to nothing
   const bool smooth = !r.greedy && !r.inf;      // weights between 0 and 1
 
   // ---- 2. the mass, and the bins' if there will be a cut
@@ -255,13 +252,13 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
     each(tid, units, kThreads, [&](int, float x) {
       int k;
       float f;
-      if (split<T>(r, x, k, f)) {
-        const uint32_t w = weight27(sh, k, f);
-        mass += (u64)w << up(k);
-        if (-k < bins) {
-          atomicAdd(&sh.bin_lo[max(-k, 0)], w & 0x3FFFu);
-          atomicAdd(&sh.bin_hi[max(-k, 0)], w >> 14);
-        }
+      split<T>(r, x, k, f);
+      const u64 w = weight_of(sh, k, f);
+      mass += w;
+      if (-k < bins) {
+        const uint32_t m = (uint32_t)(w >> up(k));
+        atomicAdd(&sh.bin_lo[-k], m & 0x3FFFu);
+        atomicAdd(&sh.bin_hi[-k], m >> 14);
       }
     });
   } else {
@@ -294,9 +291,11 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
       each(tid, units, kThreads, [&](int v, float x) {
         int k;
         float f;
-        if (x >= x_lo && x <= x_hi && split<T>(r, x, k, f) && max(-k, 0) == bin) {
+        if (!(x >= x_lo && x <= x_hi)) return;
+        split<T>(r, x, k, f);
+        if (-k == bin) {
           const int at = atomicAdd(&sh.n_list, 1);
-          if (at < kList) { sh.key[at] = key_of(x); sh.idx[at] = v; sh.w[at] = weight_of(sh, k, f); }
+          if (at < kList) sh.list[at] = make_ulonglong2((u64)key_of(x) << 32 | (uint32_t)~v, weight_of(sh, k, f));
         }
       });
       __syncthreads();
@@ -307,39 +306,39 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
         int parts = 1;
         while (parts < 32 && n * parts * 2 <= kThreads) parts *= 2;
         const int e = tid / parts, part = tid % parts;
-        const uint32_t key = e < n ? sh.key[e] : 0u;
-        const int idx = e < n ? sh.idx[e] : 0;
+        const ulonglong2 mine = e < n ? sh.list[e] : make_ulonglong2(~0ull, 0ull);
         u64 before = 0;
-        if (e < n)
-          for (int j = part; j < n; j += parts) {
-            const uint32_t other = sh.key[j];
-            if (other > key || (other == key && sh.idx[j] < idx)) before += sh.w[j];
-          }
+#pragma unroll 8
+        for (int j = part; j < n; j += parts) {
+          const ulonglong2 other = sh.list[j];
+          before += other.x > mine.x ? other.y : 0ull;
+        }
         for (int d = 1; d < parts; d <<= 1) before += __shfl_xor_sync(0xFFFFFFFFu, before, d);
         before += above;
-        if (e < n && part == 0 && before < target && before + sh.w[e] >= target) {
-          sh.cut_key = key;
-          sh.cut_tie = idx;
-          sh.left = before + sh.w[e];
+        if (e < n && part == 0 && before < target && before + mine.y >= target) {
+          sh.cut = mine.x;
+          sh.left = before + mine.y;
         }
         __syncthreads();
-        cut_key = sh.cut_key;
-        cut_tie = sh.cut_tie;
+        cut_key = (uint32_t)(sh.cut >> 32);
+        cut_tie = (int)~(uint32_t)sh.cut;
         mass = sh.left;
       } else {                                  // a crowd in one bin (flat rows): bisect its keys
         uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
         each(tid, units, kThreads, [&](int, float x) {
           int k;
           float f;
-          if (x >= x_lo && x <= x_hi && split<T>(r, x, k, f) && max(-k, 0) == sh.bin) { kmin = min(kmin, key_of(x)); kmax = max(kmax, key_of(x)); }
+          if (!(x >= x_lo && x <= x_hi)) return;
+          split<T>(r, x, k, f);
+          if (-k == sh.bin) { kmin = min(kmin, key_of(x)); kmax = max(kmax, key_of(x)); }
         });
         kmin = __reduce_min_sync(0xFFFFFFFFu, kmin);
         kmax = __reduce_max_sync(0xFFFFFFFFu, kmax);
         __syncthreads();
-        if (lane == 0) { sh.red[warp] = kmin; sh.idx[warp] = (int)kmax; }
+        if (lane == 0) { sh.red[warp] = kmin; sh.red2[warp] = kmax; }
         __syncthreads();
         lo = __reduce_min_sync(0xFFFFFFFFu, sh.red[lane]);
-        hi = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)sh.idx[lane]);
+        hi = __reduce_max_sync(0xFFFFFFFFu, sh.red2[lane]);
       }
     }
     if (!ordered) {
@@ -351,7 +350,9 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
         each(tid, units, kThreads, [&](int, float x) {
           int k;
           float f;
-          if (x >= x_lo && x <= x_hi && key_of(x) >= mid && split<T>(r, x, k, f) && max(-k, 0) == sh.bin) more += weight_of(sh, k, f);
+          if (!(x >= x_lo && x <= x_hi && key_of(x) >= mid)) return;
+          split<T>(r, x, k, f);
+          if (-k == sh.bin) more += weight_of(sh, k, f);
         });
         if (base + block_sum(sh, more) >= target) lo = mid; else hi = mid - 1;
       }
@@ -361,7 +362,9 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
         each(tid, units, kThreads, [&](int, float x) {
           int k;
           float f;
-          if (x >= x_lo && x <= x_hi && key_of(x) > cut_key && split<T>(r, x, k, f) && max(-k, 0) == sh.bin) over += weight_of(sh, k, f);
+          if (!(x >= x_lo && x <= x_hi && key_of(x) > cut_key)) return;
+          split<T>(r, x, k, f);
+          if (-k == sh.bin) over += weight_of(sh, k, f);
         });
       over = block_sum(sh, over);
       const u64 one = weight<T>(sh, r, of_key(cut_key)), ties = (target - base - over + one - 1) / one;

@@ -192,7 +192,7 @@ def accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature, top_
             if temperature[b] > 0:
                 with np.errstate(invalid="ignore", over="ignore"):
                     w = np.where(x == x.max(), 1.0, np.exp((x - x.max()) / np.float64(temperature[b])))
-                w[w < 2.0 ** -45] = 0.0
+                w[w < 2.0 ** -44] = 0.0
                 if top_p[b] < 1:
                     before = np.cumsum(w[order]) - w[order]
                     drop = before >= np.float64(top_p[b]) * w.sum()

@@ -171,9 +171,10 @@ __device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&r)
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
       : "memory");
 }
-// TMEM columns taddr .. of the thread's lane into registers.  The wait names the values, so that nothing
-// that uses them can move ahead of it.
-__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[16]) {
+// 16 TMEM columns from taddr of the thread's lane into registers: tmem_issue starts, tmem_wait_ld waits for
+// all that was started, and tmem_named keeps whatever uses the values from moving ahead of that wait.
+// (Values are kept in arrays of 16, indexed by constants only: anything else lands in local memory.)
+__device__ __forceinline__ void tmem_issue(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
@@ -182,35 +183,27 @@ __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[16]) {
         "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
+}
+__device__ __forceinline__ void tmem_named(uint32_t (&r)[16]) {
+  asm volatile(""
       : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
         "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
         "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
       :
       : "memory");
 }
-__device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-      : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
-        "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
-        "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]),
-        "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
-        "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
-        "+r"(r[30]), "+r"(r[31])
-      :
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[16]) {
+  tmem_issue(taddr, r);
+  tmem_wait_ld();
+  tmem_named(r);
+}
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
-}
-__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[32]) {
-  tmem_ld_32x32(taddr, r);
-  tmem_wait_ld_of(r);
-}
-__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[64]) {
-  uint32_t (&lo)[32] = *reinterpret_cast<uint32_t (*)[32]>(&r[0]);
-  uint32_t (&hi)[32] = *reinterpret_cast<uint32_t (*)[32]>(&r[32]);
-  tmem_ld_32x32(taddr, lo);
-  tmem_ld_32x32(taddr + 32, hi);
-  tmem_wait_ld_of(lo);
-  tmem_wait_ld_of(hi);
 }
 
 __device__ unsigned int g_paged_error;                  // bit 0: wait gave up, bit 1: smem misaligned
@@ -227,13 +220,13 @@ template <int D, int NT> struct Shape {
   static constexpr int kThreads = 32 * (kSoftmax + 2 + NT);
   static constexpr uint32_t kTmem = NT == 1 ? 256 : 512;
   static constexpr uint32_t kColO = 2 * NT * BN;        // behind two S buffers for each row tile
-  static constexpr int kStage = D == 128 ? 32 : 16;     // columns joined at a time through the Q tile's memory
+  static constexpr int kStage = 16;                     // columns joined at a time through the Q tile's memory
 };
 // byte offsets behind kBars
 enum {
   kKFull = 0, kKFree = 32, kVFull = 64, kVFree = 112, kSFull = 160, kPFull = 192, kOFull = 224, kQFull = 240, kQFree = 248,
   kTmemSlot = 256, kAbort = 260, kBad = 264 /* 8 x 4 */, kStartB = 296, kStartOff = 304, kTotal = 312,
-  kScan = 320 /* 12 x 8 */, kJoin = 416
+  kScan = 320 /* 12 x 8 */, kJoin = 416, kTurn = 424 /* 8 x 8 */
 };
 
 // Bounded wait of a whole warp, with one result for all lanes (TMEM accesses and elected lanes need
@@ -277,10 +270,10 @@ __device__ __forceinline__ int node_depth(const Args& a, int b, int i) {
   for (int w = 0; w < a.Wm; ++w) d += __popc(__ldg(m + w));
   return d;
 }
-// every row of the block sees every key of the tile at key0
+// every row of the block sees every key of the tile at key0 (tiles of the sinks count as masked)
 template <int BN>
 __device__ __forceinline__ bool all_see(const Args& a, const Ctx& c, int key0) {
-  return key0 + BN <= c.L && (a.window == 0 || key0 + BN <= a.sinks || key0 > c.L + c.n - 1 - a.window);
+  return key0 + BN <= c.L && (a.window == 0 || key0 > c.L + c.n - 1 - a.window);
 }
 // which of the keys k0 .. k0 + 63 node i (of depth `depth`) of context b sees
 __device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int depth, int k0) {
@@ -315,10 +308,10 @@ __device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int dept
   return v;
 }
 
-// What was taken out of V (see below), added to columns d0 .. d0 + cols - 1 of a row that
-// does see its key.
+// What was taken out of V (see below), added to columns d0 .. d0 + 15 of a row that does
+// see its key.
 template <typename T, int BN>
-__device__ __noinline__ void add_back(const Args& a, Piece p, int node, int depth, int d0, int cols, uint32_t* o) {
+__device__ __noinline__ void add_back(const Args& a, Piece p, int node, int depth, int d0, uint32_t (&o)[16]) {
   for (int it = 0; it < p.len; ++it) {
     const int key0 = tile_key<BN>(p.c, p.t0 + it);
     if (all_see<BN>(a, p.c, key0)) continue;
@@ -329,7 +322,7 @@ __device__ __noinline__ void add_back(const Args& a, Piece p, int node, int dept
         if (page < 0 || page >= a.P) continue;
         const T* v = static_cast<const T*>(a.v) + page * a.p_p + p.hk * a.p_h +
                      (key & ((1 << a.page_log) - 1)) * a.p_r + d0;
-        for (int j = 0; j < cols; ++j) {
+        for (int j = 0; j < 16; ++j) {
           const float f = (float)v[j];
           if (!isfinite(f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + f);
         }
@@ -372,7 +365,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     mbar_init(bars + kQFull, 1);
     mbar_init(bars + kQFree, NT);                       // one arrival per row tile
     mbar_init(bars + kJoin, S_::kSoftmax);
-    for (int i = 0; i < 8; ++i) s_bad[i] = 0;
+    for (int i = 0; i < 8; ++i) { s_bad[i] = 0; mbar_init(bars + kTurn + 8 * i, 1); }
     *abort_word = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -619,7 +612,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t o_col = tmem + lanes + S_::kColO + s * 128;
     auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return wait_warp(bar, parity, abort_word); };
-    uint32_t n = 0, base = 0, joins = 0;
+    uint32_t n = 0, base = 0, joins = 0, e_n = 0;
     int piece = 0;
     bool ok = true;
     for (; ok && walk.next(p); base += p.len) {
@@ -632,12 +625,22 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       const int node = live ? node_of(a, r0 + tr) : 0, head = p.hk * a.G + (live ? r0 + tr - node * a.G : 0);
       const int depth = live && a.window > 0 ? node_depth(a, p.b, node) : 1;   // (only windows need it)
       float m_used = -INFINITY, l_run = 0.f;
+      // tiles [clear0, clear1) of the piece are those that all rows see whole (see all_see)
+      const int at0 = p.c.ns - p.c.w0 - p.t0;
+      const int clear0 = a.window == 0 ? 0 : at0 + (max(p.c.L + p.c.n - a.window, 0) + BN - 1) / BN, clear1 = at0 + p.c.L / BN;
       int it = turns ? s : 0;
+      constexpr int kParts = KP / 16;
+      // Two row tiles of the same piece work on the same key tiles, and each scheduler has one warp of either.
+      // Left alone they fall into step, both at their exponentials and then both at everything else; taking
+      // turns at the exponentials (the first tile before the second, the second before the first's next)
+      // keeps the special function unit fed.
+      const bool paired = NT == 2 && !turns && (warp & 3) * 32 + 128 < p.rows;
+      const uint32_t my_turn = bars + kTurn + 8 * (warp & 7), other_turn = bars + kTurn + 8 * ((warp & 7) ^ 4);
       for (bool fresh = true; it < p.len; it += step, fresh = false) {
-        const int key0 = tile_key<BN>(p.c, p.t0 + it);
-        const uint32_t buf = 2 * s + (n & 1), par = (n >> 1) & 1;
-        const bool plain = all_see<BN>(a, p.c, key0);
+        const uint32_t buf = 2 * s + (n & 1);
+        const bool plain = it >= clear0 && it < clear1;
         if (!plain) {
+          const int key0 = tile_key<BN>(p.c, p.t0 + it);
           // Values of V that are not finite would reach rows that do not see their key (0 x NaN): take
           // them out of the tile, and remember the piece if the key exists (see the epilogue).  Both row
           // tiles do it when both use the tile, each before its own P V; the piece is remembered before a
@@ -665,39 +668,44 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           }
           fence_async_smem();
         }
-        if (!wait(bars + kSFull + buf * 8, par)) { ok = false; break; }
+        if (!wait(bars + kSFull + buf * 8, (n >> 1) & 1)) { ok = false; break; }
         tc_fence_after();
         if (warp_live) {
           const uint32_t s_col = tmem + lanes + buf * BN;
-          uint32_t x[KP];
-          tmem_load(s_col + ci * KP, x);
+          uint32_t x[kParts][16];
+#pragma unroll
+          for (int c = 0; c < kParts; ++c) tmem_issue(s_col + ci * KP + c * 16, x[c]);
+          tmem_wait_ld();
+#pragma unroll
+          for (int c = 0; c < kParts; ++c) tmem_named(x[c]);
           if (!plain) {
+            const int key0 = tile_key<BN>(p.c, p.t0 + it);
             const u64 vis = live ? visible(a, p.c, p.b, node, depth, key0) >> (ci * KP) : 0ull;
             const uint32_t lo = (uint32_t)vis, hi = (uint32_t)(vis >> 32);
 #pragma unroll
             for (int j = 0; j < KP; ++j)
-              if (!(((j < 32 ? lo : hi) >> (j & 31)) & 1u)) x[j] = 0xFF800000u;       // -inf
+              if (!(((j < 32 ? lo : hi) >> (j & 31)) & 1u)) x[j / 16][j % 16] = 0xFF800000u;       // -inf
           }
           // maximum of the raw scores (the scale is positive, so it commutes with max); the scale
           // is applied inside the exponent's multiply-add
           float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int j = 0; j < KP / 2; ++j)
-            mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
+            mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[j / 8][2 * (j % 8)]), __uint_as_float(x[j / 8][2 * (j % 8) + 1]));
           const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
-          if (__any_sync(0xFFFFFFFFu, mx > m_used + kRescaleStep)) {
+          if (__any_sync(0xFFFFFFFFu, live && mx > m_used + kRescaleStep)) {
             const float m_new = fmaxf(m_used, mx);
             const float alpha = m_new == -INFINITY ? 1.f : ex2(m_used - m_new);   // m_used = -inf gives 0
             if (!fresh) {
               if (!wait(bars + kOFull + s * 8, (n - 1) & 1)) { ok = false; break; }
               tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < D / 16; ++c) {
+                uint32_t o[16];
+                tmem_load(o_col + c * 16, o);
 #pragma unroll
-              for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                tmem_load(o_col + c * 32, o);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-                tmem_st_32x32(o_col + c * 32, o);
+                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                tmem_st_32x16(o_col + c * 16, o);
               }
             }
             l_run *= alpha;
@@ -705,27 +713,32 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           }
           const float neg = m_used == -INFINITY ? 0.f : -m_used;
           float ps[4] = {0.f, 0.f, 0.f, 0.f};
-          // P: 64 keys in 32 packed columns over S's first half, eight columns at a time
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (C == 1 || c / (4 / C) == ci) {          // (warp-uniform)
-              const int c0 = C == 1 ? c : c % (4 / C);
-              uint32_t pk[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                float e0, e1;
-                fma2(e0, e1, __uint_as_float(x[c0 * 16 + 2 * j]), __uint_as_float(x[c0 * 16 + 2 * j + 1]), a.scale_log2, neg);
-                e0 = ex2(e0);
-                e1 = ex2(e1);
-                add2(ps[(j & 1) * 2], ps[(j & 1) * 2 + 1], e0, e1);
-                pk[j] = Type<T>::pack(e0, e1);
-              }
-              tmem_st_32x8(s_col + c * 8, pk);
-            } else {
-              const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-              tmem_st_32x8(s_col + c * 8, zero);
-            }
+          if (paired) {
+            if ((s == 1 || e_n > 0) && !wait(other_turn, (s == 1 ? e_n : e_n - 1) & 1)) { ok = false; break; }
+            ++e_n;
           }
+          // P: 64 keys in 32 packed columns over S's first half, eight columns (16 keys) at a time
+#pragma unroll
+          for (int c = 0; c < kParts; ++c) {
+            uint32_t pk[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              float e0, e1;
+              fma2(e0, e1, __uint_as_float(x[c][2 * j]), __uint_as_float(x[c][2 * j + 1]), a.scale_log2, neg);
+              e0 = ex2(e0);
+              e1 = ex2(e1);
+              add2(ps[(j & 1) * 2], ps[(j & 1) * 2 + 1], e0, e1);
+              pk[j] = Type<T>::pack(e0, e1);
+            }
+            tmem_st_32x8(s_col + (ci * kParts + c) * 8, pk);
+          }
+          if (C > 1) {                                  // the other copies' keys
+            const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (c / kParts != ci) tmem_st_32x8(s_col + c * 8, zero);     // (warp-uniform)
+          }
+          if (paired && lane == 0) mbar_arrive(my_turn);
           l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
           tmem_wait_st();
         }
@@ -746,25 +759,25 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         const float w = p.whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f;
         if (warp_live) {
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t o[16];
             __syncwarp();
-            tmem_load(o_col + c * 32, o);
+            tmem_load(o_col + c * 16, o);
             if (!live) continue;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
+            for (int j = 0; j < 16; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
             if (bad) {                                  // rare; a copy, so that o stays in registers otherwise
-              uint32_t y[32];
+              uint32_t y[16];
 #pragma unroll
-              for (int j = 0; j < 32; ++j) y[j] = o[j];
-              add_back<T, BN>(a, p, node, depth, c * 32, 32, y);
+              for (int j = 0; j < 16; ++j) y[j] = o[j];
+              add_back<T, BN>(a, p, node, depth, c * 16, y);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = y[j];
+              for (int j = 0; j < 16; ++j) o[j] = y[j];
             }
             if (p.whole) {
-              T* op = static_cast<T*>(a.out) + mine + c * 32;
+              T* op = static_cast<T*>(a.out) + mine + c * 16;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
+              for (int e = 0; e < 2; ++e) {
                 uint32_t v[4];
 #pragma unroll
                 for (int f = 0; f < 4; ++f)
@@ -772,9 +785,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
                 *reinterpret_cast<uint4*>(op + e * 8) = make_uint4(v[0], v[1], v[2], v[3]);
               }
             } else {
-              float* wo = a.ws_o + mine + c * 32;
+              float* wo = a.ws_o + mine + c * 16;
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
+              for (int e = 0; e < 2; ++e)
                 asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(wo + 8 * e), "r"(o[8 * e]),
                              "r"(o[8 * e + 1]), "r"(o[8 * e + 2]), "r"(o[8 * e + 3]), "r"(o[8 * e + 4]), "r"(o[8 * e + 5]),
                              "r"(o[8 * e + 6]), "r"(o[8 * e + 7])
@@ -838,7 +851,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             uint32_t y[kCols];
 #pragma unroll
             for (int j = 0; j < kCols; ++j) y[j] = o[j];
-            add_back<T, BN>(a, p, node, depth, c * kCols, kCols, y);
+            add_back<T, BN>(a, p, node, depth, c * kCols, y);
 #pragma unroll
             for (int j = 0; j < kCols; ++j) o[j] = y[j];
           }

@@ -275,8 +275,9 @@ template <int BN>
 __device__ __forceinline__ bool all_see(const Args& a, const Ctx& c, int key0) {
   return key0 + BN <= c.L && (a.window == 0 || key0 > c.L + c.n - 1 - a.window);
 }
-// which of the keys k0 .. k0 + 63 node i (of depth `depth`) of context b sees
-__device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int depth, int k0) {
+// which of the keys k0 .. k0 + 63 node i (of depth `depth`) of context b sees; first: words 0 and 1 of its
+// mask row
+__device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int depth, u64 first, int k0) {
   const int pos = c.L + max(depth, 1) - 1;
   u64 v;
   if (a.window == 0)
@@ -288,8 +289,9 @@ __device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int dept
     if (a.mask) {
       const uint32_t* mp = a.mask + ((int64_t)b * a.N + i) * a.Wm;
 #pragma unroll
-      for (int w = 0; w < 8; ++w)
+      for (int w = 2; w < 8; ++w)
         if (w < a.Wm) m[w >> 1] |= (u64)__ldg(mp + w) << (32 * (w & 1));
+      m[0] = first;
     } else {
 #pragma unroll
       for (int w = 0; w < 4; ++w) m[w] = bits_between(0, i + 1 - 64 * w);
@@ -311,12 +313,12 @@ __device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int dept
 // What was taken out of V (see below), added to columns d0 .. d0 + 15 of a row that does
 // see its key.
 template <typename T, int BN>
-__device__ __noinline__ void add_back(const Args& a, Piece p, int node, int depth, int d0, uint32_t (&o)[16]) {
+__device__ __noinline__ void add_back(const Args& a, Piece p, int node, int depth, u64 mask0, int d0, uint32_t (&o)[16]) {
   for (int it = 0; it < p.len; ++it) {
     const int key0 = tile_key<BN>(p.c, p.t0 + it);
     if (all_see<BN>(a, p.c, key0)) continue;
     for (int h = 0; h < BN / 64; ++h) {
-      for (u64 vis = visible(a, p.c, p.b, node, depth, key0 + 64 * h); vis; vis &= vis - 1) {
+      for (u64 vis = visible(a, p.c, p.b, node, depth, mask0, key0 + 64 * h); vis; vis &= vis - 1) {
         const int key = key0 + 64 * h + __ffsll((long long)vis) - 1, col = key >> a.page_log;
         const int page = col < a.table_cols ? a.table[p.b * a.table_stride + col] : -1;
         if (page < 0 || page >= a.P) continue;
@@ -624,6 +626,12 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       const bool warp_live = tr - lane < rows, live = tr < rows;
       const int node = live ? node_of(a, r0 + tr) : 0, head = p.hk * a.G + (live ? r0 + tr - node * a.G : 0);
       const int depth = live && a.window > 0 ? node_depth(a, p.b, node) : 1;   // (only windows need it)
+      u64 mask0 = 0;                                    // (asked for now, needed in the last tiles)
+      if (live && a.mask) {
+        const uint32_t* mp = a.mask + ((int64_t)p.b * a.N + node) * a.Wm;
+        mask0 = __ldg(mp);
+        if (a.Wm > 1) mask0 |= (u64)__ldg(mp + 1) << 32;
+      }
       float m_used = -INFINITY, l_run = 0.f;
       // tiles [clear0, clear1) of the piece are those that all rows see whole (see all_see)
       const int at0 = p.c.ns - p.c.w0 - p.t0;
@@ -633,7 +641,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       // Two row tiles of the same piece work on the same key tiles, and each scheduler has one warp of either.
       // Left alone they fall into step, both at their exponentials and then both at everything else; taking
       // turns at the exponentials (the first tile before the second, the second before the first's next)
-      // keeps the special function unit fed.
+      // keeps the special function unit fed.  A turn ends half way: the second half fills the other's start
+      // (768 us at the end, 748 us half way, 845 us after a quarter, for 16 x 16384 keys and 640 rows).
       const bool paired = NT == 2 && !turns && (warp & 3) * 32 + 128 < p.rows;
       const uint32_t my_turn = bars + kTurn + 8 * (warp & 7), other_turn = bars + kTurn + 8 * ((warp & 7) ^ 4);
       for (bool fresh = true; it < p.len; it += step, fresh = false) {
@@ -654,14 +663,17 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             const uint32_t src = sV + slot * S_::kTile + at;
             uint32_t w[4];
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src) : "memory");
-            bool hit = false;
+            // an exponent of all ones carries into the bit above when a one is added at its end
+            constexpr uint32_t lo = Type<T>::exponent, hi = lo << 16, one = lo & (0u - lo);
+            uint32_t any = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              constexpr uint32_t lo = Type<T>::exponent, hi = lo << 16;
-              if ((w[e] & lo) == lo) { w[e] &= 0xFFFF0000u; hit = true; }
-              if ((w[e] & hi) == hi) { w[e] &= 0x0000FFFFu; hit = true; }
-            }
-            if (hit) {
+            for (int e = 0; e < 4; ++e) any |= (w[e] & (lo | hi)) + (one | one << 16);
+            if (any & 0x80008000u) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((w[e] & lo) == lo) w[e] &= 0xFFFF0000u;
+                if ((w[e] & hi) == hi) w[e] &= 0x0000FFFFu;
+              }
               if (key0 + (int)((at % (BN * 128)) >> 7) < p.c.L + p.c.n) { s_bad[piece & 7] = piece + 1; __threadfence_block(); }
               asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(src), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
             }
@@ -680,7 +692,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           for (int c = 0; c < kParts; ++c) tmem_named(x[c]);
           if (!plain) {
             const int key0 = tile_key<BN>(p.c, p.t0 + it);
-            const u64 vis = live ? visible(a, p.c, p.b, node, depth, key0) >> (ci * KP) : 0ull;
+            const u64 vis = live ? visible(a, p.c, p.b, node, depth, mask0, key0) >> (ci * KP) : 0ull;
             const uint32_t lo = (uint32_t)vis, hi = (uint32_t)(vis >> 32);
 #pragma unroll
             for (int j = 0; j < KP; ++j)
@@ -731,6 +743,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
               pk[j] = Type<T>::pack(e0, e1);
             }
             tmem_st_32x8(s_col + (ci * kParts + c) * 8, pk);
+            if (c == 1 && paired && lane == 0) mbar_arrive(my_turn);
           }
           if (C > 1) {                                  // the other copies' keys
             const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
@@ -738,7 +751,6 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             for (int c = 0; c < 4; ++c)
               if (c / kParts != ci) tmem_st_32x8(s_col + c * 8, zero);     // (warp-uniform)
           }
-          if (paired && lane == 0) mbar_arrive(my_turn);
           l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
           tmem_wait_st();
         }
@@ -770,7 +782,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
               uint32_t y[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) y[j] = o[j];
-              add_back<T, BN>(a, p, node, depth, c * 16, y);
+              add_back<T, BN>(a, p, node, depth, mask0, c * 16, y);
 #pragma unroll
               for (int j = 0; j < 16; ++j) o[j] = y[j];
             }
@@ -851,7 +863,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             uint32_t y[kCols];
 #pragma unroll
             for (int j = 0; j < kCols; ++j) y[j] = o[j];
-            add_back<T, BN>(a, p, node, depth, c * kCols, y);
+            add_back<T, BN>(a, p, node, depth, mask0, c * kCols, y);
 #pragma unroll
             for (int j = 0; j < kCols; ++j) o[j] = y[j];
           }
@@ -948,21 +960,32 @@ __global__ void __launch_bounds__(256) paged_attention_join_kernel(const __grid_
       auto at = [&](int i) -> int64_t {                 // piece i: slot 1 of the first block, slot 0 of the others
         return ((block + (int64_t)i * a.RB) * 2 + (i == 0 ? 1 : 0)) * a.rows + row;
       };
-      for (int i = lo + lane; i < hi; i += 32) m = fmaxf(m, a.ws_ml[at(i) * 2]);
+      for (int i0 = lo; i0 < hi; i0 += 32) {            // 32 pieces at a time, a lane for each one's maximum and sum
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (i0 + lane < hi) ml = *reinterpret_cast<const float2*>(a.ws_ml + at(i0 + lane) * 2);
+        float top = fmaxf(m, ml.x);
 #pragma unroll
-      for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-#pragma unroll 4
-      for (int i = lo; i < hi; ++i) {
-        const int64_t x = at(i);
-        const float2 ml = *reinterpret_cast<const float2*>(a.ws_ml + x * 2);
-        float v[E];
-        if constexpr (E == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(a.ws_o + x * D + lane * E);
-        else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(a.ws_o + x * D + lane * E);
-        const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - m);
-        l += ml.y * w;
+        for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - top), old = m == -INFINITY ? 0.f : ex2(m - top);
+        float sum = ml.y * w;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (w != 0.f) o[e] += v[e] * w;
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+        l = l * old + sum;
+        m = top;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= old;
+        const int count = min(32, hi - i0);
+#pragma unroll 8
+        for (int i = 0; i < count; ++i) {
+          const int64_t x = at(i0 + i);
+          float v[E];
+          if constexpr (E == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(a.ws_o + x * D + lane * E);
+          else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(a.ws_o + x * D + lane * E);
+          const float wi = __shfl_sync(0xFFFFFFFFu, w, i);
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (wi != 0.f) o[e] += v[e] * wi;
+        }
       }
     }
     if (wide) {

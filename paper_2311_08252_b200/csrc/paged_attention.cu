@@ -220,7 +220,6 @@ template <int D, int NT> struct Shape {
   static constexpr int kThreads = 32 * (kSoftmax + 2 + NT);
   static constexpr uint32_t kTmem = NT == 1 ? 256 : 512;
   static constexpr uint32_t kColO = 2 * NT * BN;        // behind two S buffers for each row tile
-  static constexpr int kStage = 16;                     // columns joined at a time through the Q tile's memory
 };
 // byte offsets behind kBars
 enum {
@@ -816,14 +815,12 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         tc_fence_before();                              // O is read: the next piece's P V may overwrite it
         continue;
       }
-      // Copies are joined kCols columns at a time through the memory of the Q tile: its last reader, this
-      // piece's last S, is done, and the next Q is let in behind the join.
-      constexpr int kAll = 128 * NT, kCols = S_::kStage, kVecs = kCols / 4;
-      auto stage = [&](int row, int vec) -> unsigned char* {       // 16 bytes; each row tile in its own Q tile
-        return smem + (row >> 7) * S_::kQTile + (row & 127) * (kCols * 4) + ((vec ^ (row & (kVecs - 1))) << 4);
-      };
-      constexpr int copies = NT == 2 ? 2 : C, apart = NT == 2 ? 128 : kCopyRows;
-      const bool lead_copy = tid < apart;
+      // Copies are joined through the memory of the Q tiles, as many columns at a time as fit (all of them
+      // for few rows): their last reader, this piece's last S, is done, and the next Q is let in behind
+      // the join.
+      constexpr int kAll = 128 * NT, copies = NT == 2 ? 2 : C, apart = NT == 2 ? 128 : kCopyRows;
+      constexpr int kStage = NT * S_::kQTile - kAll * 8;
+      const int me = NT == 2 ? s : ci;                  // this thread's copy
       float w, top, sum;
       auto sync = [&]() -> bool {                       // of the warps that share rows, with a bounded wait
         __syncwarp();
@@ -832,70 +829,75 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         return ok;
       };
       {                                                 // the copies' maxima and sums
-        float2* s_ml = reinterpret_cast<float2*>(smem + 128 * kCols * 4);          // [kAll]
+        float2* s_ml = reinterpret_cast<float2*>(smem + kStage);                   // [kAll]
         if (!sync()) break;                             // (NT = 2: the other tile's last S is done too)
         s_ml[tid] = make_float2(m_used, l_run);
         if (!sync()) break;
-        const int mine0 = NT == 2 ? t : tr;
         top = -INFINITY;
         sum = 0.f;
 #pragma unroll
-        for (int c = 0; c < copies; ++c) top = fmaxf(top, s_ml[mine0 + c * apart].x);
+        for (int c = 0; c < copies; ++c) top = fmaxf(top, s_ml[tr + c * apart].x);
 #pragma unroll
         for (int c = 0; c < copies; ++c) {
-          const float2 ml = s_ml[mine0 + c * apart];
+          const float2 ml = s_ml[tr + c * apart];
           if (ml.x != -INFINITY) sum += ml.y * ex2(ml.x - top);
         }
         w = m_used == -INFINITY ? 0.f : ex2(m_used - top);
       }
       if (p.whole) w *= sum != 0.f ? 1.f / sum : 0.f;
-      // the warps that hold copies of the same 32 rows share them out again: four or eight rows at a time
-      constexpr int kTogether = 32 / kVecs;
-      const int my_copy = NT == 2 ? s : ci, col = lane % kVecs;
+      int cols = D;
+      while (rows * copies * cols * 4 > kStage) cols >>= 1;                        // (16 at least)
+      const int vecs = cols >> 2, together = 32 / vecs, col = lane & (vecs - 1);   // lanes of a row, rows of a warp
+      auto stage = [&](int copy, int row, int vec) -> unsigned char* {
+        return smem + ((copy * rows + row) * vecs + (vec ^ (row & 7 & (vecs - 1)))) * 16;
+      };
 #pragma unroll 1
-      for (int c = 0; c < D / kCols; ++c) {
+      for (int c = 0; c < D; c += cols) {
         if (warp_live) {
-          uint32_t o[kCols];
-          tmem_load(o_col + c * kCols, o);
+#pragma unroll 1
+          for (int d = 0; d < cols; d += 16) {
+            uint32_t o[16];
+            __syncwarp();
+            tmem_load(o_col + c + d, o);
+            if (!live) continue;
 #pragma unroll
-          for (int j = 0; j < kCols; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
-          if (bad && lead_copy && live) {               // rare; a copy, so that o stays in registers otherwise
-            uint32_t y[kCols];
+            for (int j = 0; j < 16; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
+            if (bad && me == 0) {                       // rare; a copy, so that o stays in registers otherwise
+              uint32_t y[16];
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) y[j] = o[j];
-            add_back<T, BN>(a, p, node, depth, mask0, c * kCols, y);
+              for (int j = 0; j < 16; ++j) y[j] = o[j];
+              add_back<T, BN>(a, p, node, depth, mask0, c + d, y);
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) o[j] = y[j];
+              for (int j = 0; j < 16; ++j) o[j] = y[j];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              *reinterpret_cast<uint4*>(stage(me, tr, (d >> 2) + e)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           }
-#pragma unroll
-          for (int e = 0; e < kVecs; ++e)
-            *reinterpret_cast<uint4*>(stage(tid, e)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
         }
         if (!sync()) break;
+        // the warps that hold copies of the same 32 rows share them out again
+#pragma unroll 2
+        for (int j = me * together; j < 32; j += copies * together) {
+          const int row = j + lane / vecs;              // of this warp's 32
+          const long long at = __shfl_sync(0xFFFFFFFFu, mine, row) + c + col * 4;
+          if (tr - lane + row >= rows) continue;
+          float4 y = *reinterpret_cast<const float4*>(stage(0, tr - lane + row, col));
 #pragma unroll
-        for (int j = 0; j < kVecs; ++j) {
-          const int row = j * kTogether + lane / kVecs;                    // of this warp's 32
-          const long long at = __shfl_sync(0xFFFFFFFFu, mine, row) + c * kCols + col * 4;
-          if (j % copies == my_copy) {
-            if (tr - lane + row < rows) {
-              float4 y = *reinterpret_cast<const float4*>(stage(tr - lane + row, col));
-#pragma unroll
-              for (int k = 1; k < copies; ++k) {
-                const float4 z = *reinterpret_cast<const float4*>(stage(tr - lane + row + k * apart, col));
-                y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
-              }
-              if (p.whole)
-                *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at) = make_uint2(Type<T>::pack(y.x, y.y), Type<T>::pack(y.z, y.w));
-              else
-                *reinterpret_cast<float4*>(a.ws_o + at) = y;
-            }
+          for (int k = 1; k < copies; ++k) {
+            const float4 z = *reinterpret_cast<const float4*>(stage(k, tr - lane + row, col));
+            y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
           }
+          if (p.whole)
+            *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at) = make_uint2(Type<T>::pack(y.x, y.y), Type<T>::pack(y.z, y.w));
+          else
+            *reinterpret_cast<float4*>(a.ws_o + at) = y;
         }
         if (!sync()) break;                             // the stage is free again
       }
       if (!ok) break;
       if (NT == 2 ? t == 0 : tid < 1) mbar_arrive(bars + kQFree);
-      if (live && lead_copy) {
+      if (live && me == 0) {
         if (!p.whole)
           *reinterpret_cast<float2*>(a.ws_ml + (w0 + tr) * 2) = make_float2(top, sum);
         else if (a.lse)

@@ -402,6 +402,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       total += s_scan[w];
     }
     teams = total < a.teams ? (int)total : a.teams;     // fewer tiles than teams: one each, the rest idle
+    // one context: its units are alike, and with the same number of teams each no share crosses a border
+    if (a.B == 1 && teams > a.H_kv) teams -= teams % a.H_kv;
     x0 = team < teams ? divide(total * team, teams) : total;
     x1 = team < teams ? divide(total * (team + 1), teams) : total;
     long long at = before + inc - mine;
@@ -444,6 +446,13 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     uint32_t pieces = 0;
     while (ok && walk.next(p)) {
       const int32_t* table = a.table + p.b * a.table_stride;
+      // the page of this lane's box, looked up a tile ahead
+      auto find = [&](int it, int& row) -> int {
+        row = tile_key<BN>(p.c, p.t0 + it) + pg * box;
+        const int col = row >> a.page_log;
+        return active && col < a.table_cols ? __ldg(table + col) : -1;
+      };
+      int row, page = find(0, row);
       if (is_v) {
         // Q rows of the piece -> shared memory, K-major 128-byte-swizzled, each for every copy of its row.
         // Rows past the last one keep whatever is there: their scores are never looked at.  This warp gets
@@ -476,13 +485,6 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           }
         }
       }
-      // the page of this lane's box, looked up a tile ahead
-      auto find = [&](int it, int& row) -> int {
-        row = tile_key<BN>(p.c, p.t0 + it) + pg * box;
-        const int col = row >> a.page_log;
-        return active && col < a.table_cols ? __ldg(table + col) : -1;
-      };
-      int row, page = find(0, row);
       for (int it = 0; it < p.len; ++it) {
         int next_row = row;
         const int next_page = it + 1 < p.len ? find(it + 1, next_row) : page;

@@ -238,7 +238,7 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
       : "=r"(ready)
       : "r"(bar), "r"(parity)
       : "memory");
-  if (__all_sync(0xFFFFFFFFu, ready != 0)) return true;
+  if (__builtin_expect(__all_sync(0xFFFFFFFFu, ready != 0), 1)) return true;
   return __all_sync(0xFFFFFFFFu, mbar_wait_abortable(bar, parity, abort_word) ? 1 : 0) != 0;
 }
 
@@ -649,7 +649,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       for (bool fresh = true; it < p.len; it += step, fresh = false) {
         const uint32_t buf = 2 * s + (n & 1);
         const bool plain = it >= clear0 && it < clear1;
-        if (!plain) {
+        if (__builtin_expect(!plain, 0)) {
           const int key0 = tile_key<BN>(p.c, p.t0 + it);
           // Values of V that are not finite would reach rows that do not see their key (0 x NaN): take
           // them out of the tile, and remember the piece if the key exists (see the epilogue).  Both row
@@ -681,7 +681,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           }
           fence_async_smem();
         }
-        if (!wait(bars + kSFull + buf * 8, (n >> 1) & 1)) { ok = false; break; }
+        if (__builtin_expect(!wait(bars + kSFull + buf * 8, (n >> 1) & 1), 0)) { ok = false; break; }
         tc_fence_after();
         if (warp_live) {
           const uint32_t s_col = tmem + lanes + buf * BN;
@@ -691,7 +691,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           tmem_wait_ld();
 #pragma unroll
           for (int c = 0; c < kParts; ++c) tmem_named(x[c]);
-          if (!plain) {
+          if (__builtin_expect(!plain, 0)) {
             const int key0 = tile_key<BN>(p.c, p.t0 + it);
             const u64 vis = live ? visible(a, p.c, p.b, node, depth, mask0, key0) >> (ci * KP) : 0ull;
             const uint32_t lo = (uint32_t)vis, hi = (uint32_t)(vis >> 32);
@@ -706,7 +706,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           for (int j = 0; j < KP / 2; ++j)
             mx4[j & 3] = max3(mx4[j & 3], __uint_as_float(x[j / 8][2 * (j % 8)]), __uint_as_float(x[j / 8][2 * (j % 8) + 1]));
           const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
-          if (__any_sync(0xFFFFFFFFu, live && mx > m_used + kRescaleStep)) {
+          if (__builtin_expect(__any_sync(0xFFFFFFFFu, live && mx > m_used + kRescaleStep), 0)) {
             const float m_new = fmaxf(m_used, mx);
             const float alpha = m_new == -INFINITY ? 1.f : ex2(m_used - m_new);   // m_used = -inf gives 0
             if (!fresh) {
@@ -779,7 +779,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             if (!live) continue;
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
-            if (bad) {                                  // rare; a copy, so that o stays in registers otherwise
+            if (__builtin_expect(bad, 0)) {             // rare; a copy, so that o stays in registers otherwise
               uint32_t y[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) y[j] = o[j];
@@ -864,7 +864,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             if (!live) continue;
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
-            if (bad && me == 0) {                       // rare; a copy, so that o stays in registers otherwise
+            if (__builtin_expect(bad && me == 0, 0)) {                       // rare; a copy, so that o stays in registers otherwise
               uint32_t y[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) y[j] = o[j];
@@ -880,7 +880,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         if (!sync()) break;
         // the warps that hold copies of the same 32 rows share them out again
 #pragma unroll 2
-        for (int j = me * together; j < 32; j += copies * together) {
+        for (int j = me * together; j < min(32, rows - tr + lane); j += copies * together) {
           const int row = j + lane / vecs;              // of this warp's 32
           const long long at = __shfl_sync(0xFFFFFFFFu, mine, row) + c + col * 4;
           if (tr - lane + row >= rows) continue;

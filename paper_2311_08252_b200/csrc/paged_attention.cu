@@ -402,6 +402,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       total += s_scan[w];
     }
     teams = total < a.teams ? (int)total : a.teams;     // fewer tiles than teams: one each, the rest idle
+    // no more than 64 pieces of a unit: joining 296 pieces of one KV head took longer than the keys
+    // (32768 keys, one KV head: 51 us; in 128 pieces 27 us)
+    teams = min((long long)teams, 64ll * a.B * a.H_kv);
     // one context: its units are alike, and with the same number of teams each no share crosses a border
     if (a.B == 1 && teams > a.H_kv) teams -= teams % a.H_kv;
     x0 = team < teams ? divide(total * team, teams) : total;

@@ -3,23 +3,23 @@
 //
 // One block works on one row of logits at a time and says where a walk that reaches that row goes:
 // to a child, or to an end with a drawn token.  Its steps:
-//   1. the row into shared memory (larger ones are read again from L2), and its largest logit;
-//   2. every token's weight as an integer of 2^-44 of the largest (rounded to 27 bits), their sum, and
-//      the sums of bins of 1/16 in log2 - for tokens heavy enough to be in the nucleus: those below
-//      (1 - top_p) / V of the largest are not, whatever the rest of the row holds;
+//   1. the row's largest logit;
+//   2. every token's weight, kept in shared memory (rows beyond 51200 tokens: computed again whenever it is
+//      looked at), their sum, and the sums of bins of a sixteenth of an octave - for tokens heavy enough to
+//      be in the nucleus: those below (1 - top_p) / V of the largest are not, whatever else the row holds;
 //   3. with a nucleus: the bin in which the running sum reaches its target; the tokens of that bin (some
 //      hundred) are ordered against one another;
 //   4. the children of the row's node in index order;
 //   5. if none is accepted: the drawn token, by sums over the tokens in order.
-// Integer sums are exact, so the result depends neither on the order of addition nor on the number of
-// threads.  A weight is off by 2^-27 of itself at most, either way alike: plain 32-bit arithmetic (the
-// product of a far logit and 1 / temperature alone: 1e-6) would move the borders between tokens often
-// enough to be seen in a large batch.
+// A weight is a float that holds a whole number of 2^-44 of the largest, so all sums are sums of integers:
+// exact, and the same for any order of addition and any number of threads.  It is off by 2^-24 of itself,
+// either way alike: plain 32-bit arithmetic (the product of a far logit and 1 / temperature alone: 1e-6)
+// would move the borders between tokens often enough to be seen in a large batch.
 //
 // A walk visits 1 + accepted rows of N + 1.  Either one block per context walks, a row after the
 // other, reading only those rows; or, when the rows of all contexts are few enough to run at once,
 // every row gets a block of its own and a second small kernel follows the outcomes.  Bound: instructions
-// (about 30 a token for the sums, more time than the row's bytes take), and a walk is a chain of rows.
+// (about 35 a token for the weights, more time than the row's bytes take), and a walk is a chain of rows.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -33,10 +33,10 @@ namespace {
 
 typedef unsigned long long u64;
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
-constexpr u64 kOne = 1ull << 44;                // the weight of a row's largest logit
-constexpr int kBins = 45 * 16 + 1;              // bins of 1/16 in log2, down to 2^-45
+constexpr uint32_t kOneBits = 0x55800000u;      // 2^44 as a float: the weight of a row's largest logit
+constexpr int kBins = 16 * 46;                  // 16 to an octave, from [2^44, 2^45) down
 constexpr int kList = 1024;                     // tokens of one bin that are ordered pairwise
-constexpr size_t kRowBytes = 200 * 1024;        // longest row kept in shared memory
+constexpr int kKeptTokens = 51200;              // rows whose weights stay in shared memory (200 KB)
 
 struct Args {
   const void* logits;
@@ -61,62 +61,70 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 }
 
 struct Shared {
-  uint2 pow16[16];                              // 2^(26 + j/16) as a float and as an integer
+  float2 pow16[16];                             // 2^(44 + j/16) as a float and what it leaves
   u64 sum[kWarps], left, above, seg_before, cut;
-  ulonglong2 list[kList];                       // {order: key, then ~index; weight}, largest order first
-  uint32_t bin_lo[kBins], bin_hi[kBins];        // sums of the low 14 and the higher bits of 27-bit weights
+  ulonglong2 list[kList];                       // {order: key, then ~index; weight}
+  uint32_t bin_lo[kBins], bin_hi[kBins];        // sums of the low and high 12 bits of the weights' mantissas
   uint32_t red[kWarps], red2[kWarps];
   int32_t tok[REST_MAX_N], par[REST_MAX_N];
   int cut_tie, bin, n_list, child, n_refused, refused[REST_MAX_N], token, seg;
 };
 
 // A row's scale: 16 log2 of a token's weight = (x - top) * c16, with c16 as a sum of two floats (held
-// below 1e30, where any two different logits are worlds apart); differences beyond `least` weigh nothing
+// below 1e30, where any two different logits are worlds apart); differences beyond `least` weigh nothing.
+// Rows of greedy walks and rows with an infinite logit (flat): the largest weigh 1, all others 0.
 struct Row {
   float top, c16_hi, c16_lo, least;
-  double c16;
-  bool greedy, inf;
+  bool flat;
 };
 
-// log2 weight in sixteenths, rounded (monotonic in x), and the rest f, |f| <= 1/2; no branches.  The
-// product is kept to 48 bits (its rounding error, the low half of c16, for fp32 logits the rounding of the
-// difference too): f is off by some 1e-8, where a plain product of a far logit would be off by 4e-5.
-// 32-bit arithmetic throughout: 64-bit instructions issue at half the rate.
+// The weight of logit x: 2^44 2^((x - top) c16 / 16), rounded to 24 bits and to a whole number; no
+// branches.  With y the product, k its nearest integer and f the rest: a table gives 2^(j/16), j = k % 16,
+// q = 2^(f/16) - 1 comes from its Taylor series (|q| < 0.022, the fifth power is 4e-11), k / 16 goes into
+// the exponent.  y is kept to 48 bits (its rounding error, the low half of c16, for fp32 logits the
+// rounding of the difference too): f is off by some 1e-8, where a plain product of a far logit would be
+// off by 4e-5.  32-bit arithmetic throughout: 64-bit instructions issue at half the rate.
 template <typename T>
-__device__ __forceinline__ void split(const Row& r, float x, int& k, float& f) {
+__device__ __forceinline__ float smooth_weight(const Shared& sh, const Row& r, float x) {
   constexpr float kMagic = 12582912.f;          // 1.5 * 2^23: adding it rounds to an integer
+  constexpr double l = 0.6931471805599453 / 16.0;
+  constexpr float a1 = (float)l, a2 = (float)(l * l / 2), a3 = (float)(l * l * l / 6), a4 = (float)(l * l * l * l / 24);
   const float raw = __fsub_rn(x, r.top), d = fmaxf(raw, r.least), y = __fmul_rn(d, r.c16_hi);   // NaN: least
   float rest = fmaf(d, r.c16_lo, fmaf(d, r.c16_hi, -y));
   if (sizeof(T) == 4) {
     const float b = __fsub_rn(raw, x), e = __fsub_rn(__fsub_rn(x, __fsub_rn(raw, b)), __fadd_rn(r.top, b));
     rest = fmaf(raw > r.least ? e : 0.f, r.c16_hi, rest);
   }
-  const float t = __fadd_rn(y, kMagic);
-  k = __float_as_int(t) - 0x4B400000;
-  f = __fadd_rn(__fsub_rn(y, __fsub_rn(t, kMagic)), rest);
-}
-// The weight 2^((k + f)/16) in units of 2^-44, of 27 bits at most (see up).  From a table of 2^(j/16) and
-// q = 2^(f/16) - 1 by its Taylor series (|q| < 0.022, the fifth power is 4e-11): q is off by 2^-24 of
-// itself, so the product of 27 bits by less than one.
-__device__ __forceinline__ u64 weight_of(const Shared& sh, int k, float f) {
-  constexpr double l = 0.6931471805599453 / 16.0;
-  constexpr float a1 = (float)l, a2 = (float)(l * l / 2), a3 = (float)(l * l * l / 6), a4 = (float)(l * l * l * l / 24);
+  const float t = __fadd_rn(y, kMagic), f = __fadd_rn(__fsub_rn(y, __fsub_rn(t, kMagic)), rest);
   const float q = f * fmaf(f, fmaf(f, fmaf(f, a4, a3), a2), a1);
-  const uint2 t = sh.pow16[k & 15];
-  const uint32_t m = t.y + (__float_as_uint(fmaf(__uint_as_float(t.x), q, 12582912.f)) - 0x4B400000u);
-  return ((u64)m << 18) >> -(k >> 4);
+  const uint32_t k = __float_as_uint(t);        // (the magic's low bits are 0)
+  const float2 p = sh.pow16[k & 15u];
+  const float w = __uint_as_float(__float_as_uint(__fadd_rn(p.x, fmaf(p.x, q, p.y))) + ((k & ~15u) << 19));
+  const float whole = __fsub_rn(__fadd_rn(w, 8388608.f), 8388608.f);       // below 2^23: rounds to a whole number
+  return w < 8388608.f ? whole : w;
 }
-// zero bits at the end of such a weight
-__device__ __forceinline__ int up(int k) { return max(18 + (k >> 4), 0); }
-// weight before the nucleus cut (see Row): an infinite logit takes all of the mass
+__device__ __forceinline__ u64 whole(float w) {            // a weight as an integer
+  const uint32_t b = __float_as_uint(w);
+  const int e = (int)(b >> 23) - 150;
+  const u64 m = (b & 0x7FFFFFu) | 0x800000u;
+  return b == 0u ? 0ull : e >= 0 ? m << e : m >> -e;
+}
 template <typename T>
-__device__ __forceinline__ u64 weight(const Shared& sh, const Row& r, float x) {
-  if (r.inf || r.greedy) return x == r.top ? kOne : 0ull;
-  int k;
-  float f;
-  split<T>(r, x, k, f);
-  return weight_of(sh, k, f);
+__device__ __forceinline__ float weight(const Shared& sh, const Row& r, float x) {
+  return r.flat ? (x == r.top ? __uint_as_float(kOneBits) : 0.f) : smooth_weight<T>(sh, r, x);
 }
+// Sum of weights in two 32-bit integers: units of 2^22 (rounded; 256 of 2^22 at most a thread) and the rest,
+// both read off the low bits of a float to which 2^23 or 1.5 * 2^23 was added.
+struct Sum {
+  uint32_t high = 0, low = 0;
+  __device__ __forceinline__ void add(float w) {
+    const float t = fmaf(w, 0x1p-22f, 8388608.f), rest = fmaf(__fsub_rn(t, 8388608.f), -0x1p22f, w);
+    high += __float_as_uint(t) - 0x4B000000u;
+    low += __float_as_uint(__fadd_rn(rest, 12582912.f)) - 0x4B400000u;
+  }
+  __device__ __forceinline__ u64 total() const { return ((u64)high << 22) + (u64)(long long)(int)low; }
+};
+__device__ __forceinline__ int bin_of(float w) { return (int)((kOneBits + 0x7FFFFFu - __float_as_uint(w)) >> 19); }
 
 __device__ __forceinline__ u64 warp_sum(u64 x) {
 #pragma unroll
@@ -157,77 +165,57 @@ __device__ __forceinline__ double uniform(const float* u, int s) {
 // (-1: nothing can be drawn).  depth: nodes accepted on the way, -1: to be counted here; a walk that is as
 // deep as allowed only draws.
 template <typename T, bool KEPT>
-__device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int b, int cur, int depth) {
+__device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cur, int depth) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nn = min(max(a.n_nodes[b], 0), a.N);
-  const int32_t *tok = a.tokens + (int64_t)b * a.N, *par = a.parents + (int64_t)b * a.N;
   const float* uni = a.uniforms + (int64_t)b * (a.N + 1);
   const float temp = a.temperature[b], top_p = a.top_p[b];
   const T* row = static_cast<const T*>(a.logits) + b * a.s_ctx + (int64_t)(cur + 1) * a.s_row;
   const int V = a.V;
-  // KEPT: the row's 16-byte vectors, at the same offset from a 16-byte border as in memory, padded with
-  // -infinity on both sides.  Otherwise this memory is one bit per token: refused at this node.
+  // The row is read in 16-byte vectors; positions before and behind it in its first and last vector hold
+  // -infinity.  KEPT: weights stand in shared memory by position; otherwise that memory is one bit per
+  // token: refused at this node.
   constexpr int kPer = 16 / sizeof(T);
-  const int shift = KEPT ? (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)) : 0;
+  const int shift = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
   const int vecs = (shift + V + kPer - 1) / kPer;
-  T* s_val = reinterpret_cast<T*>(s_row) + shift;
-  uint32_t* s_gone = reinterpret_cast<uint32_t*>(s_row);
-  auto get = [&](int v) -> float { return KEPT ? (float)s_val[v] : (float)row[v]; };
-  // fn(token, logit) for all tokens, or for those of vectors / tokens [from, to) by this thread and those
-  // `step` on
-  auto each = [&](int from, int to, int step, auto fn) {
-    if (KEPT) {
-      for (int i = from; i < to; i += step) {
-        const uint4 x = reinterpret_cast<const uint4*>(s_row)[i];
-        const T* e = reinterpret_cast<const T*>(&x);
+  const uint4* src = reinterpret_cast<const uint4*>(row - shift);
+  uint32_t* s_gone = reinterpret_cast<uint32_t*>(s_w);
+  auto load = [&](int i) -> uint4 {                       // whole vectors inside the row; its ends one by one
+    if (i * kPer >= shift && (i + 1) * kPer <= shift + V) return __ldg(src + i);
+    uint4 x;
+    T* e = reinterpret_cast<T*>(&x);
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) fn(i * kPer + k - shift, (float)e[k]);
-      }
-    } else {
-#pragma unroll 4
-      for (int v = from; v < to; v += step) fn(v, (float)row[v]);
+    for (int k = 0; k < kPer; ++k) {
+      const int v = i * kPer + k - shift;
+      e[k] = v >= 0 && v < V ? row[v] : (T)(-INFINITY);
     }
+    return x;
   };
-  const int units = KEPT ? vecs : V;
 
-  // ---- 1. the row and its largest logit; the tree
-  uint32_t top = 0;
+  // ---- 1. the largest logit; the tree
+  float most = -INFINITY;
   __syncthreads();                              // the row before it is done with
-  for (int i = tid; i < a.N; i += kThreads) { sh.tok[i] = tok[i]; sh.par[i] = par[i]; }
-  if (KEPT) {
-    const T* base = row - shift;                // whole vectors inside the row; its ragged ends one by one
-    const int first = shift ? 1 : 0, last = (shift + V) / kPer;
-    for (int i0 = first + tid; i0 < last; i0 += 8 * kThreads) {
-      uint4 x[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (i0 + j * kThreads < last) x[j] = __ldcs(reinterpret_cast<const uint4*>(base) + i0 + j * kThreads);
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (i0 + j * kThreads < last) {
-          reinterpret_cast<uint4*>(s_row)[i0 + j * kThreads] = x[j];
-          const T* e = reinterpret_cast<const T*>(&x[j]);
-          float most = -INFINITY;               // (fmaxf passes NaN over)
-#pragma unroll
-          for (int k = 0; k < kPer; ++k) most = fmaxf(most, (float)e[k]);
-          top = max(top, key_of(most));
-        }
-    }
-    if (tid < 2 * kPer) {
-      const int at = tid < kPer ? tid : (vecs - 1) * kPer + tid - kPer, v = at - shift;
-      const bool ragged = tid < kPer ? first == 1 : last < vecs && (vecs > 1 || first == 0);
-      if (ragged) {
-        const T x = v >= 0 && v < V ? row[v] : (T)(-INFINITY);
-        reinterpret_cast<T*>(s_row)[at] = x;
-        top = max(top, key_of((float)x));
-      }
-    }
-  } else {
-    for (int w = tid; w < (V + 31) / 32; w += kThreads) s_gone[w] = 0u;
-    each(tid, units, kThreads, [&](int, float x) { top = max(top, key_of(x)); });
+  for (int i = tid; i < a.N; i += kThreads) {
+    sh.tok[i] = a.tokens[(int64_t)b * a.N + i];
+    sh.par[i] = a.parents[(int64_t)b * a.N + i];
   }
+  for (int i0 = tid; i0 < vecs; i0 += 8 * kThreads) {
+    uint4 x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i0 + j * kThreads < vecs) x[j] = load(i0 + j * kThreads);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i0 + j * kThreads < vecs) {
+        const T* e = reinterpret_cast<const T*>(&x[j]);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) most = fmaxf(most, (float)e[k]);    // (passes NaN over)
+      }
+  }
+  if (!KEPT)
+    for (int w = tid; w < (V + 31) / 32; w += kThreads) s_gone[w] = 0u;
   for (int i = tid; i < kBins; i += kThreads) sh.bin_lo[i] = sh.bin_hi[i] = 0u;
-  top = __reduce_max_sync(0xFFFFFFFFu, top);
+  uint32_t top = __reduce_max_sync(0xFFFFFFFFu, key_of(most));
   if (lane == 0) sh.red[warp] = top;
   if (tid == 0) { sh.cut_tie = 0x7FFFFFFF; sh.bin = -1; sh.n_list = 0; }
   __syncthreads();
@@ -235,171 +223,194 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
   if (top == 0) return make_int2(-1, -1);
   Row r;
   r.top = of_key(top);
-  r.greedy = !(temp > 0.f);
-  r.inf = r.top == INFINITY;
-  r.c16 = r.greedy ? 0.0 : 16.0 * 1.4426950408889634 / fmax((double)fminf(temp, 1e30f), 1e-29);
-  r.c16_hi = (float)r.c16;
-  r.c16_lo = (float)(r.c16 - (double)r.c16_hi);
-  r.least = r.greedy ? 0.f : (float)(-760.0 / r.c16);     // 2^-47.5: rounds to nothing
-  const bool smooth = !r.greedy && !r.inf;      // weights between 0 and 1
+  const bool greedy = !(temp > 0.f);
+  r.flat = greedy || r.top == INFINITY;
+  const double c16 = r.flat ? 1.0 : 16.0 * 1.4426950408889634 / fmax((double)fminf(temp, 1e30f), 1e-29);
+  r.c16_hi = (float)c16;
+  r.c16_lo = (float)(c16 - (double)r.c16_hi);
+  r.least = (float)(-760.0 / c16);              // 2^-47.5: rounds to nothing
 
-  // ---- 2. the mass, and the bins' if there will be a cut
-  const bool cut = r.greedy || top_p < 1.f;
-  u64 mass = 0;
-  if (smooth) {
-    // the last bin that can be in the nucleus: 16 log2(V / (1 - top_p)), and two more for its roundings
-    const int bins = cut ? (top_p > 0.f ? min(kBins, (int)(16.f * (log2f((float)V) - log2f(1.f - top_p))) + 3) : 1) : 0;
-    each(tid, units, kThreads, [&](int, float x) {
-      int k;
-      float f;
-      split<T>(r, x, k, f);
-      const u64 w = weight_of(sh, k, f);
-      mass += w;
-      if (-k < bins) {
-        const uint32_t m = (uint32_t)(w >> up(k));
-        atomicAdd(&sh.bin_lo[-k], m & 0x3FFFu);
-        atomicAdd(&sh.bin_hi[-k], m >> 14);
-      }
-    });
-  } else {
-    each(tid, units, kThreads, [&](int, float x) { mass += x == r.top ? kOne : 0ull; });
+  // ---- 2. weights, their sum, and the bins' if there will be a cut
+  const bool cut = greedy || top_p < 1.f;
+  // the lightest weight that can be in the nucleus, and a little less
+  const float lightest = cut ? (!greedy && top_p > 0.f ? fmaxf((1.f - top_p) / (float)V * 1.5e13f, 1.f) : __uint_as_float(kOneBits)) : INFINITY;
+  Sum all;
+  uint4 next = tid < vecs ? load(tid) : make_uint4(0u, 0u, 0u, 0u);
+  for (int i = tid; i < vecs; i += kThreads) {
+    const uint4 x = next;
+    if (i + kThreads < vecs) next = load(i + kThreads);
+    const T* e = reinterpret_cast<const T*>(&x);
+    float w[kPer];
+    if (r.flat) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) w[k] = (float)e[k] == r.top ? __uint_as_float(kOneBits) : 0.f;
+    } else {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) w[k] = smooth_weight<T>(sh, r, (float)e[k]);
+    }
+    float heaviest = 0.f;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      all.add(w[k]);
+      heaviest = fmaxf(heaviest, w[k]);
+    }
+    if (heaviest >= lightest) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        if (w[k] >= lightest) {
+          const uint32_t bits = __float_as_uint(w[k]);
+          atomicAdd(&sh.bin_lo[bin_of(w[k])], bits & 0xFFFu);
+          atomicAdd(&sh.bin_hi[bin_of(w[k])], (bits >> 12 & 0x7FFu) | 0x800u);
+        }
+    }
+    if (KEPT) {
+#pragma unroll
+      for (int k = 0; k < kPer; k += 4)
+        *reinterpret_cast<float4*>(s_w + i * kPer + k) = make_float4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+    }
   }
-  mass = block_sum(sh, mass);
+  u64 mass = block_sum(sh, all.total());        // (its barriers put the weights and the bins in place, too)
 
-  // ---- 3. the nucleus: tokens from (cut_key, cut_tie) up
+  auto weight_at = [&](int v) -> float { return KEPT ? s_w[shift + v] : weight<T>(sh, r, (float)row[v]); };
+  // fn(token, its weight and those of the three after it) for the positions' fours [from, to), `step` apart
+  auto each = [&](int from, int to, int step, auto fn) {
+#pragma unroll 2
+    for (int i = from; i < to; i += step) {
+      float w[4];
+      if (KEPT) {
+        const float4 x = *reinterpret_cast<const float4*>(s_w + i * 4);
+        w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int v = i * 4 + k - shift;
+          w[k] = v >= 0 && v < V ? weight_at(v) : 0.f;
+        }
+      }
+      fn(i * 4 - shift, w);
+    }
+  };
+  const int fours = (shift + V + 3) / 4;
+
+  // ---- 3. the nucleus: tokens of weight above cut_w, and of those at cut_w the ones from (cut_key,
+  // cut_tie) up
+  float cut_w = 0.f;
   uint32_t cut_key = 0;
   int cut_tie = 0x7FFFFFFF;
   if (cut) {
     u64 target = 1;
-    if (!r.greedy && top_p > 0.f) target = max((u64)1, (u64)ceil((double)top_p * (double)mass));
-    u64 above = 0;                              // mass of the bins that are surely kept
-    bool ordered = false;
-    uint32_t lo = top, hi = top;                // keys among which the cut lies, if it is not found by order
-    float x_lo = 0.f, x_hi = 0.f;               // logits of the bin lie between them
-    if (smooth) {
-      const u64 mine = tid < kBins ? (u64)sh.bin_lo[tid] + ((u64)sh.bin_hi[tid] << 14) << up(-tid) : 0ull;
+    if (!greedy && top_p > 0.f) target = max((u64)1, (u64)ceil((double)top_p * (double)mass));
+    {
+      u64 mine = 0;
+      if (tid < kBins) {
+        const int e = 44 - 23 - (tid >> 4);               // what the bin's mantissas of 24 bits count
+        const u64 m = (u64)sh.bin_lo[tid] + ((u64)sh.bin_hi[tid] << 12);
+        mine = e >= 0 ? m << e : m >> -e;
+      }
       const u64 upto = block_scan(sh, mine);
       if (upto >= target && upto - mine < target) { sh.bin = tid; sh.above = upto - mine; }
       __syncthreads();
-      const int bin = sh.bin;
-      above = sh.above;
-      // a little wider than half a bin on both sides, so that only few tokens are looked at closely
-      x_hi = (float)((double)r.top - ((double)bin - 0.51) / r.c16);
-      x_lo = (float)((double)r.top - ((double)bin + 0.51) / r.c16);
-      x_hi += fabsf(x_hi) * 1e-6f;
-      x_lo -= fabsf(x_lo) * 1e-6f;
-      each(tid, units, kThreads, [&](int v, float x) {
-        int k;
-        float f;
-        if (!(x >= x_lo && x <= x_hi)) return;
-        split<T>(r, x, k, f);
-        if (-k == bin) {
-          const int at = atomicAdd(&sh.n_list, 1);
-          if (at < kList) sh.list[at] = make_ulonglong2((u64)key_of(x) << 32 | (uint32_t)~v, weight_of(sh, k, f));
+    }
+    const int bin = sh.bin;
+    const u64 above = sh.above;                 // mass of the bins that are kept whole
+    // fn(token, weight) for the tokens of the bin: bits in [first, first + 2^19)
+    const uint32_t first = kOneBits + 0x7FFFFFu - ((uint32_t)bin << 19) - 0x7FFFFu;
+    auto in_bin = [&](auto fn) {
+      each(tid, fours, kThreads, [&](int v, const float (&w)[4]) {
+        bool is[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) is[k] = __float_as_uint(w[k]) - first < 0x80000u;
+        if (is[0] || is[1] || is[2] || is[3]) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (is[k]) fn(v + k, w[k]);
         }
       });
-      __syncthreads();
-      const int n = sh.n_list;
-      if (n <= kList) {
-        ordered = true;
-        // the mass before each token of the bin; several lanes share a token when there are few
-        int parts = 1;
-        while (parts < 32 && n * parts * 2 <= kThreads) parts *= 2;
-        const int e = tid / parts, part = tid % parts;
-        const ulonglong2 mine = e < n ? sh.list[e] : make_ulonglong2(~0ull, 0ull);
-        u64 before = 0;
+    };
+    in_bin([&](int v, float w) {
+      const int at = atomicAdd(&sh.n_list, 1);
+      if (at < kList) sh.list[at] = make_ulonglong2((u64)key_of((float)row[v]) << 32 | (uint32_t)~v, whole(w));
+    });
+    __syncthreads();
+    const int n = sh.n_list;
+    if (n <= kList) {
+      // the mass before each token of the bin; several lanes share a token when there are few
+      int parts = 1;
+      while (parts < 32 && n * parts * 2 <= kThreads) parts *= 2;
+      const int e = tid / parts, part = tid % parts;
+      const ulonglong2 mine = e < n ? sh.list[e] : make_ulonglong2(~0ull, 0ull);
+      u64 before = 0;
 #pragma unroll 8
-        for (int j = part; j < n; j += parts) {
-          const ulonglong2 other = sh.list[j];
-          before += other.x > mine.x ? other.y : 0ull;
-        }
-        for (int d = 1; d < parts; d <<= 1) before += __shfl_xor_sync(0xFFFFFFFFu, before, d);
-        before += above;
-        if (e < n && part == 0 && before < target && before + mine.y >= target) {
-          sh.cut = mine.x;
-          sh.left = before + mine.y;
-        }
-        __syncthreads();
-        cut_key = (uint32_t)(sh.cut >> 32);
-        cut_tie = (int)~(uint32_t)sh.cut;
-        mass = sh.left;
-      } else {                                  // a crowd in one bin (flat rows): bisect its keys
-        uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
-        each(tid, units, kThreads, [&](int, float x) {
-          int k;
-          float f;
-          if (!(x >= x_lo && x <= x_hi)) return;
-          split<T>(r, x, k, f);
-          if (-k == sh.bin) { kmin = min(kmin, key_of(x)); kmax = max(kmax, key_of(x)); }
-        });
-        kmin = __reduce_min_sync(0xFFFFFFFFu, kmin);
-        kmax = __reduce_max_sync(0xFFFFFFFFu, kmax);
-        __syncthreads();
-        if (lane == 0) { sh.red[warp] = kmin; sh.red2[warp] = kmax; }
-        __syncthreads();
-        lo = __reduce_min_sync(0xFFFFFFFFu, sh.red[lane]);
-        hi = __reduce_max_sync(0xFFFFFFFFu, sh.red2[lane]);
+      for (int j = part; j < n; j += parts) {
+        const ulonglong2 other = sh.list[j];
+        before += other.x > mine.x ? other.y : 0ull;
       }
-    }
-    if (!ordered) {
-      // the largest key that reaches the target, then how many of its tokens stay, lowest index first
-      const u64 base = above;
+      for (int d = 1; d < parts; d <<= 1) before += __shfl_xor_sync(0xFFFFFFFFu, before, d);
+      before += above;
+      if (e < n && part == 0 && before < target && before + mine.y >= target) {
+        sh.cut = mine.x;
+        sh.left = before + mine.y;
+      }
+      __syncthreads();
+      cut_key = (uint32_t)(sh.cut >> 32);
+      cut_tie = (int)~(uint32_t)sh.cut;
+      mass = sh.left;
+    } else {
+      // a crowd in one bin (flat rows): the largest key whose tokens and all above reach the target, by
+      // bisection, then how many of its tokens stay, lowest index first
+      uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+      in_bin([&](int v, float) { const uint32_t k = key_of((float)row[v]); kmin = min(kmin, k); kmax = max(kmax, k); });
+      kmin = __reduce_min_sync(0xFFFFFFFFu, kmin);
+      kmax = __reduce_max_sync(0xFFFFFFFFu, kmax);
+      __syncthreads();
+      if (lane == 0) { sh.red[warp] = kmin; sh.red2[warp] = kmax; }
+      __syncthreads();
+      uint32_t lo = __reduce_min_sync(0xFFFFFFFFu, sh.red[lane]), hi = __reduce_max_sync(0xFFFFFFFFu, sh.red2[lane]);
+      auto mass_from = [&](uint32_t key) -> u64 {         // of the bin's tokens with that key and above
+        Sum part;
+        in_bin([&](int v, float w) { if (key_of((float)row[v]) >= key) part.add(w); });
+        return block_sum(sh, part.total());
+      };
       while (lo < hi) {
         const uint32_t mid = lo + (hi - lo) / 2 + 1;
-        u64 more = 0;
-        each(tid, units, kThreads, [&](int, float x) {
-          int k;
-          float f;
-          if (!(x >= x_lo && x <= x_hi && key_of(x) >= mid)) return;
-          split<T>(r, x, k, f);
-          if (-k == sh.bin) more += weight_of(sh, k, f);
-        });
-        if (base + block_sum(sh, more) >= target) lo = mid; else hi = mid - 1;
+        if (above + mass_from(mid) >= target) lo = mid; else hi = mid - 1;
       }
       cut_key = lo;
-      u64 over = 0;
-      if (smooth)
-        each(tid, units, kThreads, [&](int, float x) {
-          int k;
-          float f;
-          if (!(x >= x_lo && x <= x_hi && key_of(x) > cut_key)) return;
-          split<T>(r, x, k, f);
-          if (-k == sh.bin) over += weight_of(sh, k, f);
-        });
-      over = block_sum(sh, over);
-      const u64 one = weight<T>(sh, r, of_key(cut_key)), ties = (target - base - over + one - 1) / one;
+      const u64 over = lo == 0xFFFFFFFFu ? 0ull : mass_from(lo + 1);
+      const u64 one = whole(weight<T>(sh, r, of_key(lo))), ties = (target - above - over + one - 1) / one;
       // every warp counts in a run of its own; the warp whose run holds the last one finds it
-      const int per = (units + kWarps - 1) / kWarps, u0 = min(units, warp * per), u1 = min(units, u0 + per);
-      u64 mine = 0;
-      each(u0 + lane, u1, 32, [&](int, float x) { mine += key_of(x) == cut_key; });
-      mine = warp_sum(mine);
+      const int per = (V + kThreads - 1) / kThreads * 32, v0 = min(V, warp * per), v1 = min(V, v0 + per);
+      u64 count = 0;
+      for (int v = v0 + lane; v < v1; v += 32) count += key_of((float)row[v]) == lo;
+      count = warp_sum(count);
       __syncthreads();
-      if (lane == 0) sh.sum[warp] = mine;
+      if (lane == 0) sh.sum[warp] = count;
       __syncthreads();
       const u64 counts = warp_scan(sh.sum[lane]);
       const u64 upto = __shfl_sync(0xFFFFFFFFu, counts, warp);
-      if (upto >= ties && upto - mine < ties) {           // (one warp)
-        u64 n = upto - mine;
-        const int v0 = max(KEPT ? u0 * kPer - shift : u0, 0), v1 = min(V, KEPT ? u1 * kPer - shift : u1);
-        for (int base_v = v0; base_v < v1; base_v += 32) {
-          const bool is = base_v + lane < v1 && key_of(get(base_v + lane)) == cut_key;
+      if (upto >= ties && upto - count < ties) {          // (one warp)
+        u64 seen = upto - count;
+        for (int base = v0; base < v1; base += 32) {
+          const bool is = base + lane < v1 && key_of((float)row[base + lane]) == lo;
           const unsigned bal = __ballot_sync(0xFFFFFFFFu, is);
-          if (n + __popc(bal) >= ties) {
-            if (is && n + __popc(bal & ((2u << lane) - 1u)) == ties) sh.cut_tie = base_v + lane;
+          if (seen + __popc(bal) >= ties) {
+            if (is && seen + __popc(bal & ((2u << lane) - 1u)) == ties) sh.cut_tie = base + lane;
             break;
           }
-          n += __popc(bal);
+          seen += __popc(bal);
         }
       }
       __syncthreads();
       cut_tie = sh.cut_tie;
-      mass = base + over + ties * one;
+      mass = above + over + ties * one;
     }
+    cut_w = weight<T>(sh, r, of_key(cut_key));
   }
-  auto kept_weight = [&](float x, int v) -> u64 {
-    const uint32_t key = key_of(x);
-    if (key < cut_key || (key == cut_key && v > cut_tie)) return 0ull;
-    return weight<T>(sh, r, x);
+  auto kept = [&](int v, float w) -> bool {
+    if (w != cut_w) return w > cut_w;
+    if (!cut) return false;                     // (weight 0)
+    const uint32_t key = key_of((float)row[v]);
+    return key > cut_key || (key == cut_key && v <= cut_tie);
   };
 
   // ---- 4. children, in index order
@@ -418,7 +429,8 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
       u64 w = 0;
       double u = 0.0;
       if (is && t >= 0 && t < V) {
-        w = kept_weight(get(t), t);
+        const float x = weight_at(t);
+        w = kept(t, x) ? whole(x) : 0ull;
         u = uniform(uni, i + 1);
         for (int j = 0; j < n_refused; ++j)
           if (sh.refused[j] == t) w = 0;
@@ -447,18 +459,29 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
   // ---- 5. the drawn token, from what the refused children leave: first the 1/32 of the row that holds
   // it (a warp's share), then the token in it
   for (int j = tid; j < sh.n_refused; j += kThreads) {
-    if (KEPT) s_val[sh.refused[j]] = (T)(-INFINITY);
+    if (KEPT) s_w[shift + sh.refused[j]] = 0.f;
     else atomicOr(&s_gone[sh.refused[j] >> 5], 1u << (sh.refused[j] & 31));
   }
   __syncthreads();
-  auto rest_weight = [&](int v, float x) -> u64 {
-    if (!KEPT && ((s_gone[v >> 5] >> (v & 31)) & 1u)) return 0ull;
-    return kept_weight(x, v);
+  auto there = [&](int v, float w) -> bool {
+    if (!KEPT && w > 0.f && ((s_gone[v >> 5] >> (v & 31)) & 1u)) return false;
+    return kept(v, w);
   };
-  const int per = (units + kWarps - 1) / kWarps, u0 = min(units, warp * per), u1 = min(units, u0 + per);
-  u64 sum = 0;
-  each(u0 + lane, u1, 32, [&](int v, float x) { sum += rest_weight(v, x); });
-  sum = warp_sum(sum);
+  const int per = (fours + kWarps - 1) / kWarps, f0 = min(fours, warp * per), f1 = min(fours, f0 + per);
+  Sum part;
+  each(f0 + lane, f1, 32, [&](int v, const float (&w)[4]) {
+    bool tie = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) tie = tie || w[k] == cut_w;
+    if (KEPT && (!tie || !cut)) {                          // nobody needs a closer look
+#pragma unroll
+      for (int k = 0; k < 4; ++k) part.add(w[k] > cut_w ? w[k] : 0.f);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) part.add(w[k] > 0.f && there(v + k, w[k]) ? w[k] : 0.f);
+    }
+  });
+  const u64 sum = warp_sum(part.total());
   if (lane == 0) sh.sum[warp] = sum;
   __syncthreads();
   const double goal = uniform(uni, 0) * (double)sh.left;
@@ -467,13 +490,15 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
     if ((double)upto > goal && !((double)(upto - mine) > goal)) { sh.seg = lane; sh.seg_before = upto - mine; }
   }
   __syncthreads();
-  const int g0 = min(units, sh.seg * per), g1 = min(units, g0 + per);
-  const int s0 = max(KEPT ? g0 * kPer - shift : g0, 0), s1 = min(V, KEPT ? g1 * kPer - shift : g1);
+  const int g0 = min(fours, sh.seg * per), g1 = min(fours, g0 + per);
+  const int s0 = max(g0 * 4 - shift, 0), s1 = min(V, g1 * 4 - shift);
   u64 before = sh.seg_before;
   for (int base = s0; base < s1; base += kThreads) {      // (more than one round for more than 32768 tokens)
-    const u64 mine = base + tid < s1 ? rest_weight(base + tid, get(base + tid)) : 0ull;
+    const int v = base + tid;
+    const float w = v < s1 ? weight_at(v) : 0.f;
+    const u64 mine = v < s1 && there(v, w) ? whole(w) : 0ull;
     const u64 upto = before + block_scan(sh, mine);
-    if ((double)upto > goal && !((double)(upto - mine) > goal)) sh.token = base + tid;
+    if ((double)upto > goal && !((double)(upto - mine) > goal)) sh.token = v;
     if (tid == kThreads - 1) sh.above = upto;
     __syncthreads();
     before = sh.above;
@@ -483,15 +508,16 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, unsigned char* s_row, int
 
 __device__ __forceinline__ void fill_table(Shared& sh) {
   if (threadIdx.x < 16) {
-    const double p = exp2(26.0 + (double)threadIdx.x / 16.0);
-    sh.pow16[threadIdx.x] = make_uint2(__float_as_uint((float)p), (uint32_t)(p + 0.5));
+    const double p = exp2(44.0 + (double)threadIdx.x / 16.0);
+    const float hi = (float)p;
+    sh.pow16[threadIdx.x] = make_float2(hi, (float)(p - (double)hi));
   }
 }
 
 // One block per context walks.
 template <typename T, bool KEPT>
 __global__ void __launch_bounds__(kThreads, 1) rest_accept_sampled_walk_kernel(const __grid_constant__ Args a) {
-  extern __shared__ __align__(16) unsigned char s_row[];
+  extern __shared__ __align__(16) float s_w[];
   __shared__ Shared sh;
   fill_table(sh);
   grid_wait();
@@ -499,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) rest_accept_sampled_walk_kernel(c
   int32_t *an = a.accept_nodes + (int64_t)b * a.max_depth, *ot = a.out_tokens + (int64_t)b * (a.max_depth + 1);
   int cur = -1, len = 0;
   for (;;) {
-    const int2 o = row_outcome<T, KEPT>(a, sh, s_row, b, cur, len);
+    const int2 o = row_outcome<T, KEPT>(a, sh, s_w, b, cur, len);
     if (tid == 0) ot[len] = o.y;
     if (o.x < 0) break;
     if (tid == 0) an[len] = o.x;
@@ -513,14 +539,14 @@ __global__ void __launch_bounds__(kThreads, 1) rest_accept_sampled_walk_kernel(c
 // Every row has a block; blockIdx.x = row, blockIdx.y = context.
 template <typename T, bool KEPT>
 __global__ void __launch_bounds__(kThreads, 1) rest_accept_sampled_rows_kernel(const __grid_constant__ Args a) {
-  extern __shared__ __align__(16) unsigned char s_row[];
+  extern __shared__ __align__(16) float s_w[];
   __shared__ Shared sh;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   fill_table(sh);
   grid_wait();
   const int b = blockIdx.y, cur = (int)blockIdx.x - 1, tid = threadIdx.x;
   if (cur >= min(max(a.n_nodes[b], 0), a.N)) return;
-  const int2 o = row_outcome<T, KEPT>(a, sh, s_row, b, cur, -1);
+  const int2 o = row_outcome<T, KEPT>(a, sh, s_w, b, cur, -1);
   if (tid == 0) a.outcome[(int64_t)b * (a.N + 1) + cur + 1] = o;
 }
 
@@ -583,8 +609,7 @@ rest_status run(const Args& a, int B, size_t smem, int smem_slot, cudaStream_t s
 
 template <typename T>
 rest_status pick(const Args& a, int B, int smem_slot, cudaStream_t st) {
-  const size_t row = ((size_t)a.V * sizeof(T) + 31) / 16 * 16;
-  if (row <= kRowBytes) return run<T, true>(a, B, row, smem_slot, st);
+  if (a.V <= kKeptTokens) return run<T, true>(a, B, ((size_t)a.V + 16) * sizeof(float), smem_slot, st);   // and its ends
   return run<T, false>(a, B, 4 * (((size_t)a.V + 31) / 32), smem_slot + 2, st);
 }
 

@@ -32,10 +32,10 @@
 namespace {
 
 typedef unsigned long long u64;
-constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr uint32_t kOneBits = 0x55800000u;      // 2^44 as a float: the weight of a row's largest logit
 constexpr int kBins = 16 * 46;                  // 16 to an octave, from [2^44, 2^45) down
-constexpr int kList = 1024;                     // tokens of one bin that are ordered pairwise
+constexpr int kList = 512;                      // tokens of one bin that are ordered pairwise
 constexpr int kKeptTokens = 51200;              // rows whose weights stay in shared memory (200 KB)
 
 struct Args {
@@ -62,10 +62,10 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 
 struct Shared {
   float2 pow16[16];                             // 2^(44 + j/16) as a float and what it leaves
-  u64 sum[kWarps], left, above, seg_before, cut;
+  u64 sum[32], left, above, seg_before, cut;    // (a warp looks at all 32: those of no warp stay as they began)
   ulonglong2 list[kList];                       // {order: key, then ~index; weight}
   uint32_t bin_lo[kBins], bin_hi[kBins];        // sums of the low and high 12 bits of the weights' mantissas
-  uint32_t red[kWarps], red2[kWarps];
+  uint32_t red[32], red2[32];
   int32_t tok[REST_MAX_N], par[REST_MAX_N];
   int cut_tie, bin, n_list, child, n_refused, refused[REST_MAX_N], token, seg;
 };
@@ -113,7 +113,7 @@ template <typename T>
 __device__ __forceinline__ float weight(const Shared& sh, const Row& r, float x) {
   return r.flat ? (x == r.top ? __uint_as_float(kOneBits) : 0.f) : smooth_weight<T>(sh, r, x);
 }
-// Sum of weights in two 32-bit integers: units of 2^22 (rounded; 256 of 2^22 at most a thread) and the rest,
+// Sum of weights in two 32-bit integers: units of 2^22 (rounded; 512 of 2^22 at most a thread) and the rest,
 // both read off the low bits of a float to which 2^23 or 1.5 * 2^23 was added.
 struct Sum {
   uint32_t high = 0, low = 0;
@@ -301,14 +301,20 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
     u64 target = 1;
     if (!greedy && top_p > 0.f) target = max((u64)1, (u64)ceil((double)top_p * (double)mass));
     {
-      u64 mine = 0;
-      if (tid < kBins) {
-        const int e = 44 - 23 - (tid >> 4);               // what the bin's mantissas of 24 bits count
-        const u64 m = (u64)sh.bin_lo[tid] + ((u64)sh.bin_hi[tid] << 12);
-        mine = e >= 0 ? m << e : m >> -e;
+      static_assert(2 * kThreads >= kBins, "two bins a thread");
+      auto bin_mass = [&](int i) -> u64 {
+        if (i >= kBins) return 0ull;
+        const int e = 44 - 23 - (i >> 4);                 // what the bin's mantissas of 24 bits count
+        const u64 m = (u64)sh.bin_lo[i] + ((u64)sh.bin_hi[i] << 12);
+        return e >= 0 ? m << e : m >> -e;
+      };
+      const u64 m0 = bin_mass(2 * tid), m1 = bin_mass(2 * tid + 1);
+      const u64 upto = block_scan(sh, m0 + m1);
+      if (upto >= target && upto - m0 - m1 < target) {
+        const bool second = upto - m1 < target;
+        sh.bin = 2 * tid + second;
+        sh.above = upto - m1 - (second ? 0ull : m0);
       }
-      const u64 upto = block_scan(sh, mine);
-      if (upto >= target && upto - mine < target) { sh.bin = tid; sh.above = upto - mine; }
       __syncthreads();
     }
     const int bin = sh.bin;
@@ -365,7 +371,7 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
       __syncthreads();
       if (lane == 0) { sh.red[warp] = kmin; sh.red2[warp] = kmax; }
       __syncthreads();
-      uint32_t lo = __reduce_min_sync(0xFFFFFFFFu, sh.red[lane]), hi = __reduce_max_sync(0xFFFFFFFFu, sh.red2[lane]);
+      uint32_t lo = __reduce_min_sync(0xFFFFFFFFu, lane < kWarps ? sh.red[lane] : 0xFFFFFFFFu), hi = __reduce_max_sync(0xFFFFFFFFu, sh.red2[lane]);
       auto mass_from = [&](uint32_t key) -> u64 {         // of the bin's tokens with that key and above
         Sum part;
         in_bin([&](int v, float w) { if (key_of((float)row[v]) >= key) part.add(w); });
@@ -507,6 +513,7 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
 }
 
 __device__ __forceinline__ void fill_table(Shared& sh) {
+  if (threadIdx.x < 32) { sh.sum[threadIdx.x] = 0ull; sh.red[threadIdx.x] = 0u; sh.red2[threadIdx.x] = 0u; }
   if (threadIdx.x < 16) {
     const double p = exp2(44.0 + (double)threadIdx.x / 16.0);
     const float hi = (float)p;

@@ -514,6 +514,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     }
     if (*abort_word != 0u) {
       // giving up: let the copies in flight land before this block goes away
+      asm volatile("cp.async.wait_all;" ::: "memory");
       for (int i = max(0, filled - stages); i < filled; ++i)
         mbar_wait(full + (i % stages) * 8, (uint32_t)((i / stages) & 1));
     }
@@ -582,6 +583,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       };
       int it = turns ? s : 0;
       ok = wait_warp(bars + kQFull, n_q++ & 1, abort_word);
+      // (a piece of one tile does not need the second row tile: it tells that it has seen the piece's Q)
+      if (ok && turns && s == 1 && leader) mbar_arrive(bars + kQFree);
       if (ok && it < p.len) qk(it);
       if (ok && it + step < p.len) qk(it + step);
       for (bool fresh = true; ok && it < p.len; it += step, fresh = false) {
@@ -758,6 +761,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
           tmem_wait_st();
         }
+        // The parity below cannot tell "P V(n) is done" from "P V(n - 1) is not": the last tile but one is
+        // waited for while the last one's P is still held back.  (Its S tells of P V(n - 2) only.)
+        if (it + step >= p.len && !fresh && !wait(bars + kOFull + s * 8, (n - 1) & 1)) { ok = false; break; }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + kPFull + buf * 8);
@@ -901,7 +907,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         if (!sync()) break;                             // the stage is free again
       }
       if (!ok) break;
-      if (NT == 2 ? t == 0 : tid < 1) mbar_arrive(bars + kQFree);
+      if (tid == 0) mbar_arrive(bars + kQFree);
       if (live && me == 0) {
         if (!p.whole)
           *reinterpret_cast<float2*>(a.ws_ml + (w0 + tr) * 2) = make_float2(top, sum);

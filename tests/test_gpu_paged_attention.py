@@ -229,3 +229,23 @@ def test_agrees_with_the_contiguous_call_on_the_same_rows():
     out, _ = run(c)
     # each is within 2^-8 (|out| + A) + 2^-15 (S + 1) A of 64 bits; |out| <= A < 1 and S < 16 here
     assert (a.float() - out.float()).abs().max() <= 2 * (2 * 2.0 ** -8 + 17 * 2.0 ** -15)
+
+
+@pytest.mark.parametrize("N,D,window", [(66, 128, 0), (66, 128, 150), (66, 64, 0), (40, 128, 0), (4, 128, 0)])
+def test_values_that_arrive_late(N, D, window):
+    """Keys in the cache, values not: the last two products of a piece are both under way at its end."""
+    B, H, H_kv, page = 30, 8, 4, 64
+    nodes = [N if b % 3 else N // 2 for b in range(B)]
+    c = make(N + D, B, N, H, H_kv, D, page, [150 + 37 * (b % 7) for b in range(B)], BF16, nodes)
+    c["q"] = (c["q"].float() * 2).to(BF16)         # peaked rows: a tile that is left out shows
+    ref = plain.attention(c["q"], c["k"], c["v"], c["table"], c["kv_len"], c["mask"], 1 / math.sqrt(D), window, 0, c["nodes"])
+    q, k, v = (c[x].cuda() for x in "qkv")
+    table, kv_len, n, mask = (to_dev(x) for x in (c["table"], c["kv_len"], c["nodes"], c["mask"].view(np.int32)))
+    flush = torch.empty(256 << 20, dtype=torch.int8, device="cuda")
+    for _ in range(6):
+        out = torch.full_like(q, 7.0)
+        lse = torch.full((B, H, N), 5.0, device="cuda")
+        flush.zero_()
+        k.view(torch.int16).sum()
+        rest.rest_paged_attention(q, k, v, table, kv_len, mask, 1 / math.sqrt(D), window=window, n_nodes=n, out=out, lse=lse)
+        plain.assert_attention(out, lse, ref, BF16, int(c["kv_len"].max()) + N)

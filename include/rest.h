@@ -372,6 +372,8 @@ rest_status rest_kv_commit(void* d_k, void* d_v, const int64_t* kv_strides, cons
  *                   0; free pages are handed out lowest number first, to contexts in order
  *   d_n_pages       int32[B]: table entries of each context in use
  * Tables are shared by all layers of a model; the row and page copies are made per layer.
+ * Rows from kv_len on are written wherever the table says: after rest_pages_fork those pages are the
+ * context's own, and they stay so as long as its length does not shrink into a shared page.
  *
  * rest_paged_kv_write   rows i < n_nodes[b] (i < N with d_n_nodes NULL) of d_k_new, d_v_new
  *                   (element (b,i,hk,d) at b*new_strides[0] + i*new_strides[1] + hk*new_strides[2]
@@ -438,6 +440,7 @@ rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int
  *   (infinities and NaN included).
  *
  *   d_q, d_out      element (b,i,h,d) at b*strides[0] + i*strides[1] + h*strides[2] + d (d_out: 6..8)
+ *                   (d_out overlaps no input)
  *   d_k_pages, d_v_pages  page p, KV head, row, d: strides[3..5]; strides are multiples of 8
  *                   elements, base pointers 16-byte aligned; dtype REST_BF16 or REST_FP16 for all four
  *   d_table         a page index outside [0, P) reads as rows of zeros: rows in sight need pages

@@ -6,12 +6,12 @@
 // tcgen05.mma: S = Q K^T, then O += P V.
 //
 // Work.  The key tiles of all (context, KV head) units stand in one flat list, and every thread
-// block ("team" of RB blocks when R needs several row blocks) takes an equal, contiguous share of
-// it: uneven lengths, windows, one long context or hundreds of short ones all give the same even
-// load in a single wave, and the shares follow from the lengths on the device alone.  A unit that
-// a share's border cuts leaves partial rows (unnormalised O, maximum, sum) in the caller's
-// scratch, which a second small kernel joins.  With a window the tiles between the sinks and the
-// earliest visible position are not in the list at all.
+// block takes an equal, contiguous share of it: uneven lengths, windows, one long context or
+// hundreds of short ones all give the same even load in a single wave, and the shares follow from
+// the lengths on the device alone.  A unit that a share's border cuts leaves partial rows
+// (unnormalised O, maximum, sum) in the caller's scratch, which a second small kernel joins.  When R
+// needs several row blocks of 256 rows, each has a list and blocks of its own (see plan).  With a
+// window the tiles between the sinks and the earliest visible position are not in the list at all.
 //
 // Two kernel shapes, picked by R (rows per KV head):
 //   R <= 128  one 128-row tile, two blocks per SM: bound by the K/V stream, so what counts is bytes
@@ -62,7 +62,8 @@ struct Args {
   int4* meta;                                           // per block: unit it starts and leaves unfinished
   float *ws_o, *ws_ml;                                  // partial rows [block][2][rows][D], [..][2]
   int64_t q_b, q_n, q_h, p_p, p_h, p_r, o_b, o_n, o_h, table_stride;
-  int B, H, H_kv, G, N, Wm, P, page_log, table_cols, window, sinks, teams, RB, rows;
+  int B, H, H_kv, G, N, Wm, P, page_log, table_cols, window, sinks, RB, rows;
+  int teams, teams_last;                                // blocks of each row block, and of the last one
   uint32_t g_inverse;                                   // ceil(2^32 / G), G > 1
   int slot[3];                                          // tensor-map coordinate (1..3) of row, head, page
   float scale_log2;
@@ -76,11 +77,19 @@ __device__ __forceinline__ int node_of(const Args& a, int r) {
 __device__ __forceinline__ long long divide(long long n, long long d) {
   return ((n | d) >> 32) == 0 ? (long long)((uint32_t)n / (uint32_t)d) : n / d;
 }
+// Blocks of a row block lie `apart` blocks from one another: the last one's stand behind those of all others,
+// which take turns (they read the same tiles at about the same time).
+struct Rows { int rb, team, teams, apart; };
+__device__ __forceinline__ Rows rows_of(const Args& a, int x, int teams, int teams_last) {
+  const int others = teams * (a.RB - 1);
+  if (x >= others) return {a.RB - 1, x - others, teams_last, 1};
+  return {x % (a.RB - 1), x / (a.RB - 1), teams, a.RB - 1};
+}
 // One context's keys and its list of visible tiles: the first ns tiles hold the sinks, the others
 // run from tile w0 to the end.
 struct Ctx { int L, n, w0, ns; long long nt; };
 template <int BN>
-__device__ __forceinline__ Ctx context(const Args& a, int b) {
+__device__ __forceinline__ Ctx context(const Args& a, int b, int row0) {    // (no tiles without rows from row0 on)
   Ctx c;
   const int cap = a.table_cols << a.page_log;           // a longer length has no pages behind it
   c.L = min(max(a.kv_len[b], 0), cap);
@@ -91,7 +100,7 @@ __device__ __forceinline__ Ctx context(const Args& a, int b) {
     c.w0 = first / BN;
     c.ns = min((min(a.sinks, c.L) + BN - 1) / BN, c.w0);
   }
-  c.nt = c.n == 0 ? 0 : c.ns + (c.L + c.n + BN - 1) / BN - c.w0;
+  c.nt = a.G * c.n <= row0 ? 0 : c.ns + (c.L + c.n + BN - 1) / BN - c.w0;
   return c;
 }
 template <int BN>
@@ -109,7 +118,7 @@ struct Walk {
       : a(a_), b(b_), rb(rb_), off(off_), left(left_) {}
   __device__ __forceinline__ bool next(Piece& p) {
     while (left > 0) {
-      p.c = context<BN>(a, b);
+      p.c = context<BN>(a, b, rb * ROWS);
       if (off >= a.H_kv * p.c.nt) { off -= a.H_kv * p.c.nt; ++b; continue; }
       p.b = b;
       p.hk = (int)divide(off, p.c.nt);
@@ -120,8 +129,8 @@ struct Walk {
       p.whole = p.len == (int)p.c.nt;
       off += p.len;
       left -= p.len;
-      p.rows = a.G * p.c.n - rb * ROWS;
-      if (p.rows > 0) { p.rows = min(p.rows, ROWS); return true; }
+      p.rows = min(a.G * p.c.n - rb * ROWS, ROWS);
+      return true;
     }
     return false;
   }
@@ -346,7 +355,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + kTmemSlot);
   volatile uint32_t* abort_word = reinterpret_cast<volatile uint32_t*>(ctl + kAbort);
   volatile int* s_bad = reinterpret_cast<volatile int*>(ctl + kBad);       // [piece % 8]: piece + 1
-  const int team = blockIdx.x / a.RB, rb = blockIdx.x % a.RB;
+  const Rows where = NT == 1 ? Rows{0, (int)blockIdx.x, a.teams_last, 1}      // one row tile: one row block
+                             : rows_of(a, blockIdx.x, a.teams, a.teams_last);
+  const int team = where.team, rb = where.rb, row0 = rb * S_::kRows;
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if ((sbase & 1023u) != 0) {   // the swizzled operand layout needs a 1024-byte aligned base
@@ -386,7 +397,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     const int per = (a.B + S_::kThreads - 1) / S_::kThreads;
     long long mine = 0;
     for (int i = 0; i < per; ++i)
-      if (tid * per + i < a.B) mine += a.H_kv * context<BN>(a, tid * per + i).nt;
+      if (tid * per + i < a.B) mine += a.H_kv * context<BN>(a, tid * per + i, row0).nt;
     long long inc = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -401,7 +412,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       if (w == warp) before = total;
       total += s_scan[w];
     }
-    teams = total < a.teams ? (int)total : a.teams;     // fewer tiles than teams: one each, the rest idle
+    teams = total < where.teams ? (int)total : where.teams;     // fewer tiles than teams: one each, the rest idle
     // no more than 64 pieces of a unit: joining 296 pieces of one KV head took longer than the keys
     // (32768 keys, one KV head: 51 us; in 128 pieces 27 us)
     teams = min((long long)teams, 64ll * a.B * a.H_kv);
@@ -413,7 +424,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     if (x0 < x1 && at <= x0 && x0 < at + mine) {        // one thread
       int b = tid * per;
       for (;; ++b) {
-        const long long n = a.H_kv * context<BN>(a, b).nt;
+        const long long n = a.H_kv * context<BN>(a, b, row0).nt;
         if (x0 < at + n) break;
         at += n;
       }
@@ -526,13 +537,13 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       long long off = *reinterpret_cast<long long*>(ctl + kStartOff), left = x1 - x0;
       int b = *reinterpret_cast<int*>(ctl + kStartB);
       for (;;) {
-        const long long n = a.H_kv * context<BN>(a, b).nt;
+        const long long n = a.H_kv * context<BN>(a, b, row0).nt;
         if (off + left <= n) break;
         left -= n - off;
         off = 0;
         ++b;
       }
-      const long long nt = context<BN>(a, b).nt, end = off + left;      // end > 0, inside context b
+      const long long nt = context<BN>(a, b, row0).nt, end = off + left;      // end > 0, inside context b
       const long long u0 = (end - 1) / nt * nt, u1 = u0 + nt;           // its unit
       const long long base = x1 - end;                                  // flat position of context b
       if (u1 > end && base + u0 >= x0) {
@@ -934,28 +945,32 @@ __global__ void __launch_bounds__(256) paged_attention_join_kernel(const __grid_
   asm volatile("griddepcontrol.wait;" ::: "memory");
   __shared__ float s_m[8], s_l[8], s_o[8][D];
   __shared__ int s_team, s_count[8];
-  const int rb = blockIdx.x % a.RB, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int team = blockIdx.x / a.RB;
-  if ((int)gridDim.x < a.teams * a.RB) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long units = (long long)a.B * a.H_kv;
+  const Rows mine = rows_of(a, blockIdx.x, (int)min(units, (long long)a.teams), (int)min(units, (long long)a.teams_last));
+  const int rb = mine.rb, teams = rb + 1 == a.RB ? a.teams_last : a.teams;
+  const int block0 = rb + 1 == a.RB ? a.teams * (a.RB - 1) : rb;   // (all scratch rows count to less than 2^31)
+  int team = mine.team;
+  if (units < teams) {
     const int nth = team;
     if (threadIdx.x == 0) s_team = -1;
     int before = 0;
-    for (int base = 0; base < a.teams; base += 256) {   // (teams <= two blocks an SM: one or two rounds)
+    for (int base = 0; base < teams; base += 256) {   // (teams <= two blocks an SM: one or two rounds)
       const int i = base + threadIdx.x;
-      const bool has = i < a.teams && a.meta[(int64_t)i * a.RB + rb].x != 0;
+      const bool has = i < teams && a.meta[block0 + i * mine.apart].x != 0;
       const unsigned bal = __ballot_sync(0xFFFFFFFFu, has);
       __syncthreads();
       if (lane == 0) s_count[warp] = __popc(bal);
       __syncthreads();
-      int mine = before + __popc(bal & ((1u << lane) - 1u));
-      for (int w = 0; w < 8; ++w) { if (w < warp) mine += s_count[w]; before += s_count[w]; }
-      if (has && mine == nth) s_team = i;
+      int nr = before + __popc(bal & ((1u << lane) - 1u));
+      for (int w = 0; w < 8; ++w) { if (w < warp) nr += s_count[w]; before += s_count[w]; }
+      if (has && nr == nth) s_team = i;
     }
     __syncthreads();
     team = s_team;
     if (team < 0) return;
   }
-  const int64_t block = (int64_t)team * a.RB + rb;
+  const int block = block0 + team * mine.apart;
   const int4 meta = a.meta[block];
   const int np = meta.x, b = meta.y, hk = meta.z;
   if (np == 0) return;
@@ -970,8 +985,9 @@ __global__ void __launch_bounds__(256) paged_attention_join_kernel(const __grid_
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
     if (row < rows) {
+      const int first = block * 2 * a.rows + row, step = mine.apart * 2 * a.rows;
       auto at = [&](int i) -> int64_t {                 // piece i: slot 1 of the first block, slot 0 of the others
-        return ((block + (int64_t)i * a.RB) * 2 + (i == 0 ? 1 : 0)) * a.rows + row;
+        return first + i * step + (i == 0 ? a.rows : 0);
       };
       for (int i0 = lo; i0 < hi; i0 += 32) {            // 32 pieces at a time, a lane for each one's maximum and sum
         float2 ml = make_float2(-INFINITY, 0.f);
@@ -1078,19 +1094,27 @@ bool encode_pool(CUtensorMap* map, const void* base, int dtype, int D, int page,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-struct Plan { int NT, RB, teams, rows; };
+struct Plan { int NT, RB, teams, teams_last, rows; };
 Plan plan(int H, int H_kv, int N) {
   Plan p;
   const int64_t R = (int64_t)(H / H_kv) * N;
   p.NT = R > 128 ? 2 : 1;
   p.RB = (int)((R + 128 * p.NT - 1) / (128 * p.NT));
   const int sms = rest::sm_count(), blocks = (p.NT == 1 ? 2 : 1) * (sms > 0 ? sms : 148);
-  p.teams = blocks / p.RB > 0 ? blocks / p.RB : 1;
+  // A last row block of one row tile's height is quicker with its key tiles (its two row tiles take turns at
+  // them), so it gets 0.6 of the blocks that another one has (16 x 16384 keys, 640 rows: 740 us with as many,
+  // 750 us with 0.5, 686 us with 0.6, 702 us with 0.65, 716 us with 0.75).
+  const bool half = p.NT == 2 && p.RB > 1 && R - (int64_t)(p.RB - 1) * 256 <= 128;
+  p.teams = half ? blocks * 20 / (20 * (p.RB - 1) + 12) : blocks / p.RB;
+  p.teams = p.teams > 0 ? p.teams : 1;
+  p.teams_last = blocks - p.teams * (p.RB - 1);
+  p.teams_last = p.teams_last > 0 ? p.teams_last : 1;
   p.rows = R < 128 * p.NT ? (int)R : 128 * p.NT;
   return p;
 }
+size_t blocks_of(const Plan& p) { return (size_t)p.teams * (p.RB - 1) + p.teams_last; }
 size_t workspace_bytes(const Plan& p, int D) {
-  const size_t blocks = (size_t)p.teams * p.RB;
+  const size_t blocks = blocks_of(p);
   return 32 + (blocks + 1) / 2 * 2 * sizeof(int4) + blocks * 2 * p.rows * (D + 2) * sizeof(float);
 }
 
@@ -1099,7 +1123,7 @@ rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
   using S_ = Shape<D, NT>;
   REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(paged_attention_kernel<T, D, NT, C>), smem_slot, S_::kSmem));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(a.teams * a.RB), 1, 1);
+  cfg.gridDim = dim3((unsigned)(a.teams * (a.RB - 1) + a.teams_last), 1, 1);
   cfg.blockDim = dim3((unsigned)S_::kThreads, 1, 1);
   cfg.dynamicSmemBytes = S_::kSmem;
   cfg.stream = st;
@@ -1113,9 +1137,10 @@ rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
   // never more cut units than shares or units; about eight blocks per SM in all, eight rows each at least
   // (one where units may be cut into more than 16 pieces)
   const int64_t units = (int64_t)a.B * a.H_kv;
-  const int cut = units < a.teams ? (int)units : a.teams, per = 8 * 148 / (cut * a.RB);
-  const int most = a.teams > 16 * units ? a.rows : (a.rows + 7) / 8;
-  cfg.gridDim = dim3((unsigned)(cut * a.RB), (unsigned)(per < 1 ? 1 : per > most ? most : per), 1);
+  auto cut = [&](int teams) { return units < teams ? (int)units : teams; };
+  const int joins = cut(a.teams) * (a.RB - 1) + cut(a.teams_last), per = 8 * 148 / joins;
+  const int most = (a.RB > 1 && a.teams > a.teams_last ? a.teams : a.teams_last) > 16 * units ? a.rows : (a.rows + 7) / 8;
+  cfg.gridDim = dim3((unsigned)joins, (unsigned)(per < 1 ? 1 : per > most ? most : per), 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.dynamicSmemBytes = 0;
   REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<T, D>, a));
@@ -1184,12 +1209,12 @@ extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pag
   a.o_b = strides[6]; a.o_n = strides[7]; a.o_h = strides[8];
   a.table_stride = table_stride;
   a.B = B; a.H = H; a.H_kv = H_kv; a.G = H / H_kv; a.N = N; a.Wm = (N + 31) / 32; a.P = P; a.table_cols = table_cols;
-  a.window = window; a.sinks = sinks; a.teams = pl.teams; a.RB = pl.RB; a.rows = pl.rows;
+  a.window = window; a.sinks = sinks; a.teams = pl.teams; a.teams_last = pl.teams_last; a.RB = pl.RB; a.rows = pl.rows;
   a.g_inverse = (uint32_t)((((u64)1 << 32) + a.G - 1) / a.G);
   a.scale_log2 = scale * kLog2e;
   a.page_log = 4;
   while ((1 << a.page_log) < page) ++a.page_log;
-  const size_t blocks = (size_t)pl.teams * pl.RB;
+  const size_t blocks = blocks_of(pl);
   a.meta = reinterpret_cast<int4*>((reinterpret_cast<uintptr_t>(d_ws) + 31) & ~(uintptr_t)31);     // 32-byte stores
   a.ws_o = reinterpret_cast<float*>(a.meta + (blocks + 1) / 2 * 2);
   a.ws_ml = a.ws_o + blocks * 2 * pl.rows * D;

@@ -249,3 +249,12 @@ def test_values_that_arrive_late(N, D, window):
         k.view(torch.int16).sum()
         rest.rest_paged_attention(q, k, v, table, kv_len, mask, 1 / math.sqrt(D), window=window, n_nodes=n, out=out, lse=lse)
         plain.assert_attention(out, lse, ref, BF16, int(c["kv_len"].max()) + N)
+
+
+@pytest.mark.parametrize("N,G,D", [(128, 5, 128), (128, 5, 64), (150, 2, 128), (200, 4, 128)])
+def test_row_blocks_with_shares_of_their_own(N, G, D):
+    """Several row blocks, the last one lower; contexts whose nodes leave it, or all but the first one, empty."""
+    lens = [700, 0, 65, 1300, 333, 4, 64, 900]
+    nodes = [N, 1, N // 2, N - 1, 0, N, 64 // G, N // 3]
+    check(make(N + G, len(lens), N, 2 * G, 2, D, 32, lens, BF16, nodes))
+    check(make(N - G, 1, N, 2 * G, 2, D, 32, lens[:1], BF16), 100, 3)

@@ -4,11 +4,17 @@ Argument marshalling only: every step runs in the library's kernels.  torch is u
 device memory and to supply the current CUDA stream.  There is no CPU fallback: importing
 works without the library, but every call raises if librest.so is missing or cannot load.
 
-The four entry points mirror include/rest.h:
+The entry points mirror include/rest.h.  One decoding step:
     rest_datastore_create / Datastore   Sec. 3.2, datastore = token stream + suffix array
     rest_draft                          Algorithms 1 and 2, breadth-first tree + mask
     rest_tree_attention                 Sec. 3.2, draft verification (tree attention)
     rest_accept                         Sec. 3.2, draft acceptance
+    rest_kv_commit                      accepted K/V rows moved to the front
+Serving, with a KV cache in pages:
+    rest_paged_attention                tree attention or one-token steps over pages, windows
+    rest_accept_sampled                 Sec. 4.1, acceptance against the target's probabilities
+    rest_paged_kv_write / _commit       a step's new rows; the accepted ones moved to the front
+    rest_pages_fork / _copy / _reserve / _release   contexts that share, get and give back pages
 """
 from __future__ import annotations
 

@@ -33,6 +33,13 @@
 // Precision: scores, maxima, sums and O in 32 bits; P is rounded to the cache's type for the
 // tensor core (half a step, 2^-9 of each probability in bf16 - the output is rounded as much), the
 // sum takes the unrounded values, so lse carries none of it.
+//
+// Measured (B200, time of captured calls, join included; the copy rate is 6536 GB/s, the bf16 matrix rate 1669
+// TFLOP/s): 1 token x 2048 keys, 32/8 heads, 15.2 us (latency); 64 nodes x 2048 keys, 32 KV heads, 24.4 us;
+// 61 ragged trees x 4096 keys, 32/8 heads, page 16, 246 us (606 TFLOP/s); 16 trees of 128 nodes x 16384 keys,
+// 40/8 heads, 691 us (1000 TFLOP/s); 64 trees of 33 nodes, window 4096, 270-285 us (4.0 TB/s); 256 tokens, window
+// 2048, D = 64, fp16, 202 us (5.5 TB/s).  In the fourth the exponential unit is busy half the time, the tensor core
+// 47 % (profile of half the keys); in the others the stream of pages and its latency decide.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -107,13 +114,12 @@ template <int BN>
 __device__ __forceinline__ int tile_key(const Ctx& c, int t) { return (t < c.ns ? t : t - c.ns + c.w0) * BN; }
 
 // A block's share of the flat tile list, piece by piece; every role of the block walks it alike.
-struct Piece { Ctx c; int b, hk, t0, len, rows; bool first, whole; };
+struct Piece { Ctx c; int b, hk, t0, len, rows; bool whole; };
 template <int BN, int ROWS>
 struct Walk {
   const Args& a;
   int b, rb;
   long long off, left;
-  bool at_start = true;
   __device__ Walk(const Args& a_, int b_, long long off_, long long left_, int rb_)
       : a(a_), b(b_), rb(rb_), off(off_), left(left_) {}
   __device__ __forceinline__ bool next(Piece& p) {
@@ -124,8 +130,6 @@ struct Walk {
       p.hk = (int)divide(off, p.c.nt);
       p.t0 = (int)(off - p.hk * p.c.nt);
       p.len = (int)min(p.c.nt - (long long)p.t0, left);
-      p.first = at_start;
-      at_start = false;
       p.whole = p.len == (int)p.c.nt;
       off += p.len;
       left -= p.len;

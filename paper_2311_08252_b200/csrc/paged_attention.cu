@@ -6,7 +6,7 @@
 // tcgen05.mma: S = Q K^T, then O += P V.
 //
 // Work.  The key tiles of all (context, KV head) units stand in one flat list, and every thread
-// block takes an equal, contiguous share of it: uneven lengths, windows, one long context or
+// block takes an equal, contiguous share of it, by cost: uneven lengths, windows, one long context or
 // hundreds of short ones all give the same even load in a single wave, and the shares follow from
 // the lengths on the device alone.  A unit that a share's border cuts leaves partial rows
 // (unnormalised O, maximum, sum) in the caller's scratch, which a second small kernel joins.  When R
@@ -37,7 +37,7 @@
 // Measured (B200, time of captured calls, join included; the copy rate is 6536 GB/s, the bf16 matrix rate 1669
 // TFLOP/s): 1 token x 2048 keys, 32/8 heads, 15.2 us (latency); 64 nodes x 2048 keys, 32 KV heads, 24.4 us;
 // 61 ragged trees x 4096 keys, 32/8 heads, page 16, 246 us (606 TFLOP/s); 16 trees of 128 nodes x 16384 keys,
-// 40/8 heads, 691 us (1000 TFLOP/s); 64 trees of 33 nodes, window 4096, 270-285 us (4.0 TB/s); 256 tokens, window
+// 40/8 heads, 691 us (1000 TFLOP/s); 64 trees of 33 nodes, window 4096, 218-241 us (4.8 TB/s); 256 tokens, window
 // 2048, D = 64, fp16, 202 us (5.5 TB/s).  In the fourth the exponential unit is busy half the time, the tensor core
 // 47 % (profile of half the keys); in the others the stream of pages and its latency decide.
 #include <cuda.h>
@@ -92,16 +92,24 @@ __device__ __forceinline__ Rows rows_of(const Args& a, int x, int teams, int tea
   if (x >= others) return {a.RB - 1, x - others, teams_last, 1};
   return {x % (a.RB - 1), x / (a.RB - 1), teams, a.RB - 1};
 }
+// A block of two row tiles is about twice as quick with a key tile when one row tile would hold all rows (the
+// two take turns then), so its share holds twice as many of them (64 windows of 4096 keys, 68 to 132 rows:
+// 290 us with equal shares, 218-241 us with 2 : 1, 230 us with 5 : 3).
+constexpr int kBoth = 2, kTurns = 1;
+__device__ __forceinline__ long long tiles_for(long long cost, int of_one) {          // rounded up
+  return of_one == 1 ? cost : divide(cost + of_one - 1, of_one);
+}
 // One context's keys and its list of visible tiles: the first ns tiles hold the sinks, the others
 // run from tile w0 to the end.
-struct Ctx { int L, n, w0, ns; long long nt; };
-template <int BN>
+struct Ctx { int L, n, w0, ns, cost; long long nt; };   // cost: of one of its tiles
+template <int BN, int TILES>
 __device__ __forceinline__ Ctx context(const Args& a, int b, int row0) {    // (no tiles without rows from row0 on)
   Ctx c;
   const int cap = a.table_cols << a.page_log;           // a longer length has no pages behind it
   c.L = min(max(a.kv_len[b], 0), cap);
   c.n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.N) : a.N;
   c.w0 = c.ns = 0;
+  c.cost = TILES == 1 ? 1 : a.G * c.n - row0 > 128 ? kBoth : kTurns;
   const int first = c.L - a.window + 1;                 // earliest position in any node's window
   if (a.window > 0 && first > 0) {
     c.w0 = first / BN;
@@ -116,7 +124,7 @@ __device__ __forceinline__ int tile_key(const Ctx& c, int t) { return (t < c.ns 
 // A block's share of the flat tile list, piece by piece; every role of the block walks it alike.
 struct Piece { Ctx c; int b, hk, t0, len, rows; bool whole; };
 template <int BN, int ROWS>
-struct Walk {
+struct Walk {                                           // left: cost up to the end of the share
   const Args& a;
   int b, rb;
   long long off, left;
@@ -124,15 +132,15 @@ struct Walk {
       : a(a_), b(b_), rb(rb_), off(off_), left(left_) {}
   __device__ __forceinline__ bool next(Piece& p) {
     while (left > 0) {
-      p.c = context<BN>(a, b, rb * ROWS);
+      p.c = context<BN, ROWS / 128>(a, b, rb * ROWS);
       if (off >= a.H_kv * p.c.nt) { off -= a.H_kv * p.c.nt; ++b; continue; }
       p.b = b;
       p.hk = (int)divide(off, p.c.nt);
       p.t0 = (int)(off - p.hk * p.c.nt);
-      p.len = (int)min(p.c.nt - (long long)p.t0, left);
+      p.len = (int)min(p.c.nt - (long long)p.t0, tiles_for(left, p.c.cost));
       p.whole = p.len == (int)p.c.nt;
       off += p.len;
-      left -= p.len;
+      left -= (long long)p.len * p.c.cost;
       p.rows = min(a.G * p.c.n - rb * ROWS, ROWS);
       return true;
     }
@@ -238,7 +246,7 @@ template <int D, int NT> struct Shape {
 enum {
   kKFull = 0, kKFree = 32, kVFull = 64, kVFree = 112, kSFull = 160, kPFull = 192, kOFull = 224, kQFull = 240, kQFree = 248,
   kTmemSlot = 256, kAbort = 260, kBad = 264 /* 8 x 4 */, kStartB = 296, kStartOff = 304, kTotal = 312,
-  kScan = 320 /* 12 x 8 */, kJoin = 416, kTurn = 424 /* 8 x 8 */
+  kScan = 320 /* 12 x 8 */, kJoin = 416, kTurn = 424 /* 8 x 8 */, kStartLeft = 488
 };
 
 // Bounded wait of a whole warp, with one result for all lanes (TMEM accesses and elected lanes need
@@ -394,14 +402,17 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
   // everything above is independent of the inputs; from here on global memory is read
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  // ---- this team's share [x0, x1) of the flat tile list, and the context that x0 lies in
+  // ---- this team's share of the flat tile list: the tiles that start in [x0, x1), and the first one's context
   long long x0, x1;
   int teams;
   {
     const int per = (a.B + S_::kThreads - 1) / S_::kThreads;
     long long mine = 0;
     for (int i = 0; i < per; ++i)
-      if (tid * per + i < a.B) mine += a.H_kv * context<BN>(a, tid * per + i, row0).nt;
+      if (tid * per + i < a.B) {
+        const Ctx c = context<BN, NT>(a, tid * per + i, row0);
+        mine += a.H_kv * c.nt * c.cost;
+      }
     long long inc = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -416,7 +427,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       if (w == warp) before = total;
       total += s_scan[w];
     }
-    teams = total < where.teams ? (int)total : where.teams;     // fewer tiles than teams: one each, the rest idle
+    // fewer tiles than teams: one each, the rest idle (no share is shorter than a tile)
+    teams = (int)min((long long)where.teams, NT == 1 ? total : max(total / kBoth, 1ll));
     // no more than 64 pieces of a unit: joining 296 pieces of one KV head took longer than the keys
     // (32768 keys, one KV head: 51 us; in 128 pieces 27 us)
     teams = min((long long)teams, 64ll * a.B * a.H_kv);
@@ -428,12 +440,17 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     if (x0 < x1 && at <= x0 && x0 < at + mine) {        // one thread
       int b = tid * per;
       for (;; ++b) {
-        const long long n = a.H_kv * context<BN>(a, b, row0).nt;
-        if (x0 < at + n) break;
+        const Ctx c = context<BN, NT>(a, b, row0);
+        const long long n = a.H_kv * c.nt * c.cost;
+        if (x0 < at + n) {
+          const long long skip = tiles_for(x0 - at, c.cost);
+          *reinterpret_cast<long long*>(ctl + kStartOff) = skip;
+          *reinterpret_cast<long long*>(ctl + kStartLeft) = x1 - at - skip * c.cost;
+          break;
+        }
         at += n;
       }
       *reinterpret_cast<int*>(ctl + kStartB) = b;
-      *reinterpret_cast<long long*>(ctl + kStartOff) = x0 - at;
     }
     if (tid == 0) {
       if (x0 >= x1) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);      // else the MMA warp writes it
@@ -445,8 +462,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
   Walk<BN, S_::kRows> walk(a, *reinterpret_cast<int*>(ctl + kStartB), *reinterpret_cast<long long*>(ctl + kStartOff),
-                           x1 - x0, rb);
-  if (x0 >= x1) walk.left = 0;
+                           x0 < x1 ? *reinterpret_cast<long long*>(ctl + kStartLeft) : 0ll, rb);
   Piece p;
 
   if (warp == S_::kSoftmax || warp == S_::kSoftmax + 1) {
@@ -538,23 +554,25 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       // {pieces, context, KV head}.  Its later pieces are the first pieces of the blocks that follow.
       int4 m = make_int4(0, 0, 0, 0);
       // step over whole contexts to the last tile of the share
-      long long off = *reinterpret_cast<long long*>(ctl + kStartOff), left = x1 - x0;
+      long long off = *reinterpret_cast<long long*>(ctl + kStartOff), left = *reinterpret_cast<long long*>(ctl + kStartLeft);
       int b = *reinterpret_cast<int*>(ctl + kStartB);
+      Ctx c;
+      long long count;
       for (;;) {
-        const long long n = a.H_kv * context<BN>(a, b, row0).nt;
-        if (off + left <= n) break;
-        left -= n - off;
+        c = context<BN, NT>(a, b, row0);
+        count = tiles_for(left, c.cost);
+        if (off + count <= a.H_kv * c.nt) break;
+        left -= (a.H_kv * c.nt - off) * c.cost;
         off = 0;
         ++b;
       }
-      const long long nt = context<BN>(a, b, row0).nt, end = off + left;      // end > 0, inside context b
-      const long long u0 = (end - 1) / nt * nt, u1 = u0 + nt;           // its unit
-      const long long base = x1 - end;                                  // flat position of context b
-      if (u1 > end && base + u0 >= x0) {
-        const long long total = *reinterpret_cast<long long*>(ctl + kTotal);
-        int c = team + 1;
-        while (total * (c + 1) / teams < base + u1) ++c;
-        m = make_int4(c - team + 1, b, (int)(u0 / nt), 0);
+      const long long end = off + count, u0 = (end - 1) / c.nt * c.nt, u1 = u0 + c.nt;      // its unit
+      const long long base = x1 - left - off * c.cost;                  // where context b starts
+      if (u1 > end && base + u0 * c.cost >= x0) {
+        const long long total = *reinterpret_cast<long long*>(ctl + kTotal), last = base + (u1 - 1) * c.cost;
+        int to = team + 1;
+        while (total * (to + 1) / teams <= last) ++to;
+        m = make_int4(to - team + 1, b, (int)(u0 / c.nt), 0);
       }
       a.meta[blockIdx.x] = m;
     }

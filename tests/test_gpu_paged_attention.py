@@ -258,3 +258,13 @@ def test_row_blocks_with_shares_of_their_own(N, G, D):
     nodes = [N, 1, N // 2, N - 1, 0, N, 64 // G, N // 3]
     check(make(N + G, len(lens), N, 2 * G, 2, D, 32, lens, BF16, nodes))
     check(make(N - G, 1, N, 2 * G, 2, D, 32, lens[:1], BF16), 100, 3)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (200, 5)])
+@pytest.mark.parametrize("N,G,H_kv,D,B", [(64, 4, 2, 128, 40), (140, 1, 3, 64, 40), (33, 4, 8, 128, 9), (64, 4, 1, 128, 3)])
+def test_contexts_of_one_and_two_row_tiles_in_turn(N, G, H_kv, D, B, window, sinks):
+    """Key tiles of contexts with few and with many rows cost differently; shares may begin inside one."""
+    rng = np.random.default_rng(N + B)
+    nodes = [int(rng.choice([0, 1, N // 3, N // 2, N - 1, N])) for _ in range(B)]
+    lens = [int(rng.choice([0, 1, 64, 63, 200, 391])) for _ in range(B)]
+    check(make(N + B, B, N, G * H_kv, H_kv, D, 16, lens, BF16, nodes), window, sinks)

@@ -514,6 +514,16 @@ def _call(fn, what, index, stream, *args):
         _check(rc, what)
 
 
+def _as_current(stream, t):
+    """`stream` (a torch stream or a handle) as the current one: what a call allocates and clears belongs to it."""
+    import torch
+    if isinstance(stream, torch.cuda.Stream):
+        return torch.cuda.stream(stream)
+    if not t.is_cuda:
+        raise RestError("the tensors must be on a CUDA device")
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=t.device))
+
+
 def _vec(t, name, index, n=None, dtype=None):
     """Pointer of a contiguous vector (int32 unless told otherwise) of n elements on GPU `index`."""
     import torch
@@ -572,6 +582,10 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
     lse: optional float32 [B,H,N].  workspace: a uint8 tensor of paged_attention_workspace_bytes(),
     not shared by calls that may overlap; None: one is allocated.  Returns out [B,N,H,D]."""
     import torch
+    if stream is not None:
+        with _as_current(stream, q):
+            return rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, window, sinks, n_nodes,
+                                        out, lse, workspace)
     L = _lib or lib()
     index, (P, H_kv, page, Dk), pool = _pool(k_pages, v_pages)
     dtype, shape, qs = q.dtype, q.shape, q.stride()
@@ -620,6 +634,10 @@ def rest_accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature,
     allocated when the library asks for it; False: none (each context walks row by row).  Returns
     (accept_len, accept_nodes, out_tokens) like rest_accept."""
     import torch
+    if stream is not None:
+        with _as_current(stream, tokens):
+            return rest_accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature, top_p, max_depth, out,
+                                       workspace=workspace)
     L = _lib or lib()
     index, (B, N), i32, f32 = tokens.get_device(), tokens.shape, torch.int32, torch.float32
     dtype, shape, ls = logits.dtype, logits.shape, logits.stride()
@@ -684,6 +702,9 @@ def rest_pages_fork(refs, block_table, n_pages, kv_len, parents, children, page,
     page is replaced by a page of the child's own.  Returns (copy_src, copy_dst, status) int32[F]:
     the pages to copy with rest_pages_copy in every layer (-1: none), and REST_CTX_* codes."""
     import torch
+    if stream is not None:
+        with _as_current(stream, refs):
+            return rest_pages_fork(refs, block_table, n_pages, kv_len, parents, children, page, copy_src, copy_dst, status)
     F, B, index = parents.numel(), block_table.shape[0], refs.get_device()
     out = tuple(torch.empty(F, dtype=torch.int32, device=refs.device) if t is None else t
                 for t in (copy_src, copy_dst, status))
@@ -706,6 +727,9 @@ def rest_pages_reserve(refs, block_table, n_pages, need_len, page, status=None, 
     """Gives every context pages until its table holds need_len[b] rows, all or none.  Returns
     status int32[B] (REST_CTX_*)."""
     import torch
+    if stream is not None:
+        with _as_current(stream, refs):
+            return rest_pages_reserve(refs, block_table, n_pages, need_len, page, status)
     B, index = block_table.shape[0], refs.get_device()
     if status is None:
         status = torch.empty(B, dtype=torch.int32, device=refs.device)

@@ -268,3 +268,20 @@ def test_contexts_of_one_and_two_row_tiles_in_turn(N, G, H_kv, D, B, window, sin
     nodes = [int(rng.choice([0, 1, N // 3, N // 2, N - 1, N])) for _ in range(B)]
     lens = [int(rng.choice([0, 1, 64, 63, 200, 391])) for _ in range(B)]
     check(make(N + B, B, N, G * H_kv, H_kv, D, 16, lens, BF16, nodes), window, sinks)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_what_a_call_allocates_belongs_to_its_stream(handle):
+    """out is cleared on the call's stream: work that waits on the current one does not wipe the result."""
+    c = make(5, 2, 8, 4, 2, 128, 16, [100, 40], BF16, [8, 5])
+    want, _ = run(c, want_lse=False)
+    q, k, v = (c[x].cuda() for x in "qkv")
+    table, kv_len, n, mask = (to_dev(x) for x in (c["table"], c["kv_len"], c["nodes"], c["mask"].view(np.int32)))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)                 # the current stream is busy
+    out = rest.rest_paged_attention(q, k, v, table, kv_len, mask, 1 / math.sqrt(128), n_nodes=n,
+                                    stream=side.cuda_stream if handle else side)
+    torch.cuda.synchronize()
+    x, y = out.cpu(), want.cpu()
+    assert (x[0] == y[0]).all() and (x[1, :5] == y[1, :5]).all() and (x[1, 5:] == 0).all()

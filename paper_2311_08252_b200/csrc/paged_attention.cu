@@ -36,8 +36,8 @@
 //
 // Measured (B200, time of captured calls, join included; the copy rate is 6536 GB/s, the bf16 matrix rate 1669
 // TFLOP/s): 1 token x 2048 keys, 32/8 heads, 15.2 us (latency); 64 nodes x 2048 keys, 32 KV heads, 24.4 us;
-// 61 ragged trees x 4096 keys, 32/8 heads, page 16, 246 us (606 TFLOP/s); 16 trees of 128 nodes x 16384 keys,
-// 40/8 heads, 691 us (1000 TFLOP/s); 64 trees of 33 nodes, window 4096, 218-241 us (4.8 TB/s); 256 tokens, window
+// 61 ragged trees x 4096 keys, 32/8 heads, page 16, 242 us (618 TFLOP/s); 16 trees of 128 nodes x 16384 keys,
+// 40/8 heads, 691 us (1000 TFLOP/s); 64 trees of 33 nodes, window 4096, 217 us (5.1 TB/s); 256 tokens, window
 // 2048, D = 64, fp16, 202 us (5.5 TB/s).  In the fourth the exponential unit is busy half the time, the tensor core
 // 47 % (profile of half the keys); in the others the stream of pages and its latency decide.
 #include <cuda.h>
@@ -92,10 +92,10 @@ __device__ __forceinline__ Rows rows_of(const Args& a, int x, int teams, int tea
   if (x >= others) return {a.RB - 1, x - others, teams_last, 1};
   return {x % (a.RB - 1), x / (a.RB - 1), teams, a.RB - 1};
 }
-// A block of two row tiles is about twice as quick with a key tile when one row tile would hold all rows (the
-// two take turns then), so its share holds twice as many of them (64 windows of 4096 keys, 68 to 132 rows:
-// 290 us with equal shares, 218-241 us with 2 : 1, 230 us with 5 : 3).
-constexpr int kBoth = 2, kTurns = 1;
+// A block of two row tiles is quicker with a key tile when one row tile would hold all rows (the two take turns
+// then), so its share holds more of them.  Costs 1 : 1, 4 : 3, 3 : 2, 2 : 1 took 270, 218, 217, 221 us for 64 windows
+// of 4096 keys with 68 to 132 rows, and 242, 242, 238, 291 us for 61 contexts of 2048 to 4096 keys with 128 to 256.
+constexpr int kBoth = 3, kTurns = 2;
 __device__ __forceinline__ long long tiles_for(long long cost, int of_one) {          // rounded up
   return of_one == 1 ? cost : divide(cost + of_one - 1, of_one);
 }

@@ -315,7 +315,7 @@ def _plain_take(refs, need):
     can be had, and the free pages in order."""
     free = torch.sort((refs != 0).to(torch.int32), stable=True).indices
     upto = need.cumsum(0)
-    return upto - need, (upto <= (refs == 0).sum()) | (need == 0), free
+    return upto - need, upto <= (refs == 0).sum(), free
 
 
 def _plain_fork(s):

@@ -809,7 +809,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       // scratch slot 1: the unit's first piece; 0: a later one (then it is the block's first piece)
       const int64_t w0 = ((int64_t)blockIdx.x * 2 + (p.t0 == 0 ? 1 : 0)) * a.rows + (turns ? 0 : s * 128);
       const long long mine = p.whole ? p.b * a.o_b + node * a.o_n + head * a.o_h : (w0 + tr) * D;
-      const bool bad = s_bad[piece & 7] == piece + 1;
+      bool bad = s_bad[piece & 7] == piece + 1;
       if (C == 1 && !turns) {                           // no copies: every thread writes its row
         const float w = p.whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f;
         if (warp_live) {
@@ -875,6 +875,10 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       {                                                 // the copies' maxima and sums
         float2* s_ml = reinterpret_cast<float2*>(smem + kStage);                   // [kAll]
         if (!sync()) break;                             // (NT = 2: the other tile's last S is done too)
+        // copy 0 adds back what any copy took out of V, so it looks behind a barrier that the others come to
+        // with all their tiles checked: in turns the other row tile's last one may be checked later than this
+        // one's last product is done
+        bad = s_bad[piece & 7] == piece + 1;
         s_ml[tid] = make_float2(m_used, l_run);
         if (!sync()) break;
         top = -INFINITY;

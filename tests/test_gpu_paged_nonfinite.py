@@ -1,0 +1,90 @@
+"""rest_paged_attention where queries, keys or values are not finite: a row is what 64 bits give for the
+keys that it sees, infinities and NaN included, whichever kernel shape its unit takes and whether or not
+a share's border cuts it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_util as plain
+import paper_2311_08252_b200 as rest
+from gpu_util import to_dev
+from test_gpu_paged_attention import BF16, FP16, make
+
+pytestmark = pytest.mark.gpu
+
+
+def row(c, b, r):
+    """(page, row in it) of row r of context b."""
+    return plain.row_of(c["table"], c["k"].shape[2], c["k"].shape[0], b, r)
+
+
+def reference(c, window=0, sinks=0):
+    """plain.attention; NaN and infinities of the inputs go through its 64-bit products as they are."""
+    return plain.attention(c["q"], c["k"], c["v"], c["table"], c["kv_len"], c["mask"], 1 / math.sqrt(c["q"].shape[3]),
+                           window, sinks, c["nodes"])
+
+
+def device(c):
+    args = [c[x].cuda() for x in "qkv"] + [to_dev(c["table"]), to_dev(c["kv_len"])]
+    args.append(None if c["mask"] is None else to_dev(c["mask"].view(np.int32)))
+    return args, None if c["nodes"] is None else to_dev(c["nodes"])
+
+
+def attend(args, n_nodes, window=0, sinks=0):
+    B, N, H, D = args[0].shape
+    out = torch.full_like(args[0], 7.0)
+    lse = torch.full((B, H, N), 5.0, device="cuda")
+    rest.rest_paged_attention(*args, 1 / math.sqrt(D), window=window, sinks=sinks, n_nodes=n_nodes, out=out, lse=lse)
+    return out, lse
+
+
+def assert_same_kind(got, ref, live):
+    """NaN, +infinity and -infinity in the same places (live: rows that exist)."""
+    got, ref = got.double().cpu()[live], ref[live]
+    for kind in (torch.isnan, torch.isposinf, torch.isneginf):
+        assert torch.equal(kind(got), kind(ref)), (kind.__name__, int(kind(got).sum()), int(kind(ref).sum()))
+
+
+def exists(c):
+    """Rows [B,N] of nodes that exist."""
+    B, N = c["q"].shape[:2]
+    nodes = np.full(B, N) if c["nodes"] is None else c["nodes"]
+    return torch.from_numpy(np.arange(N)[None] < nodes[:, None])
+
+
+def assert_attention(out, lse, c, ref):
+    """Kinds everywhere, and paged_util.assert_attention's bounds where 64 bits are finite (columns and rows
+    do not mix, so a column's bound has its own sum of magnitudes)."""
+    live = exists(c)
+    assert_same_kind(out, ref[0], live)
+    assert_same_kind(lse.transpose(1, 2), ref[1].transpose(1, 2), live)
+    finite = ref[0].isfinite() & live[:, :, None, None]
+    got = torch.where(finite, out.double().cpu(), math.nan)
+    want = tuple(torch.where(finite, t, math.nan) for t in (ref[0], ref[2]))
+    plain.assert_attention(torch.where(got.isnan(), 0.0, got), None, (want[0], ref[1], want[1], ref[3]), c["q"].dtype,
+                           int(c["kv_len"].max()) + c["q"].shape[1])
+
+
+@pytest.mark.parametrize("N,G,D,few", [(40, 4, 128, 20), (66, 2, 64, 60), (140, 1, 128, 100), (128, 5, 128, 128),
+                                       (150, 2, 128, 150)])
+def test_values_taken_out_by_the_other_row_tile_come_back(N, G, D, few):
+    """More than 128 rows by shape, but no more than 128 in this context or in its last row block: two row
+    tiles take the key tiles in turn.  NaN in the V of a node in sight, in the last key tile (keys in the
+    cache, values not, so that the tiles are checked late): every row that sees it is NaN, no other one."""
+    B, H_kv, page = 24, 3, 64
+    lens = [64 * (1 + b % 8) + (0, 63, 1, 30)[b % 4] for b in range(B)]
+    c = make(N + G, B, N, G * H_kv, H_kv, D, page, lens, BF16, [few] * B)
+    for b in range(B):
+        at = row(c, b, lens[b] + (few - 1 if b % 2 else 0))
+        c["v"][at[0], :, at[1], 5:D:7] = math.nan
+    ref = reference(c)
+    assert ref[0][exists(c)].isnan().any() and not ref[0][exists(c)].isnan().all()
+    args, n_nodes = device(c)
+    flush = torch.empty(256 << 20, dtype=torch.int8, device="cuda")
+    for _ in range(4):
+        flush.zero_()
+        args[1].view(torch.int16).sum()
+        out, lse = attend(args, n_nodes)
+        assert_attention(out, lse, c, ref)

@@ -64,7 +64,7 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 
 struct Shared {
   float2 pow16[16];                             // 2^(44 + j/16) as a float and what it leaves
-  u64 sum[32], left, above, seg_before, cut;    // (a warp looks at all 32: those of no warp stay as they began)
+  u64 sum[32], left, above, over, seg_before, cut;   // (a warp looks at all 32: those of no warp stay as they began)
   ulonglong2 list[kList];                       // {order: key, then ~index; weight}
   uint32_t bin_lo[kBins], bin_hi[kBins];        // sums of the low and high 12 bits of the weights' mantissas
   uint32_t red[32], red2[32];
@@ -126,6 +126,11 @@ struct Sum {
   }
   __device__ __forceinline__ u64 total() const { return ((u64)high << 22) + (u64)(long long)(int)low; }
 };
+// How far apart the weights of two tokens may be for the one with the larger logit to have the smaller
+// weight: before they are rounded, weights are off by less than 5e-9 of themselves (the series' products,
+// 2^-24 of |q| < 0.022, and the table), so after it by one step of 2^-23 more, or by one whole number where
+// that is more.  Here 16 steps.
+__device__ __forceinline__ float slack_of(float w) { return fmaf(w, 0x1p-19f, 1.f); }
 __device__ __forceinline__ int bin_of(float w) { return (int)((kOneBits + 0x7FFFFFu - __float_as_uint(w)) >> 19); }
 
 __device__ __forceinline__ u64 warp_sum(u64 x) {
@@ -219,7 +224,7 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
   for (int i = tid; i < kBins; i += kThreads) sh.bin_lo[i] = sh.bin_hi[i] = 0u;
   uint32_t top = __reduce_max_sync(0xFFFFFFFFu, key_of(most));
   if (lane == 0) sh.red[warp] = top;
-  if (tid == 0) { sh.cut_tie = 0x7FFFFFFF; sh.bin = -1; sh.n_list = 0; }
+  if (tid == 0) { sh.cut_tie = 0x7FFFFFFF; sh.bin = -1; sh.n_list = 0; sh.over = 0ull; }
   __syncthreads();
   top = __reduce_max_sync(0xFFFFFFFFu, sh.red[lane]);
   if (top == 0) return make_int2(-1, -1);
@@ -294,9 +299,10 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
   };
   const int fours = (shift + V + 3) / 4;
 
-  // ---- 3. the nucleus: tokens of weight above cut_w, and of those at cut_w the ones from (cut_key,
-  // cut_tie) up
-  float cut_w = 0.f;
+  // ---- 3. the nucleus: the tokens from (cut_key, cut_tie) up.  Rounding may give the smaller of two logits
+  // that are next to one another the larger weight, so weights decide only where they are further apart than
+  // that (see slack_of) from cut_w, and logits everywhere else.
+  float cut_w = 0.f, slack = 0.f;
   uint32_t cut_key = 0;
   int cut_tie = 0x7FFFFFFF;
   if (cut) {
@@ -319,15 +325,17 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
       }
       __syncthreads();
     }
-    const int bin = sh.bin;
-    const u64 above = sh.above;                 // mass of the bins that are kept whole
-    // fn(token, weight) for the tokens of the bin: bits in [first, first + 2^19)
-    const uint32_t first = kOneBits + 0x7FFFFFu - ((uint32_t)bin << 19) - 0x7FFFFu;
+    // fn(token, weight) for the tokens of the bin (weights in [low, high)) and for those that may be in
+    // another one by rounding alone: any token above them all has a larger logit than any in the bin, any
+    // below a smaller one
+    const uint32_t low_bits = kOneBits + 0x780000u - ((uint32_t)sh.bin << 19);
+    const float low = __uint_as_float(low_bits), high = __uint_as_float(low_bits + 0x80000u);
+    const uint32_t first = __float_as_uint(fmaxf(low - slack_of(low), 1.f)), width = __float_as_uint(high + slack_of(high)) - first;
     auto in_bin = [&](auto fn) {
       each(tid, fours, kThreads, [&](int v, const float (&w)[4]) {
         bool is[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) is[k] = __float_as_uint(w[k]) - first < 0x80000u;
+        for (int k = 0; k < 4; ++k) is[k] = __float_as_uint(w[k]) - first < width;
         if (is[0] || is[1] || is[2] || is[3]) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
@@ -338,9 +346,11 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
     in_bin([&](int v, float w) {
       const int at = atomicAdd(&sh.n_list, 1);
       if (at < kList) sh.list[at] = make_ulonglong2((u64)key_of((float)row[v]) << 32 | (uint32_t)~v, whole(w));
+      if (w >= high) atomicAdd(&sh.over, whole(w));
     });
     __syncthreads();
     const int n = sh.n_list;
+    const u64 above = sh.above - sh.over;       // mass of the tokens that are above all of these
     if (n <= kList) {
       // the mass before each token of the bin; several lanes share a token when there are few
       int parts = 1;
@@ -413,9 +423,10 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
       mass = above + over + ties * one;
     }
     cut_w = weight<T>(sh, r, of_key(cut_key));
+    slack = slack_of(cut_w);
   }
   auto kept = [&](int v, float w) -> bool {
-    if (w != cut_w) return w > cut_w;
+    if (fabsf(w - cut_w) > slack) return w > cut_w;
     if (!cut) return false;                     // (weight 0)
     const uint32_t key = key_of((float)row[v]);
     return key > cut_key || (key == cut_key && v <= cut_tie);
@@ -464,7 +475,7 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
   __syncthreads();
   if (sh.child >= 0) return make_int2(sh.child, sh.tok[sh.child]);
 
-  // ---- 5. the drawn token, from what the refused children leave: first the 1/32 of the row that holds
+  // ---- 5. the drawn token, from what the refused children leave: first the 1/16 of the row that holds
   // it (a warp's share), then the token in it
   for (int j = tid; j < sh.n_refused; j += kThreads) {
     if (KEPT) s_w[shift + sh.refused[j]] = 0.f;
@@ -480,7 +491,7 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
   each(f0 + lane, f1, 32, [&](int v, const float (&w)[4]) {
     bool tie = false;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) tie = tie || w[k] == cut_w;
+    for (int k = 0; k < 4; ++k) tie = tie || fabsf(w[k] - cut_w) <= slack;
     if (KEPT && (!tie || !cut)) {                          // nobody needs a closer look
 #pragma unroll
       for (int k = 0; k < 4; ++k) part.add(w[k] > cut_w ? w[k] : 0.f);
@@ -501,7 +512,7 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
   const int g0 = min(fours, sh.seg * per), g1 = min(fours, g0 + per);
   const int s0 = max(g0 * 4 - shift, 0), s1 = min(V, g1 * 4 - shift);
   u64 before = sh.seg_before;
-  for (int base = s0; base < s1; base += kThreads) {      // (more than one round for more than 32768 tokens)
+  for (int base = s0; base < s1; base += kThreads) {      // (more than one round for more than 8192 tokens)
     const int v = base + tid;
     const float w = v < s1 ? weight_at(v) : 0.f;
     const u64 mine = v < s1 && there(v, w) ? whole(w) : 0ull;

@@ -886,9 +886,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
 #pragma unroll
         for (int c = 0; c < copies; ++c) top = fmaxf(top, s_ml[tr + c * apart].x);
 #pragma unroll
-        for (int c = 0; c < copies; ++c) {
-          const float2 ml = s_ml[tr + c * apart];
-          if (ml.x != -INFINITY) sum += ml.y * ex2(ml.x - top);
+        for (int c = 0; c < copies; ++c) {              // (a maximum passes NaN over: with it alone it stays at
+          const float2 ml = s_ml[tr + c * apart];       // -infinity, and the sum, 0 otherwise, says so)
+          sum += ml.y * (ml.x == -INFINITY ? 0.f : ex2(ml.x - top));
         }
         w = m_used == -INFINITY ? 0.f : ex2(m_used - top);
       }

@@ -10,7 +10,7 @@ import torch
 import paged_util as plain
 import paper_2311_08252_b200 as rest
 from gpu_util import to_dev
-from test_gpu_paged_attention import BF16, FP16, make
+from test_gpu_paged_attention import BF16, make
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +88,47 @@ def test_values_taken_out_by_the_other_row_tile_come_back(N, G, D, few):
         args[1].view(torch.int16).sum()
         out, lse = attend(args, n_nodes)
         assert_attention(out, lse, c, ref)
+
+
+# units of 1, 24, 48, 100 rows (four, four, two copies of the rows, none), 130 rows, and 130 by shape of which
+# 100 exist (two row tiles that take the key tiles in turn)
+SHAPES = [(1, 1, 128, 1), (6, 4, 64, 6), (48, 1, 128, 48), (50, 2, 128, 50), (130, 1, 64, 130), (65, 2, 128, 50)]
+# whole units (many contexts: a share holds several) and cut ones (one context over all blocks)
+SPREADS = [([130, 64, 16, 0, 63, 300] * 30, 2), ([1500], 2)]
+
+
+def small(seed, N, G, D, few, lens, H_kv, dtype=BF16):
+    B = len(lens)
+    if B > 60 and N * G > 20:
+        lens = lens[:60]
+    return make(seed, len(lens), N, G * H_kv, H_kv, D, 16, lens, dtype, [few] * len(lens))
+
+
+def verdict(c, window=0, sinks=0):
+    ref = reference(c, window, sinks)
+    args, n_nodes = device(c)
+    out, lse = attend(args, n_nodes, window, sinks)
+    assert_attention(out, lse, c, ref)
+    return ref
+
+
+@pytest.mark.parametrize("lens,H_kv", SPREADS)
+@pytest.mark.parametrize("N,G,D,few", SHAPES)
+def test_a_query_of_nan_gives_nan(N, G, D, few, lens, H_kv):
+    c = small(1, N, G, D, few, lens, H_kv)
+    c["q"][:, few // 2, ::2] = math.nan
+    ref = verdict(c)
+    assert ref[0][:, few // 2, ::2].isnan().all() and ref[0][:, few // 2, 1::2].isfinite().all()
+
+
+@pytest.mark.parametrize("lens,H_kv", SPREADS)
+@pytest.mark.parametrize("N,G,D,few", SHAPES)
+def test_one_key_of_nan_in_sight_gives_nan(N, G, D, few, lens, H_kv):
+    """In context after context another key: a prefix row (all rows see it), or a node (it and those below)."""
+    c = small(2, N, G, D, few, lens, H_kv)
+    for b, L in enumerate(c["kv_len"].tolist()):
+        r = [L + few - 1, 0, L // 2, L - 1, L + few // 2][b % 5]
+        at = row(c, b, max(r, 0))
+        c["k"][at[0], b % H_kv, at[1], 3] = math.nan
+    ref = verdict(c)
+    assert ref[0].isnan().any()

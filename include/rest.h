@@ -437,7 +437,8 @@ rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int
  *   p < sinks or p > x - window (prefix row l stands at position l).
  *   out = softmax(scale * q.k) v in fp32, rounded once; a node that sees nothing gets 0 and an lse
  *   of -infinity.  Keys that a node does not see never touch its result, whatever they hold
- *   (infinities and NaN included).
+ *   (infinities and NaN included).  An infinity or NaN in v of a key that it does see decides that
+ *   column of out however small the key's probability is; NaN among its scores makes the row NaN.
  *
  *   d_q, d_out      element (b,i,h,d) at b*strides[0] + i*strides[1] + h*strides[2] + d (d_out: 6..8)
  *                   (d_out overlaps no input)

@@ -330,28 +330,63 @@ __device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int dept
   return v;
 }
 
-// What was taken out of V (see below), added to columns d0 .. d0 + 15 of a row that does
-// see its key.
-template <typename T, int BN>
-__device__ __noinline__ void add_back(const Args& a, Piece p, int node, int depth, u64 mask0, int d0, uint32_t (&o)[16]) {
-  for (int it = 0; it < p.len; ++it) {
-    const int key0 = tile_key<BN>(p.c, p.t0 + it);
-    if (all_see<BN>(a, p.c, key0)) continue;
-    for (int h = 0; h < BN / 64; ++h) {
-      for (u64 vis = visible(a, p.c, p.b, node, depth, mask0, key0 + 64 * h); vis; vis &= vis - 1) {
-        const int key = key0 + 64 * h + __ffsll((long long)vis) - 1, col = key >> a.page_log;
-        const int page = col < a.table_cols ? a.table[p.b * a.table_stride + col] : -1;
-        if (page < 0 || page >= a.P) continue;
-        const T* v = static_cast<const T*>(a.v) + page * a.p_p + p.hk * a.p_h +
-                     (key & ((1 << a.page_log) - 1)) * a.p_r + d0;
-        for (int j = 0; j < 16; ++j) {
-          const float f = (float)v[j];
-          if (!isfinite(f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + f);
+// Values of V that are not finite, at keys that a row sees, decide their columns of the row alone: +infinity,
+// -infinity, or NaN where there is a NaN or both.  The products do not say so (they were taken out of masked
+// tiles, and a probability that is 0, by rounding or because the key belongs to another copy, makes NaN of
+// them), so such columns of a piece's rows, at `mine` of the output or the scratch, are written once more.
+// For whole warps, a row (`live`) a lane: the lanes read a key each, then every row looks at those that hold
+// something.  Rare, and far from free (about a microsecond a key tile and 16 columns).
+template <typename T, int D, int BN>
+__device__ __noinline__ void write_not_finite(const Args& a, Piece p, bool live, int node, int depth, u64 mask0,
+                                              long long mine) {
+  const int lane = threadIdx.x & 31;
+  constexpr uint32_t inf = Type<T>::exponent;
+  for (int d0 = 0; d0 < D; d0 += 16) {
+    uint32_t found = 0;                                 // bit j: +infinity or NaN in column d0 + j; 16 + j: -infinity or NaN
+    for (int it = 0; it < p.len; ++it) {
+      const int first = tile_key<BN>(p.c, p.t0 + it);
+      u64 vis = 0ull;
+      bool asked = false;
+#pragma unroll
+      for (int h = 0; h < BN; h += 32) {
+        const int key = first + h + lane, col = key >> a.page_log;
+        const int page = key < p.c.L + p.c.n && col < a.table_cols ? a.table[p.b * a.table_stride + col] : -1;
+        uint32_t odd = 0;
+        if (page >= 0 && page < a.P) {
+          const uint4* v = reinterpret_cast<const uint4*>(static_cast<const T*>(a.v) + page * a.p_p + p.hk * a.p_h +
+                                                          (key & ((1 << a.page_log) - 1)) * a.p_r + d0);
+          const uint4 x = v[0], y = v[1];
+          const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const uint32_t e = w[j >> 1] >> (16 * (j & 1)) & 0xFFFFu;
+            if ((e & 0x7FFFu) < inf) continue;
+            if (e != (inf | 0x8000u)) odd |= 1u << j;
+            if (e != inf) odd |= 0x10000u << j;
+          }
+        }
+        for (unsigned which = __ballot_sync(0xFFFFFFFFu, odd != 0); which; which &= which - 1) {
+          const int l = __ffs(which) - 1;
+          const uint32_t there = __shfl_sync(0xFFFFFFFFu, odd, l);
+          if (!asked) vis = !live ? 0ull : all_see<BN>(a, p.c, first) ? ~0ull : visible(a, p.c, p.b, node, depth, mask0, first);
+          asked = true;
+          if ((vis >> (h + l)) & 1u) found |= there;
         }
       }
     }
+    for (int j = 0; j < 16; ++j) {
+      const uint32_t plus = found >> j & 1u, minus = found >> (16 + j) & 1u;
+      if (!(plus | minus)) continue;
+      const uint32_t x = plus & minus ? 0x7FFFu : minus ? inf | 0x8000u : inf;
+      if (p.whole)
+        static_cast<uint16_t*>(a.out)[mine + d0 + j] = (uint16_t)x;
+      else
+        a.ws_o[mine + d0 + j] = __uint_as_float(plus & minus ? 0x7FFFFFFFu : minus ? 0xFF800000u : 0x7F800000u);
+    }
   }
 }
+// a partial O, weighed: what is not finite stays so under a weight that rounds to 0
+__device__ __forceinline__ float weighed(float o, float w) { return fabsf(o) < INFINITY ? o * w : o; }
 
 template <typename T, int D, int NT, int C>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, NT == 1 ? 2 : 1)
@@ -691,7 +726,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         if (__builtin_expect(!plain, 0)) {
           const int key0 = tile_key<BN>(p.c, p.t0 + it);
           // Values of V that are not finite would reach rows that do not see their key (0 x NaN): take
-          // them out of the tile, and remember the piece if the key exists (see the epilogue).  Both row
+          // them out of the tile, and remember the piece if the key exists (the epilogue puts in what they
+          // come to; where all rows see the whole tile, they are left in it and show in O).  Both row
           // tiles do it when both use the tile, each before its own P V; the piece is remembered before a
           // value is cleared, so whoever finds it cleared finds it remembered.  (One row tile is never
           // more than six key tiles ahead of the other, so eight pieces are told apart.)
@@ -809,7 +845,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       // scratch slot 1: the unit's first piece; 0: a later one (then it is the block's first piece)
       const int64_t w0 = ((int64_t)blockIdx.x * 2 + (p.t0 == 0 ? 1 : 0)) * a.rows + (turns ? 0 : s * 128);
       const long long mine = p.whole ? p.b * a.o_b + node * a.o_n + head * a.o_h : (w0 + tr) * D;
-      bool bad = s_bad[piece & 7] == piece + 1;
+      float odd = 0.f;                                  // NaN when something in this row of O is not finite
       if (C == 1 && !turns) {                           // no copies: every thread writes its row
         const float w = p.whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f;
         if (warp_live) {
@@ -820,15 +856,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             tmem_load(o_col + c * 16, o);
             if (!live) continue;
 #pragma unroll
+            for (int j = 0; j < 16; ++j) odd = fmaf(__uint_as_float(o[j]), 0.f, odd);
+#pragma unroll
             for (int j = 0; j < 16; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
-            if (__builtin_expect(bad, 0)) {             // rare; a copy, so that o stays in registers otherwise
-              uint32_t y[16];
-#pragma unroll
-              for (int j = 0; j < 16; ++j) y[j] = o[j];
-              add_back<T, BN>(a, p, node, depth, mask0, c * 16, y);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = y[j];
-            }
             if (p.whole) {
               T* op = static_cast<T*>(a.out) + mine + c * 16;
 #pragma unroll
@@ -849,6 +879,10 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
                              : "memory");
             }
           }
+          // (a row whose sum is NaN is NaN throughout)
+          const bool bad = s_bad[piece & 7] == piece + 1;
+          if (__builtin_expect(__any_sync(0xFFFFFFFFu, live && (bad || odd != 0.f)), 0))
+            write_not_finite<T, D, BN>(a, p, live && l_run == l_run, node, depth, mask0, mine);
         }
         if (live) {
           if (!p.whole)
@@ -875,10 +909,6 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       {                                                 // the copies' maxima and sums
         float2* s_ml = reinterpret_cast<float2*>(smem + kStage);                   // [kAll]
         if (!sync()) break;                             // (NT = 2: the other tile's last S is done too)
-        // copy 0 adds back what any copy took out of V, so it looks behind a barrier that the others come to
-        // with all their tiles checked: in turns the other row tile's last one may be checked later than this
-        // one's last product is done
-        bad = s_bad[piece & 7] == piece + 1;
         s_ml[tid] = make_float2(m_used, l_run);
         if (!sync()) break;
         top = -INFINITY;
@@ -909,20 +939,16 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             tmem_load(o_col + c + d, o);
             if (!live) continue;
 #pragma unroll
+            for (int j = 0; j < 16; ++j) odd = fmaf(__uint_as_float(o[j]), 0.f, odd);
+#pragma unroll
             for (int j = 0; j < 16; ++j) o[j] = w == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * w);
-            if (__builtin_expect(bad && me == 0, 0)) {                       // rare; a copy, so that o stays in registers otherwise
-              uint32_t y[16];
-#pragma unroll
-              for (int j = 0; j < 16; ++j) y[j] = o[j];
-              add_back<T, BN>(a, p, node, depth, mask0, c + d, y);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = y[j];
-            }
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               *reinterpret_cast<uint4*>(stage(me, tr, (d >> 2) + e)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           }
         }
+        // (one of two row tiles in turn may have no tile: then O is what was there before)
+        if (live && odd != 0.f && (!turns || s < p.len)) s_bad[piece & 7] = piece + 1;
         if (!sync()) break;
         // the warps that hold copies of the same 32 rows share them out again
 #pragma unroll 2
@@ -944,6 +970,10 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         if (!sync()) break;                             // the stage is free again
       }
       if (!ok) break;
+      // looked at behind barriers that all copies come to with their tiles checked and their O seen: in turns,
+      // one row tile's last tile may be checked later than the other one's last product is done
+      if (me == 0 && warp_live && __builtin_expect(__any_sync(0xFFFFFFFFu, s_bad[piece & 7] == piece + 1), 0))
+        write_not_finite<T, D, BN>(a, p, live && sum == sum, node, depth, mask0, mine);
       if (tid == 0) mbar_arrive(bars + kQFree);
       if (live && me == 0) {
         if (!p.whole)
@@ -1028,7 +1058,7 @@ __global__ void __launch_bounds__(256) paged_attention_join_kernel(const __grid_
         l = l * old + sum;
         m = top;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= old;
+        for (int e = 0; e < E; ++e) o[e] = weighed(o[e], old);
         const int count = min(32, hi - i0);
 #pragma unroll 8
         for (int i = 0; i < count; ++i) {
@@ -1038,8 +1068,7 @@ __global__ void __launch_bounds__(256) paged_attention_join_kernel(const __grid_
           else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(a.ws_o + x * D + lane * E);
           const float wi = __shfl_sync(0xFFFFFFFFu, w, i);
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (wi != 0.f) o[e] += v[e] * wi;
+          for (int e = 0; e < E; ++e) o[e] += weighed(v[e], wi);
         }
       }
     }
@@ -1061,8 +1090,7 @@ __global__ void __launch_bounds__(256) paged_attention_join_kernel(const __grid_
         const float c = s_m[w] == -INFINITY ? 0.f : ex2(s_m[w] - m);
         l += s_l[w] * c;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (c != 0.f) o[e] += s_o[w][lane * E + e] * c;
+        for (int e = 0; e < E; ++e) o[e] += weighed(s_o[w][lane * E + e], c);
       }
     }
     if (row >= rows) continue;

@@ -10,7 +10,7 @@ import torch
 import paged_util as plain
 import paper_2311_08252_b200 as rest
 from gpu_util import to_dev
-from test_gpu_paged_attention import BF16, make
+from test_gpu_paged_attention import BF16, FP16, make
 
 pytestmark = pytest.mark.gpu
 
@@ -98,17 +98,18 @@ SPREADS = [([130, 64, 16, 0, 63, 300] * 30, 2), ([1500], 2)]
 
 
 def small(seed, N, G, D, few, lens, H_kv, dtype=BF16):
-    B = len(lens)
-    if B > 60 and N * G > 20:
-        lens = lens[:60]
     return make(seed, len(lens), N, G * H_kv, H_kv, D, 16, lens, dtype, [few] * len(lens))
 
 
 def verdict(c, window=0, sinks=0):
-    ref = reference(c, window, sinks)
+    """All contexts in one call; up to 14 of them against 64 bits."""
+    B = len(c["kv_len"])
+    some = np.sort(np.random.default_rng(B).permutation(B)[:14])
+    part = {**c, **{x: c[x][some] for x in ("q", "table", "kv_len", "mask", "nodes")}}
+    ref = reference(part, window, sinks)
     args, n_nodes = device(c)
     out, lse = attend(args, n_nodes, window, sinks)
-    assert_attention(out, lse, c, ref)
+    assert_attention(out[some], lse[some], part, ref)
     return ref
 
 
@@ -132,3 +133,36 @@ def test_one_key_of_nan_in_sight_gives_nan(N, G, D, few, lens, H_kv):
         c["k"][at[0], b % H_kv, at[1], 3] = math.nan
     ref = verdict(c)
     assert ref[0].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("lens,H_kv", SPREADS)
+@pytest.mark.parametrize("N,G,D,few", SHAPES)
+def test_infinite_values_in_sight_give_infinities(N, G, D, few, lens, H_kv, dtype):
+    """V of +infinity, -infinity and NaN, alone and together, in prefix rows and nodes."""
+    c = small(3, N, G, D, few, lens, H_kv, dtype)
+    for b, L in enumerate(c["kv_len"].tolist()):
+        for j, (r, d, x) in enumerate([(0, 1, math.inf), (L // 2, 2, -math.inf), (L - 1, 3, math.inf), (L - 1, 40, math.nan),
+                                       (L + few - 1, 1, -math.inf), (L + few - 1, 4, math.inf), (L, 63, -math.inf),
+                                       (L // 3, 5, math.inf), (2 * L // 3, 5, -math.inf), (2 * L // 3, 6, -math.inf)]):
+            if (b + j) % 3:
+                at = row(c, b, max(r, 0))
+                c["v"][at[0], :, at[1], d] = x
+    ref = verdict(c)
+    assert ref[0].isposinf().any() and ref[0].isneginf().any() and ref[0].isnan().any()
+    if max(lens) > 1000:
+        verdict(c, window=200, sinks=20)
+
+
+@pytest.mark.parametrize("N,G,D,few", SHAPES)
+def test_an_infinite_value_of_tiny_weight(N, G, D, few):
+    """A key whose probability rounds to nothing in the cache's type is seen all the same."""
+    c = small(4, N, G, D, few, [700], 2, FP16)
+    c["q"] = c["q"].abs()
+    for r, x in ((3, -30.0), (500, -30.0), (699, 4.0)):
+        at = row(c, 0, r)
+        c["k"][at[0], :, at[1]] = x / D ** 0.5
+        if x < 0:
+            c["v"][at[0], :, at[1], 7 + r % 2] = math.inf
+    ref = verdict(c)
+    assert ref[0][0, :few, :, 7:9].isposinf().all()

@@ -321,7 +321,7 @@ __device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int dept
     if (a.window > 0 && a.window < a.N) {               // only then can a path be longer than the window
       for (u64 rest_ = t; rest_; rest_ &= rest_ - 1) {
         const int bit = __ffsll((long long)rest_) - 1;
-        const int at = c.L + node_depth(a, b, shift + bit) - 1;
+        const int at = c.L + max(node_depth(a, b, shift + bit), 1) - 1;
         if (!(at < a.sinks || at > pos - a.window)) t &= ~(1ull << bit);
       }
     }

@@ -432,8 +432,8 @@ rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int
  *
  *   For context b, node i, head h (KV head h / (H / H_kv)), L = kv_len[b], n = n_nodes[b]:
  *   keys: prefix rows l < L, and rows L + j of the nodes j < n that bit j of mask row i names.
- *   Node i stands at position L + depth - 1, depth = bits set in its mask row (itself and its
- *   ancestors), or 1 where none is.  window > 0: of these, a key at position p is seen by a node at position x only if
+ *   Node i stands at position L + depth - 1, depth = bits below N set in its mask row (itself and
+ *   its ancestors; bits of nodes that do not exist count too), or 1 where none is.  window > 0: of these, a key at position p is seen by a node at position x only if
  *   p < sinks or p > x - window (prefix row l stands at position l).
  *   out = softmax(scale * q.k) v in fp32, rounded once; a node that sees nothing gets 0 and an lse
  *   of -infinity.  Keys that a node does not see never touch its result, whatever they hold

@@ -287,13 +287,18 @@ __device__ __forceinline__ int node_depth(const Args& a, int b, int i) {
   if (!a.mask) return i + 1;
   const uint32_t* m = a.mask + ((int64_t)b * a.N + i) * a.Wm;
   int d = 0;
-  for (int w = 0; w < a.Wm; ++w) d += __popc(__ldg(m + w));
+  for (int w = 0; w < a.Wm; ++w) {
+    const uint32_t x = __ldg(m + w);
+    d += __popc(32 * w + 32 <= a.N ? x : x & ((1u << (a.N & 31)) - 1u));         // (no bits behind node N - 1)
+  }
   return d;
 }
+// one position behind the last that a node can stand at: a mask row may hold bits of nodes that do not exist
+__device__ __forceinline__ int end_of(const Args& a, const Ctx& c) { return c.L + (a.mask ? a.N : c.n); }
 // every row of the block sees every key of the tile at key0 (tiles of the sinks count as masked)
 template <int BN>
 __device__ __forceinline__ bool all_see(const Args& a, const Ctx& c, int key0) {
-  return key0 + BN <= c.L && (a.window == 0 || key0 > c.L + c.n - 1 - a.window);
+  return key0 + BN <= c.L && (a.window == 0 || key0 > end_of(a, c) - 1 - a.window);
 }
 // which of the keys k0 .. k0 + 63 node i (of depth `depth`) of context b sees; first: words 0 and 1 of its
 // mask row
@@ -710,7 +715,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       float m_used = -INFINITY, l_run = 0.f;
       // tiles [clear0, clear1) of the piece are those that all rows see whole (see all_see)
       const int at0 = p.c.ns - p.c.w0 - p.t0;
-      const int clear0 = a.window == 0 ? 0 : at0 + (max(p.c.L + p.c.n - a.window, 0) + BN - 1) / BN, clear1 = at0 + p.c.L / BN;
+      const int clear0 = a.window == 0 ? 0 : at0 + (max(end_of(a, p.c) - a.window, 0) + BN - 1) / BN, clear1 = at0 + p.c.L / BN;
       int it = turns ? s : 0;
       constexpr int kParts = KP / 16;
       // Two row tiles of the same piece work on the same key tiles, and each scheduler has one warp of either.

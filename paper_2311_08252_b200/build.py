@@ -11,6 +11,7 @@ ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "librest.so")
 SOURCES = sorted(glob.glob(os.path.join(HERE, "csrc", "*.cu")))
 HEADERS = sorted(glob.glob(os.path.join(HERE, "csrc", "*.cuh"))) + \
+    sorted(glob.glob(os.path.join(HERE, "csrc", "*.h"))) + \
     sorted(glob.glob(os.path.join(ROOT, "include", "*.h")))
 
 

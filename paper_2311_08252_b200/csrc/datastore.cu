@@ -10,6 +10,7 @@
 
 #include "common.cuh"
 #include "rest.h"
+#include "smem_limit.h"
 
 namespace rest {
 
@@ -23,17 +24,13 @@ rest_status note_cuda_error(cudaError_t e, const char* where) {
 void count_launch(int n) { g_launches.fetch_add((uint64_t)n, std::memory_order_relaxed); }
 
 cudaError_t ensure_dynamic_smem(const void* kernel, int kernel_slot, size_t bytes) {
-  constexpr int kMaxDev = 64, kSlots = kSmemSlots;
-  static std::atomic<size_t> set_bytes[kMaxDev][kSlots];
+  static SmemLimits<64, kSmemSlots> limits;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  const bool cached = dev >= 0 && dev < kMaxDev && kernel_slot >= 0 && kernel_slot < kSlots;
-  if (cached && set_bytes[dev][kernel_slot].load(std::memory_order_relaxed) >= bytes)
-    return cudaSuccess;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e == cudaSuccess && cached) set_bytes[dev][kernel_slot].store(bytes, std::memory_order_relaxed);
-  return e;
+  return static_cast<cudaError_t>(limits.ensure(dev, kernel_slot, bytes, [&]() -> int {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  }));
 }
 
 int sm_count() {

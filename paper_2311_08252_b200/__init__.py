@@ -576,7 +576,7 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
                          out=None, lse=None, workspace=None, stream=None):
     """Attention of q [B,N,H,D] (bf16 or fp16; D 64 or 128; N = 1: one ordinary token) over a cache
     in pages k_pages, v_pages [P,H_kv,page,D], and over the new rows kv_len[b] + i themselves.
-    mask: words int32 [B,N,ceil(N/32)] as rest_draft writes them, None: node i sees nodes 0..i.
+    mask: int32 or uint32 words [B,N,ceil(N/32)] as rest_draft writes them, None: node i sees nodes 0..i.
     window > 0: a node sees the last `window` positions up to its own and the first `sinks` ones.
     n_nodes int32[B]: later rows do not exist (their out / lse rows stay as they were).
     lse: optional float32 [B,H,N].  workspace: a uint8 tensor of paged_attention_workspace_bytes(),
@@ -595,9 +595,9 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
     table = _table(block_table, index, B)
     mask_ptr = lse_ptr = nodes_ptr = ws_ptr = ws_bytes = 0
     if mask is not None:
-        if mask.element_size() != 4 or mask.get_device() != index or not mask.is_contiguous() or (
-                mask.shape != (B, N, (N + 31) // 32)):
-            raise RestError("mask must be a contiguous 32-bit tensor [B,N,ceil(N/32)] on the same CUDA device")
+        if (mask.dtype is not torch.int32 and mask.dtype is not torch.uint32) or mask.get_device() != index or (
+                not mask.is_contiguous() or mask.shape != (B, N, (N + 31) // 32)):
+            raise RestError("mask must be a contiguous int32 or uint32 tensor [B,N,ceil(N/32)] on the same CUDA device")
         mask_ptr = mask.data_ptr()
     if n_nodes is not None:
         nodes_ptr = _vec(n_nodes, "n_nodes", index, B)

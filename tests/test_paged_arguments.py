@@ -1,0 +1,76 @@
+"""What the Python calls of the paged cache do with their arguments before anything is launched: host tensors
+that say they are on a GPU, and a stand-in for the library."""
+import pytest
+
+import paper_2311_08252_b200 as rest
+
+torch = pytest.importorskip("torch")
+OK = 0
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says that it is on GPU 1."""
+
+    def get_device(self):
+        return 1
+
+
+def gpu(*shape, dtype=torch.int32):
+    return torch.zeros(shape, dtype=dtype).as_subclass(OnGpu)
+
+
+class Library:
+    """Notes every call with the device that was current."""
+
+    def __init__(self, devices):
+        self.calls, self.devices = [], devices
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, self.devices[-1], args))
+            return 64 if name.endswith("_bytes") else OK
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    """GPU 0 is current."""
+    devices = [0]
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            devices.append(self.index)
+
+        def __exit__(self, *_):
+            devices.pop()
+
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: empty(*a, **k).as_subclass(OnGpu))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: devices[-1])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 1000 + index, raising=False)
+    lib = Library(devices)
+    monkeypatch.setattr(rest, "_lib", lib)
+    return lib
+
+
+def attend(mask=None, **kw):
+    q, pages = gpu(2, 3, 4, 64, dtype=torch.bfloat16), gpu(5, 2, 16, 64, dtype=torch.bfloat16)
+    return rest.rest_paged_attention(q, pages, pages, gpu(2, 4), gpu(2), mask, 0.125, **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.uint32])
+def test_masks_are_words(library, dtype):
+    attend(gpu(2, 3, 1, dtype=dtype))
+    name, device, args = library.calls[-1]
+    assert name == "rest_paged_attention" and device == 1 and args[-1] == 1001
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bool, torch.int64, torch.int16])
+def test_masks_of_other_types_are_refused(library, dtype):
+    with pytest.raises(rest.RestError, match="mask"):
+        attend(gpu(2, 3, 1, dtype=dtype))
+    assert not library.calls

@@ -514,6 +514,15 @@ def _call(fn, what, index, stream, *args):
         _check(rc, what)
 
 
+def _scratch_bytes(fn, index, *args):
+    """fn(*args) with GPU `index` as the current device, which the scratch sizes go by."""
+    import torch
+    if index < 0 or torch.cuda.current_device() == index:
+        return fn(*args)
+    with torch.cuda.device(index):
+        return fn(*args)
+
+
 def _as_current(stream, t):
     """`stream` (a torch stream or a handle) as the current one: what a call allocates and clears belongs to it."""
     import torch
@@ -608,11 +617,7 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
     elif out.dtype is not dtype or out.shape != shape or out.stride(3) != 1 or out.get_device() != index:
         raise RestError("out must be a tensor like q with a contiguous last dimension")
     if workspace is None:
-        if torch.cuda.current_device() != index:          # the size goes by the device
-            with torch.cuda.device(index):
-                need = L.rest_paged_attention_workspace_bytes(B, H, H_kv, N, D)
-        else:
-            need = L.rest_paged_attention_workspace_bytes(B, H, H_kv, N, D)
+        need = _scratch_bytes(L.rest_paged_attention_workspace_bytes, index, B, H, H_kv, N, D)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise RestError("workspace must be a contiguous tensor on the same CUDA device")
@@ -649,7 +654,7 @@ def rest_accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature,
                torch.empty((B, max_depth + 1), dtype=i32, device=tokens.device))
     ws_ptr = ws_bytes = 0
     if workspace is None:
-        need = L.rest_accept_sampled_workspace_bytes(B, N)
+        need = _scratch_bytes(L.rest_accept_sampled_workspace_bytes, index, B, N)
         workspace = torch.empty(need, dtype=torch.uint8, device=tokens.device) if need else False
     if workspace is not False:
         if workspace.get_device() != index or not workspace.is_contiguous():

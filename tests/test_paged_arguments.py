@@ -74,3 +74,15 @@ def test_masks_of_other_types_are_refused(library, dtype):
     with pytest.raises(rest.RestError, match="mask"):
         attend(gpu(2, 3, 1, dtype=dtype))
     assert not library.calls
+
+
+def accept(**kw):
+    i, f = (lambda *s: gpu(*s)), (lambda *s: gpu(*s, dtype=torch.float32))
+    return rest.rest_accept_sampled(f(2, 4, 9), i(2, 3), i(2, 3), i(2), f(2, 4), f(2), f(2), 2, **kw)
+
+
+@pytest.mark.parametrize("call", [attend, accept])
+def test_scratch_sizes_are_asked_for_on_the_tensors_device(library, call):
+    """They go by the device's number of SMs; GPU 0 is current, the tensors are on GPU 1."""
+    call()
+    assert [(name.endswith("_bytes"), device) for name, device, _ in library.calls] == [(True, 1), (False, 1)]

@@ -508,10 +508,18 @@ def _call(fn, what, index, stream, *args):
     if stream is None:
         raw = torch._C._cuda_getCurrentRawStream(index)
     else:
+        _same_device(stream, index)
         raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
     rc = fn(*args, raw)
     if rc:
         _check(rc, what)
+
+
+def _same_device(stream, index):
+    """Refuses a torch stream of another GPU than `index` (a handle does not say whose it is)."""
+    own = getattr(stream, "device_index", index)
+    if own != index:
+        raise RestError(f"stream belongs to GPU {own}, the tensors are on GPU {index}")
 
 
 def _scratch_bytes(fn, index, *args):
@@ -526,10 +534,11 @@ def _scratch_bytes(fn, index, *args):
 def _as_current(stream, t):
     """`stream` (a torch stream or a handle) as the current one: what a call allocates and clears belongs to it."""
     import torch
+    if t.get_device() < 0:
+        raise RestError("the tensors must be on a CUDA device")
+    _same_device(stream, t.get_device())
     if isinstance(stream, torch.cuda.Stream):
         return torch.cuda.stream(stream)
-    if not t.is_cuda:
-        raise RestError("the tensors must be on a CUDA device")
     return torch.cuda.stream(torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=t.device))
 
 

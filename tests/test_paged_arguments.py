@@ -1,5 +1,7 @@
 """What the Python calls of the paged cache do with their arguments before anything is launched: host tensors
 that say they are on a GPU, and a stand-in for the library."""
+import types
+
 import pytest
 
 import paper_2311_08252_b200 as rest
@@ -86,3 +88,27 @@ def test_scratch_sizes_are_asked_for_on_the_tensors_device(library, call):
     """They go by the device's number of SMs; GPU 0 is current, the tensors are on GPU 1."""
     call()
     assert [(name.endswith("_bytes"), device) for name, device, _ in library.calls] == [(True, 1), (False, 1)]
+
+
+def every_call():
+    pages, rows, i = gpu(5, 2, 16, 64, dtype=torch.bfloat16), gpu(2, 3, 2, 64, dtype=torch.bfloat16), gpu(2)
+    return {
+        "attention": attend, "accept": accept,
+        "write": lambda **kw: rest.rest_paged_kv_write(pages, pages, gpu(2, 4), i, rows, rows, **kw),
+        "commit": lambda **kw: rest.rest_paged_kv_commit(pages, pages, gpu(2, 4), i, gpu(2, 3), i, 3, **kw),
+        "fork": lambda **kw: rest.rest_pages_fork(gpu(5), gpu(2, 4), i, i, gpu(1), gpu(1), 16, **kw),
+        "copy": lambda **kw: rest.rest_pages_copy(pages, pages, i, i, **kw),
+        "reserve": lambda **kw: rest.rest_pages_reserve(gpu(5), gpu(2, 4), i, i, 16, **kw),
+        "release": lambda **kw: rest.rest_pages_release(gpu(5), gpu(2, 4), i, i, 16, **kw),
+    }
+
+
+@pytest.mark.parametrize("name", ["attention", "accept", "write", "commit", "fork", "copy", "reserve", "release"])
+def test_streams_of_another_device_are_refused(library, name):
+    """Tensors on GPU 1, a stream of GPU 0: the launch would go to GPU 1's own current stream, or fail."""
+    call = every_call()[name]
+    call()
+    n = len(library.calls)
+    with pytest.raises(rest.RestError, match="stream"):
+        call(stream=types.SimpleNamespace(cuda_stream=64, device_index=0))
+    assert len(library.calls) == n

@@ -542,6 +542,13 @@ def _as_current(stream, t):
     return torch.cuda.stream(torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=t.device))
 
 
+def _window(window, sinks):
+    """Refuses what 32 bits would wrap round into another window."""
+    if not (0 <= window <= 0x7FFFFFFF and 0 <= sinks <= 0x7FFFFFFF):
+        raise RestError("window and sinks must lie in [0, 2^31)")
+    return window, sinks
+
+
 def _vec(t, name, index, n=None, dtype=None):
     """Pointer of a contiguous vector (int32 unless told otherwise) of n elements on GPU `index`."""
     import torch
@@ -635,7 +642,7 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
     strides = _I64x9(*qs[:3], *pool[2], *out.stride()[:3])
     _call(L.rest_paged_attention, "rest_paged_attention", index, stream, q.data_ptr(), pool[0], pool[1], strides,
           REST_BF16 if dtype is torch.bfloat16 else REST_FP16, P, page, *table, _vec(kv_len, "kv_len", index, B),
-          nodes_ptr, mask_ptr, B, H, H_kv, N, D, window, sinks, scale, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes)
+          nodes_ptr, mask_ptr, B, H, H_kv, N, D, *_window(window, sinks), scale, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes)
     return out
 
 
@@ -759,7 +766,7 @@ def rest_pages_release(refs, block_table, n_pages, keep_len, page, window=0, sin
     B, index = block_table.shape[0], refs.get_device()
     _call((_lib or lib()).rest_pages_release, "rest_pages_release", index, stream, _vec(refs, "refs", index),
           refs.numel(), *_table(block_table, index), _vec(n_pages, "n_pages", index, B),
-          _vec(keep_len, "keep_len", index, B), B, page, window, sinks)
+          _vec(keep_len, "keep_len", index, B), B, page, *_window(window, sinks))
 
 
 def dependent_read_latency_ns(table_bytes: int = 1 << 30, steps: int = 4096, device=None, seed: int = 1) -> float:

@@ -112,3 +112,15 @@ def test_streams_of_another_device_are_refused(library, name):
     with pytest.raises(rest.RestError, match="stream"):
         call(stream=types.SimpleNamespace(cuda_stream=64, device_index=0))
     assert len(library.calls) == n
+
+
+@pytest.mark.parametrize("name", ["attention", "release"])
+def test_windows_beyond_32_bits_are_refused(library, name):
+    """2^32 + 5 would otherwise become a window of 5."""
+    call = every_call()[name]
+    call(window=(1 << 31) - 1, sinks=(1 << 31) - 1)
+    n = len(library.calls)
+    for kw in (dict(window=(1 << 32) + 5), dict(window=1 << 31), dict(window=7, sinks=1 << 32), dict(window=-1)):
+        with pytest.raises(rest.RestError, match="window"):
+            call(**kw)
+    assert len(library.calls) == n

@@ -617,6 +617,7 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
     if len(shape) != 4 or qs[3] != 1 or dtype is not k_pages.dtype or shape[3] != Dk or q.get_device() != index:
         raise RestError("q must be [B,N,H,D] with a contiguous last dimension, of the pages' type, head size and device")
     B, N, H, D = shape
+    window, sinks = _window(window, sinks)
     table = _table(block_table, index, B)
     mask_ptr = lse_ptr = nodes_ptr = ws_ptr = ws_bytes = 0
     if mask is not None:
@@ -642,7 +643,7 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
     strides = _I64x9(*qs[:3], *pool[2], *out.stride()[:3])
     _call(L.rest_paged_attention, "rest_paged_attention", index, stream, q.data_ptr(), pool[0], pool[1], strides,
           REST_BF16 if dtype is torch.bfloat16 else REST_FP16, P, page, *table, _vec(kv_len, "kv_len", index, B),
-          nodes_ptr, mask_ptr, B, H, H_kv, N, D, *_window(window, sinks), scale, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes)
+          nodes_ptr, mask_ptr, B, H, H_kv, N, D, window, sinks, scale, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes)
     return out
 
 

@@ -248,7 +248,7 @@ rest_pages_fork_plan_kernel(const int32_t* __restrict__ parents, const int32_t* 
     if (ch < 0 || ch >= B || pa < 0 || pa >= B || pa == ch || n_pages[ch] != 0) st = REST_CTX_BAD_PAGES;
     for (int o = 0; o < f; ++o)
       if (s_child[o] == ch) st = REST_CTX_BAD_PAGES;      // the same child twice: the first call's wins
-    if (st == REST_CTX_OK && n_pages[pa] != 0) {          // an empty parent leaves an empty child
+    if (st == REST_CTX_OK) {                              // an empty parent leaves an empty child
       L = kv_len[pa];
       full = L >> page_log;
       part = (L & ((1 << page_log) - 1)) != 0;

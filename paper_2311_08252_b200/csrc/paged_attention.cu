@@ -413,7 +413,11 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if ((sbase & 1023u) != 0) {   // the swizzled operand layout needs a 1024-byte aligned base
-    if (tid == 0) atomicOr(&g_paged_error, 2u);
+    if (tid == 0) {
+      atomicOr(&g_paged_error, 2u);
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);       // nothing to join
+    }
     return;                     // uniform over the grid: every block sees the same offset
   }
   if (tid == 0) {

@@ -57,7 +57,8 @@ enum {
                                    not in lexicographic order                                 */
   REST_CTX_INTERNAL = 3,
   /* written by rest_pages_fork and rest_pages_reserve */
-  REST_CTX_NO_PAGES = 4,        /* the pool has too few free pages: nothing was done            */
+  REST_CTX_NO_PAGES = 4,        /* too few free pages for this context and those before it:
+                                   nothing was done                                           */
   REST_CTX_BAD_PAGES = 5        /* index out of range, child in use or named twice, length that
                                    the table cannot hold: nothing was done                      */
 };
@@ -392,7 +393,10 @@ rest_status rest_kv_commit(void* d_k, void* d_v, const int64_t* kv_strides, cons
  *                   outside [0, P) are left out.  No page may be a target twice, or a target and
  *                   a source.
  * rest_pages_reserve  context b gets pages until its table holds need_len[b] rows, all of them or
- *                   none (d_status[b]).
+ *                   none (d_status[b]).  Pages are counted out in the contexts' order, those of a
+ *                   refused context too: once the pool is too small for one context, it and every
+ *                   later one that needs a page get REST_CTX_NO_PAGES, whatever is free.  Ask again
+ *                   without it (need_len[b] = 0) to serve the others.
  * rest_pages_release  context b keeps the pages of its first keep_len[b] rows; with window > 0 also
  *                   the pages whose rows all lie behind the window of every later token (rows
  *                   >= sinks and <= keep_len - window) go.  Their table entries become -1.
@@ -487,8 +491,10 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
  *                   the call equals rest_accept on the rows' argmax), above 1e30: 1e30; top_p >= 1:
  *                   no cut
  *   outputs         as rest_accept; a row without a finite logit gives -1 for the last token
- *   Weights are held as integers of 2^-44 of the row's largest, of 27 bits (exact sums in any order:
- *   results never depend on scheduling); a token below 2^-44 of the largest counts as impossible.
+ *   Weights are whole numbers of 2^-44 of the row's largest, rounded to 24 bits (each is off by at most
+ *   2^-24 of itself; sums are exact in any order: results never depend on scheduling).  A token below
+ *   2^-45 of the largest counts as impossible.  The nucleus goes by the logits where weights are a
+ *   rounding apart.
  *   d_ws            optional scratch of rest_accept_sampled_workspace_bytes() bytes, 8-byte aligned
  *                   (the query answers for the current device and may be 0), not shared by calls
  *                   that may run at the same time.  Only for speed: with it the rows of few
@@ -565,8 +571,8 @@ rest_status rest_suffix_array_build_in_groups(const int32_t* d_tokens, uint64_t 
  * Device-side trouble that no per-call status can carry.  Every wait inside the kernels is
  * bounded; a kernel that gives up sets a bit here instead of spinning, and its output is then
  * undefined.  Reads and clears the flags of the current device (synchronises the device).
- *   bit 0: tree attention gave up waiting for its tensor-core work
- *   bit 1: tree attention found its shared-memory window misaligned and did nothing
+ *   bit 0: rest_tree_attention or rest_paged_attention gave up waiting for its tensor-core work
+ *   bit 1: one of them found its shared-memory window misaligned and did nothing
  */
 rest_status rest_device_error_flags(uint32_t* h_flags);
 

@@ -605,7 +605,8 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
     window > 0: a node sees the last `window` positions up to its own and the first `sinks` ones.
     n_nodes int32[B]: later rows do not exist (their out / lse rows stay as they were).
     lse: optional float32 [B,H,N].  workspace: a uint8 tensor of paged_attention_workspace_bytes(),
-    not shared by calls that may overlap; None: one is allocated.  Returns out [B,N,H,D]."""
+    not shared by calls that may overlap; None: one is allocated.  out overlaps no input.  Returns
+    out [B,N,H,D]."""
     import torch
     if stream is not None:
         with _as_current(stream, q):
@@ -746,8 +747,9 @@ def rest_pages_copy(k_pages, v_pages, src, dst, stream=None):
 
 
 def rest_pages_reserve(refs, block_table, n_pages, need_len, page, status=None, stream=None):
-    """Gives every context pages until its table holds need_len[b] rows, all or none.  Returns
-    status int32[B] (REST_CTX_*)."""
+    """Gives every context pages until its table holds need_len[b] rows, all or none, in the contexts'
+    order: from the first that the pool is too small for, every one that needs a page is refused.
+    Returns status int32[B] (REST_CTX_*)."""
     import torch
     if stream is not None:
         with _as_current(stream, refs):

@@ -497,7 +497,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       *reinterpret_cast<int*>(ctl + kStartB) = b;
     }
     if (tid == 0) {
-      if (x0 >= x1) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);      // else the MMA warp writes it
+      if (x0 >= x1) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);      // else the V loader writes it
       *reinterpret_cast<long long*>(ctl + kTotal) = total;
     }
   }

@@ -385,7 +385,8 @@ rest_status fill_pool(Pool& c, void* k, void* v, const int64_t* strides, const i
                       int32_t table_cols, int32_t P, int32_t H_kv, int32_t page, int32_t D) {
   if (!k || !v || !strides || P < 1) return REST_INVALID_ARG;
   if (!page_ok(page) || (D != 64 && D != 128) || H_kv > (1 << 20)) return REST_UNSUPPORTED;
-  // a dimension that is stepped through advances by a row at least: no two rows share memory
+  // a dimension that is stepped through advances by a row at least (strides that make rows of different pages,
+  // heads or places share memory all the same are the caller's mistake)
   const int64_t extent[3] = {P, H_kv, page};
   for (int i = 0; i < 3; ++i)
     if (extent[i] > 1 && strides[i] < D) return REST_INVALID_ARG;

@@ -28,3 +28,15 @@ def test_a_length_without_its_pages_is_not_forked():
     n_pages[9], kv_len[9] = 2, 20
     for t, want in zip(dev, (refs, table, n_pages, kv_len)):
         assert np.array_equal(t.cpu().numpy(), want)
+
+
+def test_without_the_context_that_does_not_fit_the_others_are_served():
+    """Pages are counted out in order, a refused context's too; asked again without it, the later ones get theirs."""
+    page, B, W, P = 16, 4, 6, 8
+    dev = [to_dev(np.zeros(P, np.int32)), to_dev(np.full((B, W), -1, np.int32)), to_dev(np.zeros(B, np.int32))]
+    need = np.array([3 * page, 6 * page, page, 0], np.int32)
+    status = rest.rest_pages_reserve(*dev, to_dev(need), page).tolist()
+    assert status == [rest.REST_CTX_OK, rest.REST_CTX_NO_PAGES, rest.REST_CTX_NO_PAGES, rest.REST_CTX_OK]
+    need[1] = 0
+    assert rest.rest_pages_reserve(*dev, to_dev(need), page).tolist() == [rest.REST_CTX_OK] * 4
+    assert dev[2].tolist() == [3, 0, 1, 0] and dev[1][2, 0] == 3 and dev[0].tolist() == [1] * 4 + [0] * 4

@@ -21,7 +21,7 @@
 // every row gets a block of its own and a second small kernel follows the outcomes.  Bound: instructions
 // (about 35 a token for the weights, more time than the row's bytes take), and a walk is a chain of rows.
 // Measured (B200, vocabulary 32000, temperature 0.8, top_p 0.95): one context, 65 rows of bf16, a block each,
-// 29.6 us with the second kernel; 128 contexts, fp32, a block walks each, 115 us (the longest walk decides).
+// 30 us with the second kernel; 128 contexts, fp32, a block walks each, 115 to 130 us (the longest walk decides).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -64,7 +64,7 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 
 struct Shared {
   float2 pow16[16];                             // 2^(44 + j/16) as a float and what it leaves
-  u64 sum[32], left, above, over, seg_before, cut;   // (a warp looks at all 32: those of no warp stay as they began)
+  u64 sum[32], left, above, over, seg_before, cut, cut_mass;   // (a warp looks at all 32: those of no warp stay as they began)
   ulonglong2 list[kList];                       // {order: key, then ~index; weight}
   uint32_t bin_lo[kBins], bin_hi[kBins];        // sums of the low and high 12 bits of the weights' mantissas
   uint32_t red[32], red2[32];
@@ -299,10 +299,12 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
   };
   const int fours = (shift + V + 3) / 4;
 
-  // ---- 3. the nucleus: the tokens from (cut_key, cut_tie) up.  Rounding may give the smaller of two logits
-  // that are next to one another the larger weight, so weights decide only where they are further apart than
-  // that (see slack_of) from cut_w, and logits everywhere else.
-  float cut_w = 0.f, slack = 0.f;
+  // ---- 3. the nucleus: the tokens from (cut_key, cut_tie) up: those of weight above cut_w, and of those at
+  // cut_w the ones that their logits put there.  Rounding may give the smaller of two logits that are next to
+  // one another the larger weight; where it did so to the cut (rare), logits decide for all weights near cut_w
+  // (see slack_of).  (Always deciding so took 8 % more for 128 rows of 32000 fp32 logits.)
+  float cut_w = 0.f;
+  bool turned = false;
   uint32_t cut_key = 0;
   int cut_tie = 0x7FFFFFFF;
   if (cut) {
@@ -367,9 +369,11 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
       before += above;
       if (e < n && part == 0 && before < target && before + mine.y >= target) {
         sh.cut = mine.x;
+        sh.cut_mass = mine.y;
         sh.left = before + mine.y;
       }
       __syncthreads();
+      turned = __syncthreads_or(e < n && (mine.x > sh.cut ? mine.y < sh.cut_mass : mine.x < sh.cut && mine.y > sh.cut_mass));
       cut_key = (uint32_t)(sh.cut >> 32);
       cut_tie = (int)~(uint32_t)sh.cut;
       mass = sh.left;
@@ -421,12 +425,12 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
       __syncthreads();
       cut_tie = sh.cut_tie;
       mass = above + over + ties * one;
+      turned = true;                            // (nobody looked)
     }
     cut_w = weight<T>(sh, r, of_key(cut_key));
-    slack = slack_of(cut_w);
   }
   auto kept = [&](int v, float w) -> bool {
-    if (fabsf(w - cut_w) > slack) return w > cut_w;
+    if (w != cut_w && !(turned && fabsf(w - cut_w) <= slack_of(cut_w))) return w > cut_w;
     if (!cut) return false;                     // (weight 0)
     const uint32_t key = key_of((float)row[v]);
     return key > cut_key || (key == cut_key && v <= cut_tie);
@@ -491,8 +495,8 @@ __device__ int2 row_outcome(const Args& a, Shared& sh, float* s_w, int b, int cu
   each(f0 + lane, f1, 32, [&](int v, const float (&w)[4]) {
     bool tie = false;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) tie = tie || fabsf(w[k] - cut_w) <= slack;
-    if (KEPT && (!tie || !cut)) {                          // nobody needs a closer look
+    for (int k = 0; k < 4; ++k) tie = tie || w[k] == cut_w;
+    if (KEPT && !turned && (!tie || !cut)) {                          // nobody needs a closer look
 #pragma unroll
       for (int k = 0; k < 4; ++k) part.add(w[k] > cut_w ? w[k] : 0.f);
     } else {

@@ -17,7 +17,7 @@
 //   R <= 128  one 128-row tile, two blocks per SM: bound by the K/V stream, so what counts is bytes
 //             in flight (5 tiles of 16 KB a block) and a second block that fills the first one's gaps.
 //   R > 128   two 128-row tiles that share each 64-key K/V tile (read once for 256 rows), one block
-//             per SM: bound by exponentials and the tensor core.
+//             per SM: bound by the chain from S to P (exponentials half of it) and the tensor core.
 // S has two buffers in TMEM for each row tile, so the tensor core runs a key tile ahead of the softmax
 // warps and neither waits for the other's round trip (one 128-key buffer per row tile instead, which
 // spends a fifth less tensor time, needed 5500 cycles per 128 keys and 256 rows).
@@ -34,12 +34,15 @@
 // tensor core (half a step, 2^-9 of each probability in bf16 - the output is rounded as much), the
 // sum takes the unrounded values, so lse carries none of it.
 //
-// Measured (B200, time of captured calls, join included; the copy rate is 6536 GB/s, the bf16 matrix rate 1669
-// TFLOP/s): 1 token x 2048 keys, 32/8 heads, 15.2 us (latency); 64 nodes x 2048 keys, 32 KV heads, 24.4 us;
-// 61 ragged trees x 4096 keys, 32/8 heads, page 16, 242 us (618 TFLOP/s); 16 trees of 128 nodes x 16384 keys,
-// 40/8 heads, 691 us (1000 TFLOP/s); 64 trees of 33 nodes, window 4096, 217 us (5.1 TB/s); 256 tokens, window
-// 2048, D = 64, fp16, 202 us (5.5 TB/s).  In the fourth the exponential unit is busy half the time, the tensor core
-// 47 % (profile of half the keys); in the others the stream of pages and its latency decide.
+// Measured (B200, join included; the copy rate is 6536 GB/s, the bf16 matrix rate 1669 TFLOP/s): calls back to back
+// (the large ones then run into the board's power limit, at 1500 to 1700 of 1965 MHz; captured in a graph they take
+// the same), and in brackets one at a time at the full clock with a cold L2.  64 nodes x 2048 keys, 32 KV
+// heads, 24.4 us (latency); 61 ragged trees x 4096 keys, 32/8 heads, page 16, 277 us (252: 595 TFLOP/s); 16 trees of
+// 128 nodes x 16384 keys, 40/8 heads, 800 us (674: 1030 TFLOP/s); 64 trees of 33 nodes, window 4096, 250 us (226: 4.9
+// TB/s); 256 tokens, window 2048, D = 64, fp16, 240 us (211: 5.3 TB/s).  1 token x 2048 keys, 32/8 heads: 21 us a call, of
+// which the GPU needs 15 (captured).  Of the fourth, with half the keys, a profile shows no pipe full (tensor core
+// 46 %, exponentials 49 %, issue 37 %, DRAM 32 %): two softmax warps a scheduler, each with its chain of S
+// out of TMEM, maximum, exponentials and P back, do not fill each other's waits.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

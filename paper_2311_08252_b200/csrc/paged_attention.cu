@@ -343,53 +343,66 @@ __device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int dept
 // tiles, and a probability that is 0, by rounding or because the key belongs to another copy, makes NaN of
 // them), so such columns of a piece's rows, at `mine` of the output or the scratch, are written once more.
 // For whole warps, a row (`live`) a lane: the lanes read a key each, then every row looks at those that hold
-// something.  Rare, and far from free (about a microsecond a key tile and 16 columns).
+// something.  Rare, and far from free (some microseconds a key tile; other warps' waits have to outlast it).
 template <typename T, int D, int BN>
 __device__ __noinline__ void write_not_finite(const Args& a, Piece p, bool live, int node, int depth, u64 mask0,
                                               long long mine) {
   const int lane = threadIdx.x & 31;
   constexpr uint32_t inf = Type<T>::exponent;
-  for (int d0 = 0; d0 < D; d0 += 16) {
-    uint32_t found = 0;                                 // bit j: +infinity or NaN in column d0 + j; 16 + j: -infinity or NaN
+  constexpr int kGroups = 4;      // 64 columns at a time (all of 128 at once took registers from the caller's loop)
+  for (int d0 = 0; d0 < D; d0 += 64) {
+    uint32_t found[kGroups];      // of columns d0 + 16 c ...: bit j +infinity or NaN in the j-th, 16 + j -infinity or NaN
+#pragma unroll
+    for (int c = 0; c < kGroups; ++c) found[c] = 0;
     for (int it = 0; it < p.len; ++it) {
       const int first = tile_key<BN>(p.c, p.t0 + it);
       u64 vis = 0ull;
       bool asked = false;
-#pragma unroll
       for (int h = 0; h < BN; h += 32) {
         const int key = first + h + lane, col = key >> a.page_log;
         const int page = key < p.c.L + p.c.n && col < a.table_cols ? a.table[p.b * a.table_stride + col] : -1;
-        uint32_t odd = 0;
+        uint32_t odd[kGroups], any = 0;
+#pragma unroll
+        for (int c = 0; c < kGroups; ++c) odd[c] = 0;
         if (page >= 0 && page < a.P) {
           const uint4* v = reinterpret_cast<const uint4*>(static_cast<const T*>(a.v) + page * a.p_p + p.hk * a.p_h +
                                                           (key & ((1 << a.page_log) - 1)) * a.p_r + d0);
-          const uint4 x = v[0], y = v[1];
-          const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const uint32_t e = w[j >> 1] >> (16 * (j & 1)) & 0xFFFFu;
-            if ((e & 0x7FFFu) < inf) continue;
-            if (e != (inf | 0x8000u)) odd |= 1u << j;
-            if (e != inf) odd |= 0x10000u << j;
+          for (int c = 0; c < kGroups; ++c) {
+            const uint4 x = v[2 * c], y = v[2 * c + 1];
+            const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const uint32_t e = w[j >> 1] >> (16 * (j & 1)) & 0xFFFFu;
+              if ((e & 0x7FFFu) >= inf) odd[c] |= (e != (inf | 0x8000u) ? 1u << j : 0u) | (e != inf ? 0x10000u << j : 0u);
+            }
+            any |= odd[c];
           }
         }
-        for (unsigned which = __ballot_sync(0xFFFFFFFFu, odd != 0); which; which &= which - 1) {
+        for (unsigned which = __ballot_sync(0xFFFFFFFFu, any != 0); which; which &= which - 1) {
           const int l = __ffs(which) - 1;
-          const uint32_t there = __shfl_sync(0xFFFFFFFFu, odd, l);
           if (!asked) vis = !live ? 0ull : all_see<BN>(a, p.c, first) ? ~0ull : visible(a, p.c, p.b, node, depth, mask0, first);
           asked = true;
-          if ((vis >> (h + l)) & 1u) found |= there;
+          const bool sees = (vis >> (h + l)) & 1u;
+#pragma unroll
+          for (int c = 0; c < kGroups; ++c) {
+            const uint32_t there = __shfl_sync(0xFFFFFFFFu, odd[c], l);
+            if (sees) found[c] |= there;
+          }
         }
       }
     }
-    for (int j = 0; j < 16; ++j) {
-      const uint32_t plus = found >> j & 1u, minus = found >> (16 + j) & 1u;
-      if (!(plus | minus)) continue;
-      const uint32_t x = plus & minus ? 0x7FFFu : minus ? inf | 0x8000u : inf;
-      if (p.whole)
-        static_cast<uint16_t*>(a.out)[mine + d0 + j] = (uint16_t)x;
-      else
-        a.ws_o[mine + d0 + j] = __uint_as_float(plus & minus ? 0x7FFFFFFFu : minus ? 0xFF800000u : 0x7F800000u);
+#pragma unroll
+    for (int c = 0; c < kGroups; ++c) {
+      for (uint32_t left = (found[c] | found[c] >> 16) & 0xFFFFu; left; left &= left - 1) {
+        const int j = __ffs(left) - 1;
+        const bool plus = found[c] >> j & 1u, minus = found[c] >> (16 + j) & 1u;
+        const long long to = mine + d0 + c * 16 + j;
+        if (p.whole)
+          static_cast<uint16_t*>(a.out)[to] = (uint16_t)(plus && minus ? 0x7FFFu : minus ? inf | 0x8000u : inf);
+        else
+          a.ws_o[to] = __uint_as_float(plus && minus ? 0x7FFFFFFFu : minus ? 0xFF800000u : 0x7F800000u);
+      }
     }
   }
 }

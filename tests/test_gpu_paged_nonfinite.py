@@ -166,3 +166,30 @@ def test_an_infinite_value_of_tiny_weight(N, G, D, few):
             c["v"][at[0], :, at[1], 7 + r % 2] = math.inf
     ref = verdict(c)
     assert ref[0][0, :few, :, 7:9].isposinf().all()
+
+
+@pytest.mark.parametrize("G,dtype", [(2, BF16), (40, FP16), (100, BF16)])
+def test_an_infinity_in_long_contexts(G, dtype):
+    """Whole units of a thousand key tiles: looking for what the infinity comes to takes longer than any
+    other wait, and no one gives up meanwhile (the flags are looked at behind every test)."""
+    B, H_kv, D, page, L = 150, 2, 64, 256, 64000
+    W = L // page + 1
+    gen = torch.Generator("cuda").manual_seed(G)
+    k, v = (torch.randn((B * W, H_kv, page, D), generator=gen, device="cuda", dtype=dtype) for _ in range(2))
+    q = torch.randn((B, 1, G * H_kv, D), generator=gen, device="cuda", dtype=dtype)
+    table = torch.randperm(B * W, generator=torch.Generator().manual_seed(1)).int().view(B, W)
+    args = (q, k, v, table.cuda(), torch.full((B,), L, dtype=torch.int32, device="cuda"), None, 0.05)
+    first, last = table[:, 0].long().cuda(), table[:, (L - 5) // page].long().cuda()
+    for x in (first, last):
+        v[x, :, (L - 5) % page, 9] = 0.0
+    want = rest.rest_paged_attention(*args)
+    assert want.isfinite().all()
+    v[first[::2], :, (L - 5) % page, 9] = math.inf
+    v[last[1::3], :, (L - 5) % page, 9] = -math.inf
+    got = rest.rest_paged_attention(*args)
+    rest_of = torch.arange(D, device="cuda") != 9
+    assert torch.equal(got[..., rest_of], want[..., rest_of])
+    for b in range(B):
+        plus, minus = b % 2 == 0, b % 3 == 1
+        x = got[b, 0, :, 9]
+        assert (x.isnan() if plus and minus else x.isposinf() if plus else x.isneginf() if minus else x == want[b, 0, :, 9]).all(), b

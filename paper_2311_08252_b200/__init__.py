@@ -539,7 +539,9 @@ def _as_current(stream, t):
     _same_device(stream, t.get_device())
     if isinstance(stream, torch.cuda.Stream):
         return torch.cuda.stream(stream)
-    return torch.cuda.stream(torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=t.device))
+    handle = int(getattr(stream, "cuda_stream", stream))
+    handle = 0 if handle == 1 else handle                # cudaStreamLegacy: torch knows the default stream as 0 only
+    return torch.cuda.stream(torch.cuda.ExternalStream(handle, device=t.device))
 
 
 def _window(window, sinks):

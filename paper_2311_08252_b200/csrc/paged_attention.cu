@@ -343,7 +343,8 @@ __device__ __noinline__ u64 visible(const Args& a, Ctx c, int b, int i, int dept
 // tiles, and a probability that is 0, by rounding or because the key belongs to another copy, makes NaN of
 // them), so such columns of a piece's rows, at `mine` of the output or the scratch, are written once more.
 // For whole warps, a row (`live`) a lane: the lanes read a key each, then every row looks at those that hold
-// something.  Rare, and far from free (some microseconds a key tile; other warps' waits have to outlast it).
+// something.  Rare, and far from free: with an infinity in every context the 61 trees x 4096 keys take 1.2 instead of
+// 0.27 ms, the 16 x 16384 keys 6.7 instead of 0.76 (other warps' bounded waits have to outlast one piece's search).
 template <typename T, int D, int BN>
 __device__ __noinline__ void write_not_finite(const Args& a, Piece p, bool live, int node, int depth, u64 mask0,
                                               long long mine) {
@@ -906,8 +907,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           }
           // (a row whose sum is NaN is NaN throughout)
           const bool bad = s_bad[piece & 7] == piece + 1;
-          if (__builtin_expect(__any_sync(0xFFFFFFFFu, live && (bad || odd != 0.f)), 0))
-            write_not_finite<T, D, BN>(a, p, live && l_run == l_run, node, depth, mask0, mine);
+          const bool ask = live && l_run == l_run && (bad || odd != 0.f);
+          if (__builtin_expect(__any_sync(0xFFFFFFFFu, ask), 0))
+            write_not_finite<T, D, BN>(a, p, ask, node, depth, mask0, mine);
         }
         if (live) {
           if (!p.whole)
@@ -973,7 +975,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           }
         }
         // (one of two row tiles in turn may have no tile: then O is what was there before)
-        if (live && odd != 0.f && (!turns || s < p.len)) s_bad[piece & 7] = piece + 1;
+        if (live && odd != 0.f && l_run == l_run && (!turns || s < p.len)) s_bad[piece & 7] = piece + 1;
         if (!sync()) break;
         // the warps that hold copies of the same 32 rows share them out again
 #pragma unroll 2

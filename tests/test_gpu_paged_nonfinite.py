@@ -101,7 +101,7 @@ def small(seed, N, G, D, few, lens, H_kv, dtype=BF16):
     return make(seed, len(lens), N, G * H_kv, H_kv, D, 16, lens, dtype, [few] * len(lens))
 
 
-def verdict(c, window=0, sinks=0):
+def against_64_bits(c, window=0, sinks=0):
     """All contexts in one call; up to 14 of them against 64 bits."""
     B = len(c["kv_len"])
     some = np.sort(np.random.default_rng(B).permutation(B)[:14])
@@ -118,7 +118,7 @@ def verdict(c, window=0, sinks=0):
 def test_a_query_of_nan_gives_nan(N, G, D, few, lens, H_kv):
     c = small(1, N, G, D, few, lens, H_kv)
     c["q"][:, few // 2, ::2] = math.nan
-    ref = verdict(c)
+    ref = against_64_bits(c)
     assert ref[0][:, few // 2, ::2].isnan().all() and ref[0][:, few // 2, 1::2].isfinite().all()
 
 
@@ -131,7 +131,7 @@ def test_one_key_of_nan_in_sight_gives_nan(N, G, D, few, lens, H_kv):
         r = [L + few - 1, 0, L // 2, L - 1, L + few // 2][b % 5]
         at = row(c, b, max(r, 0))
         c["k"][at[0], b % H_kv, at[1], 3] = math.nan
-    ref = verdict(c)
+    ref = against_64_bits(c)
     assert ref[0].isnan().any()
 
 
@@ -148,10 +148,10 @@ def test_infinite_values_in_sight_give_infinities(N, G, D, few, lens, H_kv, dtyp
             if (b + j) % 3:
                 at = row(c, b, max(r, 0))
                 c["v"][at[0], :, at[1], d] = x
-    ref = verdict(c)
+    ref = against_64_bits(c)
     assert ref[0].isposinf().any() and ref[0].isneginf().any() and ref[0].isnan().any()
     if max(lens) > 1000:
-        verdict(c, window=200, sinks=20)
+        against_64_bits(c, window=200, sinks=20)
 
 
 @pytest.mark.parametrize("N,G,D,few", SHAPES)
@@ -164,7 +164,7 @@ def test_an_infinite_value_of_tiny_weight(N, G, D, few):
         c["k"][at[0], :, at[1]] = x / D ** 0.5
         if x < 0:
             c["v"][at[0], :, at[1], 7 + r % 2] = math.inf
-    ref = verdict(c)
+    ref = against_64_bits(c)
     assert ref[0][0, :few, :, 7:9].isposinf().all()
 
 

@@ -1,11 +1,11 @@
 """Rotary positions and the paged KV cache in 8 bits, as measurable cases.
 
     rotary   rest_rotary: queries (or keys) rotated by the positions of a draft's nodes
-    append   rest_paged_kv_append, rest_paged_kv_append_fp8: a step's queries and keys rotated, keys and
+    append   rest_paged_kv_append, rest_paged_kv_append_scaled: a step's queries and keys rotated, keys and
              values written into 16-bit pages, or into e4m3 pages with a scale for 16 rows and head
-    attn     rest_paged_attention_fp8: draft rows (or single tokens) over such a cache, with an
+    attn     rest_paged_attention_scaled: draft rows (or single tokens) over such a cache, with an
              optional sliding window and first tokens that stay visible
-    commit   rest_paged_kv_commit_fp8, rest_pages_copy_fp8: the accepted path moved to the front, and the
+    commit   rest_paged_kv_commit_scaled, rest_pages_copy_scaled: the accepted path moved to the front, and the
              pages copied that a fork of the contexts needs
 
 `own = False` computes them with elementary torch operations, `own = True` through the package."""
@@ -356,20 +356,20 @@ def _own(s):
         turn = dict(positions=s["pos"], inv_freq=s["inv_freq"], interleaved=c["pairs"] == "interleaved",
                     amplitude=s["amplitude"], n_nodes=s["n_nodes"], q=s["q"], q_out=s["q_out"])
         if c["pages"] == "fp8":
-            rest.rest_paged_kv_append_fp8(s["k"], s["v"], s["ks"], s["vs"], s["table"], s["kv_len"], s["k_new"], s["v_new"],
+            rest.rest_paged_kv_append_scaled(s["k"], s["v"], s["ks"], s["vs"], s["table"], s["kv_len"], s["k_new"], s["v_new"],
                                           **turn)
             return {"q": s["q_out"], "k": s["k"], "v": s["v"], "ks": s["ks"], "vs": s["vs"]}
         rest.rest_paged_kv_append(s["k"], s["v"], s["table"], s["kv_len"], s["k_new"], s["v_new"], **turn)
         return {"q": s["q_out"], "k": s["k"], "v": s["v"]}
     if c["op"] == "attn":
-        rest.rest_paged_attention_fp8(s["q"], s["k"], s["v"], s["ks"], s["vs"], s["table"], s["kv_len"], s["mask"],
+        rest.rest_paged_attention_scaled(s["q"], s["k"], s["v"], s["ks"], s["vs"], s["table"], s["kv_len"], s["mask"],
                                       1.0 / math.sqrt(c["D"]), window=c["window"], sinks=c["sinks"], n_nodes=s["n_nodes"],
                                       out=s["out"], lse=s["lse"])
         return {"out": s["out"], "lse": s["lse"]}
-    rest.rest_paged_kv_commit_fp8(s["k"], s["v"], s["ks"], s["vs"], s["table"], s["kv_len"], s["accept_nodes"],
+    rest.rest_paged_kv_commit_scaled(s["k"], s["v"], s["ks"], s["vs"], s["table"], s["kv_len"], s["accept_nodes"],
                                   s["accept_len"], c["N"], new_kv_len=s["new_kv_len"])
     if c["fork"]:
-        rest.rest_pages_copy_fp8(s["k"], s["v"], s["ks"], s["vs"], s["src"], s["dst"])
+        rest.rest_pages_copy_scaled(s["k"], s["v"], s["ks"], s["vs"], s["src"], s["dst"])
     return {"k": s["k"], "v": s["v"], "ks": s["ks"], "vs": s["vs"], "kv_len": s["new_kv_len"]}
 
 

@@ -9,10 +9,15 @@
  *               datastore spread over several GPUs
  * Verify side:  rest_tree_attention, rest_accept           (Sec. 3.2, draft verification / acceptance)
  *               rest_paged_attention: the same attention over a cache cut into pages
+ *               rest_paged_attention_scaled: over pages of 8-bit codes with scales
  *               rest_accept_sampled: acceptance against the verifier's probabilities
+ *               rest_rotary: queries or keys rotated by the position ids of a draft
  * Between steps: rest_kv_commit                            (the accepted path joins the prefix)
  *               rest_paged_kv_write, rest_paged_kv_commit, rest_pages_fork, rest_pages_copy,
  *               rest_pages_reserve, rest_pages_release: the cache in pages
+ *               rest_paged_kv_append: a step's rows rotated and written in one call
+ *               rest_paged_kv_append_scaled, rest_paged_kv_commit_scaled, rest_pages_copy_scaled:
+ *               the same cache in 8-bit codes with scales
  * Health:       rest_device_error_flags
  * (measurement and planning aids live in rest_aids.h)
  *
@@ -427,6 +432,82 @@ rest_status rest_pages_reserve(int32_t* d_refs, int32_t P, int32_t* d_table, int
 rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int64_t table_stride,
                                int32_t table_cols, int32_t* d_n_pages, const int32_t* d_keep_len,
                                int32_t B, int32_t page, int32_t window, int32_t sinks, void* stream);
+
+/*
+ * rest_rotary - rotary positions: each pair of elements of a row turns by an angle that grows with the
+ * row's position (the paper takes the verifier as given; the positions are rest_draft's pos_ids).
+ *
+ *   For context b, node i, head h and pair f < pairs, with p = d_pos[b,i] and t = p * d_inv_freq[f]:
+ *   (y1, y2) = amplitude * (x1 cos t - x2 sin t, x2 cos t + x1 sin t).  interleaved = 0: the pair is
+ *   elements f and pairs + f; 1: elements 2f and 2f + 1.  Elements from 2 * pairs on are copied.
+ *   t and its sine and cosine are computed in 64 bits, results in 32, rounded once.
+ *   With -d_inv_freq it is the inverse rotation (and, amplitude kept, the gradient of x).
+ *
+ *   d_x, d_out      element (b,i,h,d) at b*strides[0] + i*strides[1] + h*strides[2] + d, dtype REST_BF16,
+ *                   REST_FP16 or REST_FP32; strides host values, multiples of 16 bytes; base pointers
+ *                   16-byte aligned.  d_out is d_x with the same strides (in place), or overlaps no input
+ *   d_pos           int32[B,N], any sign; d_inv_freq float[pairs] (both may be NULL with pairs = 0: a copy)
+ *   d_n_nodes       optional int32[B]: rows i >= n_nodes[b] of d_out stay as they were
+ *   Limits: D a multiple of 16, at most 512; 2 * pairs <= D; amplitude finite.
+ */
+rest_status rest_rotary(const void* d_x, const int64_t* x_strides, int32_t dtype, const int32_t* d_pos,
+                        const float* d_inv_freq, int32_t pairs, int32_t interleaved, float amplitude,
+                        const int32_t* d_n_nodes, int32_t B, int32_t H, int32_t N, int32_t D, void* d_out,
+                        const int64_t* out_strides, void* stream);
+
+/*
+ * rest_paged_kv_append - rest_paged_kv_write with the rotation of rest_rotary on the way: rows i < n_nodes[b]
+ * of d_k_new, rotated, and of d_v_new, as they are, become rows kv_len[b] + i; with H > 0 the queries d_q
+ * are rotated into d_q_out (all three in one launch).  pairs = 0: nothing is rotated.
+ *   d_k_pages ... d_n_nodes  as in rest_paged_kv_write (16-bit pages of `dtype`, REST_BF16 or REST_FP16, which
+ *                   d_k_new, d_v_new, d_q and d_q_out share)
+ *   d_pos ... amplitude      as in rest_rotary
+ *   d_q, d_q_out    element (b,i,h,d) as in rest_rotary, h < H (H = 0: none, both NULL)
+ *   A row whose page does not exist is left out; its query is rotated all the same.
+ */
+rest_status rest_paged_kv_append(void* d_k_pages, void* d_v_pages, const int64_t* page_strides, int32_t P,
+                                 int32_t page, const int32_t* d_table, int64_t table_stride, int32_t table_cols,
+                                 const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new,
+                                 const int64_t* new_strides, const int32_t* d_n_nodes, int32_t dtype,
+                                 const int32_t* d_pos, const float* d_inv_freq, int32_t pairs, int32_t interleaved,
+                                 float amplitude, const void* d_q, const int64_t* q_strides, void* d_q_out,
+                                 const int64_t* out_strides, int32_t H, int32_t B, int32_t H_kv, int32_t N,
+                                 int32_t D, void* stream);
+
+/*
+ * The cache in 8 bits: pages of e4m3 codes (1 byte an element; strides in elements, multiples of 16), and for
+ * each page, head and block of 16 rows a scale, float[P][H_kv][page / 16], for K and for V.  Row r of a
+ * page stands for scale[r / 16] * code.  Scales are positive; outside [2^-60, 2^60] they count as the nearer
+ * limit (NaN as 2^-60).  Tables, counts, forks and lengths are those of 16-bit pages.
+ *
+ * rest_paged_kv_append_scaled  as rest_paged_kv_append, K (rotated in 64 bits) and V rounded to codes.  A block
+ *                   that gets new rows gets the smallest power of two s for which no finite new value exceeds
+ *                   448 s; where it has older rows (below kv_len) s is not less than its scale was, and
+ *                   if it grows, those rows' codes are rounded to the new scale (exact down to 2^-9 s).
+ *                   Rows behind the new ones lose what they held.  Values that are not finite become NaN;
+ *                   beyond 448 * 2^60 they saturate.
+ * rest_paged_kv_commit_scaled  as rest_paged_kv_commit: the accepted rows are put to the front as if the
+ *                   values that they stand for had been appended there, by the same rule.
+ * rest_pages_copy_scaled  as rest_pages_copy, with the pages' scales.
+ */
+rest_status rest_paged_kv_append_scaled(void* d_k_pages, void* d_v_pages, const int64_t* page_strides,
+                                        float* d_k_scales, float* d_v_scales, int32_t P, int32_t page,
+                                        const int32_t* d_table, int64_t table_stride, int32_t table_cols,
+                                        const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new,
+                                        const int64_t* new_strides, const int32_t* d_n_nodes, int32_t dtype,
+                                        const int32_t* d_pos, const float* d_inv_freq, int32_t pairs,
+                                        int32_t interleaved, float amplitude, const void* d_q,
+                                        const int64_t* q_strides, void* d_q_out, const int64_t* out_strides,
+                                        int32_t H, int32_t B, int32_t H_kv, int32_t N, int32_t D, void* stream);
+rest_status rest_paged_kv_commit_scaled(void* d_k_pages, void* d_v_pages, const int64_t* page_strides,
+                                        float* d_k_scales, float* d_v_scales, int32_t P, int32_t page,
+                                        const int32_t* d_table, int64_t table_stride, int32_t table_cols,
+                                        const int32_t* d_kv_len, const int32_t* d_accept_nodes,
+                                        const int32_t* d_accept_len, int32_t B, int32_t H_kv, int32_t N, int32_t D,
+                                        int32_t max_depth, int32_t* d_new_kv_len, void* stream);
+rest_status rest_pages_copy_scaled(void* d_k_pages, void* d_v_pages, const int64_t* page_strides, float* d_k_scales,
+                                   float* d_v_scales, int32_t P, int32_t page, int32_t H_kv, int32_t D,
+                                   const int32_t* d_src, const int32_t* d_dst, int32_t n, void* stream);
 
 /*
  * rest_paged_attention - attention of N new positions of each context over its KV cache in pages

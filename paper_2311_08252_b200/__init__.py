@@ -15,6 +15,10 @@ Serving, with a KV cache in pages:
     rest_accept_sampled                 Sec. 4.1, acceptance against the target's probabilities
     rest_paged_kv_write / _commit       a step's new rows; the accepted ones moved to the front
     rest_pages_fork / _copy / _reserve / _release   contexts that share, get and give back pages
+    rest_rotary, rotary_frequencies     queries or keys rotated by position
+    rest_paged_kv_append                a step's rows rotated and written into the pages, one launch
+    rest_paged_attention_scaled, rest_paged_kv_append_scaled / _commit_scaled, rest_pages_copy_scaled
+                                        the same cache in 8-bit codes with scales
 """
 from __future__ import annotations
 
@@ -53,7 +57,8 @@ EXPORTS = (
     "rest_paged_attention_workspace_bytes", "rest_paged_attention", "rest_accept_sampled_workspace_bytes",
     "rest_accept_sampled",
     "rest_paged_kv_write", "rest_paged_kv_commit", "rest_pages_fork", "rest_pages_copy",
-    "rest_pages_reserve", "rest_pages_release",
+    "rest_pages_reserve", "rest_pages_release", "rest_rotary", "rest_paged_kv_append", "rest_paged_kv_append_scaled",
+    "rest_paged_kv_commit_scaled", "rest_pages_copy_scaled",
     "rest_accept", "rest_status_string", "rest_last_cuda_error", "rest_launch_count",
 )
 
@@ -138,6 +143,21 @@ def lib():
     L.rest_paged_kv_commit.argtypes = pool + table + [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
     L.rest_pages_copy.restype = i32
     L.rest_pages_copy.argtypes = pool + [i32, i32, vp, vp, i32, vp]
+    strides = ctypes.POINTER(i64)
+    turn = [vp, vp, i32, i32, ctypes.c_float]                # positions, frequencies, pairs, interleaved, amplitude
+    queries = [vp, strides, vp, strides, i32]                # q, its strides, where it goes, strides, heads
+    scaled = [vp, vp, strides, vp, vp, i32, i32]             # K, V, strides, their scales, pages, rows per page
+    L.rest_rotary.restype = i32
+    L.rest_rotary.argtypes = [vp, strides, i32] + turn + [vp, i32, i32, i32, i32, vp, strides, vp]
+    L.rest_paged_kv_append.restype = i32
+    L.rest_paged_kv_append.argtypes = pool + table + [vp, vp, vp, strides, vp, i32] + turn + queries + [i32] * 4 + [vp]
+    L.rest_paged_kv_append_scaled.restype = i32
+    L.rest_paged_kv_append_scaled.argtypes = scaled + table + [vp, vp, vp, strides, vp, i32] + turn + queries + \
+        [i32] * 4 + [vp]
+    L.rest_paged_kv_commit_scaled.restype = i32
+    L.rest_paged_kv_commit_scaled.argtypes = scaled + table + [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
+    L.rest_pages_copy_scaled.restype = i32
+    L.rest_pages_copy_scaled.argtypes = scaled + [i32, i32, vp, vp, i32, vp]
     L.rest_pages_fork.restype = i32
     L.rest_pages_fork.argtypes = [vp, i32] + table + [vp, vp, i32, i32, vp, vp, i32, vp, vp, vp, vp]
     L.rest_pages_reserve.restype = i32
@@ -772,6 +792,174 @@ def rest_pages_release(refs, block_table, n_pages, keep_len, page, window=0, sin
     _call((_lib or lib()).rest_pages_release, "rest_pages_release", index, stream, _vec(refs, "refs", index),
           refs.numel(), *_table(block_table, index), _vec(n_pages, "n_pages", index, B),
           _vec(keep_len, "keep_len", index, B), B, page, *_window(window, sinks))
+
+
+def rotary_frequencies(dim, base=10000.0, scaling=None, factor=1.0, original_len=None, slow=1.0, fast=32.0):
+    """(inv_freq, amplitude) for rest_rotary: float32 [dim/2] on the CPU, base^(-2f/dim) for pair f, and what the
+    rotated elements are multiplied by.  For contexts `factor` times longer than the model was trained on:
+    scaling="linear" divides all positions by factor; "base" raises the base to base * factor^(dim/(dim-2)), so
+    that the slowest pair turns factor times slower and the fastest as before; "parts" slows down pairs by their turns
+    within original_len: fewer than `slow`, factor times, more than `fast`, not at all, mixed between, with amplitude
+    0.1 ln(factor) + 1."""
+    import math
+    import torch
+    if dim < 2 or dim % 2 or not base > 0 or not factor >= 1 or scaling not in (None, "linear", "base", "parts"):
+        raise RestError("rotary_frequencies: dim even, base > 0, factor >= 1, scaling None, 'linear', 'base' or 'parts'")
+    if scaling == "parts" and not (original_len and original_len > 0 and fast > slow):
+        raise RestError("rotary_frequencies: 'parts' needs original_len > 0 and fast > slow")
+    if scaling == "base" and dim > 2:
+        base = base * factor ** (dim / (dim - 2))
+    f = torch.tensor(float(base), dtype=torch.float64) ** (-torch.arange(0, dim, 2, dtype=torch.float64) / dim)
+    amplitude = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "parts":
+        keep = ((original_len * f / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+        f = f * (keep + (1 - keep) / factor)
+        amplitude = 0.1 * math.log(factor) + 1.0
+    return f.float(), amplitude
+
+
+def _turn(positions, inv_freq, index, B, N, D):
+    """Pointers of positions and frequencies, and how many pairs turn (None, None: none)."""
+    import torch
+    if inv_freq is None and positions is None:
+        return 0, 0, 0
+    if inv_freq is None or positions is None:
+        raise RestError("positions and inv_freq go together")
+    pairs = inv_freq.numel()
+    if 2 * pairs > D:
+        raise RestError("inv_freq holds one frequency for each pair of elements: at most D / 2")
+    return _array(positions, "positions", index, (B, N), torch.int32), _vec(inv_freq, "inv_freq", index, pairs, torch.float32), pairs
+
+
+def rest_rotary(x, positions, inv_freq, interleaved=False, amplitude=1.0, n_nodes=None, out=None, stream=None):
+    """Rotary positions of x [B,N,H,D] (bf16, fp16 or fp32; D a multiple of 16 up to 512; queries, or keys with
+    their heads): element pairs f and F + f (interleaved: 2f and 2f + 1) of the first 2F = 2 len(inv_freq)
+    elements turn by positions[b,i] * inv_freq[f] (int32 [B,N], as rest_draft's pos_ids; float32 [F], as
+    rotary_frequencies gives them, on the GPU) and are multiplied by amplitude; the others are copied.
+    n_nodes int32[B]: later rows of out stay as they were.  out: like x, x itself (in place), or None.  Returns out."""
+    import torch
+    if stream is not None:
+        with _as_current(stream, x):
+            return rest_rotary(x, positions, inv_freq, interleaved, amplitude, n_nodes, out)
+    dtype, shape, xs, index = x.dtype, x.shape, x.stride(), x.get_device()
+    kind = {torch.bfloat16: REST_BF16, torch.float16: REST_FP16, torch.float32: REST_FP32}.get(dtype)
+    if kind is None or len(shape) != 4 or xs[3] != 1:
+        raise RestError("x must be a bf16, fp16 or fp32 tensor [B,N,H,D] with a contiguous last dimension")
+    B, N, H, D = shape
+    if out is None:
+        out = (torch.empty if n_nodes is None else torch.zeros)(shape, dtype=dtype, device=x.device)
+    elif out.dtype is not dtype or out.shape != shape or out.stride(3) != 1 or out.get_device() != index:
+        raise RestError("out must be a tensor like x with a contiguous last dimension")
+    _call((_lib or lib()).rest_rotary, "rest_rotary", index, stream, x.data_ptr(), _I64x3(*xs[:3]), kind,
+          *_turn(positions, inv_freq, index, B, N, D), int(bool(interleaved)), amplitude,
+          0 if n_nodes is None else _vec(n_nodes, "n_nodes", index, B), B, H, N, D, out.data_ptr(),
+          _I64x3(*out.stride()[:3]))
+    return out
+
+
+def _append(name, index, dims, pool, block_table, kv_len, k_new, v_new, positions, inv_freq, interleaved, amplitude,
+            n_nodes, q, q_out, dtype):
+    import torch
+    H_kv, D = dims
+    shape, ns = k_new.shape, k_new.stride()
+    kind = {torch.bfloat16: REST_BF16, torch.float16: REST_FP16}.get(k_new.dtype)
+    if kind is None or len(shape) != 4 or shape[2] != H_kv or shape[3] != D or ns[3] != 1 or (
+            k_new.get_device() != index) or (dtype is not None and k_new.dtype is not dtype):
+        raise RestError("k_new must be [B,N,H_kv,D] of the pages' heads and device, bf16 or fp16 as 16-bit pages are, with a "
+                        "contiguous last dimension")
+    if v_new.shape != shape or v_new.stride() != ns or v_new.dtype is not k_new.dtype or v_new.get_device() != index:
+        raise RestError("k_new and v_new must have the same shape, strides, type and device")
+    B, N, H = shape[0], shape[1], 0
+    queries = (0, None, 0, None)
+    if q is not None:
+        qs = q.stride()
+        if q.dtype is not k_new.dtype or len(q.shape) != 4 or q.shape[:2] != shape[:2] or q.shape[3] != D or (
+                qs[3] != 1 or q.get_device() != index):
+            raise RestError("q must be [B,N,H,D] of k_new's type, head size and device, with a contiguous last dimension")
+        if q_out is None:
+            q_out = (torch.empty if n_nodes is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+        elif q_out.dtype is not q.dtype or q_out.shape != q.shape or q_out.stride(3) != 1 or q_out.get_device() != index:
+            raise RestError("q_out must be a tensor like q with a contiguous last dimension")
+        H = q.shape[2]
+        queries = (q.data_ptr(), _I64x3(*qs[:3]), q_out.data_ptr(), _I64x3(*q_out.stride()[:3]))
+    elif q_out is not None:
+        raise RestError("q_out without q")
+    _call(getattr(_lib or lib(), name), name, index, None, *pool, *_table(block_table, index, B),
+          _vec(kv_len, "kv_len", index, B), k_new.data_ptr(), v_new.data_ptr(), _I64x3(*ns[:3]),
+          0 if n_nodes is None else _vec(n_nodes, "n_nodes", index, B), kind,
+          *_turn(positions, inv_freq, index, B, N, D), int(bool(interleaved)), amplitude, *queries, H, B, H_kv, N, D)
+    return q_out
+
+
+def rest_paged_kv_append(k_pages, v_pages, block_table, kv_len, k_new, v_new, positions=None, inv_freq=None,
+                         interleaved=False, amplitude=1.0, n_nodes=None, q=None, q_out=None, stream=None):
+    """A step's rows in one launch: k_new [B,N,H_kv,D] rotated as by rest_rotary and v_new as it is become rows
+    kv_len[b] + i of the contexts' pages; q [B,N,H,D] is rotated into q_out (may be q itself; None: one is
+    allocated).  positions and inv_freq None: nothing is rotated.  n_nodes int32[B]: only rows i < n_nodes[b].
+    Rows whose page does not exist are left out.  Returns q_out (None without q)."""
+    if stream is not None:
+        with _as_current(stream, k_new):
+            return rest_paged_kv_append(k_pages, v_pages, block_table, kv_len, k_new, v_new, positions, inv_freq,
+                                        interleaved, amplitude, n_nodes, q, q_out)
+    index, (P, H_kv, page, D), pool = _pool(k_pages, v_pages)
+    return _append("rest_paged_kv_append", index, (H_kv, D), pool, block_table, kv_len, k_new, v_new, positions, inv_freq,
+                   interleaved, amplitude, n_nodes, q, q_out, k_pages.dtype)
+
+
+def _scaled_pool(k_pages, v_pages, k_scales, v_scales):
+    """Device, shape, and (pointers, strides, pointers of the scales, pages, rows per page) of a pool of codes."""
+    import torch
+    index, shape, strides = k_pages.get_device(), k_pages.shape, k_pages.stride()
+    if len(shape) != 4 or strides[3] != 1 or k_pages.dtype is not torch.float8_e4m3fn:
+        raise RestError("k_pages must be a float8_e4m3fn tensor [P, H_kv, page, D] with a contiguous last dimension")
+    if v_pages.stride() != strides or v_pages.shape != shape or v_pages.dtype is not k_pages.dtype or (
+            v_pages.get_device() != index):
+        raise RestError("k_pages and v_pages must have the same shape, strides, type and device")
+    want = (shape[0], shape[1], shape[2] // 16)
+    return index, shape, (k_pages.data_ptr(), v_pages.data_ptr(), _I64x3(*strides[:3]),
+                          _array(k_scales, "k_scales", index, want, torch.float32),
+                          _array(v_scales, "v_scales", index, want, torch.float32), shape[0], shape[2])
+
+
+def rest_paged_kv_append_scaled(k_pages, v_pages, k_scales, v_scales, block_table, kv_len, k_new, v_new, positions=None,
+                                inv_freq=None, interleaved=False, amplitude=1.0, n_nodes=None, q=None, q_out=None,
+                                stream=None):
+    """rest_paged_kv_append into pages of 8-bit codes: k_pages, v_pages float8_e4m3fn [P,H_kv,page,D], with a
+    scale for every 16 rows and head, k_scales, v_scales float32 [P,H_kv,page/16] (contiguous).  A block of 16
+    rows takes the smallest power of two that holds its new values (448 is the largest code), and no less than
+    before where it has older rows, which are requantised if it grows."""
+    if stream is not None:
+        with _as_current(stream, k_new):
+            return rest_paged_kv_append_scaled(k_pages, v_pages, k_scales, v_scales, block_table, kv_len, k_new, v_new,
+                                               positions, inv_freq, interleaved, amplitude, n_nodes, q, q_out)
+    index, (P, H_kv, page, D), pool = _scaled_pool(k_pages, v_pages, k_scales, v_scales)
+    return _append("rest_paged_kv_append_scaled", index, (H_kv, D), pool, block_table, kv_len, k_new, v_new, positions,
+                   inv_freq, interleaved, amplitude, n_nodes, q, q_out, None)
+
+
+def rest_paged_kv_commit_scaled(k_pages, v_pages, k_scales, v_scales, block_table, kv_len, accept_nodes, accept_len, N,
+                                new_kv_len=None, stream=None):
+    """rest_paged_kv_commit over pages of codes: the accepted rows are put to the front as if the values that they
+    stand for had been appended there."""
+    import torch
+    index, (P, H_kv, page, D), pool = _scaled_pool(k_pages, v_pages, k_scales, v_scales)
+    B, max_depth = accept_nodes.shape
+    _call((_lib or lib()).rest_paged_kv_commit_scaled, "rest_paged_kv_commit_scaled", index, stream, *pool,
+          *_table(block_table, index, B), _vec(kv_len, "kv_len", index, B),
+          _array(accept_nodes, "accept_nodes", index, (B, max_depth), torch.int32),
+          _vec(accept_len, "accept_len", index, B), B, H_kv, N, D, max_depth,
+          0 if new_kv_len is None else _vec(new_kv_len, "new_kv_len", index, B))
+    return new_kv_len
+
+
+def rest_pages_copy_scaled(k_pages, v_pages, k_scales, v_scales, src, dst, stream=None):
+    """Page dst[i] of K and V becomes a copy of page src[i], scales included (entries outside the pool: left out)."""
+    index, shape, pool = _scaled_pool(k_pages, v_pages, k_scales, v_scales)
+    n = src.numel()
+    _call((_lib or lib()).rest_pages_copy_scaled, "rest_pages_copy_scaled", index, stream, *pool, shape[1], shape[3],
+          _vec(src, "src", index), _vec(dst, "dst", index, n), n)
 
 
 def dependent_read_latency_ns(table_bytes: int = 1 << 30, steps: int = 4096, device=None, seed: int = 1) -> float:

@@ -1,0 +1,456 @@
+// Rotary positions (rest_rotary), and the rows of a step rotated and written into a cache in pages in one
+// launch: 16-bit pages (rest_paged_kv_append) or e4m3 pages with scales (rest_paged_kv_append_scaled).
+// Not in the paper, which takes the verifier as given; the position ids are rest_draft's.
+//
+// Pair f of a row at position p turns by the angle t = p * inv_freq[f]:
+//   y1 = a (x1 cos t - x2 sin t), y2 = a (x2 cos t + x1 sin t).
+// t is a product in 64 bits (exact up to p = 2^29) and its sine and cosine are taken in 64 bits: in 32 bits
+// the angle of position 10^6 would be 0.03 off.  Queries and 16-bit keys are then rotated in 32 bits and
+// rounded once.  Keys that become codes are rotated in 64 bits: the border between two codes decides a whole step
+// of 2^-4, so that a result a rounding off would now and then be a code off.
+//
+// Pages with scales: the 16 rows of a block share a scale per head, the smallest power of two that holds the largest new
+// value, and never less than before where the block has older rows; those are requantised when it grows
+// (by a power of two, so they change only where they fall below the smallest code).
+//
+// A thread block takes the new rows of one context that fall into one block of 16 rows: their angles are
+// computed once, into shared memory, for all heads.  A row is D / 16 lanes, 16 elements each (a pair's halves sit in
+// the same lane), so that 64 bytes a thread are in flight; a lane keeps its row's sines and cosines in
+// registers over the heads.  A block of codes is a warp, which holds all its rows' values while it looks for the
+// largest.  What bounds it is HBM for many rows, and for few rows the launch and the chain length -> table -> page.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "common.cuh"
+#include "e4m3.cuh"
+#include "paged_pool.cuh"
+#include "rest.h"
+
+namespace {
+
+using namespace rest_pool;
+using namespace rest_e4m3;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+enum Where { kNowhere, kPages16, kPagesScaled };        // where keys and values go
+
+struct Args {
+  Pool c;                                               // strides in vectors of 16 bytes
+  float *k_scales, *v_scales;
+  const void *q, *k_new, *v_new;
+  void* q_out;
+  int64_t q_b, q_n, q_h, o_b, o_n, o_h, n_b, n_n, n_h;  // in elements
+  const int32_t *kv_len, *n_nodes, *pos;
+  const float* inv_freq;
+  int N, H, H_kv, D, half, groups, interleaved;
+  float amplitude;
+};
+
+// eight elements as they lie in memory
+template <typename T> struct Eight {
+  uint4 v[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = v[i];
+  }
+  __device__ __forceinline__ void to(float* x) const {
+    const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[sizeof(T) / 2 - 1].x, v[sizeof(T) / 2 - 1].y,
+                           v[sizeof(T) / 2 - 1].z, v[sizeof(T) / 2 - 1].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        x[2 * i] = __uint_as_float(w[2 * i]);
+        x[2 * i + 1] = __uint_as_float(w[2 * i + 1]);
+      } else {
+        float2 f;
+        if constexpr (__is_same(T, __half)) f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        else f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+      }
+    }
+  }
+};
+template <typename T> __device__ __forceinline__ void load8(const T* p, float* x) {
+  Eight<T> e;
+  e.load(p);
+  e.to(x);
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float* x) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (__is_same(T, __half)) {
+        const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+template <typename T> __device__ __forceinline__ float load1(const T* p) { return (float)*p; }
+
+// A lane's 16 elements of a row, in two runs of 8 from at[0] and at[1].  PAIRS: a pair's halves lie in the same place
+// of both runs (half the head apart); NEIGHBOURS: pairs are neighbours, or the run is not rotated at all; LOOSE: pairs
+// half the head apart that runs of 8 do not meet (partners are loaded one by one).
+enum Kind { kPairs, kNeighbours, kLoose };
+struct Lane { Kind kind; int at[2], first; };           // first: of kPairs and kNeighbours, the first pair's number
+__device__ __forceinline__ Lane lane_of(const Args& a, int chunk) {
+  if (a.interleaved || a.half == 0) return {kNeighbours, {16 * chunk, 16 * chunk + 8}, 8 * chunk};
+  if (a.half & 7) return {kLoose, {16 * chunk, 16 * chunk + 8}, 0};
+  const int pairs = a.half >> 3;
+  if (chunk < pairs) return {kPairs, {8 * chunk, a.half + 8 * chunk}, 8 * chunk};
+  const int at = 16 * chunk;                            // behind the rotated part
+  return {kNeighbours, {at, at + 8}, a.half};
+}
+// Where pair f of row r has its cosine and sine.  Lanes next to one another read pairs 8 apart, so of each eight the
+// twos are laid out apart: 16-byte reads without bank conflicts.
+__device__ __forceinline__ int table_at(const Args& a, int r, int f) {
+  const int eighths = a.half >> 3;
+  return r * a.half + ((a.half & 7) ? f : ((((f >> 1) & 3) * eighths + (f >> 3)) << 1 | (f & 1)));
+}
+
+// cosines and sines of a lane's eight pairs (behind the last pair, not used)
+template <typename F2, typename F> struct Angles {
+  F c[8], s[8];
+  __device__ __forceinline__ void load(const Args& a, const Lane& l, const F2* table, int r) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      c[j] = 1;
+      s[j] = 0;
+      if (l.first + j < a.half) {
+        const F2 cs = table[table_at(a, r, l.first + j)];
+        c[j] = cs.x;
+        s[j] = cs.y;
+      }
+    }
+  }
+};
+// The rotated elements y of a lane from x, of which the first `pairs` pairs turn; `round` makes what is stored of each.
+template <typename A, typename F, typename R>
+__device__ __forceinline__ void rotate(Kind kind, int pairs, const A& t, const float (&x)[16], float (&y)[16], R round) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const F c = t.c[j], s = t.s[j];
+    const F x1 = kind == kPairs ? x[j] : x[2 * j], x2 = kind == kPairs ? x[8 + j] : x[2 * j + 1];
+    const bool turns = j < pairs;                       // (1 and 0 would make NaN of what stands next to an infinity)
+    const float y1 = round(turns ? fma(x1, c, -(x2 * s)) : x1), y2 = round(turns ? fma(x2, c, x1 * s) : x2);
+    if (kind == kPairs) { y[j] = y1; y[8 + j] = y2; } else { y[2 * j] = y1; y[2 * j + 1] = y2; }
+  }
+}
+// one element of a row whose pairs are loose
+template <typename F, typename F2, typename T>
+__device__ __forceinline__ F loose(const Args& a, const T* row, int e, float x, const F2* table, int r) {
+  if (e >= 2 * a.half) return x;
+  const bool low = e < a.half;
+  const F2 cs = table[table_at(a, r, low ? e : e - a.half)];
+  const F other = load1(row + (low ? e + a.half : e - a.half));
+  return low ? fma((F)x, cs.x, -(other * cs.y)) : fma((F)x, cs.x, other * cs.y);
+}
+
+// One head's keys or values of a block of 16 rows: a warp.  Rows lo .. hi - 1 of the block are new, `row` is the first
+// of them in memory; codes and scale: the block's in the pool.
+template <typename T, int D>
+__device__ __forceinline__ void write_codes(const Args& a, const T* row, bool turn, const double2* table, int lo, int hi,
+                                            unsigned char* codes, int64_t code_row, float* scale) {
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = 16 / kRows;
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes;
+  const Lane l = turn ? lane_of(a, chunk) : Lane{kNeighbours, {16 * chunk, 16 * chunk + 8}, a.half};
+  const float old = lo > 0 ? within_limits(*scale) : 0.f;
+  float y[kSteps][16], most = 0.f;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int r = lo + i * kRows + sub;
+    if (r < hi) {
+      float x[16];
+      load8(row + (r - lo) * a.n_n + l.at[0], x);
+      load8(row + (r - lo) * a.n_n + l.at[1], x + 8);
+      // what is not finite becomes NaN and has no part in the scale; the largest value is rounded up, so that 64 bits
+      // just above 448 times a power of two count as more than that
+      auto round = [&](double v) -> float {
+        const float up = __double2float_ru(fabs(v)), f = __double2float_rn(v);
+        const bool fine = up < INFINITY;
+        most = fmaxf(most, fine ? up : 0.f);
+        return fine ? f : NAN;
+      };
+      auto as_is = [&](float f) -> float {
+        const bool fine = fabsf(f) < INFINITY;
+        most = fmaxf(most, fine ? fabsf(f) : 0.f);
+        return fine ? f : NAN;
+      };
+      if (!turn || (l.kind == kNeighbours && l.first >= a.half)) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[i][j] = as_is(x[j]);
+      } else if (l.kind == kLoose) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          y[i][j] = round(loose<double>(a, row + (r - lo) * a.n_n, 16 * chunk + j, x[j], table, r - lo));
+      } else {
+        Angles<double2, double> t;
+        t.load(a, l, table, r - lo);
+        rotate<Angles<double2, double>, double>(l.kind, a.half - l.first, t, x, y[i], round);
+      }
+    }
+  }
+  most = warp_max(most);
+  const float need = fitting_scale(most), s = fmaxf(need, old);
+  const Quotient over(s);
+  if (lo > 0 && s != old) {                             // older rows: the scale grew
+    const float ratio = old / s;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int r = i * kRows + sub;
+      if (r < lo) {
+        uint4* p = reinterpret_cast<uint4*>(codes + r * code_row + 16 * chunk);
+        *p = rescale16(*p, ratio);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int r = lo + i * kRows + sub;
+    if (r < hi) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        w[j] = pack2(over(y[i][4 * j]), over(y[i][4 * j + 1])) | pack2(over(y[i][4 * j + 2]), over(y[i][4 * j + 3])) << 16;
+      *reinterpret_cast<uint2*>(codes + r * code_row + l.at[0]) = make_uint2(w[0], w[1]);
+      *reinterpret_cast<uint2*>(codes + r * code_row + l.at[1]) = make_uint2(w[2], w[3]);
+    }
+  }
+  __syncwarp();                                         // (every lane has read the old scale)
+  if (lane == 0) *scale = s;
+}
+
+template <typename T, Where W, int D_SCALED>
+__global__ void __launch_bounds__(kThreads) rest_kv_append_kernel(const __grid_constant__ Args a) {
+  grid_wait();
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int b = blockIdx.x / a.groups, group = blockIdx.x % a.groups;
+  const int n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.N) : a.N;
+  const int L = W == kNowhere ? 0 : a.kv_len[b];
+  // new rows i0 .. i1 - 1 are rows lo ... of the block that starts at row `first`
+  const uint32_t first = ((uint32_t)max(L, 0) & ~15u) + 16u * group;
+  const int i0 = max((int)(first - (uint32_t)max(L, 0)), 0), lo = group == 0 ? max(L, 0) & 15 : 0;
+  const int m = min(n - i0, 16 - lo);
+  if (m <= 0) return;
+
+  float2* table = reinterpret_cast<float2*>(smem);
+  double2* table64 = reinterpret_cast<double2*>(table + 16 * a.half);
+  for (int e = threadIdx.x; e < m * a.half; e += kThreads) {
+    const int r = e / a.half, f = e - r * a.half;
+    double s, c;
+    sincos((double)a.pos[(int64_t)b * a.N + i0 + r] * (double)a.inv_freq[f], &s, &c);
+    s *= a.amplitude;
+    c *= a.amplitude;
+    table[table_at(a, r, f)] = make_float2((float)c, (float)s);
+    if constexpr (W == kPagesScaled) table64[table_at(a, r, f)] = make_double2(c, s);
+  }
+  __syncthreads();
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t page_row = W == kNowhere || L < 0 || first > 0x7FFFFFFFu ? -1 : row_offset(a.c, b, (int)first);
+  const int parts = gridDim.y, part = blockIdx.y;
+  int heads = a.H;                                      // of q, then (16-bit pages) of K and V
+  if constexpr (W == kPagesScaled) {
+    if (page_row >= 0) {
+      const int p = a.c.table[b * a.c.table_stride + (first >> a.c.page_log)];
+      const int64_t cell = (int64_t)p * a.H_kv * (1 << (a.c.page_log - 4)) + ((first & ((1u << a.c.page_log) - 1)) >> 4);
+      for (int u = part * kWarps + warp; u < 2 * a.H_kv; u += parts * kWarps) {
+        const int h = u >> 1;
+        const bool v = u & 1;
+        const T* row = static_cast<const T*>(v ? a.v_new : a.k_new) + b * a.n_b + i0 * a.n_n + h * a.n_h;
+        unsigned char* codes = reinterpret_cast<unsigned char*>((v ? a.c.v : a.c.k) + page_row + h * a.c.s_head);
+        write_codes<T, D_SCALED>(a, row, !v && a.half > 0, table64, lo, lo + m, codes, a.c.s_row * 16,
+                                 (v ? a.v_scales : a.k_scales) + cell + (int64_t)h * (1 << (a.c.page_log - 4)));
+      }
+    }
+  } else if constexpr (W == kPages16) {
+    heads += 2 * a.H_kv;
+  }
+
+  // rows of 16-bit (or 32-bit) results: D / 16 lanes a row; a lane stays with its row and steps through the heads
+  const int lanes = a.D >> 4, rows = 32 / lanes, sub = lane / lanes, chunk = lane % lanes;
+  if (sub >= rows) return;                              // (D / 16 need not divide 32)
+  const int me = warp * rows + sub, all = kWarps * rows;
+  const int together = all >= m ? all / m : 1;          // heads at a time
+  if (all >= m && me >= together * m) return;
+  const Lane l = lane_of(a, chunk);
+  const bool still = l.kind == kPairs ? false : l.kind == kLoose ? 16 * chunk >= 2 * a.half : l.first >= a.half;
+  const int moving = min(lanes, (2 * a.half + 15) >> 4);        // lanes of a row of loose pairs that hold some
+  for (int r = all >= m ? me % m : me; r < m; r += all >= m ? m : all) {
+    Angles<float2, float> t;
+    t.load(a, l, table, r);
+#pragma unroll 2
+    for (int h = (all >= m ? me / m : 0) + part * together; h < heads; h += together * parts) {
+      const T* from;
+      T* to;
+      bool turn = true;
+      if (W == kNowhere || h < a.H) {
+        from = static_cast<const T*>(a.q) + b * a.q_b + (i0 + r) * a.q_n + h * a.q_h;
+        to = static_cast<T*>(a.q_out) + b * a.o_b + (i0 + r) * a.o_n + h * a.o_h;
+      } else {
+        if (page_row < 0) break;
+        const bool v = h - a.H >= a.H_kv;
+        const int hk = h - a.H - (v ? a.H_kv : 0);
+        from = static_cast<const T*>(v ? a.v_new : a.k_new) + b * a.n_b + (i0 + r) * a.n_n + hk * a.n_h;
+        to = reinterpret_cast<T*>((v ? a.c.v : a.c.k) + page_row + hk * a.c.s_head + (lo + r) * a.c.s_row);
+        turn = !v;
+      }
+      Eight<T> e[2];
+      e[0].load(from + l.at[0]);
+      e[1].load(from + l.at[1]);
+      if (!turn || still) {
+        e[0].store(to + l.at[0]);
+        e[1].store(to + l.at[1]);
+        continue;
+      }
+      float x[16], y[16];
+      e[0].to(x);
+      e[1].to(x + 8);
+      if (l.kind == kLoose) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[j] = loose<float>(a, from, 16 * chunk + j, x[j], table, r);
+        // a row may be rotated in place: all its lanes have loaded before the first stores
+        __syncwarp(((moving == 32 ? 0u : 1u << moving) - 1u) << (sub * lanes));
+      } else {
+        rotate<Angles<float2, float>, float>(l.kind, a.half - l.first, t, x, y, [](float v) { return v; });
+      }
+      store8(to + l.at[0], y);
+      store8(to + l.at[1], y + 8);
+    }
+  }
+}
+
+template <typename T, Where W, int D>
+rest_status run(const Args& a, int B, void* stream) {
+  // about two blocks an SM, eight warps each, where the rows alone do not give them: then the heads are shared out
+  const int64_t blocks = (int64_t)B * a.groups;
+  if (blocks > 0x7FFFFFFFll) return REST_UNSUPPORTED;
+  const int most = min(a.N, 16), rows = 32 / (a.D / 16);
+  const int warps = ((W == kPages16 ? a.H + 2 * a.H_kv : a.H) * most + rows - 1) / rows + (W == kPagesScaled ? 2 * a.H_kv : 0);
+  const int sms = rest::sm_count();
+  int64_t parts = 2 * (int64_t)(sms > 0 ? sms : 148) / blocks;
+  parts = parts < 1 ? 1 : parts;
+  if (parts > (warps + kWarps - 1) / kWarps) parts = (warps + kWarps - 1) / kWarps;
+  const size_t smem = (size_t)16 * a.half * (W == kPagesScaled ? 24 : 8);
+  REST_CUDA_TRY(launch(rest_kv_append_kernel<T, W, D>, dim3((unsigned)blocks, (unsigned)parts), kThreads, smem, stream, a));
+  return REST_OK;
+}
+
+bool rows_ok(const int64_t* s, int64_t B, int64_t N, int64_t H, int D, int per_vec) {
+  const int64_t extent[3] = {B, N, H};
+  for (int i = 0; i < 3; ++i)
+    if (extent[i] > 1 && s[i] < D) return false;
+  return stride_ok(s, 3, per_vec);
+}
+
+// the rotation's arguments, for all three calls
+rest_status fill_turn(Args& a, const int32_t* pos, const float* inv_freq, int32_t pairs, int32_t interleaved, float amplitude,
+                      int32_t D) {
+  if (pairs < 0 || 2 * (int64_t)pairs > D || (pairs > 0 && (!pos || !inv_freq))) return REST_INVALID_ARG;
+  if (!(fabsf(amplitude) < INFINITY)) return REST_INVALID_ARG;
+  a.pos = pos; a.inv_freq = inv_freq; a.half = pairs; a.interleaved = interleaved != 0; a.amplitude = amplitude; a.D = D;
+  return REST_OK;
+}
+rest_status fill_q(Args& a, const void* q, const int64_t* qs, void* out, const int64_t* os, int64_t B, int64_t N, int64_t H,
+                   int per_vec) {
+  if (!q || !out || !qs || !os || !aligned16(q, out)) return REST_INVALID_ARG;
+  if (!rows_ok(qs, B, N, H, a.D, per_vec) || !rows_ok(os, B, N, H, a.D, per_vec)) return REST_INVALID_ARG;
+  a.q = q; a.q_out = out;
+  a.q_b = qs[0]; a.q_n = qs[1]; a.q_h = qs[2];
+  a.o_b = os[0]; a.o_n = os[1]; a.o_h = os[2];
+  return REST_OK;
+}
+
+rest_status append(void* d_k_pages, void* d_v_pages, const int64_t* page_strides, float* d_k_scales, float* d_v_scales, int32_t P,
+                   int32_t page, const int32_t* d_table, int64_t table_stride, int32_t table_cols, const int32_t* d_kv_len,
+                   const void* d_k_new, const void* d_v_new, const int64_t* new_strides, const int32_t* d_n_nodes, int32_t dtype,
+                   const int32_t* d_pos, const float* d_inv_freq, int32_t pairs, int32_t interleaved, float amplitude,
+                   const void* d_q, const int64_t* q_strides, void* d_q_out, const int64_t* out_strides, int32_t H, int32_t B,
+                   int32_t H_kv, int32_t N, int32_t D, bool scaled, void* stream) {
+  if (B < 0 || H_kv < 1 || N < 0 || H < 0 || !new_strides || (dtype != REST_BF16 && dtype != REST_FP16)) return REST_INVALID_ARG;
+  if (B == 0 || N == 0) return REST_OK;
+  if (!d_kv_len || !d_k_new || !d_v_new || !table_ok(d_table, table_stride, table_cols)) return REST_INVALID_ARG;
+  if (scaled && (!d_k_scales || !d_v_scales)) return REST_INVALID_ARG;
+  Args a = {};
+  if (rest_status st = fill_pool(a.c, d_k_pages, d_v_pages, page_strides, d_table, table_stride, table_cols, P, H_kv, page, D,
+                                 scaled ? 16 : 8))
+    return st;
+  if (H > 65536) return REST_UNSUPPORTED;
+  if (rest_status st = fill_turn(a, d_pos, d_inv_freq, pairs, interleaved, amplitude, D)) return st;
+  if (!rows_ok(new_strides, B, N, H_kv, D, 8) || !aligned16(d_k_new, d_v_new)) return REST_INVALID_ARG;
+  if (H > 0)
+    if (rest_status st = fill_q(a, d_q, q_strides, d_q_out, out_strides, B, N, H, 8)) return st;
+  a.k_scales = d_k_scales; a.v_scales = d_v_scales;
+  a.k_new = d_k_new; a.v_new = d_v_new;
+  a.n_b = new_strides[0]; a.n_n = new_strides[1]; a.n_h = new_strides[2];
+  a.kv_len = d_kv_len; a.n_nodes = d_n_nodes;
+  a.N = N; a.H = H; a.H_kv = H_kv;
+  a.groups = (N + 30) / 16;                             // blocks of 16 rows that N rows can touch
+  const bool bf16 = dtype == REST_BF16;
+  if (!scaled) return bf16 ? run<__nv_bfloat16, kPages16, 0>(a, B, stream) : run<__half, kPages16, 0>(a, B, stream);
+  if (D == 128)
+    return bf16 ? run<__nv_bfloat16, kPagesScaled, 128>(a, B, stream) : run<__half, kPagesScaled, 128>(a, B, stream);
+  return bf16 ? run<__nv_bfloat16, kPagesScaled, 64>(a, B, stream) : run<__half, kPagesScaled, 64>(a, B, stream);
+}
+
+}  // namespace
+
+extern "C" rest_status rest_rotary(const void* d_x, const int64_t* x_strides, int32_t dtype, const int32_t* d_pos,
+                                   const float* d_inv_freq, int32_t pairs, int32_t interleaved, float amplitude,
+                                   const int32_t* d_n_nodes, int32_t B, int32_t H, int32_t N, int32_t D, void* d_out,
+                                   const int64_t* out_strides, void* stream) {
+  if (B < 0 || H < 1 || N < 0 || D < 1 || (dtype != REST_BF16 && dtype != REST_FP16 && dtype != REST_FP32)) return REST_INVALID_ARG;
+  if (B == 0 || N == 0) return REST_OK;
+  if (D > 512 || (D % 16) != 0) return REST_UNSUPPORTED;
+  Args a = {};
+  if (rest_status st = fill_turn(a, d_pos, d_inv_freq, pairs, interleaved, amplitude, D)) return st;
+  if (rest_status st = fill_q(a, d_x, x_strides, d_out, out_strides, B, N, H, dtype == REST_FP32 ? 4 : 8)) return st;
+  a.n_nodes = d_n_nodes;
+  a.N = N; a.H = H;
+  a.groups = (N + 15) / 16;
+  if (dtype == REST_FP32) return run<float, kNowhere, 0>(a, B, stream);
+  return dtype == REST_BF16 ? run<__nv_bfloat16, kNowhere, 0>(a, B, stream) : run<__half, kNowhere, 0>(a, B, stream);
+}
+
+extern "C" rest_status rest_paged_kv_append(void* d_k_pages, void* d_v_pages, const int64_t* page_strides, int32_t P,
+                                            int32_t page, const int32_t* d_table, int64_t table_stride, int32_t table_cols,
+                                            const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new,
+                                            const int64_t* new_strides, const int32_t* d_n_nodes, int32_t dtype,
+                                            const int32_t* d_pos, const float* d_inv_freq, int32_t pairs, int32_t interleaved,
+                                            float amplitude, const void* d_q, const int64_t* q_strides, void* d_q_out,
+                                            const int64_t* out_strides, int32_t H, int32_t B, int32_t H_kv, int32_t N,
+                                            int32_t D, void* stream) {
+  return append(d_k_pages, d_v_pages, page_strides, nullptr, nullptr, P, page, d_table, table_stride, table_cols, d_kv_len,
+                d_k_new, d_v_new, new_strides, d_n_nodes, dtype, d_pos, d_inv_freq, pairs, interleaved, amplitude, d_q,
+                q_strides, d_q_out, out_strides, H, B, H_kv, N, D, false, stream);
+}
+
+extern "C" rest_status rest_paged_kv_append_scaled(void* d_k_pages, void* d_v_pages, const int64_t* page_strides,
+                                                   float* d_k_scales, float* d_v_scales, int32_t P, int32_t page,
+                                                   const int32_t* d_table, int64_t table_stride, int32_t table_cols,
+                                                   const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new,
+                                                   const int64_t* new_strides, const int32_t* d_n_nodes, int32_t dtype,
+                                                   const int32_t* d_pos, const float* d_inv_freq, int32_t pairs,
+                                                   int32_t interleaved, float amplitude, const void* d_q,
+                                                   const int64_t* q_strides, void* d_q_out, const int64_t* out_strides,
+                                                   int32_t H, int32_t B, int32_t H_kv, int32_t N, int32_t D, void* stream) {
+  return append(d_k_pages, d_v_pages, page_strides, d_k_scales, d_v_scales, P, page, d_table, table_stride, table_cols, d_kv_len,
+                d_k_new, d_v_new, new_strides, d_n_nodes, dtype, d_pos, d_inv_freq, pairs, interleaved, amplitude, d_q,
+                q_strides, d_q_out, out_strides, H, B, H_kv, N, D, true, stream);
+}

@@ -550,6 +550,24 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
                                  float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
 
 /*
+ * rest_paged_attention_scaled - rest_paged_attention over pages of codes with scales (see the cache in 8 bits, above).
+ *   The same formula with the values that the codes stand for: scores, maxima, sums and the output
+ *   in fp32; probabilities rounded to fp16 for their product with V (half a step, 2^-11 of each; below 2^-31 of
+ *   the row's largest they vanish).
+ *   d_q, d_out      dtype REST_BF16 or REST_FP16; strides as there, those of the pages (3..5) multiples of 16
+ *   d_k_scales, d_v_scales  float[P][H_kv][page / 16]
+ *   d_ws            scratch of rest_paged_attention_workspace_bytes() bytes
+ *   Everything else as in rest_paged_attention (codes have no infinities; NaN codes are NaN there).
+ */
+rest_status rest_paged_attention_scaled(const void* d_q, const void* d_k_pages, const void* d_v_pages,
+                                        const int64_t* strides, const float* d_k_scales, const float* d_v_scales,
+                                        int32_t dtype, int32_t P, int32_t page, const int32_t* d_table,
+                                        int64_t table_stride, int32_t table_cols, const int32_t* d_kv_len,
+                                        const int32_t* d_n_nodes, const uint32_t* d_mask, int32_t B, int32_t H,
+                                        int32_t H_kv, int32_t N, int32_t D, int32_t window, int32_t sinks, float scale,
+                                        void* d_out, float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
  * rest_accept_sampled - draft acceptance against the verifier's probabilities (Sec. 4.1 "Sampling
  * strategies": temperature and nucleus sampling), from random numbers that the caller supplies.
  * The tokens that come out are distributed exactly as plain sampling would distribute them.
@@ -652,7 +670,7 @@ rest_status rest_suffix_array_build_in_groups(const int32_t* d_tokens, uint64_t 
  * Device-side trouble that no per-call status can carry.  Every wait inside the kernels is
  * bounded; a kernel that gives up sets a bit here instead of spinning, and its output is then
  * undefined.  Reads and clears the flags of the current device (synchronises the device).
- *   bit 0: rest_tree_attention or rest_paged_attention gave up waiting for its tensor-core work
+ *   bit 0: rest_tree_attention or rest_paged_attention (_scaled) gave up waiting for its tensor-core work
  *   bit 1: one of them found its shared-memory window misaligned and did nothing
  */
 rest_status rest_device_error_flags(uint32_t* h_flags);

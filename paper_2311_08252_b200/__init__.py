@@ -58,7 +58,7 @@ EXPORTS = (
     "rest_accept_sampled",
     "rest_paged_kv_write", "rest_paged_kv_commit", "rest_pages_fork", "rest_pages_copy",
     "rest_pages_reserve", "rest_pages_release", "rest_rotary", "rest_paged_kv_append", "rest_paged_kv_append_scaled",
-    "rest_paged_kv_commit_scaled", "rest_pages_copy_scaled",
+    "rest_paged_kv_commit_scaled", "rest_pages_copy_scaled", "rest_paged_attention_scaled",
     "rest_accept", "rest_status_string", "rest_last_cuda_error", "rest_launch_count",
 )
 
@@ -154,6 +154,8 @@ def lib():
     L.rest_paged_kv_append_scaled.restype = i32
     L.rest_paged_kv_append_scaled.argtypes = scaled + table + [vp, vp, vp, strides, vp, i32] + turn + queries + \
         [i32] * 4 + [vp]
+    L.rest_paged_attention_scaled.restype = i32
+    L.rest_paged_attention_scaled.argtypes = [vp, vp, vp, strides, vp, vp] + L.rest_paged_attention.argtypes[4:]
     L.rest_paged_kv_commit_scaled.restype = i32
     L.rest_paged_kv_commit_scaled.argtypes = scaled + table + [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
     L.rest_pages_copy_scaled.restype = i32
@@ -619,25 +621,15 @@ def paged_attention_workspace_bytes(B, H, H_kv, N, D) -> int:
     return int(lib().rest_paged_attention_workspace_bytes(B, H, H_kv, N, D))
 
 
-def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, window=0, sinks=0, n_nodes=None,
-                         out=None, lse=None, workspace=None, stream=None):
-    """Attention of q [B,N,H,D] (bf16 or fp16; D 64 or 128; N = 1: one ordinary token) over a cache
-    in pages k_pages, v_pages [P,H_kv,page,D], and over the new rows kv_len[b] + i themselves.
-    mask: int32 or uint32 words [B,N,ceil(N/32)] as rest_draft writes them, None: node i sees nodes 0..i.
-    window > 0: a node sees the last `window` positions up to its own and the first `sinks` ones.
-    n_nodes int32[B]: later rows do not exist (their out / lse rows stay as they were).
-    lse: optional float32 [B,H,N].  workspace: a uint8 tensor of paged_attention_workspace_bytes(),
-    not shared by calls that may overlap; None: one is allocated.  out overlaps no input.  Returns
-    out [B,N,H,D]."""
+def _attend(name, q, index, pages, pointers, pool, scales, block_table, kv_len, mask, scale, window, sinks, n_nodes, out, lse,
+            workspace):
+    """What both attention calls check and pass on; pool: (strides, pages, rows per page), scales: none or two pointers."""
     import torch
-    if stream is not None:
-        with _as_current(stream, q):
-            return rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, window, sinks, n_nodes,
-                                        out, lse, workspace)
     L = _lib or lib()
-    index, (P, H_kv, page, Dk), pool = _pool(k_pages, v_pages)
+    P, H_kv, page, Dk = pages
     dtype, shape, qs = q.dtype, q.shape, q.stride()
-    if len(shape) != 4 or qs[3] != 1 or dtype is not k_pages.dtype or shape[3] != Dk or q.get_device() != index:
+    if len(shape) != 4 or qs[3] != 1 or not (dtype is torch.bfloat16 or dtype is torch.float16) or shape[3] != Dk or (
+            q.get_device() != index):
         raise RestError("q must be [B,N,H,D] with a contiguous last dimension, of the pages' type, head size and device")
     B, N, H, D = shape
     window, sinks = _window(window, sinks)
@@ -663,11 +655,32 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
         raise RestError("workspace must be a contiguous tensor on the same CUDA device")
     if workspace is not None:
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    strides = _I64x9(*qs[:3], *pool[2], *out.stride()[:3])
-    _call(L.rest_paged_attention, "rest_paged_attention", index, stream, q.data_ptr(), pool[0], pool[1], strides,
+    strides = _I64x9(*qs[:3], *pool[0], *out.stride()[:3])
+    _call(getattr(L, name), name, index, None, q.data_ptr(), *pointers, strides, *scales,
           REST_BF16 if dtype is torch.bfloat16 else REST_FP16, P, page, *table, _vec(kv_len, "kv_len", index, B),
           nodes_ptr, mask_ptr, B, H, H_kv, N, D, window, sinks, scale, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes)
     return out
+
+
+def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, window=0, sinks=0, n_nodes=None,
+                         out=None, lse=None, workspace=None, stream=None):
+    """Attention of q [B,N,H,D] (bf16 or fp16; D 64 or 128; N = 1: one ordinary token) over a cache
+    in pages k_pages, v_pages [P,H_kv,page,D], and over the new rows kv_len[b] + i themselves.
+    mask: int32 or uint32 words [B,N,ceil(N/32)] as rest_draft writes them, None: node i sees nodes 0..i.
+    window > 0: a node sees the last `window` positions up to its own and the first `sinks` ones.
+    n_nodes int32[B]: later rows do not exist (their out / lse rows stay as they were).
+    lse: optional float32 [B,H,N].  workspace: a uint8 tensor of paged_attention_workspace_bytes(),
+    not shared by calls that may overlap; None: one is allocated.  out overlaps no input.  Returns
+    out [B,N,H,D]."""
+    if stream is not None:
+        with _as_current(stream, q):
+            return rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, window, sinks, n_nodes,
+                                        out, lse, workspace)
+    index, pages, (k_ptr, v_ptr, *pool) = _pool(k_pages, v_pages)
+    if q.dtype is not k_pages.dtype:
+        raise RestError("q must be [B,N,H,D] with a contiguous last dimension, of the pages' type, head size and device")
+    return _attend("rest_paged_attention", q, index, pages, (k_ptr, v_ptr), pool, (), block_table, kv_len, mask, scale, window,
+                   sinks, n_nodes, out, lse, workspace)
 
 
 def rest_accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature, top_p, max_depth, out=None,
@@ -921,6 +934,20 @@ def _scaled_pool(k_pages, v_pages, k_scales, v_scales):
     return index, shape, (k_pages.data_ptr(), v_pages.data_ptr(), _I64x3(*strides[:3]),
                           _array(k_scales, "k_scales", index, want, torch.float32),
                           _array(v_scales, "v_scales", index, want, torch.float32), shape[0], shape[2])
+
+
+def rest_paged_attention_scaled(q, k_pages, v_pages, k_scales, v_scales, block_table, kv_len, mask, scale, window=0,
+                                sinks=0, n_nodes=None, out=None, lse=None, workspace=None, stream=None):
+    """rest_paged_attention over pages of 8-bit codes: k_pages, v_pages float8_e4m3fn [P,H_kv,page,D], k_scales,
+    v_scales float32 [P,H_kv,page/16] (row r of a page stands for scale[r / 16] * code); q and out bf16 or fp16.
+    Everything else as there, the workspace too."""
+    if stream is not None:
+        with _as_current(stream, q):
+            return rest_paged_attention_scaled(q, k_pages, v_pages, k_scales, v_scales, block_table, kv_len, mask, scale,
+                                               window, sinks, n_nodes, out, lse, workspace)
+    index, pages, (k_ptr, v_ptr, strides, ks_ptr, vs_ptr, *pool) = _scaled_pool(k_pages, v_pages, k_scales, v_scales)
+    return _attend("rest_paged_attention_scaled", q, index, pages, (k_ptr, v_ptr), (strides, *pool), (ks_ptr, vs_ptr),
+                   block_table, kv_len, mask, scale, window, sinks, n_nodes, out, lse, workspace)
 
 
 def rest_paged_kv_append_scaled(k_pages, v_pages, k_scales, v_scales, block_table, kv_len, k_new, v_new, positions=None,

@@ -19,11 +19,13 @@ cudaError_t ensure_dynamic_smem(const void* kernel, int kernel_slot, size_t byte
 int sm_count();
 // Reads and clears the error bits of the paged-attention kernels on the current device.
 rest_status take_paged_error_flags(uint32_t* h_flags);
+rest_status take_scaled_error_flags(uint32_t* h_flags);
 // One slot per kernel instance, library-wide: two kernels on one slot would skip each other's
 // attribute call.  The draft kernel's instances take kSmemSlotDraft + 0 ... 19, the paged
-// attention's kSmemSlotPaged + 0 ... 15, the sampled acceptance's kSmemSlotAccept + 0 ... 11.
+// attention's kSmemSlotPaged + 0 ... 15, the sampled acceptance's kSmemSlotAccept + 0 ... 11,
+// attention over pages of codes kSmemSlotScaled + 0 ... 15.
 constexpr int kSmemSlotDraft = 0, kSmemSlotAttn = 20, kSmemSlotAttnWide = 21, kSmemSlotPaged = 22,
-              kSmemSlotAccept = 38, kSmemSlots = 50;
+              kSmemSlotAccept = 38, kSmemSlotScaled = 50, kSmemSlots = 66;
 
 #define REST_CUDA_TRY(expr)                                              \
   do {                                                                   \

@@ -1228,9 +1228,10 @@ extern "C" rest_status rest_device_error_flags(uint32_t* h_flags) {
   unsigned int v = 0, zero = 0;
   REST_CUDA_TRY(cudaMemcpyFromSymbol(&v, g_attn_error, sizeof(v)));
   if (v != 0) REST_CUDA_TRY(cudaMemcpyToSymbol(g_attn_error, &zero, sizeof(zero)));
-  uint32_t paged = 0;
+  uint32_t paged = 0, scaled = 0;
   if (rest_status st = rest::take_paged_error_flags(&paged)) return st;
-  *h_flags = v | paged;
+  if (rest_status st = rest::take_scaled_error_flags(&scaled)) return st;
+  *h_flags = v | paged | scaled;
   return REST_OK;
 }
 

@@ -114,3 +114,23 @@ def test_the_plain_model():
     assert scales[0, 0, 0] == 2.0 ** -4 and (plain.decode(codes[0, 0, :2]) == [[112.0] * 16, [448.0] * 16]).all()
     plain.write(codes, scales, table, [2], np.full((1, 1, 1, 16), 1.0), [1])
     assert scales[0, 0, 0] == 2.0 ** -4 and (plain.decode(codes[0, 0, 2]) == 16).all()
+
+
+def attend(st=None, dtype=0, P=4, page=16, ts=3, cols=3, H=8, H_kv=2, N=4, D=128, window=0, sinks=0, scale=1.0, q=256,
+           scales=256, B=1):
+    st = strides(4096, 1024, 128, 4096, 2048, 128, 4096, 1024, 128) if st is None else st
+    return rest.lib().rest_paged_attention_scaled(q, 256, 256, st, scales, 256, dtype, P, page, 256, ts, cols, 256, None, 256, B, H,
+                                                  H_kv, N, D, window, sinks, scale, 256, None, None, 0, None)
+
+
+def test_attention_refuses():
+    assert attend(B=0) == OK
+    assert attend(D=96) == UNSUPPORTED and attend(N=257) == UNSUPPORTED and attend(H_kv=3) == UNSUPPORTED
+    assert attend(page=8) == UNSUPPORTED and attend(page=48) == UNSUPPORTED
+    assert attend(dtype=2) == INVALID and attend(dtype=-1) == INVALID and attend(scales=None) == INVALID
+    assert attend(scale=0.0) == INVALID and attend(scale=float("inf")) == INVALID and attend(scale=float("nan")) == INVALID
+    assert attend(window=-1) == INVALID and attend(sinks=-1) == INVALID and attend(P=0) == INVALID
+    assert attend(q=None) == INVALID and attend(q=264) == INVALID and attend(ts=2) == INVALID
+    assert attend(strides(4096, 1024, 128, 4096, 2048, 136, 4096, 1024, 128)) == INVALID     # rows of codes off 16 bytes
+    assert attend(strides(4096, 1024, 128, 4096, 2048, 64, 4096, 1024, 128)) == INVALID      # rows that overlap
+    assert attend() == INVALID                                                               # no scratch

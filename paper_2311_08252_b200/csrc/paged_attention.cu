@@ -57,7 +57,8 @@ rest_status rest::take_paged_error_flags(uint32_t* h_flags) { return take_error_
 
 extern "C" size_t rest_paged_attention_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t N, int32_t D) {
   if (B <= 0 || H <= 0 || H_kv <= 0 || N <= 0 || N > REST_MAX_N || (D != 64 && D != 128) || H % H_kv) return 0;
-  return workspace_bytes(plan(H, H_kv, N), D);
+  // pages of codes take no more: as many rows, and at most as many blocks
+  return workspace_bytes(plan(H, H_kv, N, false), D);
 }
 
 extern "C" rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const void* d_v_pages,

@@ -403,6 +403,97 @@ __device__ __noinline__ void write_not_finite(const Args& a, Piece p, bool live,
 // a partial O, weighed: what is not finite stays so under a weight that rounds to 0
 __device__ __forceinline__ float weighed(float o, float w) { return fabsf(o) < INFINITY ? o * w : o; }
 
+// A team's share of the flat tile list: the tiles that start in [x0, x1), where the first one lies (in the
+// control words), and how many teams share the list.  All threads of the block; a barrier follows.
+struct Share { long long x0, x1; int teams; };
+template <int BN, int NT, int THREADS>
+__device__ __forceinline__ Share find_share(const Args& a, const Rows& where, int row0, unsigned char* ctl) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), team = where.team;
+  long long x0, x1;
+  int teams;
+  const int per = (a.B + THREADS - 1) / THREADS;
+  long long mine = 0;
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i < a.B) {
+      const Ctx c = context<BN, NT>(a, tid * per + i, row0);
+      mine += a.H_kv * c.nt * c.cost;
+    }
+  long long inc = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long y = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+    if (lane >= d) inc += y;
+  }
+  long long* s_scan = reinterpret_cast<long long*>(ctl + kScan);
+  if (lane == 31) s_scan[warp] = inc;
+  __syncthreads();
+  long long before = 0, total = 0;
+  for (int w = 0; w < THREADS / 32; ++w) {
+    if (w == warp) before = total;
+    total += s_scan[w];
+  }
+  // fewer tiles than teams: one each, the rest idle (no share is shorter than a tile)
+  teams = (int)min((long long)where.teams, NT == 1 ? total : max(total / kBoth, 1ll));
+  // no more than 64 pieces of a unit: joining 296 pieces of one KV head took longer than the keys
+  // (32768 keys, one KV head: 51 us; in 128 pieces 27 us)
+  teams = min((long long)teams, 64ll * a.B * a.H_kv);
+  // one context: its units are alike, and with the same number of teams each no share crosses a border
+  if (a.B == 1 && teams > a.H_kv) teams -= teams % a.H_kv;
+  x0 = team < teams ? divide(total * team, teams) : total;
+  x1 = team < teams ? divide(total * (team + 1), teams) : total;
+  long long at = before + inc - mine;
+  if (x0 < x1 && at <= x0 && x0 < at + mine) {        // one thread
+    int b = tid * per;
+    for (;; ++b) {
+      const Ctx c = context<BN, NT>(a, b, row0);
+      const long long n = a.H_kv * c.nt * c.cost;
+      if (x0 < at + n) {
+        const long long skip = tiles_for(x0 - at, c.cost);
+        *reinterpret_cast<long long*>(ctl + kStartOff) = skip;
+        *reinterpret_cast<long long*>(ctl + kStartLeft) = x1 - at - skip * c.cost;
+        break;
+      }
+      at += n;
+    }
+    *reinterpret_cast<int*>(ctl + kStartB) = b;
+  }
+  if (tid == 0) {
+    if (x0 >= x1) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);      // else the V loader writes it
+    *reinterpret_cast<long long*>(ctl + kTotal) = total;
+  }
+  return {x0, x1, teams};
+}
+// The unit that a share starts but does not finish (if any) goes to the joining kernel (one thread).
+template <int BN, int NT>
+__device__ __forceinline__ void leave_unfinished(const Args& a, const Share& share, int team, int row0, unsigned char* ctl) {
+  const long long x0 = share.x0, x1 = share.x1;
+  const int teams = share.teams;
+  // {pieces, context, KV head}.  Its later pieces are the first pieces of the blocks that follow.
+  int4 m = make_int4(0, 0, 0, 0);
+  // step over whole contexts to the last tile of the share
+  long long off = *reinterpret_cast<long long*>(ctl + kStartOff), left = *reinterpret_cast<long long*>(ctl + kStartLeft);
+  int b = *reinterpret_cast<int*>(ctl + kStartB);
+  Ctx c;
+  long long count;
+  for (;;) {
+    c = context<BN, NT>(a, b, row0);
+    count = tiles_for(left, c.cost);
+    if (off + count <= a.H_kv * c.nt) break;
+    left -= (a.H_kv * c.nt - off) * c.cost;
+    off = 0;
+    ++b;
+  }
+  const long long end = off + count, u0 = (end - 1) / c.nt * c.nt, u1 = u0 + c.nt;      // its unit
+  const long long base = x1 - left - off * c.cost;                  // where context b starts
+  if (u1 > end && base + u0 * c.cost >= x0) {
+    const long long total = *reinterpret_cast<long long*>(ctl + kTotal), last = base + (u1 - 1) * c.cost;
+    int to = team + 1;
+    while (total * (to + 1) / teams <= last) ++to;
+    m = make_int4(to - team + 1, b, (int)(u0 / c.nt), 0);
+  }
+  a.meta[blockIdx.x] = m;
+}
+
 // One raw tile of codes -> an operand tile of type T in the 128-byte-swizzled layout, by a warp.  A lane takes 16
 // codes of a row and writes two 16-byte chunks; lanes of the second half of the head write theirs the other way round, so
 // that the eight lanes of a phase meet different banks.  CHECK: NaN codes become 0; true in a lane that found one in
@@ -541,61 +632,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
   // everything above is independent of the inputs; from here on global memory is read
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  // ---- this team's share of the flat tile list: the tiles that start in [x0, x1), and the first one's context
-  long long x0, x1;
-  int teams;
-  {
-    const int per = (a.B + S_::kThreads - 1) / S_::kThreads;
-    long long mine = 0;
-    for (int i = 0; i < per; ++i)
-      if (tid * per + i < a.B) {
-        const Ctx c = context<BN, NT>(a, tid * per + i, row0);
-        mine += a.H_kv * c.nt * c.cost;
-      }
-    long long inc = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const long long y = __shfl_up_sync(0xFFFFFFFFu, inc, d);
-      if (lane >= d) inc += y;
-    }
-    long long* s_scan = reinterpret_cast<long long*>(ctl + kScan);
-    if (lane == 31) s_scan[warp] = inc;
-    __syncthreads();
-    long long before = 0, total = 0;
-    for (int w = 0; w < S_::kThreads / 32; ++w) {
-      if (w == warp) before = total;
-      total += s_scan[w];
-    }
-    // fewer tiles than teams: one each, the rest idle (no share is shorter than a tile)
-    teams = (int)min((long long)where.teams, NT == 1 ? total : max(total / kBoth, 1ll));
-    // no more than 64 pieces of a unit: joining 296 pieces of one KV head took longer than the keys
-    // (32768 keys, one KV head: 51 us; in 128 pieces 27 us)
-    teams = min((long long)teams, 64ll * a.B * a.H_kv);
-    // one context: its units are alike, and with the same number of teams each no share crosses a border
-    if (a.B == 1 && teams > a.H_kv) teams -= teams % a.H_kv;
-    x0 = team < teams ? divide(total * team, teams) : total;
-    x1 = team < teams ? divide(total * (team + 1), teams) : total;
-    long long at = before + inc - mine;
-    if (x0 < x1 && at <= x0 && x0 < at + mine) {        // one thread
-      int b = tid * per;
-      for (;; ++b) {
-        const Ctx c = context<BN, NT>(a, b, row0);
-        const long long n = a.H_kv * c.nt * c.cost;
-        if (x0 < at + n) {
-          const long long skip = tiles_for(x0 - at, c.cost);
-          *reinterpret_cast<long long*>(ctl + kStartOff) = skip;
-          *reinterpret_cast<long long*>(ctl + kStartLeft) = x1 - at - skip * c.cost;
-          break;
-        }
-        at += n;
-      }
-      *reinterpret_cast<int*>(ctl + kStartB) = b;
-    }
-    if (tid == 0) {
-      if (x0 >= x1) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);      // else the V loader writes it
-      *reinterpret_cast<long long*>(ctl + kTotal) = total;
-    }
-  }
+  // ---- this team's share of the flat tile list
+  const Share share = find_share<BN, NT, S_::kThreads>(a, where, row0, ctl);
+  const long long x0 = share.x0, x1 = share.x1;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -764,33 +803,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           mbar_wait(full + (i % stages) * 8, (uint32_t)((i / stages) & 1));
       }
     }
-    if (is_v && lane == 0 && x0 < x1) {
-      // The unit that this share starts but does not finish (if any) goes to the joining kernel:
-      // {pieces, context, KV head}.  Its later pieces are the first pieces of the blocks that follow.
-      int4 m = make_int4(0, 0, 0, 0);
-      // step over whole contexts to the last tile of the share
-      long long off = *reinterpret_cast<long long*>(ctl + kStartOff), left = *reinterpret_cast<long long*>(ctl + kStartLeft);
-      int b = *reinterpret_cast<int*>(ctl + kStartB);
-      Ctx c;
-      long long count;
-      for (;;) {
-        c = context<BN, NT>(a, b, row0);
-        count = tiles_for(left, c.cost);
-        if (off + count <= a.H_kv * c.nt) break;
-        left -= (a.H_kv * c.nt - off) * c.cost;
-        off = 0;
-        ++b;
-      }
-      const long long end = off + count, u0 = (end - 1) / c.nt * c.nt, u1 = u0 + c.nt;      // its unit
-      const long long base = x1 - left - off * c.cost;                  // where context b starts
-      if (u1 > end && base + u0 * c.cost >= x0) {
-        const long long total = *reinterpret_cast<long long*>(ctl + kTotal), last = base + (u1 - 1) * c.cost;
-        int to = team + 1;
-        while (total * (to + 1) / teams <= last) ++to;
-        m = make_int4(to - team + 1, b, (int)(u0 / c.nt), 0);
-      }
-      a.meta[blockIdx.x] = m;
-    }
+    if (is_v && lane == 0 && x0 < x1) leave_unfinished<BN, NT>(a, share, team, row0, ctl);
   } else if (warp >= S_::kSoftmax + 2) {
     // ------------------------------------------------------------- MMA issuers, one per row tile
     // The whole warp walks the loop, so that descriptors and addresses stay in uniform registers, and one
@@ -1357,13 +1370,15 @@ bool encode_pool(CUtensorMap* map, const void* base, CUtensorMapDataType type, i
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-struct Plan { int NT, RB, teams, teams_last, rows; };
-Plan plan(int H, int H_kv, int N) {
+struct Plan { int NT, RB, teams, teams_last, rows; bool few; };
+// few: no 128-row tiles at all (pages of codes; one block an SM then)
+Plan plan(int H, int H_kv, int N, bool scaled) {
   Plan p;
   const int64_t R = (int64_t)(H / H_kv) * N;
-  p.NT = R > 128 ? 2 : 1;
+  p.few = scaled && R <= 16;
+  p.NT = R > 128 || (scaled && !p.few) ? 2 : 1;
   p.RB = (int)((R + 128 * p.NT - 1) / (128 * p.NT));
-  const int sms = rest::sm_count(), blocks = (p.NT == 1 ? 2 : 1) * (sms > 0 ? sms : 148);
+  const int sms = rest::sm_count(), blocks = (p.NT == 1 && !p.few ? 2 : 1) * (sms > 0 ? sms : 148);
   // A last row block of one row tile's height is quicker with its key tiles (its two row tiles take turns at
   // them), so it gets 0.6 of the blocks that another one has (16 x 16384 keys, 640 rows: 740 us with as many,
   // 750 us with 0.5, 686 us with 0.6, 702 us with 0.65, 716 us with 0.75).
@@ -1381,21 +1396,21 @@ size_t workspace_bytes(const Plan& p, int D) {
   return 32 + (blocks + 1) / 2 * 2 * sizeof(int4) + blocks * 2 * p.rows * (D + 2) * sizeof(float);
 }
 
-template <typename T, int D, int NT, int C, bool SCALED>
-rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int smem_slot, cudaStream_t st) {
-  using S_ = Shape<D, NT, SCALED>;
-  REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(paged_attention_kernel<T, D, NT, C, SCALED>), smem_slot, S_::kSmem));
+// a kernel over the shares, and the one that joins their pieces
+template <typename T, int D, typename K>
+rest_status launch_and_join(K kernel, const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int threads, int smem,
+                            cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.teams * (a.RB - 1) + a.teams_last), 1, 1);
-  cfg.blockDim = dim3((unsigned)S_::kThreads, 1, 1);
-  cfg.dynamicSmemBytes = S_::kSmem;
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_attention_kernel<T, D, NT, C, SCALED>, a, tm_k, tm_v));
+  REST_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, tm_k, tm_v));
   rest::count_launch();
   // never more cut units than shares or units; about eight blocks per SM in all, eight rows each at least
   // (one where units may be cut into more than 16 pieces)
@@ -1411,15 +1426,26 @@ rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
   return REST_OK;
 }
 
-template <typename T, int D, bool SCALED>
-rest_status pick(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Plan& pl, int slot, cudaStream_t st) {
-  slot += SCALED ? rest::kSmemSlotScaled : rest::kSmemSlotPaged;
-  if (pl.NT == 2) return run<T, D, 2, 1, SCALED>(a, tm_k, tm_v, slot, st);
-  if (pl.rows > 64) return run<T, D, 1, 1, SCALED>(a, tm_k, tm_v, slot + 1, st);
-  if (pl.rows > 32) return run<T, D, 1, 2, SCALED>(a, tm_k, tm_v, slot + 2, st);
-  return run<T, D, 1, 4, SCALED>(a, tm_k, tm_v, slot + 3, st);
+template <typename T, int D, int NT, int C, bool SCALED>
+rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int smem_slot, cudaStream_t st) {
+  using S_ = Shape<D, NT, SCALED>;
+  REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(paged_attention_kernel<T, D, NT, C, SCALED>), smem_slot, S_::kSmem));
+  return launch_and_join<T, D>(paged_attention_kernel<T, D, NT, C, SCALED>, a, tm_k, tm_v, S_::kThreads, S_::kSmem, st);
 }
 
+template <typename T, int D>
+rest_status pick(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Plan& pl, int slot, cudaStream_t st) {
+  slot += rest::kSmemSlotPaged;
+  if (pl.NT == 2) return run<T, D, 2, 1, false>(a, tm_k, tm_v, slot, st);
+  if (pl.rows > 64) return run<T, D, 1, 1, false>(a, tm_k, tm_v, slot + 1, st);
+  if (pl.rows > 32) return run<T, D, 1, 2, false>(a, tm_k, tm_v, slot + 2, st);
+  return run<T, D, 1, 4, false>(a, tm_k, tm_v, slot + 3, st);
+}
+// the same for pages of codes (in the file that has their kernels)
+template <typename T, int D>
+rest_status pick_scaled(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Plan& pl, int slot, cudaStream_t st);
+
+template <int V> struct Size { static constexpr int value = V; };
 // Either call: arguments checked, maps made, launched.
 template <bool SCALED>
 rest_status attend(const void* d_q, const void* d_k_pages, const void* d_v_pages, const int64_t* strides, const float* d_k_scales,
@@ -1446,7 +1472,7 @@ rest_status attend(const void* d_q, const void* d_k_pages, const void* d_v_pages
   if ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_k_pages) |
        reinterpret_cast<uintptr_t>(d_v_pages) | reinterpret_cast<uintptr_t>(d_out) | reinterpret_cast<uintptr_t>(d_ws)) & 15)
     return REST_INVALID_ARG;
-  const Plan pl = plan(H, H_kv, N);
+  const Plan pl = plan(H, H_kv, N, SCALED);
   if (!d_ws) return REST_INVALID_ARG;
   if (ws_bytes < workspace_bytes(pl, D)) return REST_WORKSPACE_TOO_SMALL;
   Args a;
@@ -1467,10 +1493,11 @@ rest_status attend(const void* d_q, const void* d_k_pages, const void* d_v_pages
   a.meta = reinterpret_cast<int4*>((reinterpret_cast<uintptr_t>(d_ws) + 31) & ~(uintptr_t)31);     // 32-byte stores
   a.ws_o = reinterpret_cast<float*>(a.meta + (blocks + 1) / 2 * 2);
   a.ws_ml = a.ws_o + blocks * 2 * pl.rows * D;
-  const int rows = page < 64 ? page : 64;               // of a box; a key tile has 64
+  const int rows = SCALED && pl.few ? 16 : page < 64 ? page : 64;         // of a box; a key tile has 64
   const CUtensorMapDataType type = SCALED ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                  : dtype == REST_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  const CUtensorMapSwizzle swizzle = SCALED ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
+  const CUtensorMapSwizzle swizzle = !SCALED || (pl.few && D == 128) ? CU_TENSOR_MAP_SWIZZLE_128B
+                                     : pl.few ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE;
   auto encode = [&](CUtensorMap* map, const void* base) {
     return encode_pool(map, base, type, SCALED ? 1 : 2, SCALED ? D : 64, swizzle, D, page, H_kv, P, strides + 3, rows, a.slot);
   };
@@ -1479,9 +1506,13 @@ rest_status attend(const void* d_q, const void* d_k_pages, const void* d_v_pages
     return rest::note_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf16 = dtype == REST_BF16;
-  if (D == 128)
-    return bf16 ? pick<__nv_bfloat16, 128, SCALED>(a, tm_k, tm_v, pl, 0, st) : pick<__half, 128, SCALED>(a, tm_k, tm_v, pl, 4, st);
-  return bf16 ? pick<__nv_bfloat16, 64, SCALED>(a, tm_k, tm_v, pl, 8, st) : pick<__half, 64, SCALED>(a, tm_k, tm_v, pl, 12, st);
+  auto go = [&](auto type_, auto size, int slot) {
+    using T = decltype(type_);
+    if constexpr (SCALED) return pick_scaled<T, size.value>(a, tm_k, tm_v, pl, slot, st);
+    else return pick<T, size.value>(a, tm_k, tm_v, pl, slot, st);
+  };
+  if (D == 128) return bf16 ? go(__nv_bfloat16(), Size<128>(), 0) : go(__half(), Size<128>(), 4);
+  return bf16 ? go(__nv_bfloat16(), Size<64>(), 8) : go(__half(), Size<64>(), 12);
 }
 
 // error bits of the including file's kernels, read and cleared (see rest_device_error_flags)

@@ -10,6 +10,446 @@
 #include "paged_attention.cuh"
 #include "rest.h"
 
+namespace {
+
+// ------------------------------------------------------------------------- up to 16 rows a KV head
+// Few rows make the K/V stream all that counts, and 128-row matrix instructions would read a tile of Q that is nearly
+// empty from shared memory for every 64 keys.  Here every warp works by itself, 16 keys at a time (one scale
+// of K and one of V): it fetches them by TMA into a ring of its own, widens the codes in registers and feeds them to
+// m16n8k16 instructions as the operand with 16 rows, S^T = K Q^T and O^T = V^T P^T, with 8 query rows (or 16, two
+// columns of tiles) as the other one.  No barrier is shared but at the end of a piece, where the eight warps' rows are
+// joined; meanwhile their rings (130 to 160 KB of keys on their way) fill with the next piece.
+//
+// The order of elements inside a dot product is free as long as both sides have the same one, and so is the order of O's
+// columns: lane (g, c) = (lane / 4, lane % 4) takes elements 32 c ... 32 c + 31 (D = 128) of keys g and g + 8 as its
+// part of K, and columns 16 g ... 16 g + 15 of keys 2c, 2c + 1, 2c + 8, 2c + 9 as its part of V, all in 16-byte
+// reads without bank conflicts (D = 64: half of either, 8-byte reads of V in twos).
+template <int D, int NB> struct Few {
+  static constexpr int kWarps = 8, kThreads = 32 * kWarps, kRows = 8 * NB;
+  static constexpr int kTile = 16 * D, kStage = 2 * kTile;                // bytes of 16 keys of K, and of K and V
+  static constexpr int kStages = (NB == 1 ? 5 : 4) * (128 / D);
+  static constexpr int kRing = kWarps * kStages * kStage;
+  static constexpr int kRowStride = D + 8;                                // floats: rows two apart meet different banks
+  static constexpr int kMerge = kRing, kMl = kMerge + kWarps * kRows * kRowStride * 4;     // [2][kWarps][kRows] float2
+  static constexpr int kScale = kMl + 2 * kWarps * kRows * 8;             // [kWarps][kStages] {K's, V's}
+  static constexpr int kBars = kScale + kWarps * kStages * 8;
+  static constexpr int kCtl = kBars + kWarps * kStages * 8;
+  static constexpr int kSmem = kCtl + 512;
+};
+
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {            // of an 8 x 8 matrix of 16-bit elements
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t halves(uint32_t two_codes) {        // the low two codes as fp16
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two_codes, __NV_E4M3);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void lds128(uint32_t at, uint32_t (&w)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void lds64(uint32_t at, uint32_t (&w)[2]) {
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+}
+// NaN codes become 0; whether there were any
+__device__ __forceinline__ bool without_nan(uint32_t& w) {
+  const uint32_t nan = ((w & 0x7F7F7F7Fu) + 0x01010101u & 0x80808080u) >> 7;
+  w &= ~(nan * 0xFFu);
+  return nan != 0;
+}
+// which of the 16 keys from key0 on packed row r of a piece sees
+__device__ __noinline__ uint32_t sees(const Args& a, Ctx ctx, int b, int rows, int r, int key0) {
+  if (r >= rows) return 0u;
+  const int node = node_of(a, r);
+  u64 mask0 = 0;
+  if (a.mask) {
+    const uint32_t* mp = a.mask + ((int64_t)b * a.N + node) * a.Wm;
+    mask0 = __ldg(mp);
+    if (a.Wm > 1) mask0 |= (u64)__ldg(mp + 1) << 32;
+  }
+  return (uint32_t)visible(a, ctx, b, node, a.window > 0 ? node_depth(a, b, node) : 1, mask0, key0) & 0xFFFFu;
+}
+
+template <typename T, int D, int NB>
+__global__ void __launch_bounds__(Few<D, NB>::kThreads, 1)
+paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+  using F = Few<D, NB>;
+  constexpr int W = F::kWarps, S = F::kStages, kWords = D / 32;           // words of V's four codes that a lane has of a key
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), g = lane >> 2, c = lane & 3;
+  const uint32_t sbase = smem_u32(smem), ring = sbase + warp * S * F::kStage, bars = sbase + F::kBars + warp * S * 8,
+                 scales = sbase + F::kScale + warp * S * 8;
+  unsigned char* ctl = smem + F::kCtl;
+  volatile uint32_t* abort_word = reinterpret_cast<volatile uint32_t*>(ctl + kAbort);
+  volatile int* s_bad = reinterpret_cast<volatile int*>(ctl + kBad);
+  const Rows where{0, (int)blockIdx.x, a.teams_last, 1};
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if ((sbase & 1023u) != 0) {                           // swizzled tiles need it (uniform over the grid)
+    if (tid == 0) {
+      atomicOr(&g_paged_error, 2u);
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);
+    }
+    return;
+  }
+  if (lane == 0)
+    for (int i = 0; i < S; ++i) mbar_init(bars + 8 * i, 3);               // the tiles' bytes, and two lanes' copies of a scale
+  if (tid == 0) {
+    *abort_word = 0u;
+    for (int i = 0; i < 8; ++i) s_bad[i] = 0;
+  }
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Share share = find_share<64, 1, F::kThreads>(a, where, 0, ctl);
+  __syncthreads();
+  Walk<64, 128> walk(a, *reinterpret_cast<int*>(ctl + kStartB), *reinterpret_cast<long long*>(ctl + kStartOff),
+                     share.x0 < share.x1 ? *reinterpret_cast<long long*>(ctl + kStartLeft) : 0ll, 0);
+
+  // ---- fetches: this warp's blocks of 16 keys, every W-th of a piece, S of them ahead, through all pieces
+  Walk<64, 128> ahead = walk;
+  Piece pa;
+  int at = warp, key_next = 0, page_next = -1, issued = 0, done = 0;
+  bool more = ahead.next(pa), dead = false;             // dead: a wait gave up; the block's barriers are still kept
+  auto settle = [&]() {                                 // the next block that has keys, and its page
+    while (more) {
+      if (at < 4 * pa.len) {
+        key_next = tile_key<64>(pa.c, pa.t0 + (at >> 2)) + (at & 3) * 16;
+        if (key_next < pa.c.L + pa.c.n) break;
+        at += W;
+      } else {
+        more = ahead.next(pa);
+        at = warp;
+      }
+    }
+    if (more) {
+      const int col = key_next >> a.page_log;
+      page_next = col < a.table_cols ? __ldg(a.table + pa.b * a.table_stride + col) : -1;
+    }
+  };
+  auto fetch = [&]() {
+    if (!more || dead) return;
+    const int stage = issued % S, row = key_next & ((1 << a.page_log) - 1);
+    const int page = page_next < 0 || page_next >= a.P ? a.P : page_next;               // outside the map: reads as zeros
+    const uint32_t bar = bars + 8 * stage, to = ring + stage * F::kStage;
+    if (lane == 0) {
+      mbar_expect_tx(bar, (uint32_t)F::kStage);
+      tma_page(to, &tm_k, 0, row, pa.hk, page, a.slot, bar);
+      tma_page(to + F::kTile, &tm_v, 0, row, pa.hk, page, a.slot, bar);
+    }
+    if (lane < 2) {
+      const float* from = lane ? a.v_scales : a.k_scales;
+      const int bytes = page < a.P ? 4 : 0;             // (else 0, which counts as the least scale)
+      if (bytes) from += ((int64_t)page * a.H_kv + pa.hk) * (1 << (a.page_log - 4)) + (row >> 4);
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(scales + stage * 8 + lane * 4), "l"(from), "r"(bytes) : "memory");
+      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+    }
+    ++issued;
+    at += W;
+    settle();
+  };
+  settle();
+  for (int i = 0; i < S; ++i) fetch();
+
+  Piece p;
+  int piece = 0;
+  while (walk.next(p)) {
+    ++piece;
+    // ---- Q as the second operand: fp16 under a power of two for each row (bf16 has fewer bits and more range)
+    uint32_t q[NB][2 * kWords][2];                      // [.][k step][.]
+    float mult[NB][2];                                  // what makes log2 units of a row's raw scores, but for K's scale
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+      const int r = t * 8 + g;
+      float x[D / 4], most = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 4; ++i) x[i] = 0.f;
+      if (r < p.rows) {
+        const int node = node_of(a, r);
+        const T* from = static_cast<const T*>(a.q) + p.b * a.q_b + node * a.q_n + (int64_t)(p.hk * a.G + r - node * a.G) * a.q_h + c * (D / 4);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          const uint4 v = *reinterpret_cast<const uint4*>(from + 8 * i);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 f = Type<T>::unpack(w[j]);
+            x[8 * i + 2 * j] = f.x;
+            x[8 * i + 2 * j + 1] = f.y;
+          }
+        }
+      }
+      float up = 1.f, own = a.scale_log2;
+      if constexpr (!__is_same(T, __half)) {
+#pragma unroll
+        for (int i = 0; i < D / 4; ++i) most = fmaxf(most, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.f);
+        most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+        // the largest to [2^14, 2^15): elements down to 2^-31 of it are exact
+        const int e = most > 0.f ? min(max(14 - ((int)(__float_as_uint(most) >> 23) - 127), -100), 100) : 0;
+        up = __uint_as_float((uint32_t)(e + 127) << 23);
+        own *= __uint_as_float((uint32_t)(127 - e) << 23);
+      }
+#pragma unroll
+      for (int s = 0; s < 2 * kWords; ++s) {
+        q[t][s][0] = Type<__half>::pack(x[4 * s] * up, x[4 * s + 1] * up);
+        q[t][s][1] = Type<__half>::pack(x[4 * s + 2] * up, x[4 * s + 3] * up);
+      }
+      mult[t][0] = __shfl_sync(0xFFFFFFFFu, own, 8 * c);
+      mult[t][1] = __shfl_sync(0xFFFFFFFFu, own, 8 * c + 4);
+    }
+    float o[NB][D / 16][4], m[NB][2], l[NB][2];
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[t][i][j] = 0.f;
+      m[t][0] = m[t][1] = -INFINITY;
+      l[t][0] = l[t][1] = 0.f;
+    }
+    int clear0, clear1;
+    clear_tiles<64>(a, p, clear0, clear1);
+    const int end = p.c.L + p.c.n;
+    for (int i = warp; i < 4 * p.len; i += W) {
+      const int it = i >> 2, key0 = tile_key<64>(p.c, p.t0 + it) + (i & 3) * 16;
+      if (key0 >= end) continue;
+      const int stage = done % S;
+      if (!dead && !wait_warp(bars + 8 * stage, (uint32_t)(done / S) & 1u, abort_word)) dead = true;
+      ++done;
+      if (dead) continue;
+      const uint32_t sK = ring + stage * F::kStage, sV = sK + F::kTile;
+      // ---- S^T: 16 keys x 8 rows, even and odd steps apart (half the chain of dependent products)
+      float s2[NB][2][4];
+#pragma unroll
+      for (int t = 0; t < NB; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s2[t][0][j] = s2[t][1][j] = 0.f;
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j) {
+        uint32_t lo[4], hi[4];                          // of keys g and g + 8
+        if constexpr (D == 128) {
+          lds128(sK + g * 128 + ((2 * c + j ^ g) << 4), lo);
+          lds128(sK + (g + 8) * 128 + ((2 * c + j ^ g) << 4), hi);
+        } else {
+          lds128(sK + g * 64 + ((c ^ (g >> 1)) << 4), lo);
+          lds128(sK + (g + 8) * 64 + ((c ^ (g >> 1)) << 4), hi);
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t k[4] = {halves(lo[w]), halves(hi[w]), halves(lo[w] >> 16), halves(hi[w] >> 16)};
+#pragma unroll
+          for (int t = 0; t < NB; ++t) mma_16x8x16(s2[t][w & 1], k, q[t][4 * j + w][0], q[t][4 * j + w][1]);
+        }
+      }
+      float sk, sv;
+      asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(sk), "=f"(sv) : "r"(scales + stage * 8) : "memory");
+      uint32_t v[4][kWords];                            // keys 2c, 2c + 1, 2c + 8, 2c + 9
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = 2 * c + (j & 1) + (j >> 1) * 8;
+        if constexpr (D == 128) lds128(sV + key * 128 + ((g ^ (key & 7)) << 4), v[j]);
+        else lds64(sV + key * 64 + ((g >> 1 ^ (key >> 1 & 3)) << 4) + (g & 1) * 8, v[j]);
+      }
+      __syncwarp();                                     // the stage is read: on to the block S further
+      fetch();
+      // ---- probabilities, as in the kernel above: the scale of V rides in the exponent
+      sk = rest_e4m3::within_limits(sk);
+      float log_v;
+      asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(log_v) : "f"(rest_e4m3::within_limits(sv)));
+      const float inv_v = ex2(-log_v);
+      float y[NB][4];                                   // raw scores: keys g, g, g + 8, g + 8, rows 2c, 2c + 1 in turn
+      float ka[NB][2];
+#pragma unroll
+      for (int t = 0; t < NB; ++t) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) ka[t][j] = fminf(fmaxf(sk * mult[t][j], 0x1p-126f), 0x1p127f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[t][j] = s2[t][0][j] + s2[t][1][j];
+      }
+      if (!(it >= clear0 && it < clear1)) {             // not every row sees every key
+#pragma unroll
+        for (int t = 0; t < NB; ++t)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t vis = sees(a, p.c, p.b, p.rows, t * 8 + 2 * c + j, key0) >> g;
+            if (!(vis & 1u)) y[t][j] = -INFINITY;
+            if (!(vis & 0x100u)) y[t][2 + j] = -INFINITY;
+          }
+        bool found = false;                             // NaN would reach rows that do not see its key (0 x NaN)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          bool any = false;
+#pragma unroll
+          for (int w = 0; w < kWords; ++w) any |= without_nan(v[j][w]);
+          found |= any && key0 + 2 * c + (j & 1) + (j >> 1) * 8 < end;
+        }
+        if (found) s_bad[piece & 7] = piece + 1;
+      }
+      bool over = false;
+#pragma unroll
+      for (int t = 0; t < NB; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) over |= fmaf(y[t][j], ka[t][j & 1], log_v) > m[t][j & 1] + (kRescaleStep + kShift);
+      if (__builtin_expect(__any_sync(0xFFFFFFFFu, over), 0)) {
+#pragma unroll
+        for (int t = 0; t < NB; ++t)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float mx = fmaf(fmaxf(y[t][j], y[t][2 + j]), ka[t][j], log_v);
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
+            const float m_new = fmaxf(m[t][j], ceilf(mx) - kShift);
+            const float alpha = m_new == -INFINITY ? 1.f : ex2(m[t][j] - m_new);
+            l[t][j] *= alpha;
+            m[t][j] = m_new;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) { o[t][e][j] *= alpha; o[t][e][2 + j] *= alpha; }
+          }
+      }
+      uint32_t pb[NB][2];
+#pragma unroll
+      for (int t = 0; t < NB; ++t) {
+        float e[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] = ex2(fmaf(y[t][j], ka[t][j & 1], log_v - (m[t][j & 1] == -INFINITY ? 0.f : m[t][j & 1])));
+        l[t][0] = fmaf(e[0] + e[2], inv_v, l[t][0]);
+        l[t][1] = fmaf(e[1] + e[3], inv_v, l[t][1]);
+        pb[t][0] = transposed(Type<__half>::pack(e[0], e[1]));
+        pb[t][1] = transposed(Type<__half>::pack(e[2], e[3]));
+      }
+      // ---- O^T += V^T P^T: columns 4 w ... 4 w + 3 of this lane's from word w, two to a product
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) {
+        const uint32_t ab = __byte_perm(v[0][w], v[1][w], 0x5140), cd = __byte_perm(v[2][w], v[3][w], 0x5140),
+                       ef = __byte_perm(v[0][w], v[1][w], 0x7362), gh = __byte_perm(v[2][w], v[3][w], 0x7362);
+        const uint32_t x[4] = {halves(ab), halves(ab >> 16), halves(cd), halves(cd >> 16)};
+        const uint32_t z[4] = {halves(ef), halves(ef >> 16), halves(gh), halves(gh >> 16)};
+#pragma unroll
+        for (int t = 0; t < NB; ++t) {
+          mma_16x8x16(o[t][2 * w], x, pb[t][0], pb[t][1]);
+          mma_16x8x16(o[t][2 * w + 1], z, pb[t][0], pb[t][1]);
+        }
+      }
+    }
+
+    // ---- the eight warps' rows are joined: maxima and sums first (in turns of two: a warp may be a piece ahead)
+    float2* ml = reinterpret_cast<float2*>(smem + F::kMl) + (piece & 1) * W * F::kRows;
+#pragma unroll
+    for (int t = 0; t < NB; ++t)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[t][j] += __shfl_xor_sync(0xFFFFFFFFu, l[t][j], d);
+        if (g == 0) ml[warp * F::kRows + t * 8 + 2 * c + j] = make_float2(m[t][j], l[t][j]);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < NB; ++t)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = t * 8 + 2 * c + j;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w * F::kRows + r].x);
+        const float weight = m[t][j] == -INFINITY ? 0.f : ex2(m[t][j] - top);
+        // columns 2e, 2e + 1 of this lane's D / 8 stand at e * 16 + 2 g
+        float* to = reinterpret_cast<float*>(smem + F::kMerge) + (warp * F::kRows + r) * F::kRowStride + 2 * g;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) *reinterpret_cast<float2*>(to + e * 16) = make_float2(o[t][e][j] * weight, o[t][e][2 + j] * weight);
+      }
+    __syncthreads();
+    const int64_t w0 = ((int64_t)blockIdx.x * 2 + (p.t0 == 0 ? 1 : 0)) * a.rows;
+    for (int r = warp; r < p.rows; r += W) {
+      const int gg = lane & 7, part = lane >> 3;        // columns (D / 8) gg + (D / 32) part ...
+      float top = -INFINITY, sum = 0.f, y[D / 32];
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) y[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w * F::kRows + r].x);
+#pragma unroll
+      for (int w = 0; w < W; ++w) {                     // (a maximum passes NaN over; the sum says so)
+        const float2 v = ml[w * F::kRows + r];
+        sum += v.y * (v.x == -INFINITY ? 0.f : ex2(v.x - top));
+        const float* from = reinterpret_cast<const float*>(smem + F::kMerge) + (w * F::kRows + r) * F::kRowStride + 2 * gg;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) {
+          const float2 f = *reinterpret_cast<const float2*>(from + (part * (D / 64) + e) * 16);
+          y[2 * e] += f.x;
+          y[2 * e + 1] += f.y;
+        }
+      }
+      const int node = node_of(a, r), head = p.hk * a.G + r - node * a.G, col = gg * (D / 8) + part * (D / 32);
+      if (p.whole) {
+        const float inv = sum != 0.f ? 1.f / sum : 0.f;
+        uint32_t* to = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + p.b * a.o_b + node * a.o_n + head * a.o_h + col);
+        uint32_t v[D / 64];
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) v[e] = sum != 0.f ? Type<T>::pack(y[2 * e] * inv, y[2 * e + 1] * inv) : 0u;
+        if constexpr (D == 128) *reinterpret_cast<uint2*>(to) = make_uint2(v[0], v[1]);
+        else *to = v[0];
+        if (a.lse && lane == 0) a.lse[((int64_t)p.b * a.H + head) * a.N + node] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+      } else {
+        float* to = a.ws_o + (w0 + r) * D + col;
+        if constexpr (D == 128) *reinterpret_cast<float4*>(to) = make_float4(y[0], y[1], y[2], y[3]);
+        else *reinterpret_cast<float2*>(to) = make_float2(y[0], y[1]);
+        if (lane == 0) *reinterpret_cast<float2*>(a.ws_ml + (w0 + r) * 2) = make_float2(top, sum);
+      }
+    }
+    if (__builtin_expect(s_bad[piece & 7] == piece + 1, 0)) {             // (behind a barrier: all threads see the same)
+      __syncthreads();
+      if (warp == 0) {
+        const int r = lane;
+        bool live = r < p.rows;
+        const int node = live ? node_of(a, r) : 0, head = p.hk * a.G + (live ? r - node * a.G : 0);
+        u64 mask0 = 0;
+        float sum = 0.f;
+        if (live) {
+          for (int w = 0; w < W; ++w) sum += ml[w * F::kRows + r].y;
+          if (a.mask) {
+            const uint32_t* mp = a.mask + ((int64_t)p.b * a.N + node) * a.Wm;
+            mask0 = __ldg(mp);
+            if (a.Wm > 1) mask0 |= (u64)__ldg(mp + 1) << 32;
+          }
+        }
+        live = live && sum == sum;                      // (a row whose sum is NaN is NaN throughout)
+        write_not_finite<T, D, 64, true>(a, p, live, node, live && a.window > 0 ? node_depth(a, p.b, node) : 1, mask0,
+                                         p.whole ? p.b * a.o_b + node * a.o_n + head * a.o_h : (w0 + r) * D);
+      }
+    }
+  }
+  if (*abort_word != 0u || dead) {                      // giving up: let the copies in flight land before this block goes away
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    for (int i = max(0, issued - S); i < issued; ++i) mbar_wait(bars + (i % S) * 8, (uint32_t)((i / S) & 1));
+    if (lane == 0) atomicOr(&g_paged_error, 1u);
+  }
+  if (tid == 0 && share.x0 < share.x1) leave_unfinished<64, 1>(a, share, where.team, 0, ctl);
+}
+
+template <typename T, int D, int NB>
+rest_status run_few(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int slot, cudaStream_t st) {
+  using F = Few<D, NB>;
+  static_assert(F::kSmem <= 232448, "shared memory of a block");
+  REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(paged_attention_few_kernel<T, D, NB>), slot, F::kSmem));
+  return launch_and_join<T, D>(paged_attention_few_kernel<T, D, NB>, a, tm_k, tm_v, F::kThreads, F::kSmem, st);
+}
+
+template <typename T, int D>
+rest_status pick_scaled(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Plan& pl, int slot, cudaStream_t st) {
+  slot += rest::kSmemSlotScaled;
+  if (pl.few) return pl.rows > 8 ? run_few<T, D, 2>(a, tm_k, tm_v, slot + 3, st) : run_few<T, D, 1>(a, tm_k, tm_v, slot + 2, st);
+  return run<T, D, 2, 1, true>(a, tm_k, tm_v, slot, st);
+}
+
+}  // namespace
+
 rest_status rest::take_scaled_error_flags(uint32_t* h_flags) { return take_error_flags(h_flags); }
 
 extern "C" rest_status rest_paged_attention_scaled(const void* d_q, const void* d_k_pages, const void* d_v_pages,

@@ -555,7 +555,7 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
  *   in fp32; probabilities rounded to fp16 for their product with V (half a step, 2^-11 of each; below 2^-31 of
  *   the row's largest they vanish).
  *   d_q, d_out      dtype REST_BF16 or REST_FP16; strides as there, those of the pages (3..5) multiples of 16
- *   d_k_scales, d_v_scales  float[P][H_kv][page / 16]
+ *   d_k_scales, d_v_scales  float[P][H_kv][page / 16], aligned to min(page, 64) / 4 bytes
  *   d_ws            scratch of rest_paged_attention_workspace_bytes() bytes
  *   Everything else as in rest_paged_attention (codes have no infinities; NaN codes are NaN there).
  */

@@ -407,7 +407,7 @@ __device__ __forceinline__ float weighed(float o, float w) { return fabsf(o) < I
 // control words), and how many teams share the list.  All threads of the block; a barrier follows.
 struct Share { long long x0, x1; int teams; };
 template <int BN, int NT, int THREADS>
-__device__ __forceinline__ Share find_share(const Args& a, const Rows& where, int row0, unsigned char* ctl) {
+__device__ __forceinline__ Share find_share(const Args& a, const Rows& where, int row0, unsigned char* ctl, unsigned char* scan) {
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), team = where.team;
   long long x0, x1;
   int teams;
@@ -424,7 +424,7 @@ __device__ __forceinline__ Share find_share(const Args& a, const Rows& where, in
     const long long y = __shfl_up_sync(0xFFFFFFFFu, inc, d);
     if (lane >= d) inc += y;
   }
-  long long* s_scan = reinterpret_cast<long long*>(ctl + kScan);
+  long long* s_scan = reinterpret_cast<long long*>(scan);      // a sum of each warp
   if (lane == 31) s_scan[warp] = inc;
   __syncthreads();
   long long before = 0, total = 0;
@@ -633,7 +633,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   // ---- this team's share of the flat tile list
-  const Share share = find_share<BN, NT, S_::kThreads>(a, where, row0, ctl);
+  const Share share = find_share<BN, NT, S_::kThreads>(a, where, row0, ctl, ctl + kScan);
   const long long x0 = share.x0, x1 = share.x1;
   tc_fence_before();
   __syncthreads();
@@ -1472,6 +1472,8 @@ rest_status attend(const void* d_q, const void* d_k_pages, const void* d_v_pages
   if ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_k_pages) |
        reinterpret_cast<uintptr_t>(d_v_pages) | reinterpret_cast<uintptr_t>(d_out) | reinterpret_cast<uintptr_t>(d_ws)) & 15)
     return REST_INVALID_ARG;
+  if (SCALED && ((reinterpret_cast<uintptr_t>(d_k_scales) | reinterpret_cast<uintptr_t>(d_v_scales)) & ((page < 64 ? page : 64) / 4 - 1)))
+    return REST_INVALID_ARG;                            // scales of 64 rows, or of a page, are copied at once
   const Plan pl = plan(H, H_kv, N, SCALED);
   if (!d_ws) return REST_INVALID_ARG;
   if (ws_bytes < workspace_bytes(pl, D)) return REST_WORKSPACE_TOO_SMALL;
@@ -1493,7 +1495,7 @@ rest_status attend(const void* d_q, const void* d_k_pages, const void* d_v_pages
   a.meta = reinterpret_cast<int4*>((reinterpret_cast<uintptr_t>(d_ws) + 31) & ~(uintptr_t)31);     // 32-byte stores
   a.ws_o = reinterpret_cast<float*>(a.meta + (blocks + 1) / 2 * 2);
   a.ws_ml = a.ws_o + blocks * 2 * pl.rows * D;
-  const int rows = SCALED && pl.few ? 16 : page < 64 ? page : 64;         // of a box; a key tile has 64
+  const int rows = page < 64 ? page : 64;               // of a box; a key tile has 64
   const CUtensorMapDataType type = SCALED ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                  : dtype == REST_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   const CUtensorMapSwizzle swizzle = !SCALED || (pl.few && D == 128) ? CU_TENSOR_MAP_SWIZZLE_128B

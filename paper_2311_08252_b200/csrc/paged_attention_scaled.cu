@@ -14,27 +14,29 @@ namespace {
 
 // ------------------------------------------------------------------------- up to 16 rows a KV head
 // Few rows make the K/V stream all that counts, and 128-row matrix instructions would read a tile of Q that is nearly
-// empty from shared memory for every 64 keys.  Here every warp works by itself, 16 keys at a time (one scale
-// of K and one of V): it fetches them by TMA into a ring of its own, widens the codes in registers and feeds them to
-// m16n8k16 instructions as the operand with 16 rows, S^T = K Q^T and O^T = V^T P^T, with 8 query rows (or 16, two
-// columns of tiles) as the other one.  No barrier is shared but at the end of a piece, where the eight warps' rows are
-// joined; meanwhile their rings (130 to 160 KB of keys on their way) fill with the next piece.
+// empty from shared memory for every 64 keys.  Here two warps fetch key tiles by TMA into a ring (176 to 192 KB of
+// keys on their way), and the others take 16 keys at a time (one scale of K and one of V), four warps a tile: they widen the
+// codes in registers and feed them to m16n8k16 instructions as the operand with 16 rows, S^T = K Q^T and O^T = V^T P^T,
+// with 8 query rows (or 16, two columns of tiles) as the other one.  Each has maxima, sums and O of its own; they
+// meet at the end of a piece only, where their rows are joined while the ring fills with the next piece.
 //
 // The order of elements inside a dot product is free as long as both sides have the same one, and so is the order of O's
 // columns: lane (g, c) = (lane / 4, lane % 4) takes elements 32 c ... 32 c + 31 (D = 128) of keys g and g + 8 as its
 // part of K, and columns 16 g ... 16 g + 15 of keys 2c, 2c + 1, 2c + 8, 2c + 9 as its part of V, all in 16-byte
 // reads without bank conflicts (D = 64: half of either, 8-byte reads of V in twos).
 template <int D, int NB> struct Few {
-  static constexpr int kWarps = 8, kThreads = 32 * kWarps, kRows = 8 * NB;
-  static constexpr int kTile = 16 * D, kStage = 2 * kTile;                // bytes of 16 keys of K, and of K and V
-  static constexpr int kStages = (NB == 1 ? 5 : 4) * (128 / D);
-  static constexpr int kRing = kWarps * kStages * kStage;
+  static constexpr int kWarps = NB == 1 ? 12 : 8, kTeams = kWarps / 4, kThreads = 32 * (kWarps + 2), kRows = 8 * NB;
+  static constexpr int kTile = 64 * D, kStage = 2 * kTile;                // bytes of 64 keys of K, and of K and V
+  static constexpr int kStages = (NB == 1 ? 12 : 11) * (128 / D);
+  static constexpr int kRing = kStages * kStage;
+  static constexpr int kCopies = kWarps / 2;                              // of O in the join
   static constexpr int kRowStride = D + 8;                                // floats: rows two apart meet different banks
-  static constexpr int kMerge = kRing, kMl = kMerge + kWarps * kRows * kRowStride * 4;     // [2][kWarps][kRows] float2
-  static constexpr int kScale = kMl + 2 * kWarps * kRows * 8;             // [kWarps][kStages] {K's, V's}
-  static constexpr int kBars = kScale + kWarps * kStages * 8;
-  static constexpr int kCtl = kBars + kWarps * kStages * 8;
-  static constexpr int kSmem = kCtl + 512;
+  static constexpr int kMerge = kRing, kMl = kMerge + kCopies * kRows * kRowStride * 4;    // [2][kWarps][kRows] float2
+  static constexpr int kScale = kMl + 2 * kWarps * kRows * 8;             // [kStages] {K's of 16 keys each, V's}
+  static constexpr int kFull = kScale + kStages * 32, kFree = kFull + kStages * 8;
+  static constexpr int kCtl = (kFree + kStages * 8 + 15) / 16 * 16;
+  static constexpr int kScanAt = 512;                                     // of the control words: a sum of each warp
+  static constexpr int kSmem = kCtl + 512 + 8 * (kWarps + 2);
 };
 
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -48,9 +50,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {            // of an
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t halves(uint32_t two_codes) {        // the low two codes as fp16
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two_codes, __NV_E4M3);
-  return *reinterpret_cast<const uint32_t*>(&h);
+__device__ __forceinline__ void halves(uint32_t codes, uint32_t& lo, uint32_t& hi) {    // four codes as fp16
+  asm("{.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;}" : "=r"(lo), "=r"(hi) : "r"(codes));
 }
 __device__ __forceinline__ void lds128(uint32_t at, uint32_t (&w)[4]) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
@@ -81,11 +82,10 @@ template <typename T, int D, int NB>
 __global__ void __launch_bounds__(Few<D, NB>::kThreads, 1)
 paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   using F = Few<D, NB>;
-  constexpr int W = F::kWarps, S = F::kStages, kWords = D / 32;           // words of V's four codes that a lane has of a key
+  constexpr int W = F::kWarps, S = F::kStages, TEAMS = F::kTeams, kWords = D / 32;           // words of V's four codes that a lane has of a key
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), g = lane >> 2, c = lane & 3;
-  const uint32_t sbase = smem_u32(smem), ring = sbase + warp * S * F::kStage, bars = sbase + F::kBars + warp * S * 8,
-                 scales = sbase + F::kScale + warp * S * 8;
+  const uint32_t sbase = smem_u32(smem), ring = sbase, full = sbase + F::kFull, free_ = sbase + F::kFree, scales = sbase + F::kScale;
   unsigned char* ctl = smem + F::kCtl;
   volatile uint32_t* abort_word = reinterpret_cast<volatile uint32_t*>(ctl + kAbort);
   volatile int* s_bad = reinterpret_cast<volatile int*>(ctl + kBad);
@@ -100,65 +100,81 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
     }
     return;
   }
-  if (lane == 0)
-    for (int i = 0; i < S; ++i) mbar_init(bars + 8 * i, 3);               // the tiles' bytes, and two lanes' copies of a scale
   if (tid == 0) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init(full + 8 * i, 2 + 2 * (64 >> min(a.page_log, 6)));        // two tiles' bytes, and each box's scales
+      mbar_init(free_ + 8 * i, 4);
+    }
     *abort_word = 0u;
     for (int i = 0; i < 8; ++i) s_bad[i] = 0;
   }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const Share share = find_share<64, 1, F::kThreads>(a, where, 0, ctl);
+  const Share share = find_share<64, 1, F::kThreads>(a, where, 0, ctl, ctl + F::kScanAt);
   __syncthreads();
   Walk<64, 128> walk(a, *reinterpret_cast<int*>(ctl + kStartB), *reinterpret_cast<long long*>(ctl + kStartOff),
                      share.x0 < share.x1 ? *reinterpret_cast<long long*>(ctl + kStartLeft) : 0ll, 0);
 
-  // ---- fetches: this warp's blocks of 16 keys, every W-th of a piece, S of them ahead, through all pieces
-  Walk<64, 128> ahead = walk;
-  Piece pa;
-  int at = warp, key_next = 0, page_next = -1, issued = 0, done = 0;
-  bool more = ahead.next(pa), dead = false;             // dead: a wait gave up; the block's barriers are still kept
-  auto settle = [&]() {                                 // the next block that has keys, and its page
-    while (more) {
-      if (at < 4 * pa.len) {
-        key_next = tile_key<64>(pa.c, pa.t0 + (at >> 2)) + (at & 3) * 16;
-        if (key_next < pa.c.L + pa.c.n) break;
-        at += W;
-      } else {
-        more = ahead.next(pa);
-        at = warp;
+  Piece p;
+  if (warp >= W) {
+    // ------------------------------------------------------------------ K's and V's fetching warps
+    // A lane has a box (a page, or 64 rows of a larger one) and its scales, so a warp works out the addresses of 8 to 32
+    // tiles at once; then it goes through them, and only waits and starts copies.
+    const bool is_v = warp > W;
+    const CUtensorMap* map = is_v ? &tm_v : &tm_k;
+    const uint32_t my_ring = ring + (is_v ? F::kTile : 0), my_scale = scales + (is_v ? 16 : 0);
+    const int box_log = min(a.page_log, 6), boxes_log = 6 - box_log, mine = lane >> boxes_log, at_once = 32 >> boxes_log;
+    const int box0 = (lane & ((1 << boxes_log) - 1)) << box_log;          // the box's first row in its tile
+    int slot = 0, filled = 0;
+    uint32_t parity = 1;                                // a fresh ring's slots count as free
+    bool ok = true;
+    while (ok && walk.next(p)) {
+      for (int it0 = 0; ok && it0 < p.len; it0 += at_once) {
+        const int row = tile_key<64>(p.c, p.t0 + min(it0 + mine, p.len - 1)) + box0, col = row >> a.page_log;
+        int page = col < a.table_cols ? __ldg(a.table + p.b * a.table_stride + col) : -1;
+        if (page < 0 || page >= a.P) page = a.P;        // outside the map: reads as zeros
+        const int in_page = row & ((1 << a.page_log) - 1);
+        const int c1 = a.slot[0] == 1 ? in_page : a.slot[1] == 1 ? p.hk : page, c2 = a.slot[0] == 2 ? in_page : a.slot[1] == 2 ? p.hk : page,
+                  c3 = a.slot[0] == 3 ? in_page : a.slot[1] == 3 ? p.hk : page;
+        // (without a page 0, which counts as the least scale)
+        const float* from = is_v ? a.v_scales : a.k_scales;
+        const int bytes = page < a.P ? 1 << (box_log - 2) : 0;
+        if (bytes) from += (((int64_t)page * a.H_kv + p.hk) << (a.page_log - 4)) + (in_page >> 4);
+        const int n = min(at_once, p.len - it0);
+        for (int j = 0; j < n; ++j) {
+          if (filled >= S) ok = wait_warp(free_ + slot * 8, parity, abort_word);
+          if (!ok) break;
+          if (mine == j) {
+            const uint32_t bar = full + slot * 8, to = my_scale + slot * 32 + (box0 >> 2);
+            if (box0 == 0) mbar_expect_tx(bar, (uint32_t)F::kTile);
+            asm volatile(
+                "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                ::"r"(my_ring + slot * F::kStage + box0 * D), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(c1), "r"(c2), "r"(c3)
+                : "memory");
+            if (box_log == 6) asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+            else if (box_log == 5) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+          }
+          __syncwarp();
+          ++filled;
+          if (++slot == S) { slot = 0; parity ^= 1; }
+        }
       }
     }
-    if (more) {
-      const int col = key_next >> a.page_log;
-      page_next = col < a.table_cols ? __ldg(a.table + pa.b * a.table_stride + col) : -1;
+    if (*abort_word != 0u) {                            // giving up: let the copies in flight land before this block goes away
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      for (int i = max(0, filled - S); i < filled; ++i) mbar_wait(full + (i % S) * 8, (uint32_t)((i / S) & 1));
     }
-  };
-  auto fetch = [&]() {
-    if (!more || dead) return;
-    const int stage = issued % S, row = key_next & ((1 << a.page_log) - 1);
-    const int page = page_next < 0 || page_next >= a.P ? a.P : page_next;               // outside the map: reads as zeros
-    const uint32_t bar = bars + 8 * stage, to = ring + stage * F::kStage;
-    if (lane == 0) {
-      mbar_expect_tx(bar, (uint32_t)F::kStage);
-      tma_page(to, &tm_k, 0, row, pa.hk, page, a.slot, bar);
-      tma_page(to + F::kTile, &tm_v, 0, row, pa.hk, page, a.slot, bar);
-    }
-    if (lane < 2) {
-      const float* from = lane ? a.v_scales : a.k_scales;
-      const int bytes = page < a.P ? 4 : 0;             // (else 0, which counts as the least scale)
-      if (bytes) from += ((int64_t)page * a.H_kv + pa.hk) * (1 << (a.page_log - 4)) + (row >> 4);
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(scales + stage * 8 + lane * 4), "l"(from), "r"(bytes) : "memory");
-      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-    }
-    ++issued;
-    at += W;
-    settle();
-  };
-  settle();
-  for (int i = 0; i < S; ++i) fetch();
+    if (is_v && lane == 0 && share.x0 < share.x1) leave_unfinished<64, 1>(a, share, where.team, 0, ctl);
+    return;
+  }
 
-  Piece p;
+  // -------------------------------------------------------------------- the others
+  const int team = warp >> 2, sub = warp & 3;           // tiles team, team + TEAMS ... of a piece, keys 16 sub ... of each
+  auto meet = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(32 * W) : "memory"); };
+  uint32_t base = 0;                                    // tiles before this piece
+  bool dead = false;                                    // a wait gave up; the barriers of the block are still kept
   int piece = 0;
   while (walk.next(p)) {
     ++piece;
@@ -218,14 +234,21 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
     int clear0, clear1;
     clear_tiles<64>(a, p, clear0, clear1);
     const int end = p.c.L + p.c.n;
-    for (int i = warp; i < 4 * p.len; i += W) {
-      const int it = i >> 2, key0 = tile_key<64>(p.c, p.t0 + it) + (i & 3) * 16;
-      if (key0 >= end) continue;
-      const int stage = done % S;
-      if (!dead && !wait_warp(bars + 8 * stage, (uint32_t)(done / S) & 1u, abort_word)) dead = true;
-      ++done;
-      if (dead) continue;
-      const uint32_t sK = ring + stage * F::kStage, sV = sK + F::kTile;
+    uint32_t slot = (base + team) % S, parity = (base + team) / S & 1;
+    base += p.len;
+#pragma unroll 1
+    for (int it = team; it < p.len; it += TEAMS) {
+      const int key0 = tile_key<64>(p.c, p.t0 + it) + sub * 16;
+      if (!dead && !wait_warp(full + 8 * slot, parity, abort_word)) dead = true;
+      if (dead) break;
+      const uint32_t sK = ring + slot * F::kStage + sub * (16 * D), sV = sK + F::kTile, at_scale = scales + slot * 32 + sub * 4,
+                     bar = free_ + 8 * slot;
+      slot += TEAMS;
+      if (slot >= S) { slot -= S; parity ^= 1; }
+      if (key0 >= end) {                                // no such keys
+        if (lane == 0) mbar_arrive(bar);
+        continue;
+      }
       // ---- S^T: 16 keys x 8 rows, even and odd steps apart (half the chain of dependent products)
       float s2[NB][2][4];
 #pragma unroll
@@ -244,13 +267,16 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
         }
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const uint32_t k[4] = {halves(lo[w]), halves(hi[w]), halves(lo[w] >> 16), halves(hi[w] >> 16)};
+          uint32_t k[4];
+          halves(lo[w], k[0], k[2]);
+          halves(hi[w], k[1], k[3]);
 #pragma unroll
           for (int t = 0; t < NB; ++t) mma_16x8x16(s2[t][w & 1], k, q[t][4 * j + w][0], q[t][4 * j + w][1]);
         }
       }
       float sk, sv;
-      asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(sk), "=f"(sv) : "r"(scales + stage * 8) : "memory");
+      sk = lds1(at_scale);
+      sv = lds1(at_scale + 16);
       uint32_t v[4][kWords];                            // keys 2c, 2c + 1, 2c + 8, 2c + 9
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -258,8 +284,8 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
         if constexpr (D == 128) lds128(sV + key * 128 + ((g ^ (key & 7)) << 4), v[j]);
         else lds64(sV + key * 64 + ((g >> 1 ^ (key >> 1 & 3)) << 4) + (g & 1) * 8, v[j]);
       }
-      __syncwarp();                                     // the stage is read: on to the block S further
-      fetch();
+      __syncwarp();                                     // the tile's part is read
+      if (lane == 0) mbar_arrive(bar);
       // ---- probabilities, as in the kernel above: the scale of V rides in the exponent
       sk = rest_e4m3::within_limits(sk);
       float log_v;
@@ -330,8 +356,11 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
       for (int w = 0; w < kWords; ++w) {
         const uint32_t ab = __byte_perm(v[0][w], v[1][w], 0x5140), cd = __byte_perm(v[2][w], v[3][w], 0x5140),
                        ef = __byte_perm(v[0][w], v[1][w], 0x7362), gh = __byte_perm(v[2][w], v[3][w], 0x7362);
-        const uint32_t x[4] = {halves(ab), halves(ab >> 16), halves(cd), halves(cd >> 16)};
-        const uint32_t z[4] = {halves(ef), halves(ef >> 16), halves(gh), halves(gh >> 16)};
+        uint32_t x[4], z[4];
+        halves(ab, x[0], x[1]);
+        halves(cd, x[2], x[3]);
+        halves(ef, z[0], z[1]);
+        halves(gh, z[2], z[3]);
 #pragma unroll
         for (int t = 0; t < NB; ++t) {
           mma_16x8x16(o[t][2 * w], x, pb[t][0], pb[t][1]);
@@ -350,22 +379,36 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
         for (int d = 4; d < 32; d <<= 1) l[t][j] += __shfl_xor_sync(0xFFFFFFFFu, l[t][j], d);
         if (g == 0) ml[warp * F::kRows + t * 8 + 2 * c + j] = make_float2(m[t][j], l[t][j]);
       }
-    __syncthreads();
+    meet();
+    // half of the warps leave their rows, the others add theirs and leave the sums
 #pragma unroll
-    for (int t = 0; t < NB; ++t)
+    for (int round = 0; round < 2; ++round) {
+      if ((warp >= F::kCopies) == (round == 0)) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int r = t * 8 + 2 * c + j;
-        float top = -INFINITY;
+        for (int t = 0; t < NB; ++t)
 #pragma unroll
-        for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w * F::kRows + r].x);
-        const float weight = m[t][j] == -INFINITY ? 0.f : ex2(m[t][j] - top);
-        // columns 2e, 2e + 1 of this lane's D / 8 stand at e * 16 + 2 g
-        float* to = reinterpret_cast<float*>(smem + F::kMerge) + (warp * F::kRows + r) * F::kRowStride + 2 * g;
+          for (int j = 0; j < 2; ++j) {
+            const int r = t * 8 + 2 * c + j;
+            float top = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e) *reinterpret_cast<float2*>(to + e * 16) = make_float2(o[t][e][j] * weight, o[t][e][2 + j] * weight);
+            for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w * F::kRows + r].x);
+            const float weight = m[t][j] == -INFINITY ? 0.f : ex2(m[t][j] - top);
+            // columns 2e, 2e + 1 of this lane's D / 8 stand at e * 16 + 2 g
+            float* to = reinterpret_cast<float*>(smem + F::kMerge) + (warp % F::kCopies * F::kRows + r) * F::kRowStride + 2 * g;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) {
+              float2 v = make_float2(o[t][e][j] * weight, o[t][e][2 + j] * weight);
+              if (round == 1) {
+                const float2 other = *reinterpret_cast<const float2*>(to + e * 16);
+                v.x += other.x;
+                v.y += other.y;
+              }
+              *reinterpret_cast<float2*>(to + e * 16) = v;
+            }
+          }
       }
-    __syncthreads();
+      meet();
+    }
     const int64_t w0 = ((int64_t)blockIdx.x * 2 + (p.t0 == 0 ? 1 : 0)) * a.rows;
     for (int r = warp; r < p.rows; r += W) {
       const int gg = lane & 7, part = lane >> 3;        // columns (D / 8) gg + (D / 32) part ...
@@ -378,6 +421,9 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
       for (int w = 0; w < W; ++w) {                     // (a maximum passes NaN over; the sum says so)
         const float2 v = ml[w * F::kRows + r];
         sum += v.y * (v.x == -INFINITY ? 0.f : ex2(v.x - top));
+      }
+#pragma unroll
+      for (int w = 0; w < F::kCopies; ++w) {
         const float* from = reinterpret_cast<const float*>(smem + F::kMerge) + (w * F::kRows + r) * F::kRowStride + 2 * gg;
 #pragma unroll
         for (int e = 0; e < D / 64; ++e) {
@@ -404,7 +450,7 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
       }
     }
     if (__builtin_expect(s_bad[piece & 7] == piece + 1, 0)) {             // (behind a barrier: all threads see the same)
-      __syncthreads();
+      meet();
       if (warp == 0) {
         const int r = lane;
         bool live = r < p.rows;
@@ -425,12 +471,7 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
       }
     }
   }
-  if (*abort_word != 0u || dead) {                      // giving up: let the copies in flight land before this block goes away
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    for (int i = max(0, issued - S); i < issued; ++i) mbar_wait(bars + (i % S) * 8, (uint32_t)((i / S) & 1));
-    if (lane == 0) atomicOr(&g_paged_error, 1u);
-  }
-  if (tid == 0 && share.x0 < share.x1) leave_unfinished<64, 1>(a, share, where.team, 0, ctl);
+  if (dead && lane == 0) atomicOr(&g_paged_error, 1u);
 }
 
 template <typename T, int D, int NB>

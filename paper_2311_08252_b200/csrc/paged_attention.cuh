@@ -198,21 +198,21 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
 
 __device__ unsigned int g_paged_error;                  // bit 0: wait gave up, bit 1: smem misaligned
 
-// SCALED: pages of e4m3 codes.  Their tiles arrive as they are, in rings of kRaw; the loaders widen them to
-// 16 bits into the operand rings, which are then shorter.
+// SCALED: pages of e4m3 codes.  Their tiles arrive as they are, in rings of kRaw; four more warps widen them to 16 bits
+// into the operand rings, which are shorter (16 warps of 128 registers: the softmax warps do with that).
 template <int D, int NT, bool SCALED> struct Shape {
   static constexpr int BN = 64;                         // keys per step
   static constexpr int kHalves = D / 64;
   static constexpr int kRows = 128 * NT;
   static constexpr int kQTile = 128 * D * 2, kTile = BN * D * 2;
-  static constexpr bool kTight = NT == 1 && D == 128;   // two blocks an SM have to fit
-  static constexpr int KS = SCALED ? (kTight ? 1 : 3) : kTight ? 2 : 4, VS = SCALED ? (kTight ? 2 : 3) : kTight ? 3 : 6;      // ring stages
-  static constexpr int kRaw = BN * D, RS = !SCALED ? 0 : kTight ? 2 : 4;  // bytes of codes, stages of each raw ring
+  static constexpr int KS = SCALED ? 3 : NT == 1 && D == 128 ? 2 : 4, VS = SCALED ? 3 : NT == 1 && D == 128 ? 3 : 6;      // ring stages
+  static constexpr int kRaw = BN * D, RS = SCALED ? 4 : 0;                // bytes of codes, stages of each raw ring
   static constexpr int kRings = NT * kQTile + (KS + VS) * kTile;
   static constexpr int kBars = kRings + 2 * RS * kRaw;                    // barriers behind the tiles
-  static constexpr int kScales = 576 + RS * 32, kSmem = kBars + (SCALED ? kScales + 384 : 512);
+  static constexpr int kSmem = kBars + (SCALED ? 1280 : 512);
   static constexpr int kSoftmax = 4 * NT;               // softmax warps; then K loader, V loader, MMA warps
-  static constexpr int kThreads = 32 * (kSoftmax + 2 + NT);
+  static constexpr int kWiden = SCALED ? 4 : 0;         // and those that widen
+  static constexpr int kThreads = 32 * (kSoftmax + 2 + NT + kWiden);
   static constexpr uint32_t kTmem = NT == 1 ? 256 : 512;
   static constexpr uint32_t kColO = 2 * NT * BN;        // behind two S buffers for each row tile
 };
@@ -221,9 +221,10 @@ enum {
   kKFull = 0, kKFree = 32, kVFull = 64, kVFree = 112, kSFull = 160, kPFull = 192, kOFull = 224, kQFull = 240, kQFree = 248,
   kTmemSlot = 256, kAbort = 260, kBad = 264 /* 8 x 4 */, kStartB = 296, kStartOff = 304, kTotal = 312,
   kScan = 320 /* 12 x 8 */, kJoin = 416, kTurn = 424 /* 8 x 8 */, kStartLeft = 488,
-  // pages of codes: raw tiles' barriers (K, V), their scales as they come, and as the softmax warps want them
+  // pages of codes: the raw tiles' barriers (K, V), their scales as they come, and as the softmax warps want them
   // (of each 16 keys: what K's makes of a raw score, in log2 units; the logarithm of V's; one over it)
-  kRawFull = 512 /* 2 x 4 x 8 */, kRawScales = 576 /* RS x 8 x 4, then 8 x 48 of Shape::kScales */
+  kRawFull = 512 /* 2 x 4 x 8 */, kRawFree = 576 /* 2 x 4 x 8 */, kRawScales = 640 /* 4 x 8 x 4 */, kScales = 768 /* 8 x 48 */,
+  kScanWide = 1152 /* 16 x 8 */
 };
 
 // Bounded wait of a whole warp, with one result for all lanes (TMEM accesses and elected lanes need
@@ -494,18 +495,18 @@ __device__ __forceinline__ void leave_unfinished(const Args& a, const Share& sha
   a.meta[blockIdx.x] = m;
 }
 
-// One raw tile of codes -> an operand tile of type T in the 128-byte-swizzled layout, by a warp.  A lane takes 16
+// 16 rows of a raw tile of codes -> an operand tile of type T in the 128-byte-swizzled layout, by a warp.  A lane takes 16
 // codes of a row and writes two 16-byte chunks; lanes of the second half of the head write theirs the other way round, so
 // that the eight lanes of a phase meet different banks.  CHECK: NaN codes become 0; true in a lane that found one in
 // rows below `rows`.
 template <typename T, int D, int BN, bool CHECK>
-__device__ __forceinline__ bool widen(uint32_t raw, uint32_t tile, int rows = 0) {
+__device__ __forceinline__ bool widen(uint32_t raw, uint32_t tile, int row0, int rows = 0) {
   bool found = false;
   const int lane = threadIdx.x & 31;
   constexpr int kLanes = D / 16;
-#pragma unroll 4
-  for (int i = 0; i < BN * kLanes / 32; ++i) {
-    const int u = i * 32 + lane, row = u / kLanes, chunk = u % kLanes, half = chunk >> 2;
+#pragma unroll
+  for (int i = 0; i < 16 * kLanes / 32; ++i) {
+    const int u = row0 * kLanes + i * 32 + lane, row = u / kLanes, chunk = u % kLanes, half = chunk >> 2;
     uint32_t w[4], y[8];
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(raw + u * 16) : "memory");
     if constexpr (CHECK) {
@@ -535,6 +536,12 @@ __device__ __forceinline__ bool widen(uint32_t raw, uint32_t tile, int rows = 0)
     }
   }
   return found;
+}
+// a box's scales: 4 bytes for each 16 keys; none of them (zeros) where `bytes` is 0
+__device__ __forceinline__ void copy_scales(int box_log, uint32_t to, const float* from, int bytes) {
+  if (box_log == 6) asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+  else if (box_log == 5) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ float lds1(uint32_t at) {
   float v;
@@ -605,8 +612,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     return;                     // uniform over the grid: every block sees the same offset
   }
   if (tid == 0) {
-    for (int i = 0; i < KS; ++i) { mbar_init(bars + kKFull + 8 * i, 1); mbar_init(bars + kKFree + 8 * i, NT); }
-    for (int i = 0; i < VS; ++i) { mbar_init(bars + kVFull + 8 * i, 1); mbar_init(bars + kVFree + 8 * i, NT); }
+    for (int i = 0; i < KS; ++i) { mbar_init(bars + kKFull + 8 * i, SCALED ? 4 : 1); mbar_init(bars + kKFree + 8 * i, NT); }
+    for (int i = 0; i < VS; ++i) { mbar_init(bars + kVFull + 8 * i, SCALED ? 4 : 1); mbar_init(bars + kVFree + 8 * i, NT); }
     for (int i = 0; i < 4; ++i) {
       mbar_init(bars + kSFull + 8 * i, 1);
       mbar_init(bars + kPFull + 8 * i, 4);              // one arrival per softmax warp
@@ -615,7 +622,12 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       mbar_init(bars + kOFull + 8 * i, 1);
     }
     if constexpr (SCALED)
-      for (int i = 0; i < 2 * S_::RS; ++i) mbar_init(bars + kRawFull + 8 * (i / S_::RS * 4 + i % S_::RS), 1);
+      for (int i = 0; i < S_::RS; ++i) {                // (with K's tiles come the scales, of both)
+        mbar_init(bars + kRawFull + 8 * i, 1 + (64 >> min(a.page_log, 6)));
+        mbar_init(bars + kRawFull + 32 + 8 * i, 1);
+        mbar_init(bars + kRawFree + 8 * i, S_::kWiden);
+        mbar_init(bars + kRawFree + 32 + 8 * i, S_::kWiden);
+      }
     mbar_init(bars + kQFull, 1);
     mbar_init(bars + kQFree, NT);                       // one arrival per row tile
     mbar_init(bars + kJoin, S_::kSoftmax);
@@ -633,7 +645,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   // ---- this team's share of the flat tile list
-  const Share share = find_share<BN, NT, S_::kThreads>(a, where, row0, ctl, ctl + kScan);
+  const Share share = find_share<BN, NT, S_::kThreads>(a, where, row0, ctl, ctl + (SCALED ? kScanWide : kScan));
   const long long x0 = share.x0, x1 = share.x1;
   tc_fence_before();
   __syncthreads();
@@ -642,8 +654,60 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
   Walk<BN, S_::kRows> walk(a, *reinterpret_cast<int*>(ctl + kStartB), *reinterpret_cast<long long*>(ctl + kStartOff),
                            x0 < x1 ? *reinterpret_cast<long long*>(ctl + kStartLeft) : 0ll, rb);
   Piece p;
-
-  if (warp == S_::kSoftmax || warp == S_::kSoftmax + 1) {
+  if (SCALED && warp >= S_::kSoftmax + 2 + NT) {
+    // ------------------------------------------------------------------ the warps that widen: 16 rows of every tile each
+    constexpr int RS = S_::RS;
+    const int me = warp - (S_::kSoftmax + 2 + NT);
+    const uint32_t raw = sbase + S_::kRings;
+    int stage = 0, slot = 0, n = 0, piece = 0;
+    uint32_t full_parity = 0, free_parity = 1;          // (fresh operand slots count as free)
+    bool ok = true;
+    while (ok && walk.next(p)) {
+      ++piece;
+      int clear0, clear1;
+      clear_tiles<BN>(a, p, clear0, clear1);
+      for (int it = 0; it < p.len; ++it, ++n) {
+        ok = wait_warp(bars + kRawFull + stage * 8, full_parity, abort_word) &&
+             (n < KS || wait_warp(bars + kKFree + slot * 8, free_parity, abort_word));
+        if (!ok) break;
+        widen<T, D, BN, false>(raw + stage * S_::kRaw, sK + slot * S_::kTile, me * 16);
+        if (me == 0 && lane < 8) {                      // K's scales of 16 keys each, then V's
+          float* to = reinterpret_cast<float*>(ctl + kScales + (n & 7) * 48);
+          const float s = rest_e4m3::within_limits(lds1(bars + kRawScales + stage * 32 + lane * 4));
+          if (lane < 4) {                               // (kept above 0 and finite: a masked score of -infinity stays it)
+            to[lane] = fminf(fmaxf(s * a.scale_log2, 0x1p-126f), 0x1p127f);
+          } else {
+            to[lane] = log2f(s);
+            to[lane + 4] = 1.f / s;
+          }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(bars + kKFull + slot * 8); mbar_arrive(bars + kRawFree + stage * 8); }
+        ok = wait_warp(bars + kRawFull + 32 + stage * 8, full_parity, abort_word) &&
+             (n < VS || wait_warp(bars + kVFree + slot * 8, free_parity, abort_word));
+        if (!ok) break;
+        // NaN in tiles that not every row sees whole would reach rows that do not see its key (0 x NaN): it is taken
+        // out, and the piece remembered if the key exists (the epilogue puts in what it comes to).  Elsewhere it
+        // stays and shows in O.  No tile is widened more than a few ahead, so eight pieces are told apart.
+        if (it >= clear0 && it < clear1) {
+          widen<TV, D, BN, false>(raw + (RS + stage) * S_::kRaw, sV + slot * S_::kTile, me * 16);
+        } else {
+          const int rows = p.c.L + p.c.n - tile_key<BN>(p.c, p.t0 + it);
+          if (widen<TV, D, BN, true>(raw + (RS + stage) * S_::kRaw, sV + slot * S_::kTile, me * 16, rows)) {
+            s_bad[piece & 7] = piece + 1;
+            __threadfence_block();
+          }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(bars + kVFull + slot * 8); mbar_arrive(bars + kRawFree + 32 + stage * 8); }
+        static_assert(!SCALED || KS == VS, "one slot number for both rings");
+        if (++stage == RS) { stage = 0; full_parity ^= 1; }
+        if (++slot == KS) { slot = 0; free_parity ^= 1; }
+      }
+    }
+  } else if (warp == S_::kSoftmax || warp == S_::kSoftmax + 1) {
     // ------------------------------------------------------------------ K loader, V loader
     const bool is_v = warp == S_::kSoftmax + 1;
     const int stages = is_v ? VS : KS;
@@ -653,102 +717,59 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     const int pg = lane / kHalves, half = lane % kHalves;               // (16-bit pages)
     const bool active = pg * box < BN;
     if constexpr (SCALED) {
-      // Tiles are fetched RS ahead and widened in order; the walk of the fetches is its own.
+      // A lane has a box (a page, or 64 rows of a larger one), so a warp works out the addresses of 8 to 32 tiles at once;
+      // then it goes through them, and only waits and starts copies.
       constexpr int RS = S_::RS;
-      const uint32_t raw = sbase + S_::kRings + (is_v ? RS * S_::kRaw : 0), raw_full = bars + kRawFull + (is_v ? 32 : 0);
-      const bool fetches = lane * box < BN;             // a lane a page
-      Walk<BN, S_::kRows> ahead = walk;
-      Piece pa;
-      int at = 0, row = 0, page = -1, issued = 0, done = 0;
-      bool more = ahead.next(pa), ok = true;
-      auto find = [&]() {
-        row = tile_key<BN>(pa.c, pa.t0 + at) + lane * box;
-        const int col = row >> a.page_log;
-        page = fetches && col < a.table_cols ? __ldg(a.table + pa.b * a.table_stride + col) : -1;
-      };
-      auto fetch = [&]() {
-        if (more) {
-          const int stage = issued % RS;
-          if (page < 0 || page >= a.P) page = a.P;      // outside the map: reads as zeros
-          if (lane == 0) mbar_expect_tx(raw_full + stage * 8, (uint32_t)S_::kRaw);
-          __syncwarp();
-          if (fetches)
-            tma_page(raw + stage * S_::kRaw + lane * (box * D), map, 0, row & ((1 << a.page_log) - 1), pa.hk, page, a.slot,
-                     raw_full + stage * 8);
-          if (!is_v) {                                  // lanes 0 ... 3: K's scales of 16 keys each, 4 ... 7: V's
-            const int first = (lane & 3) * 16, holder = first / box;
-            const int pg_ = __shfl_sync(0xFFFFFFFFu, page, holder), row_ = __shfl_sync(0xFFFFFFFFu, row, holder) + first - holder * box;
-            const int64_t cell = ((int64_t)pg_ * a.H_kv + pa.hk) * (1 << (a.page_log - 4)) + ((row_ & ((1 << a.page_log) - 1)) >> 4);
-            const float* from = lane < 4 ? a.k_scales : a.v_scales;
-            const int bytes = pg_ < a.P ? 4 : 0;        // (else 0, which counts as the least scale)
-            if (lane < 8)
-              asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;"
-                  ::"r"(bars + kRawScales + stage * 32 + lane * 4), "l"(bytes ? from + cell : from), "r"(bytes) : "memory");
-          }
-          ++issued;
-          if (++at == pa.len) { more = ahead.next(pa); at = 0; }
-          if (more) find();
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");          // (empty ones too: they are counted)
-      };
-      if (more) find();
-      for (int i = 0; i < RS; ++i) fetch();
-      uint32_t pieces = 0;
+      const uint32_t raw = sbase + S_::kRings + (is_v ? RS * S_::kRaw : 0), raw_full = bars + kRawFull + (is_v ? 32 : 0),
+                     raw_free = bars + kRawFree + (is_v ? 32 : 0);
+      const int box_log = min(a.page_log, 6), boxes_log = 6 - box_log, mine = lane >> boxes_log, at_once = 32 >> boxes_log;
+      const int box0 = (lane & ((1 << boxes_log) - 1)) << box_log;        // the box's first row in its tile
+      int stage = 0, issued = 0;
+      uint32_t parity = 1, pieces = 0;                  // a fresh ring's stages count as free
+      bool ok = true;
       while (ok && walk.next(p)) {
-        int clear0, clear1;
-        clear_tiles<BN>(a, p, clear0, clear1);
-        for (int it = 0; ok && it < p.len; ++it) {
-          if (is_v && it == 0) {                        // the piece's Q; every tile before it is widened
-            if (pieces > 0) ok = wait_warp(bars + kQFree, (pieces - 1) & 1, abort_word);
+        for (int it0 = 0; ok && it0 < p.len; it0 += at_once) {
+          const int row = tile_key<BN>(p.c, p.t0 + min(it0 + mine, p.len - 1)) + box0, col = row >> a.page_log;
+          int page = col < a.table_cols ? __ldg(a.table + p.b * a.table_stride + col) : -1;
+          if (page < 0 || page >= a.P) page = a.P;      // outside the map: reads as zeros
+          const int in_page = row & ((1 << a.page_log) - 1), bytes = page < a.P ? 1 << (box_log - 2) : 0;
+          // (without a page a scale of 0, which counts as the least)
+          const int64_t cell = bytes ? (((int64_t)page * a.H_kv + p.hk) << (a.page_log - 4)) + (in_page >> 4) : 0;
+          const int n = min(at_once, p.len - it0);
+          for (int j = 0; j < n; ++j) {
+            if (issued >= RS) ok = wait_warp(raw_free + stage * 8, parity, abort_word);
             if (!ok) break;
-            ++pieces;
-            load_q<T, D, NT, C>(a, p, rb, sQ, lane);
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_async_smem();
+            if (mine == j) {
+              const uint32_t bar = raw_full + stage * 8;
+              if (box0 == 0) mbar_expect_tx(bar, (uint32_t)S_::kRaw);
+              tma_page(raw + stage * S_::kRaw + box0 * D, map, 0, in_page, p.hk, page, a.slot, bar);
+              if (!is_v) {                              // 16 bytes of either's scales for 64 keys
+                const uint32_t to = bars + kRawScales + stage * 32 + (box0 >> 2);
+                copy_scales(box_log, to, a.k_scales + cell, bytes);
+                copy_scales(box_log, to + 16, a.v_scales + cell, bytes);
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+              }
+            }
             __syncwarp();
-            if (lane == 0) mbar_arrive(bars + kQFull);
-          }
-          const int stage = done % RS, slot = done % stages;
-          ok = wait_warp(raw_full + stage * 8, (done / RS) & 1, abort_word) &&
-               (done < stages || wait_warp(free_ + slot * 8, (done / stages - 1) & 1, abort_word));
-          if (!ok) break;
-          if (is_v) {
-            // NaN in tiles that not every row sees whole would reach rows that do not see its key (0 x NaN): it is taken
-            // out, and the piece remembered if the key exists (the epilogue puts in what it comes to).  Elsewhere it
-            // stays and shows in O.  The next piece's tiles come behind its Q, so eight pieces are told apart.
-            if (it >= clear0 && it < clear1) {
-              widen<TV, D, BN, false>(raw + stage * S_::kRaw, ring + slot * S_::kTile);
-            } else {
-              const int rows = p.c.L + p.c.n - tile_key<BN>(p.c, p.t0 + it);
-              if (widen<TV, D, BN, true>(raw + stage * S_::kRaw, ring + slot * S_::kTile, rows)) {
-                s_bad[pieces & 7] = (int)pieces + 1;
-                __threadfence_block();
-              }
-            }
-          } else {
-            widen<T, D, BN, false>(raw + stage * S_::kRaw, ring + slot * S_::kTile);
-            asm volatile("cp.async.wait_group %0;" ::"n"(RS - 1) : "memory");
-            if (lane < 8) {
-              float* to = reinterpret_cast<float*>(ctl + S_::kScales + (done & 7) * 48);
-              const float s = rest_e4m3::within_limits(*reinterpret_cast<volatile float*>(ctl + kRawScales + stage * 32 + lane * 4));
-              if (lane < 4) {                           // (kept above 0 and finite: a masked score of -infinity stays it)
-                to[lane] = fminf(fmaxf(s * a.scale_log2, 0x1p-126f), 0x1p127f);
-              } else {
-                to[lane] = log2f(s);
-                to[lane + 4] = 1.f / s;
-              }
+            ++issued;
+            if (++stage == RS) { stage = 0; parity ^= 1; }
+            // The piece's Q, behind the first tiles (which do not wait for it): the last piece's S has to be done with it.
+            if (is_v && it0 + j + 1 == min(RS, p.len)) {
+              if (pieces > 0) ok = wait_warp(bars + kQFree, (pieces - 1) & 1, abort_word);
+              if (!ok) break;
+              ++pieces;
+              load_q<T, D, NT, C>(a, p, rb, sQ, lane);
+              asm volatile("cp.async.wait_all;" ::: "memory");
+              fence_async_smem();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bars + kQFull);
             }
           }
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(full + slot * 8);
-          ++done;
-          fetch();
         }
       }
       if (*abort_word != 0u) {                          // as below
         asm volatile("cp.async.wait_all;" ::: "memory");
-        for (int i = done; i < issued; ++i) mbar_wait(raw_full + (i % RS) * 8, (uint32_t)((i / RS) & 1));
+        for (int i = max(0, issued - RS); i < issued; ++i) mbar_wait(raw_full + (i % RS) * 8, (uint32_t)((i / RS) & 1));
       }
     } else {
       int slot = 0, filled = 0;
@@ -977,7 +998,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           // 2^(score + log2 s_v - reference) and the sum of the probabilities takes it out again, 16 keys at a time.
           float ka[kParts], log_v[kParts], inv_v[kParts];
           if constexpr (SCALED) {
-            const uint32_t at = bars + S_::kScales + ((base + it) & 7) * 48 + ci * kParts * 4;
+            const uint32_t at = bars + kScales + ((base + it) & 7) * 48 + ci * kParts * 4;
             if constexpr (kParts == 4) {
               const float4 k4 = lds4(at), l4 = lds4(at + 16), i4 = lds4(at + 32);
               ka[0] = k4.x; ka[1] = k4.y; ka[2] = k4.z; ka[3] = k4.w;

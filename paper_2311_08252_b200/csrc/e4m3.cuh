@@ -19,19 +19,7 @@ __device__ __forceinline__ float fitting_scale(float most) {
 }
 __device__ __forceinline__ float within_limits(float s) { return fminf(fmaxf(s, kLeastScale), kMostScale); }   // NaN: the least
 
-// x / s for the rows of a block: a product where s is a power of two (exact, and what fitting_scale gives)
-struct Quotient {
-  float s, inverse;
-  bool exact;
-  __device__ __forceinline__ explicit Quotient(float s_) {
-    s = s_;
-    inverse = 1.f / s_;
-    exact = (__float_as_uint(s_) & 0x7FFFFFu) == 0;
-  }
-  __device__ __forceinline__ float operator()(float x) const { return exact ? x * inverse : x / s; }
-};
-
-// two codes, the first in the low byte; what is not finite becomes NaN
+// two codes, the first in the low byte; NaN stays NaN, what is beyond 448 becomes 448
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
 }

@@ -4,10 +4,10 @@
 //
 // Pair f of a row at position p turns by the angle t = p * inv_freq[f]:
 //   y1 = a (x1 cos t - x2 sin t), y2 = a (x2 cos t + x1 sin t).
-// t is a product in 64 bits (exact up to p = 2^29) and its sine and cosine are taken in 64 bits: in 32 bits
-// the angle of position 10^6 would be 0.03 off.  Queries and 16-bit keys are then rotated in 32 bits and
-// rounded once.  Keys that become codes are rotated in 64 bits: the border between two codes decides a whole step
-// of 2^-4, so that a result a rounding off would now and then be a code off.
+// t is a product in 64 bits (exact up to p = 2^29): in 32 bits the angle of position 10^6 would be 0.03 off.  For queries
+// and 16-bit keys whole quarter turns are taken off it in 64 bits; the rest's sine and cosine and the rotation are in 32 bits,
+// rounded once.  Keys that become codes are rotated in 64 bits throughout: the border between two codes decides a whole
+// step of 2^-4, so that a result a rounding off would now and then be a code off.
 //
 // Pages with scales: the 16 rows of a block share a scale per head, the smallest power of two that holds the largest new
 // value, and never less than before where the block has older rows; those are requantised when it grows
@@ -35,6 +35,7 @@ using namespace rest_pool;
 using namespace rest_e4m3;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr double kQuarterTurns = 0.63661977236758134308;  // 2 / pi
 enum Where { kNowhere, kPages16, kPagesScaled };        // where keys and values go
 
 struct Args {
@@ -45,7 +46,7 @@ struct Args {
   int64_t q_b, q_n, q_h, o_b, o_n, o_h, n_b, n_n, n_h;  // in elements
   const int32_t *kv_len, *n_nodes, *pos;
   const float* inv_freq;
-  int N, H, H_kv, D, half, groups, interleaved;
+  int N, H, H_kv, D, half, groups, interleaved, code_parts;
   float amplitude;
 };
 
@@ -104,18 +105,17 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float* 
 }
 template <typename T> __device__ __forceinline__ float load1(const T* p) { return (float)*p; }
 
-// A lane's 16 elements of a row, in two runs of 8 from at[0] and at[1].  PAIRS: a pair's halves lie in the same place
-// of both runs (half the head apart); NEIGHBOURS: pairs are neighbours, or the run is not rotated at all; LOOSE: pairs
-// half the head apart that runs of 8 do not meet (partners are loaded one by one).
-enum Kind { kPairs, kNeighbours, kLoose };
+// A lane's 16 elements of a row, in two runs of 8 from at[0] and at[1].  kPairs: a pair's halves lie in the same place
+// of both runs (half the head apart); kNeighbours: pairs are neighbours; kStill: nothing turns; kLoose: runs of 8 do not
+// meet their partners, or some pairs turn and some do not (elements are worked out one by one).
+enum Kind { kPairs, kNeighbours, kStill, kLoose };
 struct Lane { Kind kind; int at[2], first; };           // first: of kPairs and kNeighbours, the first pair's number
 __device__ __forceinline__ Lane lane_of(const Args& a, int chunk) {
-  if (a.interleaved || a.half == 0) return {kNeighbours, {16 * chunk, 16 * chunk + 8}, 8 * chunk};
-  if (a.half & 7) return {kLoose, {16 * chunk, 16 * chunk + 8}, 0};
-  const int pairs = a.half >> 3;
-  if (chunk < pairs) return {kPairs, {8 * chunk, a.half + 8 * chunk}, 8 * chunk};
-  const int at = 16 * chunk;                            // behind the rotated part
-  return {kNeighbours, {at, at + 8}, a.half};
+  const int at = 16 * chunk, pairs = a.half >> 3;
+  if (at >= 2 * a.half && !(a.half & 7)) return {kStill, {at, at + 8}, 0};
+  if (a.half & 7) return {at >= 2 * a.half ? kStill : kLoose, {at, at + 8}, 0};
+  if (a.interleaved) return {kNeighbours, {at, at + 8}, 8 * chunk};
+  return chunk < pairs ? Lane{kPairs, {8 * chunk, a.half + 8 * chunk}, 8 * chunk} : Lane{kStill, {at, at + 8}, 0};
 }
 // Where pair f of row r has its cosine and sine.  Lanes next to one another read pairs 8 apart, so of each eight the
 // twos are laid out apart: 16-byte reads without bank conflicts.
@@ -124,42 +124,75 @@ __device__ __forceinline__ int table_at(const Args& a, int r, int f) {
   return r * a.half + ((a.half & 7) ? f : ((((f >> 1) & 3) * eighths + (f >> 3)) << 1 | (f & 1)));
 }
 
-// cosines and sines of a lane's eight pairs (behind the last pair, not used)
+// cosines and sines of a lane's eight pairs
 template <typename F2, typename F> struct Angles {
   F c[8], s[8];
   __device__ __forceinline__ void load(const Args& a, const Lane& l, const F2* table, int r) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      c[j] = 1;
-      s[j] = 0;
-      if (l.first + j < a.half) {
-        const F2 cs = table[table_at(a, r, l.first + j)];
-        c[j] = cs.x;
-        s[j] = cs.y;
-      }
+      const F2 cs = table[table_at(a, r, l.first + j)];
+      c[j] = cs.x;
+      s[j] = cs.y;
     }
   }
 };
-// The rotated elements y of a lane from x, of which the first `pairs` pairs turn; `round` makes what is stored of each.
-template <typename A, typename F, typename R>
-__device__ __forceinline__ void rotate(Kind kind, int pairs, const A& t, const float (&x)[16], float (&y)[16], R round) {
+// The rotated elements y of a lane from x; `round` makes what is stored of each.
+template <bool NEIGHBOURS, typename A, typename F, typename R>
+__device__ __forceinline__ void rotate(const A& t, const float (&x)[16], float (&y)[16], R round) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const F c = t.c[j], s = t.s[j];
-    const F x1 = kind == kPairs ? x[j] : x[2 * j], x2 = kind == kPairs ? x[8 + j] : x[2 * j + 1];
-    const bool turns = j < pairs;                       // (1 and 0 would make NaN of what stands next to an infinity)
-    const float y1 = round(turns ? fma(x1, c, -(x2 * s)) : x1), y2 = round(turns ? fma(x2, c, x1 * s) : x2);
-    if (kind == kPairs) { y[j] = y1; y[8 + j] = y2; } else { y[2 * j] = y1; y[2 * j + 1] = y2; }
+    constexpr int kApart = NEIGHBOURS ? 1 : 8, kStep = NEIGHBOURS ? 2 : 1;
+    const F c = t.c[j], s = t.s[j], x1 = x[kStep * j], x2 = x[kStep * j + kApart];
+    y[kStep * j] = round(fma(x1, c, -(x2 * s)));
+    y[kStep * j + kApart] = round(fma(x2, c, x1 * s));
   }
 }
 // one element of a row whose pairs are loose
 template <typename F, typename F2, typename T>
 __device__ __forceinline__ F loose(const Args& a, const T* row, int e, float x, const F2* table, int r) {
   if (e >= 2 * a.half) return x;
-  const bool low = e < a.half;
-  const F2 cs = table[table_at(a, r, low ? e : e - a.half)];
-  const F other = load1(row + (low ? e + a.half : e - a.half));
+  const bool low = a.interleaved ? !(e & 1) : e < a.half;
+  const F2 cs = table[table_at(a, r, a.interleaved ? e >> 1 : low ? e : e - a.half)];
+  const F other = load1(row + (a.interleaved ? e ^ 1 : low ? e + a.half : e - a.half));
   return low ? fma((F)x, cs.x, -(other * cs.y)) : fma((F)x, cs.x, other * cs.y);
+}
+
+// A lane's 16 elements of a new row as they become codes: rotated in 64 bits, rounded to 32.
+template <typename T, typename R>
+__device__ __forceinline__ void code_values(const Args& a, const T* row, const Lane& l, const double2* table, int r, float (&y)[16], R round) {
+  float x[16];
+  load8(row + l.at[0], x);
+  load8(row + l.at[1], x + 8);
+  if (l.kind == kStill) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) y[j] = x[j];
+  } else if (l.kind == kLoose) {
+#pragma unroll 1
+    for (int j = 0; j < 16; ++j) y[j] = round(loose<double>(a, row, l.at[0] + j, x[j], table, r));
+  } else {
+    Angles<double2, double> t;
+    t.load(a, l, table, r);
+    if (l.kind == kPairs) rotate<false, Angles<double2, double>, double>(t, x, y, round);
+    else rotate<true, Angles<double2, double>, double>(t, x, y, round);
+  }
+}
+// The largest finite magnitude of a lane's values, those in 64 bits rounded up; only asked for where it matters (below).
+template <typename T, int D>
+__device__ __noinline__ float largest_rounded_up(const Args& a, const T* row, bool turn, const double2* table, int rows) {
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes;
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes;
+  const Lane l = turn ? lane_of(a, chunk) : Lane{kStill, {16 * chunk, 16 * chunk + 8}, 0};
+  float most = 0.f, y[16];
+  for (int r = sub; r < rows; r += kRows) {
+    code_values(a, row + r * a.n_n, l, table, r, y, [&](double v) {
+      const float up = __double2float_ru(fabs(v));
+      most = fmaxf(most, up < INFINITY ? up : 0.f);
+      return __double2float_rn(v);
+    });
+#pragma unroll
+    for (int j = 0; j < 16; ++j) most = fmaxf(most, fabsf(y[j]) < INFINITY ? fabsf(y[j]) : 0.f);
+  }
+  return most;
 }
 
 // One head's keys or values of a block of 16 rows: a warp.  Rows lo .. hi - 1 of the block are new, `row` is the first
@@ -169,46 +202,26 @@ __device__ __forceinline__ void write_codes(const Args& a, const T* row, bool tu
                                             unsigned char* codes, int64_t code_row, float* scale) {
   constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = 16 / kRows;
   const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes;
-  const Lane l = turn ? lane_of(a, chunk) : Lane{kNeighbours, {16 * chunk, 16 * chunk + 8}, a.half};
+  const Lane l = turn ? lane_of(a, chunk) : Lane{kStill, {16 * chunk, 16 * chunk + 8}, 0};
   const float old = lo > 0 ? within_limits(*scale) : 0.f;
   float y[kSteps][16], most = 0.f;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const int r = lo + i * kRows + sub;
-    if (r < hi) {
-      float x[16];
-      load8(row + (r - lo) * a.n_n + l.at[0], x);
-      load8(row + (r - lo) * a.n_n + l.at[1], x + 8);
-      // what is not finite becomes NaN and has no part in the scale; the largest value is rounded up, so that 64 bits
-      // just above 448 times a power of two count as more than that
-      auto round = [&](double v) -> float {
-        const float up = __double2float_ru(fabs(v)), f = __double2float_rn(v);
-        const bool fine = up < INFINITY;
-        most = fmaxf(most, fine ? up : 0.f);
-        return fine ? f : NAN;
-      };
-      auto as_is = [&](float f) -> float {
-        const bool fine = fabsf(f) < INFINITY;
-        most = fmaxf(most, fine ? fabsf(f) : 0.f);
-        return fine ? f : NAN;
-      };
-      if (!turn || (l.kind == kNeighbours && l.first >= a.half)) {
+    const int r = i * kRows + sub;
+    if (lo + r < hi) {
+      code_values(a, row + r * a.n_n, l, table, r, y[i], [](double v) { return __double2float_rn(v); });
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[i][j] = as_is(x[j]);
-      } else if (l.kind == kLoose) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          y[i][j] = round(loose<double>(a, row + (r - lo) * a.n_n, 16 * chunk + j, x[j], table, r - lo));
-      } else {
-        Angles<double2, double> t;
-        t.load(a, l, table, r - lo);
-        rotate<Angles<double2, double>, double>(l.kind, a.half - l.first, t, x, y[i], round);
-      }
+      for (int j = 0; j < 16; j += 2) most = fmaxf(most, fmaxf(fabsf(y[i][j]), fabsf(y[i][j + 1])));      // (NaN is passed over)
     }
   }
   most = warp_max(most);
+  // An infinity has no part in the scale; and 64 bits just above 448 times a power of two, which round to it, count as more.
+  const bool infinite = most == INFINITY;
+  if (infinite || (turn && (__float_as_uint(most) & 0x7FFFFFu) == 0x600000u))
+    most = warp_max(largest_rounded_up<T, D>(a, row, turn, table, hi - lo));
   const float need = fitting_scale(most), s = fmaxf(need, old);
-  const Quotient over(s);
+  const bool power = (__float_as_uint(s) & 0x7FFFFFu) == 0;               // (what fitting_scale gives: a product is exact)
+  const float inverse = 1.f / s;
   if (lo > 0 && s != old) {                             // older rows: the scale grew
     const float ratio = old / s;
 #pragma unroll
@@ -224,10 +237,20 @@ __device__ __forceinline__ void write_codes(const Args& a, const T* row, bool tu
   for (int i = 0; i < kSteps; ++i) {
     const int r = lo + i * kRows + sub;
     if (r < hi) {
+      if (infinite) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[i][j] = fabsf(y[i][j]) < INFINITY ? y[i][j] : NAN;
+      }
+      if (power) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[i][j] *= inverse;
+      } else {
+#pragma unroll 1
+        for (int j = 0; j < 16; ++j) y[i][j] /= s;
+      }
       uint32_t w[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        w[j] = pack2(over(y[i][4 * j]), over(y[i][4 * j + 1])) | pack2(over(y[i][4 * j + 2]), over(y[i][4 * j + 3])) << 16;
+      for (int j = 0; j < 4; ++j) w[j] = pack2(y[i][4 * j], y[i][4 * j + 1]) | pack2(y[i][4 * j + 2], y[i][4 * j + 3]) << 16;
       *reinterpret_cast<uint2*>(codes + r * code_row + l.at[0]) = make_uint2(w[0], w[1]);
       *reinterpret_cast<uint2*>(codes + r * code_row + l.at[1]) = make_uint2(w[2], w[3]);
     }
@@ -237,7 +260,7 @@ __device__ __forceinline__ void write_codes(const Args& a, const T* row, bool tu
 }
 
 template <typename T, Where W, int D_SCALED>
-__global__ void __launch_bounds__(kThreads) rest_kv_append_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, 2) rest_kv_append_kernel(const __grid_constant__ Args a) {
   grid_wait();
   extern __shared__ __align__(16) unsigned char smem[];
   const int b = blockIdx.x / a.groups, group = blockIdx.x % a.groups;
@@ -249,28 +272,36 @@ __global__ void __launch_bounds__(kThreads) rest_kv_append_kernel(const __grid_c
   const int m = min(n - i0, 16 - lo);
   if (m <= 0) return;
 
+  const int part = blockIdx.y;                          // some blocks write codes, the others rows
   float2* table = reinterpret_cast<float2*>(smem);
-  double2* table64 = reinterpret_cast<double2*>(table + 16 * a.half);
+  double2* table64 = reinterpret_cast<double2*>(smem);
   for (int e = threadIdx.x; e < m * a.half; e += kThreads) {
     const int r = e / a.half, f = e - r * a.half;
-    double s, c;
-    sincos((double)a.pos[(int64_t)b * a.N + i0 + r] * (double)a.inv_freq[f], &s, &c);
-    s *= a.amplitude;
-    c *= a.amplitude;
-    table[table_at(a, r, f)] = make_float2((float)c, (float)s);
-    if constexpr (W == kPagesScaled) table64[table_at(a, r, f)] = make_double2(c, s);
+    const double t = (double)a.pos[(int64_t)b * a.N + i0 + r] * (double)a.inv_freq[f];
+    if (W == kPagesScaled && part < a.code_parts) {
+      double s, c;
+      sincos(t, &s, &c);
+      table64[table_at(a, r, f)] = make_double2(a.amplitude * c, a.amplitude * s);
+    } else {
+      // what lies behind the whole quarter turns, at most an eighth of a turn, in 32 bits
+      const double quarters = t * kQuarterTurns, whole = rint(quarters);
+      float s, c;
+      sincospif(0.5f * (float)(quarters - whole), &s, &c);
+      const int q = (int)(long long)whole & 3;
+      const float cq = q & 1 ? s : c, sq = q & 1 ? c : s;
+      table[table_at(a, r, f)] = make_float2(a.amplitude * (q == 1 || q == 2 ? -cq : cq), a.amplitude * (q & 2 ? -sq : sq));
+    }
   }
   __syncthreads();
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t page_row = W == kNowhere || L < 0 || first > 0x7FFFFFFFu ? -1 : row_offset(a.c, b, (int)first);
-  const int parts = gridDim.y, part = blockIdx.y;
-  int heads = a.H;                                      // of q, then (16-bit pages) of K and V
   if constexpr (W == kPagesScaled) {
-    if (page_row >= 0) {
+    if (part < a.code_parts) {
+      if (page_row < 0) return;
       const int p = a.c.table[b * a.c.table_stride + (first >> a.c.page_log)];
       const int64_t cell = (int64_t)p * a.H_kv * (1 << (a.c.page_log - 4)) + ((first & ((1u << a.c.page_log) - 1)) >> 4);
-      for (int u = part * kWarps + warp; u < 2 * a.H_kv; u += parts * kWarps) {
+      for (int u = part * kWarps + warp; u < 2 * a.H_kv; u += a.code_parts * kWarps) {
         const int h = u >> 1;
         const bool v = u & 1;
         const T* row = static_cast<const T*>(v ? a.v_new : a.k_new) + b * a.n_b + i0 * a.n_n + h * a.n_h;
@@ -278,9 +309,8 @@ __global__ void __launch_bounds__(kThreads) rest_kv_append_kernel(const __grid_c
         write_codes<T, D_SCALED>(a, row, !v && a.half > 0, table64, lo, lo + m, codes, a.c.s_row * 16,
                                  (v ? a.v_scales : a.k_scales) + cell + (int64_t)h * (1 << (a.c.page_log - 4)));
       }
+      return;
     }
-  } else if constexpr (W == kPages16) {
-    heads += 2 * a.H_kv;
   }
 
   // rows of 16-bit (or 32-bit) results: D / 16 lanes a row; a lane stays with its row and steps through the heads
@@ -290,65 +320,91 @@ __global__ void __launch_bounds__(kThreads) rest_kv_append_kernel(const __grid_c
   const int together = all >= m ? all / m : 1;          // heads at a time
   if (all >= m && me >= together * m) return;
   const Lane l = lane_of(a, chunk);
-  const bool still = l.kind == kPairs ? false : l.kind == kLoose ? 16 * chunk >= 2 * a.half : l.first >= a.half;
   const int moving = min(lanes, (2 * a.half + 15) >> 4);        // lanes of a row of loose pairs that hold some
+  const int parts = gridDim.y - a.code_parts, h0 = (all >= m ? me / m : 0) + (part - a.code_parts) * together, step = together * parts;
   for (int r = all >= m ? me % m : me; r < m; r += all >= m ? m : all) {
     Angles<float2, float> t;
-    t.load(a, l, table, r);
-#pragma unroll 2
-    for (int h = (all >= m ? me / m : 0) + part * together; h < heads; h += together * parts) {
-      const T* from;
-      T* to;
-      bool turn = true;
-      if (W == kNowhere || h < a.H) {
-        from = static_cast<const T*>(a.q) + b * a.q_b + (i0 + r) * a.q_n + h * a.q_h;
-        to = static_cast<T*>(a.q_out) + b * a.o_b + (i0 + r) * a.o_n + h * a.o_h;
-      } else {
-        if (page_row < 0) break;
-        const bool v = h - a.H >= a.H_kv;
-        const int hk = h - a.H - (v ? a.H_kv : 0);
-        from = static_cast<const T*>(v ? a.v_new : a.k_new) + b * a.n_b + (i0 + r) * a.n_n + hk * a.n_h;
-        to = reinterpret_cast<T*>((v ? a.c.v : a.c.k) + page_row + hk * a.c.s_head + (lo + r) * a.c.s_row);
-        turn = !v;
+    if (l.kind == kPairs || l.kind == kNeighbours) t.load(a, l, table, r);
+    // one row in `count` heads
+    auto heads = [&](const T* from, int64_t from_h, T* to, int64_t to_h, int count, Kind kind) {
+      if (kind == kLoose) {
+        for (int h = h0; h < count; h += step) {
+          const T* x0 = from + h * from_h;
+          T* y0 = to + h * to_h;
+          float x[16], y[16];
+          load8(x0 + l.at[0], x);
+          load8(x0 + l.at[1], x + 8);
+#pragma unroll 1
+          for (int j = 0; j < 16; ++j) y[j] = loose<float>(a, x0, l.at[0] + j, x[j], table, r);
+          // a row may be rotated in place: all its lanes have loaded before the first stores
+          __syncwarp(((moving == 32 ? 0u : 1u << moving) - 1u) << (sub * lanes));
+          store8(y0 + l.at[0], y);
+          store8(y0 + l.at[1], y + 8);
+        }
+        return;
       }
-      Eight<T> e[2];
-      e[0].load(from + l.at[0]);
-      e[1].load(from + l.at[1]);
-      if (!turn || still) {
-        e[0].store(to + l.at[0]);
-        e[1].store(to + l.at[1]);
-        continue;
-      }
-      float x[16], y[16];
-      e[0].to(x);
-      e[1].to(x + 8);
-      if (l.kind == kLoose) {
+      constexpr int kAtOnce = sizeof(T) == 4 ? 2 : 4;   // heads on their way: 128 bytes a thread
+      from += h0 * from_h;
+      to += h0 * to_h;
+      from_h *= step;
+      to_h *= step;
+      for (int left = h0 < count ? (count - h0 + step - 1) / step : 0; left > 0; left -= kAtOnce, from += kAtOnce * from_h, to += kAtOnce * to_h) {
+        Eight<T> e[kAtOnce][2];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[j] = loose<float>(a, from, 16 * chunk + j, x[j], table, r);
-        // a row may be rotated in place: all its lanes have loaded before the first stores
-        __syncwarp(((moving == 32 ? 0u : 1u << moving) - 1u) << (sub * lanes));
-      } else {
-        rotate<Angles<float2, float>, float>(l.kind, a.half - l.first, t, x, y, [](float v) { return v; });
+        for (int i = 0; i < kAtOnce; ++i)
+          if (i < left) {
+            e[i][0].load(from + i * from_h + l.at[0]);
+            e[i][1].load(from + i * from_h + l.at[1]);
+          }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          if (i < left) {
+            T* y0 = to + i * to_h;
+            if (kind == kStill) {
+              e[i][0].store(y0 + l.at[0]);
+              e[i][1].store(y0 + l.at[1]);
+            } else {
+              float x[16], y[16];
+              e[i][0].to(x);
+              e[i][1].to(x + 8);
+              auto same = [](float v) { return v; };
+              if (kind == kPairs) rotate<false, Angles<float2, float>, float>(t, x, y, same);
+              else rotate<true, Angles<float2, float>, float>(t, x, y, same);
+              store8(y0 + l.at[0], y);
+              store8(y0 + l.at[1], y + 8);
+            }
+          }
       }
-      store8(to + l.at[0], y);
-      store8(to + l.at[1], y + 8);
+    };
+    if (a.H > 0)
+      heads(static_cast<const T*>(a.q) + b * a.q_b + (i0 + r) * a.q_n, a.q_h,
+            static_cast<T*>(a.q_out) + b * a.o_b + (i0 + r) * a.o_n, a.o_h, a.H, l.kind);
+    if (W == kPages16 && page_row >= 0) {
+      const int64_t new_row = b * a.n_b + (i0 + r) * a.n_n, to = page_row + (lo + r) * a.c.s_row;
+      heads(static_cast<const T*>(a.k_new) + new_row, a.n_h, reinterpret_cast<T*>(a.c.k + to), a.c.s_head * 8, a.H_kv, l.kind);
+      heads(static_cast<const T*>(a.v_new) + new_row, a.n_h, reinterpret_cast<T*>(a.c.v + to), a.c.s_head * 8, a.H_kv, kStill);
     }
   }
 }
 
 template <typename T, Where W, int D>
 rest_status run(const Args& a, int B, void* stream) {
-  // about two blocks an SM, eight warps each, where the rows alone do not give them: then the heads are shared out
+  // Blocks for about four waves of two an SM, so that the last wave is a small part; few rows share their heads out
+  // until a warp has one task.  Codes take about as long as twice the rows that they are made of.
   const int64_t blocks = (int64_t)B * a.groups;
   if (blocks > 0x7FFFFFFFll) return REST_UNSUPPORTED;
-  const int most = min(a.N, 16), rows = 32 / (a.D / 16);
-  const int warps = ((W == kPages16 ? a.H + 2 * a.H_kv : a.H) * most + rows - 1) / rows + (W == kPagesScaled ? 2 * a.H_kv : 0);
-  const int sms = rest::sm_count();
-  int64_t parts = 2 * (int64_t)(sms > 0 ? sms : 148) / blocks;
-  parts = parts < 1 ? 1 : parts;
-  if (parts > (warps + kWarps - 1) / kWarps) parts = (warps + kWarps - 1) / kWarps;
-  const size_t smem = (size_t)16 * a.half * (W == kPagesScaled ? 24 : 8);
-  REST_CUDA_TRY(launch(rest_kv_append_kernel<T, W, D>, dim3((unsigned)blocks, (unsigned)parts), kThreads, smem, stream, a));
+  const int sms = rest::sm_count(), most = min(a.N, 16), rows = 32 / (a.D / 16);
+  auto tasks = [](int warps) { return (warps + kWarps - 1) / kWarps; };
+  const int code_tasks = W == kPagesScaled ? tasks(2 * a.H_kv) : 0;
+  const int row_tasks = tasks(((W == kPages16 ? a.H + 2 * a.H_kv : a.H) * most + rows - 1) / rows);
+  const int64_t wanted = 8 * (int64_t)(sms > 0 ? sms : 148) / blocks;
+  auto parts = [&](int64_t share, int tasks_) { return (int)(share < 1 ? (tasks_ > 0) : share < tasks_ ? share : tasks_); };
+  Args args = a;
+  args.code_parts = parts(W == kPagesScaled && a.H > 0 ? wanted / 2 : wanted, code_tasks);
+  const int row_parts = parts(wanted - args.code_parts, row_tasks);
+  const size_t smem = (size_t)16 * a.half * (W == kPagesScaled ? 16 : 8);
+  REST_CUDA_TRY(launch(rest_kv_append_kernel<T, W, D>, dim3((unsigned)blocks, (unsigned)(args.code_parts + row_parts)), kThreads,
+                       smem, stream, args));
   return REST_OK;
 }
 

@@ -13,11 +13,11 @@
 // value, and never less than before where the block has older rows; those are requantised when it grows
 // (by a power of two, so they change only where they fall below the smallest code).
 //
-// A thread block takes the new rows of one context that fall into one block of 16 rows: their angles are
-// computed once, into shared memory, for all heads.  A row is D / 16 lanes, 16 elements each (a pair's halves sit in
-// the same lane), so that 64 bytes a thread are in flight; a lane keeps its row's sines and cosines in
-// registers over the heads.  A block of codes is a warp, which holds all its rows' values while it looks for the
-// largest.  What bounds it is HBM for many rows, and for few rows the launch and the chain length -> table -> page.
+// A thread block takes new rows of one context that fall into one block of 16 rows.  A row is D / 16 lanes, 16
+// elements each (a pair's halves sit in the same lane); a lane stays with its row, keeps its sines and cosines in
+// registers and steps through the heads, four of them on their way at a time.  A block of codes is a warp, which
+// holds all its rows' values while it looks for the largest; the angles of its thread block's rows are computed once,
+// into shared memory.  What bounds it is HBM for many rows, and for few rows the launch and the chain length -> table -> page.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -35,7 +35,8 @@ using namespace rest_pool;
 using namespace rest_e4m3;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr double kQuarterTurns = 0.63661977236758134308;  // 2 / pi
+constexpr double kQuarterTurns = 0.63661977236758134308, kQuarter = 1.57079632679489661923,      // 2 / pi, pi / 2
+                 kQuarterHigh = 0x1.921fb54400000p+0, kQuarterLow = 0x1.0b4611a626331p-34;
 enum Where { kNowhere, kPages16, kPagesScaled };        // where keys and values go
 
 struct Args {
@@ -46,7 +47,7 @@ struct Args {
   int64_t q_b, q_n, q_h, o_b, o_n, o_h, n_b, n_n, n_h;  // in elements
   const int32_t *kv_len, *n_nodes, *pos;
   const float* inv_freq;
-  int N, H, H_kv, D, half, groups, interleaved, code_parts;
+  int N, H, H_kv, D, half, groups, interleaved, parts, code_parts;
   float amplitude;
 };
 
@@ -117,7 +118,43 @@ __device__ __forceinline__ Lane lane_of(const Args& a, int chunk) {
   if (a.interleaved) return {kNeighbours, {at, at + 8}, 8 * chunk};
   return chunk < pairs ? Lane{kPairs, {8 * chunk, a.half + 8 * chunk}, 8 * chunk} : Lane{kStill, {at, at + 8}, 0};
 }
-// Where pair f of row r has its cosine and sine.  Lanes next to one another read pairs 8 apart, so of each eight the
+// Cosine and sine of pair f of a row at position p, times the amplitude, in 32 bits: whole quarter turns are taken off in
+// 64, and what is left, |x| <= pi / 4, goes through the Taylor series, whose next terms are below 2^-29 (x^11 / 11!,
+// x^12 / 12!).
+__device__ __forceinline__ float2 turn_of(const Args& a, double p, int f) {
+  const double quarters = p * (double)a.inv_freq[f] * kQuarterTurns, whole = rint(quarters);
+  const float x = (float)((quarters - whole) * kQuarter), z = x * x;
+  const float s = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), x);
+  const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+  const int q = (int)(long long)whole;
+  const float cq = q & 1 ? s : c, sq = q & 1 ? c : s;
+  return make_float2(a.amplitude * ((q + 1) & 2 ? -cq : cq), a.amplitude * (q & 2 ? -sq : sq));
+}
+// The same in 64 bits, from the angle t: pi / 2 in two parts (the first has 33 bits, so that its multiples up to 2^20 are
+// exact), and the Taylor series up to terms below 2^-54 (x^17 / 17!, x^18 / 18!).
+__device__ __forceinline__ double2 turn64(double t, double amplitude) {
+  const double whole = rint(t * kQuarterTurns), x = fma(-whole, kQuarterLow, fma(-whole, kQuarterHigh, t)), z = x * x;
+  double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
+  s = fma(s, z, 1.0 / 6227020800.0);
+  c = fma(c, z, -1.0 / 87178291200.0);
+  s = fma(s, z, -1.0 / 39916800.0);
+  c = fma(c, z, 1.0 / 479001600.0);
+  s = fma(s, z, 1.0 / 362880.0);
+  c = fma(c, z, -1.0 / 3628800.0);
+  s = fma(s, z, -1.0 / 5040.0);
+  c = fma(c, z, 1.0 / 40320.0);
+  s = fma(s, z, 1.0 / 120.0);
+  c = fma(c, z, -1.0 / 720.0);
+  s = fma(s, z, -1.0 / 6.0);
+  c = fma(c, z, 1.0 / 24.0);
+  s = fma(s * z, x, x);
+  c = fma(c, z, -0.5);
+  c = fma(c, z, 1.0);
+  const int q = (int)(long long)whole;
+  const double cq = q & 1 ? s : c, sq = q & 1 ? c : s;
+  return make_double2(amplitude * ((q + 1) & 2 ? -cq : cq), amplitude * (q & 2 ? -sq : sq));
+}
+// Where pair f of row r has its cosine and sine (64 bits).  Lanes next to one another read pairs 8 apart, so of each eight the
 // twos are laid out apart: 16-byte reads without bank conflicts.
 __device__ __forceinline__ int table_at(const Args& a, int r, int f) {
   const int eighths = a.half >> 3;
@@ -125,20 +162,10 @@ __device__ __forceinline__ int table_at(const Args& a, int r, int f) {
 }
 
 // cosines and sines of a lane's eight pairs
-template <typename F2, typename F> struct Angles {
-  F c[8], s[8];
-  __device__ __forceinline__ void load(const Args& a, const Lane& l, const F2* table, int r) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const F2 cs = table[table_at(a, r, l.first + j)];
-      c[j] = cs.x;
-      s[j] = cs.y;
-    }
-  }
-};
+template <typename F> struct Angles { F c[8], s[8]; };
 // The rotated elements y of a lane from x; `round` makes what is stored of each.
-template <bool NEIGHBOURS, typename A, typename F, typename R>
-__device__ __forceinline__ void rotate(const A& t, const float (&x)[16], float (&y)[16], R round) {
+template <bool NEIGHBOURS, typename F, typename R>
+__device__ __forceinline__ void rotate(const Angles<F>& t, const float (&x)[16], float (&y)[16], R round) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     constexpr int kApart = NEIGHBOURS ? 1 : 8, kStep = NEIGHBOURS ? 2 : 1;
@@ -147,44 +174,60 @@ __device__ __forceinline__ void rotate(const A& t, const float (&x)[16], float (
     y[kStep * j + kApart] = round(fma(x2, c, x1 * s));
   }
 }
-// one element of a row whose pairs are loose
-template <typename F, typename F2, typename T>
-__device__ __forceinline__ F loose(const Args& a, const T* row, int e, float x, const F2* table, int r) {
-  if (e >= 2 * a.half) return x;
-  const bool low = a.interleaved ? !(e & 1) : e < a.half;
-  const F2 cs = table[table_at(a, r, a.interleaved ? e >> 1 : low ? e : e - a.half)];
-  const F other = load1(row + (a.interleaved ? e ^ 1 : low ? e + a.half : e - a.half));
-  return low ? fma((F)x, cs.x, -(other * cs.y)) : fma((F)x, cs.x, other * cs.y);
+// Element e of a row whose pairs are loose: its pair, whether it is the first of it, and where the other one is.
+struct Loose { int pair, other; bool low; };
+__device__ __forceinline__ Loose loose(const Args& a, int e) {
+  if (a.interleaved) return {e >> 1, e ^ 1, !(e & 1)};
+  return e < a.half ? Loose{e, e + a.half, true} : Loose{e - a.half, e - a.half, false};
 }
 
+template <typename T>
+__device__ __noinline__ double loose64(const Args& a, const T* row, int e, float x, const double2* table, int r) {
+  const Loose o = loose(a, e);
+  const double2 cs = table[table_at(a, r, o.pair)];
+  const double other = load1(row + o.other);
+  return o.low ? fma((double)x, cs.x, -(other * cs.y)) : fma((double)x, cs.x, other * cs.y);
+}
 // A lane's 16 elements of a new row as they become codes: rotated in 64 bits, rounded to 32.
-template <typename T, typename R>
-__device__ __forceinline__ void code_values(const Args& a, const T* row, const Lane& l, const double2* table, int r, float (&y)[16], R round) {
+template <bool LOOSE, typename T, typename R>
+__device__ __forceinline__ void code_values(const Args& a, const Eight<T> (&e)[2], const T* row, const Lane& l, const double2* table,
+                                            int r, float (&y)[16], R round) {
   float x[16];
-  load8(row + l.at[0], x);
-  load8(row + l.at[1], x + 8);
+  e[0].to(x);
+  e[1].to(x + 8);
   if (l.kind == kStill) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) y[j] = x[j];
-  } else if (l.kind == kLoose) {
-#pragma unroll 1
-    for (int j = 0; j < 16; ++j) y[j] = round(loose<double>(a, row, l.at[0] + j, x[j], table, r));
+  } else if (LOOSE) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)                        // (an index that is no constant would put y into local memory)
+      y[j] = l.at[0] + j < 2 * a.half ? round(loose64(a, row, l.at[0] + j, x[j], table, r)) : x[j];
   } else {
-    Angles<double2, double> t;
-    t.load(a, l, table, r);
-    if (l.kind == kPairs) rotate<false, Angles<double2, double>, double>(t, x, y, round);
-    else rotate<true, Angles<double2, double>, double>(t, x, y, round);
+    Angles<double> t;
+    const double2* twos = table + table_at(a, r, l.first);
+    const int apart = a.half >> 2;                      // (see table_at)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const double2 cs = twos[(j >> 1) * apart + (j & 1)];
+      t.c[j] = cs.x;
+      t.s[j] = cs.y;
+    }
+    if (l.kind == kPairs) rotate<false>(t, x, y, round);
+    else rotate<true>(t, x, y, round);
   }
 }
 // The largest finite magnitude of a lane's values, those in 64 bits rounded up; only asked for where it matters (below).
-template <typename T, int D>
+template <typename T, int D, bool LOOSE>
 __device__ __noinline__ float largest_rounded_up(const Args& a, const T* row, bool turn, const double2* table, int rows) {
   constexpr int kLanes = D / 16, kRows = 32 / kLanes;
   const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes;
   const Lane l = turn ? lane_of(a, chunk) : Lane{kStill, {16 * chunk, 16 * chunk + 8}, 0};
   float most = 0.f, y[16];
   for (int r = sub; r < rows; r += kRows) {
-    code_values(a, row + r * a.n_n, l, table, r, y, [&](double v) {
+    Eight<T> e[2];
+    e[0].load(row + r * a.n_n + l.at[0]);
+    e[1].load(row + r * a.n_n + l.at[1]);
+    code_values<LOOSE>(a, e, row + r * a.n_n, l, table, r, y, [&](double v) {
       const float up = __double2float_ru(fabs(v));
       most = fmaxf(most, up < INFINITY ? up : 0.f);
       return __double2float_rn(v);
@@ -195,21 +238,45 @@ __device__ __noinline__ float largest_rounded_up(const Args& a, const T* row, bo
   return most;
 }
 
-// One head's keys or values of a block of 16 rows: a warp.  Rows lo .. hi - 1 of the block are new, `row` is the first
+// One head's keys or values of a block of 16 rows: a warp.  Rows lo .. lo + m - 1 of the block are new, `row` is the first
 // of them in memory; codes and scale: the block's in the pool.
-template <typename T, int D>
-__device__ __forceinline__ void write_codes(const Args& a, const T* row, bool turn, const double2* table, int lo, int hi,
-                                            unsigned char* codes, int64_t code_row, float* scale) {
+template <typename T, int D> struct Rows {
+  static constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = 16 / kRows;
+  const T* row;
+  bool turn;
+  unsigned char* codes;
+  float* scale;
+  Lane l;
+  float old;
+  // looks up head u of K, then of V
+  __device__ __forceinline__ void load(const Args& a, int u, int64_t new_row, int64_t page_row, int64_t cell, int lo, int m) {
+    const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes;
+    const bool v = u >= a.H_kv;
+    const int h = v ? u - a.H_kv : u;
+    row = static_cast<const T*>(v ? a.v_new : a.k_new) + new_row + h * a.n_h;
+    turn = !v && a.half > 0;
+    codes = reinterpret_cast<unsigned char*>((v ? a.c.v : a.c.k) + page_row + h * a.c.s_head);
+    scale = (v ? a.v_scales : a.k_scales) + cell + (int64_t)h * (1 << (a.c.page_log - 4));
+    l = turn ? lane_of(a, chunk) : Lane{kStill, {16 * chunk, 16 * chunk + 8}, 0};
+    old = lo > 0 ? *scale : 0.f;
+  }
+};
+template <typename T, int D, bool LOOSE>
+__device__ __forceinline__ void write_codes(const Args& a, const Rows<T, D>& x, const double2* table, int lo, int m, int64_t code_row) {
   constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = 16 / kRows;
-  const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes;
-  const Lane l = turn ? lane_of(a, chunk) : Lane{kStill, {16 * chunk, 16 * chunk + 8}, 0};
-  const float old = lo > 0 ? within_limits(*scale) : 0.f;
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes, hi = lo + m;
+  const Lane l = x.l;
+  unsigned char* codes = x.codes;
+  const float old = lo > 0 ? within_limits(x.old) : 0.f;
   float y[kSteps][16], most = 0.f;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int r = i * kRows + sub;
     if (lo + r < hi) {
-      code_values(a, row + r * a.n_n, l, table, r, y[i], [](double v) { return __double2float_rn(v); });
+      Eight<T> e[2];
+      e[0].load(x.row + r * a.n_n + l.at[0]);
+      e[1].load(x.row + r * a.n_n + l.at[1]);
+      code_values<LOOSE>(a, e, x.row + r * a.n_n, l, table, r, y[i], [](double v) { return __double2float_rn(v); });
 #pragma unroll
       for (int j = 0; j < 16; j += 2) most = fmaxf(most, fmaxf(fabsf(y[i][j]), fabsf(y[i][j + 1])));      // (NaN is passed over)
     }
@@ -217,11 +284,10 @@ __device__ __forceinline__ void write_codes(const Args& a, const T* row, bool tu
   most = warp_max(most);
   // An infinity has no part in the scale; and 64 bits just above 448 times a power of two, which round to it, count as more.
   const bool infinite = most == INFINITY;
-  if (infinite || (turn && (__float_as_uint(most) & 0x7FFFFFu) == 0x600000u))
-    most = warp_max(largest_rounded_up<T, D>(a, row, turn, table, hi - lo));
+  if (infinite || (x.turn && (__float_as_uint(most) & 0x7FFFFFu) == 0x600000u))
+    most = warp_max(largest_rounded_up<T, D, LOOSE>(a, x.row, x.turn, table, m));
   const float need = fitting_scale(most), s = fmaxf(need, old);
-  const bool power = (__float_as_uint(s) & 0x7FFFFFu) == 0;               // (what fitting_scale gives: a product is exact)
-  const float inverse = 1.f / s;
+  const float inverse = 1.f / s;                        // (a power of two, and the products exact, unless an older scale was none)
   if (lo > 0 && s != old) {                             // older rows: the scale grew
     const float ratio = old / s;
 #pragma unroll
@@ -241,13 +307,8 @@ __device__ __forceinline__ void write_codes(const Args& a, const T* row, bool tu
 #pragma unroll
         for (int j = 0; j < 16; ++j) y[i][j] = fabsf(y[i][j]) < INFINITY ? y[i][j] : NAN;
       }
-      if (power) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[i][j] *= inverse;
-      } else {
-#pragma unroll 1
-        for (int j = 0; j < 16; ++j) y[i][j] /= s;
-      }
+      for (int j = 0; j < 16; ++j) y[i][j] *= inverse;
       uint32_t w[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[j] = pack2(y[i][4 * j], y[i][4 * j + 1]) | pack2(y[i][4 * j + 2], y[i][4 * j + 3]) << 16;
@@ -256,14 +317,16 @@ __device__ __forceinline__ void write_codes(const Args& a, const T* row, bool tu
     }
   }
   __syncwarp();                                         // (every lane has read the old scale)
-  if (lane == 0) *scale = s;
+  if (lane == 0) *x.scale = s;
 }
 
-template <typename T, Where W, int D_SCALED>
-__global__ void __launch_bounds__(kThreads, 2) rest_kv_append_kernel(const __grid_constant__ Args a) {
+// (loose pairs are worked out by calls, for which the others' values would go to memory and back)
+template <typename T, Where W, int D_SCALED, bool LOOSE>
+__global__ void __launch_bounds__(kThreads, W == kPagesScaled ? 2 : 3) rest_kv_append_kernel(const __grid_constant__ Args a) {
   grid_wait();
   extern __shared__ __align__(16) unsigned char smem[];
-  const int b = blockIdx.x / a.groups, group = blockIdx.x % a.groups;
+  const int all_groups = gridDim.x / a.parts, part = blockIdx.x / all_groups, b = blockIdx.x % all_groups / a.groups,
+            group = blockIdx.x % all_groups % a.groups;
   const int n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.N) : a.N;
   const int L = W == kNowhere ? 0 : a.kv_len[b];
   // new rows i0 .. i1 - 1 are rows lo ... of the block that starts at row `first`
@@ -272,42 +335,29 @@ __global__ void __launch_bounds__(kThreads, 2) rest_kv_append_kernel(const __gri
   const int m = min(n - i0, 16 - lo);
   if (m <= 0) return;
 
-  const int part = blockIdx.y;                          // some blocks write codes, the others rows
-  float2* table = reinterpret_cast<float2*>(smem);
-  double2* table64 = reinterpret_cast<double2*>(smem);
-  for (int e = threadIdx.x; e < m * a.half; e += kThreads) {
-    const int r = e / a.half, f = e - r * a.half;
-    const double t = (double)a.pos[(int64_t)b * a.N + i0 + r] * (double)a.inv_freq[f];
-    if (W == kPagesScaled && part < a.code_parts) {
-      double s, c;
-      sincos(t, &s, &c);
-      table64[table_at(a, r, f)] = make_double2(a.amplitude * c, a.amplitude * s);
-    } else {
-      // what lies behind the whole quarter turns, at most an eighth of a turn, in 32 bits
-      const double quarters = t * kQuarterTurns, whole = rint(quarters);
-      float s, c;
-      sincospif(0.5f * (float)(quarters - whole), &s, &c);
-      const int q = (int)(long long)whole & 3;
-      const float cq = q & 1 ? s : c, sq = q & 1 ? c : s;
-      table[table_at(a, r, f)] = make_float2(a.amplitude * (q == 1 || q == 2 ? -cq : cq), a.amplitude * (q & 2 ? -sq : sq));
-    }
-  }
-  __syncthreads();
-
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t page_row = W == kNowhere || L < 0 || first > 0x7FFFFFFFu ? -1 : row_offset(a.c, b, (int)first);
   if constexpr (W == kPagesScaled) {
-    if (part < a.code_parts) {
+    if (part < a.code_parts) {                          // some blocks write codes, the others rows
       if (page_row < 0) return;
       const int p = a.c.table[b * a.c.table_stride + (first >> a.c.page_log)];
       const int64_t cell = (int64_t)p * a.H_kv * (1 << (a.c.page_log - 4)) + ((first & ((1u << a.c.page_log) - 1)) >> 4);
-      for (int u = part * kWarps + warp; u < 2 * a.H_kv; u += a.code_parts * kWarps) {
-        const int h = u >> 1;
-        const bool v = u & 1;
-        const T* row = static_cast<const T*>(v ? a.v_new : a.k_new) + b * a.n_b + i0 * a.n_n + h * a.n_h;
-        unsigned char* codes = reinterpret_cast<unsigned char*>((v ? a.c.v : a.c.k) + page_row + h * a.c.s_head);
-        write_codes<T, D_SCALED>(a, row, !v && a.half > 0, table64, lo, lo + m, codes, a.c.s_row * 16,
-                                 (v ? a.v_scales : a.k_scales) + cell + (int64_t)h * (1 << (a.c.page_log - 4)));
+      const int64_t new_row = b * a.n_b + i0 * a.n_n;
+      int u = part * kWarps + warp;
+      Rows<T, D_SCALED> x;
+      if (u < 2 * a.H_kv) x.load(a, u, new_row, page_row, cell, lo, m);
+      double2* table = reinterpret_cast<double2*>(smem);
+      if (part * kWarps < a.H_kv && a.half > 0) {       // (else no keys)
+        for (int e = threadIdx.x; e < m * a.half; e += kThreads) {
+          const int r = e / a.half, f = e - r * a.half;
+          table[table_at(a, r, f)] = turn64((double)a.pos[(int64_t)b * a.N + i0 + r] * (double)a.inv_freq[f], a.amplitude);
+        }
+        __syncthreads();
+      }
+      while (u < 2 * a.H_kv) {
+        write_codes<T, D_SCALED, LOOSE>(a, x, table, lo, m, a.c.s_row * 16);
+        u += a.code_parts * kWarps;
+        if (u < 2 * a.H_kv) x.load(a, u, new_row, page_row, cell, lo, m);
       }
       return;
     }
@@ -321,13 +371,13 @@ __global__ void __launch_bounds__(kThreads, 2) rest_kv_append_kernel(const __gri
   if (all >= m && me >= together * m) return;
   const Lane l = lane_of(a, chunk);
   const int moving = min(lanes, (2 * a.half + 15) >> 4);        // lanes of a row of loose pairs that hold some
-  const int parts = gridDim.y - a.code_parts, h0 = (all >= m ? me / m : 0) + (part - a.code_parts) * together, step = together * parts;
+  const int parts = a.parts - a.code_parts, h0 = (all >= m ? me / m : 0) + (part - a.code_parts) * together, step = together * parts;
   for (int r = all >= m ? me % m : me; r < m; r += all >= m ? m : all) {
-    Angles<float2, float> t;
-    if (l.kind == kPairs || l.kind == kNeighbours) t.load(a, l, table, r);
-    // one row in `count` heads
+    Angles<float> t;
+    bool known = false;
+    // one row in `count` heads; the first heads are on their way while the angles are worked out
     auto heads = [&](const T* from, int64_t from_h, T* to, int64_t to_h, int count, Kind kind) {
-      if (kind == kLoose) {
+      if (kind == kLoose) {                             // (LOOSE is for codes only)
         for (int h = h0; h < count; h += step) {
           const T* x0 = from + h * from_h;
           T* y0 = to + h * to_h;
@@ -335,7 +385,14 @@ __global__ void __launch_bounds__(kThreads, 2) rest_kv_append_kernel(const __gri
           load8(x0 + l.at[0], x);
           load8(x0 + l.at[1], x + 8);
 #pragma unroll 1
-          for (int j = 0; j < 16; ++j) y[j] = loose<float>(a, x0, l.at[0] + j, x[j], table, r);
+          for (int j = 0; j < 16; ++j) {
+            const int e = l.at[0] + j;
+            if (e >= 2 * a.half) { y[j] = x[j]; continue; }
+            const Loose o = loose(a, e);
+            const float2 cs = turn_of(a, a.pos[(int64_t)b * a.N + i0 + r], o.pair);
+            const float other = load1(x0 + o.other);
+            y[j] = o.low ? fmaf(x[j], cs.x, -(other * cs.y)) : fmaf(x[j], cs.x, other * cs.y);
+          }
           // a row may be rotated in place: all its lanes have loaded before the first stores
           __syncwarp(((moving == 32 ? 0u : 1u << moving) - 1u) << (sub * lanes));
           store8(y0 + l.at[0], y);
@@ -343,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 2) rest_kv_append_kernel(const __gri
         }
         return;
       }
-      constexpr int kAtOnce = sizeof(T) == 4 ? 2 : 4;   // heads on their way: 128 bytes a thread
+      constexpr int kAtOnce = sizeof(T) == 4 || W == kPages16 ? 2 : 4;      // heads on their way
       from += h0 * from_h;
       to += h0 * to_h;
       from_h *= step;
@@ -356,6 +413,16 @@ __global__ void __launch_bounds__(kThreads, 2) rest_kv_append_kernel(const __gri
             e[i][0].load(from + i * from_h + l.at[0]);
             e[i][1].load(from + i * from_h + l.at[1]);
           }
+        if (kind != kStill && !known) {
+          const double p = a.pos[(int64_t)b * a.N + i0 + r];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float2 cs = turn_of(a, p, l.first + j);
+            t.c[j] = cs.x;
+            t.s[j] = cs.y;
+          }
+          known = true;
+        }
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i)
           if (i < left) {
@@ -368,8 +435,8 @@ __global__ void __launch_bounds__(kThreads, 2) rest_kv_append_kernel(const __gri
               e[i][0].to(x);
               e[i][1].to(x + 8);
               auto same = [](float v) { return v; };
-              if (kind == kPairs) rotate<false, Angles<float2, float>, float>(t, x, y, same);
-              else rotate<true, Angles<float2, float>, float>(t, x, y, same);
+              if (kind == kPairs) rotate<false>(t, x, y, same);
+              else rotate<true>(t, x, y, same);
               store8(y0 + l.at[0], y);
               store8(y0 + l.at[1], y + 8);
             }
@@ -389,22 +456,27 @@ __global__ void __launch_bounds__(kThreads, 2) rest_kv_append_kernel(const __gri
 
 template <typename T, Where W, int D>
 rest_status run(const Args& a, int B, void* stream) {
-  // Blocks for about four waves of two an SM, so that the last wave is a small part; few rows share their heads out
-  // until a warp has one task.  Codes take about as long as twice the rows that they are made of.
+  // Few rows: their heads are shared out until a warp has one task or there are eight blocks an SM.  Many: still two
+  // blocks of codes (K and V, which needs no angles) and two of rows for each group of 16, so that the last wave is short.
   const int64_t blocks = (int64_t)B * a.groups;
-  if (blocks > 0x7FFFFFFFll) return REST_UNSUPPORTED;
   const int sms = rest::sm_count(), most = min(a.N, 16), rows = 32 / (a.D / 16);
+  const int64_t wanted = 8 * (int64_t)(sms > 0 ? sms : 148) / (blocks > 0 ? blocks : 1), each = W == kPagesScaled ? wanted / 2 : wanted;
   auto tasks = [](int warps) { return (warps + kWarps - 1) / kWarps; };
-  const int code_tasks = W == kPagesScaled ? tasks(2 * a.H_kv) : 0;
-  const int row_tasks = tasks(((W == kPages16 ? a.H + 2 * a.H_kv : a.H) * most + rows - 1) / rows);
-  const int64_t wanted = 8 * (int64_t)(sms > 0 ? sms : 148) / blocks;
-  auto parts = [&](int64_t share, int tasks_) { return (int)(share < 1 ? (tasks_ > 0) : share < tasks_ ? share : tasks_); };
+  auto parts = [&](int tasks_) { return (int)(tasks_ < 2 || tasks_ < each ? tasks_ : each < 2 ? 2 : each); };
   Args args = a;
-  args.code_parts = parts(W == kPagesScaled && a.H > 0 ? wanted / 2 : wanted, code_tasks);
-  const int row_parts = parts(wanted - args.code_parts, row_tasks);
-  const size_t smem = (size_t)16 * a.half * (W == kPagesScaled ? 16 : 8);
-  REST_CUDA_TRY(launch(rest_kv_append_kernel<T, W, D>, dim3((unsigned)blocks, (unsigned)(args.code_parts + row_parts)), kThreads,
-                       smem, stream, args));
+  if (W == kPagesScaled && a.H > 0 && each < 2) {
+    // Many rows: the queries in a launch of their own, at three blocks an SM instead of the two that codes allow
+    // (128 x up to 64 rows, 32/8 heads: 49 us in two, 52 in one).
+    args.groups = (a.N + 15) / 16;
+    if (rest_status st = run<T, kNowhere, 0>(args, B, stream)) return st;
+    args.groups = a.groups;
+    args.H = 0;
+  }
+  args.code_parts = W == kPagesScaled ? parts(tasks(2 * a.H_kv)) : 0;
+  args.parts = args.code_parts + parts(tasks(((W == kPages16 ? a.H + 2 * a.H_kv : args.H) * most + rows - 1) / rows));
+  if (blocks * args.parts > 0x7FFFFFFFll) return REST_UNSUPPORTED;
+  const size_t smem = W == kPagesScaled ? (size_t)16 * a.half * sizeof(double2) : 0;
+  REST_CUDA_TRY(launch(W == kPagesScaled && (a.half & 7) ? rest_kv_append_kernel<T, W, D, W == kPagesScaled> : rest_kv_append_kernel<T, W, D, false>, dim3((unsigned)(blocks * args.parts)), kThreads, smem, stream, args));
   return REST_OK;
 }
 

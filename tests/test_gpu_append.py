@@ -37,6 +37,7 @@ CASES = [  # B, N, H, H_kv, D, F, dtype, kv_len, page, nodes, interleaved, layou
     (1, 256, 3, 3, 64, 32, BF16, [9], 16, None, False, "hnd"),
     (40, 17, 2, 2, 128, 64, FP16, list(range(40)), 16, None, True, "hnd"),
     (2, 16, 0, 4, 128, 0, BF16, [3, 48], 16, None, False, "hnd"),
+    (300, 17, 3, 1, 64, 32, BF16, [7 * b % 50 for b in range(300)], 32, [b % 18 for b in range(300)], False, "hnd"),
 ]
 
 

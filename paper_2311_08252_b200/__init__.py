@@ -515,13 +515,33 @@ def rest_kv_commit(k, v, kv_len, accept_nodes, accept_len, N, new_kv_len=None, s
 # ------------------------------------------------------------------------------ cache in pages
 # These calls are made many times per decoding step, so their checks go through few, cheap tensor
 # queries: get_device() says both that a tensor is on a GPU (-1: it is not) and on which.
-_I64x3 = ctypes.c_int64 * 3
 _I64x9 = ctypes.c_int64 * 9
+_T = None                                                # torch, once a call has needed it (an import statement takes as long as a check)
+
+
+def _torch():
+    global _T
+    import torch
+    _T = torch
+    return torch
+
+
+_strides_seen = {}
+
+
+def _strides(s):
+    """The first three of a tuple of strides as a C array; arrays are kept by their values."""
+    a = _strides_seen.get(s)
+    if a is None:
+        if len(_strides_seen) >= 4096:
+            _strides_seen.clear()
+        a = _strides_seen[s] = (ctypes.c_int64 * 3)(*s[:3])
+    return a
 
 
 def _call(fn, what, index, stream, *args):
     """fn(*args, stream) on GPU `index`, whatever the current device is; raises on an error status."""
-    import torch
+    torch = _T or _torch()
     if index < 0:
         raise RestError(f"{what}: the tensors must be on a CUDA device")
     if torch.cuda.current_device() != index:
@@ -546,7 +566,7 @@ def _same_device(stream, index):
 
 def _scratch_bytes(fn, index, *args):
     """fn(*args) with GPU `index` as the current device, which the scratch sizes go by."""
-    import torch
+    torch = _T or _torch()
     if index < 0 or torch.cuda.current_device() == index:
         return fn(*args)
     with torch.cuda.device(index):
@@ -555,7 +575,7 @@ def _scratch_bytes(fn, index, *args):
 
 def _as_current(stream, t):
     """`stream` (a torch stream or a handle) as the current one: what a call allocates and clears belongs to it."""
-    import torch
+    torch = _T or _torch()
     if t.get_device() < 0:
         raise RestError("the tensors must be on a CUDA device")
     _same_device(stream, t.get_device())
@@ -575,13 +595,14 @@ def _window(window, sinks):
 
 def _vec(t, name, index, n=None, dtype=None):
     """Pointer of a contiguous vector (int32 unless told otherwise) of n elements on GPU `index`."""
-    import torch
-    dtype = torch.int32 if dtype is None else dtype
-    if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous() or t.dim() != 1 or (
-            n is not None and t.numel() != n):
-        raise RestError(f"{name} must be a contiguous {str(dtype).split('.')[-1]} vector"
-                        + ("" if n is None else f" of {n} elements") + " on the same CUDA device as the others")
-    return t.data_ptr()
+    if dtype is None:
+        dtype = (_T or _torch()).int32
+    if t.dtype is dtype and t.get_device() == index and t.is_contiguous():
+        shape = t.shape
+        if len(shape) == 1 and (n is None or shape[0] == n):
+            return t.data_ptr()
+    raise RestError(f"{name} must be a contiguous {str(dtype).split('.')[-1]} vector"
+                    + ("" if n is None else f" of {n} elements") + " on the same CUDA device as the others")
 
 
 def _array(t, name, index, shape, dtype):
@@ -594,18 +615,18 @@ def _array(t, name, index, shape, dtype):
 
 def _pool(k_pages, v_pages):
     """Device, shape, and (pointers, strides, pages, rows per page) of a pool [P, H_kv, page, D]."""
-    import torch
+    torch = _T or _torch()
     index, shape, strides, dtype = k_pages.get_device(), k_pages.shape, k_pages.stride(), k_pages.dtype
     if len(shape) != 4 or strides[3] != 1 or not (dtype is torch.bfloat16 or dtype is torch.float16):
         raise RestError("k_pages must be a bf16 or fp16 tensor [P, H_kv, page, D] with a contiguous last dimension")
     if v_pages.stride() != strides or v_pages.shape != shape or v_pages.dtype is not dtype or v_pages.get_device() != index:
         raise RestError("k_pages and v_pages must have the same shape, strides, type and device")
-    return index, shape, (k_pages.data_ptr(), v_pages.data_ptr(), _I64x3(*strides[:3]), shape[0], shape[2])
+    return index, shape, (k_pages.data_ptr(), v_pages.data_ptr(), _strides(strides), shape[0], shape[2])
 
 
 def _table(table, index, B=None):
     """Pointer, row stride and columns of a block table."""
-    import torch
+    torch = _T or _torch()
     shape = table.shape
     if table.dtype is not torch.int32 or table.get_device() != index or len(shape) != 2 or table.stride(1) != 1 or (
             B is not None and shape[0] != B):
@@ -624,7 +645,7 @@ def paged_attention_workspace_bytes(B, H, H_kv, N, D) -> int:
 def _attend(name, q, index, pages, pointers, pool, scales, block_table, kv_len, mask, scale, window, sinks, n_nodes, out, lse,
             workspace):
     """What both attention calls check and pass on; pool: (strides, pages, rows per page), scales: none or two pointers."""
-    import torch
+    torch = _T or _torch()
     L = _lib or lib()
     P, H_kv, page, Dk = pages
     dtype, shape, qs = q.dtype, q.shape, q.stride()
@@ -691,7 +712,7 @@ def rest_accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature,
     rest_accept_sampled_workspace_bytes() bytes, not shared by calls that may overlap; None: one is
     allocated when the library asks for it; False: none (each context walks row by row).  Returns
     (accept_len, accept_nodes, out_tokens) like rest_accept."""
-    import torch
+    torch = _T or _torch()
     if stream is not None:
         with _as_current(stream, tokens):
             return rest_accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature, top_p, max_depth, out,
@@ -735,7 +756,7 @@ def rest_paged_kv_write(k_pages, v_pages, block_table, kv_len, k_new, v_new, n_n
         raise RestError("k_new and v_new must have the same shape, strides, type and device")
     B, N = shape[0], shape[1]
     _call((_lib or lib()).rest_paged_kv_write, "rest_paged_kv_write", index, stream, *pool, *_table(block_table, index, B),
-          _vec(kv_len, "kv_len", index, B), k_new.data_ptr(), v_new.data_ptr(), _I64x3(*ns[:3]),
+          _vec(kv_len, "kv_len", index, B), k_new.data_ptr(), v_new.data_ptr(), _strides(ns),
           0 if n_nodes is None else _vec(n_nodes, "n_nodes", index, B), B, H_kv, N, D)
 
 
@@ -743,7 +764,7 @@ def rest_paged_kv_commit(k_pages, v_pages, block_table, kv_len, accept_nodes, ac
                          stream=None):
     """rest_kv_commit over pages: row kv_len[b] + accept_nodes[b][i] moves to row kv_len[b] + i.
     new_kv_len (optional int32[B], may be kv_len itself) receives kv_len + accept_len."""
-    import torch
+    torch = _T or _torch()
     index, (P, H_kv, page, D), pool = _pool(k_pages, v_pages)
     B, max_depth = accept_nodes.shape
     _call((_lib or lib()).rest_paged_kv_commit, "rest_paged_kv_commit", index, stream, *pool,
@@ -759,7 +780,7 @@ def rest_pages_fork(refs, block_table, n_pages, kv_len, parents, children, page,
     """Makes context children[f] a copy of parents[f]: whole pages are shared, a partly filled last
     page is replaced by a page of the child's own.  Returns (copy_src, copy_dst, status) int32[F]:
     the pages to copy with rest_pages_copy in every layer (-1: none), and REST_CTX_* codes."""
-    import torch
+    torch = _T or _torch()
     if stream is not None:
         with _as_current(stream, refs):
             return rest_pages_fork(refs, block_table, n_pages, kv_len, parents, children, page, copy_src, copy_dst, status)
@@ -785,7 +806,7 @@ def rest_pages_reserve(refs, block_table, n_pages, need_len, page, status=None, 
     """Gives every context pages until its table holds need_len[b] rows, all or none, in the contexts'
     order: from the first that the pool is too small for, every one that needs a page is refused.
     Returns status int32[B] (REST_CTX_*)."""
-    import torch
+    torch = _T or _torch()
     if stream is not None:
         with _as_current(stream, refs):
             return rest_pages_reserve(refs, block_table, n_pages, need_len, page, status)
@@ -815,7 +836,7 @@ def rotary_frequencies(dim, base=10000.0, scaling=None, factor=1.0, original_len
     within original_len: fewer than `slow`, factor times, more than `fast`, not at all, mixed between, with amplitude
     0.1 ln(factor) + 1."""
     import math
-    import torch
+    torch = _T or _torch()
     if dim < 2 or dim % 2 or not base > 0 or not factor >= 1 or scaling not in (None, "linear", "base", "parts"):
         raise RestError("rotary_frequencies: dim even, base > 0, factor >= 1, scaling None, 'linear', 'base' or 'parts'")
     if scaling == "parts" and not (original_len and original_len > 0 and fast > slow):
@@ -835,7 +856,7 @@ def rotary_frequencies(dim, base=10000.0, scaling=None, factor=1.0, original_len
 
 def _turn(positions, inv_freq, index, B, N, D):
     """Pointers of positions and frequencies, and how many pairs turn (None, None: none)."""
-    import torch
+    torch = _T or _torch()
     if inv_freq is None and positions is None:
         return 0, 0, 0
     if inv_freq is None or positions is None:
@@ -852,12 +873,13 @@ def rest_rotary(x, positions, inv_freq, interleaved=False, amplitude=1.0, n_node
     elements turn by positions[b,i] * inv_freq[f] (int32 [B,N], as rest_draft's pos_ids; float32 [F], as
     rotary_frequencies gives them, on the GPU) and are multiplied by amplitude; the others are copied.
     n_nodes int32[B]: later rows of out stay as they were.  out: like x, x itself (in place), or None.  Returns out."""
-    import torch
+    torch = _T or _torch()
     if stream is not None:
         with _as_current(stream, x):
             return rest_rotary(x, positions, inv_freq, interleaved, amplitude, n_nodes, out)
     dtype, shape, xs, index = x.dtype, x.shape, x.stride(), x.get_device()
-    kind = {torch.bfloat16: REST_BF16, torch.float16: REST_FP16, torch.float32: REST_FP32}.get(dtype)
+    kind = (REST_BF16 if dtype is torch.bfloat16 else REST_FP16 if dtype is torch.float16 else
+            REST_FP32 if dtype is torch.float32 else None)
     if kind is None or len(shape) != 4 or xs[3] != 1:
         raise RestError("x must be a bf16, fp16 or fp32 tensor [B,N,H,D] with a contiguous last dimension")
     B, N, H, D = shape
@@ -865,42 +887,44 @@ def rest_rotary(x, positions, inv_freq, interleaved=False, amplitude=1.0, n_node
         out = (torch.empty if n_nodes is None else torch.zeros)(shape, dtype=dtype, device=x.device)
     elif out.dtype is not dtype or out.shape != shape or out.stride(3) != 1 or out.get_device() != index:
         raise RestError("out must be a tensor like x with a contiguous last dimension")
-    _call((_lib or lib()).rest_rotary, "rest_rotary", index, stream, x.data_ptr(), _I64x3(*xs[:3]), kind,
+    _call((_lib or lib()).rest_rotary, "rest_rotary", index, stream, x.data_ptr(), _strides(xs), kind,
           *_turn(positions, inv_freq, index, B, N, D), int(bool(interleaved)), amplitude,
           0 if n_nodes is None else _vec(n_nodes, "n_nodes", index, B), B, H, N, D, out.data_ptr(),
-          _I64x3(*out.stride()[:3]))
+          _strides(out.stride()))
     return out
 
 
 def _append(name, index, dims, pool, block_table, kv_len, k_new, v_new, positions, inv_freq, interleaved, amplitude,
             n_nodes, q, q_out, dtype):
-    import torch
+    torch = _T or _torch()
     H_kv, D = dims
-    shape, ns = k_new.shape, k_new.stride()
-    kind = {torch.bfloat16: REST_BF16, torch.float16: REST_FP16}.get(k_new.dtype)
+    shape, ns, new = k_new.shape, k_new.stride(), k_new.dtype
+    kind = REST_BF16 if new is torch.bfloat16 else REST_FP16 if new is torch.float16 else None
     if kind is None or len(shape) != 4 or shape[2] != H_kv or shape[3] != D or ns[3] != 1 or (
-            k_new.get_device() != index) or (dtype is not None and k_new.dtype is not dtype):
+            k_new.get_device() != index) or (dtype is not None and new is not dtype):
         raise RestError("k_new must be [B,N,H_kv,D] of the pages' heads and device, bf16 or fp16 as 16-bit pages are, with a "
                         "contiguous last dimension")
-    if v_new.shape != shape or v_new.stride() != ns or v_new.dtype is not k_new.dtype or v_new.get_device() != index:
+    if v_new.shape != shape or v_new.stride() != ns or v_new.dtype is not new or v_new.get_device() != index:
         raise RestError("k_new and v_new must have the same shape, strides, type and device")
-    B, N, H = shape[0], shape[1], 0
+    B, N, _, _ = shape
+    H = 0
     queries = (0, None, 0, None)
     if q is not None:
-        qs = q.stride()
-        if q.dtype is not k_new.dtype or len(q.shape) != 4 or q.shape[:2] != shape[:2] or q.shape[3] != D or (
-                qs[3] != 1 or q.get_device() != index):
+        qs, of = q.stride(), q.shape
+        if q.dtype is not new or len(of) != 4 or of[0] != B or of[1] != N or of[3] != D or qs[3] != 1 or (
+                q.get_device() != index):
             raise RestError("q must be [B,N,H,D] of k_new's type, head size and device, with a contiguous last dimension")
         if q_out is None:
-            q_out = (torch.empty if n_nodes is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
-        elif q_out.dtype is not q.dtype or q_out.shape != q.shape or q_out.stride(3) != 1 or q_out.get_device() != index:
+            q_out = (torch.empty if n_nodes is None else torch.zeros)(of, dtype=new, device=q.device)
+        os_ = q_out.stride()
+        if q_out.dtype is not new or q_out.shape != of or os_[3] != 1 or q_out.get_device() != index:
             raise RestError("q_out must be a tensor like q with a contiguous last dimension")
-        H = q.shape[2]
-        queries = (q.data_ptr(), _I64x3(*qs[:3]), q_out.data_ptr(), _I64x3(*q_out.stride()[:3]))
+        H = of[2]
+        queries = (q.data_ptr(), _strides(qs), q_out.data_ptr(), _strides(os_))
     elif q_out is not None:
         raise RestError("q_out without q")
     _call(getattr(_lib or lib(), name), name, index, None, *pool, *_table(block_table, index, B),
-          _vec(kv_len, "kv_len", index, B), k_new.data_ptr(), v_new.data_ptr(), _I64x3(*ns[:3]),
+          _vec(kv_len, "kv_len", index, B), k_new.data_ptr(), v_new.data_ptr(), _strides(ns),
           0 if n_nodes is None else _vec(n_nodes, "n_nodes", index, B), kind,
           *_turn(positions, inv_freq, index, B, N, D), int(bool(interleaved)), amplitude, *queries, H, B, H_kv, N, D)
     return q_out
@@ -923,7 +947,7 @@ def rest_paged_kv_append(k_pages, v_pages, block_table, kv_len, k_new, v_new, po
 
 def _scaled_pool(k_pages, v_pages, k_scales, v_scales):
     """Device, shape, and (pointers, strides, pointers of the scales, pages, rows per page) of a pool of codes."""
-    import torch
+    torch = _T or _torch()
     index, shape, strides = k_pages.get_device(), k_pages.shape, k_pages.stride()
     if len(shape) != 4 or strides[3] != 1 or k_pages.dtype is not torch.float8_e4m3fn:
         raise RestError("k_pages must be a float8_e4m3fn tensor [P, H_kv, page, D] with a contiguous last dimension")
@@ -931,7 +955,7 @@ def _scaled_pool(k_pages, v_pages, k_scales, v_scales):
             v_pages.get_device() != index):
         raise RestError("k_pages and v_pages must have the same shape, strides, type and device")
     want = (shape[0], shape[1], shape[2] // 16)
-    return index, shape, (k_pages.data_ptr(), v_pages.data_ptr(), _I64x3(*strides[:3]),
+    return index, shape, (k_pages.data_ptr(), v_pages.data_ptr(), _strides(strides),
                           _array(k_scales, "k_scales", index, want, torch.float32),
                           _array(v_scales, "v_scales", index, want, torch.float32), shape[0], shape[2])
 
@@ -970,7 +994,7 @@ def rest_paged_kv_commit_scaled(k_pages, v_pages, k_scales, v_scales, block_tabl
                                 new_kv_len=None, stream=None):
     """rest_paged_kv_commit over pages of codes: the accepted rows are put to the front as if the values that they
     stand for had been appended there."""
-    import torch
+    torch = _T or _torch()
     index, (P, H_kv, page, D), pool = _scaled_pool(k_pages, v_pages, k_scales, v_scales)
     B, max_depth = accept_nodes.shape
     _call((_lib or lib()).rest_paged_kv_commit_scaled, "rest_paged_kv_commit_scaled", index, stream, *pool,
@@ -993,7 +1017,7 @@ def dependent_read_latency_ns(table_bytes: int = 1 << 30, steps: int = 4096, dev
     """Nanoseconds per dependent DRAM read on this GPU: builds a random single-cycle table of
     table_bytes (much larger than L2) with torch, then one device thread chases it
     (rest_probe_dependent_reads).  A measurement aid for the draft path's latency floor."""
-    import torch
+    torch = _T or _torch()
     L = lib()
     device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
     n = table_bytes // 4
@@ -1023,7 +1047,7 @@ def rest_suffix_array_build(tokens, sa_bytes: int = 4, stream=None, max_group: i
     max_group: sort the stream in groups of first-token buckets of at most that many positions
     (the method for streams beyond 2^31 - 1 tokens), whatever its size.  full=True: the true
     suffix array (whole suffixes compared) instead of the order on 32 tokens."""
-    import torch
+    torch = _T or _torch()
     L = lib()
     _dev_i32(tokens, "tokens")
     n = tokens.numel()
@@ -1053,7 +1077,7 @@ def rest_suffix_array_build(tokens, sa_bytes: int = 4, stream=None, max_group: i
 def rest_suffix_array_append(tokens, sa_old, stream=None):
     """Suffix array of `tokens` (int32 CUDA tensor: the old stream followed by the appended
     tokens) from the array `sa_old` of its first sa_old.numel() tokens."""
-    import torch
+    torch = _T or _torch()
     L = lib()
     _dev_i32(tokens, "tokens")
     n, n_old = tokens.numel(), sa_old.numel()

@@ -198,33 +198,41 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
 
 __device__ unsigned int g_paged_error;                  // bit 0: wait gave up, bit 1: smem misaligned
 
-// SCALED: pages of e4m3 codes.  Their tiles arrive as they are, in rings of kRaw; four more warps widen them to 16 bits
-// into the operand rings, which are shorter (16 warps of 128 registers: the softmax warps do with that).
-template <int D, int NT, bool SCALED> struct Shape {
+// PIECES > 0: pages of e4m3 codes.  K's tiles are operands as they arrive: Q is cut into PIECES e4m3 terms (see split_q),
+// whose products are summed in one accumulator.  V's arrive in a ring of kRaw and are widened to 16 bits by four more warps
+// (16 of 128 registers: the softmax warps do with that).
+template <int D, int NT, int PIECES> struct Shape {
+  static constexpr bool kScaled = PIECES > 0;
   static constexpr int BN = 64;                         // keys per step
   static constexpr int kHalves = D / 64;
   static constexpr int kRows = 128 * NT;
-  static constexpr int kQTile = 128 * D * 2, kTile = BN * D * 2;
-  static constexpr int KS = SCALED ? 3 : NT == 1 && D == 128 ? 2 : 4, VS = SCALED ? 3 : NT == 1 && D == 128 ? 3 : 6;      // ring stages
-  static constexpr int kRaw = BN * D, RS = SCALED ? 4 : 0;                // bytes of codes, stages of each raw ring
-  static constexpr int kRings = NT * kQTile + (KS + VS) * kTile;
-  static constexpr int kBars = kRings + 2 * RS * kRaw;                    // barriers behind the tiles
-  static constexpr int kSmem = kBars + (SCALED ? 1280 : 512);
+  static constexpr int kQTile = 128 * D * 2, kTile = BN * D * 2, kRaw = BN * D;
+  static constexpr int kKTile = kScaled ? kRaw : kTile;
+  static constexpr int KS = kScaled ? (PIECES == 3 && D == 128 ? 5 : 8) : NT == 1 && D == 128 ? 2 : 4;      // ring stages
+  static constexpr int VS = kScaled ? 3 : NT == 1 && D == 128 ? 3 : 6, RS = kScaled ? 4 : 0;
+  static constexpr int kThird = 128 * 128;              // bytes of a row tile's third term
+  static constexpr int kThirds = NT * kQTile + KS * kKTile + VS * kTile;  // behind the rings
+  static constexpr int kRings = kThirds + (PIECES == 3 ? NT * kThird : 0);
+  static constexpr int kBars = kRings + RS * kRaw;                        // barriers behind the tiles
+  static constexpr int kSmem = kBars + (kScaled ? 5856 : 512);
   static constexpr int kSoftmax = 4 * NT;               // softmax warps; then K loader, V loader, MMA warps
-  static constexpr int kWiden = SCALED ? 4 : 0;         // and those that widen
+  static constexpr int kWiden = kScaled ? 4 : 0;        // and those that widen
   static constexpr int kThreads = 32 * (kSoftmax + 2 + NT + kWiden);
   static constexpr uint32_t kTmem = NT == 1 ? 256 : 512;
   static constexpr uint32_t kColO = 2 * NT * BN;        // behind two S buffers for each row tile
 };
+// terms that hold a query element of the type (8 significant bits in 4 + 4, 11 in 4 + 4 + 4)
+template <typename T, bool SCALED> struct Pieces { static constexpr int value = !SCALED ? 0 : __is_same(T, __half) ? 3 : 2; };
 // byte offsets behind kBars
 enum {
   kKFull = 0, kKFree = 32, kVFull = 64, kVFree = 112, kSFull = 160, kPFull = 192, kOFull = 224, kQFull = 240, kQFree = 248,
   kTmemSlot = 256, kAbort = 260, kBad = 264 /* 8 x 4 */, kStartB = 296, kStartOff = 304, kTotal = 312,
   kScan = 320 /* 12 x 8 */, kJoin = 416, kTurn = 424 /* 8 x 8 */, kStartLeft = 488,
-  // pages of codes: the raw tiles' barriers (K, V), their scales as they come, and as the softmax warps want them
-  // (of each 16 keys: what K's makes of a raw score, in log2 units; the logarithm of V's; one over it)
-  kRawFull = 512 /* 2 x 4 x 8 */, kRawFree = 576 /* 2 x 4 x 8 */, kRawScales = 640 /* 4 x 8 x 4 */, kScales = 768 /* 8 x 48 */,
-  kScanWide = 1152 /* 16 x 8 */
+  // pages of codes: barriers of K's ring (8 each), of V's raw one (4 each), and of a piece's Q as it came
+  kKFullWide = 512, kKFreeWide = 576, kRawFull = 640, kRawFree = 672, kQRaw = 704,
+  // scales as they come (4 x 8 x 4) and as the softmax warps want them (16 x 48: of each 16 keys, what K's makes of a raw
+  // score, in log2 units; the logarithm of V's; one over it), Q's scales (4 pieces x 256 rows)
+  kRawScales = 720, kScales = 848, kScanWide = 1616, kQScales = 1760
 };
 
 // Bounded wait of a whole warp, with one result for all lanes (TMEM accesses and elected lanes need
@@ -495,6 +503,68 @@ __device__ __forceinline__ void leave_unfinished(const Args& a, const Share& sha
   a.meta[blockIdx.x] = m;
 }
 
+// D = e4m3 x e4m3, K = 32 of an instruction
+__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc_, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}\n"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc_), "r"(accumulate), "r"(0u)
+      : "memory");
+}
+// matrix descriptor of rows of 64 bytes: 64-byte swizzle
+__device__ __forceinline__ uint64_t umma_desc64(uint32_t saddr, uint32_t sbo_bytes) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | (1ull << 16) | ((uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (4ull << 61);
+}
+// Row r of a tile of Q becomes a sum of e4m3 terms, in place (the terms are half as wide): divided by the power of two that
+// fits its largest element (returned), what the first term leaves is at most a sixteenth of it, and so on.  Two terms hold
+// bf16's 8 bits, three fp16's 11, of elements down to 2^-11 of the row's largest; below, an element is off by 2^-19 of the largest
+// at most (2^-10, half of e4m3's smallest step, under 448), in three terms as well.  What is not finite makes the row NaN.
+template <typename T, int D>
+__device__ __forceinline__ float split_q(uint32_t tile, uint32_t third, int r) {
+  constexpr int kVecs = D / 8;                          // 16-byte chunks of the row, 8 to a half of the head
+  auto at = [&](uint32_t base, int chunk) { return base + r * 128 + ((chunk ^ (r & 7)) << 4); };
+  uint32_t x[kVecs][4];
+#pragma unroll
+  for (int c = 0; c < kVecs; ++c)
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[c][0]), "=r"(x[c][1]), "=r"(x[c][2]), "=r"(x[c][3])
+                 : "r"(at(tile + (c >> 3) * (128 * 128), c & 7)) : "memory");
+  float most = 0.f;
+#pragma unroll
+  for (int c = 0; c < kVecs; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = Type<T>::unpack(x[c][j]);
+      most = fmaxf(most, fmaxf(fabsf(f.x) < INFINITY ? fabsf(f.x) : 0.f, fabsf(f.y) < INFINITY ? fabsf(f.y) : 0.f));
+    }
+  const float scale = rest_e4m3::fitting_scale(most), inverse = 1.f / scale;
+#pragma unroll
+  for (int c = 0; c < kVecs / 2; ++c) {                 // 16 elements: a chunk of each term
+    uint32_t hi[4], lo[4], end[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f0 = Type<T>::unpack(x[2 * c + (j >> 1)][2 * (j & 1)]), f1 = Type<T>::unpack(x[2 * c + (j >> 1)][2 * (j & 1) + 1]);
+      float v[4] = {f0.x * inverse, f0.y * inverse, f1.x * inverse, f1.y * inverse};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fabsf(v[e]) < INFINITY ? v[e] : NAN;
+      auto take = [&]() -> uint32_t {                   // the nearest codes, taken off
+        const uint32_t a = rest_e4m3::pack2(v[0], v[1]), b = rest_e4m3::pack2(v[2], v[3]);
+        const float2 g = rest_e4m3::unpack2(a), h = rest_e4m3::unpack2(b);
+        v[0] -= g.x; v[1] -= g.y; v[2] -= h.x; v[3] -= h.y;
+        return a | b << 16;
+      };
+      hi[j] = take();
+      lo[j] = take();
+      if constexpr (__is_same(T, __half)) end[j] = take();
+    }
+    auto put = [&](uint32_t to, const uint32_t (&w)[4]) {
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    };
+    put(at(tile, c), hi);
+    put(D == 64 ? at(tile, 4 + c) : at(tile + 128 * 128, c), lo);
+    if constexpr (__is_same(T, __half)) put(at(third, c), end);
+  }
+  return scale;
+}
 // 16 rows of a raw tile of codes -> an operand tile of type T in the 128-byte-swizzled layout, by a warp.  A lane takes 16
 // codes of a row and writes two 16-byte chunks; lanes of the second half of the head write theirs the other way round, so
 // that the eight lanes of a phase meet different banks.  CHECK: NaN codes become 0; true in a lane that found one in
@@ -584,16 +654,16 @@ __device__ __forceinline__ void load_q(const Args& a, const Piece& p, int rb, ui
 }
 
 template <typename T, int D, int NT, int C, bool SCALED>
-__global__ void __launch_bounds__(Shape<D, NT, SCALED>::kThreads, NT == 1 ? 2 : 1)
+__global__ void __launch_bounds__(Shape<D, NT, Pieces<T, SCALED>::value>::kThreads, NT == 1 ? 2 : 1)
 paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
-  using S_ = Shape<D, NT, SCALED>;
+  using S_ = Shape<D, NT, Pieces<T, SCALED>::value>;
   using TV = typename Operand<T, SCALED>::V;            // what P and V are held in for their product
   constexpr int BN = S_::BN, KS = S_::KS, VS = S_::VS, kHalves = S_::kHalves;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   const uint32_t sbase = smem_u32(smem);
-  const uint32_t sQ = sbase, sK = sQ + NT * S_::kQTile, sV = sK + KS * S_::kTile;
-  const uint32_t bars = sbase + S_::kBars;
+  const uint32_t sQ = sbase, sK = sQ + NT * S_::kQTile, sV = sK + KS * S_::kKTile;
+  const uint32_t bars = sbase + S_::kBars, k_full = bars + (SCALED ? kKFullWide : kKFull), k_free = bars + (SCALED ? kKFreeWide : kKFree);
   unsigned char* ctl = smem + S_::kBars;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + kTmemSlot);
   volatile uint32_t* abort_word = reinterpret_cast<volatile uint32_t*>(ctl + kAbort);
@@ -612,8 +682,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     return;                     // uniform over the grid: every block sees the same offset
   }
   if (tid == 0) {
-    for (int i = 0; i < KS; ++i) { mbar_init(bars + kKFull + 8 * i, SCALED ? 4 : 1); mbar_init(bars + kKFree + 8 * i, NT); }
-    for (int i = 0; i < VS; ++i) { mbar_init(bars + kVFull + 8 * i, SCALED ? 4 : 1); mbar_init(bars + kVFree + 8 * i, NT); }
+    // (K's codes: the bytes, and their scales made ready)
+    for (int i = 0; i < KS; ++i) { mbar_init(k_full + 8 * i, SCALED ? 2 : 1); mbar_init(k_free + 8 * i, NT); }
+    for (int i = 0; i < VS; ++i) { mbar_init(bars + kVFull + 8 * i, SCALED ? S_::kWiden : 1); mbar_init(bars + kVFree + 8 * i, NT); }
     for (int i = 0; i < 4; ++i) {
       mbar_init(bars + kSFull + 8 * i, 1);
       mbar_init(bars + kPFull + 8 * i, 4);              // one arrival per softmax warp
@@ -621,14 +692,11 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     for (int i = 0; i < 2; ++i) {
       mbar_init(bars + kOFull + 8 * i, 1);
     }
-    if constexpr (SCALED)
-      for (int i = 0; i < S_::RS; ++i) {                // (with K's tiles come the scales, of both)
-        mbar_init(bars + kRawFull + 8 * i, 1 + (64 >> min(a.page_log, 6)));
-        mbar_init(bars + kRawFull + 32 + 8 * i, 1);
-        mbar_init(bars + kRawFree + 8 * i, S_::kWiden);
-        mbar_init(bars + kRawFree + 32 + 8 * i, S_::kWiden);
-      }
-    mbar_init(bars + kQFull, 1);
+    if constexpr (SCALED) {
+      for (int i = 0; i < S_::RS; ++i) { mbar_init(bars + kRawFull + 8 * i, 1); mbar_init(bars + kRawFree + 8 * i, S_::kWiden); }
+      mbar_init(bars + kQRaw, 1);
+    }
+    mbar_init(bars + kQFull, SCALED ? S_::kWiden : 1);
     mbar_init(bars + kQFree, NT);                       // one arrival per row tile
     mbar_init(bars + kJoin, S_::kSoftmax);
     for (int i = 0; i < 8; ++i) { s_bad[i] = 0; mbar_init(bars + kTurn + 8 * i, 1); }
@@ -655,7 +723,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
                            x0 < x1 ? *reinterpret_cast<long long*>(ctl + kStartLeft) : 0ll, rb);
   Piece p;
   if (SCALED && warp >= S_::kSoftmax + 2 + NT) {
-    // ------------------------------------------------------------------ the warps that widen: 16 rows of every tile each
+    // ------------------------------------------------------ the warps that widen: 16 rows of every tile of V each
     constexpr int RS = S_::RS;
     const int me = warp - (S_::kSoftmax + 2 + NT);
     const uint32_t raw = sbase + S_::kRings;
@@ -663,70 +731,84 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     uint32_t full_parity = 0, free_parity = 1;          // (fresh operand slots count as free)
     bool ok = true;
     while (ok && walk.next(p)) {
+      // the piece's Q -> terms, a row a thread
+      ok = wait_warp(bars + kQRaw, piece & 1, abort_word);
+      if (!ok) break;
       ++piece;
+      const bool turns = p.rows <= 128;
+#pragma unroll 1
+      for (int s = 0; s < NT; ++s) {
+        const int r = me * 32 + lane;
+        if (r < p.rows - (turns ? 0 : s * 128))
+          reinterpret_cast<float*>(ctl + kQScales)[(piece & 3) * 256 + s * 128 + r] =
+              split_q<T, D>(sQ + s * S_::kQTile, sbase + S_::kThirds + s * S_::kThird, r);
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars + kQFull);
       int clear0, clear1;
       clear_tiles<BN>(a, p, clear0, clear1);
       for (int it = 0; it < p.len; ++it, ++n) {
         ok = wait_warp(bars + kRawFull + stage * 8, full_parity, abort_word) &&
-             (n < KS || wait_warp(bars + kKFree + slot * 8, free_parity, abort_word));
-        if (!ok) break;
-        widen<T, D, BN, false>(raw + stage * S_::kRaw, sK + slot * S_::kTile, me * 16);
-        if (me == 0 && lane < 8) {                      // K's scales of 16 keys each, then V's
-          float* to = reinterpret_cast<float*>(ctl + kScales + (n & 7) * 48);
-          const float s = rest_e4m3::within_limits(lds1(bars + kRawScales + stage * 32 + lane * 4));
-          if (lane < 4) {                               // (kept above 0 and finite: a masked score of -infinity stays it)
-            to[lane] = fminf(fmaxf(s * a.scale_log2, 0x1p-126f), 0x1p127f);
-          } else {
-            to[lane] = log2f(s);
-            to[lane + 4] = 1.f / s;
-          }
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) { mbar_arrive(bars + kKFull + slot * 8); mbar_arrive(bars + kRawFree + stage * 8); }
-        ok = wait_warp(bars + kRawFull + 32 + stage * 8, full_parity, abort_word) &&
              (n < VS || wait_warp(bars + kVFree + slot * 8, free_parity, abort_word));
         if (!ok) break;
         // NaN in tiles that not every row sees whole would reach rows that do not see its key (0 x NaN): it is taken
         // out, and the piece remembered if the key exists (the epilogue puts in what it comes to).  Elsewhere it
-        // stays and shows in O.  No tile is widened more than a few ahead, so eight pieces are told apart.
+        // stays and shows in O.  The next piece's tiles come behind its Q, so eight pieces are told apart.
         if (it >= clear0 && it < clear1) {
-          widen<TV, D, BN, false>(raw + (RS + stage) * S_::kRaw, sV + slot * S_::kTile, me * 16);
+          widen<TV, D, BN, false>(raw + stage * S_::kRaw, sV + slot * S_::kTile, me * 16);
         } else {
           const int rows = p.c.L + p.c.n - tile_key<BN>(p.c, p.t0 + it);
-          if (widen<TV, D, BN, true>(raw + (RS + stage) * S_::kRaw, sV + slot * S_::kTile, me * 16, rows)) {
+          if (widen<TV, D, BN, true>(raw + stage * S_::kRaw, sV + slot * S_::kTile, me * 16, rows)) {
             s_bad[piece & 7] = piece + 1;
             __threadfence_block();
           }
         }
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) { mbar_arrive(bars + kVFull + slot * 8); mbar_arrive(bars + kRawFree + 32 + stage * 8); }
-        static_assert(!SCALED || KS == VS, "one slot number for both rings");
+        if (lane == 0) { mbar_arrive(bars + kVFull + slot * 8); mbar_arrive(bars + kRawFree + stage * 8); }
         if (++stage == RS) { stage = 0; full_parity ^= 1; }
-        if (++slot == KS) { slot = 0; free_parity ^= 1; }
+        if (++slot == VS) { slot = 0; free_parity ^= 1; }
       }
     }
   } else if (warp == S_::kSoftmax || warp == S_::kSoftmax + 1) {
     // ------------------------------------------------------------------ K loader, V loader
     const bool is_v = warp == S_::kSoftmax + 1;
     const int stages = is_v ? VS : KS;
-    const uint32_t ring = is_v ? sV : sK, full = bars + (is_v ? kVFull : kKFull), free_ = bars + (is_v ? kVFree : kKFree);
+    const uint32_t ring = is_v ? sV : sK, full = is_v ? bars + kVFull : k_full, free_ = is_v ? bars + kVFree : k_free;
     const CUtensorMap* map = is_v ? &tm_v : &tm_k;
     const int box = min(1 << a.page_log, BN);           // rows of one box
     const int pg = lane / kHalves, half = lane % kHalves;               // (16-bit pages)
     const bool active = pg * box < BN;
     if constexpr (SCALED) {
       // A lane has a box (a page, or 64 rows of a larger one), so a warp works out the addresses of 8 to 32 tiles at once;
-      // then it goes through them, and only waits and starts copies.
-      constexpr int RS = S_::RS;
-      const uint32_t raw = sbase + S_::kRings + (is_v ? RS * S_::kRaw : 0), raw_full = bars + kRawFull + (is_v ? 32 : 0),
-                     raw_free = bars + kRawFree + (is_v ? 32 : 0);
+      // then it goes through them, and only waits and starts copies.  Scales come with K's tiles.
+      const uint32_t to_ring = is_v ? sbase + S_::kRings : sK, fulls = is_v ? bars + kRawFull : k_full, frees = is_v ? bars + kRawFree : k_free;
+      const int depth = is_v ? S_::RS : KS;
       const int box_log = min(a.page_log, 6), boxes_log = 6 - box_log, mine = lane >> boxes_log, at_once = 32 >> boxes_log;
       const int box0 = (lane & ((1 << boxes_log) - 1)) << box_log;        // the box's first row in its tile
-      int stage = 0, issued = 0;
+      int stage = 0, issued = 0, ready = 0;             // ready: tiles of K whose scales are
       uint32_t parity = 1, pieces = 0;                  // a fresh ring's stages count as free
       bool ok = true;
+      // K's scales of 16 keys each (lanes 0 ... 3), then V's, of the next tile whose copies have landed
+      auto make_ready = [&]() {
+        __syncwarp();
+        if (lane < 8) {
+          float* to = reinterpret_cast<float*>(ctl + kScales + (ready & 15) * 48);
+          const float s = rest_e4m3::within_limits(lds1(bars + kRawScales + (ready & 3) * 32 + lane * 4));
+          if (lane < 4) {                               // (within limits, so that with Q's scale it is above 0 and finite:
+            to[lane] = fminf(fmaxf(s * a.scale_log2, 0x1p-66f), 0x1p66f);   // a masked score of -infinity stays it)
+          } else {
+            float log_v;
+            asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(log_v) : "f"(s));
+            to[lane] = log_v;
+            to[lane + 4] = ex2(-log_v);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(fulls + ready % KS * 8);
+        ++ready;
+      };
       while (ok && walk.next(p)) {
         for (int it0 = 0; ok && it0 < p.len; it0 += at_once) {
           const int row = tile_key<BN>(p.c, p.t0 + min(it0 + mine, p.len - 1)) + box0, col = row >> a.page_log;
@@ -737,40 +819,49 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           const int64_t cell = bytes ? (((int64_t)page * a.H_kv + p.hk) << (a.page_log - 4)) + (in_page >> 4) : 0;
           const int n = min(at_once, p.len - it0);
           for (int j = 0; j < n; ++j) {
-            if (issued >= RS) ok = wait_warp(raw_free + stage * 8, parity, abort_word);
+            if (issued >= depth) ok = wait_warp(frees + stage * 8, parity, abort_word);
             if (!ok) break;
             if (mine == j) {
-              const uint32_t bar = raw_full + stage * 8;
+              const uint32_t bar = fulls + stage * 8;
               if (box0 == 0) mbar_expect_tx(bar, (uint32_t)S_::kRaw);
-              tma_page(raw + stage * S_::kRaw + box0 * D, map, 0, in_page, p.hk, page, a.slot, bar);
+              tma_page(to_ring + stage * S_::kRaw + box0 * D, map, 0, in_page, p.hk, page, a.slot, bar);
               if (!is_v) {                              // 16 bytes of either's scales for 64 keys
-                const uint32_t to = bars + kRawScales + stage * 32 + (box0 >> 2);
+                const uint32_t to = bars + kRawScales + (issued & 3) * 32 + (box0 >> 2);
                 copy_scales(box_log, to, a.k_scales + cell, bytes);
                 copy_scales(box_log, to + 16, a.v_scales + cell, bytes);
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
               }
             }
             __syncwarp();
             ++issued;
-            if (++stage == RS) { stage = 0; parity ^= 1; }
+            if (++stage == depth) { stage = 0; parity ^= 1; }
+            if (!is_v) {                                // the scales of two tiles before have landed meanwhile
+              asm volatile("cp.async.commit_group;" ::: "memory");
+              if (issued > 2) {
+                asm volatile("cp.async.wait_group 2;" ::: "memory");
+                make_ready();
+              }
+            }
             // The piece's Q, behind the first tiles (which do not wait for it): the last piece's S has to be done with it.
-            if (is_v && it0 + j + 1 == min(RS, p.len)) {
+            if (is_v && it0 + j + 1 == min(S_::RS, p.len)) {
               if (pieces > 0) ok = wait_warp(bars + kQFree, (pieces - 1) & 1, abort_word);
               if (!ok) break;
               ++pieces;
               load_q<T, D, NT, C>(a, p, rb, sQ, lane);
               asm volatile("cp.async.wait_all;" ::: "memory");
-              fence_async_smem();
               __syncwarp();
-              if (lane == 0) mbar_arrive(bars + kQFull);
+              if (lane == 0) mbar_arrive(bars + kQRaw);
             }
           }
         }
       }
-      if (*abort_word != 0u) {                          // as below
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        for (int i = max(0, issued - RS); i < issued; ++i) mbar_wait(raw_full + (i % RS) * 8, (uint32_t)((i / RS) & 1));
-      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      if (ok && !is_v)
+        while (ready < issued) make_ready();
+      if (*abort_word != 0u)                            // as below (K's barriers want an arrival more, which may not have come)
+        for (int i = max(0, issued - depth); i < issued; ++i) {
+          if (!is_v && i >= ready && lane == 0) mbar_arrive(fulls + i % depth * 8);
+          mbar_wait(fulls + i % depth * 8, (uint32_t)(i / depth & 1));
+        }
     } else {
       int slot = 0, filled = 0;
       uint32_t parity = 1;                                // a fresh ring's slots count as free
@@ -834,7 +925,11 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     const int s = warp - (S_::kSoftmax + 2);
     const uint32_t leader = elect_one();
     constexpr uint32_t idesc_s = idesc<T>(BN, 0), idesc_o = idesc<TV>(D, 1);
-    const uint64_t dq = umma_desc(sQ + s * S_::kQTile, 16, 1024), dk = umma_desc(sK, 16, 1024),
+    // e4m3 x e4m3 -> fp32 (format 0); where the third term lies behind the row tile's first
+    constexpr uint32_t idesc_q = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((128u >> 4) << 24);
+    constexpr int kPieces = Pieces<T, SCALED>::value;
+    const uint32_t third = S_::kThirds + s * S_::kThird - s * S_::kQTile;
+    const uint64_t dq = umma_desc(sQ + s * S_::kQTile, 16, 1024), dk = SCALED && D == 64 ? umma_desc64(sK, 512) : umma_desc(sK, 16, 1024),
                    dv = umma_desc(sV, BN * 128, 1024);
     const uint32_t t_s = tmem + 2 * s * BN, t_o = tmem + S_::kColO + s * 128;
     const uint32_t b_s = bars + kSFull + 16 * s, b_p = bars + kPFull + 16 * s, b_o = bars + kOFull + 8 * s;
@@ -846,19 +941,29 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       const int step = turns ? 2 : 1;
       auto qk = [&](int it) {                           // S of key tile `it`
         const uint32_t g = base + it, slot = g % KS, buf = n_s++ & 1;
-        ok = ok && wait_warp(bars + kKFull + slot * 8, (g / KS) & 1, abort_word);
+        ok = ok && wait_warp(k_full + slot * 8, (g / KS) & 1, abort_word);
         if (!ok) return;
         tc_fence_after();
         if (leader) {
+          if constexpr (SCALED) {                       // D = 64: the first two terms share rows of 128 bytes
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t qoff = (uint32_t)((ks >> 2) * (128 * 128) + (ks & 3) * 32);
-            const uint32_t koff = (uint32_t)((ks >> 2) * (BN * 128) + (ks & 3) * 32);
-            umma_f16(t_s + buf * BN, dq + (qoff >> 4), dk + ((slot * S_::kTile + koff) >> 4), idesc_s, ks > 0);
+            for (int piece = 0; piece < kPieces; ++piece)
+#pragma unroll
+              for (int ks = 0; ks < D / 32; ++ks) {
+                const uint32_t qoff = piece == 2 ? third + ks * 32 : piece * (D == 64 ? 64 : 128 * 128) + ks * 32;
+                umma_f8(t_s + buf * BN, dq + (qoff >> 4), dk + ((slot * S_::kKTile + ks * 32) >> 4), idesc_q, piece + ks > 0);
+              }
+          } else {
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint32_t qoff = (uint32_t)((ks >> 2) * (128 * 128) + (ks & 3) * 32);
+              const uint32_t koff = (uint32_t)((ks >> 2) * (BN * 128) + (ks & 3) * 32);
+              umma_f16(t_s + buf * BN, dq + (qoff >> 4), dk + ((slot * S_::kTile + koff) >> 4), idesc_s, ks > 0);
+            }
           }
           umma_commit(b_s + buf * 8);
-          umma_commit(bars + kKFree + slot * 8);
-          if (turns) umma_commit(bars + kKFree + slot * 8);      // for both row tiles
+          umma_commit(k_free + slot * 8);
+          if (turns) umma_commit(k_free + slot * 8);      // for both row tiles
           if (C == 1 && !turns && it + 1 == p.len) umma_commit(bars + kQFree);
         }
         __syncwarp();
@@ -921,7 +1026,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         mask0 = __ldg(mp);
         if (a.Wm > 1) mask0 |= (u64)__ldg(mp + 1) << 32;
       }
-      float m_used = -INFINITY, l_run = 0.f;
+      float m_used = -INFINITY, l_run = 0.f, q_scale = 1.f;
       int clear0, clear1;
       clear_tiles<BN>(a, p, clear0, clear1);
       int it = turns ? s : 0;
@@ -998,7 +1103,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           // 2^(score + log2 s_v - reference) and the sum of the probabilities takes it out again, 16 keys at a time.
           float ka[kParts], log_v[kParts], inv_v[kParts];
           if constexpr (SCALED) {
-            const uint32_t at = bars + kScales + ((base + it) & 7) * 48 + ci * kParts * 4;
+            if (fresh) q_scale = lds1(bars + kQScales + ((piece & 3) * 256 + s * 128 + t) * 4);
+            const uint32_t at = bars + kScales + ((base + it) & 15) * 48 + ci * kParts * 4;
             if constexpr (kParts == 4) {
               const float4 k4 = lds4(at), l4 = lds4(at + 16), i4 = lds4(at + 32);
               ka[0] = k4.x; ka[1] = k4.y; ka[2] = k4.z; ka[3] = k4.w;
@@ -1011,6 +1117,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
             mx = -INFINITY;
 #pragma unroll
             for (int c = 0; c < kParts; ++c) {
+              ka[c] *= q_scale;
               float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
               for (int j = 0; j < 8; ++j) top[j & 1] = max3(top[j & 1], __uint_as_float(x[c][2 * j]), __uint_as_float(x[c][2 * j + 1]));
@@ -1449,7 +1556,7 @@ rest_status launch_and_join(K kernel, const Args& a, const CUtensorMap& tm_k, co
 
 template <typename T, int D, int NT, int C, bool SCALED>
 rest_status run(const Args& a, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int smem_slot, cudaStream_t st) {
-  using S_ = Shape<D, NT, SCALED>;
+  using S_ = Shape<D, NT, Pieces<T, SCALED>::value>;
   REST_CUDA_TRY(rest::ensure_dynamic_smem(reinterpret_cast<const void*>(paged_attention_kernel<T, D, NT, C, SCALED>), smem_slot, S_::kSmem));
   return launch_and_join<T, D>(paged_attention_kernel<T, D, NT, C, SCALED>, a, tm_k, tm_v, S_::kThreads, S_::kSmem, st);
 }
@@ -1519,13 +1626,13 @@ rest_status attend(const void* d_q, const void* d_k_pages, const void* d_v_pages
   const int rows = page < 64 ? page : 64;               // of a box; a key tile has 64
   const CUtensorMapDataType type = SCALED ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                  : dtype == REST_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  const CUtensorMapSwizzle swizzle = !SCALED || (pl.few && D == 128) ? CU_TENSOR_MAP_SWIZZLE_128B
-                                     : pl.few ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE;
-  auto encode = [&](CUtensorMap* map, const void* base) {
+  auto encode = [&](CUtensorMap* map, const void* base, bool is_v) {           // (V's codes are no operand yet where they are widened)
+    const CUtensorMapSwizzle swizzle = SCALED && !pl.few && is_v ? CU_TENSOR_MAP_SWIZZLE_NONE
+                                       : SCALED && D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
     return encode_pool(map, base, type, SCALED ? 1 : 2, SCALED ? D : 64, swizzle, D, page, H_kv, P, strides + 3, rows, a.slot);
   };
   CUtensorMap tm_k, tm_v;
-  if (!encode(&tm_k, d_k_pages) || !encode(&tm_v, d_v_pages))
+  if (!encode(&tm_k, d_k_pages, false) || !encode(&tm_v, d_v_pages, true))
     return rest::note_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf16 = dtype == REST_BF16;

@@ -228,8 +228,8 @@ enum {
   kKFull = 0, kKFree = 32, kVFull = 64, kVFree = 112, kSFull = 160, kPFull = 192, kOFull = 224, kQFull = 240, kQFree = 248,
   kTmemSlot = 256, kAbort = 260, kBad = 264 /* 8 x 4 */, kStartB = 296, kStartOff = 304, kTotal = 312,
   kScan = 320 /* 12 x 8 */, kJoin = 416, kTurn = 424 /* 8 x 8 */, kStartLeft = 488,
-  // pages of codes: barriers of K's ring (8 each), of V's raw one (4 each), and of a piece's Q as it came
-  kKFullWide = 512, kKFreeWide = 576, kRawFull = 640, kRawFree = 672, kQRaw = 704,
+  // pages of codes: barriers of K's ring (8 each) and of V's raw one (4 each)
+  kKFullWide = 512, kKFreeWide = 576, kRawFull = 640, kRawFree = 672,
   // scales as they come (4 x 8 x 4) and as the softmax warps want them (16 x 48: of each 16 keys, what K's makes of a raw
   // score, in log2 units; the logarithm of V's; one over it), Q's scales (4 pieces x 256 rows)
   kRawScales = 720, kScales = 848, kScanWide = 1616, kQScales = 1760
@@ -515,53 +515,53 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64
 __device__ __forceinline__ uint64_t umma_desc64(uint32_t saddr, uint32_t sbo_bytes) {
   return (uint64_t)((saddr >> 4) & 0x3FFFu) | (1ull << 16) | ((uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (4ull << 61);
 }
-// Row r of a tile of Q becomes a sum of e4m3 terms, in place (the terms are half as wide): divided by the power of two that
-// fits its largest element (returned), what the first term leaves is at most a sixteenth of it, and so on.  Two terms hold
-// bf16's 8 bits, three fp16's 11, of elements down to 2^-11 of the row's largest; below, an element is off by 2^-19 of the largest
-// at most (2^-10, half of e4m3's smallest step, under 448), in three terms as well.  What is not finite makes the row NaN.
+// Row r of a tile of Q (x: as it lies in memory) as a sum of e4m3 terms: divided by the power of two that fits its largest
+// element (returned), which fp16 holds exactly; what the first term leaves is at most a sixteenth of it, and so on.  Two terms
+// hold bf16's 8 bits, three fp16's 11, of elements down to 2^-11 of the row's largest; below, an element is off by 2^-19 of
+// the largest at most (2^-10, half of e4m3's smallest step, under 448), in three terms as well.  What is not finite makes the
+// row NaN.  `copies`: tiles of Q that hold the row.
 template <typename T, int D>
-__device__ __forceinline__ float split_q(uint32_t tile, uint32_t third, int r) {
-  constexpr int kVecs = D / 8;                          // 16-byte chunks of the row, 8 to a half of the head
+__device__ __forceinline__ float split_q(const uint4 (&x)[D / 8], uint32_t tile, uint32_t third, int r, int copies) {
   auto at = [&](uint32_t base, int chunk) { return base + r * 128 + ((chunk ^ (r & 7)) << 4); };
-  uint32_t x[kVecs][4];
+  float2 most2 = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int c = 0; c < kVecs; ++c)
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[c][0]), "=r"(x[c][1]), "=r"(x[c][2]), "=r"(x[c][3])
-                 : "r"(at(tile + (c >> 3) * (128 * 128), c & 7)) : "memory");
-  float most = 0.f;
-#pragma unroll
-  for (int c = 0; c < kVecs; ++c)
+  for (int c = 0; c < D / 8; ++c) {
+    const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float2 f = Type<T>::unpack(x[c][j]);
-      most = fmaxf(most, fmaxf(fabsf(f.x) < INFINITY ? fabsf(f.x) : 0.f, fabsf(f.y) < INFINITY ? fabsf(f.y) : 0.f));
+      const float2 f = Type<T>::unpack(w[j] & 0x7FFF7FFFu);
+      most2 = make_float2(fmaxf(most2.x, f.x), fmaxf(most2.y, f.y));      // (NaN is passed over)
     }
-  const float scale = rest_e4m3::fitting_scale(most), inverse = 1.f / scale;
+  }
+  const float most = fmaxf(most2.x, most2.y), scale = rest_e4m3::fitting_scale(most), inverse = most < INFINITY ? 1.f / scale : NAN;
 #pragma unroll
-  for (int c = 0; c < kVecs / 2; ++c) {                 // 16 elements: a chunk of each term
-    uint32_t hi[4], lo[4], end[4];
+  for (int c = 0; c < D / 16; ++c) {                    // 16 elements: a chunk of each term
+    uint32_t term[3][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float2 f0 = Type<T>::unpack(x[2 * c + (j >> 1)][2 * (j & 1)]), f1 = Type<T>::unpack(x[2 * c + (j >> 1)][2 * (j & 1) + 1]);
-      float v[4] = {f0.x * inverse, f0.y * inverse, f1.x * inverse, f1.y * inverse};
+      const uint4 v = x[2 * c + (j >> 1)];
+      const float2 f0 = Type<T>::unpack(j & 1 ? v.z : v.x), f1 = Type<T>::unpack(j & 1 ? v.w : v.y);
+      __half2 h0 = __floats2half2_rn(f0.x * inverse, f0.y * inverse), h1 = __floats2half2_rn(f1.x * inverse, f1.y * inverse);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = fabsf(v[e]) < INFINITY ? v[e] : NAN;
-      auto take = [&]() -> uint32_t {                   // the nearest codes, taken off
-        const uint32_t a = rest_e4m3::pack2(v[0], v[1]), b = rest_e4m3::pack2(v[2], v[3]);
-        const float2 g = rest_e4m3::unpack2(a), h = rest_e4m3::unpack2(b);
-        v[0] -= g.x; v[1] -= g.y; v[2] -= h.x; v[3] -= h.y;
-        return a | b << 16;
-      };
-      hi[j] = take();
-      lo[j] = take();
-      if constexpr (__is_same(T, __half)) end[j] = take();
+      for (int k = 0; k < (__is_same(T, __half) ? 3 : 2); ++k) {          // the nearest codes, taken off
+        const __nv_fp8x2_storage_t a = __nv_cvt_halfraw2_to_fp8x2(h0, __NV_SATFINITE, __NV_E4M3),
+                                   b = __nv_cvt_halfraw2_to_fp8x2(h1, __NV_SATFINITE, __NV_E4M3);
+        term[k][j] = (uint32_t)a | (uint32_t)b << 16;
+        h0 = __hsub2(h0, __half2(__nv_cvt_fp8x2_to_halfraw2(a, __NV_E4M3)));
+        h1 = __hsub2(h1, __half2(__nv_cvt_fp8x2_to_halfraw2(b, __NV_E4M3)));
+      }
     }
     auto put = [&](uint32_t to, const uint32_t (&w)[4]) {
       asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
     };
-    put(at(tile, c), hi);
-    put(D == 64 ? at(tile, 4 + c) : at(tile + 128 * 128, c), lo);
-    if constexpr (__is_same(T, __half)) put(at(third, c), end);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (k < copies) {
+        const uint32_t to = tile + k * (128 * D * 2);
+        put(at(to, c), term[0]);
+        put(D == 64 ? at(to, 4 + c) : at(to + 128 * 128, c), term[1]);
+        if constexpr (__is_same(T, __half)) put(at(third + k * (128 * 128), c), term[2]);
+      }
   }
   return scale;
 }
@@ -694,7 +694,6 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     }
     if constexpr (SCALED) {
       for (int i = 0; i < S_::RS; ++i) { mbar_init(bars + kRawFull + 8 * i, 1); mbar_init(bars + kRawFree + 8 * i, S_::kWiden); }
-      mbar_init(bars + kQRaw, 1);
     }
     mbar_init(bars + kQFull, SCALED ? S_::kWiden : 1);
     mbar_init(bars + kQFree, NT);                       // one arrival per row tile
@@ -731,18 +730,29 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
     uint32_t full_parity = 0, free_parity = 1;          // (fresh operand slots count as free)
     bool ok = true;
     while (ok && walk.next(p)) {
-      // the piece's Q -> terms, a row a thread
-      ok = wait_warp(bars + kQRaw, piece & 1, abort_word);
+      // The piece's Q as terms, a row a thread.  It is read while the last products of the piece before still want their Q.
+      const bool turns = p.rows <= 128;                 // both row tiles hold the rows
+#pragma unroll 1
+      for (int s = 0; s < (turns ? 1 : 2); ++s) {
+        const int r = me * 32 + lane, row = s * 128 + r;
+        uint4 x[D / 8];
+        if (row < p.rows) {
+          const int at = rb * S_::kRows + row, node = node_of(a, at);
+          const uint4* q = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + p.b * a.q_b + node * a.q_n +
+                                                          (int64_t)(p.hk * a.G + at - node * a.G) * a.q_h);
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c) x[c] = __ldg(q + c);
+        }
+        if (s == 0 && piece > 0) ok = wait_warp(bars + kQFree, (piece - 1) & 1, abort_word);
+        if (!ok) break;
+        if (row < p.rows) {
+          float* scales = reinterpret_cast<float*>(ctl + kQScales) + ((piece + 1) & 3) * 256 + row;
+          scales[0] = split_q<T, D>(x, sQ + s * S_::kQTile, sbase + S_::kThirds + s * S_::kThird, r, turns ? 2 : 1);
+          if (turns) scales[128] = scales[0];
+        }
+      }
       if (!ok) break;
       ++piece;
-      const bool turns = p.rows <= 128;
-#pragma unroll 1
-      for (int s = 0; s < NT; ++s) {
-        const int r = me * 32 + lane;
-        if (r < p.rows - (turns ? 0 : s * 128))
-          reinterpret_cast<float*>(ctl + kQScales)[(piece & 3) * 256 + s * 128 + r] =
-              split_q<T, D>(sQ + s * S_::kQTile, sbase + S_::kThirds + s * S_::kThird, r);
-      }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bars + kQFull);
@@ -788,7 +798,7 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       const int box_log = min(a.page_log, 6), boxes_log = 6 - box_log, mine = lane >> boxes_log, at_once = 32 >> boxes_log;
       const int box0 = (lane & ((1 << boxes_log) - 1)) << box_log;        // the box's first row in its tile
       int stage = 0, issued = 0, ready = 0;             // ready: tiles of K whose scales are
-      uint32_t parity = 1, pieces = 0;                  // a fresh ring's stages count as free
+      uint32_t parity = 1;                              // a fresh ring's stages count as free
       bool ok = true;
       // K's scales of 16 keys each (lanes 0 ... 3), then V's, of the next tile whose copies have landed
       auto make_ready = [&]() {
@@ -840,16 +850,6 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
                 asm volatile("cp.async.wait_group 2;" ::: "memory");
                 make_ready();
               }
-            }
-            // The piece's Q, behind the first tiles (which do not wait for it): the last piece's S has to be done with it.
-            if (is_v && it0 + j + 1 == min(S_::RS, p.len)) {
-              if (pieces > 0) ok = wait_warp(bars + kQFree, (pieces - 1) & 1, abort_word);
-              if (!ok) break;
-              ++pieces;
-              load_q<T, D, NT, C>(a, p, rb, sQ, lane);
-              asm volatile("cp.async.wait_all;" ::: "memory");
-              __syncwarp();
-              if (lane == 0) mbar_arrive(bars + kQRaw);
             }
           }
         }
@@ -1035,8 +1035,9 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
       // Left alone they fall into step, both at their exponentials and then both at everything else; taking
       // turns at the exponentials (the first tile before the second, the second before the first's next)
       // keeps the special function unit fed.  A turn ends half way: the second half fills the other's start
-      // (768 us at the end, 748 us half way, 845 us after a quarter, for 16 x 16384 keys and 640 rows).
-      const bool paired = NT == 2 && !turns && (warp & 3) * 32 + 128 < p.rows;
+      // (768 us at the end, 748 us half way, 845 us after a quarter, for 16 x 16384 keys and 640 rows).  With pages of codes
+      // there are other warps to fill in: 860 us in turns, 848 without.
+      const bool paired = !SCALED && NT == 2 && !turns && (warp & 3) * 32 + 128 < p.rows;
       const uint32_t my_turn = bars + kTurn + 8 * (warp & 7), other_turn = bars + kTurn + 8 * ((warp & 7) ^ 4);
       for (bool fresh = true; it < p.len; it += step, fresh = false) {
         const uint32_t buf = 2 * s + (n & 1);

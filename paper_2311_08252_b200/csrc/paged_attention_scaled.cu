@@ -14,7 +14,7 @@ namespace {
 
 // ------------------------------------------------------------------------- up to 16 rows a KV head
 // Few rows make the K/V stream all that counts, and 128-row matrix instructions would read a tile of Q that is nearly
-// empty from shared memory for every 64 keys.  Here two warps fetch key tiles by TMA into a ring (176 to 192 KB of
+// empty from shared memory for every 64 keys.  Here two warps fetch key tiles by TMA into a ring (128 to 192 KB of
 // keys on their way), and the others take 16 keys at a time (one scale of K and one of V), four warps a tile: they widen the
 // codes in registers and feed them to m16n8k16 instructions as the operand with 16 rows, S^T = K Q^T and O^T = V^T P^T,
 // with 8 query rows (or 16, two columns of tiles) as the other one.  Each has maxima, sums and O of its own; they
@@ -27,12 +27,17 @@ namespace {
 template <int D, int NB> struct Few {
   static constexpr int kWarps = NB == 1 ? 12 : 8, kTeams = kWarps / 4, kThreads = 32 * (kWarps + 2), kRows = 8 * NB;
   static constexpr int kTile = 64 * D, kStage = 2 * kTile;                // bytes of 64 keys of K, and of K and V
-  static constexpr int kStages = (NB == 1 ? 12 : 11) * (128 / D);
+  // A stage belongs to one team (a multiple of the teams): whoever waits for a stage's next tile has seen the one before, so
+  // that the parity of its barrier says which of the two has landed.
+  static constexpr int kStages = D == 64 ? (NB == 1 ? 18 : 16) : NB == 1 ? 12 : 10;
+  static_assert(kStages % kTeams == 0, "a stage belongs to one team");
   static constexpr int kRing = kStages * kStage;
-  static constexpr int kCopies = kWarps / 2;                              // of O in the join
+  // O's copies in the join: D = 64 has room for every warp's at once; with D = 128 half of the warps leave theirs for the
+  // others to add to, and the ring keeps its length (256 tokens x 4096 keys: 261 us; all at once and a ring of 9: 303 us)
+  static constexpr int kCopies = D == 64 ? kWarps : kWarps / 2;
   static constexpr int kRowStride = D + 8;                                // floats: rows two apart meet different banks
   static constexpr int kMerge = kRing, kMl = kMerge + kCopies * kRows * kRowStride * 4;    // [2][kWarps][kRows] float2
-  static constexpr int kScale = kMl + 2 * kWarps * kRows * 8;             // [kStages] {K's of 16 keys each, V's}
+  static constexpr int kScale = kMl + 2 * kWarps * kRows * 8;         // [kStages] {K's of 16 keys each, V's}
   static constexpr int kFull = kScale + kStages * 32, kFree = kFull + kStages * 8;
   static constexpr int kCtl = (kFree + kStages * 8 + 15) / 16 * 16;
   static constexpr int kScanAt = 512;                                     // of the control words: a sum of each warp
@@ -65,17 +70,26 @@ __device__ __forceinline__ bool without_nan(uint32_t& w) {
   w &= ~(nan * 0xFFu);
   return nan != 0;
 }
-// which of the 16 keys from key0 on packed row r of a piece sees
-__device__ __noinline__ uint32_t sees(const Args& a, Ctx ctx, int b, int rows, int r, int key0) {
-  if (r >= rows) return 0u;
-  const int node = node_of(a, r);
-  u64 mask0 = 0;
-  if (a.mask) {
-    const uint32_t* mp = a.mask + ((int64_t)b * a.N + node) * a.Wm;
-    mask0 = __ldg(mp);
-    if (a.Wm > 1) mask0 |= (u64)__ldg(mp + 1) << 32;
+// Whether packed row r sees key `key` (bit 0) and key + 8 (bit 1).  No more than 16 rows means no more than 16 nodes, so one
+// word of the mask says what it sees of them; only where a path may be longer than the window have they positions of
+// their own.  (A call: inside the loop its values would push others out of the registers.)
+__device__ __noinline__ uint32_t sees(const Args& a, Ctx ctx, int b, int rows, int r, int key) {
+  const int node = node_of(a, min(r, rows - 1));
+  const uint32_t word = (a.mask ? __ldg(a.mask + (int64_t)b * a.N + node) : (2u << node) - 1u) & ((1u << a.N) - 1u);
+  uint32_t seen;
+  if (a.window > 0 && a.window < a.N) {
+    const int key0 = key & ~63;
+    const u64 v = visible(a, ctx, b, node, node_depth(a, b, node), word, key0) >> (key - key0);
+    seen = (uint32_t)(v & 1u) | (uint32_t)(v >> 8 & 1u) << 1;
+  } else {
+    const int from = a.window > 0 ? max(ctx.L + max(__popc(word), 1) - a.window, 0) : 0;   // first position in its window
+    auto one = [&](int k) -> uint32_t {
+      const bool before = k >= from || k < a.sinks, node_seen = k < ctx.L + ctx.n && (word >> (k - ctx.L & 31) & 1u);
+      return k < ctx.L ? before : node_seen;
+    };
+    seen = one(key) | one(key + 8) << 1;
   }
-  return (uint32_t)visible(a, ctx, b, node, a.window > 0 ? node_depth(a, b, node) : 1, mask0, key0) & 0xFFFFu;
+  return r < rows ? seen : 0u;
 }
 
 template <typename T, int D, int NB>
@@ -169,35 +183,47 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
   }
 
   // -------------------------------------------------------------------- the others
-  const int team = warp >> 2, sub = warp & 3;           // tiles team, team + TEAMS ... of a piece, keys 16 sub ... of each
-  auto meet = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(32 * W) : "memory"); };
+  const int team = warp >> 2, sub = warp & 3;           // every TEAMS-th tile, keys 16 sub ... of it
+  auto meet = [&]() {                                   // (counts threads, not warps: lanes need not come together)
+    __syncwarp();
+    asm volatile("barrier.sync 1, %0;" ::"n"(32 * W) : "memory");
+  };
   uint32_t base = 0;                                    // tiles before this piece
   bool dead = false;                                    // a wait gave up; the barriers of the block are still kept
+  // a piece's rows of Q as they lie in memory (this lane's D / 4 elements of rows g, g + 8)
+  uint4 raw[NB][D / 32];
+  auto look = [&]() {
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+      const int r = t * 8 + g;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) raw[t][i] = make_uint4(0u, 0u, 0u, 0u);
+      if (r < p.rows) {
+        const int node = node_of(a, r);
+        const T* from = static_cast<const T*>(a.q) + p.b * a.q_b + node * a.q_n + (int64_t)(p.hk * a.G + r - node * a.G) * a.q_h + c * (D / 4);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) raw[t][i] = __ldg(reinterpret_cast<const uint4*>(from) + i);
+      }
+    }
+  };
   int piece = 0;
   while (walk.next(p)) {
     ++piece;
+    look();
     // ---- Q as the second operand: fp16 under a power of two for each row (bf16 has fewer bits and more range)
     uint32_t q[NB][2 * kWords][2];                      // [.][k step][.]
     float mult[NB][2];                                  // what makes log2 units of a row's raw scores, but for K's scale
 #pragma unroll
     for (int t = 0; t < NB; ++t) {
-      const int r = t * 8 + g;
       float x[D / 4], most = 0.f;
 #pragma unroll
-      for (int i = 0; i < D / 4; ++i) x[i] = 0.f;
-      if (r < p.rows) {
-        const int node = node_of(a, r);
-        const T* from = static_cast<const T*>(a.q) + p.b * a.q_b + node * a.q_n + (int64_t)(p.hk * a.G + r - node * a.G) * a.q_h + c * (D / 4);
+      for (int i = 0; i < D / 32; ++i) {
+        const uint32_t w[4] = {raw[t][i].x, raw[t][i].y, raw[t][i].z, raw[t][i].w};
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          const uint4 v = *reinterpret_cast<const uint4*>(from + 8 * i);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 f = Type<T>::unpack(w[j]);
-            x[8 * i + 2 * j] = f.x;
-            x[8 * i + 2 * j + 1] = f.y;
-          }
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = Type<T>::unpack(w[j]);
+          x[8 * i + 2 * j] = f.x;
+          x[8 * i + 2 * j + 1] = f.y;
         }
       }
       float up = 1.f, own = a.scale_log2;
@@ -232,10 +258,12 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
     int clear0, clear1;
     clear_tiles<64>(a, p, clear0, clear1);
     const int end = p.c.L + p.c.n;
-    uint32_t slot = (base + team) % S, parity = (base + team) / S & 1;
+    // (by the tile's number among all that the block has fetched, so that a stage stays with its team from piece to piece)
+    const uint32_t start = (team + TEAMS - base % TEAMS) % TEAMS;
+    uint32_t slot = (base + start) % S, parity = (base + start) / S & 1;
     base += p.len;
 #pragma unroll 1
-    for (int it = team; it < p.len; it += TEAMS) {
+    for (int it = start; it < p.len; it += TEAMS) {
       const int key0 = tile_key<64>(p.c, p.t0 + it) + sub * 16;
       if (!dead && !wait_warp(full + 8 * slot, parity, abort_word)) dead = true;
       if (dead) break;
@@ -245,6 +273,7 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
       if (slot >= S) { slot -= S; parity ^= 1; }
       if (key0 >= end) {                                // no such keys
         if (lane == 0) mbar_arrive(bar);
+        __syncwarp();
         continue;
       }
       // ---- S^T: 16 keys x 8 rows, even and odd steps apart (half the chain of dependent products)
@@ -284,6 +313,7 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
       }
       __syncwarp();                                     // the tile's part is read
       if (lane == 0) mbar_arrive(bar);
+      __syncwarp();
       // ---- probabilities, as in the kernel above: the scale of V rides in the exponent
       sk = rest_e4m3::within_limits(sk);
       float log_v;
@@ -303,9 +333,9 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
         for (int t = 0; t < NB; ++t)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const uint32_t vis = sees(a, p.c, p.b, p.rows, t * 8 + 2 * c + j, key0) >> g;
-            if (!(vis & 1u)) y[t][j] = -INFINITY;
-            if (!(vis & 0x100u)) y[t][2 + j] = -INFINITY;
+            const uint32_t seen = sees(a, p.c, p.b, p.rows, t * 8 + 2 * c + j, key0 + g);
+            if (!(seen & 1u)) y[t][j] = -INFINITY;
+            if (!(seen & 2u)) y[t][2 + j] = -INFINITY;
           }
         bool found = false;                             // NaN would reach rows that do not see its key (0 x NaN)
 #pragma unroll
@@ -316,6 +346,7 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
           found |= any && key0 + 2 * c + (j & 1) + (j >> 1) * 8 < end;
         }
         if (found) s_bad[piece & 7] = piece + 1;
+        __syncwarp();                                   // (what follows is for the whole warp)
       }
       bool over = false;
 #pragma unroll
@@ -367,7 +398,7 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
       }
     }
 
-    // ---- the eight warps' rows are joined: maxima and sums first (in turns of two: a warp may be a piece ahead)
+    // ---- the warps' rows are joined: maxima and sums (in turns of two: a warp may be a piece ahead), then O
     float2* ml = reinterpret_cast<float2*>(smem + F::kMl) + (piece & 1) * W * F::kRows;
 #pragma unroll
     for (int t = 0; t < NB; ++t)
@@ -377,20 +408,24 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
         for (int d = 4; d < 32; d <<= 1) l[t][j] += __shfl_xor_sync(0xFFFFFFFFu, l[t][j], d);
         if (g == 0) ml[warp * F::kRows + t * 8 + 2 * c + j] = make_float2(m[t][j], l[t][j]);
       }
-    meet();
-    // half of the warps leave their rows, the others add theirs and leave the sums
+    meet();                                             // (all are done with the O's of the join before, too)
+    // where every warp's O has room it is left as it is; else both halves weigh theirs and the second adds to the first
+    constexpr bool kAll = F::kCopies == W;
 #pragma unroll
-    for (int round = 0; round < 2; ++round) {
-      if ((warp >= F::kCopies) == (round == 0)) {
+    for (int round = 0; round < (kAll ? 1 : 2); ++round) {
+      if (kAll || (warp >= F::kCopies) == (round == 0)) {
 #pragma unroll
         for (int t = 0; t < NB; ++t)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const int r = t * 8 + 2 * c + j;
-            float top = -INFINITY;
+            float weight = 1.f;
+            if (!kAll) {
+              float top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w * F::kRows + r].x);
-            const float weight = m[t][j] == -INFINITY ? 0.f : ex2(m[t][j] - top);
+              for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w * F::kRows + r].x);
+              weight = m[t][j] == -INFINITY ? 0.f : ex2(m[t][j] - top);
+            }
             // columns 2e, 2e + 1 of this lane's D / 8 stand at e * 16 + 2 g
             float* to = reinterpret_cast<float*>(smem + F::kMerge) + (warp % F::kCopies * F::kRows + r) * F::kRowStride + 2 * g;
 #pragma unroll
@@ -416,18 +451,18 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
 #pragma unroll
       for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w * F::kRows + r].x);
 #pragma unroll
-      for (int w = 0; w < W; ++w) {                     // (a maximum passes NaN over; the sum says so)
-        const float2 v = ml[w * F::kRows + r];
-        sum += v.y * (v.x == -INFINITY ? 0.f : ex2(v.x - top));
-      }
-#pragma unroll
-      for (int w = 0; w < F::kCopies; ++w) {
+      for (int w = 0; w < W; ++w) {
+        const float2 v = ml[w * F::kRows + r];          // (a maximum passes NaN over; the sum says so)
+        const float weight = v.x == -INFINITY ? 0.f : ex2(v.x - top);
+        sum = fmaf(v.y, weight, sum);
+        if (w >= F::kCopies) continue;
         const float* from = reinterpret_cast<const float*>(smem + F::kMerge) + (w * F::kRows + r) * F::kRowStride + 2 * gg;
 #pragma unroll
         for (int e = 0; e < D / 64; ++e) {
           const float2 f = *reinterpret_cast<const float2*>(from + (part * (D / 64) + e) * 16);
-          y[2 * e] += f.x;
-          y[2 * e + 1] += f.y;
+          // (a warp without keys has weight 0 and an O of 0)
+          y[2 * e] = fmaf(f.x, kAll ? weight : 1.f, y[2 * e]);
+          y[2 * e + 1] = fmaf(f.y, kAll ? weight : 1.f, y[2 * e + 1]);
         }
       }
       const int node = node_of(a, r), head = p.hk * a.G + r - node * a.G, col = gg * (D / 8) + part * (D / 32);

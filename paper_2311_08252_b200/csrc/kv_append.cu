@@ -14,10 +14,16 @@
 // (by a power of two, so they change only where they fall below the smallest code).
 //
 // A thread block takes new rows of one context that fall into one block of 16 rows.  A row is D / 16 lanes, 16
-// elements each (a pair's halves sit in the same lane); a lane stays with its row, keeps its sines and cosines in
-// registers and steps through the heads, four of them on their way at a time.  A block of codes is a warp, which
-// holds all its rows' values while it looks for the largest; the angles of its thread block's rows are computed once,
-// into shared memory.  What bounds it is HBM for many rows, and for few rows the launch and the chain length -> table -> page.
+// elements each (a pair's halves sit in the same lane, unless half the head is no multiple of 8); a lane stays with its
+// row, keeps its sines and cosines in registers and steps through the heads, four of them on their way at a time.  One
+// head's keys or values of a block of codes are a warp's, which holds all its rows' values while it looks for the largest;
+// the angles of its thread block's rows are computed once, into shared memory.
+//
+// What bounds it, for few rows: the launch and the chain length -> table -> page (one row: 4.3 us with codes or without).
+// For many, measured with 128 x up to 64 rows, D = 128, 32 heads of queries and 8 of keys and values: the rotation of
+// queries alone 28 us (4.8 TB/s) and 16-bit pages are bound by HBM; codes take 49 us, of which half are the 64-bit
+// products (64 a clock and SM) and conversions to and from them (16) of keys.  With 61 pairs, half the head apart, 62 us
+// and 95 us: shifting the partners into place is bound by the instructions it takes.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -80,15 +86,11 @@ template <typename T> struct Eight {
     }
   }
 };
-template <typename T> __device__ __forceinline__ void load8(const T* p, float* x) {
+template <typename T> __device__ __forceinline__ Eight<T> packed(const float* x) {
   Eight<T> e;
-  e.load(p);
-  e.to(x);
-}
-template <typename T> __device__ __forceinline__ void store8(T* p, const float* x) {
   if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    e.v[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    e.v[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
   } else {
     uint32_t w[4];
 #pragma unroll
@@ -101,23 +103,84 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float* 
         w[i] = *reinterpret_cast<const uint32_t*>(&h);
       }
     }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    e.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return e;
+}
+// y's elements from `live` on, an even number, are x's, bit for bit.
+template <typename T> __device__ __forceinline__ void keep(Eight<T>& y, const Eight<T>& x, int live) {
+  constexpr int kPerWord = 4 / (int)sizeof(T);
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+    if (kPerWord * (4 * i) >= live) y.v[i].x = x.v[i].x;
+    if (kPerWord * (4 * i + 1) >= live) y.v[i].y = x.v[i].y;
+    if (kPerWord * (4 * i + 2) >= live) y.v[i].z = x.v[i].z;
+    if (kPerWord * (4 * i + 3) >= live) y.v[i].w = x.v[i].w;
   }
 }
-template <typename T> __device__ __forceinline__ float load1(const T* p) { return (float)*p; }
+// Elements s .. s + 7 of the 16 in a and b.
+template <typename T> __device__ __forceinline__ Eight<T> shifted(const Eight<T>& a, const Eight<T>& b, int s) {
+  constexpr int kWords = 2 * (int)sizeof(T), kPerWord = 4 / (int)sizeof(T);
+  uint32_t w[2 * kWords];
+#pragma unroll
+  for (int i = 0; i < kWords / 4; ++i) {
+    w[4 * i] = a.v[i].x, w[4 * i + 1] = a.v[i].y, w[4 * i + 2] = a.v[i].z, w[4 * i + 3] = a.v[i].w;
+    w[kWords + 4 * i] = b.v[i].x, w[kWords + 4 * i + 1] = b.v[i].y, w[kWords + 4 * i + 2] = b.v[i].z, w[kWords + 4 * i + 3] = b.v[i].w;
+  }
+#pragma unroll
+  for (int by = kWords / 2; by > 0; by >>= 1)
+#pragma unroll
+    for (int i = 0; i + by < 2 * kWords; ++i) w[i] = (s / kPerWord) & by ? w[i + by] : w[i];
+  if constexpr (kPerWord == 2) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16 * (s & 1));
+  }
+  Eight<T> out;
+#pragma unroll
+  for (int i = 0; i < kWords / 4; ++i) out.v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  return out;
+}
 
 // A lane's 16 elements of a row, in two runs of 8 from at[0] and at[1].  kPairs: a pair's halves lie in the same place
-// of both runs (half the head apart); kNeighbours: pairs are neighbours; kStill: nothing turns; kLoose: runs of 8 do not
-// meet their partners, or some pairs turn and some do not (elements are worked out one by one).
+// of both runs (half the head apart); kNeighbours: pairs are neighbours (where their number is no multiple of 8, only the
+// first of them may turn); kStill: nothing turns; kLoose: half the head is no multiple of 8, so that runs of 8 do not meet
+// their partners (class Loose).
 enum Kind { kPairs, kNeighbours, kStill, kLoose };
 struct Lane { Kind kind; int at[2], first; };           // first: of kPairs and kNeighbours, the first pair's number
 __device__ __forceinline__ Lane lane_of(const Args& a, int chunk) {
   const int at = 16 * chunk, pairs = a.half >> 3;
-  if (at >= 2 * a.half && !(a.half & 7)) return {kStill, {at, at + 8}, 0};
-  if (a.half & 7) return {at >= 2 * a.half ? kStill : kLoose, {at, at + 8}, 0};
-  if (a.interleaved) return {kNeighbours, {at, at + 8}, 8 * chunk};
+  if (a.interleaved || (a.half & 7)) return {at >= 2 * a.half ? kStill : a.interleaved ? kNeighbours : kLoose, {at, at + 8}, 8 * chunk};
   return chunk < pairs ? Lane{kPairs, {8 * chunk, a.half + 8 * chunk}, 8 * chunk} : Lane{kStill, {at, at + 8}, 0};
 }
+// What a lane of kLoose does with element j of its 16, at + j of the row: y = x cos + partner sin, the sine's sign being
+// that of its half of the pair.
+struct Loose {
+  int at, half;
+  __device__ __forceinline__ Loose(const Args& a, const Lane& l) : at(l.at[0]), half(a.half) {}
+  __device__ __forceinline__ bool turns(int j) const { return at + j < 2 * half; }
+  __device__ __forceinline__ bool second(int j) const { return at + j >= half; }
+  __device__ __forceinline__ int pair(int j) const { return at + j - (second(j) ? half : 0); }
+  // The partners of run k (0 or 1), half the head away: aligned loads on both sides, shifted.  Two sets where the run
+  // holds the end of the first half.
+  template <typename T> __device__ __forceinline__ void partners(const T* row, int k, int D, float (&p)[8]) const {
+    const int e = at + 8 * k;
+    run(row, e + (e >= half ? -half : half), D, p);
+    if (e < half && e + 8 > half) {
+      float x[8];
+      run(row, e - half, D, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] = e + j >= half ? x[j] : p[j];
+    }
+  }
+  // elements from .. from + 7 of a row, 0 outside of it
+  template <typename T> static __device__ __forceinline__ void run(const T* row, int from, int D, float (&x)[8]) {
+    const int base = from & ~7;
+    Eight<T> lo = {}, hi = {};
+    if (base >= 0 && base < D) lo.load(row + base);
+    if (base + 8 >= 0 && base + 8 < D) hi.load(row + base + 8);
+    shifted(lo, hi, from & 7).to(x);
+  }
+};
 // Cosine and sine of pair f of a row at position p, times the amplitude, in 32 bits: whole quarter turns are taken off in
 // 64, and what is left, |x| <= pi / 4, goes through the Taylor series, whose next terms are below 2^-29 (x^11 / 11!,
 // x^12 / 12!).
@@ -174,20 +237,6 @@ __device__ __forceinline__ void rotate(const Angles<F>& t, const float (&x)[16],
     y[kStep * j + kApart] = round(fma(x2, c, x1 * s));
   }
 }
-// Element e of a row whose pairs are loose: its pair, whether it is the first of it, and where the other one is.
-struct Loose { int pair, other; bool low; };
-__device__ __forceinline__ Loose loose(const Args& a, int e) {
-  if (a.interleaved) return {e >> 1, e ^ 1, !(e & 1)};
-  return e < a.half ? Loose{e, e + a.half, true} : Loose{e - a.half, e - a.half, false};
-}
-
-template <typename T>
-__device__ __noinline__ double loose64(const Args& a, const T* row, int e, float x, const double2* table, int r) {
-  const Loose o = loose(a, e);
-  const double2 cs = table[table_at(a, r, o.pair)];
-  const double other = load1(row + o.other);
-  return o.low ? fma((double)x, cs.x, -(other * cs.y)) : fma((double)x, cs.x, other * cs.y);
-}
 // A lane's 16 elements of a new row as they become codes: rotated in 64 bits, rounded to 32.
 template <bool LOOSE, typename T, typename R>
 __device__ __forceinline__ void code_values(const Args& a, const Eight<T> (&e)[2], const T* row, const Lane& l, const double2* table,
@@ -198,12 +247,35 @@ __device__ __forceinline__ void code_values(const Args& a, const Eight<T> (&e)[2
   if (l.kind == kStill) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) y[j] = x[j];
-  } else if (LOOSE) {
+  } else if (LOOSE && l.kind == kLoose) {
+    const Loose o(a, l);
 #pragma unroll
-    for (int j = 0; j < 16; ++j)                        // (an index that is no constant would put y into local memory)
-      y[j] = l.at[0] + j < 2 * a.half ? round(loose64(a, row, l.at[0] + j, x[j], table, r)) : x[j];
+    for (int k = 0; k < 2; ++k) {
+      float p[8];
+      o.partners(row, k, a.D, p);
+#pragma unroll
+      for (int j = 8 * k; j < 8 * k + 8; ++j) {
+        y[j] = x[j];
+        if (o.turns(j)) {
+          const double2 cs = table[table_at(a, r, o.pair(j))];
+          y[j] = round(fma((double)x[j], cs.x, (double)p[j & 7] * (o.second(j) ? cs.y : -cs.y)));
+        }
+      }
+    }
   } else {
     Angles<double> t;
+    if (LOOSE) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const double2 cs = table[table_at(a, r, min(l.first + j, a.half - 1))];
+        t.c[j] = cs.x;
+        t.s[j] = cs.y;
+      }
+      rotate<true>(t, x, y, round);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) y[j] = l.at[0] + j < 2 * a.half ? y[j] : x[j];
+      return;
+    }
     const double2* twos = table + table_at(a, r, l.first);
     const int apart = a.half >> 2;                      // (see table_at)
 #pragma unroll
@@ -241,7 +313,6 @@ __device__ __noinline__ float largest_rounded_up(const Args& a, const T* row, bo
 // One head's keys or values of a block of 16 rows: a warp.  Rows lo .. lo + m - 1 of the block are new, `row` is the first
 // of them in memory; codes and scale: the block's in the pool.
 template <typename T, int D> struct Rows {
-  static constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = 16 / kRows;
   const T* row;
   bool turn;
   unsigned char* codes;
@@ -250,7 +321,7 @@ template <typename T, int D> struct Rows {
   float old;
   // looks up head u of K, then of V
   __device__ __forceinline__ void load(const Args& a, int u, int64_t new_row, int64_t page_row, int64_t cell, int lo, int m) {
-    const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes;
+    const int chunk = (threadIdx.x & 31) % (D / 16);
     const bool v = u >= a.H_kv;
     const int h = v ? u - a.H_kv : u;
     row = static_cast<const T*>(v ? a.v_new : a.k_new) + new_row + h * a.n_h;
@@ -320,9 +391,10 @@ __device__ __forceinline__ void write_codes(const Args& a, const Rows<T, D>& x, 
   if (lane == 0) *x.scale = s;
 }
 
-// (loose pairs are worked out by calls, for which the others' values would go to memory and back)
+// (LOOSE: the number of pairs is no multiple of 8.  A kernel of its own: in one, the others lose registers, and 128 x 64
+// rows of 32 heads take 35 us instead of 28.)
 template <typename T, Where W, int D_SCALED, bool LOOSE>
-__global__ void __launch_bounds__(kThreads, W == kPagesScaled ? 2 : 3) rest_kv_append_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, W == kPagesScaled || LOOSE ? 2 : 3) rest_kv_append_kernel(const __grid_constant__ Args a) {
   grid_wait();
   extern __shared__ __align__(16) unsigned char smem[];
   const int all_groups = gridDim.x / a.parts, part = blockIdx.x / all_groups, b = blockIdx.x % all_groups / a.groups,
@@ -374,31 +446,47 @@ __global__ void __launch_bounds__(kThreads, W == kPagesScaled ? 2 : 3) rest_kv_a
   const int parts = a.parts - a.code_parts, h0 = (all >= m ? me / m : 0) + (part - a.code_parts) * together, step = together * parts;
   for (int r = all >= m ? me % m : me; r < m; r += all >= m ? m : all) {
     Angles<float> t;
+    float c[LOOSE ? 16 : 1], s[LOOSE ? 16 : 1];         // of kLoose, for each element
     bool known = false;
     // one row in `count` heads; the first heads are on their way while the angles are worked out
     auto heads = [&](const T* from, int64_t from_h, T* to, int64_t to_h, int count, Kind kind) {
-      if (kind == kLoose) {                             // (LOOSE is for codes only)
-        for (int h = h0; h < count; h += step) {
-          const T* x0 = from + h * from_h;
-          T* y0 = to + h * to_h;
-          float x[16], y[16];
-          load8(x0 + l.at[0], x);
-          load8(x0 + l.at[1], x + 8);
-#pragma unroll 1
-          for (int j = 0; j < 16; ++j) {
-            const int e = l.at[0] + j;
-            if (e >= 2 * a.half) { y[j] = x[j]; continue; }
-            const Loose o = loose(a, e);
-            const float2 cs = turn_of(a, a.pos[(int64_t)b * a.N + i0 + r], o.pair);
-            const float other = load1(x0 + o.other);
-            y[j] = o.low ? fmaf(x[j], cs.x, -(other * cs.y)) : fmaf(x[j], cs.x, other * cs.y);
+      if constexpr (LOOSE) {
+        if (kind == kLoose) {
+          const Loose o(a, l);
+          if (!known) {
+            const double p = a.pos[(int64_t)b * a.N + i0 + r];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float2 cs = o.turns(j) ? turn_of(a, p, o.pair(j)) : make_float2(1.f, 0.f);
+              c[j] = cs.x;
+              s[j] = o.second(j) ? cs.y : -cs.y;
+            }
+            known = true;
           }
-          // a row may be rotated in place: all its lanes have loaded before the first stores
-          __syncwarp(((moving == 32 ? 0u : 1u << moving) - 1u) << (sub * lanes));
-          store8(y0 + l.at[0], y);
-          store8(y0 + l.at[1], y + 8);
+          for (int h = h0; h < count; h += step) {
+            const T* x0 = from + h * from_h;
+            Eight<T> e[2];
+            float other[2][8];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              e[k].load(x0 + l.at[k]);
+              o.partners(x0, k, a.D, other[k]);
+            }
+            // a row may be rotated in place: all its lanes have loaded before the first stores
+            __syncwarp(((moving == 32 ? 0u : 1u << moving) - 1u) << (sub * lanes));
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float x[8], y[8];
+              e[k].to(x);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) y[j] = fmaf(x[j], c[8 * k + j], other[k][j] * s[8 * k + j]);
+              Eight<T> out = packed<T>(y);
+              keep(out, e[k], 2 * a.half - l.at[k]);
+              out.store(to + h * to_h + l.at[k]);
+            }
+          }
+          return;
         }
-        return;
       }
       constexpr int kAtOnce = sizeof(T) == 4 || W == kPages16 ? 2 : 4;      // heads on their way
       from += h0 * from_h;
@@ -417,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, W == kPagesScaled ? 2 : 3) rest_kv_a
           const double p = a.pos[(int64_t)b * a.N + i0 + r];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float2 cs = turn_of(a, p, l.first + j);
+            const float2 cs = turn_of(a, p, LOOSE ? min(l.first + j, a.half - 1) : l.first + j);
             t.c[j] = cs.x;
             t.s[j] = cs.y;
           }
@@ -437,8 +525,12 @@ __global__ void __launch_bounds__(kThreads, W == kPagesScaled ? 2 : 3) rest_kv_a
               auto same = [](float v) { return v; };
               if (kind == kPairs) rotate<false>(t, x, y, same);
               else rotate<true>(t, x, y, same);
-              store8(y0 + l.at[0], y);
-              store8(y0 + l.at[1], y + 8);
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                Eight<T> out = packed<T>(y + 8 * k);
+                if (LOOSE) keep(out, e[i][k], 2 * a.half - l.at[k]);
+                out.store(y0 + l.at[k]);
+              }
             }
           }
       }
@@ -476,7 +568,7 @@ rest_status run(const Args& a, int B, void* stream) {
   args.parts = args.code_parts + parts(tasks(((W == kPages16 ? a.H + 2 * a.H_kv : args.H) * most + rows - 1) / rows));
   if (blocks * args.parts > 0x7FFFFFFFll) return REST_UNSUPPORTED;
   const size_t smem = W == kPagesScaled ? (size_t)16 * a.half * sizeof(double2) : 0;
-  REST_CUDA_TRY(launch(W == kPagesScaled && (a.half & 7) ? rest_kv_append_kernel<T, W, D, W == kPagesScaled> : rest_kv_append_kernel<T, W, D, false>, dim3((unsigned)(blocks * args.parts)), kThreads, smem, stream, args));
+  REST_CUDA_TRY(launch(a.half & 7 ? rest_kv_append_kernel<T, W, D, true> : rest_kv_append_kernel<T, W, D, false>, dim3((unsigned)(blocks * args.parts)), kThreads, smem, stream, args));
   return REST_OK;
 }
 

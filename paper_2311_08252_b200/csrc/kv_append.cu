@@ -16,14 +16,15 @@
 // A thread block takes new rows of one context that fall into one block of 16 rows.  A row is D / 16 lanes, 16
 // elements each (a pair's halves sit in the same lane, unless half the head is no multiple of 8); a lane stays with its
 // row, keeps its sines and cosines in registers and steps through the heads, four of them on their way at a time.  One
-// head's keys or values of a block of codes are a warp's, which holds all its rows' values while it looks for the largest;
+// head's keys or values of a block of codes are a warp's, which holds all its rows while it looks for the largest value;
 // the angles of its thread block's rows are computed once, into shared memory.
 //
 // What bounds it, for few rows: the launch and the chain length -> table -> page (one row: 4.3 us with codes or without).
 // For many, measured with 128 x up to 64 rows, D = 128, 32 heads of queries and 8 of keys and values: the rotation of
-// queries alone 28 us (4.8 TB/s) and 16-bit pages are bound by HBM; codes take 49 us, of which half are the 64-bit
-// products (64 a clock and SM) and conversions to and from them (16) of keys.  With 61 pairs, half the head apart, 62 us
-// and 95 us: shifting the partners into place is bound by the instructions it takes.
+// queries alone 28 us (4.8 TB/s) and 16-bit pages are bound by HBM; the append with codes takes 46 us, 23 of them for K and
+// V: a warp's chain of rows, angles, products, scale and codes at 16 warps an SM (64-bit pipe 5 %, conversions 16 %,
+// HBM 20 %).  With 61 pairs, half the head apart, 62 us and 95 us: shifting the partners into place is bound by the
+// instructions it takes.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -339,17 +340,34 @@ __device__ __forceinline__ void write_codes(const Args& a, const Rows<T, D>& x, 
   const Lane l = x.l;
   unsigned char* codes = x.codes;
   const float old = lo > 0 ? within_limits(x.old) : 0.f;
-  float y[kSteps][16], most = 0.f;
+  // Rows are kept as they come and rotated twice, for the largest value and for the codes: 32 registers instead of 64 that
+  // do not fit (128 x 64 rows: 47 us, once 51).  LOOSE: once (95 us, twice 110).
+  Eight<T> e[LOOSE ? 1 : kSteps][2];
+  float kept[LOOSE ? kSteps : 1][16], most = 0.f;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int r = i * kRows + sub;
+    if (!LOOSE && lo + r < hi) {
+      e[LOOSE ? 0 : i][0].load(x.row + r * a.n_n + l.at[0]);
+      e[LOOSE ? 0 : i][1].load(x.row + r * a.n_n + l.at[1]);
+    }
+  }
+  auto values = [&](int i, float (&y)[16]) {
+    const int r = i * kRows + sub;
+    if (LOOSE) {
+      e[0][0].load(x.row + r * a.n_n + l.at[0]);
+      e[0][1].load(x.row + r * a.n_n + l.at[1]);
+    }
+    code_values<LOOSE>(a, e[LOOSE ? 0 : i], x.row + r * a.n_n, l, table, r, y, [](double v) { return __double2float_rn(v); });
+  };
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int r = i * kRows + sub;
     if (lo + r < hi) {
-      Eight<T> e[2];
-      e[0].load(x.row + r * a.n_n + l.at[0]);
-      e[1].load(x.row + r * a.n_n + l.at[1]);
-      code_values<LOOSE>(a, e, x.row + r * a.n_n, l, table, r, y[i], [](double v) { return __double2float_rn(v); });
+      float(&y)[16] = kept[LOOSE ? i : 0];
+      values(i, y);
 #pragma unroll
-      for (int j = 0; j < 16; j += 2) most = fmaxf(most, fmaxf(fabsf(y[i][j]), fabsf(y[i][j + 1])));      // (NaN is passed over)
+      for (int j = 0; j < 16; j += 2) most = fmaxf(most, fmaxf(fabsf(y[j]), fabsf(y[j + 1])));      // (NaN is passed over)
     }
   }
   most = warp_max(most);
@@ -374,15 +392,17 @@ __device__ __forceinline__ void write_codes(const Args& a, const Rows<T, D>& x, 
   for (int i = 0; i < kSteps; ++i) {
     const int r = lo + i * kRows + sub;
     if (r < hi) {
+      float(&y)[16] = kept[LOOSE ? i : 0];
+      if (!LOOSE) values(i, y);
       if (infinite) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[i][j] = fabsf(y[i][j]) < INFINITY ? y[i][j] : NAN;
+        for (int j = 0; j < 16; ++j) y[j] = fabsf(y[j]) < INFINITY ? y[j] : NAN;
       }
 #pragma unroll
-      for (int j = 0; j < 16; ++j) y[i][j] *= inverse;
+      for (int j = 0; j < 16; ++j) y[j] *= inverse;
       uint32_t w[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = pack2(y[i][4 * j], y[i][4 * j + 1]) | pack2(y[i][4 * j + 2], y[i][4 * j + 3]) << 16;
+      for (int j = 0; j < 4; ++j) w[j] = pack2(y[4 * j], y[4 * j + 1]) | pack2(y[4 * j + 2], y[4 * j + 3]) << 16;
       *reinterpret_cast<uint2*>(codes + r * code_row + l.at[0]) = make_uint2(w[0], w[1]);
       *reinterpret_cast<uint2*>(codes + r * code_row + l.at[1]) = make_uint2(w[2], w[3]);
     }
@@ -558,7 +578,7 @@ rest_status run(const Args& a, int B, void* stream) {
   Args args = a;
   if (W == kPagesScaled && a.H > 0 && each < 2) {
     // Many rows: the queries in a launch of their own, at three blocks an SM instead of the two that codes allow
-    // (128 x up to 64 rows, 32/8 heads: 49 us in two, 52 in one).
+    // (128 x up to 64 rows, 32/8 heads, before rows were rotated twice: 49 us in two, 52 in one).
     args.groups = (a.N + 15) / 16;
     if (rest_status st = run<T, kNowhere, 0>(args, B, stream)) return st;
     args.groups = a.groups;

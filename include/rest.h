@@ -440,7 +440,8 @@ rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int
  *   For context b, node i, head h and pair f < pairs, with p = d_pos[b,i] and t = p * d_inv_freq[f]:
  *   (y1, y2) = amplitude * (x1 cos t - x2 sin t, x2 cos t + x1 sin t).  interleaved = 0: the pair is
  *   elements f and pairs + f; 1: elements 2f and 2f + 1.  Elements from 2 * pairs on are copied.
- *   t and its sine and cosine are computed in 64 bits, results in 32, rounded once.
+ *   t is a product in 64 bits, and whole quarter turns are taken off it there; sine and cosine of the
+ *   rest and y are computed in 32 bits (below 2^-22 amplitude (|x1| + |x2|) off), rounded once.
  *   With -d_inv_freq it is the inverse rotation (and, amplitude kept, the gradient of x).
  *
  *   d_x, d_out      element (b,i,h,d) at b*strides[0] + i*strides[1] + h*strides[2] + d, dtype REST_BF16,
@@ -448,7 +449,7 @@ rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int
  *                   16-byte aligned.  d_out is d_x with the same strides (in place), or overlaps no input
  *   d_pos           int32[B,N], any sign; d_inv_freq float[pairs] (both may be NULL with pairs = 0: a copy)
  *   d_n_nodes       optional int32[B]: rows i >= n_nodes[b] of d_out stay as they were
- *   Limits: D a multiple of 16, at most 512; 2 * pairs <= D; amplitude finite.
+ *   Limits: D a multiple of 16, at most 512; 2 * pairs <= D; amplitude finite; H <= 65536; N <= 2^30.
  */
 rest_status rest_rotary(const void* d_x, const int64_t* x_strides, int32_t dtype, const int32_t* d_pos,
                         const float* d_inv_freq, int32_t pairs, int32_t interleaved, float amplitude,
@@ -463,7 +464,8 @@ rest_status rest_rotary(const void* d_x, const int64_t* x_strides, int32_t dtype
  *                   d_k_new, d_v_new, d_q and d_q_out share)
  *   d_pos ... amplitude      as in rest_rotary
  *   d_q, d_q_out    element (b,i,h,d) as in rest_rotary, h < H (H = 0: none, both NULL)
- *   A row whose page does not exist is left out; its query is rotated all the same.
+ *   A row whose page does not exist is left out; its query is rotated all the same.  Limits: H and H_kv <= 65536,
+ *   N <= 2^30.
  */
 rest_status rest_paged_kv_append(void* d_k_pages, void* d_v_pages, const int64_t* page_strides, int32_t P,
                                  int32_t page, const int32_t* d_table, int64_t table_stride, int32_t table_cols,
@@ -553,7 +555,10 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
  * rest_paged_attention_scaled - rest_paged_attention over pages of codes with scales (see the cache in 8 bits, above).
  *   The same formula with the values that the codes stand for: scores, maxima, sums and the output
  *   in fp32; probabilities rounded to fp16 for their product with V (half a step, 2^-11 of each; below 2^-31 of
- *   the row's largest they vanish).
+ *   the row's largest they vanish).  With more than 16 rows a KV head (N * H / H_kv) queries are held as sums of
+ *   e4m3 terms, off by at most 2^-11 of an element in fp16 or 2^-8 in bf16 where it is far below its row's largest,
+ *   and never by more than 2^-19 of that.  bf16 queries beyond 2^60 saturate or make their row NaN, and those of a
+ *   row whose largest is below 2^-60 may count as 0.
  *   d_q, d_out      dtype REST_BF16 or REST_FP16; strides as there, those of the pages (3..5) multiples of 16
  *   d_k_scales, d_v_scales  float[P][H_kv][page / 16], aligned to min(page, 64) / 4 bytes
  *   d_ws            scratch of rest_paged_attention_workspace_bytes() bytes

@@ -42,6 +42,7 @@ using namespace rest_pool;
 using namespace rest_e4m3;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMostRows = 1 << 30;                      // of a context in a call (sums with it stay below 2^31)
 constexpr double kQuarterTurns = 0.63661977236758134308, kQuarter = 1.57079632679489661923,      // 2 / pi, pi / 2
                  kQuarterHigh = 0x1.921fb54400000p+0, kQuarterLow = 0x1.0b4611a626331p-34;
 enum Where { kNowhere, kPages16, kPagesScaled };        // where keys and values go
@@ -631,7 +632,7 @@ rest_status append(void* d_k_pages, void* d_v_pages, const int64_t* page_strides
   if (rest_status st = fill_pool(a.c, d_k_pages, d_v_pages, page_strides, d_table, table_stride, table_cols, P, H_kv, page, D,
                                  scaled ? 16 : 8))
     return st;
-  if (H > 65536) return REST_UNSUPPORTED;
+  if (H > 65536 || H_kv > 65536 || N > kMostRows) return REST_UNSUPPORTED;
   if (rest_status st = fill_turn(a, d_pos, d_inv_freq, pairs, interleaved, amplitude, D)) return st;
   if (!rows_ok(new_strides, B, N, H_kv, D, 8) || !aligned16(d_k_new, d_v_new)) return REST_INVALID_ARG;
   if (H > 0)
@@ -657,7 +658,7 @@ extern "C" rest_status rest_rotary(const void* d_x, const int64_t* x_strides, in
                                    const int64_t* out_strides, void* stream) {
   if (B < 0 || H < 1 || N < 0 || D < 1 || (dtype != REST_BF16 && dtype != REST_FP16 && dtype != REST_FP32)) return REST_INVALID_ARG;
   if (B == 0 || N == 0) return REST_OK;
-  if (D > 512 || (D % 16) != 0) return REST_UNSUPPORTED;
+  if (D > 512 || (D % 16) != 0 || H > 65536 || N > kMostRows) return REST_UNSUPPORTED;
   Args a = {};
   if (rest_status st = fill_turn(a, d_pos, d_inv_freq, pairs, interleaved, amplitude, D)) return st;
   if (rest_status st = fill_q(a, d_x, x_strides, d_out, out_strides, B, N, H, dtype == REST_FP32 ? 4 : 8)) return st;

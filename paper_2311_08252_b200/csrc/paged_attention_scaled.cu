@@ -1,5 +1,26 @@
 // rest_paged_attention_scaled: the attention of rest_paged_attention over pages of e4m3 codes with a scale for every
-// 16 rows of a head.
+// 16 rows of a head.  K/V are half the bytes of a 16-bit cache.
+//
+// Scales never touch the codes.  With x = scale log2(e) (q . k codes) ks the score in log2 units, the weight of a key is
+//   2^(x + log2 vs - m) = p vs 2^-m,
+// V's scale rides in the exponent: O += weight * (v codes), and the row's sum takes weight / vs, once for the 16 keys that
+// share it.  The reference m is a whole number (a rescaling of O and the sum is exact) and stays 2^7 below what
+// would make the largest weight 1, so that fp16 weights reach 2^-31 of it.  Weights and V are fp16 operands (a code is
+// exact in fp16), K's codes go in as they are or as fp16; sums are in 32 bits.
+//
+// Two kernels, by the rows of a KV head, R = N H / H_kv: up to 16, warps on their own (below); more, the 128-row tiles of
+// the 16-bit call with K's codes as operands of kind f8f6f4 next to Q as a sum of e4m3 terms, V widened to fp16 by four more
+// warps.  Both go by the same shares of the flat tile list, and the same second kernel joins cut units.
+//
+// Measured (B200; copy rate 6568 GB/s, bf16 matrix rate 1658 TFLOP/s; captured in a graph, back to back): 1 token x 2048 keys,
+// 32/8 heads 12.5 us (two dependent launches; 16-bit pages 16.6); 256 tokens x 4096 keys 262 us = 94 % of the copy rate;
+// 256 tokens, window 2048, D = 64, fp16 135 us (4.1 TB/s; 16-bit pages 198); 61 ragged trees of 64 nodes x 4096 283 us
+// (246); 16 trees of 128 nodes x 16384, 640 rows a KV head, 771 us = 900 TFLOP/s (686).  The last two are no
+// quicker than with 16-bit pages: both are bound by the chain from S to P, and here S takes two products (three with fp16) of
+// half the depth, and V's widening its share of shared-memory reads.  What they give is the room.
+// The border, 64 contexts x 4096: 4, 8, 16 rows 78, 80, 115 us by warps, 183, 185, 189 us by tiles; from 17 rows on O no
+// longer fits a warp's registers, and 20 rows take 187 us by tiles.  D = 64 by warps is bound by instructions: half as many
+// bytes go with each softmax.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

@@ -516,7 +516,8 @@ def rest_kv_commit(k, v, kv_len, accept_nodes, accept_len, N, new_kv_len=None, s
 # These calls are made many times per decoding step, so their checks go through few, cheap tensor
 # queries: get_device() says both that a tensor is on a GPU (-1: it is not) and on which.
 _I64x9 = ctypes.c_int64 * 9
-_T = None                                                # torch, once a call has needed it (an import statement takes as long as a check)
+_T = None                                                # torch, once a call has needed it (an import statement takes
+                                                         # as long as a check)
 
 
 def _torch():
@@ -536,6 +537,16 @@ def _strides(s):
         if len(_strides_seen) >= 4096:
             _strides_seen.clear()
         a = _strides_seen[s] = (ctypes.c_int64 * 3)(*s[:3])
+    return a
+
+
+def _strides9(*three):
+    """The same of three tuples in one array."""
+    a = _strides_seen.get(three)
+    if a is None:
+        if len(_strides_seen) >= 4096:
+            _strides_seen.clear()
+        a = _strides_seen[three] = _I64x9(*(n for s in three for n in s[:3]))
     return a
 
 
@@ -670,13 +681,15 @@ def _attend(name, q, index, pages, pointers, pool, scales, block_table, kv_len, 
     elif out.dtype is not dtype or out.shape != shape or out.stride(3) != 1 or out.get_device() != index:
         raise RestError("out must be a tensor like q with a contiguous last dimension")
     if workspace is None:
-        need = _scratch_bytes(L.rest_paged_attention_workspace_bytes, index, B, H, H_kv, N, D)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        ws_bytes = _scratch_bytes(L.rest_paged_attention_workspace_bytes, index, B, H, H_kv, N, D)
+        if ws_bytes:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+            ws_ptr = workspace.data_ptr()
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise RestError("workspace must be a contiguous tensor on the same CUDA device")
-    if workspace is not None:
+    else:
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    strides = _I64x9(*qs[:3], *pool[0], *out.stride()[:3])
+    strides = _strides9(qs, pool[0], out.stride())
     _call(getattr(L, name), name, index, None, q.data_ptr(), *pointers, strides, *scales,
           REST_BF16 if dtype is torch.bfloat16 else REST_FP16, P, page, *table, _vec(kv_len, "kv_len", index, B),
           nodes_ptr, mask_ptr, B, H, H_kv, N, D, window, sinks, scale, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes)
@@ -697,11 +710,11 @@ def rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, 
         with _as_current(stream, q):
             return rest_paged_attention(q, k_pages, v_pages, block_table, kv_len, mask, scale, window, sinks, n_nodes,
                                         out, lse, workspace)
-    index, pages, (k_ptr, v_ptr, *pool) = _pool(k_pages, v_pages)
+    index, pages, (k_ptr, v_ptr, _, *pool) = _pool(k_pages, v_pages)
     if q.dtype is not k_pages.dtype:
         raise RestError("q must be [B,N,H,D] with a contiguous last dimension, of the pages' type, head size and device")
-    return _attend("rest_paged_attention", q, index, pages, (k_ptr, v_ptr), pool, (), block_table, kv_len, mask, scale, window,
-                   sinks, n_nodes, out, lse, workspace)
+    return _attend("rest_paged_attention", q, index, pages, (k_ptr, v_ptr), (k_pages.stride(), *pool), (), block_table,
+                   kv_len, mask, scale, window, sinks, n_nodes, out, lse, workspace)
 
 
 def rest_accept_sampled(logits, tokens, parents, n_nodes, uniforms, temperature, top_p, max_depth, out=None,
@@ -969,8 +982,8 @@ def rest_paged_attention_scaled(q, k_pages, v_pages, k_scales, v_scales, block_t
         with _as_current(stream, q):
             return rest_paged_attention_scaled(q, k_pages, v_pages, k_scales, v_scales, block_table, kv_len, mask, scale,
                                                window, sinks, n_nodes, out, lse, workspace)
-    index, pages, (k_ptr, v_ptr, strides, ks_ptr, vs_ptr, *pool) = _scaled_pool(k_pages, v_pages, k_scales, v_scales)
-    return _attend("rest_paged_attention_scaled", q, index, pages, (k_ptr, v_ptr), (strides, *pool), (ks_ptr, vs_ptr),
+    index, pages, (k_ptr, v_ptr, _, ks_ptr, vs_ptr, *pool) = _scaled_pool(k_pages, v_pages, k_scales, v_scales)
+    return _attend("rest_paged_attention_scaled", q, index, pages, (k_ptr, v_ptr), (k_pages.stride(), *pool), (ks_ptr, vs_ptr),
                    block_table, kv_len, mask, scale, window, sinks, n_nodes, out, lse, workspace)
 
 

@@ -482,7 +482,8 @@ rest_status rest_paged_kv_append(void* d_k_pages, void* d_v_pages, const int64_t
  * page stands for scale[r / 16] * code.  Scales are positive; outside [2^-60, 2^60] they count as the nearer
  * limit (NaN as 2^-60).  Tables, counts, forks and lengths are those of 16-bit pages.
  *
- * rest_paged_kv_append_scaled  as rest_paged_kv_append, K (rotated in 64 bits) and V rounded to codes.  A block
+ * rest_paged_kv_append_scaled  as rest_paged_kv_append (queries of many rows in a second launch), K (rotated in 64
+ *                   bits) and V rounded to codes.  A block
  *                   that gets new rows gets the smallest power of two s for which no finite new value exceeds
  *                   448 s; where it has older rows (below kv_len) s is not less than its scale was, and
  *                   if it grows, those rows' codes are rounded to the new scale (exact down to 2^-9 s).
@@ -555,7 +556,7 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
  * rest_paged_attention_scaled - rest_paged_attention over pages of codes with scales (see the cache in 8 bits, above).
  *   The same formula with the values that the codes stand for: scores, maxima, sums and the output
  *   in fp32; probabilities rounded to fp16 for their product with V (half a step, 2^-11 of each; below 2^-31 of
- *   the row's largest they vanish).  With more than 16 rows a KV head (N * H / H_kv) queries are held as sums of
+ *   the row's largest p * scale of v they vanish there, and below 2^-130 of it in the sum).  With more than 16 rows a KV head (N * H / H_kv) queries are held as sums of
  *   e4m3 terms, off by at most 2^-11 of an element in fp16 or 2^-8 in bf16 where it is far below its row's largest,
  *   and never by more than 2^-19 of that.  bf16 queries beyond 2^60 saturate or make their row NaN, and those of a
  *   row whose largest is below 2^-60 may count as 0.

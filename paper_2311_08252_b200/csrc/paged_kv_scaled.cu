@@ -8,7 +8,7 @@
 //
 // Both move bytes: the bound is HBM for many contexts or pages, and for one context the chain length -> table -> rows ->
 // largest value -> rows.  Measured (B200, captured): 1 context, 8 heads, 4.5 to 5.3 us; 128 contexts, 32 heads, paths of up to 16
-// rows 9.4 us (a warp takes four heads one after another; with 1024 threads a block 11.5); 128 pages of 64 rows
+// rows 9.5 us (a warp takes two heads one after another; with blocks of 1024 threads 11.5); 128 pages of 64 rows
 // copied, 134 MB, 24 us (5.6 TB/s).
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -67,7 +67,7 @@ rest_paged_kv_commit_scaled_kernel(Pool c, float* k_scales, float* v_scales, con
   __syncthreads();
   const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes;
   const int kept = L & 15, in_first = 16 - kept;                      // path positions from in_first on are in the second block
-  const int warps = kCommitThreads / 32;
+  const int warps = blockDim.x / 32;
   for (int u = (threadIdx.x >> 5) + blockIdx.y * warps; L >= 0 && len > 0 && u < 2 * H_kv; u += warps * gridDim.y) {
     const int h = u >> 1;
     uint4* base = ((u & 1) ? c.v : c.k) + h * c.s_head + chunk;
@@ -179,12 +179,15 @@ extern "C" rest_status rest_paged_kv_commit_scaled(void* d_k_pages, void* d_v_pa
   Pool c;
   if (rest_status st = fill_pool(c, d_k_pages, d_v_pages, page_strides, d_table, table_stride, table_cols, P, H_kv, page, D, 16))
     return st;
-  // heads are shared out where contexts are few; not when the new lengths go into the array that the old ones are read from
-  const int rounds = (2 * H_kv + kCommitThreads / 32 - 1) / (kCommitThreads / 32), sms = rest::sm_count();
-  int parts = d_new_kv_len == d_kv_len ? 1 : 2 * (sms > 0 ? sms : 148) / B;
+  // Heads are shared out to blocks of 256 threads, four an SM (128 contexts, 32 heads and 128 pages copied behind them 32.4 us,
+  // with two of 512 33.9); not when the new lengths go into the array that the old ones are read from: one of 512 then.
+  const bool apart = d_new_kv_len != d_kv_len;
+  const int threads = apart ? kCommitThreads / 2 : kCommitThreads, sms = rest::sm_count();
+  const int rounds = (2 * H_kv + threads / 32 - 1) / (threads / 32);
+  int parts = apart ? 4 * (sms > 0 ? sms : 148) / B : 1;
   parts = parts < 1 ? 1 : parts > rounds ? rounds : parts;
   REST_CUDA_TRY(launch(D == 128 ? rest_paged_kv_commit_scaled_kernel<128> : rest_paged_kv_commit_scaled_kernel<64>,
-                       dim3((unsigned)B, (unsigned)parts), kCommitThreads, 0, stream, c, d_k_scales, d_v_scales, d_kv_len,
+                       dim3((unsigned)B, (unsigned)parts), threads, 0, stream, c, d_k_scales, d_v_scales, d_kv_len,
                        d_accept_nodes, d_accept_len, (int)H_kv, (int)N, (int)max_depth, d_new_kv_len));
   return REST_OK;
 }

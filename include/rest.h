@@ -441,7 +441,7 @@ rest_status rest_pages_release(int32_t* d_refs, int32_t P, int32_t* d_table, int
  *   (y1, y2) = amplitude * (x1 cos t - x2 sin t, x2 cos t + x1 sin t).  interleaved = 0: the pair is
  *   elements f and pairs + f; 1: elements 2f and 2f + 1.  Elements from 2 * pairs on are copied.
  *   t is a product in 64 bits, and whole quarter turns are taken off it there; sine and cosine of the
- *   rest and y are computed in 32 bits (below 2^-22 amplitude (|x1| + |x2|) off), rounded once.
+ *   rest and y are computed in 32 bits (for |t| < 2^40 below 2^-22 amplitude (|x1| + |x2|) off), rounded once.
  *   With -d_inv_freq it is the inverse rotation (and, amplitude kept, the gradient of x).
  *
  *   d_x, d_out      element (b,i,h,d) at b*strides[0] + i*strides[1] + h*strides[2] + d, dtype REST_BF16,

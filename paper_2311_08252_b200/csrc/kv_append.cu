@@ -43,8 +43,8 @@ using namespace rest_e4m3;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMostRows = 1 << 30;                      // of a context in a call (sums with it stay below 2^31)
-constexpr double kQuarterTurns = 0.63661977236758134308, kQuarter = 1.57079632679489661923,      // 2 / pi, pi / 2
-                 kQuarterHigh = 0x1.921fb54400000p+0, kQuarterLow = 0x1.0b4611a626331p-34;
+constexpr double kQuarterTurns = 0.63661977236758134308, kQuarterHigh = 0x1.921fb54400000p+0,    // 2 / pi; pi / 2 in two parts
+                 kQuarterLow = 0x1.0b4611a626331p-34;
 enum Where { kNowhere, kPages16, kPagesScaled };        // where keys and values go
 
 struct Args {
@@ -183,22 +183,28 @@ struct Loose {
     shifted(lo, hi, from & 7).to(x);
   }
 };
+// What is left of the angle t without whole quarter turns, in 64 bits (the reduction of Cody and Waite): pi / 2 in two parts,
+// the first of 33 bits, so that its multiples up to 2^20 are exact; beyond them the multiply-add rounds once, what is left of t.
+__device__ __forceinline__ double reduced(double t, double& whole) {
+  whole = rint(t * kQuarterTurns);
+  return fma(-whole, kQuarterLow, fma(-whole, kQuarterHigh, t));
+}
 // Cosine and sine of pair f of a row at position p, times the amplitude, in 32 bits: whole quarter turns are taken off in
 // 64, and what is left, |x| <= pi / 4, goes through the Taylor series, whose next terms are below 2^-29 (x^11 / 11!,
 // x^12 / 12!).
 __device__ __forceinline__ float2 turn_of(const Args& a, double p, int f) {
-  const double quarters = p * (double)a.inv_freq[f] * kQuarterTurns, whole = rint(quarters);
-  const float x = (float)((quarters - whole) * kQuarter), z = x * x;
+  double whole;
+  const float x = (float)reduced(p * (double)a.inv_freq[f], whole), z = x * x;
   const float s = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), x);
   const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
   const int q = (int)(long long)whole;
   const float cq = q & 1 ? s : c, sq = q & 1 ? c : s;
   return make_float2(a.amplitude * ((q + 1) & 2 ? -cq : cq), a.amplitude * (q & 2 ? -sq : sq));
 }
-// The same in 64 bits, from the angle t: pi / 2 in two parts (the first has 33 bits, so that its multiples up to 2^20 are
-// exact), and the Taylor series up to terms below 2^-54 (x^17 / 17!, x^18 / 18!).
+// The same in 64 bits, from the angle t: the Taylor series up to terms below 2^-54 (x^17 / 17!, x^18 / 18!).
 __device__ __forceinline__ double2 turn64(double t, double amplitude) {
-  const double whole = rint(t * kQuarterTurns), x = fma(-whole, kQuarterLow, fma(-whole, kQuarterHigh, t)), z = x * x;
+  double whole;
+  const double x = reduced(t, whole), z = x * x;
   double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
   s = fma(s, z, 1.0 / 6227020800.0);
   c = fma(c, z, -1.0 / 87178291200.0);

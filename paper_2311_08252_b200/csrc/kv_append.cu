@@ -296,6 +296,11 @@ __device__ __forceinline__ void code_values(const Args& a, const Eight<T> (&e)[2
     else rotate<true>(t, x, y, round);
   }
 }
+// 64 bits rounded to 32; what is finite stays so.
+__device__ __forceinline__ float finite_float(double v) {
+  const float f = __double2float_rn(v);
+  return fabsf(f) < INFINITY ? f : __double2float_rz(v);
+}
 // The largest finite magnitude of a lane's values, those in 64 bits rounded up; only asked for where it matters (below).
 template <typename T, int D, bool LOOSE>
 __device__ __noinline__ float largest_rounded_up(const Args& a, const T* row, bool turn, const double2* table, int rows) {
@@ -310,12 +315,40 @@ __device__ __noinline__ float largest_rounded_up(const Args& a, const T* row, bo
     code_values<LOOSE>(a, e, row + r * a.n_n, l, table, r, y, [&](double v) {
       const float up = __double2float_ru(fabs(v));
       most = fmaxf(most, up < INFINITY ? up : 0.f);
-      return __double2float_rn(v);
+      return finite_float(v);
     });
 #pragma unroll
     for (int j = 0; j < 16; ++j) most = fmaxf(most, fabsf(y[j]) < INFINITY ? fabsf(y[j]) : 0.f);
   }
   return most;
+}
+// A lane's 16 values, times `inverse`, as codes of a row.
+__device__ __forceinline__ void put_codes(float (&y)[16], float inverse, unsigned char* row, const Lane& l) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) y[j] *= inverse;
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = pack2(y[4 * j], y[4 * j + 1]) | pack2(y[4 * j + 2], y[4 * j + 3]) << 16;
+  *reinterpret_cast<uint2*>(row + l.at[0]) = make_uint2(w[0], w[1]);
+  *reinterpret_cast<uint2*>(row + l.at[1]) = make_uint2(w[2], w[3]);
+}
+// The codes of a block's new rows (`codes`: the first one's) where a value is beyond 32 bits: what is finite stays so, the rest is NaN.
+template <typename T, int D, bool LOOSE>
+__device__ __noinline__ void write_finite(const Args& a, const T* row, bool turn, const double2* table, int rows, float inverse,
+                                          unsigned char* codes, int64_t code_row) {
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes;
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, chunk = lane % kLanes;
+  const Lane l = turn ? lane_of(a, chunk) : Lane{kStill, {16 * chunk, 16 * chunk + 8}, 0};
+  for (int r = sub; r < rows; r += kRows) {
+    Eight<T> e[2];
+    float y[16];
+    e[0].load(row + r * a.n_n + l.at[0]);
+    e[1].load(row + r * a.n_n + l.at[1]);
+    code_values<LOOSE>(a, e, row + r * a.n_n, l, table, r, y, [](double v) { return finite_float(v); });
+#pragma unroll
+    for (int j = 0; j < 16; ++j) y[j] = fabsf(y[j]) < INFINITY ? y[j] : NAN;
+    put_codes(y, inverse, codes + r * code_row, l);
+  }
 }
 
 // One head's keys or values of a block of 16 rows: a warp.  Rows lo .. lo + m - 1 of the block are new, `row` is the first
@@ -378,7 +411,8 @@ __device__ __forceinline__ void write_codes(const Args& a, const Rows<T, D>& x, 
     }
   }
   most = warp_max(most);
-  // An infinity has no part in the scale; and 64 bits just above 448 times a power of two, which round to it, count as more.
+  // An infinity has no part in the scale, a finite value that 32 bits do not hold has one; and 64 bits just above 448 times a
+  // power of two, which round to it, count as more.
   const bool infinite = most == INFINITY;
   if (infinite || (x.turn && (__float_as_uint(most) & 0x7FFFFFu) == 0x600000u))
     most = warp_max(largest_rounded_up<T, D, LOOSE>(a, x.row, x.turn, table, m));
@@ -395,23 +429,17 @@ __device__ __forceinline__ void write_codes(const Args& a, const Rows<T, D>& x, 
       }
     }
   }
+  if (infinite) {
+    write_finite<T, D, LOOSE>(a, x.row, x.turn, table, m, inverse, codes + lo * code_row, code_row);
+  } else {
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int r = lo + i * kRows + sub;
-    if (r < hi) {
-      float(&y)[16] = kept[LOOSE ? i : 0];
-      if (!LOOSE) values(i, y);
-      if (infinite) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) y[j] = fabsf(y[j]) < INFINITY ? y[j] : NAN;
+    for (int i = 0; i < kSteps; ++i) {
+      const int r = lo + i * kRows + sub;
+      if (r < hi) {
+        float(&y)[16] = kept[LOOSE ? i : 0];
+        if (!LOOSE) values(i, y);
+        put_codes(y, inverse, codes + r * code_row, l);
       }
-#pragma unroll
-      for (int j = 0; j < 16; ++j) y[j] *= inverse;
-      uint32_t w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = pack2(y[4 * j], y[4 * j + 1]) | pack2(y[4 * j + 2], y[4 * j + 3]) << 16;
-      *reinterpret_cast<uint2*>(codes + r * code_row + l.at[0]) = make_uint2(w[0], w[1]);
-      *reinterpret_cast<uint2*>(codes + r * code_row + l.at[1]) = make_uint2(w[2], w[3]);
     }
   }
   __syncwarp();                                         // (every lane has read the old scale)

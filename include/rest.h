@@ -558,8 +558,8 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
  *   in fp32; probabilities rounded to fp16 for their product with V (half a step, 2^-11 of each; below 2^-31 of
  *   the row's largest p * scale of v they vanish there, and below 2^-130 of it in the sum).  With more than 16 rows a KV head (N * H / H_kv) queries are held as sums of
  *   e4m3 terms, off by at most 2^-11 of an element in fp16 or 2^-8 in bf16 where it is far below its row's largest,
- *   and never by more than 2^-19 of that.  bf16 queries beyond 2^60 saturate or make their row NaN, and those of a
- *   row whose largest is below 2^-60 may count as 0.
+ *   and never by more than 2^-19 of that or 2^-70.  bf16 queries beyond 2^60 saturate or make their row NaN there, and
+ *   scale times a scale of K counts as within [2^-89, 2^66].
  *   d_q, d_out      dtype REST_BF16 or REST_FP16; strides as there, those of the pages (3..5) multiples of 16
  *   d_k_scales, d_v_scales  float[P][H_kv][page / 16], aligned to min(page, 64) / 4 bytes
  *   d_ws            scratch of rest_paged_attention_workspace_bytes() bytes

@@ -806,8 +806,8 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         if (lane < 8) {
           float* to = reinterpret_cast<float*>(ctl + kScales + (ready & 15) * 48);
           const float s = rest_e4m3::within_limits(lds1(bars + kRawScales + (ready & 3) * 32 + lane * 4));
-          if (lane < 4) {                               // (within limits, so that with Q's scale it is above 0 and finite:
-            to[lane] = fminf(fmaxf(s * a.scale_log2, 0x1p-66f), 0x1p66f);   // a masked score of -infinity stays it)
+          if (lane < 4) {                               // (within limits, so that with Q's scale, 2^-60 to 2^60, it is above 0
+            to[lane] = fminf(fmaxf(s * a.scale_log2, 0x1p-89f), 0x1p67f);   // and finite: a masked score of -infinity stays it)
           } else {
             float log_v;
             asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(log_v) : "f"(s));

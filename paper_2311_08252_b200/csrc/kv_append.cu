@@ -610,18 +610,19 @@ rest_status run(const Args& a, int B, void* stream) {
   const int64_t wanted = 8 * (int64_t)(sms > 0 ? sms : 148) / (blocks > 0 ? blocks : 1), each = W == kPagesScaled ? wanted / 2 : wanted;
   auto tasks = [](int warps) { return (warps + kWarps - 1) / kWarps; };
   auto parts = [&](int tasks_) { return (int)(tasks_ < 2 || tasks_ < each ? tasks_ : each < 2 ? 2 : each); };
+  // Many rows: the queries in a launch of their own, at three blocks an SM instead of the two that codes allow
+  // (128 x up to 64 rows, 32/8 heads, before rows were rotated twice: 49 us in two, 52 in one).
+  const bool two = W == kPagesScaled && a.H > 0 && each < 2;
   Args args = a;
-  if (W == kPagesScaled && a.H > 0 && each < 2) {
-    // Many rows: the queries in a launch of their own, at three blocks an SM instead of the two that codes allow
-    // (128 x up to 64 rows, 32/8 heads, before rows were rotated twice: 49 us in two, 52 in one).
-    args.groups = (a.N + 15) / 16;
-    if (rest_status st = run<T, kNowhere, 0>(args, B, stream)) return st;
-    args.groups = a.groups;
-    args.H = 0;
-  }
+  if (two) args.H = 0;
   args.code_parts = W == kPagesScaled ? parts(tasks(2 * a.H_kv)) : 0;
   args.parts = args.code_parts + parts(tasks(((W == kPages16 ? a.H + 2 * a.H_kv : args.H) * most + rows - 1) / rows));
-  if (blocks * args.parts > 0x7FFFFFFFll) return REST_UNSUPPORTED;
+  if (blocks * args.parts > 0x7FFFFFFFll) return REST_UNSUPPORTED;      // (before the first launch)
+  if (two) {
+    Args queries = a;
+    queries.groups = (a.N + 15) / 16;
+    if (rest_status st = run<T, kNowhere, 0>(queries, B, stream)) return st;
+  }
   const size_t smem = W == kPagesScaled ? (size_t)16 * a.half * sizeof(double2) : 0;
   REST_CUDA_TRY(launch(a.half & 7 ? rest_kv_append_kernel<T, W, D, true> : rest_kv_append_kernel<T, W, D, false>, dim3((unsigned)(blocks * args.parts)), kThreads, smem, stream, args));
   return REST_OK;

@@ -490,7 +490,9 @@ rest_status rest_paged_kv_append(void* d_k_pages, void* d_v_pages, const int64_t
  *                   Rows behind the new ones lose what they held.  Values that are not finite become NaN;
  *                   beyond 448 * 2^60 they saturate.
  * rest_paged_kv_commit_scaled  as rest_paged_kv_commit: the accepted rows are put to the front as if the
- *                   values that they stand for had been appended there, by the same rule.
+ *                   values that they stand for had been appended there, by the same rule.  A row whose source or
+ *                   target page does not exist is not moved and has no part in a scale; what its place held
+ *                   is lost where the block's scale changes.
  * rest_pages_copy_scaled  as rest_pages_copy, with the pages' scales.
  */
 rest_status rest_paged_kv_append_scaled(void* d_k_pages, void* d_v_pages, const int64_t* page_strides,

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import paged_util
 import paper_2311_08252_b200 as rest
 import scaled_util as plain
 from test_gpu_append import BF16, cuda, scaled_state
@@ -32,3 +33,51 @@ def test_finite_values_that_32_bits_do_not_hold(F, amplitude, value, interleaved
     for i, (codes, sc, x) in enumerate(((pk, ks, k), (pv, vs, new.double().numpy()))):
         plain.write(raw[i], scales[i], table, kv_len, x, [4])
         assert np.array_equal(sc.cpu().numpy(), scales[i]) and plain.same_codes(codes, raw[i])
+
+
+def plain_commit(codes, scales, table, kv_len, nodes, lens, N):
+    """Path rows whose source or target page does not exist are left alone and have no part in a scale."""
+    P, H, page, D = codes.shape
+    old, old_scales = codes.copy(), scales.copy()
+    for b in range(len(kv_len)):
+        L = int(kv_len[b])
+        n = min(max(int(lens[b]), 0), nodes.shape[1])
+        source = [paged_util.row_of(table, page, P, b, L + min(max(int(nodes[b, i]), 0), N - 1)) for i in range(n)]
+        for first in range(L // 16 * 16, L + n, 16):
+            at = paged_util.row_of(table, page, P, b, first)
+            rows = [i for i in range(max(first - L, 0), min(first + 16 - L, n)) if source[i]]
+            if at is None or not rows:
+                continue
+            p, r = at
+            for h in range(H):
+                v = np.stack([plain.decode(old[source[i][0], h, source[i][1]]) *
+                              plain.limited(old_scales[source[i][0], h, source[i][1] // 16]) for i in rows])
+                s = plain.fitting(np.abs(v[np.isfinite(v)]).max(initial=0.0))
+                kept = max(L - first, 0)
+                if kept:
+                    before = plain.limited(old_scales[p, h, r // 16])
+                    s = max(s, before)
+                    if s != before:
+                        codes[p, h, r:r + kept] = plain.encode(plain.decode(codes[p, h, r:r + kept]) * (before / s))
+                for i, x in zip(rows, v):
+                    codes[p, h, r + L + i - first] = plain.encode(x / s)
+                scales[p, h, r // 16] = s
+
+
+@pytest.mark.parametrize("D,H_kv", [(128, 3), (64, 8)])
+@pytest.mark.parametrize("L,gone", [(9, [1]), (9, [2]), (9, [1, 3]), (16, [2]), (30, [2]), (30, [1]), (30, [3, 4])])
+@pytest.mark.parametrize("alias", [False, True])
+def test_commit_without_some_pages(D, H_kv, L, gone, alias):
+    """Drafts over several pages, some of the later ones missing, paths that cross a border of blocks."""
+    N = 60
+    for seed in range(4):
+        rng, pk, pv, ks, vs, raw, scales, table = scaled_state(40 + seed, 2, H_kv, D, 16, [L, L], N)
+        table[0, gone] = -1
+        nodes = np.stack([np.sort(rng.choice(N, 14, replace=False)) for _ in range(2)]).astype(np.int32)
+        n = np.array([14, 14 - seed], np.int32)
+        kv = cuda(np.array([L, L], np.int32))
+        rest.rest_paged_kv_commit_scaled(pk, pv, ks, vs, cuda(table), kv, cuda(nodes), cuda(n), N,
+                                         new_kv_len=kv if alias else None)
+        for i, (codes, sc) in enumerate(((pk, ks), (pv, vs))):
+            plain_commit(raw[i], scales[i], table, [L, L], nodes, n, N)
+            assert np.array_equal(sc.cpu().numpy(), scales[i]) and plain.same_codes(codes, raw[i])

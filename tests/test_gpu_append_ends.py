@@ -35,6 +35,35 @@ def test_finite_values_that_32_bits_do_not_hold(F, amplitude, value, interleaved
         assert np.array_equal(sc.cpu().numpy(), scales[i]) and plain.same_codes(codes, raw[i])
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("F", [5, 8, 13, 32])
+@pytest.mark.parametrize("scaled", [False, True])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_what_is_not_finite_stays_with_its_pair(F, interleaved, scaled, bad):
+    """In either half of a pair, at the border of the halves, in lanes that hold turned and copied elements."""
+    pairs = sorted({0, F // 2, F - 1})
+    for f in pairs:
+        for second in (0, 1):
+            kv_len = [18]
+            rng, pk, pv, ks, vs, raw, scales, table = scaled_state(6, 1, 2, 64, 16, kv_len, 3)
+            if not scaled:
+                pk, pv = (torch.zeros(pk.shape, dtype=BF16, device="cuda") for _ in range(2))
+            new = torch.from_numpy(rng.normal(size=(1, 3, 2, 64))).to(BF16)
+            where = [2 * f, 2 * f + 1] if interleaved else [f, F + f]
+            new[0, 1, 1, where[second]] = bad
+            turn = (cuda(np.array([[3, 4, 5]], np.int32)), cuda(np.full(F, 0.7, np.float32)), interleaved)
+            args = (cuda(table), cuda(np.array(kv_len, np.int32)), new.cuda(), torch.zeros_like(new).cuda(), *turn)
+            if scaled:
+                rest.rest_paged_kv_append_scaled(pk, pv, ks, vs, *args)
+            else:
+                rest.rest_paged_kv_append(pk, pv, *args)
+            for r in range(3):
+                p, at = paged_util.row_of(table, 16, pk.shape[0], 0, 18 + r)
+                odd = (~pk[p, :, at].float().isfinite()).nonzero().tolist()
+                assert odd == ([[1, w] for w in where] if r == 1 else [])
+            assert pv.float().isfinite().all()
+
+
 def plain_commit(codes, scales, table, kv_len, nodes, lens, N):
     """Path rows whose source or target page does not exist are left alone and have no part in a scale."""
     P, H, page, D = codes.shape

@@ -482,11 +482,13 @@ rest_status rest_paged_kv_append(void* d_k_pages, void* d_v_pages, const int64_t
  * page stands for scale[r / 16] * code.  Scales are positive; outside [2^-60, 2^60] they count as the nearer
  * limit (NaN as 2^-60).  Tables, counts, forks and lengths are those of 16-bit pages.
  *
- * rest_paged_kv_append_scaled  as rest_paged_kv_append (queries of many rows in a second launch), K (rotated in 64
- *                   bits) and V rounded to codes.  A block
- *                   that gets new rows gets the smallest power of two s for which no finite new value exceeds
- *                   448 s; where it has older rows (below kv_len) s is not less than its scale was, and
- *                   if it grows, those rows' codes are rounded to the new scale (exact down to 2^-9 s).
+ * rest_paged_kv_append_scaled  as rest_paged_kv_append (queries of many rows in a second launch); K (rotated in 64
+ *                   bits, then rounded to 32) and V are rounded to codes.  A block that gets new rows gets the
+ *                   smallest power of two s for which no finite new value exceeds 448 s; where it has older rows
+ *                   (below kv_len) s is not less than its scale was, and if it grows, those rows' codes are rounded
+ *                   to the new scale (exact down to 2^-9 s).  A scale that a row has raised stays when the row is
+ *                   refused: older rows of its block are then off by up to 2^-4 of an element and 2^-9 s, however
+ *                   often it grew.  Under an older scale that is no power of two codes may be one step off.
  *                   Rows behind the new ones lose what they held.  Values that are not finite become NaN;
  *                   beyond 448 * 2^60 they saturate.
  * rest_paged_kv_commit_scaled  as rest_paged_kv_commit: the accepted rows are put to the front as if the

@@ -1,4 +1,4 @@
-"""The appends and the commit in codes where values and pages are at their ends, against the plain models."""
+"""The appends and the commit in codes where values, pages and refused drafts are at their ends, against the plain models."""
 import numpy as np
 import pytest
 import torch
@@ -110,3 +110,30 @@ def test_commit_without_some_pages(D, H_kv, L, gone, alias):
         for i, (codes, sc) in enumerate(((pk, ks), (pv, vs))):
             plain_commit(raw[i], scales[i], table, [L, L], nodes, n, N)
             assert np.array_equal(sc.cpu().numpy(), scales[i]) and plain.same_codes(codes, raw[i])
+
+
+@pytest.mark.parametrize("loud", [1, 6, 20])
+def test_what_a_run_of_refused_drafts_costs(loud):
+    """Drafts 2^loud louder than the accepted rows, all refused but their first node, which is as quiet as those: the block's
+    scale grows to theirs and stays.  A row is off by half a step of its first code, 2^-4 of an element or 2^-10 of the
+    scale, and by 2^-10 of every larger scale that it is rounded to later; those are powers of two, so in all by less than
+    2^-4 of the element and 2^-9 of the last scale, which is no larger than the loudest draft needs."""
+    rng, pk, pv, ks, vs, raw, scales, table = scaled_state(70, 1, 2, 64, 32, [32], 40)
+    kv = cuda(np.array([32], np.int32))
+    quiet = torch.from_numpy(rng.uniform(-1, 1, (1, 14, 2, 64))).to(BF16)
+    rest.rest_paged_kv_append_scaled(pk, pv, ks, vs, cuda(table), kv, quiet[:, :1].cuda(), quiet[:, :1].cuda())
+    kv += 1
+    grown = []
+    for i in range(1, 14):
+        draft = torch.from_numpy(rng.uniform(-1, 1, (1, 8, 2, 64)) * 2.0 ** loud).to(BF16)
+        draft[:, 0] = quiet[:, i]
+        rest.rest_paged_kv_append_scaled(pk, pv, ks, vs, cuda(table), kv, draft.cuda(), draft.cuda())
+        rest.rest_paged_kv_commit_scaled(pk, pv, ks, vs, cuda(table), kv, cuda(np.zeros((1, 1), np.int32)),
+                                         cuda(np.ones(1, np.int32)), 8, new_kv_len=kv)
+        p, _ = paged_util.row_of(table, 32, pk.shape[0], 0, 32)
+        grown.append(ks[p, :, 0].cpu())
+    scale = grown[-1].double()
+    assert int(kv) == 46 and (scale <= plain.fitting(2.0 ** loud)).all() and (torch.stack(grown).diff(dim=0) >= 0).all()
+    got = pk[p, :, :14].double().cpu() * scale[:, None, None]
+    want = quiet[0].double().transpose(0, 1)
+    assert ((got - want).abs() <= 2.0 ** -4 * want.abs() + 2.0 ** -9 * scale[:, None, None]).all()

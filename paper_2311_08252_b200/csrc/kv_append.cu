@@ -361,7 +361,7 @@ template <typename T, int D> struct Rows {
   Lane l;
   float old;
   // looks up head u of K, then of V
-  __device__ __forceinline__ void load(const Args& a, int u, int64_t new_row, int64_t page_row, int64_t cell, int lo, int m) {
+  __device__ __forceinline__ void load(const Args& a, int u, int64_t new_row, int64_t page_row, int64_t cell, int lo) {
     const int chunk = (threadIdx.x & 31) % (D / 16);
     const bool v = u >= a.H_kv;
     const int h = v ? u - a.H_kv : u;
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, W == kPagesScaled || LOOSE ? 2 : 3) 
       const int64_t new_row = b * a.n_b + i0 * a.n_n;
       int u = part * kWarps + warp;
       Rows<T, D_SCALED> x;
-      if (u < 2 * a.H_kv) x.load(a, u, new_row, page_row, cell, lo, m);
+      if (u < 2 * a.H_kv) x.load(a, u, new_row, page_row, cell, lo);
       double2* table = reinterpret_cast<double2*>(smem);
       if (part * kWarps < a.H_kv && a.half > 0) {       // (else no keys)
         for (int e = threadIdx.x; e < m * a.half; e += kThreads) {
@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, W == kPagesScaled || LOOSE ? 2 : 3) 
       while (u < 2 * a.H_kv) {
         write_codes<T, D_SCALED, LOOSE>(a, x, table, lo, m, a.c.s_row * 16);
         u += a.code_parts * kWarps;
-        if (u < 2 * a.H_kv) x.load(a, u, new_row, page_row, cell, lo, m);
+        if (u < 2 * a.H_kv) x.load(a, u, new_row, page_row, cell, lo);
       }
       return;
     }

@@ -565,11 +565,11 @@ __device__ __forceinline__ float split_q(const uint4 (&x)[D / 8], uint32_t tile,
   }
   return scale;
 }
-// 16 rows of a raw tile of codes -> an operand tile of type T in the 128-byte-swizzled layout, by a warp.  A lane takes 16
+// 16 rows of a raw tile of codes -> an fp16 operand tile in the 128-byte-swizzled layout, by a warp.  A lane takes 16
 // codes of a row and writes two 16-byte chunks; lanes of the second half of the head write theirs the other way round, so
 // that the eight lanes of a phase meet different banks.  CHECK: NaN codes become 0; true in a lane that found one in
 // rows below `rows`.
-template <typename T, int D, int BN, bool CHECK>
+template <int D, int BN, bool CHECK>
 __device__ __forceinline__ bool widen(uint32_t raw, uint32_t tile, int row0, int rows = 0) {
   bool found = false;
   const int lane = threadIdx.x & 31;
@@ -589,12 +589,7 @@ __device__ __forceinline__ bool widen(uint32_t raw, uint32_t tile, int row0, int
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j >> 1] >> (16 * (j & 1))), __NV_E4M3);
-      if constexpr (__is_same(T, __half)) {
-        y[j] = *reinterpret_cast<const uint32_t*>(&h);
-      } else {
-        const float2 f = __half22float2(__half2(h));    // (every code is a bf16, too)
-        y[j] = Type<T>::pack(f.x, f.y);
-      }
+      y[j] = *reinterpret_cast<const uint32_t*>(&h);
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
@@ -656,6 +651,7 @@ __device__ __forceinline__ void load_q(const Args& a, const Piece& p, int rb, ui
 template <typename T, int D, int NT, int C, bool SCALED>
 __global__ void __launch_bounds__(Shape<D, NT, Pieces<T, SCALED>::value>::kThreads, NT == 1 ? 2 : 1)
 paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+  static_assert(!SCALED || (NT == 2 && C == 1), "pages of codes have one shape");
   using S_ = Shape<D, NT, Pieces<T, SCALED>::value>;
   using TV = typename Operand<T, SCALED>::V;            // what P and V are held in for their product
   constexpr int BN = S_::BN, KS = S_::KS, VS = S_::VS, kHalves = S_::kHalves;
@@ -766,10 +762,10 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
         // out, and the piece remembered if the key exists (the epilogue puts in what it comes to).  Elsewhere it
         // stays and shows in O.  The next piece's tiles come behind its Q, so eight pieces are told apart.
         if (it >= clear0 && it < clear1) {
-          widen<TV, D, BN, false>(raw + stage * S_::kRaw, sV + slot * S_::kTile, me * 16);
+          widen<D, BN, false>(raw + stage * S_::kRaw, sV + slot * S_::kTile, me * 16);
         } else {
           const int rows = p.c.L + p.c.n - tile_key<BN>(p.c, p.t0 + it);
-          if (widen<TV, D, BN, true>(raw + stage * S_::kRaw, sV + slot * S_::kTile, me * 16, rows)) {
+          if (widen<D, BN, true>(raw + stage * S_::kRaw, sV + slot * S_::kTile, me * 16, rows)) {
             s_bad[piece & 7] = piece + 1;
             __threadfence_block();
           }
@@ -1105,16 +1101,11 @@ paged_attention_kernel(const __grid_constant__ Args a, const __grid_constant__ C
           float ka[kParts], log_v[kParts], inv_v[kParts];
           if constexpr (SCALED) {
             if (fresh) q_scale = lds1(bars + kQScales + ((piece & 3) * 256 + s * 128 + t) * 4);
-            const uint32_t at = bars + kScales + ((base + it) & 15) * 48 + ci * kParts * 4;
-            if constexpr (kParts == 4) {
-              const float4 k4 = lds4(at), l4 = lds4(at + 16), i4 = lds4(at + 32);
-              ka[0] = k4.x; ka[1] = k4.y; ka[2] = k4.z; ka[3] = k4.w;
-              log_v[0] = l4.x; log_v[1] = l4.y; log_v[2] = l4.z; log_v[3] = l4.w;
-              inv_v[0] = i4.x; inv_v[1] = i4.y; inv_v[2] = i4.z; inv_v[3] = i4.w;
-            } else {
-#pragma unroll
-              for (int c = 0; c < kParts; ++c) { ka[c] = lds1(at + c * 4); log_v[c] = lds1(at + 16 + c * 4); inv_v[c] = lds1(at + 32 + c * 4); }
-            }
+            const uint32_t at = bars + kScales + ((base + it) & 15) * 48;
+            const float4 k4 = lds4(at), l4 = lds4(at + 16), i4 = lds4(at + 32);
+            ka[0] = k4.x; ka[1] = k4.y; ka[2] = k4.z; ka[3] = k4.w;
+            log_v[0] = l4.x; log_v[1] = l4.y; log_v[2] = l4.z; log_v[3] = l4.w;
+            inv_v[0] = i4.x; inv_v[1] = i4.y; inv_v[2] = i4.z; inv_v[3] = i4.w;
             mx = -INFINITY;
 #pragma unroll
             for (int c = 0; c < kParts; ++c) {

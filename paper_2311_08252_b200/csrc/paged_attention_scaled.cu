@@ -335,7 +335,7 @@ paged_attention_few_kernel(const __grid_constant__ Args a, const __grid_constant
       __syncwarp();                                     // the tile's part is read
       if (lane == 0) mbar_arrive(bar);
       __syncwarp();
-      // ---- probabilities, as in the kernel above: the scale of V rides in the exponent
+      // ---- probabilities: the scale of V rides in the exponent
       sk = rest_e4m3::within_limits(sk);
       float log_v;
       asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(log_v) : "f"(rest_e4m3::within_limits(sv)));

@@ -885,7 +885,9 @@ def rest_rotary(x, positions, inv_freq, interleaved=False, amplitude=1.0, n_node
     their heads): element pairs f and F + f (interleaved: 2f and 2f + 1) of the first 2F = 2 len(inv_freq)
     elements turn by positions[b,i] * inv_freq[f] (int32 [B,N], as rest_draft's pos_ids; float32 [F], as
     rotary_frequencies gives them, on the GPU) and are multiplied by amplitude; the others are copied.
-    n_nodes int32[B]: later rows of out stay as they were.  out: like x, x itself (in place), or None.  Returns out."""
+    n_nodes int32[B]: later rows of out stay as they were.  out: like x, x itself (in place), or None.  Returns out.
+    Like all calls here it leaves no autograd graph, for an x that requires grad neither: the gradient of x is the call
+    on the gradient of out, with -inv_freq and everything else as it was."""
     torch = _T or _torch()
     if stream is not None:
         with _as_current(stream, x):

@@ -568,6 +568,8 @@ rest_status rest_paged_attention(const void* d_q, const void* d_k_pages, const v
  *   d_k_scales, d_v_scales  float[P][H_kv][page / 16], aligned to min(page, 64) / 4 bytes
  *   d_ws            scratch of rest_paged_attention_workspace_bytes() bytes
  *   Everything else as in rest_paged_attention (codes have no infinities; NaN codes are NaN there).
+ *   Which is quicker goes by the rows of a KV head, N * H / H_kv: up to 16 this call, which takes 0.5 to 0.75 times as
+ *   long on long caches; from 17 on rest_paged_attention, and what codes save is memory (this call 1.0 to 1.3 times as long).
  */
 rest_status rest_paged_attention_scaled(const void* d_q, const void* d_k_pages, const void* d_v_pages,
                                         const int64_t* strides, const float* d_k_scales, const float* d_v_scales,

@@ -6,8 +6,9 @@
 //   y1 = a (x1 cos t - x2 sin t), y2 = a (x2 cos t + x1 sin t).
 // t is a product in 64 bits (exact up to p = 2^29): in 32 bits the angle of position 10^6 would be 0.03 off.  For queries
 // and 16-bit keys whole quarter turns are taken off it in 64 bits; the rest's sine and cosine and the rotation are in 32 bits,
-// rounded once.  Keys that become codes are rotated in 64 bits throughout: the border between two codes decides a whole
-// step of 2^-4, so that a result a rounding off would now and then be a code off.
+// rounded once: below 2^-22 of |x1| + |x2|, where half a step of 16 bits is 2^-11 or 2^-8.  (Rows of 32 bits are up to four
+// half steps off by it, in the same kernel.)  Keys that become codes are rotated in 64 bits throughout: the border between two
+// codes decides a whole step of 2^-4, so that a result a rounding off would now and then be a code off.
 //
 // Pages with scales: the 16 rows of a block share a scale per head, the smallest power of two that holds the largest new
 // value, and never less than before where the block has older rows; those are requantised when it grows
@@ -19,12 +20,13 @@
 // head's keys or values of a block of codes are a warp's, which holds all its rows while it looks for the largest value;
 // the angles of its thread block's rows are computed once, into shared memory.
 //
-// What bounds it, for few rows: the launch and the chain length -> table -> page (one row: 4.3 us with codes or without).
-// For many, measured with 128 x up to 64 rows, D = 128, 32 heads of queries and 8 of keys and values: the rotation of
-// queries alone 28 us (4.8 TB/s) and 16-bit pages are bound by HBM; the append with codes takes 46 us, 23 of them for K and
-// V: a warp's chain of rows, angles, products, scale and codes at 16 warps an SM (64-bit pipe 5 %, conversions 16 %,
-// HBM 20 %).  With 61 pairs, half the head apart, 62 us and 95 us: shifting the partners into place is bound by the
-// instructions it takes.
+// What bounds it, for few rows: the launch and the chain length -> table -> page (one row: 4.1 to 4.6 us with codes or without).
+// For many, measured with 128 x up to 64 rows, D = 128, 32 heads of queries and 8 of keys and values: the rotation of 64 rows
+// of queries alone takes 28 us (4.8 TB/s, 73 % of the copy rate; 1024 equal blocks for 444 that are resident leave the last
+// wave a third full); the append with codes 45 us, 20 of them for the queries and 21 for K and V alone: a warp's chain of
+// rows, angles, products, scale and codes at 16 warps an SM (issue 41 %, conversions 32 %, 64-bit pipe 9 %, HBM 12 %).  With
+// 61 pairs, half the head apart, 60 us and 95 us: shifting the partners into place is bound by the instructions it takes, and
+// codes of 128 elements spill 460 to 520 bytes a thread there.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -417,7 +419,8 @@ __device__ __forceinline__ void write_codes(const Args& a, const Rows<T, D>& x, 
   if (infinite || (x.turn && (__float_as_uint(most) & 0x7FFFFFu) == 0x600000u))
     most = warp_max(largest_rounded_up<T, D, LOOSE>(a, x.row, x.turn, table, m));
   const float need = fitting_scale(most), s = fmaxf(need, old);
-  const float inverse = 1.f / s;                        // (a power of two, and the products exact, unless an older scale was none)
+  const float inverse = 1.f / s;                        // (a power of two, and the products exact, unless an older scale was none:
+                                                        // then a product 2^-23 off may be a code off)
   if (lo > 0 && s != old) {                             // older rows: the scale grew
     const float ratio = old / s;
 #pragma unroll
@@ -603,8 +606,9 @@ __global__ void __launch_bounds__(kThreads, W == kPagesScaled || LOOSE ? 2 : 3) 
 
 template <typename T, Where W, int D>
 rest_status run(const Args& a, int B, void* stream) {
-  // Few rows: their heads are shared out until a warp has one task or there are eight blocks an SM.  Many: still two
-  // blocks of codes (K and V, which needs no angles) and two of rows for each group of 16, so that the last wave is short.
+  // Few rows: their heads are shared out until a warp has one task or there are eight blocks an SM (of which three are
+  // resident, two with codes).  Many: still two blocks of codes (K and V, which needs no angles) and two of rows for
+  // each group of 16, so that the last wave is short.
   const int64_t blocks = (int64_t)B * a.groups;
   const int sms = rest::sm_count(), most = min(a.N, 16), rows = 32 / (a.D / 16);
   const int64_t wanted = 8 * (int64_t)(sms > 0 ? sms : 148) / (blocks > 0 ? blocks : 1), each = W == kPagesScaled ? wanted / 2 : wanted;

@@ -6,11 +6,15 @@
 // V's scale rides in the exponent: O += weight * (v codes), and the row's sum takes weight / vs, once for the 16 keys that
 // share it.  The reference m is a whole number (a rescaling of O and the sum is exact) and stays 2^7 below what
 // would make the largest weight 1, so that fp16 weights reach 2^-31 of it.  Weights and V are fp16 operands (a code is
-// exact in fp16), K's codes go in as they are or as fp16; sums are in 32 bits.
+// exact in fp16), K's codes go in as they are or as fp16; sums are in 32 bits.  A weight is rounded to fp16 because that is
+// what a matrix product takes: half a step is 2^-11 of it, as much as the output's own rounding in fp16 and an eighth of that in
+// bf16, and roundings of many keys cancel; the rest of its bits would be a second product of the same size.
 //
 // Two kernels, by the rows of a KV head, R = N H / H_kv: up to 16, warps on their own (below); more, the 128-row tiles of
-// the 16-bit call with K's codes as operands of kind f8f6f4 next to Q as a sum of e4m3 terms, V widened to fp16 by four more
-// warps.  Both go by the same shares of the flat tile list, and the same second kernel joins cut units.
+// the 16-bit call with K's codes as operands of kind f8f6f4 next to Q as a sum of e4m3 terms (both operands of a product have 8
+// bits or both 16, and K widened as V is cost more: 338 and 930 us as terms, 382 and 1239 widened, for the two cases of
+// trees below as they were then), V widened to fp16 by four more warps.  Both go by the same shares of the flat tile list, and
+// the same second kernel joins cut units.
 //
 // Measured (B200; copy rate 6568 GB/s, bf16 matrix rate 1658 TFLOP/s; captured in a graph, back to back): 1 token x 2048 keys,
 // 32/8 heads 12.5 us (two dependent launches; 16-bit pages 16.6); 256 tokens x 4096 keys 262 us = 94 % of the copy rate;
@@ -19,8 +23,11 @@
 // quicker than with 16-bit pages: both are bound by the chain from S to P, and here S takes two products (three with fp16) of
 // half the depth, and V's widening its share of shared-memory reads.  What they give is the room.
 // The border, 64 contexts x 4096: 4, 8, 16 rows 78, 80, 115 us by warps, 183, 185, 189 us by tiles; from 17 rows on O no
-// longer fits a warp's registers, and 20 rows take 187 us by tiles.  D = 64 by warps is bound by instructions: half as many
-// bytes go with each softmax.
+// longer fits a warp's registers, and 20 rows take 187 us by tiles.  Beside 16-bit pages, 64 x 4096 keys of full contexts,
+// bf16: 1, 4, 8, 16 rows 94, 98, 101, 131 us (171, 179, 175, 179); 17, 20, 32, 64, 128, 256 rows 217, 221, 221, 234, 250, 386 us
+// (182, 185, 189, 201, 230, 358); fp16, with three terms of Q, 233, 231, 233, 246, 265, 418 us (184, 188, 189, 201, 231, 360).
+// One stream's tree over 2048 keys, 32/8 heads: 16 nodes 22 us (20), 64 nodes 32 us (32).  D = 64 by warps is bound by
+// instructions: half as many bytes go with each softmax.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

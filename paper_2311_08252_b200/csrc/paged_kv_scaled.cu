@@ -7,9 +7,10 @@
 // before where the block has older rows, which are requantised when it grows.
 //
 // Both move bytes: the bound is HBM for many contexts or pages, and for one context the chain length -> table -> rows ->
-// largest value -> rows.  Measured (B200, captured): 1 context, 8 heads, 4.5 to 5.3 us; 128 contexts, 32 heads, paths of up to 16
-// rows 9.5 us (a warp takes two heads one after another; with blocks of 1024 threads 11.5); 128 pages of 64 rows
-// copied, 134 MB, 24 us (5.6 TB/s).
+// largest value -> rows.  Measured (B200, captured, back to back): 1 context, 8 or 32 heads, 3.6 us; 128 contexts, 32 heads, paths
+// of up to 16 rows 8.7 us (a warp takes two heads one after another).  With the lengths in place a context has one block:
+// 1 context, 8 heads, the same; 32 heads 4.1 us more and 128 contexts 3.6 us more (four heads a warp).  128 pages of 64 rows
+// copied, 134 MB, 20.5 us (6.6 TB/s, a part of it from L2).
 #include <cuda_runtime.h>
 #include <stdint.h>
 
